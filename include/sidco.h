@@ -54,6 +54,13 @@ extern "C" {
 #define SIDCO_E_SIZE        (-10)  /* size beyond the limit of this entry point */
 #define SIDCO_E_CAPTURE     (-11)  /* the call would have to allocate or upload tables while `stream` is capturing */
 #define SIDCO_E_UNSUPPORTED (-12)  /* the function needs a build of the library with another compile-time switch */
+#define SIDCO_E_TYPE        (-13)  /* unknown element type */
+#define SIDCO_E_ALIGN       (-14)  /* a pointer is not aligned as the entry point asks */
+
+/* element types of the matrix operators */
+#define SIDCO_T_F32  0
+#define SIDCO_T_BF16 1
+#define SIDCO_T_F16  2
 
 /* per-segment status bits */
 #define SIDCO_ST_NONFINITE  1   /* a magnitude was NaN/Inf: nothing is selected in the segment */
@@ -236,6 +243,116 @@ int sidco_topk(const float* grad, float* residual, int64_t d, int64_t k, int32_t
 int sidco_dgc(const float* grad, float* residual, int64_t d, float delta, const int32_t* sample_idx,
               int64_t n_sample, int32_t* out_idx, float* out_val, int32_t* out_k, void* workspace,
               size_t workspace_bytes, void* stream);
+
+/*
+ * Microscaled 4-bit numbers (mx4): blocks of 32 neighbours, each with one power-of-two scale.
+ *
+ * A block's scale is 2^e with e = floor(log2 max|x|) - 2, held to [-127, 125] and stored as the byte e + 127 (E8M0); an
+ * all-zero block has the byte 0.  Its 32 codes (E2M1) are x 2^-e rounded to the nearest of
+ * {0, 0.5, 1, 1.5, 2, 3, 4, 6}, ties to the even code, larger magnitudes to 6, the sign kept.  A block that holds a NaN or
+ * an infinity has the scale byte 255 and decodes to NaN throughout.
+ *
+ * A quantised matrix [rows, cols] has its blocks along the columns; the last block of a row is filled with zeros.
+ *   codes   sidco_mx4_code_bytes(rows, cols) = rows * 16 * ceil(cols / 32) bytes, row by row, element 2i of a block in
+ *           the low half of its byte i.
+ *   scales  sidco_mx4_scale_bytes(rows, cols) bytes in tiles of 128 rows x 4 blocks = 512 bytes, tiles of a row block
+ *           next to each other.  With nb = ceil(cols / 32), the byte of (row r, block j) lies at
+ *           ((r / 128) * ceil(nb / 4) + j / 4) * 512 + (r % 32) * 16 + (r % 128) / 32 * 4 + j % 4; unused bytes are 0.
+ * A quantised flat vector of d elements is 16 bytes of codes and one scale byte per block of 32, in order:
+ * 16 * ceil(d / 32) and ceil(d / 32) bytes.
+ *
+ * Codes and the scales of matrices are 16-byte aligned (SIDCO_E_ALIGN), other buffers aligned to their element.  All
+ * work is enqueued on `stream`; nothing is allocated or synchronised, and the calls may be captured in a graph.
+ */
+int64_t sidco_mx4_code_bytes(int64_t rows, int64_t cols);      /* negative: SIDCO_E_SIZE */
+int64_t sidco_mx4_scale_bytes(int64_t rows, int64_t cols);
+
+/*
+ * sidco_mx4_quantize - quantise a matrix along its rows, along its columns, or both from one read (a layer's training
+ * step contracts its operands over one axis in the forward and over the other in the backward products).
+ *
+ * x        device, x_type[rows][ld], ld >= cols.  Any element alignment; 16-byte aligned rows take the vector path.
+ * codes, scales       device, the quantised matrix [rows, cols]; both NULL to leave this form out.
+ * codes_t, scales_t   device, the quantised transpose [cols, rows] (blocks along the rows of x); both NULL to leave out.
+ */
+int sidco_mx4_quantize(const void* x, int x_type, int64_t rows, int64_t cols, int64_t ld, uint8_t* codes, uint8_t* scales,
+                       uint8_t* codes_t, uint8_t* scales_t, void* stream);
+
+/* sidco_mx4_dequantize - the values of a quantised matrix as out_type[rows][ld].  fp32 and bf16 hold them exactly; fp16
+ * rounds to its own range. */
+int sidco_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t rows, int64_t cols, void* out, int out_type,
+                         int64_t ld, void* stream);
+
+/*
+ * sidco_mx4_matmul - C = A B^T, or C += A B^T, of quantised matrices A [m, k] and B [n, k].
+ *
+ * Sums are held in fp32 and rounded once to c_type (with `add`, after the addition in fp32).  For a linear layer
+ * Y = X W^T the three products of a training step are this one: Y from the row forms of X and W, dX = dY W from the row
+ * form of dY and the transposed form of W, dW = dY^T X from the transposed forms of dY and X.
+ *
+ * c        device, c_type[m][ldc], ldc >= n.
+ * k = 0 gives zeros (with `add`: leaves C).
+ */
+int sidco_mx4_matmul(const uint8_t* a_codes, const uint8_t* a_scales, const uint8_t* b_codes, const uint8_t* b_scales,
+                     int64_t m, int64_t n, int64_t k, void* c, int c_type, int64_t ldc, int add, void* stream);
+
+/*
+ * sidco_mx4_compress - the dense counterpart of sidco_compress: error-compensated quantisation of a flat gradient to
+ * 4.25 bits per element.  acc = (float)grad + residual (one fp32 addition); codes and scales of acc;
+ * residual <- acc - value of the codes (one rounding).  Blocks run through segment boundaries.  A non-finite element
+ * makes its block, and the residual of its block, NaN.
+ *
+ * grad     device, grad_type[d], read only, must not overlap residual (SIDCO_E_ALIAS).
+ * residual device, float[d], in/out.     d <= 2^31 - 2^16.
+ * codes    device, uint8[16 * ceil(d / 32)];   scales   device, uint8[ceil(d / 32)].
+ * No state is kept: the residual is all there is.
+ */
+int sidco_mx4_compress(const void* grad, int grad_type, float* residual, int64_t d, uint8_t* codes, uint8_t* scales,
+                       void* stream);
+
+/*
+ * sidco_mx4_mean - dense mean of N workers' quantised gradients (the counterpart of sidco_aggregate): after an all-gather
+ * of codes and scales, worker w's lie at codes_all + w * 16 * ceil(d / 32) and scales_all + w * ceil(d / 32).
+ * out_dense[j] = (v_1[j] + ... + v_N[j]) * (1 / N), added in fp32 in worker order.  N = 1 decodes one vector.
+ * n_workers 1 .. SIDCO_AGG_MAX_WORKERS.
+ */
+int sidco_mx4_mean(const uint8_t* codes_all, const uint8_t* scales_all, int n_workers, int64_t d, float* out_dense,
+                   void* stream);
+
+/*
+ * sidco_orthogonalize - momentum and orthogonalised update of the matrices of a flat model vector: the optimiser step
+ * that follows the averaged gradient.
+ *
+ * For every matrix i, rows[i] x cols[i], stored row by row from element offsets[i] of grad, momentum and out:
+ *     momentum <- mu * momentum + grad;     U = grad + mu * momentum (nesterov) or momentum;
+ *     X = U / (|U|_F + eps);   `steps` times: A = X X^T, X <- a X + (b A + c A^2) X;     out <- X
+ * with (a, b, c) = (3.4445, -4.7750, 2.0315); a matrix with more rows than columns goes through its transpose.  Five
+ * steps bring all but the smallest singular values close to one.  Products are of fp16 operands with fp32 sums (for the
+ * first two fp16 parts of X); the result is within about 3e-3 of the formula.  A matrix with a NaN or an infinity
+ * becomes NaN; the others are not affected.  Elements outside the matrices are neither read nor written.
+ *
+ * grad      device, grad_type[], read only.
+ * momentum  device, float[], in/out; NULL: U = grad (mu and nesterov are not used).
+ * mu        in [0, 1).     eps >= 0.     steps in 1 .. SIDCO_ORTHO_MAX_STEPS.
+ * offsets, rows, cols   HOST, int64[n_mats], read during the call only.  Empty matrices are allowed; the longer side is
+ *           at most SIDCO_ORTHO_MAX_DIM, the shorter at most SIDCO_ORTHO_MAX_SHORT.  Matrices must not overlap.
+ * out_bf16  device, bf16 bit patterns, same layout as grad; must not overlap grad or momentum.
+ * workspace device, 256-byte aligned, at least sidco_orthogonalize_workspace_bytes(rows, cols, n_mats) bytes; caller-owned,
+ *           nothing is kept in it between calls; not to be shared by calls that overlap.
+ * stream    everything is enqueued here (about twenty launches for five steps); no synchronisation, no allocation.
+ */
+#define SIDCO_ORTHO_MAX_DIM   4194304
+#define SIDCO_ORTHO_MAX_SHORT 16384
+#define SIDCO_ORTHO_MAX_STEPS 32
+int64_t sidco_orthogonalize_workspace_bytes(const int64_t* rows, const int64_t* cols, int n_mats); /* negative: SIDCO_E_* */
+int sidco_orthogonalize(const void* grad, int grad_type, float* momentum, float mu, int nesterov, const int64_t* offsets,
+                        const int64_t* rows, const int64_t* cols, int n_mats, int steps, float eps, uint16_t* out_bf16,
+                        void* workspace, size_t workspace_bytes, void* stream);
+
+/* How many CTAs of the product kernels (sidco_mx4_matmul, sidco_orthogonalize) have given up a bounded wait since the
+ * library was loaded; anything but 0 means that an output is incomplete.  Negative: a CUDA error.  Synchronises the
+ * device; meant for tests and logging. */
+int sidco_wait_timeouts(void);
 
 /* Bytes of device scratch one residual key needs for a vector of d elements in n_segs segments. */
 size_t sidco_workspace_bytes(int64_t d, int n_segs);

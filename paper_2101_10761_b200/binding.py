@@ -45,6 +45,9 @@ EXPORTS = [
     "sidco_get_phase_times", "sidco_get_cta_sweep_times", "sidco_compress_static",
     "sidco_reset_state_async", "sidco_set_test_hooks", "sidco_build_flags", "sidco_aggregate", "sidco_compress_bf16", "sidco_get_cta_selection_info",
     "sidco_reference_workspace_bytes", "sidco_topk", "sidco_dgc", "sidco_set_policy",
+    "sidco_mx4_code_bytes", "sidco_mx4_scale_bytes", "sidco_mx4_quantize", "sidco_mx4_dequantize", "sidco_mx4_matmul",
+    "sidco_mx4_compress", "sidco_mx4_mean", "sidco_orthogonalize_workspace_bytes", "sidco_orthogonalize",
+    "sidco_wait_timeouts",
 ]
 
 _lib = None
@@ -123,6 +126,25 @@ def lib() -> C.CDLL:
     L.sidco_set_policy.restype = i32
     L.sidco_aggregate.argtypes = [vp, vp, vp, i32, i64, i64, vp, vp, vp]
     L.sidco_aggregate.restype = i32
+    pi64 = C.POINTER(i64)
+    L.sidco_mx4_code_bytes.argtypes = L.sidco_mx4_scale_bytes.argtypes = [i64, i64]
+    L.sidco_mx4_code_bytes.restype = L.sidco_mx4_scale_bytes.restype = i64
+    L.sidco_mx4_quantize.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp, vp, vp]
+    L.sidco_mx4_quantize.restype = i32
+    L.sidco_mx4_dequantize.argtypes = [vp, vp, i64, i64, vp, i32, i64, vp]
+    L.sidco_mx4_dequantize.restype = i32
+    L.sidco_mx4_matmul.argtypes = [vp, vp, vp, vp, i64, i64, i64, vp, i32, i64, i32, vp]
+    L.sidco_mx4_matmul.restype = i32
+    L.sidco_mx4_compress.argtypes = [vp, i32, vp, i64, vp, vp, vp]
+    L.sidco_mx4_compress.restype = i32
+    L.sidco_mx4_mean.argtypes = [vp, vp, i32, i64, vp, vp]
+    L.sidco_mx4_mean.restype = i32
+    L.sidco_orthogonalize_workspace_bytes.argtypes = [pi64, pi64, i32]
+    L.sidco_orthogonalize_workspace_bytes.restype = i64
+    L.sidco_orthogonalize.argtypes = [vp, i32, vp, f32, i32, pi64, pi64, pi64, i32, i32, f32, vp, vp, C.c_size_t, vp]
+    L.sidco_orthogonalize.restype = i32
+    L.sidco_wait_timeouts.argtypes = []
+    L.sidco_wait_timeouts.restype = i32
     _lib = L
     return L
 
@@ -355,3 +377,111 @@ def sidco_reset_state_async(residual, stream=None) -> None:
     rc = lib().sidco_reset_state_async(_ptr(residual), _stream(stream))
     if rc:
         raise SidcoError(rc, "sidco_reset_state_async")
+
+
+# ---- microscaled 4-bit numbers and the orthogonalised update (formats and arguments: see sidco.h)
+
+T_F32, T_BF16, T_F16 = 0, 1, 2
+ORTHO_MAX_DIM, ORTHO_MAX_SHORT, ORTHO_MAX_STEPS = 4194304, 16384, 32
+_TYPES = {"torch.float32": T_F32, "torch.bfloat16": T_BF16, "torch.float16": T_F16, "float32": T_F32, "float16": T_F16}
+
+
+def _type(x, given: Optional[int]) -> int:
+    """The SIDCO_T_* code of a tensor or array; raw addresses need `given`."""
+    if given is not None:
+        return given
+    code = _TYPES.get(str(getattr(x, "dtype", None)))
+    if code is None:
+        raise SidcoError(-13, "element type %s:" % getattr(x, "dtype", "of a raw address"))
+    return code
+
+
+def _sizes(values):
+    arr = np.ascontiguousarray(values, dtype=np.int64)
+    return arr, arr.ctypes.data_as(C.POINTER(C.c_int64))
+
+
+def sidco_mx4_code_bytes(rows: int, cols: int) -> int:
+    n = int(lib().sidco_mx4_code_bytes(rows, cols))
+    if n < 0:
+        raise SidcoError(n, "sidco_mx4_code_bytes")
+    return n
+
+
+def sidco_mx4_scale_bytes(rows: int, cols: int) -> int:
+    n = int(lib().sidco_mx4_scale_bytes(rows, cols))
+    if n < 0:
+        raise SidcoError(n, "sidco_mx4_scale_bytes")
+    return n
+
+
+def sidco_mx4_quantize(x, rows: int, cols: int, ld: int, codes, scales, codes_t=None, scales_t=None, x_type=None,
+                       stream=None) -> None:
+    """Quantise x[rows][ld] along its rows (codes, scales) and / or its columns (codes_t, scales_t); see sidco.h."""
+    rc = lib().sidco_mx4_quantize(_ptr(x), _type(x, x_type), rows, cols, ld, _ptr(codes), _ptr(scales), _ptr(codes_t),
+                                  _ptr(scales_t), _stream(stream))
+    if rc:
+        raise SidcoError(rc, "sidco_mx4_quantize")
+
+
+def sidco_mx4_dequantize(codes, scales, rows: int, cols: int, out, ld: int, out_type=None, stream=None) -> None:
+    """The values of a quantised matrix."""
+    rc = lib().sidco_mx4_dequantize(_ptr(codes), _ptr(scales), rows, cols, _ptr(out), _type(out, out_type), ld,
+                                    _stream(stream))
+    if rc:
+        raise SidcoError(rc, "sidco_mx4_dequantize")
+
+
+def sidco_mx4_matmul(a_codes, a_scales, b_codes, b_scales, m: int, n: int, k: int, c, ldc: int, add: bool = False,
+                     c_type=None, stream=None) -> None:
+    """C[m][ldc] = A[m, k] B[n, k]^T of quantised matrices; `add`: C += A B^T."""
+    rc = lib().sidco_mx4_matmul(_ptr(a_codes), _ptr(a_scales), _ptr(b_codes), _ptr(b_scales), m, n, k, _ptr(c),
+                                _type(c, c_type), ldc, int(add), _stream(stream))
+    if rc:
+        raise SidcoError(rc, "sidco_mx4_matmul")
+
+
+def sidco_mx4_compress(grad, residual, d: int, codes, scales, grad_type=None, stream=None) -> None:
+    """Error-compensated 4-bit quantisation of a flat gradient (dense counterpart of sidco_compress)."""
+    rc = lib().sidco_mx4_compress(_ptr(grad), _type(grad, grad_type), _ptr(residual), d, _ptr(codes), _ptr(scales),
+                                  _stream(stream))
+    if rc:
+        raise SidcoError(rc, "sidco_mx4_compress")
+
+
+def sidco_mx4_mean(codes_all, scales_all, n_workers: int, d: int, out_dense, stream=None) -> None:
+    """Dense mean of n_workers gathered 4-bit gradients (counterpart of sidco_aggregate)."""
+    rc = lib().sidco_mx4_mean(_ptr(codes_all), _ptr(scales_all), n_workers, d, _ptr(out_dense), _stream(stream))
+    if rc:
+        raise SidcoError(rc, "sidco_mx4_mean")
+
+
+def sidco_orthogonalize_workspace_bytes(rows: Sequence[int], cols: Sequence[int]) -> int:
+    (r, rp), (c, cp) = _sizes(rows), _sizes(cols)
+    if r.size != c.size:
+        raise ValueError("rows and cols have different lengths")
+    n = int(lib().sidco_orthogonalize_workspace_bytes(rp, cp, r.size))
+    if n < 0:
+        raise SidcoError(n, "sidco_orthogonalize_workspace_bytes")
+    return n
+
+
+def sidco_orthogonalize(grad, momentum, mu: float, nesterov: bool, offsets: Sequence[int], rows: Sequence[int],
+                        cols: Sequence[int], steps: int, out_bf16, workspace, workspace_bytes: int, eps: float = 1e-7,
+                        grad_type=None, stream=None) -> None:
+    """Momentum and orthogonalised update of the matrices at `offsets` of a flat vector (device buffers; see sidco.h)."""
+    (o, op), (r, rp), (c, cp) = _sizes(offsets), _sizes(rows), _sizes(cols)
+    if not o.size == r.size == c.size:
+        raise ValueError("offsets, rows and cols have different lengths")
+    rc = lib().sidco_orthogonalize(_ptr(grad), _type(grad, grad_type), _ptr(momentum), mu, int(nesterov), op, rp, cp,
+                                   o.size, steps, eps, _ptr(out_bf16), _ptr(workspace), workspace_bytes,
+                                   _stream(stream))
+    if rc:
+        raise SidcoError(rc, "sidco_orthogonalize")
+
+
+def sidco_wait_timeouts() -> int:
+    n = int(lib().sidco_wait_timeouts())
+    if n < 0:
+        raise SidcoError(-n, "sidco_wait_timeouts")
+    return n

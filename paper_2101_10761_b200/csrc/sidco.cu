@@ -946,6 +946,8 @@ const char* sidco_error_string(int code) {
         case SIDCO_E_CAPTURE:
             return "first call for this residual and segment table must be made before stream capture begins";
         case SIDCO_E_UNSUPPORTED: return "not available in this build of the library";
+        case SIDCO_E_TYPE: return "unknown element type";
+        case SIDCO_E_ALIGN: return "a pointer is not aligned as the entry point asks";
         default: break;
     }
     if (code > 0) return cudaGetErrorString((cudaError_t)code);

@@ -1,0 +1,412 @@
+// Quantising to microscaled 4-bit blocks and reading them back (formulas and layout: sidco_mx4.cuh), for sm_100a.
+//
+//   quantize_kernel    matrix -> codes and scales along its rows and / or of its transpose, from one read
+//   dequantize_kernel  the values of a quantised matrix
+//   compress_kernel    error-compensated quantisation of a flat gradient: acc = g + r, codes of acc, r <- acc - value
+//   mean_kernel        dense mean of N workers' gathered codes
+//
+// All four are bound by memory traffic: a few conversions and one four-lane maximum per eight elements.  A lane holds
+// eight neighbours (one 16-byte load of a 16-bit type, two of fp32; its codes are one word), four lanes hold a block.
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "../../include/sidco.h"
+#include "sidco_internal.h"
+#include "sidco_mx4.cuh"
+
+namespace sidco_mx4 {
+
+constexpr unsigned kFull = 0xffffffffu;
+
+__device__ __forceinline__ float widen(float x) { return x; }
+__device__ __forceinline__ float widen(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ float widen(__half x) { return __half2float(x); }
+
+template <typename T> __device__ __forceinline__ T narrow(float x);
+template <> __device__ __forceinline__ float narrow<float>(float x) { return x; }
+template <> __device__ __forceinline__ __nv_bfloat16 narrow<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+template <> __device__ __forceinline__ __half narrow<__half>(float x) { return __float2half_rn(x); }
+
+// Eight neighbours as loaded: 16 or 32 bytes.
+template <typename T> struct Raw { uint4 w[sizeof(T) / 2]; };
+
+template <typename T>
+__device__ __forceinline__ Raw<T> load_raw(const T* p) {
+    Raw<T> r;
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.w[i] = __ldcs(reinterpret_cast<const uint4*>(p) + i);
+    return r;
+}
+
+template <typename T>
+__device__ __forceinline__ void unpack(const Raw<T>& r, float (&x)[8]) {
+    const T* t = reinterpret_cast<const T*>(r.w);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = widen(t[i]);
+}
+
+// The first n of eight neighbours, zeros behind them.
+template <typename T, bool Vec>
+__device__ __forceinline__ void load8(const T* p, int n, float (&x)[8]) {
+    if (Vec && n >= 8) {
+        unpack<T>(load_raw(p), x);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = i < n ? widen(p[i]) : 0.0f;
+}
+
+template <typename T, bool Vec>
+__device__ __forceinline__ void store8(T* p, int n, const float (&x)[8]) {
+    if (Vec && n >= 8) {
+        alignas(16) T t[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) t[i] = narrow<T>(x[i]);
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i)
+            reinterpret_cast<uint4*>(p)[i] = reinterpret_cast<const uint4*>(t)[i];
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i < n) p[i] = narrow<T>(x[i]);
+}
+
+__device__ __forceinline__ uint32_t max8(const float (&x)[8]) {
+    uint32_t m = magnitude_bits(x[0]);
+#pragma unroll
+    for (int i = 1; i < 8; ++i) m = max(m, magnitude_bits(x[i]));
+    return m;
+}
+
+// Largest magnitude over the four lanes of a block.
+__device__ __forceinline__ uint32_t block_max(uint32_t m) {
+    m = max(m, __shfl_xor_sync(kFull, m, 1));
+    return max(m, __shfl_xor_sync(kFull, m, 2));
+}
+
+__device__ __forceinline__ uint32_t encode(const float (&x)[8], uint32_t byte) {
+    const uint32_t c = encode8(x, inverse_scale_of(byte));
+    return byte == 255u ? 0u : c;
+}
+
+// ------------------------------------------------------------------------------------------------ matrices
+
+constexpr int kQuantThreads = 512;
+constexpr int kTile = 128;            // a CTA takes 128 x 128 elements: whole scale tiles in both directions
+
+struct QuantArgs {
+    const void* x;
+    int64_t rows, cols, ld;
+    uint8_t *codes, *scales, *codes_t, *scales_t;
+    int64_t pitch, pitch_t;           // bytes of a row of codes
+    int64_t ktiles, ktiles_t;         // scale tiles along a row
+    int64_t tiles_c;                  // CTA tiles along the columns
+};
+
+// Rows are quantised as they are loaded (four lanes of a warp hold a block); for the transpose the tile goes through
+// shared memory, where one thread then reads 32 elements of a column.  A row of the tile starts 8 words later in
+// every group of 32 rows, so that the lanes of a warp (8 columns x 4 groups) read from 32 different banks and write
+// 64 neighbouring bytes of a column's codes.
+template <typename T, bool Vec>
+__global__ void __launch_bounds__(kQuantThreads) quantize_kernel(const QuantArgs A) {
+    extern __shared__ float s_x[];                                   // [128][128], skewed; only with codes_t
+    __shared__ __align__(16) uint8_t s_scale[kTileBytes];
+    const int64_t r0 = (int64_t)(blockIdx.x / A.tiles_c) * kTile, c0 = (int64_t)(blockIdx.x % A.tiles_c) * kTile;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int oct = lane & 15;                                       // which eight columns
+    const int64_t c = c0 + oct * 8;
+    const int left = (int)min((int64_t)8, A.cols - c);               // may be <= 0
+    float x[4][8];
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+        const int64_t r = r0 + p * 32 + warp * 2 + (lane >> 4);
+        const bool in = r < A.rows && left > 0;
+        load8<T, Vec>(in ? (const T*)A.x + r * A.ld + c : (const T*)A.x, in ? left : 0, x[p]);
+    }
+    if (A.codes_t) {
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+            float* at = s_x + (p * 32 + warp * 2 + (lane >> 4)) * kTile + p * 8 + oct * 8;
+            reinterpret_cast<float4*>(at)[0] = make_float4(x[p][0], x[p][1], x[p][2], x[p][3]);
+            reinterpret_cast<float4*>(at)[1] = make_float4(x[p][4], x[p][5], x[p][6], x[p][7]);
+        }
+    }
+    if (A.codes) {
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+            const int rt = p * 32 + warp * 2 + (lane >> 4);
+            const int64_t r = r0 + rt;
+            const uint32_t byte = scale_byte(block_max(max8(x[p])));
+            // (rows and columns behind the matrix hold zeros, so that the unused bytes of a scale tile become 0)
+            if ((lane & 3) == 0) s_scale[scale_in_tile(rt, oct >> 2)] = (uint8_t)byte;
+            if (r < A.rows && c - (oct & 3) * 8 < A.cols)            // the last block is written whole
+                *reinterpret_cast<uint32_t*>(A.codes + r * A.pitch + (c >> 1)) = encode(x[p], byte);
+        }
+        __syncthreads();
+        if (threadIdx.x < kTileBytes / 16)
+            reinterpret_cast<uint4*>(A.scales + ((r0 / kTile) * A.ktiles + c0 / kTile) * kTileBytes)[threadIdx.x] =
+                reinterpret_cast<const uint4*>(s_scale)[threadIdx.x];
+    }
+    if (!A.codes_t) return;
+    __syncthreads();
+    const int col = warp * 8 + (lane & 7), g = lane >> 3;            // a column and one of its four blocks
+    const float* from = s_x + g * (32 * kTile + 8) + col;
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) m = max(m, magnitude_bits(from[i * kTile]));
+    const uint32_t byte = scale_byte(m);
+    uint4 codes;
+    uint32_t* w = &codes.x;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        float y[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = from[(q * 8 + i) * kTile];
+        w[q] = encode(y, byte);
+    }
+    s_scale[scale_in_tile(col, g)] = (uint8_t)byte;
+    if (c0 + col < A.cols && r0 + g * 32 < A.rows)
+        *reinterpret_cast<uint4*>(A.codes_t + (c0 + col) * A.pitch_t + (r0 + g * 32) / 2) = codes;
+    __syncthreads();
+    if (threadIdx.x < kTileBytes / 16)
+        reinterpret_cast<uint4*>(A.scales_t + ((c0 / kTile) * A.ktiles_t + r0 / kTile) * kTileBytes)[threadIdx.x] =
+            reinterpret_cast<const uint4*>(s_scale)[threadIdx.x];
+}
+
+// A lane reads one word of codes and writes eight values.
+template <typename T, bool Vec>
+__global__ void __launch_bounds__(256) dequantize_kernel(const uint8_t* __restrict__ codes,
+                                                         const uint8_t* __restrict__ scales, int64_t rows, int64_t cols,
+                                                         int64_t pitch, int64_t ktiles, T* __restrict__ out, int64_t ld,
+                                                         int64_t octs) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= rows * octs) return;
+    const int64_t r = i / octs, o = i - r * octs, j = o >> 2;
+    const uint32_t c = *reinterpret_cast<const uint32_t*>(codes + r * pitch + o * 4);
+    const uint32_t byte = scales[((r / kTileRows) * ktiles + j / kTileBlocks) * kTileBytes +
+                                 scale_in_tile((int)(r % kTileRows), (int)(j & 3))];
+    float v[8];
+    decode8(c, v);
+    const float s = scale_of(byte);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] *= s;
+    store8<T, Vec>(out + r * ld + o * 8, (int)min((int64_t)8, cols - o * 8), v);
+}
+
+// ------------------------------------------------------------------------------------------------ flat vectors
+
+template <typename T, bool Vec, int U>
+__global__ void __launch_bounds__(256) compress_kernel(const T* __restrict__ grad, float* __restrict__ residual,
+                                                       int64_t d, uint8_t* __restrict__ codes,
+                                                       uint8_t* __restrict__ scales) {
+    const int64_t first = (int64_t)blockIdx.x * (256 * U) + threadIdx.x;
+    const int64_t octs = blocks_of(d) * 4;                            // whole blocks
+    float g[U][8], r[U][8];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int64_t at = (first + u * 256) * 8;
+        const int n = (int)max((int64_t)0, min((int64_t)8, d - at));
+        load8<T, Vec>(n ? grad + at : grad, n, g[u]);
+        load8<float, Vec>(n ? residual + at : residual, n, r[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int64_t o = first + u * 256, at = o * 8;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) g[u][k] += r[u][k];               // one fp32 addition
+        const uint32_t byte = scale_byte(block_max(max8(g[u])));
+        const uint32_t c = encode(g[u], byte);
+        if (o >= octs) continue;
+        *reinterpret_cast<uint32_t*>(codes + o * 4) = c;
+        if ((threadIdx.x & 3) == 0) scales[o >> 2] = (uint8_t)byte;
+        float v[8];
+        decode8(c, v);
+        const float s = scale_of(byte);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) g[u][k] = fmaf(-v[k], s, g[u][k]);   // v s is exact: one rounding
+        const int n = (int)max((int64_t)0, min((int64_t)8, d - at));
+        if (n) store8<float, Vec>(residual + at, n, g[u]);
+    }
+}
+
+// The workers are added in their order, in fp32 (a decoded value has two significant bits), then scaled by 1/N.
+template <bool Vec>
+__global__ void __launch_bounds__(256) mean_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
+                                                   int n_workers, int64_t d, float* __restrict__ out) {
+    const int64_t nb = blocks_of(d), o = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t at = o * 8;
+    if (at >= d) return;
+    float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    const uint8_t* cp = codes + o * 4;
+    const uint8_t* sp = scales + (o >> 2);
+    constexpr int kAhead = 8;
+    for (int w0 = 0; w0 < n_workers; w0 += kAhead) {
+        uint32_t c[kAhead], b[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const bool on = w0 + i < n_workers;
+            c[i] = on ? *reinterpret_cast<const uint32_t*>(cp + (int64_t)(w0 + i) * nb * 16) : 0u;
+            b[i] = on ? sp[(int64_t)(w0 + i) * nb] : 0u;
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            if (w0 + i >= n_workers) break;
+            float v[8];
+            decode8(c[i], v);
+            const float s = scale_of(b[i]);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) sum[k] = fmaf(v[k], s, sum[k]);
+        }
+    }
+    const float inv = 1.0f / (float)n_workers;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum[k] *= inv;
+    store8<float, Vec>(out + at, (int)min((int64_t)8, d - at), sum);
+}
+
+// ------------------------------------------------------------------------------------------------ host side
+
+static bool aligned(const void* p, uintptr_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
+
+static int finish(cudaError_t e) {
+    if (e != cudaSuccess) return (int)e;
+    sidco_internal::note_launch();
+    return 0;
+}
+
+template <typename T, bool Vec>
+static int launch_quantize(const QuantArgs& a, int64_t grid, cudaStream_t s) {
+    static bool sized[64] = {};
+    const size_t smem = a.codes_t ? (kTile * kTile + 32) * sizeof(float) : 0;
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return (int)e;
+    if (dev < 0 || dev >= 64) return SIDCO_E_SIZE;
+    if (!sized[dev]) {                      // (setting it twice from two threads is harmless)
+        e = cudaFuncSetAttribute(quantize_kernel<T, Vec>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                 (int)((kTile * kTile + 32) * sizeof(float)));
+        if (e != cudaSuccess) return (int)e;
+        sized[dev] = true;
+    }
+    quantize_kernel<T, Vec><<<(unsigned)grid, kQuantThreads, smem, s>>>(a);
+    return finish(cudaGetLastError());
+}
+
+template <typename T>
+static int quantize_typed(const QuantArgs& a, int64_t grid, cudaStream_t s) {
+    const bool vec = aligned(a.x, 16) && a.ld * sizeof(T) % 16 == 0;
+    return vec ? launch_quantize<T, true>(a, grid, s) : launch_quantize<T, false>(a, grid, s);
+}
+
+template <typename T>
+static int dequantize_typed(const uint8_t* codes, const uint8_t* scales, int64_t rows, int64_t cols, void* out, int64_t ld,
+                            cudaStream_t s) {
+    const int64_t octs = (cols + 7) / 8, pitch = blocks_of(cols) * 16, ktiles = (blocks_of(cols) + 3) / 4;
+    const int64_t grid = (rows * octs + 255) / 256;
+    if (grid > 0x7fffffff) return SIDCO_E_SIZE;
+    if (aligned(out, 16) && ld * sizeof(T) % 16 == 0)
+        dequantize_kernel<T, true><<<(unsigned)grid, 256, 0, s>>>(codes, scales, rows, cols, pitch, ktiles, (T*)out, ld, octs);
+    else
+        dequantize_kernel<T, false><<<(unsigned)grid, 256, 0, s>>>(codes, scales, rows, cols, pitch, ktiles, (T*)out, ld, octs);
+    return finish(cudaGetLastError());
+}
+
+template <typename T>
+static int compress_typed(const void* grad, float* residual, int64_t d, uint8_t* codes, uint8_t* scales, cudaStream_t s) {
+    constexpr int U = 2;
+    const int64_t grid = (blocks_of(d) * 4 + 256 * U - 1) / (256 * U);
+    if (aligned(grad, 16) && aligned(residual, 16))
+        compress_kernel<T, true, U><<<(unsigned)grid, 256, 0, s>>>((const T*)grad, residual, d, codes, scales);
+    else
+        compress_kernel<T, false, U><<<(unsigned)grid, 256, 0, s>>>((const T*)grad, residual, d, codes, scales);
+    return finish(cudaGetLastError());
+}
+
+constexpr int64_t kMaxDim = ((int64_t)1 << 31) - ((int64_t)1 << 16);
+
+}  // namespace sidco_mx4
+
+extern "C" {
+
+int64_t sidco_mx4_code_bytes(int64_t rows, int64_t cols) {
+    if (rows < 0 || cols < 0 || rows > sidco_mx4::kMaxDim || cols > sidco_mx4::kMaxDim) return SIDCO_E_SIZE;
+    return rows * sidco_mx4::blocks_of(cols) * 16;
+}
+
+int64_t sidco_mx4_scale_bytes(int64_t rows, int64_t cols) {
+    if (rows < 0 || cols < 0 || rows > sidco_mx4::kMaxDim || cols > sidco_mx4::kMaxDim) return SIDCO_E_SIZE;
+    return (rows + 127) / 128 * ((sidco_mx4::blocks_of(cols) + 3) / 4) * sidco_mx4::kTileBytes;
+}
+
+int sidco_mx4_quantize(const void* x, int x_type, int64_t rows, int64_t cols, int64_t ld, uint8_t* codes, uint8_t* scales,
+                       uint8_t* codes_t, uint8_t* scales_t, void* stream) {
+    using namespace sidco_mx4;
+    if (rows < 0 || cols < 0 || rows > kMaxDim || cols > kMaxDim) return SIDCO_E_SIZE;
+    if (x_type < SIDCO_T_F32 || x_type > SIDCO_T_F16) return SIDCO_E_TYPE;
+    if (ld < cols) return SIDCO_E_PARAMS;
+    if (rows == 0 || cols == 0) return 0;
+    if (!x || (!codes && !codes_t) || !codes != !scales || !codes_t != !scales_t) return SIDCO_E_NULL;
+    const size_t size = x_type == SIDCO_T_F32 ? 4 : 2;
+    if (!aligned(x, size) || !aligned(codes, 16) || !aligned(scales, 16) || !aligned(codes_t, 16) || !aligned(scales_t, 16))
+        return SIDCO_E_ALIGN;
+    QuantArgs a{x, rows, cols, ld, codes, scales, codes_t, scales_t, blocks_of(cols) * 16, blocks_of(rows) * 16,
+                (blocks_of(cols) + 3) / 4, (blocks_of(rows) + 3) / 4, (cols + kTile - 1) / kTile};
+    const int64_t grid = (rows + kTile - 1) / kTile * a.tiles_c;
+    if (grid > 0x7fffffff) return SIDCO_E_SIZE;
+    cudaStream_t s = (cudaStream_t)stream;
+    if (x_type == SIDCO_T_F32) return quantize_typed<float>(a, grid, s);
+    if (x_type == SIDCO_T_BF16) return quantize_typed<__nv_bfloat16>(a, grid, s);
+    return quantize_typed<__half>(a, grid, s);
+}
+
+int sidco_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t rows, int64_t cols, void* out, int out_type,
+                         int64_t ld, void* stream) {
+    using namespace sidco_mx4;
+    if (rows < 0 || cols < 0 || rows > kMaxDim || cols > kMaxDim) return SIDCO_E_SIZE;
+    if (out_type < SIDCO_T_F32 || out_type > SIDCO_T_F16) return SIDCO_E_TYPE;
+    if (ld < cols) return SIDCO_E_PARAMS;
+    if (rows == 0 || cols == 0) return 0;
+    if (!codes || !scales || !out) return SIDCO_E_NULL;
+    if (!aligned(codes, 16) || !aligned(scales, 16) || !aligned(out, out_type == SIDCO_T_F32 ? 4 : 2)) return SIDCO_E_ALIGN;
+    cudaStream_t s = (cudaStream_t)stream;
+    if (out_type == SIDCO_T_F32) return dequantize_typed<float>(codes, scales, rows, cols, out, ld, s);
+    if (out_type == SIDCO_T_BF16) return dequantize_typed<__nv_bfloat16>(codes, scales, rows, cols, out, ld, s);
+    return dequantize_typed<__half>(codes, scales, rows, cols, out, ld, s);
+}
+
+int sidco_mx4_compress(const void* grad, int grad_type, float* residual, int64_t d, uint8_t* codes, uint8_t* scales,
+                       void* stream) {
+    using namespace sidco_mx4;
+    if (d < 0 || d > kMaxDim) return SIDCO_E_SIZE;
+    if (grad_type < SIDCO_T_F32 || grad_type > SIDCO_T_F16) return SIDCO_E_TYPE;
+    if (d == 0) return 0;
+    if (!grad || !residual || !codes || !scales) return SIDCO_E_NULL;
+    const uintptr_t size = grad_type == SIDCO_T_F32 ? 4 : 2;
+    if (!aligned(grad, size) || !aligned(residual, 4) || !aligned(codes, 16)) return SIDCO_E_ALIGN;
+    const uintptr_t g = (uintptr_t)grad, r = (uintptr_t)residual;
+    if (g < r + (uintptr_t)d * 4 && r < g + (uintptr_t)d * size) return SIDCO_E_ALIAS;
+    cudaStream_t s = (cudaStream_t)stream;
+    if (grad_type == SIDCO_T_F32) return compress_typed<float>(grad, residual, d, codes, scales, s);
+    if (grad_type == SIDCO_T_BF16) return compress_typed<__nv_bfloat16>(grad, residual, d, codes, scales, s);
+    return compress_typed<__half>(grad, residual, d, codes, scales, s);
+}
+
+int sidco_mx4_mean(const uint8_t* codes_all, const uint8_t* scales_all, int n_workers, int64_t d, float* out_dense,
+                   void* stream) {
+    using namespace sidco_mx4;
+    if (n_workers < 1 || n_workers > SIDCO_AGG_MAX_WORKERS) return SIDCO_E_PARAMS;
+    if (d < 0 || d > kMaxDim) return SIDCO_E_SIZE;
+    if (d == 0) return 0;
+    if (!codes_all || !scales_all || !out_dense) return SIDCO_E_NULL;
+    if (!aligned(codes_all, 16) || !aligned(out_dense, 4)) return SIDCO_E_ALIGN;
+    cudaStream_t s = (cudaStream_t)stream;
+    const int64_t grid = ((d + 7) / 8 + 255) / 256;
+    if (aligned(out_dense, 16))
+        mean_kernel<true><<<(unsigned)grid, 256, 0, s>>>(codes_all, scales_all, n_workers, d, out_dense);
+    else
+        mean_kernel<false><<<(unsigned)grid, 256, 0, s>>>(codes_all, scales_all, n_workers, d, out_dense);
+    return finish(cudaGetLastError());
+}
+
+}  // extern "C"

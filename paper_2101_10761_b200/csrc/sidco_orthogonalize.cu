@@ -1,0 +1,693 @@
+// Momentum and orthogonalised update of the matrices of a flat model vector, for sm_100a.
+//
+// For every matrix:  M <- mu M + G;  U = G + mu M (Nesterov) or M;  X = U / (|U|_F + eps); then `steps` times
+//     A = X X^T,   X <- (a I + b A + c A^2) X,          (a, b, c) = (3.4445, -4.7750, 2.0315),
+// tall matrices through their transpose, so that X is s x l with s <= l.
+//
+// The steps are taken in groups (two, then one if their number is odd, then twos).  Inside a group only s x s matrices
+// are multiplied: with B = a I + b A + c A^2 the Gram matrix of the next X is B A B, and the group's product of the B is
+// applied to X once.  That replaces a Gram product and an application over the long side (3 s^2 l) by four products
+// (4 s^3) of which only half the tiles are computed and mirrored (all of them are symmetric: polynomials of one A).
+// Longer groups would save more, but each step of a group amplifies the rounding of A by up to a^2: groups of three
+// and two have 3e-3 of error where these have 1.1e-3 to 2e-3, as much as single steps (Laplace entries with eight
+// strong directions, 64 x 64 to 512 x 4608).
+//
+// Operands are fp16 (eleven significant bits; bf16's eight would leave 1e-2 of error in the result), sums fp32.  Every
+// singular value stays below 1.2 and every eigenvalue of a B within [0.6, 3.45], so fixed powers of two (kX, kA, ...)
+// keep all entries inside fp16's normal range.  The first X is kept as a sum of two fp16 parts in the application,
+// where its rounding would otherwise be the largest error (small singular values are scaled up by a^5 in the end).
+//
+// Workspace matrices are stored as units of 64 x 64 fp16 in the 128-byte-swizzled image that the tensor cores read, so
+// that a stage of operands is one or two contiguous bulk copies, the same unit serves as K-major operand (Gram) and as
+// MN-major operand (application), and nothing depends on the caller's alignment.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <vector>
+
+#include "../../include/sidco.h"
+#include "sidco_internal.h"
+#include "sidco_tc.cuh"
+
+namespace sidco_ortho {
+
+using namespace sidco_tc;
+
+constexpr float kCa = 3.4445f, kCb = -4.7750f, kCc = 2.0315f;
+
+// stored value = value * 2^k
+constexpr int kX = 14;                // X (entries <= 1.2)
+constexpr int kA = 14;                // A and B A (eigenvalues <= 1.44)
+constexpr int kB = 13;                // B (<= 3.45)
+constexpr int kP = 10;                // products of two or three B (<= 41)
+
+constexpr int kUnit = 64;             // units of 64 x 64
+constexpr int kUnitBytes = kUnit * kUnit * 2;
+constexpr int kMaxMats = 128;         // matrices of one chain of launches
+constexpr int kChunk = 16384;         // elements of a matrix per CTA of the momentum pass
+
+enum Buffer { kBufA, kBufA2, kBufB, kBufT, kBufP, kBufP2, kSmallBuffers };
+
+struct Mat {
+    int64_t offset;                   // of the matrix in the flat vectors
+    int64_t x_hi, x_lo, x_next;       // bytes into the workspace: s x l matrices
+    int64_t small;                    // first of the s x s matrices
+    int rows, cols, s, l;
+    int sp, lp;                       // s to a multiple of 128, l to a multiple of 64
+    int partial0, n_chunks;           // partial sums of squares
+};
+
+struct Table {
+    int n;
+    int chunk_at[kMaxMats + 1];       // first CTA of every matrix: momentum pass,
+    int unit_at[kMaxMats + 1];        // normalisation,
+    int sym_at[kMaxMats + 1];         // symmetric products,
+    int apply_at[kMaxMats + 1];       // applications
+    Mat m[kMaxMats];
+};
+
+__device__ __forceinline__ int find(const int* at, int n, int i) {
+    int lo = 0, hi = n;               // at[lo] <= i < at[hi]
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (at[mid] <= i) lo = mid; else hi = mid;
+    }
+    return lo;
+}
+
+__device__ __forceinline__ float widen(float x) { return x; }
+__device__ __forceinline__ float widen(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ float widen(__half x) { return __half2float(x); }
+
+// ---------------------------------------------------------------------------------------------- momentum, norm
+
+// M <- mu M + G and the sum of squares of U per chunk of 16384 elements (fp64: gradients may be tiny or huge).  The
+// last chunk of a matrix to arrive adds the chunks' sums in their order.
+template <typename T>
+__global__ void __launch_bounds__(256) momentum_kernel(const __grid_constant__ Table t, const T* __restrict__ grad,
+                                                       float* __restrict__ momentum, float mu, int nesterov, float eps,
+                                                       double* __restrict__ partial, int* __restrict__ arrived,
+                                                       float* __restrict__ inv_norm) {
+    __shared__ double s_sum[8];
+    __shared__ int s_last;
+    launch_dependents();
+    const int i = find(t.chunk_at, t.n, blockIdx.x), chunk = blockIdx.x - t.chunk_at[i];
+    const Mat& m = t.m[i];
+    const int64_t n = (int64_t)m.rows * m.cols, from = (int64_t)chunk * kChunk;
+    const int64_t to = min(n, from + kChunk);
+    double sum = 0.0;
+    for (int64_t e0 = from + threadIdx.x; e0 < to; e0 += 256 * 8) {
+        float g[8], v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int64_t e = e0 + k * 256;
+            g[k] = e < to ? widen(grad[m.offset + e]) : 0.0f;
+            v[k] = e < to && momentum ? momentum[m.offset + e] : 0.0f;
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int64_t e = e0 + k * 256;
+            float u = g[k];
+            if (momentum) {
+                const float mom = fmaf(mu, v[k], g[k]);
+                if (e < to) momentum[m.offset + e] = mom;
+                u = nesterov ? fmaf(mu, mom, g[k]) : mom;
+            }
+            sum += (double)u * (double)u;
+        }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_down_sync(0xffffffffu, sum, o);
+    if ((threadIdx.x & 31) == 0) s_sum[threadIdx.x >> 5] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        sum = 0.0;
+        for (int w = 0; w < 8; ++w) sum += s_sum[w];
+        partial[m.partial0 + chunk] = sum;
+        __threadfence();
+        s_last = atomicAdd(arrived + i, 1) == m.n_chunks - 1;
+        __threadfence();
+    }
+    __syncthreads();
+    if (!s_last) return;
+    sum = 0.0;
+    for (int c = threadIdx.x; c < m.n_chunks; c += 256) sum += __ldcg(partial + m.partial0 + c);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_down_sync(0xffffffffu, sum, o);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) s_sum[threadIdx.x >> 5] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        sum = 0.0;
+        for (int w = 0; w < 8; ++w) sum += s_sum[w];
+        inv_norm[i] = (float)(1.0 / (sqrt(sum) + (double)eps));
+    }
+}
+
+// Eight neighbours of a row of a unit: where they lie in the swizzled image.
+__device__ __forceinline__ int in_unit(int r, int c8) { return r * 128 + ((c8 ^ (r & 7)) << 4); }
+
+__device__ __forceinline__ uint4 pack8(const float (&v)[8]) {
+    uint4 w;
+    uint32_t* p = &w.x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const __half2 h = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
+        p[i] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+    return w;
+}
+
+// One CTA per unit: U again (from what the momentum pass left), scaled, transposed if tall, split in two fp16 parts.
+template <typename T>
+__global__ void __launch_bounds__(256) normalize_kernel(const __grid_constant__ Table t, const T* __restrict__ grad,
+                                                        const float* __restrict__ momentum, float mu, int nesterov,
+                                                        const float* __restrict__ inv_norm, uint8_t* __restrict__ ws,
+                                                        Table* __restrict__ table_out) {
+    __shared__ float s_u[kUnit][kUnit + 1];
+    launch_dependents();
+    const int i = find(t.unit_at, t.n, blockIdx.x), u = blockIdx.x - t.unit_at[i];
+    const Mat& m = t.m[i];
+    const int rb = u % (m.sp / kUnit), cb = u / (m.sp / kUnit);
+    const bool tall = m.rows > m.cols;
+    wait_prerequisites();
+    // the kernels behind this one read the table from memory
+    if (blockIdx.x == 0)
+        for (int w = threadIdx.x; w < (int)(sizeof(Table) / 4); w += 256)
+            reinterpret_cast<int*>(table_out)[w] = reinterpret_cast<const int*>(&t)[w];
+    const float inv = __ldcg(inv_norm + i);
+    // neighbours along the matrix's own rows: X's columns, or X's rows if tall
+    const int along = threadIdx.x & 63, across0 = threadIdx.x >> 6;
+    const int my_r = (tall ? rb : cb) * kUnit + along;                // index along the matrix's row
+#pragma unroll 4
+    for (int k = 0; k < 16; ++k) {
+        const int across = across0 + k * 4;
+        const int my_a = (tall ? cb : rb) * kUnit + across;
+        float x = 0.0f;
+        if (my_a < m.rows && my_r < m.cols) {
+            const int64_t e = m.offset + (int64_t)my_a * m.cols + my_r;
+            if (momentum) {
+                x = __ldcg(momentum + e);
+                if (nesterov) x = fmaf(mu, x, widen(grad[e]));
+            } else {
+                x = widen(grad[e]);
+            }
+        }
+        if (tall) s_u[along][across] = x; else s_u[across][along] = x;
+    }
+    __syncthreads();
+    const float scale = inv * (float)(1 << kX);
+    const int64_t unit = ((int64_t)cb * (m.sp / kUnit) + rb) * kUnitBytes;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int r = (threadIdx.x >> 3) + k * 32, c8 = threadIdx.x & 7;
+        float v[8], lo[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            v[j] = s_u[r][c8 * 8 + j] * scale;
+            lo[j] = v[j] - __half2float(__float2half_rn(v[j]));
+        }
+        *reinterpret_cast<uint4*>(ws + m.x_hi + unit + in_unit(r, c8)) = pack8(v);
+        *reinterpret_cast<uint4*>(ws + m.x_lo + unit + in_unit(r, c8)) = pack8(lo);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- products
+
+constexpr int kTile = 128;
+constexpr int kStageBytes = 2 * kTile * kUnit * 2;                    // 128 x 64 of both operands: 32 KB
+constexpr int kStages = 3;
+constexpr int kProductThreads = 128;
+constexpr int kProductSmem = kStages * kStageBytes + 1024;            // (base rounded up to 1024)
+
+struct Product {
+    int left, right;                  // s x s operands; left = -1: the Gram product of X
+    int plus;                         // matrix added times beta (-1: none)
+    int to;
+    float alpha, beta, gamma;         // to = alpha (left right) + beta plus + gamma I
+};
+
+struct Chain {
+    Product p[2];                     // symmetric products: blockIdx.y takes one
+    int x_in, parts;                  // which of the two X buffers holds X; 2: with the second part of the first X
+    // application
+    int op;                           // s x s operand
+    int last;                         // write bf16 into the caller's vector instead of the next X
+    float alpha;
+};
+
+__device__ __forceinline__ const uint8_t* unit_at(const uint8_t* base, int sp, int cb, int rb) {
+    return base + ((int64_t)cb * (sp / kUnit) + rb) * kUnitBytes;
+}
+
+// One 128 x 128 tile per CTA, two CTAs per SM (the end of one runs under the products of the other).  Thread 0 feeds the
+// stages, thread 32 issues the products; then all four warps take a quarter of the rows each out of tensor memory.
+template <bool kSym>
+__global__ void __launch_bounds__(kProductThreads, 2) product_kernel(const Table* t, uint8_t* ws,
+                                                                     const __grid_constant__ Chain c,
+                                                                     __nv_bfloat16* __restrict__ out, int* timeouts) {
+    extern __shared__ uint8_t s_raw[];
+    __shared__ uint64_t s_full[kStages], s_free[kStages], s_done;
+    __shared__ uint32_t s_tmem;
+    __shared__ int s_failed;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    uint8_t* smem = (uint8_t*)(((uintptr_t)s_raw + 1023) & ~(uintptr_t)1023);
+    const uint32_t stage0 = smem_addr(smem);
+    if (warp == 0) tmem_alloc(&s_tmem, kTile);
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kStages; ++i) {
+            mbar_init(smem_addr(&s_full[i]), 1);
+            mbar_init(smem_addr(&s_free[i]), 1);
+        }
+        mbar_init(smem_addr(&s_done), 1);
+        s_failed = 0;
+        mbar_init_fence();
+    }
+    fence_before_sync();
+    __syncthreads();
+    fence_after_sync();
+    launch_dependents();
+    wait_prerequisites();
+    const uint32_t tmem = s_tmem;
+
+    const int* at = kSym ? t->sym_at : t->apply_at;
+    const int mi = find(at, t->n, blockIdx.x);
+    int tile = blockIdx.x - at[mi];
+    const Mat m = t->m[mi];
+    const int sp = m.sp, mt = sp / kTile;
+    const int64_t small_bytes = (int64_t)sp * sp * 2;
+    const uint8_t* x_in = ws + (c.x_in ? m.x_next : m.x_hi);
+    const Product& p = c.p[kSym ? blockIdx.y : 0];
+    int ti, tj;                                                       // tile row, tile column
+    const uint8_t *left, *right;
+    int steps;                                                        // K in units of 64
+    bool gram = false;
+    if (kSym) {
+        ti = (int)((sqrtf(8.0f * tile + 1.0f) - 1.0f) * 0.5f);        // lower triangle, row by row
+        while ((ti + 1) * (ti + 2) / 2 <= tile) ++ti;
+        while (ti * (ti + 1) / 2 > tile) --ti;
+        tj = tile - ti * (ti + 1) / 2;
+        gram = p.left < 0;
+        left = gram ? x_in : ws + m.small + p.left * small_bytes;
+        right = gram ? x_in : ws + m.small + p.right * small_bytes;
+        steps = (gram ? m.lp : (m.s + kUnit - 1) / kUnit * kUnit) / kUnit;
+    } else {
+        ti = tile % mt;
+        tj = tile / mt;
+        left = ws + m.small + c.op * small_bytes;
+        right = x_in;
+        steps = (m.s + kUnit - 1) / kUnit * c.parts;
+    }
+    const int half = kSym ? 0 : (m.s + kUnit - 1) / kUnit;
+    const int cols_here = kSym ? 2 : min(2, m.lp / kUnit - tj * 2);   // units of X that the tile has
+
+    if (threadIdx.x == 0) {
+        for (int k = 0; k < steps; ++k) {
+            const int st = k % kStages;
+            if (k >= kStages && !mbar_wait(smem_addr(&s_free[st]), (k / kStages - 1) & 1, &s_failed)) break;
+            const uint32_t a = stage0 + st * kStageBytes, b = a + kTile * kUnit * 2, bar = smem_addr(&s_full[st]);
+            if (kSym) {
+                mbar_expect_tx(bar, ti == tj && left == right ? kStageBytes / 2 : kStageBytes);
+                bulk_load(a, unit_at(left, sp, k, ti * 2), kStageBytes / 2, bar);
+                if (ti != tj || left != right) bulk_load(b, unit_at(right, sp, k, tj * 2), kStageBytes / 2, bar);
+            } else {
+                const int kb = k < half ? k : k - half;
+                const uint8_t* x = k < half ? right : ws + m.x_lo;
+                mbar_expect_tx(bar, kStageBytes / 2 + cols_here * kUnitBytes);
+                bulk_load(a, unit_at(left, sp, kb, ti * 2), kStageBytes / 2, bar);
+                for (int u = 0; u < cols_here; ++u)
+                    bulk_load(b + u * kUnitBytes, unit_at(x, sp, tj * 2 + u, kb), kUnitBytes, bar);
+            }
+        }
+    } else if (threadIdx.x == 32) {
+        const uint32_t shape = f16_shape(kTile, kTile, !kSym);
+        bool ok = true;
+        for (int k = 0; k < steps && ok; ++k) {
+            const int st = k % kStages;
+            ok = mbar_wait(smem_addr(&s_full[st]), (k / kStages) & 1, &s_failed);
+            if (!ok) break;
+            fence_after_sync();
+            const uint32_t a = stage0 + st * kStageBytes;
+            const uint32_t b = kSym && ti == tj && left == right ? a : a + kTile * kUnit * 2;
+#pragma unroll
+            for (int q = 0; q < kUnit / 16; ++q) {
+                const uint64_t da = swizzled_operand(a + q * 32, 16, 1024);
+                const uint64_t db = kSym ? swizzled_operand(b + q * 32, 16, 1024)
+                                         : swizzled_operand(b + q * 2048, kUnitBytes, 1024);
+                mma_f16(tmem, da, db, shape, k > 0 || q > 0);
+            }
+            tc_commit(smem_addr(&s_free[st]));
+        }
+        tc_commit(smem_addr(&s_done));
+    }
+    __syncwarp();
+    mbar_wait(smem_addr(&s_done), 0, &s_failed);
+    __syncwarp();
+    fence_after_sync();
+
+    // ---- the tile, 32 columns at a time: stages are free now and hold the images on their way out
+    const int row = warp * 32 + lane;
+    const bool mirror = kSym && ti != tj;
+    if (kSym) {
+        const uint8_t* plus = p.plus >= 0 ? ws + m.small + p.plus * small_bytes : nullptr;
+#pragma unroll 1
+        for (int q = 0; q < kTile / 32; ++q) {
+            uint32_t acc[32];
+            tmem_load32(tmem + ((uint32_t)(warp * 32) << 16) + q * 32, acc);
+#pragma unroll
+            for (int o = 0; o < 4; ++o) {
+                const int c8 = (q * 4 + o) & 7, cu = q >> 1;          // eight columns of the tile's unit column cu
+                float v[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = p.alpha * __uint_as_float(acc[o * 8 + j]);
+                if (plus) {
+                    const uint4 w = __ldcg(reinterpret_cast<const uint4*>(
+                        unit_at(plus, sp, tj * 2 + cu, ti * 2 + (row >> 6)) + in_unit(row & 63, c8)));
+                    const __half2* h = reinterpret_cast<const __half2*>(&w);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float2 f = __half22float2(h[j]);
+                        v[2 * j] = fmaf(p.beta, f.x, v[2 * j]);
+                        v[2 * j + 1] = fmaf(p.beta, f.y, v[2 * j + 1]);
+                    }
+                }
+                if (ti == tj) {
+                    const int d = row - (q * 32 + o * 8);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (d == j) v[j] += p.gamma;
+                }
+                *reinterpret_cast<uint4*>(smem + (cu * 2 + (row >> 6)) * kUnitBytes + in_unit(row & 63, c8)) = pack8(v);
+                if (mirror) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const int col = q * 32 + o * 8 + j;           // becomes a row
+                        *reinterpret_cast<__half*>(smem + kStageBytes + ((row >> 6) * 2 + (col >> 6)) * kUnitBytes +
+                                                   in_unit(col & 63, (row & 63) >> 3) + (row & 7) * 2) =
+                            __float2half_rn(v[j]);
+                    }
+                }
+            }
+        }
+        fence_async_shared();
+        __syncthreads();
+        if (threadIdx.x == 0 && !s_failed) {
+            uint8_t* to = ws + m.small + p.to * small_bytes;
+            for (int cu = 0; cu < 2; ++cu) {
+                bulk_store((void*)unit_at(to, sp, tj * 2 + cu, ti * 2), stage0 + cu * 2 * kUnitBytes, 2 * kUnitBytes);
+                if (mirror)
+                    bulk_store((void*)unit_at(to, sp, ti * 2 + cu, tj * 2), stage0 + kStageBytes + cu * 2 * kUnitBytes,
+                               2 * kUnitBytes);
+            }
+            bulk_store_commit();
+            bulk_store_wait();
+        }
+    } else if (!c.last) {
+#pragma unroll 1
+        for (int q = 0; q < kTile / 32; ++q) {
+            uint32_t acc[32];
+            tmem_load32(tmem + ((uint32_t)(warp * 32) << 16) + q * 32, acc);
+#pragma unroll
+            for (int o = 0; o < 4; ++o) {
+                float v[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = c.alpha * __uint_as_float(acc[o * 8 + j]);
+                *reinterpret_cast<uint4*>(smem + ((q >> 1) * 2 + (row >> 6)) * kUnitBytes +
+                                          in_unit(row & 63, (q * 4 + o) & 7)) = pack8(v);
+            }
+        }
+        fence_async_shared();
+        __syncthreads();
+        if (threadIdx.x == 0 && !s_failed) {
+            for (int cu = 0; cu < cols_here; ++cu)
+                bulk_store((void*)unit_at(ws + (c.x_in ? m.x_hi : m.x_next), sp, tj * 2 + cu, ti * 2), stage0 + cu * 2 * kUnitBytes,
+                           2 * kUnitBytes);
+            bulk_store_commit();
+            bulk_store_wait();
+        }
+    } else {
+        // bf16 into the caller's vector: neighbours of a row of the caller's matrix are rows of X if it is tall
+        const bool tall = m.rows > m.cols;
+        constexpr int kPad = kTile + 2;                               // bf16 per row of the staged tile
+        __nv_bfloat16* s_out = reinterpret_cast<__nv_bfloat16*>(smem);
+#pragma unroll 1
+        for (int q = 0; q < kTile / 32; ++q) {
+            uint32_t acc[32];
+            tmem_load32(tmem + ((uint32_t)(warp * 32) << 16) + q * 32, acc);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+                const __nv_bfloat16 b = __float2bfloat16_rn(c.alpha * __uint_as_float(acc[j]));
+                if (tall) s_out[(q * 32 + j) * kPad + row] = b; else s_out[row * kPad + q * 32 + j] = b;
+            }
+        }
+        __syncthreads();
+        const int a0 = (tall ? tj : ti) * kTile, r0 = (tall ? ti : tj) * kTile;   // first row / column in the caller's
+        if (!s_failed) {
+            for (int a = warp; a < kTile && a0 + a < m.rows; a += kProductThreads / 32) {
+                __nv_bfloat16* to = out + m.offset + (int64_t)(a0 + a) * m.cols + r0;
+#pragma unroll
+                for (int k = 0; k < kTile / 32; ++k)
+                    if (r0 + k * 32 + lane < m.cols) to[k * 32 + lane] = s_out[a * kPad + k * 32 + lane];
+            }
+        }
+    }
+    fence_before_sync();
+    __syncthreads();
+    if (threadIdx.x == 0 && s_failed) atomicAdd(timeouts, 1);
+    if (warp == 0) tmem_free(tmem, kTile);
+}
+
+__device__ int g_timeouts;
+
+// ---------------------------------------------------------------------------------------------- host side
+
+static int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
+
+// Lays the matrices order[0..n) out in the workspace and numbers the CTAs of the passes.  Returns the bytes needed.
+static int64_t lay_out(const int64_t* offsets, const int64_t* rows, const int64_t* cols, const int* order, int n, Table* t) {
+    int64_t at = up(sizeof(Table), 1024);
+    int64_t chunks = 0, units = 0, sym = 0, apply = 0;
+    t->n = n;
+    for (int k = 0; k < n; ++k) {
+        Mat& m = t->m[k];
+        const int64_t r = rows[order[k]], c = cols[order[k]];
+        m.offset = offsets ? offsets[order[k]] : 0;
+        m.rows = (int)r;
+        m.cols = (int)c;
+        m.s = (int)std::min(r, c);
+        m.l = (int)std::max(r, c);
+        m.sp = (int)up(m.s, kTile);
+        m.lp = (int)up(m.l, kUnit);
+        t->chunk_at[k] = (int)chunks;
+        t->unit_at[k] = (int)units;
+        t->sym_at[k] = (int)sym;
+        t->apply_at[k] = (int)apply;
+        m.partial0 = (int)chunks;
+        m.n_chunks = (int)((r * c + kChunk - 1) / kChunk);
+        chunks += m.n_chunks;
+        units += (int64_t)(m.sp / kUnit) * (m.lp / kUnit);
+        const int64_t mt = m.sp / kTile;
+        sym += mt * (mt + 1) / 2;
+        apply += mt * ((m.lp + kTile - 1) / kTile);
+    }
+    t->chunk_at[n] = (int)chunks;
+    t->unit_at[n] = (int)units;
+    t->sym_at[n] = (int)sym;
+    t->apply_at[n] = (int)apply;
+    if (chunks > 0x7fffffff || units > 0x7fffffff || sym > 0x7fffffff || apply > 0x7fffffff) return -1;
+    at = up(at + chunks * 8, 1024);
+    at = up(at + n * 8, 1024);                                        // inverse norms, arrival counters
+    for (int k = 0; k < n; ++k) {
+        Mat& m = t->m[k];
+        const int64_t big = (int64_t)m.sp * m.lp * 2;
+        m.x_hi = at;
+        m.x_lo = at + big;
+        m.x_next = at + 2 * big;
+        m.small = at + 3 * big;
+        at = m.small + (int64_t)kSmallBuffers * m.sp * m.sp * 2;
+    }
+    return at;
+}
+
+// Larger matrices first, so that the last tiles of a launch are short ones; chunks of kMaxMats per chain.
+static std::vector<int> order_of(const int64_t* rows, const int64_t* cols, int n) {
+    std::vector<int> o;
+    for (int i = 0; i < n; ++i)
+        if (rows[i] > 0 && cols[i] > 0) o.push_back(i);
+    std::stable_sort(o.begin(), o.end(), [&](int x, int y) {
+        const int64_t sx = std::max(rows[x], cols[x]), sy = std::max(rows[y], cols[y]);
+        return sx > sy;
+    });
+    return o;
+}
+
+static int check_shapes(const int64_t* rows, const int64_t* cols, int n) {
+    if (n < 0) return SIDCO_E_PARAMS;
+    if (n > 0 && (!rows || !cols)) return SIDCO_E_NULL;
+    for (int i = 0; i < n; ++i) {
+        if (rows[i] < 0 || cols[i] < 0 || rows[i] > SIDCO_ORTHO_MAX_DIM || cols[i] > SIDCO_ORTHO_MAX_DIM) return SIDCO_E_SIZE;
+        if (std::min(rows[i], cols[i]) > SIDCO_ORTHO_MAX_SHORT) return SIDCO_E_SIZE;
+    }
+    return 0;
+}
+
+static int64_t workspace_bytes(const int64_t* rows, const int64_t* cols, int n) {
+    const std::vector<int> order = order_of(rows, cols, n);
+    std::vector<Table> t(1);
+    int64_t most = 0;
+    for (size_t from = 0; from < order.size(); from += kMaxMats) {
+        const int64_t b = lay_out(nullptr, rows, cols, order.data() + from, (int)std::min<size_t>(kMaxMats, order.size() - from),
+                                  t.data());
+        if (b < 0) return SIDCO_E_SIZE;
+        most = std::max(most, b);
+    }
+    return most;
+}
+
+template <typename... Args>
+static cudaError_t launch(void (*kernel)(Args...), dim3 grid, int threads, size_t smem, cudaStream_t s, Args... args) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, args...);
+    if (e == cudaSuccess) sidco_internal::note_launch();
+    return e;
+}
+
+template <typename T>
+static cudaError_t chain(const Table& t, const void* grad, float* momentum, float mu, int nesterov, int steps, float eps,
+                         uint16_t* out, uint8_t* ws, int* timeouts, cudaStream_t s) {
+    cudaError_t e;
+    int64_t at = up(sizeof(Table), 1024);
+    Table* table = reinterpret_cast<Table*>(ws);
+    double* partial = reinterpret_cast<double*>(ws + at);
+    at = up(at + (int64_t)t.chunk_at[t.n] * 8, 1024);
+    float* inv_norm = reinterpret_cast<float*>(ws + at);
+    int* arrived = reinterpret_cast<int*>(ws + at) + t.n;
+    if ((e = cudaMemsetAsync(arrived, 0, t.n * sizeof(int), s)) != cudaSuccess) return e;
+    // (a plain launch: the first kernel waits for everything before it)
+    momentum_kernel<T><<<t.chunk_at[t.n], 256, 0, s>>>(t, (const T*)grad, momentum, mu, nesterov, eps, partial, arrived,
+                                                       inv_norm);
+    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    sidco_internal::note_launch();
+    if ((e = launch(normalize_kernel<T>, dim3(t.unit_at[t.n]), 256, 0, s, t, (const T*)grad, (const float*)momentum, mu,
+                    nesterov, (const float*)inv_norm, ws, table)) != cudaSuccess)
+        return e;
+    const auto two = [](int k) { return ldexpf(1.0f, k); };
+    const auto sym = [&](const Chain& c, int products) {
+        return launch(product_kernel<true>, dim3(t.sym_at[t.n], products), kProductThreads, kProductSmem, s,
+                      (const Table*)table, ws, c, (__nv_bfloat16*)out, timeouts);
+    };
+    int done = 0, in = 0;
+    while (done < steps) {
+        const int group = steps == 1 || (done == 2 && steps % 2) ? 1 : 2;
+        Chain c{};
+        c.x_in = in;
+        c.parts = done ? 1 : 2;
+        in ^= 1;
+        int A = kBufA, A2 = kBufA2, P = kBufP, P2 = kBufP2, scale_p = kB;
+        c.p[0] = Product{-1, -1, -1, A, two(kA - 2 * kX), 0.0f, 0.0f};
+        if ((e = sym(c, 1)) != cudaSuccess) return e;
+        for (int i = 0; i < group; ++i) {
+            const int B = i == 0 ? P : (int)kBufB;
+            c.p[0] = Product{A, A, A, B, kCc * two(kB - 2 * kA), kCb * two(kB - kA), kCa * two(kB)};
+            if ((e = sym(c, 1)) != cudaSuccess) return e;
+            int n = 0;
+            const bool more = i + 1 < group;
+            if (more) c.p[n++] = Product{B, A, -1, kBufT, two(-kB), 0.0f, 0.0f};
+            if (i > 0) {
+                c.p[n++] = Product{B, P, -1, P2, two(kP - kB - scale_p), 0.0f, 0.0f};
+                std::swap(P, P2);
+                scale_p = kP;
+            }
+            if (n > 0 && (e = sym(c, n)) != cudaSuccess) return e;
+            if (more) {
+                c.p[0] = Product{kBufT, B, -1, A2, two(-kB), 0.0f, 0.0f};
+                if ((e = sym(c, 1)) != cudaSuccess) return e;
+                std::swap(A, A2);
+            }
+        }
+        done += group;
+        c.op = P;
+        c.last = done == steps;
+        c.alpha = c.last ? two(-scale_p - kX) : two(-scale_p);
+        if ((e = launch(product_kernel<false>, dim3(t.apply_at[t.n]), kProductThreads, kProductSmem, s, (const Table*)table,
+                        ws, c, (__nv_bfloat16*)out, timeouts)) != cudaSuccess)
+            return e;
+    }
+    return cudaSuccess;
+}
+
+}  // namespace sidco_ortho
+
+int sidco_internal::orthogonalize_timeouts(int* count) {
+    return (int)cudaMemcpyFromSymbol(count, sidco_ortho::g_timeouts, sizeof(int));
+}
+
+extern "C" {
+
+int64_t sidco_orthogonalize_workspace_bytes(const int64_t* rows, const int64_t* cols, int n_mats) {
+    const int rc = sidco_ortho::check_shapes(rows, cols, n_mats);
+    return rc ? rc : sidco_ortho::workspace_bytes(rows, cols, n_mats);
+}
+
+int sidco_orthogonalize(const void* grad, int grad_type, float* momentum, float mu, int nesterov, const int64_t* offsets,
+                        const int64_t* rows, const int64_t* cols, int n_mats, int steps, float eps, uint16_t* out_bf16,
+                        void* workspace, size_t workspace_bytes, void* stream) {
+    using namespace sidco_ortho;
+    int rc = check_shapes(rows, cols, n_mats);
+    if (rc) return rc;
+    if (grad_type < SIDCO_T_F32 || grad_type > SIDCO_T_F16) return SIDCO_E_TYPE;
+    if (steps < 1 || steps > SIDCO_ORTHO_MAX_STEPS || !(eps >= 0.0f) || !(mu >= 0.0f && mu < 1.0f)) return SIDCO_E_PARAMS;
+    const std::vector<int> order = order_of(rows, cols, n_mats);
+    if (order.empty()) return 0;
+    if (!grad || !out_bf16 || !offsets || !workspace) return SIDCO_E_NULL;
+    for (int i : order)
+        if (offsets[i] < 0) return SIDCO_E_SEGMENTS;
+    const uintptr_t size = grad_type == SIDCO_T_F32 ? 4 : 2;
+    if ((uintptr_t)grad % size || (uintptr_t)momentum % 4 || (uintptr_t)out_bf16 % 2) return SIDCO_E_ALIGN;
+    const int64_t need = sidco_ortho::workspace_bytes(rows, cols, n_mats);
+    if (need < 0) return (int)need;
+    if ((uintptr_t)workspace % 256 || workspace_bytes < (size_t)need) return SIDCO_E_WORKSPACE;
+    static bool ready[64] = {};
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return (int)e;
+    if (dev < 0 || dev >= 64) return SIDCO_E_SIZE;
+    if (!ready[dev]) {                       // (setting it twice from two threads is harmless)
+        if ((e = cudaFuncSetAttribute(product_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kProductSmem)) !=
+                cudaSuccess ||
+            (e = cudaFuncSetAttribute(product_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kProductSmem)) !=
+                cudaSuccess)
+            return (int)e;
+        ready[dev] = true;
+    }
+    int* timeouts = nullptr;
+    if ((e = cudaGetSymbolAddress((void**)&timeouts, g_timeouts)) != cudaSuccess) return (int)e;
+    std::vector<Table> t(1);
+    for (size_t from = 0; from < order.size(); from += kMaxMats) {
+        lay_out(offsets, rows, cols, order.data() + from, (int)std::min<size_t>(kMaxMats, order.size() - from), t.data());
+        uint8_t* ws = (uint8_t*)workspace;
+        cudaStream_t s = (cudaStream_t)stream;
+        if (grad_type == SIDCO_T_F32)
+            e = chain<float>(t[0], grad, momentum, mu, nesterov, steps, eps, out_bf16, ws, timeouts, s);
+        else if (grad_type == SIDCO_T_BF16)
+            e = chain<__nv_bfloat16>(t[0], grad, momentum, mu, nesterov, steps, eps, out_bf16, ws, timeouts, s);
+        else
+            e = chain<__half>(t[0], grad, momentum, mu, nesterov, steps, eps, out_bf16, ws, timeouts, s);
+        if (e != cudaSuccess) return (int)e;
+    }
+    return 0;
+}
+
+}  // extern "C"

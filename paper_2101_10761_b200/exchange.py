@@ -47,3 +47,19 @@ def gather_sparse(out_idx: torch.Tensor, out_val: torch.Tensor, k_hat: int, grou
     else:
         idx_all, val_all = pad_idx, pad_val
     return idx_all, val_all, counts, stride
+
+
+def gather_mx4(codes: torch.Tensor, scales: torch.Tensor, group=None) -> Tuple[torch.Tensor, torch.Tensor, int]:
+    """All-gather this worker's 4-bit gradient (``sidco_mx4_compress``).
+
+    Returns (codes_all, scales_all, n_workers) as ``sidco_mx4_mean`` takes them, worker n's part at n times this
+    worker's size.  All workers have vectors of one length, so nothing is counted or padded."""
+    import torch.distributed as dist
+    world = dist.get_world_size(group) if dist.is_available() and dist.is_initialized() else 1
+    if world == 1:
+        return codes, scales, 1
+    codes_all = torch.empty(world * codes.numel(), dtype=torch.uint8, device=codes.device)
+    scales_all = torch.empty(world * scales.numel(), dtype=torch.uint8, device=scales.device)
+    dist.all_gather_into_tensor(codes_all, codes, group=group)
+    dist.all_gather_into_tensor(scales_all, scales, group=group)
+    return codes_all, scales_all, world
