@@ -151,9 +151,7 @@ def lib() -> C.CDLL:
 
 def _ptr(x) -> Optional[int]:
     """Raw address of a torch tensor, a numpy array or an int; None stays NULL."""
-    if x is None:
-        return None
-    if isinstance(x, int):
+    if x is None or isinstance(x, int):
         return x
     if isinstance(x, np.ndarray):
         return x.ctypes.data
@@ -165,10 +163,25 @@ def _offsets(seg_offsets: Sequence[int]):
     return arr, arr.ctypes.data_as(C.POINTER(C.c_int64)), int(arr.size - 1)
 
 
+_current = None
+
+
+def _current_stream() -> int:
+    """torch's current stream as a raw handle (looked up without building a Stream object where torch allows it)."""
+    global _current
+    if _current is None:
+        import torch
+        raw, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
+        if raw is None or device is None:
+            return torch.cuda.current_stream().cuda_stream
+        torch.cuda.current_stream()                          # initialises CUDA
+        _current = lambda: raw(device())                     # noqa: E731
+    return _current()
+
+
 def _stream(stream) -> Optional[int]:
     if stream is None:
-        import torch
-        return torch.cuda.current_stream().cuda_stream
+        return _current_stream()
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -384,15 +397,20 @@ def sidco_reset_state_async(residual, stream=None) -> None:
 T_F32, T_BF16, T_F16 = 0, 1, 2
 ORTHO_MAX_DIM, ORTHO_MAX_SHORT, ORTHO_MAX_STEPS = 4194304, 16384, 32
 _TYPES = {"torch.float32": T_F32, "torch.bfloat16": T_BF16, "torch.float16": T_F16, "float32": T_F32, "float16": T_F16}
+_seen_types = {}
 
 
 def _type(x, given: Optional[int]) -> int:
     """The SIDCO_T_* code of a tensor or array; raw addresses need `given`."""
     if given is not None:
         return given
-    code = _TYPES.get(str(getattr(x, "dtype", None)))
+    dtype = getattr(x, "dtype", None)
+    code = _seen_types.get(dtype)
     if code is None:
-        raise SidcoError(-13, "element type %s:" % getattr(x, "dtype", "of a raw address"))
+        code = _TYPES.get(str(dtype))
+        if code is None:
+            raise SidcoError(-13, "element type %s:" % ("of a raw address" if dtype is None else dtype))
+        _seen_types[dtype] = code
     return code
 
 

@@ -27,44 +27,61 @@ template <> __device__ __forceinline__ float narrow<float>(float x) { return x; 
 template <> __device__ __forceinline__ __nv_bfloat16 narrow<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
 template <> __device__ __forceinline__ __half narrow<__half>(float x) { return __float2half_rn(x); }
 
-// Eight neighbours as loaded: 16 or 32 bytes.
-template <typename T> struct Raw { uint4 w[sizeof(T) / 2]; };
+// Eight neighbours in accesses of W bytes (the widest that the addresses allow: see width_of): 32-byte accesses of fp32
+// move whole sectors per lane, two 16-byte ones half a sector each.
+template <int W> struct Word;
+template <> struct Word<2> { using type = uint16_t; };
+template <> struct Word<4> { using type = uint32_t; };
+template <> struct Word<8> { using type = uint2; };
+template <> struct Word<16> { using type = uint4; };
 
-template <typename T>
-__device__ __forceinline__ Raw<T> load_raw(const T* p) {
-    Raw<T> r;
+template <typename T, int W>
+__device__ __forceinline__ void move_in(const T* p, uint32_t* w) {
+    if constexpr (W == 32) {
+        asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                     : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
+                     : "l"(p));
+    } else {
+        using V = typename Word<W>::type;
 #pragma unroll
-    for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.w[i] = __ldcs(reinterpret_cast<const uint4*>(p) + i);
-    return r;
+        for (int i = 0; i < (int)sizeof(T) * 8 / W; ++i) reinterpret_cast<V*>(w)[i] = reinterpret_cast<const V*>(p)[i];
+    }
 }
 
-template <typename T>
-__device__ __forceinline__ void unpack(const Raw<T>& r, float (&x)[8]) {
-    const T* t = reinterpret_cast<const T*>(r.w);
+template <typename T, int W>
+__device__ __forceinline__ void move_out(T* p, const uint32_t* w) {
+    if constexpr (W == 32) {
+        asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]),
+                     "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                     : "memory");
+    } else {
+        using V = typename Word<W>::type;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = widen(t[i]);
+        for (int i = 0; i < (int)sizeof(T) * 8 / W; ++i) reinterpret_cast<V*>(p)[i] = reinterpret_cast<const V*>(w)[i];
+    }
 }
 
 // The first n of eight neighbours, zeros behind them.
-template <typename T, bool Vec>
+template <typename T, int W>
 __device__ __forceinline__ void load8(const T* p, int n, float (&x)[8]) {
-    if (Vec && n >= 8) {
-        unpack<T>(load_raw(p), x);
+    if (n >= 8) {
+        alignas(16) uint32_t w[2 * sizeof(T)];
+        move_in<T, W>(p, w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = widen(reinterpret_cast<const T*>(w)[i]);
         return;
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = i < n ? widen(p[i]) : 0.0f;
 }
 
-template <typename T, bool Vec>
+template <typename T, int W>
 __device__ __forceinline__ void store8(T* p, int n, const float (&x)[8]) {
-    if (Vec && n >= 8) {
-        alignas(16) T t[8];
+    if (n >= 8) {
+        alignas(16) uint32_t w[2 * sizeof(T)];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) t[i] = narrow<T>(x[i]);
-#pragma unroll
-        for (int i = 0; i < (int)sizeof(T) / 2; ++i)
-            reinterpret_cast<uint4*>(p)[i] = reinterpret_cast<const uint4*>(t)[i];
+        for (int i = 0; i < 8; ++i) reinterpret_cast<T*>(w)[i] = narrow<T>(x[i]);
+        move_out<T, W>(p, w);
         return;
     }
 #pragma unroll
@@ -108,7 +125,7 @@ struct QuantArgs {
 // shared memory, where one thread then reads 32 elements of a column.  A row of the tile starts 8 words later in
 // every group of 32 rows, so that the lanes of a warp (8 columns x 4 groups) read from 32 different banks and write
 // 64 neighbouring bytes of a column's codes.
-template <typename T, bool Vec>
+template <typename T, int W>
 __global__ void __launch_bounds__(kQuantThreads) quantize_kernel(const QuantArgs A) {
     extern __shared__ float s_x[];                                   // [128][128], skewed; only with codes_t
     __shared__ __align__(16) uint8_t s_scale[kTileBytes];
@@ -122,7 +139,7 @@ __global__ void __launch_bounds__(kQuantThreads) quantize_kernel(const QuantArgs
     for (int p = 0; p < 4; ++p) {
         const int64_t r = r0 + p * 32 + warp * 2 + (lane >> 4);
         const bool in = r < A.rows && left > 0;
-        load8<T, Vec>(in ? (const T*)A.x + r * A.ld + c : (const T*)A.x, in ? left : 0, x[p]);
+        load8<T, W>(in ? (const T*)A.x + r * A.ld + c : (const T*)A.x, in ? left : 0, x[p]);
     }
     if (A.codes_t) {
 #pragma unroll
@@ -175,7 +192,7 @@ __global__ void __launch_bounds__(kQuantThreads) quantize_kernel(const QuantArgs
 }
 
 // A lane reads one word of codes and writes eight values.
-template <typename T, bool Vec>
+template <typename T, int W>
 __global__ void __launch_bounds__(256) dequantize_kernel(const uint8_t* __restrict__ codes,
                                                          const uint8_t* __restrict__ scales, int64_t rows, int64_t cols,
                                                          int64_t pitch, int64_t ktiles, T* __restrict__ out, int64_t ld,
@@ -191,12 +208,12 @@ __global__ void __launch_bounds__(256) dequantize_kernel(const uint8_t* __restri
     const float s = scale_of(byte);
 #pragma unroll
     for (int k = 0; k < 8; ++k) v[k] *= s;
-    store8<T, Vec>(out + r * ld + o * 8, (int)min((int64_t)8, cols - o * 8), v);
+    store8<T, W>(out + r * ld + o * 8, (int)min((int64_t)8, cols - o * 8), v);
 }
 
 // ------------------------------------------------------------------------------------------------ flat vectors
 
-template <typename T, bool Vec, int U>
+template <typename T, int W, int WR, int U>
 __global__ void __launch_bounds__(256) compress_kernel(const T* __restrict__ grad, float* __restrict__ residual,
                                                        int64_t d, uint8_t* __restrict__ codes,
                                                        uint8_t* __restrict__ scales) {
@@ -207,8 +224,8 @@ __global__ void __launch_bounds__(256) compress_kernel(const T* __restrict__ gra
     for (int u = 0; u < U; ++u) {
         const int64_t at = (first + u * 256) * 8;
         const int n = (int)max((int64_t)0, min((int64_t)8, d - at));
-        load8<T, Vec>(n ? grad + at : grad, n, g[u]);
-        load8<float, Vec>(n ? residual + at : residual, n, r[u]);
+        load8<T, W>(n ? grad + at : grad, n, g[u]);
+        load8<float, WR>(n ? residual + at : residual, n, r[u]);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -226,43 +243,48 @@ __global__ void __launch_bounds__(256) compress_kernel(const T* __restrict__ gra
 #pragma unroll
         for (int k = 0; k < 8; ++k) g[u][k] = fmaf(-v[k], s, g[u][k]);   // v s is exact: one rounding
         const int n = (int)max((int64_t)0, min((int64_t)8, d - at));
-        if (n) store8<float, Vec>(residual + at, n, g[u]);
+        if (n) store8<float, WR>(residual + at, n, g[u]);
     }
 }
 
-// The workers are added in their order, in fp32 (a decoded value has two significant bits), then scaled by 1/N.
-template <bool Vec>
+// The workers are added in their order, in fp32 (a decoded value has two significant bits), then scaled by 1/N.  A thread
+// takes U octets and loads the codes of A workers before it uses any.
+template <int W, int A, int U>
 __global__ void __launch_bounds__(256) mean_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
                                                    int n_workers, int64_t d, float* __restrict__ out) {
-    const int64_t nb = blocks_of(d), o = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t at = o * 8;
-    if (at >= d) return;
-    float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    const uint8_t* cp = codes + o * 4;
-    const uint8_t* sp = scales + (o >> 2);
-    constexpr int kAhead = 8;
-    for (int w0 = 0; w0 < n_workers; w0 += kAhead) {
-        uint32_t c[kAhead], b[kAhead];
+    const int64_t nb = blocks_of(d), first = (int64_t)blockIdx.x * (256 * U) + threadIdx.x;
+    float sum[U][8] = {};
+    for (int w0 = 0; w0 < n_workers; w0 += A) {
+        uint32_t c[A][U], b[A][U];
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            const bool on = w0 + i < n_workers;
-            c[i] = on ? *reinterpret_cast<const uint32_t*>(cp + (int64_t)(w0 + i) * nb * 16) : 0u;
-            b[i] = on ? sp[(int64_t)(w0 + i) * nb] : 0u;
-        }
+        for (int i = 0; i < A; ++i)
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            if (w0 + i >= n_workers) break;
-            float v[8];
-            decode8(c[i], v);
-            const float s = scale_of(b[i]);
+            for (int u = 0; u < U; ++u) {
+                const int64_t o = first + u * 256;
+                const bool on = w0 + i < n_workers && o < nb * 4;
+                c[i][u] = on ? *reinterpret_cast<const uint32_t*>(codes + (w0 + i) * nb * 16 + o * 4) : 0u;
+                b[i][u] = on ? scales[(w0 + i) * nb + (o >> 2)] : 0u;
+            }
 #pragma unroll
-            for (int k = 0; k < 8; ++k) sum[k] = fmaf(v[k], s, sum[k]);
-        }
+        for (int i = 0; i < A; ++i)
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                float v[8];
+                decode8(c[i][u], v);
+                const float s = scale_of(b[i][u]);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) sum[u][k] = fmaf(v[k], s, sum[u][k]);   // (+ 0 behind the last worker)
+            }
     }
     const float inv = 1.0f / (float)n_workers;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) sum[k] *= inv;
-    store8<float, Vec>(out + at, (int)min((int64_t)8, d - at), sum);
+    for (int u = 0; u < U; ++u) {
+        const int64_t at = (first + u * 256) * 8;
+        if (at >= d) break;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sum[u][k] *= inv;
+        store8<float, W>(out + at, (int)min((int64_t)8, d - at), sum[u]);
+    }
 }
 
 // ------------------------------------------------------------------------------------------------ host side
@@ -275,7 +297,14 @@ static int finish(cudaError_t e) {
     return 0;
 }
 
-template <typename T, bool Vec>
+// Widest access (at most `most` bytes) with which every row of 8-element groups can be moved.
+static int width_of(const void* p, int64_t row_bytes, int most, int element) {
+    int w = most;
+    while (w > element && (!aligned(p, w) || row_bytes % w)) w /= 2;
+    return w;
+}
+
+template <typename T, int W>
 static int launch_quantize(const QuantArgs& a, int64_t grid, cudaStream_t s) {
     static bool sized[64] = {};
     const size_t smem = a.codes_t ? (kTile * kTile + 32) * sizeof(float) : 0;
@@ -284,19 +313,22 @@ static int launch_quantize(const QuantArgs& a, int64_t grid, cudaStream_t s) {
     if (e != cudaSuccess) return (int)e;
     if (dev < 0 || dev >= 64) return SIDCO_E_SIZE;
     if (!sized[dev]) {                      // (setting it twice from two threads is harmless)
-        e = cudaFuncSetAttribute(quantize_kernel<T, Vec>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+        e = cudaFuncSetAttribute(quantize_kernel<T, W>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                  (int)((kTile * kTile + 32) * sizeof(float)));
         if (e != cudaSuccess) return (int)e;
         sized[dev] = true;
     }
-    quantize_kernel<T, Vec><<<(unsigned)grid, kQuantThreads, smem, s>>>(a);
+    quantize_kernel<T, W><<<(unsigned)grid, kQuantThreads, smem, s>>>(a);
     return finish(cudaGetLastError());
 }
 
 template <typename T>
 static int quantize_typed(const QuantArgs& a, int64_t grid, cudaStream_t s) {
-    const bool vec = aligned(a.x, 16) && a.ld * sizeof(T) % 16 == 0;
-    return vec ? launch_quantize<T, true>(a, grid, s) : launch_quantize<T, false>(a, grid, s);
+    switch (width_of(a.x, a.ld * sizeof(T), 16, sizeof(T))) {
+        case 16: return launch_quantize<T, 16>(a, grid, s);
+        case 8: return launch_quantize<T, 8>(a, grid, s);
+        default: return launch_quantize<T, sizeof(T)>(a, grid, s);
+    }
 }
 
 template <typename T>
@@ -305,21 +337,25 @@ static int dequantize_typed(const uint8_t* codes, const uint8_t* scales, int64_t
     const int64_t octs = (cols + 7) / 8, pitch = blocks_of(cols) * 16, ktiles = (blocks_of(cols) + 3) / 4;
     const int64_t grid = (rows * octs + 255) / 256;
     if (grid > 0x7fffffff) return SIDCO_E_SIZE;
-    if (aligned(out, 16) && ld * sizeof(T) % 16 == 0)
-        dequantize_kernel<T, true><<<(unsigned)grid, 256, 0, s>>>(codes, scales, rows, cols, pitch, ktiles, (T*)out, ld, octs);
-    else
-        dequantize_kernel<T, false><<<(unsigned)grid, 256, 0, s>>>(codes, scales, rows, cols, pitch, ktiles, (T*)out, ld, octs);
-    return finish(cudaGetLastError());
+    const auto go = [&](auto kernel) {
+        kernel<<<(unsigned)grid, 256, 0, s>>>(codes, scales, rows, cols, pitch, ktiles, (T*)out, ld, octs);
+        return finish(cudaGetLastError());
+    };
+    switch (width_of(out, ld * sizeof(T), 16, sizeof(T))) {
+        case 16: return go(dequantize_kernel<T, 16>);
+        case 8: return go(dequantize_kernel<T, 8>);
+        default: return go(dequantize_kernel<T, sizeof(T)>);
+    }
 }
 
 template <typename T>
 static int compress_typed(const void* grad, float* residual, int64_t d, uint8_t* codes, uint8_t* scales, cudaStream_t s) {
-    constexpr int U = 2;
+    constexpr int U = 2, kMost = sizeof(T) * 8, kLeast = sizeof(T);
     const int64_t grid = (blocks_of(d) * 4 + 256 * U - 1) / (256 * U);
-    if (aligned(grad, 16) && aligned(residual, 16))
-        compress_kernel<T, true, U><<<(unsigned)grid, 256, 0, s>>>((const T*)grad, residual, d, codes, scales);
+    if (aligned(grad, kMost) && aligned(residual, 32))
+        compress_kernel<T, kMost, 32, U><<<(unsigned)grid, 256, 0, s>>>((const T*)grad, residual, d, codes, scales);
     else
-        compress_kernel<T, false, U><<<(unsigned)grid, 256, 0, s>>>((const T*)grad, residual, d, codes, scales);
+        compress_kernel<T, kLeast, 4, U><<<(unsigned)grid, 256, 0, s>>>((const T*)grad, residual, d, codes, scales);
     return finish(cudaGetLastError());
 }
 
@@ -401,11 +437,13 @@ int sidco_mx4_mean(const uint8_t* codes_all, const uint8_t* scales_all, int n_wo
     if (!codes_all || !scales_all || !out_dense) return SIDCO_E_NULL;
     if (!aligned(codes_all, 16) || !aligned(out_dense, 4)) return SIDCO_E_ALIGN;
     cudaStream_t s = (cudaStream_t)stream;
-    const int64_t grid = ((d + 7) / 8 + 255) / 256;
-    if (aligned(out_dense, 16))
-        mean_kernel<true><<<(unsigned)grid, 256, 0, s>>>(codes_all, scales_all, n_workers, d, out_dense);
-    else
-        mean_kernel<false><<<(unsigned)grid, 256, 0, s>>>(codes_all, scales_all, n_workers, d, out_dense);
+    const auto go = [&](auto kernel, int octs) {
+        kernel<<<(unsigned)((blocks_of(d) * 4 + 256 * octs - 1) / (256 * octs)), 256, 0, s>>>(codes_all, scales_all, n_workers,
+                                                                                            d, out_dense);
+    };
+    if (!aligned(out_dense, 32)) go(mean_kernel<4, 4, 1>, 1);
+    else if (n_workers == 1) go(mean_kernel<32, 1, 2>, 2);
+    else go(mean_kernel<32, 4, 2>, 2);
     return finish(cudaGetLastError());
 }
 
