@@ -1,10 +1,18 @@
 // Shared by the translation units of the library; not part of the C ABI.
 #pragma once
 
+#include <cuda.h>
+#include <stdint.h>
+
 namespace sidco_internal {
 
 // Count one kernel launch towards sidco_launch_count().
 void note_launch();
+
+// Tensor map over `rows` rows of `width` bytes, `pitch` bytes apart; boxes of box_width bytes (with or without the 128-byte
+// swizzle) x box_rows rows, zeros outside.  False if the driver has no such call or refuses the arguments.
+bool byte_map(CUtensorMap* map, const void* base, int64_t width, int64_t rows, int64_t pitch, int box_width, int box_rows,
+              bool swizzle);
 
 // How many CTAs of the product kernels gave up a bounded wait on the current device (synchronises it).
 int orthogonalize_timeouts(int* count);

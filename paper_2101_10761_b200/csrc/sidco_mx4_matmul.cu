@@ -155,6 +155,16 @@ __global__ void __launch_bounds__(kThreads, 2) matmul_kernel(const __grid_consta
 
 // ---------------------------------------------------------------------------------------------- host side
 
+// Codes: boxes of 128 bytes x `box` rows, swizzled, zeros outside.
+static bool code_map(CUtensorMap* map, const uint8_t* codes, int64_t rows, int64_t k, int box) {
+    const int64_t pitch = blocks_of(k) * 16;
+    return sidco_internal::byte_map(map, codes, pitch, rows, pitch, 128, box, true);
+}
+
+}  // namespace sidco_mx4mm
+
+namespace {
+
 using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
                             const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
                             CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -171,17 +181,17 @@ static Encode encoder() {
     return f;
 }
 
-// Codes as bytes: boxes of 128 bytes x `box` rows, swizzled, zeros outside.
-static bool code_map(CUtensorMap* map, const uint8_t* codes, int64_t rows, int64_t k, int box) {
-    const cuuint64_t pitch = (cuuint64_t)blocks_of(k) * 16;
-    const cuuint64_t dims[2] = {pitch, (cuuint64_t)rows}, strides[1] = {pitch};
-    const cuuint32_t boxes[2] = {128, (cuuint32_t)box}, steps[2] = {1, 1};
-    return encoder()(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, (void*)codes, dims, strides, boxes, steps,
-                     CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
+}  // namespace
 
-}  // namespace sidco_mx4mm
+bool sidco_internal::byte_map(CUtensorMap* map, const void* base, int64_t width, int64_t rows, int64_t pitch, int box_width,
+                              int box_rows, bool swizzle) {
+    if (!encoder()) return false;
+    const cuuint64_t dims[2] = {(cuuint64_t)width, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)pitch};
+    const cuuint32_t boxes[2] = {(cuuint32_t)box_width, (cuuint32_t)box_rows}, steps[2] = {1, 1};
+    return encoder()(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, boxes, steps,
+                     CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
+                     CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
 
 int sidco_internal::mx4_matmul_timeouts(int* count) {
     return (int)cudaMemcpyFromSymbol(count, sidco_mx4mm::g_timeouts, sizeof(int));
@@ -214,7 +224,6 @@ int sidco_mx4_matmul(const uint8_t* a_codes, const uint8_t* a_scales, const uint
     if ((e = cudaGetDevice(&dev)) != cudaSuccess) return (int)e;
     if (dev < 0 || dev >= 64) return SIDCO_E_SIZE;
     if (!ready[dev]) {                       // (setting it twice from two threads is harmless)
-        if (!encoder()) return SIDCO_E_UNSUPPORTED;
         if ((e = cudaFuncSetAttribute(matmul_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem)) != cudaSuccess)
             return (int)e;
         ready[dev] = true;

@@ -20,6 +20,7 @@
 // Workspace matrices are stored as units of 64 x 64 fp16 in the 128-byte-swizzled image that the tensor cores read, so
 // that a stage of operands is one or two contiguous bulk copies, the same unit serves as K-major operand (Gram) and as
 // MN-major operand (application), and nothing depends on the caller's alignment.
+#include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -48,6 +49,7 @@ constexpr int kUnit = 64;             // units of 64 x 64
 constexpr int kUnitBytes = kUnit * kUnit * 2;
 constexpr int kMaxMats = 128;         // matrices of one chain of launches
 constexpr int kChunk = 16384;         // elements of a matrix per CTA of the momentum pass
+constexpr int kPairTile = 256;
 
 enum Buffer { kBufA, kBufA2, kBufB, kBufT, kBufP, kBufP2, kSmallBuffers };
 
@@ -56,7 +58,7 @@ struct Mat {
     int64_t x_hi, x_lo, x_next;       // bytes into the workspace: s x l matrices
     int64_t small;                    // first of the s x s matrices
     int rows, cols, s, l;
-    int sp, lp;                       // s to a multiple of 128, l to a multiple of 64
+    int sp, lp;                       // s to a multiple of 128 (256: pair tiles), l to a multiple of 64
     int partial0, n_chunks;           // partial sums of squares
 };
 
@@ -66,7 +68,20 @@ struct Table {
     int unit_at[kMaxMats + 1];        // normalisation,
     int sym_at[kMaxMats + 1];         // symmetric products,
     int apply_at[kMaxMats + 1];       // applications
+    int n_pair;                       // the first matrices go through pair tiles:
+    int pair_sym_at[kMaxMats + 1];
+    int pair_apply_at[kMaxMats + 1];
+    int64_t tiles;                    // bytes into the workspace: Tile[], symmetric products, then applications
     Mat m[kMaxMats];
+};
+
+// A 256 x 256 tile of a pair of CTAs; matrices in units from the start of the workspace.
+struct __align__(16) Tile {
+    int x_hi, x_lo, x_next, small;
+    int spu, ku;                      // units along the padded s, along s
+    int lu;                           // units along l
+    uint16_t ti, tj;                  // row, column
+    int mat, pad[3];
 };
 
 __device__ __forceinline__ int find(const int* at, int n, int i) {
@@ -147,6 +162,15 @@ __global__ void __launch_bounds__(256) momentum_kernel(const __grid_constant__ T
     }
 }
 
+// Tile `i` of the lower triangle, row by row.
+__device__ __forceinline__ void triangle(int i, uint16_t* row, uint16_t* col) {
+    int r = (int)((sqrtf(8.0f * i + 1.0f) - 1.0f) * 0.5f);
+    while ((r + 1) * (r + 2) / 2 <= i) ++r;
+    while (r * (r + 1) / 2 > i) --r;
+    *row = (uint16_t)r;
+    *col = (uint16_t)(i - r * (r + 1) / 2);
+}
+
 // Eight neighbours of a row of a unit: where they lie in the swizzled image.
 __device__ __forceinline__ int in_unit(int r, int c8) { return r * 128 + ((c8 ^ (r & 7)) << 4); }
 
@@ -178,6 +202,31 @@ __global__ void __launch_bounds__(256) normalize_kernel(const __grid_constant__ 
     if (blockIdx.x == 0)
         for (int w = threadIdx.x; w < (int)(sizeof(Table) / 4); w += 256)
             reinterpret_cast<int*>(table_out)[w] = reinterpret_cast<const int*>(&t)[w];
+    const int n_sym = t.pair_sym_at[t.n_pair], n_apply = t.pair_apply_at[t.n_pair];
+    for (int w = blockIdx.x * 256 + threadIdx.x; w < n_sym + n_apply; w += gridDim.x * 256) {
+        const bool sym = w < n_sym;
+        const int k = sym ? w : w - n_sym;
+        const int* at = sym ? t.pair_sym_at : t.pair_apply_at;
+        const int j = find(at, t.n_pair, k), tile = k - at[j];
+        const Mat& q = t.m[j];
+        Tile d{};
+        d.x_hi = (int)(q.x_hi / kUnitBytes);
+        d.x_lo = (int)(q.x_lo / kUnitBytes);
+        d.x_next = (int)(q.x_next / kUnitBytes);
+        d.small = (int)(q.small / kUnitBytes);
+        d.spu = q.sp / kUnit;
+        d.ku = (q.s + kUnit - 1) / kUnit;
+        d.lu = q.lp / kUnit;
+        d.mat = j;
+        if (sym) {
+            triangle(tile, &d.ti, &d.tj);
+        } else {
+            const int mt = q.sp / kPairTile;
+            d.ti = (uint16_t)(tile % mt);
+            d.tj = (uint16_t)(tile / mt);
+        }
+        reinterpret_cast<Tile*>(ws + t.tiles)[w] = d;
+    }
     const float inv = __ldcg(inv_norm + i);
     // neighbours along the matrix's own rows: X's columns, or X's rows if tall
     const int along = threadIdx.x & 63, across0 = threadIdx.x >> 6;
@@ -286,10 +335,10 @@ __global__ void __launch_bounds__(kProductThreads, 2) product_kernel(const Table
     int steps;                                                        // K in units of 64
     bool gram = false;
     if (kSym) {
-        ti = (int)((sqrtf(8.0f * tile + 1.0f) - 1.0f) * 0.5f);        // lower triangle, row by row
-        while ((ti + 1) * (ti + 2) / 2 <= tile) ++ti;
-        while (ti * (ti + 1) / 2 > tile) --ti;
-        tj = tile - ti * (ti + 1) / 2;
+        uint16_t r16, c16;
+        triangle(tile, &r16, &c16);
+        ti = r16;
+        tj = c16;
         gram = p.left < 0;
         left = gram ? x_in : ws + m.small + p.left * small_bytes;
         right = gram ? x_in : ws + m.small + p.right * small_bytes;
@@ -353,6 +402,7 @@ __global__ void __launch_bounds__(kProductThreads, 2) product_kernel(const Table
     const bool mirror = kSym && ti != tj;
     if (kSym) {
         const uint8_t* plus = p.plus >= 0 ? ws + m.small + p.plus * small_bytes : nullptr;
+        const float gamma = ti == tj ? p.gamma : 0.0f;
 #pragma unroll 1
         for (int q = 0; q < kTile / 32; ++q) {
             uint32_t acc[32];
@@ -374,12 +424,8 @@ __global__ void __launch_bounds__(kProductThreads, 2) product_kernel(const Table
                         v[2 * j + 1] = fmaf(p.beta, f.y, v[2 * j + 1]);
                     }
                 }
-                if (ti == tj) {
-                    const int d = row - (q * 32 + o * 8);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        if (d == j) v[j] += p.gamma;
-                }
+                for (int j = 0; j < 8; ++j) v[j] += row == q * 32 + o * 8 + j ? gamma : 0.0f;
                 *reinterpret_cast<uint4*>(smem + (cu * 2 + (row >> 6)) * kUnitBytes + in_unit(row & 63, c8)) = pack8(v);
                 if (mirror) {
 #pragma unroll
@@ -460,6 +506,267 @@ __global__ void __launch_bounds__(kProductThreads, 2) product_kernel(const Table
     if (warp == 0) tmem_free(tmem, kTile);
 }
 
+// ---------------------------------------------------------------------------------------------- pair tiles
+//
+// Matrices with s > 128: 256 x 256 tiles, each by a cluster of two CTAs on two SMs (one tcgen05 product over both: every
+// operand byte is loaded once per pair, which halves the L2 traffic of 128 x 128 tiles).  Persistent: a pair takes tiles
+// in turn, and its two sets of sums in tensor memory let the end of a tile run under the products of the next.
+//   warp 0     feeds the stages (each CTA its half of the rows of A and of B)
+//   warp 1     issues the products (first CTA)
+//   warps 2-5  take the sums out, a quarter of the CTA's 128 rows each
+
+constexpr int kPairStages = 5;
+constexpr int kPairStageBytes = 4 * kUnitBytes;                       // per CTA: 128 x 64 of A and of B
+constexpr int kOutBytes = 4 * kUnitBytes;                             // 64 columns: the images of a tile part and its mirror
+constexpr int kPairThreads = 192;
+constexpr int kPairSmem = kPairStages * kPairStageBytes + 2 * kOutBytes + 1024;
+
+struct PairWork {
+    const Tile* tiles;
+    int n;                            // tiles of one product
+    int products;
+};
+
+__device__ __forceinline__ void epilogue_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
+
+template <bool kSym>
+__global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2)
+    pair_kernel(const __grid_constant__ CUtensorMap map, const PairWork w, const Table* t, uint8_t* ws,
+                const __grid_constant__ Chain c, __nv_bfloat16* __restrict__ out, int* timeouts) {
+    extern __shared__ uint8_t s_raw[];
+    __shared__ uint64_t s_full[kPairStages], s_free[kPairStages], s_sums[2], s_taken[2];
+    __shared__ uint32_t s_tmem;
+    __shared__ int s_failed;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_rank();
+    uint8_t* smem = (uint8_t*)(((uintptr_t)s_raw + 1023) & ~(uintptr_t)1023);
+    const uint32_t stage0 = smem_addr(smem);
+    if (warp == 1) tmem_alloc_pair(&s_tmem, 512);
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kPairStages; ++i) {
+            mbar_init(smem_addr(&s_full[i]), 1);
+            mbar_init(smem_addr(&s_free[i]), 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(smem_addr(&s_sums[i]), 1);
+            mbar_init(smem_addr(&s_taken[i]), 8);                     // four warps of both CTAs
+        }
+        s_failed = 0;
+        mbar_init_fence();
+    }
+    fence_before_sync();
+    __syncthreads();
+    cluster_sync();
+    fence_after_sync();
+    const uint32_t tmem = s_tmem;
+    wait_prerequisites();
+    launch_dependents();                 // (behind the wait: then all but the kernel before it are done when one starts)
+
+    const int n_pairs = gridDim.x / 2, first = blockIdx.x / 2, total = w.n * w.products;
+    const auto steps_of = [&](const Tile& d, const Product& p) {
+        return kSym ? (p.left < 0 ? d.lu : d.ku) : d.ku * c.parts;
+    };
+    if (warp == 0) {
+        if (lane == 0) {
+            int st = 0;
+            uint32_t round = 0;
+            bool ok = true;
+            for (int i = first; i < total && ok; i += n_pairs) {
+                const Tile d = w.tiles[i % w.n];
+                const Product& p = c.p[kSym ? i / w.n : 0];
+                const int steps = steps_of(d, p), small = d.spu * d.spu;
+                const int x_in = c.x_in ? d.x_next : d.x_hi;
+                const int left = !kSym ? d.small + c.op * small : p.left < 0 ? x_in : d.small + p.left * small;
+                const int right = !kSym || p.left < 0 ? x_in : d.small + p.right * small;
+                for (int k = 0; k < steps; ++k) {
+                    const uint32_t a = stage0 + st * kPairStageBytes, b = a + 2 * kUnitBytes, bar = smem_addr(&s_full[st]);
+                    ok = mbar_wait(smem_addr(&s_free[st]), (round & 1) ^ 1, &s_failed);
+                    if (!ok) break;
+                    if (rank == 0) mbar_expect_tx(bar, 2 * kPairStageBytes);
+                    const int kb = kSym || k < d.ku ? k : k - d.ku;
+                    const int ua = left + kb * d.spu + d.ti * 4 + rank * 2;
+                    tensor_load_2d_pair(a, &map, 0, ua * kUnit, bar);
+                    tensor_load_2d_pair(a + kUnitBytes, &map, 0, (ua + 1) * kUnit, bar);
+                    if (kSym) {
+                        const int ub = right + kb * d.spu + d.tj * 4 + rank * 2;
+                        tensor_load_2d_pair(b, &map, 0, ub * kUnit, bar);
+                        tensor_load_2d_pair(b + kUnitBytes, &map, 0, (ub + 1) * kUnit, bar);
+                    } else {
+                        const int ub = (k < d.ku ? right : d.x_lo) + (d.tj * 4 + rank * 2) * d.spu + kb;
+                        tensor_load_2d_pair(b, &map, 0, ub * kUnit, bar);
+                        tensor_load_2d_pair(b + kUnitBytes, &map, 0, (ub + d.spu) * kUnit, bar);
+                    }
+                    if (++st == kPairStages) { st = 0; ++round; }
+                }
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0 && rank == 0) {
+            const uint32_t shape = f16_shape(kPairTile, kPairTile, !kSym);
+            int st = 0, n = 0;
+            uint32_t round = 0;
+            bool ok = true;
+            for (int i = first; i < total && ok; i += n_pairs, ++n) {
+                const Tile d = w.tiles[i % w.n];
+                const int steps = steps_of(d, c.p[kSym ? i / w.n : 0]);
+                const int buf = n & 1;
+                const uint32_t sums = tmem + buf * kPairTile;
+                ok = mbar_wait(smem_addr(&s_taken[buf]), ((n >> 1) & 1) ^ 1, &s_failed);
+                fence_after_sync();
+                for (int k = 0; k < steps && ok; ++k) {
+                    ok = mbar_wait(smem_addr(&s_full[st]), round & 1, &s_failed);
+                    if (!ok) break;
+                    fence_after_sync();
+                    const uint32_t a = stage0 + st * kPairStageBytes, b = a + 2 * kUnitBytes;
+#pragma unroll
+                    for (int q = 0; q < kUnit / 16; ++q) {
+                        const uint64_t da = swizzled_operand(a + q * 32, 16, 1024);
+                        const uint64_t db = kSym ? swizzled_operand(b + q * 32, 16, 1024)
+                                                 : swizzled_operand(b + q * 2048, kUnitBytes, 1024);
+                        mma_f16_pair(sums, da, db, shape, k > 0 || q > 0);
+                    }
+                    tc_commit_pair(smem_addr(&s_free[st]));
+                    if (++st == kPairStages) { st = 0; ++round; }
+                }
+                tc_commit_pair(smem_addr(&s_sums[buf]));
+            }
+        }
+    } else {
+        const int quarter = warp & 3, row = quarter * 32 + lane, e0 = threadIdx.x == 64;
+        const uint32_t out0 = stage0 + kPairStages * kPairStageBytes;
+        uint8_t* out_smem = smem + kPairStages * kPairStageBytes;
+        const uint32_t taken[2] = {in_cta(smem_addr(&s_taken[0]), 0), in_cta(smem_addr(&s_taken[1]), 0)};
+        int n = 0, part = 0;
+        for (int i = first; i < total; i += n_pairs, ++n) {
+            const Tile d = w.tiles[i % w.n];
+            const Product& p = c.p[kSym ? i / w.n : 0];
+            const int small = d.spu * d.spu, buf = n & 1;
+            const int rb = d.ti * 4 + rank * 2;                       // first unit row of this CTA's part
+            const bool mirror = kSym && d.ti != d.tj;
+            const uint8_t* plus = nullptr;
+            if (kSym && p.plus >= 0)
+                plus = ws + (int64_t)(d.small + p.plus * small + rb + (row >> 6)) * kUnitBytes;
+            uint4 e[2][4];                                            // 32 columns of `plus`, fetched one step ahead
+            const auto fetch = [&](int q, uint4 (&to)[4]) {
+                const uint8_t* u = plus + (int64_t)(d.tj * 4 + (q >> 1)) * d.spu * kUnitBytes;
+#pragma unroll
+                for (int o = 0; o < 4; ++o)
+                    to[o] = __ldcg(reinterpret_cast<const uint4*>(u + in_unit(row & 63, (q & 1) * 4 + o)));
+            };
+            if (kSym && plus) fetch(0, e[0]);
+            const float gamma = kSym && d.ti == d.tj ? p.gamma : 0.0f;
+            const int diagonal = (int)rank * 128 + row;
+            const bool ok = mbar_wait(smem_addr(&s_sums[buf]), (n >> 1) & 1, &s_failed);
+            __syncwarp();
+            if (!ok) break;
+            fence_after_sync();
+#pragma unroll 1
+            for (int cu = 0; cu < 4; ++cu, ++part) {
+                uint8_t* img = out_smem + (part & 1) * kOutBytes;
+                const uint32_t img_addr = out0 + (part & 1) * kOutBytes;
+                // (the stores that read this buffer two parts ago are done reading)
+                if (e0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+                epilogue_sync();
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int q = cu * 2 + h;
+                    uint32_t acc[32];
+                    if (kSym && plus && q < 7) fetch(q + 1, e[h ^ 1]);
+                    tmem_load32(tmem + buf * kPairTile + ((uint32_t)(quarter * 32) << 16) + q * 32, acc);
+                    if (kSym || !c.last) {
+                        const float alpha = kSym ? p.alpha : c.alpha;
+#pragma unroll
+                        for (int o = 0; o < 4; ++o) {
+                            float v[8];
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) v[j] = alpha * __uint_as_float(acc[o * 8 + j]);
+                            if (kSym && plus) {
+                                const __half2* x = reinterpret_cast<const __half2*>(&e[h][o]);
+#pragma unroll
+                                for (int j = 0; j < 4; ++j) {
+                                    const float2 f = __half22float2(x[j]);
+                                    v[2 * j] = fmaf(p.beta, f.x, v[2 * j]);
+                                    v[2 * j + 1] = fmaf(p.beta, f.y, v[2 * j + 1]);
+                                }
+                            }
+                            if (kSym) {
+                                // (a select: a branch would be taken by one lane at a time)
+#pragma unroll
+                                for (int j = 0; j < 8; ++j) v[j] += diagonal == q * 32 + o * 8 + j ? gamma : 0.0f;
+                            }
+                            const uint4 packed = pack8(v);
+                            *reinterpret_cast<uint4*>(img + (row >> 6) * kUnitBytes + in_unit(row & 63, h * 4 + o)) = packed;
+                            if (mirror) {
+                                const __half* hv = reinterpret_cast<const __half*>(&packed);
+#pragma unroll
+                                for (int j = 0; j < 8; ++j)
+                                    *reinterpret_cast<__half*>(img + (2 + (row >> 6)) * kUnitBytes +
+                                                               in_unit(h * 32 + o * 8 + j, (row & 63) >> 3) +
+                                                               (row & 7) * 2) = hv[j];
+                            }
+                        }
+                    } else {
+                        const bool tall = t->m[d.mat].rows > t->m[d.mat].cols;
+                        __nv_bfloat16* s_out = reinterpret_cast<__nv_bfloat16*>(img);
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) {
+                            const __nv_bfloat16 b = __float2bfloat16_rn(c.alpha * __uint_as_float(acc[j]));
+                            if (tall) s_out[(h * 32 + j) * 130 + row] = b; else s_out[row * 66 + h * 32 + j] = b;
+                        }
+                    }
+                }
+                if (cu == 3) {                                        // the sums have been read
+                    fence_before_sync();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_cluster(taken[buf]);
+                }
+                if (kSym || !c.last) {
+                    fence_async_shared();
+                    epilogue_sync();
+                    if (e0) {
+                        const int cb = d.tj * 4 + cu;
+                        if (kSym || cb < d.lu) {
+                            const int base = kSym ? d.small + p.to * small : (c.x_in ? d.x_hi : d.x_next);
+                            bulk_store(ws + (int64_t)(base + cb * d.spu + rb) * kUnitBytes, img_addr, 2 * kUnitBytes);
+                            if (mirror)
+                                for (int u = 0; u < 2; ++u)
+                                    bulk_store(ws + (int64_t)(base + (rb + u) * d.spu + cb) * kUnitBytes,
+                                               img_addr + (2 + u) * kUnitBytes, kUnitBytes);
+                        }
+                        bulk_store_commit();
+                    }
+                } else {
+                    epilogue_sync();
+                    const Mat& m = t->m[d.mat];
+                    const bool tall = m.rows > m.cols;
+                    const __nv_bfloat16* s_out = reinterpret_cast<const __nv_bfloat16*>(img);
+                    const int r_x = rb * kUnit, c_x = (d.tj * 4 + cu) * kUnit;   // first row, column of X
+                    const int a0 = tall ? c_x : r_x, n0 = tall ? r_x : c_x;
+                    const int lines = tall ? 64 : 128, len = tall ? 128 : 64, pitch = tall ? 130 : 66;
+                    const bool even = ((m.offset | m.cols) & 1) == 0 && ((uintptr_t)out & 3) == 0;
+                    for (int a = quarter; a < lines && a0 + a < m.rows; a += 4) {
+                        __nv_bfloat16* to = out + m.offset + (int64_t)(a0 + a) * m.cols + n0;
+                        if (even) {
+                            for (int k = lane * 2; k < len && n0 + k < m.cols; k += 64)
+                                *reinterpret_cast<uint32_t*>(to + k) = *reinterpret_cast<const uint32_t*>(s_out + a * pitch + k);
+                        } else {
+                            for (int k = lane; k < len && n0 + k < m.cols; k += 32) to[k] = s_out[a * pitch + k];
+                        }
+                    }
+                    if (e0) bulk_store_commit();                      // (an empty group keeps the count of parts)
+                }
+            }
+        }
+        if (e0) bulk_store_wait();
+    }
+    __syncwarp();
+    fence_before_sync();
+    __syncthreads();
+    if (threadIdx.x == 0 && s_failed) atomicAdd(timeouts, 1);
+    cluster_sync();
+    if (warp == 1) tmem_free_pair(tmem, 512);
+}
+
 __device__ int g_timeouts;
 
 // ---------------------------------------------------------------------------------------------- host side
@@ -469,8 +776,9 @@ static int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 // Lays the matrices order[0..n) out in the workspace and numbers the CTAs of the passes.  Returns the bytes needed.
 static int64_t lay_out(const int64_t* offsets, const int64_t* rows, const int64_t* cols, const int* order, int n, Table* t) {
     int64_t at = up(sizeof(Table), 1024);
-    int64_t chunks = 0, units = 0, sym = 0, apply = 0;
+    int64_t chunks = 0, units = 0, sym = 0, apply = 0, pair_sym = 0, pair_apply = 0;
     t->n = n;
+    t->n_pair = 0;
     for (int k = 0; k < n; ++k) {
         Mat& m = t->m[k];
         const int64_t r = rows[order[k]], c = cols[order[k]];
@@ -479,7 +787,8 @@ static int64_t lay_out(const int64_t* offsets, const int64_t* rows, const int64_
         m.cols = (int)c;
         m.s = (int)std::min(r, c);
         m.l = (int)std::max(r, c);
-        m.sp = (int)up(m.s, kTile);
+        const bool pair = m.s > kTile;                                // (the order has these first)
+        m.sp = (int)up(m.s, pair ? kPairTile : kTile);
         m.lp = (int)up(m.l, kUnit);
         t->chunk_at[k] = (int)chunks;
         t->unit_at[k] = (int)units;
@@ -490,16 +799,28 @@ static int64_t lay_out(const int64_t* offsets, const int64_t* rows, const int64_
         chunks += m.n_chunks;
         units += (int64_t)(m.sp / kUnit) * (m.lp / kUnit);
         const int64_t mt = m.sp / kTile;
-        sym += mt * (mt + 1) / 2;
-        apply += mt * ((m.lp + kTile - 1) / kTile);
+        if (pair) {
+            t->n_pair = k + 1;
+            t->pair_sym_at[k] = (int)pair_sym;
+            t->pair_apply_at[k] = (int)pair_apply;
+            pair_sym += mt / 2 * (mt / 2 + 1) / 2;
+            pair_apply += mt / 2 * ((m.lp + kPairTile - 1) / kPairTile);
+        } else {
+            sym += mt * (mt + 1) / 2;
+            apply += mt * ((m.lp + kTile - 1) / kTile);
+        }
     }
+    t->pair_sym_at[t->n_pair] = (int)pair_sym;
+    t->pair_apply_at[t->n_pair] = (int)pair_apply;
     t->chunk_at[n] = (int)chunks;
     t->unit_at[n] = (int)units;
     t->sym_at[n] = (int)sym;
     t->apply_at[n] = (int)apply;
-    if (chunks > 0x7fffffff || units > 0x7fffffff || sym > 0x7fffffff || apply > 0x7fffffff) return -1;
+    if (pair_sym + pair_apply > 0x7fffffff || chunks > 0x7fffffff || units > 0x7fffffff || sym > 0x7fffffff || apply > 0x7fffffff) return -1;
     at = up(at + chunks * 8, 1024);
     at = up(at + n * 8, 1024);                                        // inverse norms, arrival counters
+    t->tiles = at;
+    at = up(at + (pair_sym + pair_apply) * (int64_t)sizeof(Tile), kUnitBytes);
     for (int k = 0; k < n; ++k) {
         Mat& m = t->m[k];
         const int64_t big = (int64_t)m.sp * m.lp * 2;
@@ -512,14 +833,15 @@ static int64_t lay_out(const int64_t* offsets, const int64_t* rows, const int64_
     return at;
 }
 
-// Larger matrices first, so that the last tiles of a launch are short ones; chunks of kMaxMats per chain.
+// Matrices of pair tiles first, then longer ones first, so that the last tiles of a launch are short ones; chunks of kMaxMats per chain.
 static std::vector<int> order_of(const int64_t* rows, const int64_t* cols, int n) {
     std::vector<int> o;
     for (int i = 0; i < n; ++i)
         if (rows[i] > 0 && cols[i] > 0) o.push_back(i);
     std::stable_sort(o.begin(), o.end(), [&](int x, int y) {
-        const int64_t sx = std::max(rows[x], cols[x]), sy = std::max(rows[y], cols[y]);
-        return sx > sy;
+        const bool px = std::min(rows[x], cols[x]) > kTile, py = std::min(rows[y], cols[y]) > kTile;
+        if (px != py) return px;
+        return std::max(rows[x], cols[x]) > std::max(rows[y], cols[y]);
     });
     return o;
 }
@@ -547,6 +869,7 @@ static int64_t workspace_bytes(const int64_t* rows, const int64_t* cols, int n) 
     return most;
 }
 
+// A launch whose set-up may overlap the end of the kernel before it (which it waits for itself).
 template <typename... Args>
 static cudaError_t launch(void (*kernel)(Args...), dim3 grid, int threads, size_t smem, cudaStream_t s, Args... args) {
     cudaLaunchConfig_t cfg{};
@@ -564,9 +887,24 @@ static cudaError_t launch(void (*kernel)(Args...), dim3 grid, int threads, size_
     return e;
 }
 
+static cudaError_t resident_pairs(int* n) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(2);
+    cfg.blockDim = dim3(kPairThreads);
+    cfg.dynamicSmemBytes = kPairSmem;
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = 2;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaOccupancyMaxActiveClusters(n, pair_kernel<true>, &cfg);
+    return e == cudaSuccess && *n < 1 ? cudaErrorInvalidConfiguration : e;
+}
+
 template <typename T>
 static cudaError_t chain(const Table& t, const void* grad, float* momentum, float mu, int nesterov, int steps, float eps,
-                         uint16_t* out, uint8_t* ws, int* timeouts, cudaStream_t s) {
+                         uint16_t* out, uint8_t* ws, int64_t ws_bytes, int max_pairs, int* timeouts, cudaStream_t s) {
     cudaError_t e;
     int64_t at = up(sizeof(Table), 1024);
     Table* table = reinterpret_cast<Table*>(ws);
@@ -584,8 +922,32 @@ static cudaError_t chain(const Table& t, const void* grad, float* momentum, floa
                     nesterov, (const float*)inv_norm, ws, table)) != cudaSuccess)
         return e;
     const auto two = [](int k) { return ldexpf(1.0f, k); };
+    // the workspace as rows of 128 bytes; a box is one unit (its bytes are in the tensor cores' order already)
+    CUtensorMap map{};
+    if (t.n_pair && !sidco_internal::byte_map(&map, ws, 128, ws_bytes / 128, 128, 128, kUnit, false))
+        return cudaErrorNotSupported;
+    const int n_sym = t.pair_sym_at[t.n_pair], n_apply = t.pair_apply_at[t.n_pair];
+    const Tile* tiles = reinterpret_cast<const Tile*>(ws + t.tiles);
     const auto sym = [&](const Chain& c, int products) {
+        if (t.n_pair) {
+            const int pairs = std::min(max_pairs, n_sym * products);
+            const cudaError_t r = launch(pair_kernel<true>, dim3(pairs * 2), kPairThreads, kPairSmem, s, map,
+                                         PairWork{tiles, n_sym, products}, (const Table*)table, ws, c,
+                                         (__nv_bfloat16*)out, timeouts);
+            if (r != cudaSuccess || t.n_pair == t.n) return r;
+        }
         return launch(product_kernel<true>, dim3(t.sym_at[t.n], products), kProductThreads, kProductSmem, s,
+                      (const Table*)table, ws, c, (__nv_bfloat16*)out, timeouts);
+    };
+    const auto apply = [&](const Chain& c) {
+        if (t.n_pair) {
+            const int pairs = std::min(max_pairs, n_apply);
+            const cudaError_t r = launch(pair_kernel<false>, dim3(pairs * 2), kPairThreads, kPairSmem, s, map,
+                                         PairWork{tiles + n_sym, n_apply, 1}, (const Table*)table, ws, c,
+                                         (__nv_bfloat16*)out, timeouts);
+            if (r != cudaSuccess || t.n_pair == t.n) return r;
+        }
+        return launch(product_kernel<false>, dim3(t.apply_at[t.n]), kProductThreads, kProductSmem, s,
                       (const Table*)table, ws, c, (__nv_bfloat16*)out, timeouts);
     };
     int done = 0, in = 0;
@@ -621,9 +983,7 @@ static cudaError_t chain(const Table& t, const void* grad, float* momentum, floa
         c.op = P;
         c.last = done == steps;
         c.alpha = c.last ? two(-scale_p - kX) : two(-scale_p);
-        if ((e = launch(product_kernel<false>, dim3(t.apply_at[t.n]), kProductThreads, kProductSmem, s, (const Table*)table,
-                        ws, c, (__nv_bfloat16*)out, timeouts)) != cudaSuccess)
-            return e;
+        if ((e = apply(c)) != cudaSuccess) return e;
     }
     return cudaSuccess;
 }
@@ -659,18 +1019,21 @@ int sidco_orthogonalize(const void* grad, int grad_type, float* momentum, float 
     const int64_t need = sidco_ortho::workspace_bytes(rows, cols, n_mats);
     if (need < 0) return (int)need;
     if ((uintptr_t)workspace % 256 || workspace_bytes < (size_t)need) return SIDCO_E_WORKSPACE;
-    static bool ready[64] = {};
+    static int pair_count[64] = {};           // pairs of CTAs that are resident at once
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return (int)e;
     if (dev < 0 || dev >= 64) return SIDCO_E_SIZE;
-    if (!ready[dev]) {                       // (setting it twice from two threads is harmless)
-        if ((e = cudaFuncSetAttribute(product_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kProductSmem)) !=
-                cudaSuccess ||
-            (e = cudaFuncSetAttribute(product_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kProductSmem)) !=
-                cudaSuccess)
+    if (!pair_count[dev]) {                  // (setting it twice from two threads is harmless)
+        const auto most = cudaFuncAttributeMaxDynamicSharedMemorySize;
+        int pairs = 0;
+        if ((e = cudaFuncSetAttribute(product_kernel<true>, most, kProductSmem)) != cudaSuccess ||
+            (e = cudaFuncSetAttribute(product_kernel<false>, most, kProductSmem)) != cudaSuccess ||
+            (e = cudaFuncSetAttribute(pair_kernel<true>, most, kPairSmem)) != cudaSuccess ||
+            (e = cudaFuncSetAttribute(pair_kernel<false>, most, kPairSmem)) != cudaSuccess ||
+            (e = resident_pairs(&pairs)) != cudaSuccess)
             return (int)e;
-        ready[dev] = true;
+        pair_count[dev] = pairs;
     }
     int* timeouts = nullptr;
     if ((e = cudaGetSymbolAddress((void**)&timeouts, g_timeouts)) != cudaSuccess) return (int)e;
@@ -680,11 +1043,11 @@ int sidco_orthogonalize(const void* grad, int grad_type, float* momentum, float 
         uint8_t* ws = (uint8_t*)workspace;
         cudaStream_t s = (cudaStream_t)stream;
         if (grad_type == SIDCO_T_F32)
-            e = chain<float>(t[0], grad, momentum, mu, nesterov, steps, eps, out_bf16, ws, timeouts, s);
+            e = chain<float>(t[0], grad, momentum, mu, nesterov, steps, eps, out_bf16, ws, need, pair_count[dev], timeouts, s);
         else if (grad_type == SIDCO_T_BF16)
-            e = chain<__nv_bfloat16>(t[0], grad, momentum, mu, nesterov, steps, eps, out_bf16, ws, timeouts, s);
+            e = chain<__nv_bfloat16>(t[0], grad, momentum, mu, nesterov, steps, eps, out_bf16, ws, need, pair_count[dev], timeouts, s);
         else
-            e = chain<__half>(t[0], grad, momentum, mu, nesterov, steps, eps, out_bf16, ws, timeouts, s);
+            e = chain<__half>(t[0], grad, momentum, mu, nesterov, steps, eps, out_bf16, ws, need, pair_count[dev], timeouts, s);
         if (e != cudaSuccess) return (int)e;
     }
     return 0;
