@@ -47,9 +47,9 @@ constexpr int kP = 10;                // products of two or three B (<= 41)
 
 constexpr int kUnit = 64;             // units of 64 x 64
 constexpr int kUnitBytes = kUnit * kUnit * 2;
+constexpr int kPairTile = 256;       // products of larger matrices: tiles of 256 x 256
 constexpr int kMaxMats = 128;         // matrices of one chain of launches
 constexpr int kChunk = 16384;         // elements of a matrix per CTA of the momentum pass
-constexpr int kPairTile = 256;
 
 enum Buffer { kBufA, kBufA2, kBufB, kBufT, kBufP, kBufP2, kSmallBuffers };
 
@@ -58,7 +58,7 @@ struct Mat {
     int64_t x_hi, x_lo, x_next;       // bytes into the workspace: s x l matrices
     int64_t small;                    // first of the s x s matrices
     int rows, cols, s, l;
-    int sp, lp;                       // s to a multiple of 128 (256: pair tiles), l to a multiple of 64
+    int sp, lp;                       // s to a multiple of 256, l to a multiple of 64
     int partial0, n_chunks;           // partial sums of squares
 };
 
@@ -66,11 +66,8 @@ struct Table {
     int n;
     int chunk_at[kMaxMats + 1];       // first CTA of every matrix: momentum pass,
     int unit_at[kMaxMats + 1];        // normalisation,
-    int sym_at[kMaxMats + 1];         // symmetric products,
+    int sym_at[kMaxMats + 1];         // first tile of every matrix: symmetric products,
     int apply_at[kMaxMats + 1];       // applications
-    int n_pair;                       // the first matrices go through pair tiles:
-    int pair_sym_at[kMaxMats + 1];
-    int pair_apply_at[kMaxMats + 1];
     int64_t tiles;                    // bytes into the workspace: Tile[], symmetric products, then applications
     Mat m[kMaxMats];
 };
@@ -202,12 +199,12 @@ __global__ void __launch_bounds__(256) normalize_kernel(const __grid_constant__ 
     if (blockIdx.x == 0)
         for (int w = threadIdx.x; w < (int)(sizeof(Table) / 4); w += 256)
             reinterpret_cast<int*>(table_out)[w] = reinterpret_cast<const int*>(&t)[w];
-    const int n_sym = t.pair_sym_at[t.n_pair], n_apply = t.pair_apply_at[t.n_pair];
+    const int n_sym = t.sym_at[t.n], n_apply = t.apply_at[t.n];
     for (int w = blockIdx.x * 256 + threadIdx.x; w < n_sym + n_apply; w += gridDim.x * 256) {
         const bool sym = w < n_sym;
         const int k = sym ? w : w - n_sym;
-        const int* at = sym ? t.pair_sym_at : t.pair_apply_at;
-        const int j = find(at, t.n_pair, k), tile = k - at[j];
+        const int* at = sym ? t.sym_at : t.apply_at;
+        const int j = find(at, t.n, k), tile = k - at[j];
         const Mat& q = t.m[j];
         Tile d{};
         d.x_hi = (int)(q.x_hi / kUnitBytes);
@@ -266,12 +263,6 @@ __global__ void __launch_bounds__(256) normalize_kernel(const __grid_constant__ 
 
 // ---------------------------------------------------------------------------------------------- products
 
-constexpr int kTile = 128;
-constexpr int kStageBytes = 2 * kTile * kUnit * 2;                    // 128 x 64 of both operands: 32 KB
-constexpr int kStages = 3;
-constexpr int kProductThreads = 128;
-constexpr int kProductSmem = kStages * kStageBytes + 1024;            // (base rounded up to 1024)
-
 struct Product {
     int left, right;                  // s x s operands; left = -1: the Gram product of X
     int plus;                         // matrix added times beta (-1: none)
@@ -287,224 +278,6 @@ struct Chain {
     int last;                         // write bf16 into the caller's vector instead of the next X
     float alpha;
 };
-
-__device__ __forceinline__ const uint8_t* unit_at(const uint8_t* base, int sp, int cb, int rb) {
-    return base + ((int64_t)cb * (sp / kUnit) + rb) * kUnitBytes;
-}
-
-// One 128 x 128 tile per CTA, two CTAs per SM (the end of one runs under the products of the other).  Thread 0 feeds the
-// stages, thread 32 issues the products; then all four warps take a quarter of the rows each out of tensor memory.
-template <bool kSym>
-__global__ void __launch_bounds__(kProductThreads, 2) product_kernel(const Table* t, uint8_t* ws,
-                                                                     const __grid_constant__ Chain c,
-                                                                     __nv_bfloat16* __restrict__ out, int* timeouts) {
-    extern __shared__ uint8_t s_raw[];
-    __shared__ uint64_t s_full[kStages], s_free[kStages], s_done;
-    __shared__ uint32_t s_tmem;
-    __shared__ int s_failed;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    uint8_t* smem = (uint8_t*)(((uintptr_t)s_raw + 1023) & ~(uintptr_t)1023);
-    const uint32_t stage0 = smem_addr(smem);
-    if (warp == 0) tmem_alloc(&s_tmem, kTile);
-    if (threadIdx.x == 0) {
-        for (int i = 0; i < kStages; ++i) {
-            mbar_init(smem_addr(&s_full[i]), 1);
-            mbar_init(smem_addr(&s_free[i]), 1);
-        }
-        mbar_init(smem_addr(&s_done), 1);
-        s_failed = 0;
-        mbar_init_fence();
-    }
-    fence_before_sync();
-    __syncthreads();
-    fence_after_sync();
-    launch_dependents();
-    wait_prerequisites();
-    const uint32_t tmem = s_tmem;
-
-    const int* at = kSym ? t->sym_at : t->apply_at;
-    const int mi = find(at, t->n, blockIdx.x);
-    int tile = blockIdx.x - at[mi];
-    const Mat m = t->m[mi];
-    const int sp = m.sp, mt = sp / kTile;
-    const int64_t small_bytes = (int64_t)sp * sp * 2;
-    const uint8_t* x_in = ws + (c.x_in ? m.x_next : m.x_hi);
-    const Product& p = c.p[kSym ? blockIdx.y : 0];
-    int ti, tj;                                                       // tile row, tile column
-    const uint8_t *left, *right;
-    int steps;                                                        // K in units of 64
-    bool gram = false;
-    if (kSym) {
-        uint16_t r16, c16;
-        triangle(tile, &r16, &c16);
-        ti = r16;
-        tj = c16;
-        gram = p.left < 0;
-        left = gram ? x_in : ws + m.small + p.left * small_bytes;
-        right = gram ? x_in : ws + m.small + p.right * small_bytes;
-        steps = (gram ? m.lp : (m.s + kUnit - 1) / kUnit * kUnit) / kUnit;
-    } else {
-        ti = tile % mt;
-        tj = tile / mt;
-        left = ws + m.small + c.op * small_bytes;
-        right = x_in;
-        steps = (m.s + kUnit - 1) / kUnit * c.parts;
-    }
-    const int half = kSym ? 0 : (m.s + kUnit - 1) / kUnit;
-    const int cols_here = kSym ? 2 : min(2, m.lp / kUnit - tj * 2);   // units of X that the tile has
-
-    if (threadIdx.x == 0) {
-        for (int k = 0; k < steps; ++k) {
-            const int st = k % kStages;
-            if (k >= kStages && !mbar_wait(smem_addr(&s_free[st]), (k / kStages - 1) & 1, &s_failed)) break;
-            const uint32_t a = stage0 + st * kStageBytes, b = a + kTile * kUnit * 2, bar = smem_addr(&s_full[st]);
-            if (kSym) {
-                mbar_expect_tx(bar, ti == tj && left == right ? kStageBytes / 2 : kStageBytes);
-                bulk_load(a, unit_at(left, sp, k, ti * 2), kStageBytes / 2, bar);
-                if (ti != tj || left != right) bulk_load(b, unit_at(right, sp, k, tj * 2), kStageBytes / 2, bar);
-            } else {
-                const int kb = k < half ? k : k - half;
-                const uint8_t* x = k < half ? right : ws + m.x_lo;
-                mbar_expect_tx(bar, kStageBytes / 2 + cols_here * kUnitBytes);
-                bulk_load(a, unit_at(left, sp, kb, ti * 2), kStageBytes / 2, bar);
-                for (int u = 0; u < cols_here; ++u)
-                    bulk_load(b + u * kUnitBytes, unit_at(x, sp, tj * 2 + u, kb), kUnitBytes, bar);
-            }
-        }
-    } else if (threadIdx.x == 32) {
-        const uint32_t shape = f16_shape(kTile, kTile, !kSym);
-        bool ok = true;
-        for (int k = 0; k < steps && ok; ++k) {
-            const int st = k % kStages;
-            ok = mbar_wait(smem_addr(&s_full[st]), (k / kStages) & 1, &s_failed);
-            if (!ok) break;
-            fence_after_sync();
-            const uint32_t a = stage0 + st * kStageBytes;
-            const uint32_t b = kSym && ti == tj && left == right ? a : a + kTile * kUnit * 2;
-#pragma unroll
-            for (int q = 0; q < kUnit / 16; ++q) {
-                const uint64_t da = swizzled_operand(a + q * 32, 16, 1024);
-                const uint64_t db = kSym ? swizzled_operand(b + q * 32, 16, 1024)
-                                         : swizzled_operand(b + q * 2048, kUnitBytes, 1024);
-                mma_f16(tmem, da, db, shape, k > 0 || q > 0);
-            }
-            tc_commit(smem_addr(&s_free[st]));
-        }
-        tc_commit(smem_addr(&s_done));
-    }
-    __syncwarp();
-    mbar_wait(smem_addr(&s_done), 0, &s_failed);
-    __syncwarp();
-    fence_after_sync();
-
-    // ---- the tile, 32 columns at a time: stages are free now and hold the images on their way out
-    const int row = warp * 32 + lane;
-    const bool mirror = kSym && ti != tj;
-    if (kSym) {
-        const uint8_t* plus = p.plus >= 0 ? ws + m.small + p.plus * small_bytes : nullptr;
-        const float gamma = ti == tj ? p.gamma : 0.0f;
-#pragma unroll 1
-        for (int q = 0; q < kTile / 32; ++q) {
-            uint32_t acc[32];
-            tmem_load32(tmem + ((uint32_t)(warp * 32) << 16) + q * 32, acc);
-#pragma unroll
-            for (int o = 0; o < 4; ++o) {
-                const int c8 = (q * 4 + o) & 7, cu = q >> 1;          // eight columns of the tile's unit column cu
-                float v[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = p.alpha * __uint_as_float(acc[o * 8 + j]);
-                if (plus) {
-                    const uint4 w = __ldcg(reinterpret_cast<const uint4*>(
-                        unit_at(plus, sp, tj * 2 + cu, ti * 2 + (row >> 6)) + in_unit(row & 63, c8)));
-                    const __half2* h = reinterpret_cast<const __half2*>(&w);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const float2 f = __half22float2(h[j]);
-                        v[2 * j] = fmaf(p.beta, f.x, v[2 * j]);
-                        v[2 * j + 1] = fmaf(p.beta, f.y, v[2 * j + 1]);
-                    }
-                }
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] += row == q * 32 + o * 8 + j ? gamma : 0.0f;
-                *reinterpret_cast<uint4*>(smem + (cu * 2 + (row >> 6)) * kUnitBytes + in_unit(row & 63, c8)) = pack8(v);
-                if (mirror) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const int col = q * 32 + o * 8 + j;           // becomes a row
-                        *reinterpret_cast<__half*>(smem + kStageBytes + ((row >> 6) * 2 + (col >> 6)) * kUnitBytes +
-                                                   in_unit(col & 63, (row & 63) >> 3) + (row & 7) * 2) =
-                            __float2half_rn(v[j]);
-                    }
-                }
-            }
-        }
-        fence_async_shared();
-        __syncthreads();
-        if (threadIdx.x == 0 && !s_failed) {
-            uint8_t* to = ws + m.small + p.to * small_bytes;
-            for (int cu = 0; cu < 2; ++cu) {
-                bulk_store((void*)unit_at(to, sp, tj * 2 + cu, ti * 2), stage0 + cu * 2 * kUnitBytes, 2 * kUnitBytes);
-                if (mirror)
-                    bulk_store((void*)unit_at(to, sp, ti * 2 + cu, tj * 2), stage0 + kStageBytes + cu * 2 * kUnitBytes,
-                               2 * kUnitBytes);
-            }
-            bulk_store_commit();
-            bulk_store_wait();
-        }
-    } else if (!c.last) {
-#pragma unroll 1
-        for (int q = 0; q < kTile / 32; ++q) {
-            uint32_t acc[32];
-            tmem_load32(tmem + ((uint32_t)(warp * 32) << 16) + q * 32, acc);
-#pragma unroll
-            for (int o = 0; o < 4; ++o) {
-                float v[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = c.alpha * __uint_as_float(acc[o * 8 + j]);
-                *reinterpret_cast<uint4*>(smem + ((q >> 1) * 2 + (row >> 6)) * kUnitBytes +
-                                          in_unit(row & 63, (q * 4 + o) & 7)) = pack8(v);
-            }
-        }
-        fence_async_shared();
-        __syncthreads();
-        if (threadIdx.x == 0 && !s_failed) {
-            for (int cu = 0; cu < cols_here; ++cu)
-                bulk_store((void*)unit_at(ws + (c.x_in ? m.x_hi : m.x_next), sp, tj * 2 + cu, ti * 2), stage0 + cu * 2 * kUnitBytes,
-                           2 * kUnitBytes);
-            bulk_store_commit();
-            bulk_store_wait();
-        }
-    } else {
-        // bf16 into the caller's vector: neighbours of a row of the caller's matrix are rows of X if it is tall
-        const bool tall = m.rows > m.cols;
-        constexpr int kPad = kTile + 2;                               // bf16 per row of the staged tile
-        __nv_bfloat16* s_out = reinterpret_cast<__nv_bfloat16*>(smem);
-#pragma unroll 1
-        for (int q = 0; q < kTile / 32; ++q) {
-            uint32_t acc[32];
-            tmem_load32(tmem + ((uint32_t)(warp * 32) << 16) + q * 32, acc);
-#pragma unroll
-            for (int j = 0; j < 32; ++j) {
-                const __nv_bfloat16 b = __float2bfloat16_rn(c.alpha * __uint_as_float(acc[j]));
-                if (tall) s_out[(q * 32 + j) * kPad + row] = b; else s_out[row * kPad + q * 32 + j] = b;
-            }
-        }
-        __syncthreads();
-        const int a0 = (tall ? tj : ti) * kTile, r0 = (tall ? ti : tj) * kTile;   // first row / column in the caller's
-        if (!s_failed) {
-            for (int a = warp; a < kTile && a0 + a < m.rows; a += kProductThreads / 32) {
-                __nv_bfloat16* to = out + m.offset + (int64_t)(a0 + a) * m.cols + r0;
-#pragma unroll
-                for (int k = 0; k < kTile / 32; ++k)
-                    if (r0 + k * 32 + lane < m.cols) to[k * 32 + lane] = s_out[a * kPad + k * 32 + lane];
-            }
-        }
-    }
-    fence_before_sync();
-    __syncthreads();
-    if (threadIdx.x == 0 && s_failed) atomicAdd(timeouts, 1);
-    if (warp == 0) tmem_free(tmem, kTile);
-}
 
 // ---------------------------------------------------------------------------------------------- pair tiles
 //
@@ -767,6 +540,325 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2)
     if (warp == 1) tmem_free_pair(tmem, 512);
 }
 
+// ---------------------------------------------------------------------------------------------- small matrices
+//
+// Matrices with s <= 128 and l <= 2048: one cluster of CTAs per matrix does the whole update in one launch.  Every CTA
+// keeps its columns of X (up to 256: 64 KB for each of the two fp16 parts) in shared memory from the first step to the
+// last.  The only exchange between the CTAs is a sum per Gram matrix: each adds its share of the rows of all partial
+// Gram matrices through distributed shared memory, in the order of the CTAs, and hands the result to the others; the
+// s x s products that follow (a few hundred nanoseconds each) every CTA does for itself.
+
+constexpr int kSmallS = 128, kSmallUnits = 4, kSmallCluster = 8;      // units of columns per CTA, CTAs per matrix: at most
+constexpr int kSmallThreads = 256;
+constexpr int kSquareBytes = 4 * kUnitBytes;                          // 128 x 128
+constexpr int kSlabBytes = kSmallUnits * 2 * kUnitBytes;              // 128 x 256
+constexpr int kSmallSmem = 3 * kSquareBytes + 2 * kSlabBytes + 1024;
+
+struct SmallMats {
+    int n;
+    struct { int64_t offset; int rows, cols; } m[kMaxMats];
+};
+
+__device__ __forceinline__ uint4 remote_load16(uint32_t addr) {
+    uint4 v;
+    asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr));
+    return v;
+}
+
+__device__ __forceinline__ void remote_store16(uint32_t addr, uint4 v) {
+    asm volatile("st.shared::cluster.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w)
+                 : "memory");
+}
+
+__device__ __forceinline__ void remote_store_f64(uint32_t addr, double v) {
+    asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(addr), "d"(v) : "memory");
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kSmallThreads, 1)
+    small_kernel(const __grid_constant__ SmallMats mats, const T* __restrict__ grad, float* __restrict__ momentum, float mu,
+                 int nesterov, int steps, float eps, __nv_bfloat16* __restrict__ out, int* timeouts) {
+    extern __shared__ uint8_t s_raw[];
+    __shared__ double s_norm[kSmallCluster], s_sum[kSmallThreads / 32];
+    __shared__ uint64_t s_done;
+    __shared__ uint32_t s_tmem;
+    __shared__ int s_failed;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    uint32_t ctas;
+    asm("mov.u32 %0, %cluster_nctaid.x;" : "=r"(ctas));
+    const uint32_t rank = cluster_rank();
+    const auto& m = mats.m[blockIdx.x / ctas];
+    const bool tall = m.rows > m.cols;
+    const int s = tall ? m.cols : m.rows, l = tall ? m.rows : m.cols;
+    const int lu = (l + kUnit - 1) / kUnit, ku = (s + kUnit - 1) / kUnit;
+    const int first = (int)(lu * rank / ctas), units = (int)(lu * (rank + 1) / ctas) - first;   // of this CTA's columns
+
+    uint8_t* smem = (uint8_t*)(((uintptr_t)s_raw + 1023) & ~(uintptr_t)1023);
+    uint8_t *sq[3], *x_hi = smem + 3 * kSquareBytes, *x_lo = x_hi + kSlabBytes;
+    for (int i = 0; i < 3; ++i) sq[i] = smem + i * kSquareBytes;
+    if (warp == 0) tmem_alloc(&s_tmem, 256);
+    if (threadIdx.x == 0) {
+        mbar_init(smem_addr(&s_done), 1);
+        s_failed = 0;
+        mbar_init_fence();
+    }
+
+    // ---- momentum and norm; an element's place: (row r of X, column `a` of the unit)
+    const int s2 = s <= 32 ? 5 : s <= 64 ? 6 : 7;                     // s to a power of two
+    const int per_unit = tall ? kUnit << s2 : s * kUnit;
+    const auto place = [&](int u, int e, int& r, int& a) -> int64_t {  // < 0: outside the matrix
+        if (tall) {
+            r = e & ((1 << s2) - 1);
+            a = e >> s2;
+        } else {
+            a = e & (kUnit - 1);
+            r = e >> 6;
+        }
+        const int col = (first + u) * kUnit + a;
+        if (r >= s || col >= l) return -1;
+        return m.offset + (tall ? (int64_t)col * m.cols + r : (int64_t)r * m.cols + col);
+    };
+    const auto update_of = [&](float g, float mom) { return !momentum ? g : nesterov ? fmaf(mu, mom, g) : mom; };
+    constexpr int kAhead = 8;
+    double sum = 0.0;
+    for (int u = 0; u < units; ++u)
+        for (int e0 = threadIdx.x; e0 < per_unit; e0 += kSmallThreads * kAhead) {
+            float g[kAhead], v[kAhead];
+            int64_t at[kAhead];
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                int r, a;
+                at[k] = e0 + k * kSmallThreads < per_unit ? place(u, e0 + k * kSmallThreads, r, a) : -1;
+                g[k] = at[k] >= 0 ? widen(grad[at[k]]) : 0.0f;
+                v[k] = at[k] >= 0 && momentum ? momentum[at[k]] : 0.0f;
+            }
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                if (at[k] < 0) continue;
+                const float mom = fmaf(mu, v[k], g[k]);
+                if (momentum) momentum[at[k]] = mom;
+                const double x = update_of(g[k], mom);
+                sum += x * x;
+            }
+        }
+    for (int i = threadIdx.x; i < 2 * kSlabBytes / 16; i += kSmallThreads)      // rows and columns behind the matrix
+        reinterpret_cast<uint4*>(x_hi)[i] = make_uint4(0, 0, 0, 0);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_down_sync(0xffffffffu, sum, o);
+    if (lane == 0) s_sum[warp] = sum;
+    fence_before_sync();
+    __syncthreads();
+    cluster_sync();                                                   // every CTA runs, so its shared memory may be written
+    fence_after_sync();
+    const uint32_t tmem = s_tmem;
+    if (threadIdx.x < ctas) {
+        sum = 0.0;
+        for (int w = 0; w < kSmallThreads / 32; ++w) sum += s_sum[w];
+        remote_store_f64(in_cta(smem_addr(&s_norm[rank]), threadIdx.x), sum);
+    }
+    cluster_sync();
+    sum = 0.0;
+    for (uint32_t i = 0; i < ctas; ++i) sum += s_norm[i];
+    const float scale = (float)(1.0 / (sqrt(sum) + (double)eps)) * (float)(1 << kX);
+
+    // ---- X in two fp16 parts (each thread reads back what it wrote)
+    for (int u = 0; u < units; ++u)
+        for (int e0 = threadIdx.x; e0 < per_unit; e0 += kSmallThreads * kAhead) {
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                int r, a;
+                const int e = e0 + k * kSmallThreads;
+                const int64_t at = e < per_unit ? place(u, e, r, a) : -1;
+                if (at < 0) continue;
+                const float x = scale * (!momentum ? widen(grad[at]) : nesterov ? fmaf(mu, momentum[at], widen(grad[at]))
+                                                                                : momentum[at]);
+                const __half hi = __float2half_rn(x);
+                const int byte = (u * 2 + (r >> 6)) * kUnitBytes + in_unit(r & 63, a >> 3) + (a & 7) * 2;
+                *reinterpret_cast<__half*>(x_hi + byte) = hi;
+                *reinterpret_cast<__half*>(x_lo + byte) = __float2half_rn(x - __half2float(hi));
+            }
+        }
+
+    // ---- products: thread 0 issues, then everybody takes its rows and columns of the sums
+    int uses = 0;
+    const int row = (warp & 3) * 32 + lane, side = warp >> 2;         // row of the sums, half of their columns
+    const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+    const auto issue_and_wait = [&](auto products) {
+        fence_async_shared();
+        fence_before_sync();
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            fence_after_sync();
+            products();
+            tc_commit(smem_addr(&s_done));
+        }
+        __syncwarp();
+        mbar_wait(smem_addr(&s_done), uses & 1, &s_failed);
+        __syncwarp();
+        ++uses;
+        fence_after_sync();
+    };
+    // to = alpha (left right) + beta plus + gamma I, all 128 x 128
+    const auto square = [&](const uint8_t* left, const uint8_t* right, const uint8_t* plus, uint8_t* to, float alpha,
+                            float beta, float gamma) {
+        issue_and_wait([&] {
+            const uint32_t a = smem_addr(left), b = smem_addr(right);
+            for (int k = 0; k < ku * 4; ++k)
+                mma_f16(tmem, swizzled_operand(a + (k >> 2) * 2 * kUnitBytes + (k & 3) * 32, 16, 1024),
+                        swizzled_operand(b + (k >> 2) * 2 * kUnitBytes + (k & 3) * 32, 16, 1024),
+                        f16_shape(kSmallS, kSmallS, false), k > 0);
+        });
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            uint32_t acc[32];
+            tmem_load32(lanes + side * 64 + h * 32, acc);
+#pragma unroll
+            for (int o = 0; o < 4; ++o) {
+                const int at = (side * 2 + (row >> 6)) * kUnitBytes + in_unit(row & 63, h * 4 + o);
+                float v[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = alpha * __uint_as_float(acc[o * 8 + j]);
+                if (plus) {
+                    const uint4 w = *reinterpret_cast<const uint4*>(plus + at);
+                    const __half2* x = reinterpret_cast<const __half2*>(&w);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float2 f = __half22float2(x[j]);
+                        v[2 * j] = fmaf(beta, f.x, v[2 * j]);
+                        v[2 * j + 1] = fmaf(beta, f.y, v[2 * j + 1]);
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] += row == side * 64 + h * 32 + o * 8 + j ? gamma : 0.0f;
+                *reinterpret_cast<uint4*>(to + at) = pack8(v);
+            }
+        }
+    };
+    const auto two = [](int k) { return __uint_as_float((uint32_t)(127 + k) << 23); };
+
+    for (int done = 0; done < steps;) {
+        const int group = steps == 1 || (done == 2 && (steps & 1)) ? 1 : 2;
+        // A = X X^T: the partial sums of this CTA's columns
+        issue_and_wait([&] {
+            const uint32_t a = smem_addr(x_hi);
+            for (int k = 0; k < units * 4; ++k) {
+                const uint64_t x = swizzled_operand(a + (k >> 2) * 2 * kUnitBytes + (k & 3) * 32, 16, 1024);
+                mma_f16(tmem, x, x, f16_shape(kSmallS, kSmallS, false), k > 0);
+            }
+        });
+        // (a CTA without columns adds zeros)
+        float* partial = reinterpret_cast<float*>(sq[1]);             // [128][128] over two squares, words swizzled
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            uint32_t acc[32];
+            tmem_load32(lanes + side * 64 + h * 32, acc);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int c4 = side * 16 + h * 8 + j;                 // four columns; rows differ in their bank
+                const float4 v = units ? make_float4(__uint_as_float(acc[j * 4]), __uint_as_float(acc[j * 4 + 1]),
+                                                     __uint_as_float(acc[j * 4 + 2]), __uint_as_float(acc[j * 4 + 3]))
+                                       : make_float4(0, 0, 0, 0);
+                reinterpret_cast<float4*>(partial)[row * 32 + (c4 ^ (row & 7))] = v;
+            }
+        }
+        fence_before_sync();
+        __syncthreads();
+        cluster_sync();
+        // rows rank, rank + ctas, ... of the sum, eight columns at a time, to every CTA's A
+        for (int i = threadIdx.x; i < kSmallS / (int)ctas * 16; i += kSmallThreads) {
+            const int r = (i >> 4) * (int)ctas + (int)rank, c8 = i & 15;
+            float v[8] = {};
+            for (uint32_t q = 0; q < ctas; ++q) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint4 w = remote_load16(
+                        in_cta(smem_addr(partial) + (uint32_t)(r * 32 + ((c8 * 2 + h) ^ (r & 7))) * 16, q));
+                    v[h * 4] += __uint_as_float(w.x);
+                    v[h * 4 + 1] += __uint_as_float(w.y);
+                    v[h * 4 + 2] += __uint_as_float(w.z);
+                    v[h * 4 + 3] += __uint_as_float(w.w);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] *= two(kA - 2 * kX);
+            const uint4 w = pack8(v);
+            const uint32_t to = smem_addr(sq[0]) + ((c8 >> 3) * 2 + (r >> 6)) * kUnitBytes + in_unit(r & 63, c8 & 7);
+            for (uint32_t q = 0; q < ctas; ++q) remote_store16(in_cta(to, q), w);
+        }
+        fence_async_all();                                            // (read by the tensor cores of the other CTAs)
+        cluster_sync();
+
+        // A in sq[0]; B in sq[1]; for a second step T, then the next B in sq[2], A and the product in sq[0]
+        uint8_t* p = sq[1];
+        int scale_p = kB;
+        square(sq[0], sq[0], sq[0], sq[1], kCc * two(kB - 2 * kA), kCb * two(kB - kA), kCa * two(kB));
+        if (group == 2) {
+            square(sq[1], sq[0], nullptr, sq[2], two(-kB), 0.0f, 0.0f);
+            square(sq[2], sq[1], nullptr, sq[0], two(-kB), 0.0f, 0.0f);
+            square(sq[0], sq[0], sq[0], sq[2], kCc * two(kB - 2 * kA), kCb * two(kB - kA), kCa * two(kB));
+            square(sq[2], sq[1], nullptr, sq[0], two(kP - 2 * kB), 0.0f, 0.0f);
+            p = sq[0];
+            scale_p = kP;
+        }
+
+        // X <- P X on this CTA's columns
+        const bool lo = done == 0;
+        issue_and_wait([&] {
+            const uint32_t a = smem_addr(p);
+            for (int k = 0; k < ku * 4 * (lo ? 2 : 1) && units; ++k) {
+                const int q = k < ku * 4 ? k : k - ku * 4;
+                const uint32_t x = smem_addr(k < ku * 4 ? x_hi : x_lo);
+                mma_f16(tmem, swizzled_operand(a + (q >> 2) * 2 * kUnitBytes + (q & 3) * 32, 16, 1024),
+                        swizzled_operand(x + (q >> 2) * kUnitBytes + (q & 3) * 2048, 2 * kUnitBytes, 1024),
+                        f16_shape(kSmallS, units * kUnit, true), k > 0);
+            }
+        });
+        done += group;
+        const bool last = done == steps;
+        const float alpha = two(last ? -scale_p - kX : -scale_p);
+        __nv_bfloat16* s_out = reinterpret_cast<__nv_bfloat16*>(x_hi);          // (both parts of X are done with)
+        constexpr int kWide = kSmallUnits * kUnit + 2, kTall = kSmallS + 2;     // bf16 per line
+        for (int u = side; u < units; u += 2) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                uint32_t acc[32];
+                tmem_load32(lanes + u * kUnit + h * 32, acc);
+                if (!last) {
+#pragma unroll
+                    for (int o = 0; o < 4; ++o) {
+                        float v[8];
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) v[j] = alpha * __uint_as_float(acc[o * 8 + j]);
+                        *reinterpret_cast<uint4*>(x_hi + (u * 2 + (row >> 6)) * kUnitBytes + in_unit(row & 63, h * 4 + o)) =
+                            pack8(v);
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) {
+                        const int col = u * kUnit + h * 32 + j;
+                        s_out[tall ? col * kTall + row : row * kWide + col] =
+                            __float2bfloat16_rn(alpha * __uint_as_float(acc[j]));
+                    }
+                }
+            }
+        }
+        if (last) {
+            __syncthreads();
+            const int lines = tall ? units * kUnit : s, len = tall ? s : units * kUnit, pitch = tall ? kTall : kWide;
+            const int line0 = tall ? first * kUnit : 0, col0 = tall ? 0 : first * kUnit;
+            if (!s_failed)
+                for (int i = warp; i < lines && line0 + i < m.rows; i += kSmallThreads / 32)
+                    for (int k = lane; k < len && col0 + k < m.cols; k += 32)
+                        out[m.offset + (int64_t)(line0 + i) * m.cols + col0 + k] = s_out[i * pitch + k];
+        }
+    }
+    fence_before_sync();
+    __syncthreads();
+    if (threadIdx.x == 0 && s_failed) atomicAdd(timeouts, 1);
+    cluster_sync();                                                   // nobody reads or writes this CTA's memory any more
+    if (warp == 0) tmem_free(tmem, 256);
+}
+
 __device__ int g_timeouts;
 
 // ---------------------------------------------------------------------------------------------- host side
@@ -776,9 +868,8 @@ static int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 // Lays the matrices order[0..n) out in the workspace and numbers the CTAs of the passes.  Returns the bytes needed.
 static int64_t lay_out(const int64_t* offsets, const int64_t* rows, const int64_t* cols, const int* order, int n, Table* t) {
     int64_t at = up(sizeof(Table), 1024);
-    int64_t chunks = 0, units = 0, sym = 0, apply = 0, pair_sym = 0, pair_apply = 0;
+    int64_t chunks = 0, units = 0, sym = 0, apply = 0;
     t->n = n;
-    t->n_pair = 0;
     for (int k = 0; k < n; ++k) {
         Mat& m = t->m[k];
         const int64_t r = rows[order[k]], c = cols[order[k]];
@@ -787,8 +878,7 @@ static int64_t lay_out(const int64_t* offsets, const int64_t* rows, const int64_
         m.cols = (int)c;
         m.s = (int)std::min(r, c);
         m.l = (int)std::max(r, c);
-        const bool pair = m.s > kTile;                                // (the order has these first)
-        m.sp = (int)up(m.s, pair ? kPairTile : kTile);
+        m.sp = (int)up(m.s, kPairTile);
         m.lp = (int)up(m.l, kUnit);
         t->chunk_at[k] = (int)chunks;
         t->unit_at[k] = (int)units;
@@ -798,29 +888,19 @@ static int64_t lay_out(const int64_t* offsets, const int64_t* rows, const int64_
         m.n_chunks = (int)((r * c + kChunk - 1) / kChunk);
         chunks += m.n_chunks;
         units += (int64_t)(m.sp / kUnit) * (m.lp / kUnit);
-        const int64_t mt = m.sp / kTile;
-        if (pair) {
-            t->n_pair = k + 1;
-            t->pair_sym_at[k] = (int)pair_sym;
-            t->pair_apply_at[k] = (int)pair_apply;
-            pair_sym += mt / 2 * (mt / 2 + 1) / 2;
-            pair_apply += mt / 2 * ((m.lp + kPairTile - 1) / kPairTile);
-        } else {
-            sym += mt * (mt + 1) / 2;
-            apply += mt * ((m.lp + kTile - 1) / kTile);
-        }
+        const int64_t mt = m.sp / kPairTile;
+        sym += mt * (mt + 1) / 2;
+        apply += mt * ((m.lp + kPairTile - 1) / kPairTile);
     }
-    t->pair_sym_at[t->n_pair] = (int)pair_sym;
-    t->pair_apply_at[t->n_pair] = (int)pair_apply;
     t->chunk_at[n] = (int)chunks;
     t->unit_at[n] = (int)units;
     t->sym_at[n] = (int)sym;
     t->apply_at[n] = (int)apply;
-    if (pair_sym + pair_apply > 0x7fffffff || chunks > 0x7fffffff || units > 0x7fffffff || sym > 0x7fffffff || apply > 0x7fffffff) return -1;
+    if (chunks > 0x7fffffff || units > 0x7fffffff || sym + apply > 0x7fffffff) return -1;
     at = up(at + chunks * 8, 1024);
     at = up(at + n * 8, 1024);                                        // inverse norms, arrival counters
     t->tiles = at;
-    at = up(at + (pair_sym + pair_apply) * (int64_t)sizeof(Tile), kUnitBytes);
+    at = up(at + (sym + apply) * (int64_t)sizeof(Tile), kUnitBytes);
     for (int k = 0; k < n; ++k) {
         Mat& m = t->m[k];
         const int64_t big = (int64_t)m.sp * m.lp * 2;
@@ -833,14 +913,16 @@ static int64_t lay_out(const int64_t* offsets, const int64_t* rows, const int64_
     return at;
 }
 
-// Matrices of pair tiles first, then longer ones first, so that the last tiles of a launch are short ones; chunks of kMaxMats per chain.
-static std::vector<int> order_of(const int64_t* rows, const int64_t* cols, int n) {
+static bool is_small(int64_t rows, int64_t cols) {
+    return std::min(rows, cols) <= kSmallS && std::max(rows, cols) <= kSmallCluster * kSmallUnits * kUnit;
+}
+
+// The small matrices or the others; longer ones first, so that the last tiles of a launch are short ones.
+static std::vector<int> order_of(const int64_t* rows, const int64_t* cols, int n, bool small) {
     std::vector<int> o;
     for (int i = 0; i < n; ++i)
-        if (rows[i] > 0 && cols[i] > 0) o.push_back(i);
+        if (rows[i] > 0 && cols[i] > 0 && is_small(rows[i], cols[i]) == small) o.push_back(i);
     std::stable_sort(o.begin(), o.end(), [&](int x, int y) {
-        const bool px = std::min(rows[x], cols[x]) > kTile, py = std::min(rows[y], cols[y]) > kTile;
-        if (px != py) return px;
         return std::max(rows[x], cols[x]) > std::max(rows[y], cols[y]);
     });
     return o;
@@ -857,7 +939,7 @@ static int check_shapes(const int64_t* rows, const int64_t* cols, int n) {
 }
 
 static int64_t workspace_bytes(const int64_t* rows, const int64_t* cols, int n) {
-    const std::vector<int> order = order_of(rows, cols, n);
+    const std::vector<int> order = order_of(rows, cols, n, false);
     std::vector<Table> t(1);
     int64_t most = 0;
     for (size_t from = 0; from < order.size(); from += kMaxMats) {
@@ -924,31 +1006,17 @@ static cudaError_t chain(const Table& t, const void* grad, float* momentum, floa
     const auto two = [](int k) { return ldexpf(1.0f, k); };
     // the workspace as rows of 128 bytes; a box is one unit (its bytes are in the tensor cores' order already)
     CUtensorMap map{};
-    if (t.n_pair && !sidco_internal::byte_map(&map, ws, 128, ws_bytes / 128, 128, 128, kUnit, false))
+    if (!sidco_internal::byte_map(&map, ws, 128, ws_bytes / 128, 128, 128, kUnit, false))
         return cudaErrorNotSupported;
-    const int n_sym = t.pair_sym_at[t.n_pair], n_apply = t.pair_apply_at[t.n_pair];
+    const int n_sym = t.sym_at[t.n], n_apply = t.apply_at[t.n];
     const Tile* tiles = reinterpret_cast<const Tile*>(ws + t.tiles);
     const auto sym = [&](const Chain& c, int products) {
-        if (t.n_pair) {
-            const int pairs = std::min(max_pairs, n_sym * products);
-            const cudaError_t r = launch(pair_kernel<true>, dim3(pairs * 2), kPairThreads, kPairSmem, s, map,
-                                         PairWork{tiles, n_sym, products}, (const Table*)table, ws, c,
-                                         (__nv_bfloat16*)out, timeouts);
-            if (r != cudaSuccess || t.n_pair == t.n) return r;
-        }
-        return launch(product_kernel<true>, dim3(t.sym_at[t.n], products), kProductThreads, kProductSmem, s,
-                      (const Table*)table, ws, c, (__nv_bfloat16*)out, timeouts);
+        return launch(pair_kernel<true>, dim3(2 * std::min(max_pairs, n_sym * products)), kPairThreads, kPairSmem, s, map,
+                      PairWork{tiles, n_sym, products}, (const Table*)table, ws, c, (__nv_bfloat16*)out, timeouts);
     };
     const auto apply = [&](const Chain& c) {
-        if (t.n_pair) {
-            const int pairs = std::min(max_pairs, n_apply);
-            const cudaError_t r = launch(pair_kernel<false>, dim3(pairs * 2), kPairThreads, kPairSmem, s, map,
-                                         PairWork{tiles + n_sym, n_apply, 1}, (const Table*)table, ws, c,
-                                         (__nv_bfloat16*)out, timeouts);
-            if (r != cudaSuccess || t.n_pair == t.n) return r;
-        }
-        return launch(product_kernel<false>, dim3(t.apply_at[t.n]), kProductThreads, kProductSmem, s,
-                      (const Table*)table, ws, c, (__nv_bfloat16*)out, timeouts);
+        return launch(pair_kernel<false>, dim3(2 * std::min(max_pairs, n_apply)), kPairThreads, kPairSmem, s, map,
+                      PairWork{tiles + n_sym, n_apply, 1}, (const Table*)table, ws, c, (__nv_bfloat16*)out, timeouts);
     };
     int done = 0, in = 0;
     while (done < steps) {
@@ -988,6 +1056,27 @@ static cudaError_t chain(const Table& t, const void* grad, float* momentum, floa
     return cudaSuccess;
 }
 
+// Small matrices with equally many CTAs each: a cluster as large as the longest needs.
+template <typename T>
+static cudaError_t small_launch(const SmallMats& mats, int ctas, const void* grad, float* momentum, float mu, int nesterov,
+                                int steps, float eps, uint16_t* out, int* timeouts, cudaStream_t s) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(mats.n * ctas);
+    cfg.blockDim = dim3(kSmallThreads);
+    cfg.dynamicSmemBytes = kSmallSmem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = ctas;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, small_kernel<T>, mats, (const T*)grad, momentum, mu, nesterov, steps, eps,
+                                             (__nv_bfloat16*)out, timeouts);
+    if (e == cudaSuccess) sidco_internal::note_launch();
+    return e;
+}
+
 }  // namespace sidco_ortho
 
 int sidco_internal::orthogonalize_timeouts(int* count) {
@@ -1009,16 +1098,16 @@ int sidco_orthogonalize(const void* grad, int grad_type, float* momentum, float 
     if (rc) return rc;
     if (grad_type < SIDCO_T_F32 || grad_type > SIDCO_T_F16) return SIDCO_E_TYPE;
     if (steps < 1 || steps > SIDCO_ORTHO_MAX_STEPS || !(eps >= 0.0f) || !(mu >= 0.0f && mu < 1.0f)) return SIDCO_E_PARAMS;
-    const std::vector<int> order = order_of(rows, cols, n_mats);
-    if (order.empty()) return 0;
-    if (!grad || !out_bf16 || !offsets || !workspace) return SIDCO_E_NULL;
-    for (int i : order)
+    const std::vector<int> order = order_of(rows, cols, n_mats, false), small = order_of(rows, cols, n_mats, true);
+    if (order.empty() && small.empty()) return 0;
+    if (!grad || !out_bf16 || !offsets || (!workspace && !order.empty())) return SIDCO_E_NULL;
+    for (int i = 0; i < n_mats; ++i)
         if (offsets[i] < 0) return SIDCO_E_SEGMENTS;
     const uintptr_t size = grad_type == SIDCO_T_F32 ? 4 : 2;
     if ((uintptr_t)grad % size || (uintptr_t)momentum % 4 || (uintptr_t)out_bf16 % 2) return SIDCO_E_ALIGN;
     const int64_t need = sidco_ortho::workspace_bytes(rows, cols, n_mats);
     if (need < 0) return (int)need;
-    if ((uintptr_t)workspace % 256 || workspace_bytes < (size_t)need) return SIDCO_E_WORKSPACE;
+    if (need > 0 && ((uintptr_t)workspace % 256 || workspace_bytes < (size_t)need)) return SIDCO_E_WORKSPACE;
     static int pair_count[64] = {};           // pairs of CTAs that are resident at once
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
@@ -1027,8 +1116,9 @@ int sidco_orthogonalize(const void* grad, int grad_type, float* momentum, float 
     if (!pair_count[dev]) {                  // (setting it twice from two threads is harmless)
         const auto most = cudaFuncAttributeMaxDynamicSharedMemorySize;
         int pairs = 0;
-        if ((e = cudaFuncSetAttribute(product_kernel<true>, most, kProductSmem)) != cudaSuccess ||
-            (e = cudaFuncSetAttribute(product_kernel<false>, most, kProductSmem)) != cudaSuccess ||
+        if ((e = cudaFuncSetAttribute(small_kernel<float>, most, kSmallSmem)) != cudaSuccess ||
+            (e = cudaFuncSetAttribute(small_kernel<__nv_bfloat16>, most, kSmallSmem)) != cudaSuccess ||
+            (e = cudaFuncSetAttribute(small_kernel<__half>, most, kSmallSmem)) != cudaSuccess ||
             (e = cudaFuncSetAttribute(pair_kernel<true>, most, kPairSmem)) != cudaSuccess ||
             (e = cudaFuncSetAttribute(pair_kernel<false>, most, kPairSmem)) != cudaSuccess ||
             (e = resident_pairs(&pairs)) != cudaSuccess)
@@ -1037,11 +1127,26 @@ int sidco_orthogonalize(const void* grad, int grad_type, float* momentum, float 
     }
     int* timeouts = nullptr;
     if ((e = cudaGetSymbolAddress((void**)&timeouts, g_timeouts)) != cudaSuccess) return (int)e;
+    cudaStream_t s = (cudaStream_t)stream;
+    for (size_t from = 0; from < small.size();) {
+        SmallMats mats;
+        const int64_t longest = std::max(rows[small[from]], cols[small[from]]);
+        int ctas = 1;
+        while ((int64_t)ctas * kSmallUnits * kUnit < longest) ctas *= 2;
+        for (mats.n = 0; from < small.size() && mats.n < kMaxMats; ++from, ++mats.n)
+            mats.m[mats.n] = {offsets[small[from]], (int)rows[small[from]], (int)cols[small[from]]};
+        if (grad_type == SIDCO_T_F32)
+            e = small_launch<float>(mats, ctas, grad, momentum, mu, nesterov, steps, eps, out_bf16, timeouts, s);
+        else if (grad_type == SIDCO_T_BF16)
+            e = small_launch<__nv_bfloat16>(mats, ctas, grad, momentum, mu, nesterov, steps, eps, out_bf16, timeouts, s);
+        else
+            e = small_launch<__half>(mats, ctas, grad, momentum, mu, nesterov, steps, eps, out_bf16, timeouts, s);
+        if (e != cudaSuccess) return (int)e;
+    }
     std::vector<Table> t(1);
     for (size_t from = 0; from < order.size(); from += kMaxMats) {
         lay_out(offsets, rows, cols, order.data() + from, (int)std::min<size_t>(kMaxMats, order.size() - from), t.data());
         uint8_t* ws = (uint8_t*)workspace;
-        cudaStream_t s = (cudaStream_t)stream;
         if (grad_type == SIDCO_T_F32)
             e = chain<float>(t[0], grad, momentum, mu, nesterov, steps, eps, out_bf16, ws, need, pair_count[dev], timeouts, s);
         else if (grad_type == SIDCO_T_BF16)

@@ -73,7 +73,7 @@ def check(shapes, mu=0.95, nesterov=True, steps=5, dtype="float32", gap=3, scale
 
 @pytest.mark.parametrize("shape", [(1, 1), (1, 7), (7, 1), (2, 2), (16, 27), (10, 64), (64, 10), (33, 65), (64, 64), (64, 576),
                                    (65, 64), (127, 130), (128, 128), (129, 128), (10, 512), (100, 1000), (1000, 100),
-                                   (200, 200), (257, 300), (300, 257), (64, 3000), (512, 520), (640, 385)])
+                                   (200, 200), (257, 300), (300, 257), (64, 3000), (512, 520), (640, 385), (128, 2048), (2048, 128), (100, 2049), (17, 1030)])
 def test_single_matrices(shape):
     check([shape])
 
@@ -100,6 +100,7 @@ def test_a_model_of_many_shapes_in_one_call():
 
 def test_more_matrices_than_one_chain_takes():
     check([(3 + i % 20, 4 + i % 33) for i in range(300)])
+    check([(129 + i % 3, 130 + i % 5) for i in range(131)])
 
 
 def test_scales_far_from_one():

@@ -107,18 +107,21 @@ def test_orthogonalize_refuses(B):
     assert call(t=7) == -13
     assert call(mu=1.0) == -6 and call(mu=-0.1) == -6 and call(mu=float("nan")) == -6
     assert call(steps=0) == -6 and call(steps=33) == -6 and call(eps=-1.0) == -6
-    assert call(grad=None) == -1 and call(out=None) == -1 and call(ws=None) == -1
+    big = dict(rows=(300,), cols=(200,))                          # (small matrices need no workspace)
+    assert call(grad=None) == -1 and call(out=None) == -1 and call(ws=None, **big) == -1
     assert call(off=(-4,)) == -2
     assert call(grad=P + 2) == -14 and call(mom=P + 1) == -14 and call(out=P + 1) == -14
-    need = B.sidco_orthogonalize_workspace_bytes([8], [8])
-    assert call(n=need - 1) == -8 and call(ws=4 * P + 8) == -8
+    need = B.sidco_orthogonalize_workspace_bytes([300], [200])
+    assert call(n=need - 1, **big) == -8 and call(ws=4 * P + 8, **big) == -8
+    assert B.sidco_orthogonalize_workspace_bytes([128, 2048], [2048, 5]) == 0
     with pytest.raises(ValueError):
         f(P, None, 0.9, True, [0], [8, 8], [8], 5, P, P, 1 << 30, grad_type=0, stream=0)
     with pytest.raises(B.SidcoError):
         B.sidco_orthogonalize_workspace_bytes([1 << 23], [4])
     assert B.sidco_orthogonalize_workspace_bytes([], []) == 0
     # a chain's workspace is reused by the next: many matrices cost no more than the largest chain
-    assert B.sidco_orthogonalize_workspace_bytes([8] * 128, [8] * 128) == B.sidco_orthogonalize_workspace_bytes([8] * 256, [8] * 256)
+    assert B.sidco_orthogonalize_workspace_bytes([200] * 128, [150] * 128) == \
+        B.sidco_orthogonalize_workspace_bytes([200] * 256, [150] * 256) > 0
 
 
 def test_error_texts_name_the_reason(B):
