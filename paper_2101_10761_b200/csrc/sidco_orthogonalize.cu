@@ -78,7 +78,8 @@ struct __align__(16) Tile {
     int spu, ku;                      // units along the padded s, along s
     int lu;                           // units along l
     uint16_t ti, tj;                  // row, column
-    int mat, pad[3];
+    int rows, cols;                   // of the caller's matrix, which lies
+    int64_t offset;                   // here in the flat vectors
 };
 
 __device__ __forceinline__ int find(const int* at, int n, int i) {
@@ -96,39 +97,78 @@ __device__ __forceinline__ float widen(__half x) { return __half2float(x); }
 
 // ---------------------------------------------------------------------------------------------- momentum, norm
 
-// M <- mu M + G and the sum of squares of U per chunk of 16384 elements (fp64: gradients may be tiny or huge).  The
-// last chunk of a matrix to arrive adds the chunks' sums in their order.
+// Eight neighbours: fp32 32 bytes, 16-bit types 16.
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, float (&x)[8]) {
+    uint32_t w[2 * sizeof(T)];
+    if constexpr (sizeof(T) == 4) {
+        asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                     : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
+                     : "l"(p));
+    } else {
+        *reinterpret_cast<uint4*>(w) = *reinterpret_cast<const uint4*>(p);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = widen(reinterpret_cast<const T*>(w)[i]);
+}
+
+__device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
+    asm volatile("st.global.v8.f32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]),
+                 "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7])
+                 : "memory");
+}
+
+// M <- mu M + G and the sum of squares of U per chunk of 16384 elements (fp64: gradients may be tiny or huge).  Chunks
+// start at multiples of eight elements of the flat vector; eights that lie inside the matrix move in one access where
+// the vectors' bases allow it (`vec`).  The last chunk of a matrix to arrive adds the chunks' sums in their order.
 template <typename T>
 __global__ void __launch_bounds__(256) momentum_kernel(const __grid_constant__ Table t, const T* __restrict__ grad,
                                                        float* __restrict__ momentum, float mu, int nesterov, float eps,
-                                                       double* __restrict__ partial, int* __restrict__ arrived,
+                                                       int vec, double* __restrict__ partial, int* __restrict__ arrived,
                                                        float* __restrict__ inv_norm) {
     __shared__ double s_sum[8];
     __shared__ int s_last;
     launch_dependents();
     const int i = find(t.chunk_at, t.n, blockIdx.x), chunk = blockIdx.x - t.chunk_at[i];
     const Mat& m = t.m[i];
-    const int64_t n = (int64_t)m.rows * m.cols, from = (int64_t)chunk * kChunk;
-    const int64_t to = min(n, from + kChunk);
+    const int64_t lo = m.offset, hi = lo + (int64_t)m.rows * m.cols, from = (lo & ~(int64_t)7) + (int64_t)chunk * kChunk;
     double sum = 0.0;
-    for (int64_t e0 = from + threadIdx.x; e0 < to; e0 += 256 * 8) {
-        float g[8], v[8];
+    constexpr int U = 4;
+    for (int o0 = threadIdx.x; o0 < kChunk / 8; o0 += 256 * U) {
+        float g[U][8], v[U][8] = {};
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const int64_t e = e0 + k * 256;
-            g[k] = e < to ? widen(grad[m.offset + e]) : 0.0f;
-            v[k] = e < to && momentum ? momentum[m.offset + e] : 0.0f;
+        for (int u = 0; u < U; ++u) {
+            const int64_t e = from + (o0 + u * 256) * 8;
+            if (vec && e >= lo && e + 8 <= hi) {
+                load8(grad + e, g[u]);
+                if (momentum) load8(momentum + e, v[u]);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const bool in = e + k >= lo && e + k < hi;
+                    g[u][k] = in ? widen(grad[e + k]) : 0.0f;
+                    v[u][k] = in && momentum ? momentum[e + k] : 0.0f;
+                }
+            }
         }
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const int64_t e = e0 + k * 256;
-            float u = g[k];
+        for (int u = 0; u < U; ++u) {
+            const int64_t e = from + (o0 + u * 256) * 8;
             if (momentum) {
-                const float mom = fmaf(mu, v[k], g[k]);
-                if (e < to) momentum[m.offset + e] = mom;
-                u = nesterov ? fmaf(mu, mom, g[k]) : mom;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[u][k] = fmaf(mu, v[u][k], g[u][k]);
+                if (vec && e >= lo && e + 8 <= hi) {
+                    store8(momentum + e, v[u]);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        if (e + k >= lo && e + k < hi) momentum[e + k] = v[u][k];
+                }
+#pragma unroll
+                for (int k = 0; k < 8; ++k) g[u][k] = nesterov ? fmaf(mu, v[u][k], g[u][k]) : v[u][k];
             }
-            sum += (double)u * (double)u;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) sum += (double)g[u][k] * (double)g[u][k];
         }
     }
 #pragma unroll
@@ -182,23 +222,30 @@ __device__ __forceinline__ uint4 pack8(const float (&v)[8]) {
     return w;
 }
 
-// One CTA per unit: U again (from what the momentum pass left), scaled, transposed if tall, split in two fp16 parts.
+template <typename T>
+__device__ __forceinline__ void load4(const T* p, float (&x)[4]) {
+    uint32_t w[sizeof(T)];
+    if constexpr (sizeof(T) == 4) *reinterpret_cast<uint4*>(w) = *reinterpret_cast<const uint4*>(p);
+    else *reinterpret_cast<uint2*>(w) = *reinterpret_cast<const uint2*>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = widen(reinterpret_cast<const T*>(w)[i]);
+}
+
+// One CTA per unit: U again (from what the momentum pass left), scaled, transposed if tall, split in two fp16 parts.  The
+// units are taken from the last to the first: what the momentum pass touched last is still in L2.
 template <typename T>
 __global__ void __launch_bounds__(256) normalize_kernel(const __grid_constant__ Table t, const T* __restrict__ grad,
                                                         const float* __restrict__ momentum, float mu, int nesterov,
-                                                        const float* __restrict__ inv_norm, uint8_t* __restrict__ ws,
-                                                        Table* __restrict__ table_out) {
+                                                        int quads, const float* __restrict__ inv_norm,
+                                                        uint8_t* __restrict__ ws) {
     __shared__ float s_u[kUnit][kUnit + 1];
     launch_dependents();
-    const int i = find(t.unit_at, t.n, blockIdx.x), u = blockIdx.x - t.unit_at[i];
+    const int block = gridDim.x - 1 - blockIdx.x, i = find(t.unit_at, t.n, block), u = block - t.unit_at[i];
     const Mat& m = t.m[i];
     const int rb = u % (m.sp / kUnit), cb = u / (m.sp / kUnit);
     const bool tall = m.rows > m.cols;
     wait_prerequisites();
-    // the kernels behind this one read the table from memory
-    if (blockIdx.x == 0)
-        for (int w = threadIdx.x; w < (int)(sizeof(Table) / 4); w += 256)
-            reinterpret_cast<int*>(table_out)[w] = reinterpret_cast<const int*>(&t)[w];
+    // (the tiles of the kernels behind this one)
     const int n_sym = t.sym_at[t.n], n_apply = t.apply_at[t.n];
     for (int w = blockIdx.x * 256 + threadIdx.x; w < n_sym + n_apply; w += gridDim.x * 256) {
         const bool sym = w < n_sym;
@@ -214,7 +261,9 @@ __global__ void __launch_bounds__(256) normalize_kernel(const __grid_constant__ 
         d.spu = q.sp / kUnit;
         d.ku = (q.s + kUnit - 1) / kUnit;
         d.lu = q.lp / kUnit;
-        d.mat = j;
+        d.rows = q.rows;
+        d.cols = q.cols;
+        d.offset = q.offset;
         if (sym) {
             triangle(tile, &d.ti, &d.tj);
         } else {
@@ -225,25 +274,37 @@ __global__ void __launch_bounds__(256) normalize_kernel(const __grid_constant__ 
         reinterpret_cast<Tile*>(ws + t.tiles)[w] = d;
     }
     const float inv = __ldcg(inv_norm + i);
-    // neighbours along the matrix's own rows: X's columns, or X's rows if tall
-    const int along = threadIdx.x & 63, across0 = threadIdx.x >> 6;
-    const int my_r = (tall ? rb : cb) * kUnit + along;                // index along the matrix's row
-#pragma unroll 4
-    for (int k = 0; k < 16; ++k) {
-        const int across = across0 + k * 4;
-        const int my_a = (tall ? cb : rb) * kUnit + across;
-        float x = 0.0f;
-        if (my_a < m.rows && my_r < m.cols) {
-            const int64_t e = m.offset + (int64_t)my_a * m.cols + my_r;
-            if (momentum) {
-                x = __ldcg(momentum + e);
-                if (nesterov) x = fmaf(mu, x, widen(grad[e]));
-            } else {
-                x = widen(grad[e]);
+    // four neighbours along the matrix's own rows (X's columns, or X's rows if tall) per thread and step
+    const int along = (threadIdx.x & 15) * 4, across0 = threadIdx.x >> 4;
+    const int my_r = (tall ? rb : cb) * kUnit + along;
+    const bool fours = quads && ((m.offset | m.cols) & 3) == 0;
+    float x[4][4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int my_a = (tall ? cb : rb) * kUnit + across0 + k * 16;
+        const int64_t e = m.offset + (int64_t)my_a * m.cols + my_r;
+        float g[4] = {}, v[4] = {};
+        if (my_a < m.rows && fours && my_r < m.cols) {
+            if (momentum) *reinterpret_cast<float4*>(v) = __ldcg(reinterpret_cast<const float4*>(momentum + e));
+            if (!momentum || nesterov) load4(grad + e, g);
+        } else if (my_a < m.rows) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (my_r + j >= m.cols) continue;
+                if (momentum) v[j] = __ldcg(momentum + e + j);
+                if (!momentum || nesterov) g[j] = widen(grad[e + j]);
             }
         }
-        if (tall) s_u[along][across] = x; else s_u[across][along] = x;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[k][j] = !momentum ? g[j] : nesterov ? fmaf(mu, v[j], g[j]) : v[j];
     }
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int across = across0 + k * 16;
+            if (tall) s_u[along + j][across] = x[k][j]; else s_u[across][along + j] = x[k][j];
+        }
     __syncthreads();
     const float scale = inv * (float)(1 << kX);
     const int64_t unit = ((int64_t)cb * (m.sp / kUnit) + rb) * kUnitBytes;
@@ -304,10 +365,10 @@ __device__ __forceinline__ void epilogue_sync() { asm volatile("bar.sync 1, 128;
 
 template <bool kSym>
 __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2)
-    pair_kernel(const __grid_constant__ CUtensorMap map, const PairWork w, const Table* t, uint8_t* ws,
+    pair_kernel(const __grid_constant__ CUtensorMap map, const PairWork w, uint8_t* ws,
                 const __grid_constant__ Chain c, __nv_bfloat16* __restrict__ out, int* timeouts) {
     extern __shared__ uint8_t s_raw[];
-    __shared__ uint64_t s_full[kPairStages], s_free[kPairStages], s_sums[2], s_taken[2];
+    __shared__ uint64_t s_full[kPairStages], s_free[kPairStages], s_sums[2], s_taken[2], s_plus[2];
     __shared__ uint32_t s_tmem;
     __shared__ int s_failed;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -323,6 +384,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2)
         for (int i = 0; i < 2; ++i) {
             mbar_init(smem_addr(&s_sums[i]), 1);
             mbar_init(smem_addr(&s_taken[i]), 8);                     // four warps of both CTAs
+            mbar_init(smem_addr(&s_plus[i]), 1);
         }
         s_failed = 0;
         mbar_init_fence();
@@ -409,24 +471,24 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2)
         const uint32_t out0 = stage0 + kPairStages * kPairStageBytes;
         uint8_t* out_smem = smem + kPairStages * kPairStageBytes;
         const uint32_t taken[2] = {in_cta(smem_addr(&s_taken[0]), 0), in_cta(smem_addr(&s_taken[1]), 0)};
-        int n = 0, part = 0;
+        int n = 0, part = 0, fetched = 0;
         for (int i = first; i < total; i += n_pairs, ++n) {
             const Tile d = w.tiles[i % w.n];
             const Product& p = c.p[kSym ? i / w.n : 0];
             const int small = d.spu * d.spu, buf = n & 1;
             const int rb = d.ti * 4 + rank * 2;                       // first unit row of this CTA's part
-            const bool mirror = kSym && d.ti != d.tj;
-            const uint8_t* plus = nullptr;
-            if (kSym && p.plus >= 0)
-                plus = ws + (int64_t)(d.small + p.plus * small + rb + (row >> 6)) * kUnitBytes;
-            uint4 e[2][4];                                            // 32 columns of `plus`, fetched one step ahead
-            const auto fetch = [&](int q, uint4 (&to)[4]) {
-                const uint8_t* u = plus + (int64_t)(d.tj * 4 + (q >> 1)) * d.spu * kUnitBytes;
-#pragma unroll
-                for (int o = 0; o < 4; ++o)
-                    to[o] = __ldcg(reinterpret_cast<const uint4*>(u + in_unit(row & 63, (q & 1) * 4 + o)));
+            const bool mirror = kSym && d.ti != d.tj, tall = d.rows > d.cols;
+            // 64 columns of the matrix to add are brought to where their sums will be written, one part ahead
+            const bool plus = kSym && p.plus >= 0;
+            const auto fetch = [&](int cu, int to) {                  // (the buffer's last stores are done reading)
+                asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+                const uint32_t bar = smem_addr(&s_plus[to]);
+                mbar_expect_tx(bar, 2 * kUnitBytes);
+                bulk_load(out0 + to * kOutBytes,
+                          ws + (int64_t)(d.small + p.plus * small + (d.tj * 4 + cu) * d.spu + rb) * kUnitBytes,
+                          2 * kUnitBytes, bar);
             };
-            if (kSym && plus) fetch(0, e[0]);
+            if (plus && e0) fetch(0, part & 1);
             const float gamma = kSym && d.ti == d.tj ? p.gamma : 0.0f;
             const int diagonal = (int)rank * 128 + row;
             const bool ok = mbar_wait(smem_addr(&s_sums[buf]), (n >> 1) & 1, &s_failed);
@@ -437,14 +499,19 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2)
             for (int cu = 0; cu < 4; ++cu, ++part) {
                 uint8_t* img = out_smem + (part & 1) * kOutBytes;
                 const uint32_t img_addr = out0 + (part & 1) * kOutBytes;
-                // (the stores that read this buffer two parts ago are done reading)
-                if (e0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
-                epilogue_sync();
+                if (plus) {
+                    mbar_wait(smem_addr(&s_plus[part & 1]), (fetched >> 1) & 1, &s_failed);
+                    ++fetched;
+                    __syncwarp();
+                } else {
+                    // the stores that read this buffer two parts ago are done reading
+                    if (e0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+                    epilogue_sync();
+                }
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const int q = cu * 2 + h;
                     uint32_t acc[32];
-                    if (kSym && plus && q < 7) fetch(q + 1, e[h ^ 1]);
                     tmem_load32(tmem + buf * kPairTile + ((uint32_t)(quarter * 32) << 16) + q * 32, acc);
                     if (kSym || !c.last) {
                         const float alpha = kSym ? p.alpha : c.alpha;
@@ -453,8 +520,10 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2)
                             float v[8];
 #pragma unroll
                             for (int j = 0; j < 8; ++j) v[j] = alpha * __uint_as_float(acc[o * 8 + j]);
+                            uint4* at = reinterpret_cast<uint4*>(img + (row >> 6) * kUnitBytes + in_unit(row & 63, h * 4 + o));
                             if (kSym && plus) {
-                                const __half2* x = reinterpret_cast<const __half2*>(&e[h][o]);
+                                const uint4 e = *at;
+                                const __half2* x = reinterpret_cast<const __half2*>(&e);
 #pragma unroll
                                 for (int j = 0; j < 4; ++j) {
                                     const float2 f = __half22float2(x[j]);
@@ -468,7 +537,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2)
                                 for (int j = 0; j < 8; ++j) v[j] += diagonal == q * 32 + o * 8 + j ? gamma : 0.0f;
                             }
                             const uint4 packed = pack8(v);
-                            *reinterpret_cast<uint4*>(img + (row >> 6) * kUnitBytes + in_unit(row & 63, h * 4 + o)) = packed;
+                            *at = packed;
                             if (mirror) {
                                 const __half* hv = reinterpret_cast<const __half*>(&packed);
 #pragma unroll
@@ -479,7 +548,6 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2)
                             }
                         }
                     } else {
-                        const bool tall = t->m[d.mat].rows > t->m[d.mat].cols;
                         __nv_bfloat16* s_out = reinterpret_cast<__nv_bfloat16*>(img);
 #pragma unroll
                         for (int j = 0; j < 32; ++j) {
@@ -507,24 +575,32 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2)
                                                img_addr + (2 + u) * kUnitBytes, kUnitBytes);
                         }
                         bulk_store_commit();
+                        if (plus && cu < 3) fetch(cu + 1, (part & 1) ^ 1);
                     }
                 } else {
                     epilogue_sync();
-                    const Mat& m = t->m[d.mat];
-                    const bool tall = m.rows > m.cols;
                     const __nv_bfloat16* s_out = reinterpret_cast<const __nv_bfloat16*>(img);
                     const int r_x = rb * kUnit, c_x = (d.tj * 4 + cu) * kUnit;   // first row, column of X
                     const int a0 = tall ? c_x : r_x, n0 = tall ? r_x : c_x;
                     const int lines = tall ? 64 : 128, len = tall ? 128 : 64, pitch = tall ? 130 : 66;
-                    const bool even = ((m.offset | m.cols) & 1) == 0 && ((uintptr_t)out & 3) == 0;
-                    for (int a = quarter; a < lines && a0 + a < m.rows; a += 4) {
-                        __nv_bfloat16* to = out + m.offset + (int64_t)(a0 + a) * m.cols + n0;
-                        if (even) {
-                            for (int k = lane * 2; k < len && n0 + k < m.cols; k += 64)
-                                *reinterpret_cast<uint32_t*>(to + k) = *reinterpret_cast<const uint32_t*>(s_out + a * pitch + k);
-                        } else {
-                            for (int k = lane; k < len && n0 + k < m.cols; k += 32) to[k] = s_out[a * pitch + k];
+                    __nv_bfloat16* to = out + d.offset + (int64_t)a0 * d.cols + n0;
+                    const int n_lines = min(lines, d.rows - a0), n_len = min(len, d.cols - n0);
+                    const bool even = ((d.offset | d.cols) & 1) == 0 && ((uintptr_t)out & 3) == 0;
+                    if (even) {
+                        const int k = lane * 2;
+#pragma unroll 8
+                        for (int a = quarter; a < n_lines; a += 4) {
+                            const __nv_bfloat16* from = s_out + a * pitch;
+                            __nv_bfloat16* line = to + (int64_t)a * d.cols;
+                            if (k < n_len)
+                                *reinterpret_cast<uint32_t*>(line + k) = *reinterpret_cast<const uint32_t*>(from + k);
+                            if (k + 64 < n_len)
+                                *reinterpret_cast<uint32_t*>(line + k + 64) = *reinterpret_cast<const uint32_t*>(from + k + 64);
                         }
+                    } else {
+#pragma unroll 4
+                        for (int a = quarter; a < n_lines; a += 4)
+                            for (int k = lane; k < n_len; k += 32) to[(int64_t)a * d.cols + k] = s_out[a * pitch + k];
                     }
                     if (e0) bulk_store_commit();                      // (an empty group keeps the count of parts)
                 }
@@ -867,7 +943,7 @@ static int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
 // Lays the matrices order[0..n) out in the workspace and numbers the CTAs of the passes.  Returns the bytes needed.
 static int64_t lay_out(const int64_t* offsets, const int64_t* rows, const int64_t* cols, const int* order, int n, Table* t) {
-    int64_t at = up(sizeof(Table), 1024);
+    int64_t at = 0;
     int64_t chunks = 0, units = 0, sym = 0, apply = 0;
     t->n = n;
     for (int k = 0; k < n; ++k) {
@@ -885,7 +961,7 @@ static int64_t lay_out(const int64_t* offsets, const int64_t* rows, const int64_
         t->sym_at[k] = (int)sym;
         t->apply_at[k] = (int)apply;
         m.partial0 = (int)chunks;
-        m.n_chunks = (int)((r * c + kChunk - 1) / kChunk);
+        m.n_chunks = (int)((r * c + 7 + kChunk - 1) / kChunk);          // (up to seven elements before the first)
         chunks += m.n_chunks;
         units += (int64_t)(m.sp / kUnit) * (m.lp / kUnit);
         const int64_t mt = m.sp / kPairTile;
@@ -988,20 +1064,20 @@ template <typename T>
 static cudaError_t chain(const Table& t, const void* grad, float* momentum, float mu, int nesterov, int steps, float eps,
                          uint16_t* out, uint8_t* ws, int64_t ws_bytes, int max_pairs, int* timeouts, cudaStream_t s) {
     cudaError_t e;
-    int64_t at = up(sizeof(Table), 1024);
-    Table* table = reinterpret_cast<Table*>(ws);
-    double* partial = reinterpret_cast<double*>(ws + at);
-    at = up(at + (int64_t)t.chunk_at[t.n] * 8, 1024);
+    double* partial = reinterpret_cast<double*>(ws);
+    const int64_t at = up((int64_t)t.chunk_at[t.n] * 8, 1024);
     float* inv_norm = reinterpret_cast<float*>(ws + at);
     int* arrived = reinterpret_cast<int*>(ws + at) + t.n;
     if ((e = cudaMemsetAsync(arrived, 0, t.n * sizeof(int), s)) != cudaSuccess) return e;
+    // whole sectors per lane (and with them 16-byte accesses of the second pass)
+    const int vec = (uintptr_t)grad % (8 * sizeof(T)) == 0 && (uintptr_t)momentum % 32 == 0;
     // (a plain launch: the first kernel waits for everything before it)
-    momentum_kernel<T><<<t.chunk_at[t.n], 256, 0, s>>>(t, (const T*)grad, momentum, mu, nesterov, eps, partial, arrived,
-                                                       inv_norm);
+    momentum_kernel<T><<<t.chunk_at[t.n], 256, 0, s>>>(t, (const T*)grad, momentum, mu, nesterov, eps, vec,
+                                                       partial, arrived, inv_norm);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
     sidco_internal::note_launch();
     if ((e = launch(normalize_kernel<T>, dim3(t.unit_at[t.n]), 256, 0, s, t, (const T*)grad, (const float*)momentum, mu,
-                    nesterov, (const float*)inv_norm, ws, table)) != cudaSuccess)
+                    nesterov, vec, (const float*)inv_norm, ws)) != cudaSuccess)
         return e;
     const auto two = [](int k) { return ldexpf(1.0f, k); };
     // the workspace as rows of 128 bytes; a box is one unit (its bytes are in the tensor cores' order already)
@@ -1012,11 +1088,11 @@ static cudaError_t chain(const Table& t, const void* grad, float* momentum, floa
     const Tile* tiles = reinterpret_cast<const Tile*>(ws + t.tiles);
     const auto sym = [&](const Chain& c, int products) {
         return launch(pair_kernel<true>, dim3(2 * std::min(max_pairs, n_sym * products)), kPairThreads, kPairSmem, s, map,
-                      PairWork{tiles, n_sym, products}, (const Table*)table, ws, c, (__nv_bfloat16*)out, timeouts);
+                      PairWork{tiles, n_sym, products}, ws, c, (__nv_bfloat16*)out, timeouts);
     };
     const auto apply = [&](const Chain& c) {
         return launch(pair_kernel<false>, dim3(2 * std::min(max_pairs, n_apply)), kPairThreads, kPairSmem, s, map,
-                      PairWork{tiles + n_sym, n_apply, 1}, (const Table*)table, ws, c, (__nv_bfloat16*)out, timeouts);
+                      PairWork{tiles + n_sym, n_apply, 1}, ws, c, (__nv_bfloat16*)out, timeouts);
     };
     int done = 0, in = 0;
     while (done < steps) {
