@@ -47,7 +47,8 @@ constexpr int kP = 10;                // products of two or three B (<= 41)
 
 constexpr int kUnit = 64;             // units of 64 x 64
 constexpr int kUnitBytes = kUnit * kUnit * 2;
-constexpr int kPairTile = 256;       // products of larger matrices: tiles of 256 x 256
+constexpr int kRows = 256;           // products of larger matrices: tiles of 256 rows x 256 or 128 columns
+constexpr int kMostPairs = 74;        // pairs of SMs of the device
 constexpr int kMaxMats = 128;         // matrices of one chain of launches
 constexpr int kChunk = 16384;         // elements of a matrix per CTA of the momentum pass
 
@@ -68,11 +69,12 @@ struct Table {
     int unit_at[kMaxMats + 1];        // normalisation,
     int sym_at[kMaxMats + 1];         // first tile of every matrix: symmetric products,
     int apply_at[kMaxMats + 1];       // applications
+    int sym_width, apply_width;       // columns of their tiles
     int64_t tiles;                    // bytes into the workspace: Tile[], symmetric products, then applications
     Mat m[kMaxMats];
 };
 
-// A 256 x 256 tile of a pair of CTAs; matrices in units from the start of the workspace.
+// A tile of a pair of CTAs: row ti * 256, column tj * width; matrices in units from the start of the workspace.
 struct __align__(16) Tile {
     int x_hi, x_lo, x_next, small;
     int spu, ku;                      // units along the padded s, along s
@@ -122,7 +124,7 @@ __device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
 // start at multiples of eight elements of the flat vector; eights that lie inside the matrix move in one access where
 // the vectors' bases allow it (`vec`).  The last chunk of a matrix to arrive adds the chunks' sums in their order.
 template <typename T>
-__global__ void __launch_bounds__(256) momentum_kernel(const __grid_constant__ Table t, const T* __restrict__ grad,
+__global__ void __launch_bounds__(256, 4) momentum_kernel(const __grid_constant__ Table t, const T* __restrict__ grad,
                                                        float* __restrict__ momentum, float mu, int nesterov, float eps,
                                                        int vec, double* __restrict__ partial, int* __restrict__ arrived,
                                                        float* __restrict__ inv_norm) {
@@ -132,8 +134,9 @@ __global__ void __launch_bounds__(256) momentum_kernel(const __grid_constant__ T
     const int i = find(t.chunk_at, t.n, blockIdx.x), chunk = blockIdx.x - t.chunk_at[i];
     const Mat& m = t.m[i];
     const int64_t lo = m.offset, hi = lo + (int64_t)m.rows * m.cols, from = (lo & ~(int64_t)7) + (int64_t)chunk * kChunk;
-    double sum = 0.0;
-    constexpr int U = 4;
+    double sums[4] = {};
+    constexpr int U = 2;
+#pragma unroll 1
     for (int o0 = threadIdx.x; o0 < kChunk / 8; o0 += 256 * U) {
         float g[U][8], v[U][8] = {};
 #pragma unroll
@@ -168,9 +171,10 @@ __global__ void __launch_bounds__(256) momentum_kernel(const __grid_constant__ T
                 for (int k = 0; k < 8; ++k) g[u][k] = nesterov ? fmaf(mu, v[u][k], g[u][k]) : v[u][k];
             }
 #pragma unroll
-            for (int k = 0; k < 8; ++k) sum += (double)g[u][k] * (double)g[u][k];
+            for (int k = 0; k < 8; ++k) sums[k & 3] = fma((double)g[u][k], (double)g[u][k], sums[k & 3]);
         }
     }
+    double sum = (sums[0] + sums[1]) + (sums[2] + sums[3]);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_down_sync(0xffffffffu, sum, o);
     if ((threadIdx.x & 31) == 0) s_sum[threadIdx.x >> 5] = sum;
@@ -199,13 +203,14 @@ __global__ void __launch_bounds__(256) momentum_kernel(const __grid_constant__ T
     }
 }
 
-// Tile `i` of the lower triangle, row by row.
-__device__ __forceinline__ void triangle(int i, uint16_t* row, uint16_t* col) {
-    int r = (int)((sqrtf(8.0f * i + 1.0f) - 1.0f) * 0.5f);
-    while ((r + 1) * (r + 2) / 2 <= i) ++r;
-    while (r * (r + 1) / 2 > i) --r;
+// Tile `i` of those that cover the lower triangle, row by row: row r has (r + 1) * per tiles (per = 256 / width).
+__device__ __forceinline__ void triangle(int i, int per, uint16_t* row, uint16_t* col) {
+    const int q = i / per;
+    int r = (int)((sqrtf(8.0f * q + 1.0f) - 1.0f) * 0.5f);
+    while ((r + 1) * (r + 2) / 2 <= q) ++r;
+    while (r * (r + 1) / 2 > q) --r;
     *row = (uint16_t)r;
-    *col = (uint16_t)(i - r * (r + 1) / 2);
+    *col = (uint16_t)(i - r * (r + 1) / 2 * per);
 }
 
 // Eight neighbours of a row of a unit: where they lie in the swizzled image.
@@ -265,9 +270,9 @@ __global__ void __launch_bounds__(256) normalize_kernel(const __grid_constant__ 
         d.cols = q.cols;
         d.offset = q.offset;
         if (sym) {
-            triangle(tile, &d.ti, &d.tj);
+            triangle(tile, kRows / t.sym_width, &d.ti, &d.tj);
         } else {
-            const int mt = q.sp / kPairTile;
+            const int mt = q.sp / kRows;
             d.ti = (uint16_t)(tile % mt);
             d.tj = (uint16_t)(tile / mt);
         }
@@ -342,18 +347,18 @@ struct Chain {
 
 // ---------------------------------------------------------------------------------------------- pair tiles
 //
-// Matrices with s > 128: 256 x 256 tiles, each by a cluster of two CTAs on two SMs (one tcgen05 product over both: every
-// operand byte is loaded once per pair, which halves the L2 traffic of 128 x 128 tiles).  Persistent: a pair takes tiles
-// in turn, and its two sets of sums in tensor memory let the end of a tile run under the products of the next.
+// The other matrices: tiles of 256 x 256 (or 256 x 128), each by a cluster of two CTAs on two SMs (one tcgen05 product over
+// both: every operand byte is loaded once per pair, which halves the L2 traffic of 128 x 128 tiles).  Persistent: a pair
+// takes tiles in turn, and its two sets of sums in tensor memory let the end of a tile run under the products of the next.
 //   warp 0     feeds the stages (each CTA its half of the rows of A and of B)
 //   warp 1     issues the products (first CTA)
 //   warps 2-5  take the sums out, a quarter of the CTA's 128 rows each
 
-constexpr int kPairStages = 5;
-constexpr int kPairStageBytes = 4 * kUnitBytes;                       // per CTA: 128 x 64 of A and of B
 constexpr int kOutBytes = 4 * kUnitBytes;                             // 64 columns: the images of a tile part and its mirror
 constexpr int kPairThreads = 192;
-constexpr int kPairSmem = kPairStages * kPairStageBytes + 2 * kOutBytes + 1024;
+template <int N> constexpr int kPairStages = N == 256 ? 5 : 6;
+template <int N> constexpr int kPairStageBytes = (2 + N / 128) * kUnitBytes;    // per CTA: 128 x 64 of A, N / 2 x 64 of B
+template <int N> constexpr int kPairSmem = kPairStages<N> * kPairStageBytes<N> + 2 * kOutBytes + 1024;
 
 struct PairWork {
     const Tile* tiles;
@@ -363,21 +368,22 @@ struct PairWork {
 
 __device__ __forceinline__ void epilogue_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
 
-template <bool kSym>
+template <bool kSym, int N>
 __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2)
     pair_kernel(const __grid_constant__ CUtensorMap map, const PairWork w, uint8_t* ws,
                 const __grid_constant__ Chain c, __nv_bfloat16* __restrict__ out, int* timeouts) {
+    constexpr int kStages = kPairStages<N>, kStageBytes = kPairStageBytes<N>, kParts = N / 64, kUnitsB = N / 128;
     extern __shared__ uint8_t s_raw[];
-    __shared__ uint64_t s_full[kPairStages], s_free[kPairStages], s_sums[2], s_taken[2], s_plus[2];
+    __shared__ uint64_t s_full[kStages], s_free[kStages], s_sums[2], s_taken[2], s_plus[2];
     __shared__ uint32_t s_tmem;
     __shared__ int s_failed;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
     uint8_t* smem = (uint8_t*)(((uintptr_t)s_raw + 1023) & ~(uintptr_t)1023);
     const uint32_t stage0 = smem_addr(smem);
-    if (warp == 1) tmem_alloc_pair(&s_tmem, 512);
+    if (warp == 1) tmem_alloc_pair(&s_tmem, 2 * N);
     if (threadIdx.x == 0) {
-        for (int i = 0; i < kPairStages; ++i) {
+        for (int i = 0; i < kStages; ++i) {
             mbar_init(smem_addr(&s_full[i]), 1);
             mbar_init(smem_addr(&s_free[i]), 1);
         }
@@ -414,30 +420,26 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2)
                 const int left = !kSym ? d.small + c.op * small : p.left < 0 ? x_in : d.small + p.left * small;
                 const int right = !kSym || p.left < 0 ? x_in : d.small + p.right * small;
                 for (int k = 0; k < steps; ++k) {
-                    const uint32_t a = stage0 + st * kPairStageBytes, b = a + 2 * kUnitBytes, bar = smem_addr(&s_full[st]);
+                    const uint32_t a = stage0 + st * kStageBytes, b = a + 2 * kUnitBytes, bar = smem_addr(&s_full[st]);
                     ok = mbar_wait(smem_addr(&s_free[st]), (round & 1) ^ 1, &s_failed);
                     if (!ok) break;
-                    if (rank == 0) mbar_expect_tx(bar, 2 * kPairStageBytes);
+                    if (rank == 0) mbar_expect_tx(bar, 2 * kStageBytes);
                     const int kb = kSym || k < d.ku ? k : k - d.ku;
                     const int ua = left + kb * d.spu + d.ti * 4 + rank * 2;
                     tensor_load_2d_pair(a, &map, 0, ua * kUnit, bar);
                     tensor_load_2d_pair(a + kUnitBytes, &map, 0, (ua + 1) * kUnit, bar);
-                    if (kSym) {
-                        const int ub = right + kb * d.spu + d.tj * 4 + rank * 2;
-                        tensor_load_2d_pair(b, &map, 0, ub * kUnit, bar);
-                        tensor_load_2d_pair(b + kUnitBytes, &map, 0, (ub + 1) * kUnit, bar);
-                    } else {
-                        const int ub = (k < d.ku ? right : d.x_lo) + (d.tj * 4 + rank * 2) * d.spu + kb;
-                        tensor_load_2d_pair(b, &map, 0, ub * kUnit, bar);
-                        tensor_load_2d_pair(b + kUnitBytes, &map, 0, (ub + d.spu) * kUnit, bar);
-                    }
-                    if (++st == kPairStages) { st = 0; ++round; }
+                    const int at = d.tj * kParts + rank * kUnitsB;    // first unit row (symmetric) or column of B
+                    const int ub = kSym ? right + kb * d.spu + at : (k < d.ku ? right : d.x_lo) + at * d.spu + kb;
+#pragma unroll
+                    for (int u = 0; u < kUnitsB; ++u)
+                        tensor_load_2d_pair(b + u * kUnitBytes, &map, 0, (ub + u * (kSym ? 1 : d.spu)) * kUnit, bar);
+                    if (++st == kStages) { st = 0; ++round; }
                 }
             }
         }
     } else if (warp == 1) {
         if (lane == 0 && rank == 0) {
-            const uint32_t shape = f16_shape(kPairTile, kPairTile, !kSym);
+            const uint32_t shape = f16_shape(kRows, N, !kSym);
             int st = 0, n = 0;
             uint32_t round = 0;
             bool ok = true;
@@ -445,14 +447,14 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2)
                 const Tile d = w.tiles[i % w.n];
                 const int steps = steps_of(d, c.p[kSym ? i / w.n : 0]);
                 const int buf = n & 1;
-                const uint32_t sums = tmem + buf * kPairTile;
+                const uint32_t sums = tmem + buf * N;
                 ok = mbar_wait(smem_addr(&s_taken[buf]), ((n >> 1) & 1) ^ 1, &s_failed);
                 fence_after_sync();
                 for (int k = 0; k < steps && ok; ++k) {
                     ok = mbar_wait(smem_addr(&s_full[st]), round & 1, &s_failed);
                     if (!ok) break;
                     fence_after_sync();
-                    const uint32_t a = stage0 + st * kPairStageBytes, b = a + 2 * kUnitBytes;
+                    const uint32_t a = stage0 + st * kStageBytes, b = a + 2 * kUnitBytes;
 #pragma unroll
                     for (int q = 0; q < kUnit / 16; ++q) {
                         const uint64_t da = swizzled_operand(a + q * 32, 16, 1024);
@@ -461,15 +463,15 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2)
                         mma_f16_pair(sums, da, db, shape, k > 0 || q > 0);
                     }
                     tc_commit_pair(smem_addr(&s_free[st]));
-                    if (++st == kPairStages) { st = 0; ++round; }
+                    if (++st == kStages) { st = 0; ++round; }
                 }
                 tc_commit_pair(smem_addr(&s_sums[buf]));
             }
         }
     } else {
         const int quarter = warp & 3, row = quarter * 32 + lane, e0 = threadIdx.x == 64;
-        const uint32_t out0 = stage0 + kPairStages * kPairStageBytes;
-        uint8_t* out_smem = smem + kPairStages * kPairStageBytes;
+        const uint32_t out0 = stage0 + kStages * kStageBytes;
+        uint8_t* out_smem = smem + kStages * kStageBytes;
         const uint32_t taken[2] = {in_cta(smem_addr(&s_taken[0]), 0), in_cta(smem_addr(&s_taken[1]), 0)};
         int n = 0, part = 0, fetched = 0;
         for (int i = first; i < total; i += n_pairs, ++n) {
@@ -477,7 +479,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2)
             const Product& p = c.p[kSym ? i / w.n : 0];
             const int small = d.spu * d.spu, buf = n & 1;
             const int rb = d.ti * 4 + rank * 2;                       // first unit row of this CTA's part
-            const bool mirror = kSym && d.ti != d.tj, tall = d.rows > d.cols;
+            const bool mirror = kSym && d.tj < d.ti * (kRows / N), tall = d.rows > d.cols;
             // 64 columns of the matrix to add are brought to where their sums will be written, one part ahead
             const bool plus = kSym && p.plus >= 0;
             const auto fetch = [&](int cu, int to) {                  // (the buffer's last stores are done reading)
@@ -485,18 +487,17 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2)
                 const uint32_t bar = smem_addr(&s_plus[to]);
                 mbar_expect_tx(bar, 2 * kUnitBytes);
                 bulk_load(out0 + to * kOutBytes,
-                          ws + (int64_t)(d.small + p.plus * small + (d.tj * 4 + cu) * d.spu + rb) * kUnitBytes,
+                          ws + (int64_t)(d.small + p.plus * small + (d.tj * kParts + cu) * d.spu + rb) * kUnitBytes,
                           2 * kUnitBytes, bar);
             };
             if (plus && e0) fetch(0, part & 1);
-            const float gamma = kSym && d.ti == d.tj ? p.gamma : 0.0f;
-            const int diagonal = (int)rank * 128 + row;
+            const int diagonal = d.ti * kRows + (int)rank * 128 + row - d.tj * N;     // the column on the diagonal
             const bool ok = mbar_wait(smem_addr(&s_sums[buf]), (n >> 1) & 1, &s_failed);
             __syncwarp();
             if (!ok) break;
             fence_after_sync();
 #pragma unroll 1
-            for (int cu = 0; cu < 4; ++cu, ++part) {
+            for (int cu = 0; cu < kParts; ++cu, ++part) {
                 uint8_t* img = out_smem + (part & 1) * kOutBytes;
                 const uint32_t img_addr = out0 + (part & 1) * kOutBytes;
                 if (plus) {
@@ -512,7 +513,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2)
                 for (int h = 0; h < 2; ++h) {
                     const int q = cu * 2 + h;
                     uint32_t acc[32];
-                    tmem_load32(tmem + buf * kPairTile + ((uint32_t)(quarter * 32) << 16) + q * 32, acc);
+                    tmem_load32(tmem + buf * N + ((uint32_t)(quarter * 32) << 16) + q * 32, acc);
                     if (kSym || !c.last) {
                         const float alpha = kSym ? p.alpha : c.alpha;
 #pragma unroll
@@ -534,7 +535,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2)
                             if (kSym) {
                                 // (a select: a branch would be taken by one lane at a time)
 #pragma unroll
-                                for (int j = 0; j < 8; ++j) v[j] += diagonal == q * 32 + o * 8 + j ? gamma : 0.0f;
+                                for (int j = 0; j < 8; ++j) v[j] += diagonal == q * 32 + o * 8 + j ? p.gamma : 0.0f;
                             }
                             const uint4 packed = pack8(v);
                             *at = packed;
@@ -556,7 +557,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2)
                         }
                     }
                 }
-                if (cu == 3) {                                        // the sums have been read
+                if (cu == kParts - 1) {                                        // the sums have been read
                     fence_before_sync();
                     __syncwarp();
                     if (lane == 0) mbar_arrive_cluster(taken[buf]);
@@ -565,7 +566,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2)
                     fence_async_shared();
                     epilogue_sync();
                     if (e0) {
-                        const int cb = d.tj * 4 + cu;
+                        const int cb = d.tj * kParts + cu;
                         if (kSym || cb < d.lu) {
                             const int base = kSym ? d.small + p.to * small : (c.x_in ? d.x_hi : d.x_next);
                             bulk_store(ws + (int64_t)(base + cb * d.spu + rb) * kUnitBytes, img_addr, 2 * kUnitBytes);
@@ -575,12 +576,12 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2)
                                                img_addr + (2 + u) * kUnitBytes, kUnitBytes);
                         }
                         bulk_store_commit();
-                        if (plus && cu < 3) fetch(cu + 1, (part & 1) ^ 1);
+                        if (plus && cu < kParts - 1) fetch(cu + 1, (part & 1) ^ 1);
                     }
                 } else {
                     epilogue_sync();
                     const __nv_bfloat16* s_out = reinterpret_cast<const __nv_bfloat16*>(img);
-                    const int r_x = rb * kUnit, c_x = (d.tj * 4 + cu) * kUnit;   // first row, column of X
+                    const int r_x = rb * kUnit, c_x = (d.tj * kParts + cu) * kUnit;   // first row, column of X
                     const int a0 = tall ? c_x : r_x, n0 = tall ? r_x : c_x;
                     const int lines = tall ? 64 : 128, len = tall ? 128 : 64, pitch = tall ? 130 : 66;
                     __nv_bfloat16* to = out + d.offset + (int64_t)a0 * d.cols + n0;
@@ -613,7 +614,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2)
     __syncthreads();
     if (threadIdx.x == 0 && s_failed) atomicAdd(timeouts, 1);
     cluster_sync();
-    if (warp == 1) tmem_free_pair(tmem, 512);
+    if (warp == 1) tmem_free_pair(tmem, 2 * N);
 }
 
 // ---------------------------------------------------------------------------------------------- small matrices
@@ -942,7 +943,8 @@ __device__ int g_timeouts;
 static int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
 // Lays the matrices order[0..n) out in the workspace and numbers the CTAs of the passes.  Returns the bytes needed.
-static int64_t lay_out(const int64_t* offsets, const int64_t* rows, const int64_t* cols, const int* order, int n, Table* t) {
+static int64_t lay_out(const int64_t* offsets, const int64_t* rows, const int64_t* cols, const int* order, int n,
+                       int max_pairs, Table* t) {
     int64_t at = 0;
     int64_t chunks = 0, units = 0, sym = 0, apply = 0;
     t->n = n;
@@ -954,24 +956,39 @@ static int64_t lay_out(const int64_t* offsets, const int64_t* rows, const int64_
         m.cols = (int)c;
         m.s = (int)std::min(r, c);
         m.l = (int)std::max(r, c);
-        m.sp = (int)up(m.s, kPairTile);
+        m.sp = (int)up(m.s, kRows);
         m.lp = (int)up(m.l, kUnit);
         t->chunk_at[k] = (int)chunks;
         t->unit_at[k] = (int)units;
-        t->sym_at[k] = (int)sym;
-        t->apply_at[k] = (int)apply;
         m.partial0 = (int)chunks;
         m.n_chunks = (int)((r * c + 7 + kChunk - 1) / kChunk);          // (up to seven elements before the first)
         chunks += m.n_chunks;
         units += (int64_t)(m.sp / kUnit) * (m.lp / kUnit);
-        const int64_t mt = m.sp / kPairTile;
-        sym += mt * (mt + 1) / 2;
-        apply += mt * ((m.lp + kPairTile - 1) / kPairTile);
     }
+    // Columns of a tile: 256 give the tensor cores two thirds of the operand traffic per operation, 128 give twice as many
+    // tiles for few matrices.  A tile of 128 columns takes about 0.6 of the time of one of 256.
+    const auto tiles_of = [&](bool is_sym, int width) {
+        int64_t all = 0;
+        for (int k = 0; k < n; ++k) {
+            const Mat& m = t->m[k];
+            const int64_t mt = m.sp / kRows;
+            (is_sym ? t->sym_at : t->apply_at)[k] = (int)all;
+            all += is_sym ? mt * (mt + 1) / 2 * (kRows / width) : mt * ((m.lp + width - 1) / width);
+        }
+        (is_sym ? t->sym_at : t->apply_at)[n] = (int)all;
+        return all;
+    };
+    const auto choose = [&](bool is_sym, int* width) {
+        const auto rounds = [&](int64_t tiles) { return (double)((tiles + max_pairs - 1) / max_pairs); };
+        const int64_t wide = tiles_of(is_sym, 256), narrow = tiles_of(is_sym, 128);
+        *width = 0.6 * rounds(narrow) < rounds(wide) ? 128 : 256;
+        if (*width == 256) tiles_of(is_sym, 256);
+        return narrow;                                                // (room for either)
+    };
+    sym = choose(true, &t->sym_width);
+    apply = choose(false, &t->apply_width);
     t->chunk_at[n] = (int)chunks;
     t->unit_at[n] = (int)units;
-    t->sym_at[n] = (int)sym;
-    t->apply_at[n] = (int)apply;
     if (chunks > 0x7fffffff || units > 0x7fffffff || sym + apply > 0x7fffffff) return -1;
     at = up(at + chunks * 8, 1024);
     at = up(at + n * 8, 1024);                                        // inverse norms, arrival counters
@@ -1020,7 +1037,7 @@ static int64_t workspace_bytes(const int64_t* rows, const int64_t* cols, int n) 
     int64_t most = 0;
     for (size_t from = 0; from < order.size(); from += kMaxMats) {
         const int64_t b = lay_out(nullptr, rows, cols, order.data() + from, (int)std::min<size_t>(kMaxMats, order.size() - from),
-                                  t.data());
+                                  kMostPairs, t.data());
         if (b < 0) return SIDCO_E_SIZE;
         most = std::max(most, b);
     }
@@ -1049,14 +1066,15 @@ static cudaError_t resident_pairs(int* n) {
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(2);
     cfg.blockDim = dim3(kPairThreads);
-    cfg.dynamicSmemBytes = kPairSmem;
+    cfg.dynamicSmemBytes = kPairSmem<256>;
     cudaLaunchAttribute attr{};
     attr.id = cudaLaunchAttributeClusterDimension;
     attr.val.clusterDim.x = 2;
     attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    const cudaError_t e = cudaOccupancyMaxActiveClusters(n, pair_kernel<true>, &cfg);
+    const cudaError_t e = cudaOccupancyMaxActiveClusters(n, pair_kernel<true, 256>, &cfg);
+    *n = std::min(*n, kMostPairs);
     return e == cudaSuccess && *n < 1 ? cudaErrorInvalidConfiguration : e;
 }
 
@@ -1086,13 +1104,17 @@ static cudaError_t chain(const Table& t, const void* grad, float* momentum, floa
         return cudaErrorNotSupported;
     const int n_sym = t.sym_at[t.n], n_apply = t.apply_at[t.n];
     const Tile* tiles = reinterpret_cast<const Tile*>(ws + t.tiles);
+    const auto pair = [&](auto kernel, int smem, const Tile* first, int n, int products, const Chain& c) {
+        return launch(kernel, dim3(2 * std::min(max_pairs, n * products)), kPairThreads, (size_t)smem, s, map,
+                      PairWork{first, n, products}, ws, c, (__nv_bfloat16*)out, timeouts);
+    };
     const auto sym = [&](const Chain& c, int products) {
-        return launch(pair_kernel<true>, dim3(2 * std::min(max_pairs, n_sym * products)), kPairThreads, kPairSmem, s, map,
-                      PairWork{tiles, n_sym, products}, ws, c, (__nv_bfloat16*)out, timeouts);
+        return t.sym_width == 256 ? pair(pair_kernel<true, 256>, kPairSmem<256>, tiles, n_sym, products, c)
+                                  : pair(pair_kernel<true, 128>, kPairSmem<128>, tiles, n_sym, products, c);
     };
     const auto apply = [&](const Chain& c) {
-        return launch(pair_kernel<false>, dim3(2 * std::min(max_pairs, n_apply)), kPairThreads, kPairSmem, s, map,
-                      PairWork{tiles + n_sym, n_apply, 1}, ws, c, (__nv_bfloat16*)out, timeouts);
+        return t.apply_width == 256 ? pair(pair_kernel<false, 256>, kPairSmem<256>, tiles + n_sym, n_apply, 1, c)
+                                    : pair(pair_kernel<false, 128>, kPairSmem<128>, tiles + n_sym, n_apply, 1, c);
     };
     int done = 0, in = 0;
     while (done < steps) {
@@ -1195,8 +1217,10 @@ int sidco_orthogonalize(const void* grad, int grad_type, float* momentum, float 
         if ((e = cudaFuncSetAttribute(small_kernel<float>, most, kSmallSmem)) != cudaSuccess ||
             (e = cudaFuncSetAttribute(small_kernel<__nv_bfloat16>, most, kSmallSmem)) != cudaSuccess ||
             (e = cudaFuncSetAttribute(small_kernel<__half>, most, kSmallSmem)) != cudaSuccess ||
-            (e = cudaFuncSetAttribute(pair_kernel<true>, most, kPairSmem)) != cudaSuccess ||
-            (e = cudaFuncSetAttribute(pair_kernel<false>, most, kPairSmem)) != cudaSuccess ||
+            (e = cudaFuncSetAttribute(pair_kernel<true, 256>, most, kPairSmem<256>)) != cudaSuccess ||
+            (e = cudaFuncSetAttribute(pair_kernel<false, 256>, most, kPairSmem<256>)) != cudaSuccess ||
+            (e = cudaFuncSetAttribute(pair_kernel<true, 128>, most, kPairSmem<128>)) != cudaSuccess ||
+            (e = cudaFuncSetAttribute(pair_kernel<false, 128>, most, kPairSmem<128>)) != cudaSuccess ||
             (e = resident_pairs(&pairs)) != cudaSuccess)
             return (int)e;
         pair_count[dev] = pairs;
@@ -1221,7 +1245,8 @@ int sidco_orthogonalize(const void* grad, int grad_type, float* momentum, float 
     }
     std::vector<Table> t(1);
     for (size_t from = 0; from < order.size(); from += kMaxMats) {
-        lay_out(offsets, rows, cols, order.data() + from, (int)std::min<size_t>(kMaxMats, order.size() - from), t.data());
+        lay_out(offsets, rows, cols, order.data() + from, (int)std::min<size_t>(kMaxMats, order.size() - from),
+                pair_count[dev], t.data());
         uint8_t* ws = (uint8_t*)workspace;
         if (grad_type == SIDCO_T_F32)
             e = chain<float>(t[0], grad, momentum, mu, nesterov, steps, eps, out_bf16, ws, need, pair_count[dev], timeouts, s);
