@@ -27,6 +27,8 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <atomic>
+#include <mutex>
 #include <vector>
 
 #include "../../include/sidco.h"
@@ -626,7 +628,8 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2)
 // s x s products that follow (a few hundred nanoseconds each) every CTA does for itself.
 
 constexpr int kSmallS = 128, kSmallUnits = 4, kSmallCluster = 8;      // units of columns per CTA, CTAs per matrix: at most
-constexpr int kSmallThreads = 256;
+constexpr int kSmallThreads = 512;
+constexpr int kSmallHeld = kSmallS * kSmallUnits * kUnit / kSmallThreads;    // elements of X that a thread holds: 64
 constexpr int kSquareBytes = 4 * kUnitBytes;                          // 128 x 128
 constexpr int kSlabBytes = kSmallUnits * 2 * kUnitBytes;              // 128 x 256
 constexpr int kSmallSmem = 3 * kSquareBytes + 2 * kSlabBytes + 1024;
@@ -642,9 +645,8 @@ __device__ __forceinline__ uint4 remote_load16(uint32_t addr) {
     return v;
 }
 
-__device__ __forceinline__ void remote_store16(uint32_t addr, uint4 v) {
-    asm volatile("st.shared::cluster.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w)
-                 : "memory");
+__device__ __forceinline__ void remote_store8(uint32_t addr, uint32_t x, uint32_t y) {
+    asm volatile("st.shared::cluster.v2.u32 [%0], {%1, %2};" ::"r"(addr), "r"(x), "r"(y) : "memory");
 }
 
 __device__ __forceinline__ void remote_store_f64(uint32_t addr, double v) {
@@ -680,44 +682,39 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
         mbar_init_fence();
     }
 
-    // ---- momentum and norm; an element's place: (row r of X, column `a` of the unit)
-    const int s2 = s <= 32 ? 5 : s <= 64 ? 6 : 7;                     // s to a power of two
-    const int per_unit = tall ? kUnit << s2 : s * kUnit;
-    const auto place = [&](int u, int e, int& r, int& a) -> int64_t {  // < 0: outside the matrix
-        if (tall) {
-            r = e & ((1 << s2) - 1);
-            a = e >> s2;
-        } else {
-            a = e & (kUnit - 1);
-            r = e >> 6;
-        }
-        const int col = (first + u) * kUnit + a;
-        if (r >= s || col >= l) return -1;
-        return m.offset + (tall ? (int64_t)col * m.cols + r : (int64_t)r * m.cols + col);
-    };
-    const auto update_of = [&](float g, float mom) { return !momentum ? g : nesterov ? fmaf(mu, mom, g) : mom; };
-    constexpr int kAhead = 8;
-    double sum = 0.0;
-    for (int u = 0; u < units; ++u)
-        for (int e0 = threadIdx.x; e0 < per_unit; e0 += kSmallThreads * kAhead) {
-            float g[kAhead], v[kAhead];
-            int64_t at[kAhead];
+    // ---- momentum and norm.  A thread holds 16 elements of each unit of columns, threads next to each other neighbours of
+    // a row of the caller's matrix: element (unit u, j) is row r, column a of X's part here
+    const int r0 = tall ? threadIdx.x & 127 : threadIdx.x >> 6, a0 = tall ? threadIdx.x >> 7 : threadIdx.x & 63;
+    const auto row_of = [&](int j) { return tall ? r0 : r0 + 8 * j; };
+    const auto col_of = [&](int u, int j) { return u * kUnit + (tall ? a0 + 4 * j : a0); };
+    const auto inside = [&](int u, int j) { return u < units && row_of(j) < s && first * kUnit + col_of(u, j) < l; };
+    const int64_t base = m.offset + (tall ? (int64_t)(first * kUnit + a0) * m.cols + r0 : (int64_t)r0 * m.cols + first * kUnit + a0);
+    const int64_t by_u = (int64_t)kUnit * (tall ? m.cols : 1), by_j = (int64_t)(tall ? 4 : 8) * m.cols;
+    float x[kSmallHeld];
+    double sums[2] = {};
 #pragma unroll
-            for (int k = 0; k < kAhead; ++k) {
-                int r, a;
-                at[k] = e0 + k * kSmallThreads < per_unit ? place(u, e0 + k * kSmallThreads, r, a) : -1;
-                g[k] = at[k] >= 0 ? widen(grad[at[k]]) : 0.0f;
-                v[k] = at[k] >= 0 && momentum ? momentum[at[k]] : 0.0f;
-            }
+    for (int u = 0; u < kSmallUnits; ++u) {
+        if (u >= units) break;
+        float v[16];
 #pragma unroll
-            for (int k = 0; k < kAhead; ++k) {
-                if (at[k] < 0) continue;
-                const float mom = fmaf(mu, v[k], g[k]);
-                if (momentum) momentum[at[k]] = mom;
-                const double x = update_of(g[k], mom);
-                sum += x * x;
-            }
+        for (int j = 0; j < 16; ++j) {
+            const bool in = inside(u, j);
+            const int64_t at = base + u * by_u + j * by_j;
+            x[u * 16 + j] = in ? widen(grad[at]) : 0.0f;
+            v[j] = in && momentum ? momentum[at] : 0.0f;
         }
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            float& y = x[u * 16 + j];
+            if (momentum) {
+                const float mom = fmaf(mu, v[j], y);
+                if (inside(u, j)) momentum[base + u * by_u + j * by_j] = mom;
+                y = nesterov ? fmaf(mu, mom, y) : mom;
+            }
+            sums[j & 1] = fma((double)y, (double)y, sums[j & 1]);
+        }
+    }
+    double sum = sums[0] + sums[1];
     for (int i = threadIdx.x; i < 2 * kSlabBytes / 16; i += kSmallThreads)      // rows and columns behind the matrix
         reinterpret_cast<uint4*>(x_hi)[i] = make_uint4(0, 0, 0, 0);
 #pragma unroll
@@ -738,27 +735,25 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
     for (uint32_t i = 0; i < ctas; ++i) sum += s_norm[i];
     const float scale = (float)(1.0 / (sqrt(sum) + (double)eps)) * (float)(1 << kX);
 
-    // ---- X in two fp16 parts (each thread reads back what it wrote)
-    for (int u = 0; u < units; ++u)
-        for (int e0 = threadIdx.x; e0 < per_unit; e0 += kSmallThreads * kAhead) {
+    // ---- X in two fp16 parts
 #pragma unroll
-            for (int k = 0; k < kAhead; ++k) {
-                int r, a;
-                const int e = e0 + k * kSmallThreads;
-                const int64_t at = e < per_unit ? place(u, e, r, a) : -1;
-                if (at < 0) continue;
-                const float x = scale * (!momentum ? widen(grad[at]) : nesterov ? fmaf(mu, momentum[at], widen(grad[at]))
-                                                                                : momentum[at]);
-                const __half hi = __float2half_rn(x);
-                const int byte = (u * 2 + (r >> 6)) * kUnitBytes + in_unit(r & 63, a >> 3) + (a & 7) * 2;
-                *reinterpret_cast<__half*>(x_hi + byte) = hi;
-                *reinterpret_cast<__half*>(x_lo + byte) = __float2half_rn(x - __half2float(hi));
-            }
+    for (int u = 0; u < kSmallUnits; ++u) {
+        if (u >= units) break;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            if (!inside(u, j)) continue;
+            const int r = row_of(j), a = col_of(0, j);
+            const float v = scale * x[u * 16 + j];
+            const __half hi = __float2half_rn(v);
+            const int byte = (u * 2 + (r >> 6)) * kUnitBytes + in_unit(r & 63, a >> 3) + (a & 7) * 2;
+            *reinterpret_cast<__half*>(x_hi + byte) = hi;
+            *reinterpret_cast<__half*>(x_lo + byte) = __float2half_rn(v - __half2float(hi));
         }
+    }
 
     // ---- products: thread 0 issues, then everybody takes its rows and columns of the sums
     int uses = 0;
-    const int row = (warp & 3) * 32 + lane, side = warp >> 2;         // row of the sums, half of their columns
+    const int row = (warp & 3) * 32 + lane, side = warp >> 2;         // row of the sums, quarter of their columns
     const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
     const auto issue_and_wait = [&](auto products) {
         fence_async_shared();
@@ -785,30 +780,27 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
                         swizzled_operand(b + (k >> 2) * 2 * kUnitBytes + (k & 3) * 32, 16, 1024),
                         f16_shape(kSmallS, kSmallS, false), k > 0);
         });
+        uint32_t acc[32];
+        tmem_load32(lanes + side * 32, acc);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            uint32_t acc[32];
-            tmem_load32(lanes + side * 64 + h * 32, acc);
+        for (int o = 0; o < 4; ++o) {
+            const int at = ((side & ~1) + (row >> 6)) * kUnitBytes + in_unit(row & 63, (side & 1) * 4 + o);
+            float v[8];
 #pragma unroll
-            for (int o = 0; o < 4; ++o) {
-                const int at = (side * 2 + (row >> 6)) * kUnitBytes + in_unit(row & 63, h * 4 + o);
-                float v[8];
+            for (int j = 0; j < 8; ++j) v[j] = alpha * __uint_as_float(acc[o * 8 + j]);
+            if (plus) {
+                const uint4 w = *reinterpret_cast<const uint4*>(plus + at);
+                const __half2* h = reinterpret_cast<const __half2*>(&w);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = alpha * __uint_as_float(acc[o * 8 + j]);
-                if (plus) {
-                    const uint4 w = *reinterpret_cast<const uint4*>(plus + at);
-                    const __half2* x = reinterpret_cast<const __half2*>(&w);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const float2 f = __half22float2(x[j]);
-                        v[2 * j] = fmaf(beta, f.x, v[2 * j]);
-                        v[2 * j + 1] = fmaf(beta, f.y, v[2 * j + 1]);
-                    }
+                for (int j = 0; j < 4; ++j) {
+                    const float2 f = __half22float2(h[j]);
+                    v[2 * j] = fmaf(beta, f.x, v[2 * j]);
+                    v[2 * j + 1] = fmaf(beta, f.y, v[2 * j + 1]);
                 }
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] += row == side * 64 + h * 32 + o * 8 + j ? gamma : 0.0f;
-                *reinterpret_cast<uint4*>(to + at) = pack8(v);
             }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] += row == side * 32 + o * 8 + j ? gamma : 0.0f;
+            *reinterpret_cast<uint4*>(to + at) = pack8(v);
         }
     };
     const auto two = [](int k) { return __uint_as_float((uint32_t)(127 + k) << 23); };
@@ -825,13 +817,12 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
         });
         // (a CTA without columns adds zeros)
         float* partial = reinterpret_cast<float*>(sq[1]);             // [128][128] over two squares, words swizzled
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        {
             uint32_t acc[32];
-            tmem_load32(lanes + side * 64 + h * 32, acc);
+            tmem_load32(lanes + side * 32, acc);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const int c4 = side * 16 + h * 8 + j;                 // four columns; rows differ in their bank
+                const int c4 = side * 8 + j;                          // four columns; rows differ in their bank
                 const float4 v = units ? make_float4(__uint_as_float(acc[j * 4]), __uint_as_float(acc[j * 4 + 1]),
                                                      __uint_as_float(acc[j * 4 + 2]), __uint_as_float(acc[j * 4 + 3]))
                                        : make_float4(0, 0, 0, 0);
@@ -841,26 +832,31 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
         fence_before_sync();
         __syncthreads();
         cluster_sync();
-        // rows rank, rank + ctas, ... of the sum, eight columns at a time, to every CTA's A
-        for (int i = threadIdx.x; i < kSmallS / (int)ctas * 16; i += kSmallThreads) {
-            const int r = (i >> 4) * (int)ctas + (int)rank, c8 = i & 15;
-            float v[8] = {};
-            for (uint32_t q = 0; q < ctas; ++q) {
+        // rows rank, rank + ctas, ... of the sum, four columns at a time, to every CTA's A
+        for (int i = threadIdx.x; i < kSmallS / (int)ctas * 32; i += kSmallThreads) {
+            const int r = (i >> 5) * (int)ctas + (int)rank, c4 = i & 31;
+            const uint32_t from = smem_addr(partial) + (uint32_t)(r * 32 + (c4 ^ (r & 7))) * 16;
+            uint4 w[kSmallCluster];
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const uint4 w = remote_load16(
-                        in_cta(smem_addr(partial) + (uint32_t)(r * 32 + ((c8 * 2 + h) ^ (r & 7))) * 16, q));
-                    v[h * 4] += __uint_as_float(w.x);
-                    v[h * 4 + 1] += __uint_as_float(w.y);
-                    v[h * 4 + 2] += __uint_as_float(w.z);
-                    v[h * 4 + 3] += __uint_as_float(w.w);
+            for (uint32_t q = 0; q < kSmallCluster; ++q)
+                if (q < ctas) w[q] = remote_load16(in_cta(from, q));
+            float v[4] = {};
+#pragma unroll
+            for (uint32_t q = 0; q < kSmallCluster; ++q)
+                if (q < ctas) {
+                    v[0] += __uint_as_float(w[q].x);
+                    v[1] += __uint_as_float(w[q].y);
+                    v[2] += __uint_as_float(w[q].z);
+                    v[3] += __uint_as_float(w[q].w);
                 }
-            }
+            const float f = two(kA - 2 * kX);
+            const __half2 h0 = __floats2half2_rn(f * v[0], f * v[1]), h1 = __floats2half2_rn(f * v[2], f * v[3]);
+            const uint32_t to = smem_addr(sq[0]) + ((c4 >> 4) * 2 + (r >> 6)) * kUnitBytes +
+                                in_unit(r & 63, (c4 >> 1) & 7) + (c4 & 1) * 8;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] *= two(kA - 2 * kX);
-            const uint4 w = pack8(v);
-            const uint32_t to = smem_addr(sq[0]) + ((c8 >> 3) * 2 + (r >> 6)) * kUnitBytes + in_unit(r & 63, c8 & 7);
-            for (uint32_t q = 0; q < ctas; ++q) remote_store16(in_cta(to, q), w);
+            for (uint32_t q = 0; q < kSmallCluster; ++q)
+                if (q < ctas)
+                    remote_store8(in_cta(to, q), *reinterpret_cast<const uint32_t*>(&h0), *reinterpret_cast<const uint32_t*>(&h1));
         }
         fence_async_all();                                            // (read by the tensor cores of the other CTAs)
         cluster_sync();
@@ -895,7 +891,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
         const float alpha = two(last ? -scale_p - kX : -scale_p);
         __nv_bfloat16* s_out = reinterpret_cast<__nv_bfloat16*>(x_hi);          // (both parts of X are done with)
         constexpr int kWide = kSmallUnits * kUnit + 2, kTall = kSmallS + 2;     // bf16 per line
-        for (int u = side; u < units; u += 2) {
+        for (int u = side; u < units; u += 4) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 uint32_t acc[32];
@@ -1175,20 +1171,34 @@ static cudaError_t small_launch(const SmallMats& mats, int ctas, const void* gra
     return e;
 }
 
+// A stream per device on which the small matrices run beside the others (they need a third of the SMs for a part of the
+// time).  It takes over from the caller's stream and hands back to it within one call, under the lock.
+struct Beside {
+    cudaStream_t stream = nullptr;
+    cudaEvent_t fork = nullptr, join = nullptr;
+    std::mutex lock;
+
+    cudaError_t begin(cudaStream_t from) {
+        cudaError_t e;
+        if (!stream && (e = cudaStreamCreateWithFlags(&stream, cudaStreamNonBlocking)) != cudaSuccess) return e;
+        if (!fork && (e = cudaEventCreateWithFlags(&fork, cudaEventDisableTiming)) != cudaSuccess) return e;
+        if (!join && (e = cudaEventCreateWithFlags(&join, cudaEventDisableTiming)) != cudaSuccess) return e;
+        if ((e = cudaEventRecord(fork, from)) != cudaSuccess) return e;
+        return cudaStreamWaitEvent(stream, fork, 0);
+    }
+    cudaError_t end(cudaStream_t to) {
+        const cudaError_t e = cudaEventRecord(join, stream);
+        return e != cudaSuccess ? e : cudaStreamWaitEvent(to, join, 0);
+    }
+};
+
 }  // namespace sidco_ortho
 
 int sidco_internal::orthogonalize_timeouts(int* count) {
     return (int)cudaMemcpyFromSymbol(count, sidco_ortho::g_timeouts, sizeof(int));
 }
 
-extern "C" {
-
-int64_t sidco_orthogonalize_workspace_bytes(const int64_t* rows, const int64_t* cols, int n_mats) {
-    const int rc = sidco_ortho::check_shapes(rows, cols, n_mats);
-    return rc ? rc : sidco_ortho::workspace_bytes(rows, cols, n_mats);
-}
-
-int sidco_orthogonalize(const void* grad, int grad_type, float* momentum, float mu, int nesterov, const int64_t* offsets,
+static int orthogonalize(const void* grad, int grad_type, float* momentum, float mu, int nesterov, const int64_t* offsets,
                         const int64_t* rows, const int64_t* cols, int n_mats, int steps, float eps, uint16_t* out_bf16,
                         void* workspace, size_t workspace_bytes, void* stream) {
     using namespace sidco_ortho;
@@ -1206,12 +1216,12 @@ int sidco_orthogonalize(const void* grad, int grad_type, float* momentum, float 
     const int64_t need = sidco_ortho::workspace_bytes(rows, cols, n_mats);
     if (need < 0) return (int)need;
     if (need > 0 && ((uintptr_t)workspace % 256 || workspace_bytes < (size_t)need)) return SIDCO_E_WORKSPACE;
-    static int pair_count[64] = {};           // pairs of CTAs that are resident at once
+    static std::atomic<int> pair_count[64];   // pairs of CTAs that are resident at once
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return (int)e;
     if (dev < 0 || dev >= 64) return SIDCO_E_SIZE;
-    if (!pair_count[dev]) {                  // (setting it twice from two threads is harmless)
+    if (!pair_count[dev].load()) {           // (setting it twice from two threads is harmless)
         const auto most = cudaFuncAttributeMaxDynamicSharedMemorySize;
         int pairs = 0;
         if ((e = cudaFuncSetAttribute(small_kernel<float>, most, kSmallSmem)) != cudaSuccess ||
@@ -1225,38 +1235,81 @@ int sidco_orthogonalize(const void* grad, int grad_type, float* momentum, float 
             return (int)e;
         pair_count[dev] = pairs;
     }
+    const int max_pairs = pair_count[dev].load();
     int* timeouts = nullptr;
     if ((e = cudaGetSymbolAddress((void**)&timeouts, g_timeouts)) != cudaSuccess) return (int)e;
     cudaStream_t s = (cudaStream_t)stream;
-    for (size_t from = 0; from < small.size();) {
-        SmallMats mats;
-        const int64_t longest = std::max(rows[small[from]], cols[small[from]]);
-        int ctas = 1;
-        while ((int64_t)ctas * kSmallUnits * kUnit < longest) ctas *= 2;
-        for (mats.n = 0; from < small.size() && mats.n < kMaxMats; ++from, ++mats.n)
-            mats.m[mats.n] = {offsets[small[from]], (int)rows[small[from]], (int)cols[small[from]]};
-        if (grad_type == SIDCO_T_F32)
-            e = small_launch<float>(mats, ctas, grad, momentum, mu, nesterov, steps, eps, out_bf16, timeouts, s);
-        else if (grad_type == SIDCO_T_BF16)
-            e = small_launch<__nv_bfloat16>(mats, ctas, grad, momentum, mu, nesterov, steps, eps, out_bf16, timeouts, s);
-        else
-            e = small_launch<__half>(mats, ctas, grad, momentum, mu, nesterov, steps, eps, out_bf16, timeouts, s);
-        if (e != cudaSuccess) return (int)e;
+    const auto run_small = [&](cudaStream_t on) {
+        cudaError_t r = cudaSuccess;
+        for (size_t from = 0; from < small.size() && r == cudaSuccess;) {
+            SmallMats mats;
+            const int64_t longest = std::max(rows[small[from]], cols[small[from]]);
+            int ctas = 1;
+            while ((int64_t)ctas * kSmallUnits * kUnit < longest) ctas *= 2;
+            for (mats.n = 0; from < small.size() && mats.n < kMaxMats; ++from, ++mats.n)
+                mats.m[mats.n] = {offsets[small[from]], (int)rows[small[from]], (int)cols[small[from]]};
+            if (grad_type == SIDCO_T_F32)
+                r = small_launch<float>(mats, ctas, grad, momentum, mu, nesterov, steps, eps, out_bf16, timeouts, on);
+            else if (grad_type == SIDCO_T_BF16)
+                r = small_launch<__nv_bfloat16>(mats, ctas, grad, momentum, mu, nesterov, steps, eps, out_bf16, timeouts, on);
+            else
+                r = small_launch<__half>(mats, ctas, grad, momentum, mu, nesterov, steps, eps, out_bf16, timeouts, on);
+        }
+        return r;
+    };
+    // (a stream that is being captured keeps to itself: a graph being built and a running call must not meet on a stream)
+    cudaStreamCaptureStatus capture;
+    if ((e = cudaStreamIsCapturing(s, &capture)) != cudaSuccess) return (int)e;
+    const bool both = !small.empty() && !order.empty() && capture == cudaStreamCaptureStatusNone;
+    static Beside beside[64];
+    std::unique_lock<std::mutex> hold(beside[dev].lock, std::defer_lock);
+    if (both) {
+        hold.lock();
+        if ((e = beside[dev].begin(s)) != cudaSuccess) return (int)e;
+        e = run_small(beside[dev].stream);
+    } else if (!small.empty()) {
+        e = run_small(s);
     }
+    if (e != cudaSuccess && !both) return (int)e;
     std::vector<Table> t(1);
-    for (size_t from = 0; from < order.size(); from += kMaxMats) {
+    for (size_t from = 0; from < order.size() && e == cudaSuccess; from += kMaxMats) {
         lay_out(offsets, rows, cols, order.data() + from, (int)std::min<size_t>(kMaxMats, order.size() - from),
-                pair_count[dev], t.data());
+                max_pairs, t.data());
         uint8_t* ws = (uint8_t*)workspace;
         if (grad_type == SIDCO_T_F32)
-            e = chain<float>(t[0], grad, momentum, mu, nesterov, steps, eps, out_bf16, ws, need, pair_count[dev], timeouts, s);
+            e = chain<float>(t[0], grad, momentum, mu, nesterov, steps, eps, out_bf16, ws, need, max_pairs, timeouts, s);
         else if (grad_type == SIDCO_T_BF16)
-            e = chain<__nv_bfloat16>(t[0], grad, momentum, mu, nesterov, steps, eps, out_bf16, ws, need, pair_count[dev], timeouts, s);
+            e = chain<__nv_bfloat16>(t[0], grad, momentum, mu, nesterov, steps, eps, out_bf16, ws, need, max_pairs, timeouts, s);
         else
-            e = chain<__half>(t[0], grad, momentum, mu, nesterov, steps, eps, out_bf16, ws, need, pair_count[dev], timeouts, s);
-        if (e != cudaSuccess) return (int)e;
+            e = chain<__half>(t[0], grad, momentum, mu, nesterov, steps, eps, out_bf16, ws, need, max_pairs, timeouts, s);
     }
-    return 0;
+    if (both) {                              // (also after an error: what was forked is joined)
+        const cudaError_t r = beside[dev].end(s);
+        if (e == cudaSuccess) e = r;
+    }
+    return (int)e;
+}
+
+extern "C" {
+
+int64_t sidco_orthogonalize_workspace_bytes(const int64_t* rows, const int64_t* cols, int n_mats) {
+    try {
+        const int rc = sidco_ortho::check_shapes(rows, cols, n_mats);
+        return rc ? rc : sidco_ortho::workspace_bytes(rows, cols, n_mats);
+    } catch (...) {                          // (the host tables did not fit)
+        return SIDCO_E_SIZE;
+    }
+}
+
+int sidco_orthogonalize(const void* grad, int grad_type, float* momentum, float mu, int nesterov, const int64_t* offsets,
+                        const int64_t* rows, const int64_t* cols, int n_mats, int steps, float eps, uint16_t* out_bf16,
+                        void* workspace, size_t workspace_bytes, void* stream) {
+    try {
+        return orthogonalize(grad, grad_type, momentum, mu, nesterov, offsets, rows, cols, n_mats, steps, eps, out_bf16, workspace,
+                             workspace_bytes, stream);
+    } catch (...) {                          // (the host tables did not fit)
+        return (int)cudaErrorMemoryAllocation;
+    }
 }
 
 }  // extern "C"
