@@ -14,6 +14,9 @@ void note_launch();
 bool byte_map(CUtensorMap* map, const void* base, int64_t width, int64_t rows, int64_t pitch, int box_width, int box_rows,
               bool swizzle);
 
+// Tensor map for stores into a matrix of SIDCO_T_* elements: boxes of 128 bytes x box_rows rows with the 128-byte swizzle.
+bool out_map(CUtensorMap* map, void* base, int type, int64_t width, int64_t rows, int64_t pitch, int box_width, int box_rows);
+
 // How many CTAs of the product kernels gave up a bounded wait on the current device (synchronises it).
 int orthogonalize_timeouts(int* count);
 int mx4_matmul_timeouts(int* count);

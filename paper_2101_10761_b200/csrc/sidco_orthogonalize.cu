@@ -440,7 +440,8 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2)
             }
         }
     } else if (warp == 1) {
-        if (lane == 0 && rank == 0) {
+        // (the whole warp waits, one thread issues)
+        if (rank == 0) {
             const uint32_t shape = f16_shape(kRows, N, !kSym);
             int st = 0, n = 0;
             uint32_t round = 0;
@@ -451,23 +452,25 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2)
                 const int buf = n & 1;
                 const uint32_t sums = tmem + buf * N;
                 ok = mbar_wait(smem_addr(&s_taken[buf]), ((n >> 1) & 1) ^ 1, &s_failed);
-                fence_after_sync();
                 for (int k = 0; k < steps && ok; ++k) {
-                    ok = mbar_wait(smem_addr(&s_full[st]), round & 1, &s_failed);
+                    ok = __all_sync(0xffffffffu, mbar_wait(smem_addr(&s_full[st]), round & 1, &s_failed));
                     if (!ok) break;
                     fence_after_sync();
                     const uint32_t a = stage0 + st * kStageBytes, b = a + 2 * kUnitBytes;
+                    if (elect_one()) {
 #pragma unroll
-                    for (int q = 0; q < kUnit / 16; ++q) {
-                        const uint64_t da = swizzled_operand(a + q * 32, 16, 1024);
-                        const uint64_t db = kSym ? swizzled_operand(b + q * 32, 16, 1024)
-                                                 : swizzled_operand(b + q * 2048, kUnitBytes, 1024);
-                        mma_f16_pair(sums, da, db, shape, k > 0 || q > 0);
+                        for (int q = 0; q < kUnit / 16; ++q) {
+                            const uint64_t da = swizzled_operand(a + q * 32, 16, 1024);
+                            const uint64_t db = kSym ? swizzled_operand(b + q * 32, 16, 1024)
+                                                     : swizzled_operand(b + q * 2048, kUnitBytes, 1024);
+                            mma_f16_pair(sums, da, db, shape, k > 0 || q > 0);
+                        }
+                        tc_commit_pair(smem_addr(&s_free[st]));
+                        if (k + 1 == steps) tc_commit_pair(smem_addr(&s_sums[buf]));
                     }
-                    tc_commit_pair(smem_addr(&s_free[st]));
+                    __syncwarp();
                     if (++st == kStages) { st = 0; ++round; }
                 }
-                tc_commit_pair(smem_addr(&s_sums[buf]));
             }
         }
     } else {
@@ -751,7 +754,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
         }
     }
 
-    // ---- products: thread 0 issues, then everybody takes its rows and columns of the sums
+    // ---- products: one thread issues, then everybody takes its rows and columns of the sums
     int uses = 0;
     const int row = (warp & 3) * 32 + lane, side = warp >> 2;         // row of the sums, quarter of their columns
     const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
@@ -759,12 +762,14 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
         fence_async_shared();
         fence_before_sync();
         __syncthreads();
-        if (threadIdx.x == 0) {
+        if (warp == 0) {
             fence_after_sync();
-            products();
-            tc_commit(smem_addr(&s_done));
+            if (elect_one()) {
+                products();
+                tc_commit(smem_addr(&s_done));
+            }
+            __syncwarp();
         }
-        __syncwarp();
         mbar_wait(smem_addr(&s_done), uses & 1, &s_failed);
         __syncwarp();
         ++uses;

@@ -173,7 +173,29 @@ def test_product(m, n, k, dtype):
     assert B.sidco_wait_timeouts() == 0
 
 
-@pytest.mark.parametrize("m,n,k", [(1, 200, 320), (20, 300, 700), (200, 300, 700)])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m,n,k", [(5000, 1030, 300), (2560, 2304, 64), (300, 19000, 520), (19001, 100, 33), (2300, 2300, 1500)])
+def test_large_product(m, n, k, dtype):
+    """As test_product, at sizes that go by pairs of CTAs: aligned and unaligned C, ragged edges, more tiles than pairs."""
+    torch, B = torch_(), B_()
+    ac, as_, a = operands(m + 3 * k, m, k)
+    bc, bs, b = operands(n + 5 * k, n, k, k ** -0.5)
+    exact = torch.from_numpy(a).cuda() @ torch.from_numpy(b).cuda().T
+    size = torch.from_numpy(np.abs(a)).cuda() @ torch.from_numpy(np.abs(b)).cuda().T
+    held = torch.randn(m, n, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").to(getattr(torch, dtype))
+    for ldc, shift, add in (((n + 7) // 8 * 8, 0, False), ((n + 7) // 8 * 8 + 8, 8, True), (n + 3, 1, False), (n + 3, 0, True)):
+        store = torch.full((m * ldc + shift + 8,), float("nan"), dtype=held.dtype, device="cuda")
+        view = store[shift:shift + m * ldc].view(m, ldc)
+        view[:, :n] = held
+        B.sidco_mx4_matmul(ac, as_, bc, bs, m, n, k, store[shift:], ldc, add)
+        assert torch.isnan(view[:, n:]).all() and torch.isnan(store[shift + m * ldc:]).all(), "wrote outside C"
+        want, big = (exact + held.double(), size + held.double().abs()) if add else (exact, size)
+        tol = (k + 2) * 2.0 ** -23 * big + ulp_half(dtype) * want.abs() * (1 + 2.0 ** -8) + 2.0 ** -25
+        assert ((view[:, :n].double() - want).abs() <= tol).all()
+    assert B.sidco_wait_timeouts() == 0
+
+
+@pytest.mark.parametrize("m,n,k", [(1, 200, 320), (20, 300, 700), (200, 300, 700), (5000, 1100, 700)])
 def test_product_nan_block_stays_in_its_row_and_column(m, n, k):
     torch, B = torch_(), B_()
     r = rng(8)
