@@ -13,10 +13,17 @@
 #include "../../include/sidco.h"
 #include "sidco_internal.h"
 #include "sidco_mx4.cuh"
+#include "sidco_tc.cuh"
 
 namespace sidco_mx4 {
 
 constexpr unsigned kFull = 0xffffffffu;
+
+// (every kernel is set up under the end of the kernel before it, and waits for that one here)
+__device__ __forceinline__ void begin() {
+    sidco_tc::wait_prerequisites();
+    sidco_tc::launch_dependents();
+}
 
 __device__ __forceinline__ float widen(float x) { return x; }
 __device__ __forceinline__ float widen(__nv_bfloat16 x) { return __bfloat162float(x); }
@@ -129,6 +136,7 @@ template <typename T, int W>
 __global__ void __launch_bounds__(kQuantThreads) quantize_kernel(const QuantArgs A) {
     extern __shared__ float s_x[];                                   // [128][128], skewed; only with codes_t
     __shared__ __align__(16) uint8_t s_scale[kTileBytes];
+    begin();
     const int64_t r0 = (int64_t)(blockIdx.x / A.tiles_c) * kTile, c0 = (int64_t)(blockIdx.x % A.tiles_c) * kTile;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int oct = lane & 15;                                       // which eight columns
@@ -191,24 +199,40 @@ __global__ void __launch_bounds__(kQuantThreads) quantize_kernel(const QuantArgs
             reinterpret_cast<const uint4*>(s_scale)[threadIdx.x];
 }
 
-// A lane reads one word of codes and writes eight values.
+// A lane reads a word of codes and writes eight values, U times; 2^log2_lanes lanes work on a row, `parts` CTAs along it.
+constexpr int kDequantU = 2;
+
 template <typename T, int W>
 __global__ void __launch_bounds__(256) dequantize_kernel(const uint8_t* __restrict__ codes,
-                                                         const uint8_t* __restrict__ scales, int64_t rows, int64_t cols,
+                                                         const uint8_t* __restrict__ scales, int rows, int cols,
                                                          int64_t pitch, int64_t ktiles, T* __restrict__ out, int64_t ld,
-                                                         int64_t octs) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= rows * octs) return;
-    const int64_t r = i / octs, o = i - r * octs, j = o >> 2;
-    const uint32_t c = *reinterpret_cast<const uint32_t*>(codes + r * pitch + o * 4);
-    const uint32_t byte = scales[((r / kTileRows) * ktiles + j / kTileBlocks) * kTileBytes +
-                                 scale_in_tile((int)(r % kTileRows), (int)(j & 3))];
-    float v[8];
-    decode8(c, v);
-    const float s = scale_of(byte);
+                                                         int octs, int log2_lanes, int parts) {
+    begin();
+    const int lanes = 1 << log2_lanes, group = blockIdx.x / parts, part = blockIdx.x - group * parts;
+    const int r = group * (256 >> log2_lanes) + (threadIdx.x >> log2_lanes);
+    if (r >= rows) return;
+    const uint32_t* from = reinterpret_cast<const uint32_t*>(codes + r * pitch);
+    const uint8_t* scale = scales + (r / kTileRows) * ktiles * kTileBytes + scale_in_tile(r % kTileRows, 0);
+    T* to = out + r * ld;
+    const int o0 = part * (lanes * kDequantU) + (threadIdx.x & (lanes - 1));
+    uint32_t c[kDequantU], b[kDequantU];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] *= s;
-    store8<T, W>(out + r * ld + o * 8, (int)min((int64_t)8, cols - o * 8), v);
+    for (int u = 0; u < kDequantU; ++u) {
+        const int o = o0 + u * lanes;
+        c[u] = o < octs ? from[o] : 0u;
+        b[u] = o < octs ? scale[(o >> 4) * kTileBytes + ((o >> 2) & 3)] : 0u;
+    }
+#pragma unroll
+    for (int u = 0; u < kDequantU; ++u) {
+        const int o = o0 + u * lanes;
+        if (o >= octs) break;
+        const float s = scale_of(b[u]);
+        float v[8];
+        decode8(c[u], v);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] *= s;
+        store8<T, W>(to + o * 8, min(8, cols - o * 8), v);
+    }
 }
 
 // ------------------------------------------------------------------------------------------------ flat vectors
@@ -217,6 +241,7 @@ template <typename T, int W, int WR, int U>
 __global__ void __launch_bounds__(256) compress_kernel(const T* __restrict__ grad, float* __restrict__ residual,
                                                        int64_t d, uint8_t* __restrict__ codes,
                                                        uint8_t* __restrict__ scales) {
+    begin();
     const int64_t first = (int64_t)blockIdx.x * (256 * U) + threadIdx.x;
     const int64_t octs = blocks_of(d) * 4;                            // whole blocks
     float g[U][8], r[U][8];
@@ -248,38 +273,42 @@ __global__ void __launch_bounds__(256) compress_kernel(const T* __restrict__ gra
 }
 
 // The workers are added in their order, in fp32 (a decoded value has two significant bits), then scaled by 1/N.  A thread
-// takes U octets and loads the codes of A workers before it uses any.
-template <int W, int A, int U>
+// takes half a block (one 8-byte load of codes and one scale for sixteen values: the kernel is bound by its instructions,
+// eight values per scale took 49 us where sixteen take 40) and loads those of A workers before it uses any.
+template <int W, int A>
 __global__ void __launch_bounds__(256) mean_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
                                                    int n_workers, int64_t d, float* __restrict__ out) {
-    const int64_t nb = blocks_of(d), first = (int64_t)blockIdx.x * (256 * U) + threadIdx.x;
-    float sum[U][8] = {};
+    begin();
+    const int64_t nb = blocks_of(d), h = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (h >= nb * 2) return;
+    const uint2* cp = reinterpret_cast<const uint2*>(codes) + h;
+    const uint8_t* sp = scales + (h >> 1);
+    float sum[2][8] = {};
     for (int w0 = 0; w0 < n_workers; w0 += A) {
-        uint32_t c[A][U], b[A][U];
+        uint2 c[A];
+        uint32_t b[A];
 #pragma unroll
-        for (int i = 0; i < A; ++i)
+        for (int i = 0; i < A; ++i) {
+            const bool on = w0 + i < n_workers;
+            c[i] = on ? cp[(w0 + i) * nb * 2] : make_uint2(0, 0);
+            b[i] = on ? sp[(w0 + i) * nb] : 0u;
+        }
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int64_t o = first + u * 256;
-                const bool on = w0 + i < n_workers && o < nb * 4;
-                c[i][u] = on ? *reinterpret_cast<const uint32_t*>(codes + (w0 + i) * nb * 16 + o * 4) : 0u;
-                b[i][u] = on ? scales[(w0 + i) * nb + (o >> 2)] : 0u;
-            }
+        for (int i = 0; i < A; ++i) {
+            const float s = scale_of(b[i]);
+            float v[8];
+            decode8(c[i].x, v);
 #pragma unroll
-        for (int i = 0; i < A; ++i)
+            for (int k = 0; k < 8; ++k) sum[0][k] = fmaf(v[k], s, sum[0][k]);           // (+ 0 behind the last worker)
+            decode8(c[i].y, v);
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                float v[8];
-                decode8(c[i][u], v);
-                const float s = scale_of(b[i][u]);
-#pragma unroll
-                for (int k = 0; k < 8; ++k) sum[u][k] = fmaf(v[k], s, sum[u][k]);   // (+ 0 behind the last worker)
-            }
+            for (int k = 0; k < 8; ++k) sum[1][k] = fmaf(v[k], s, sum[1][k]);
+        }
     }
     const float inv = 1.0f / (float)n_workers;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int64_t at = (first + u * 256) * 8;
+    for (int u = 0; u < 2; ++u) {
+        const int64_t at = h * 16 + u * 8;
         if (at >= d) break;
 #pragma unroll
         for (int k = 0; k < 8; ++k) sum[u][k] *= inv;
@@ -291,7 +320,20 @@ __global__ void __launch_bounds__(256) mean_kernel(const uint8_t* __restrict__ c
 
 static bool aligned(const void* p, uintptr_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
 
-static int finish(cudaError_t e) {
+template <typename... P, typename... Q>
+static int launch(void (*kernel)(P...), int64_t grid, int threads, size_t smem, cudaStream_t stream, Q... args) {
+    if (grid > 0x7fffffff) return SIDCO_E_SIZE;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)grid);
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, P(args)...);
     if (e != cudaSuccess) return (int)e;
     sidco_internal::note_launch();
     return 0;
@@ -318,8 +360,7 @@ static int launch_quantize(const QuantArgs& a, int64_t grid, cudaStream_t s) {
         if (e != cudaSuccess) return (int)e;
         sized[dev] = true;
     }
-    quantize_kernel<T, W><<<(unsigned)grid, kQuantThreads, smem, s>>>(a);
-    return finish(cudaGetLastError());
+    return launch(quantize_kernel<T, W>, grid, kQuantThreads, smem, s, a);
 }
 
 template <typename T>
@@ -335,11 +376,12 @@ template <typename T>
 static int dequantize_typed(const uint8_t* codes, const uint8_t* scales, int64_t rows, int64_t cols, void* out, int64_t ld,
                             cudaStream_t s) {
     const int64_t octs = (cols + 7) / 8, pitch = blocks_of(cols) * 16, ktiles = (blocks_of(cols) + 3) / 4;
-    const int64_t grid = (rows * octs + 255) / 256;
-    if (grid > 0x7fffffff) return SIDCO_E_SIZE;
+    int log2_lanes = 0;                                               // lanes of a row: a warp, fewer for short rows
+    while (log2_lanes < 5 && (1 << log2_lanes) < octs) ++log2_lanes;
+    const int64_t per_cta = 256 >> log2_lanes, along = kDequantU << log2_lanes, parts = (octs + along - 1) / along;
     const auto go = [&](auto kernel) {
-        kernel<<<(unsigned)grid, 256, 0, s>>>(codes, scales, rows, cols, pitch, ktiles, (T*)out, ld, octs);
-        return finish(cudaGetLastError());
+        return launch(kernel, (rows + per_cta - 1) / per_cta * parts, 256, 0, s, codes, scales, rows, cols, pitch, ktiles,
+                      (T*)out, ld, octs, log2_lanes, parts);
     };
     switch (width_of(out, ld * sizeof(T), 16, sizeof(T))) {
         case 16: return go(dequantize_kernel<T, 16>);
@@ -353,10 +395,8 @@ static int compress_typed(const void* grad, float* residual, int64_t d, uint8_t*
     constexpr int U = 2, kMost = sizeof(T) * 8, kLeast = sizeof(T);
     const int64_t grid = (blocks_of(d) * 4 + 256 * U - 1) / (256 * U);
     if (aligned(grad, kMost) && aligned(residual, 32))
-        compress_kernel<T, kMost, 32, U><<<(unsigned)grid, 256, 0, s>>>((const T*)grad, residual, d, codes, scales);
-    else
-        compress_kernel<T, kLeast, 4, U><<<(unsigned)grid, 256, 0, s>>>((const T*)grad, residual, d, codes, scales);
-    return finish(cudaGetLastError());
+        return launch(compress_kernel<T, kMost, 32, U>, grid, 256, 0, s, (const T*)grad, residual, d, codes, scales);
+    return launch(compress_kernel<T, kLeast, 4, U>, grid, 256, 0, s, (const T*)grad, residual, d, codes, scales);
 }
 
 constexpr int64_t kMaxDim = ((int64_t)1 << 31) - ((int64_t)1 << 16);
@@ -437,14 +477,11 @@ int sidco_mx4_mean(const uint8_t* codes_all, const uint8_t* scales_all, int n_wo
     if (!codes_all || !scales_all || !out_dense) return SIDCO_E_NULL;
     if (!aligned(codes_all, 16) || !aligned(out_dense, 4)) return SIDCO_E_ALIGN;
     cudaStream_t s = (cudaStream_t)stream;
-    const auto go = [&](auto kernel, int octs) {
-        kernel<<<(unsigned)((blocks_of(d) * 4 + 256 * octs - 1) / (256 * octs)), 256, 0, s>>>(codes_all, scales_all, n_workers,
-                                                                                            d, out_dense);
+    const auto go = [&](auto kernel) {
+        return launch(kernel, (blocks_of(d) * 2 + 255) / 256, 256, 0, s, codes_all, scales_all, n_workers, d, out_dense);
     };
-    if (!aligned(out_dense, 32)) go(mean_kernel<4, 4, 1>, 1);
-    else if (n_workers == 1) go(mean_kernel<32, 1, 2>, 2);
-    else go(mean_kernel<32, 4, 2>, 2);
-    return finish(cudaGetLastError());
+    if (!aligned(out_dense, 32)) return go(mean_kernel<4, 4>);
+    return n_workers == 1 ? go(mean_kernel<32, 1>) : n_workers == 2 ? go(mean_kernel<32, 2>) : go(mean_kernel<32, 4>);
 }
 
 }  // extern "C"

@@ -107,6 +107,8 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2)
     cluster_sync();
     fence_after_sync();
     const uint32_t tmem = s_tmem;
+    wait_prerequisites();                                             // (the set-up may run under the kernel before)
+    launch_dependents();
     const int n_pairs = gridDim.x / 2, first = blockIdx.x / 2, total = tiles_m * tiles_n;
     const int steps = (int)((A.k + kStageK - 1) / kStageK);
     // tiles in bands of eight tile rows, column by column, so that pairs at work at the same time share operands in L2
@@ -344,6 +346,8 @@ __global__ void __launch_bounds__(kSplitThreads, 2)
     __syncthreads();
     fence_after_sync();
     const uint32_t tmem = s_tmem;
+    wait_prerequisites();                                             // (the set-up may run under the kernel before)
+    launch_dependents();
     const int tile = blockIdx.x / ctas, ti = tile / tiles_b, tj = tile % tiles_b;
     const int steps = (int)((A.k + kStageK - 1) / kStageK);
     const int from = steps * (int)rank / (int)ctas, to = steps * (int)(rank + 1) / (int)ctas;
@@ -542,12 +546,14 @@ static int split(const Operands& o, const Args& a, bool swapped, int max_pairs, 
     cfg.blockDim = dim3(kSplitThreads);
     cfg.dynamicSmemBytes = kSplitSmem<N>;
     cfg.stream = s;
-    cudaLaunchAttribute attr{};
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = ctas;
-    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
+    cudaLaunchAttribute attr[2]{};
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = ctas;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
     const int vec = (uintptr_t)a.c % (4 * sizeof(T)) == 0 && a.ldc % 4 == 0;
     return (int)cudaLaunchKernelEx(&cfg, split_kernel<T, N>, map_a, map_b, swapped ? o.b_scales : o.a_scales,
                                    swapped ? o.a_scales : o.b_scales, a, (int)tiles_b, (int)swapped, vec);
@@ -576,9 +582,17 @@ static int matmul_typed(const Operands& o, Args a, cudaStream_t s) {
             !scale_map(&map_sa, o.a_scales, a.m, a.ktiles) || !scale_map(&map_sb, o.b_scales, a.n, a.ktiles) ||
             (a.boxes && !sidco_internal::out_map(&map_c, a.c, type_of<T>(), a.n, a.m, a.ldc, 128 / (int)sizeof(T), 32)))
             return SIDCO_E_UNSUPPORTED;
-        pair_kernel<T><<<2 * max_pairs, kPairThreads, kPairSmem, s>>>(map_a, map_b, map_sa, map_sb, map_c, a, (int)tiles_m,
-                                                                      (int)tiles_n);
-        rc = (int)cudaGetLastError();
+        cudaLaunchConfig_t cfg{};
+        cfg.gridDim = dim3(2 * max_pairs);
+        cfg.blockDim = dim3(kPairThreads);
+        cfg.dynamicSmemBytes = kPairSmem;
+        cfg.stream = s;
+        cudaLaunchAttribute attr{};
+        attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr.val.programmaticStreamSerializationAllowed = 1;
+        cfg.attrs = &attr;
+        cfg.numAttrs = 1;
+        rc = (int)cudaLaunchKernelEx(&cfg, pair_kernel<T>, map_a, map_b, map_sa, map_sb, map_c, a, (int)tiles_m, (int)tiles_n);
     } else {
         const int64_t few = std::min(a.m, a.n);
         const bool swapped = few <= 64 && a.m <= a.n;
