@@ -116,8 +116,9 @@ __device__ __forceinline__ uint32_t encode(const float (&x)[8], uint32_t byte) {
 
 // ------------------------------------------------------------------------------------------------ matrices
 
-constexpr int kQuantThreads = 512;
-constexpr int kTile = 128;            // a CTA takes 128 x 128 elements: whole scale tiles in both directions
+constexpr int kQuantThreads = 256;
+constexpr int kQuantRows = 64, kQuantCols = 128;      // elements of a CTA: half a tile of scales in either direction
+constexpr int kQuantSmem = (kQuantRows * kQuantCols + 16) * (int)sizeof(float);
 
 struct QuantArgs {
     const void* x;
@@ -129,15 +130,15 @@ struct QuantArgs {
 };
 
 // Rows are quantised as they are loaded (four lanes of a warp hold a block); for the transpose the tile goes through
-// shared memory, where one thread then reads 32 elements of a column.  A row of the tile starts 8 words later in
-// every group of 32 rows, so that the lanes of a warp (8 columns x 4 groups) read from 32 different banks and write
-// 64 neighbouring bytes of a column's codes.
+// shared memory, where one thread then reads 32 elements of a column.  The second 32 rows start 16 words later, so that
+// the lanes of a warp (16 columns x 2 blocks) read from 32 different banks.  (Tiles of 128 x 128 halve the writes of
+// scales, but leave two waves of CTAs for 10000 x 1500: 21 us against 17.)
 template <typename T, int W>
 __global__ void __launch_bounds__(kQuantThreads) quantize_kernel(const QuantArgs A) {
-    extern __shared__ float s_x[];                                   // [128][128], skewed; only with codes_t
-    __shared__ __align__(16) uint8_t s_scale[kTileBytes];
+    extern __shared__ float s_x[];                                   // [64][128], skewed; only with codes_t
+    __shared__ __align__(16) uint8_t s_scale[kQuantRows * 4];
     begin();
-    const int64_t r0 = (int64_t)(blockIdx.x / A.tiles_c) * kTile, c0 = (int64_t)(blockIdx.x % A.tiles_c) * kTile;
+    const int64_t r0 = (int64_t)(blockIdx.x / A.tiles_c) * kQuantRows, c0 = (int64_t)(blockIdx.x % A.tiles_c) * kQuantCols;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int oct = lane & 15;                                       // which eight columns
     const int64_t c = c0 + oct * 8;
@@ -145,58 +146,52 @@ __global__ void __launch_bounds__(kQuantThreads) quantize_kernel(const QuantArgs
     float x[4][8];
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
-        const int64_t r = r0 + p * 32 + warp * 2 + (lane >> 4);
+        const int64_t r = r0 + p * 16 + warp * 2 + (lane >> 4);
         const bool in = r < A.rows && left > 0;
         load8<T, W>(in ? (const T*)A.x + r * A.ld + c : (const T*)A.x, in ? left : 0, x[p]);
     }
     if (A.codes_t) {
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
-            float* at = s_x + (p * 32 + warp * 2 + (lane >> 4)) * kTile + p * 8 + oct * 8;
-            reinterpret_cast<float4*>(at)[0] = make_float4(x[p][0], x[p][1], x[p][2], x[p][3]);
-            reinterpret_cast<float4*>(at)[1] = make_float4(x[p][4], x[p][5], x[p][6], x[p][7]);
+            float* at = s_x + (p * 16 + warp * 2 + (lane >> 4)) * kQuantCols + (p >> 1) * 16 + oct * 8;
+            // (every other four lanes write their second half first: eight lanes then cover all banks)
+            const int swap = (lane >> 2) & 1;
+            const float4 lo = make_float4(x[p][0], x[p][1], x[p][2], x[p][3]), hi = make_float4(x[p][4], x[p][5], x[p][6], x[p][7]);
+            reinterpret_cast<float4*>(at)[swap] = swap ? hi : lo;
+            reinterpret_cast<float4*>(at)[swap ^ 1] = swap ? lo : hi;
         }
     }
     if (A.codes) {
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
-            const int rt = p * 32 + warp * 2 + (lane >> 4);
+            const int rt = p * 16 + warp * 2 + (lane >> 4);
             const int64_t r = r0 + rt;
             const uint32_t byte = scale_byte(block_max(max8(x[p])));
             // (rows and columns behind the matrix hold zeros, so that the unused bytes of a scale tile become 0)
-            if ((lane & 3) == 0) s_scale[scale_in_tile(rt, oct >> 2)] = (uint8_t)byte;
+            if ((lane & 3) == 0) s_scale[rt * 4 + (oct >> 2)] = (uint8_t)byte;
             if (r < A.rows && c - (oct & 3) * 8 < A.cols)            // the last block is written whole
                 *reinterpret_cast<uint32_t*>(A.codes + r * A.pitch + (c >> 1)) = encode(x[p], byte);
         }
-        __syncthreads();
-        if (threadIdx.x < kTileBytes / 16)
-            reinterpret_cast<uint4*>(A.scales + ((r0 / kTile) * A.ktiles + c0 / kTile) * kTileBytes)[threadIdx.x] =
-                reinterpret_cast<const uint4*>(s_scale)[threadIdx.x];
     }
-    if (!A.codes_t) return;
     __syncthreads();
-    const int col = warp * 8 + (lane & 7), g = lane >> 3;            // a column and one of its four blocks
-    const float* from = s_x + g * (32 * kTile + 8) + col;
-    uint32_t m = 0;
+    if (A.codes && threadIdx.x < kQuantRows)                          // the four blocks of a row
+        *reinterpret_cast<uint32_t*>(A.scales + ((r0 / kTileRows) * A.ktiles + c0 / kQuantCols) * kTileBytes +
+                                     scale_in_tile((int)(r0 & 64) + threadIdx.x, 0)) =
+            *reinterpret_cast<const uint32_t*>(s_scale + threadIdx.x * 4);
+    if (!A.codes_t) return;
+    const int col = warp * 16 + (lane & 15), g = lane >> 4;          // a column and one of its two blocks
+    const float* from = s_x + g * (32 * kQuantCols + 16) + col;
+    float y[4][8];
 #pragma unroll
-    for (int i = 0; i < 32; ++i) m = max(m, magnitude_bits(from[i * kTile]));
-    const uint32_t byte = scale_byte(m);
-    uint4 codes;
-    uint32_t* w = &codes.x;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        float y[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = from[(q * 8 + i) * kTile];
-        w[q] = encode(y, byte);
-    }
-    s_scale[scale_in_tile(col, g)] = (uint8_t)byte;
+    for (int i = 0; i < 32; ++i) y[i >> 3][i & 7] = from[i * kQuantCols];
+    const uint32_t byte = scale_byte(max(max(max8(y[0]), max8(y[1])), max(max8(y[2]), max8(y[3]))));
+    const uint4 codes = make_uint4(encode(y[0], byte), encode(y[1], byte), encode(y[2], byte), encode(y[3], byte));
     if (c0 + col < A.cols && r0 + g * 32 < A.rows)
         *reinterpret_cast<uint4*>(A.codes_t + (c0 + col) * A.pitch_t + (r0 + g * 32) / 2) = codes;
-    __syncthreads();
-    if (threadIdx.x < kTileBytes / 16)
-        reinterpret_cast<uint4*>(A.scales_t + ((c0 / kTile) * A.ktiles_t + r0 / kTile) * kTileBytes)[threadIdx.x] =
-            reinterpret_cast<const uint4*>(s_scale)[threadIdx.x];
+    const uint32_t other = __shfl_down_sync(kFull, byte, 16);        // the scales of a column's two blocks together
+    if (g == 0)
+        *reinterpret_cast<uint16_t*>(A.scales_t + ((c0 / kTileRows) * A.ktiles_t + r0 / kTileRows) * kTileBytes +
+                                     scale_in_tile(col, (int)(r0 & 64) / kBlock)) = (uint16_t)(byte | other << 8);
 }
 
 // A lane reads a word of codes and writes eight values, U times; 2^log2_lanes lanes work on a row, `parts` CTAs along it.
@@ -348,19 +343,7 @@ static int width_of(const void* p, int64_t row_bytes, int most, int element) {
 
 template <typename T, int W>
 static int launch_quantize(const QuantArgs& a, int64_t grid, cudaStream_t s) {
-    static bool sized[64] = {};
-    const size_t smem = a.codes_t ? (kTile * kTile + 32) * sizeof(float) : 0;
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) return (int)e;
-    if (dev < 0 || dev >= 64) return SIDCO_E_SIZE;
-    if (!sized[dev]) {                      // (setting it twice from two threads is harmless)
-        e = cudaFuncSetAttribute(quantize_kernel<T, W>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                 (int)((kTile * kTile + 32) * sizeof(float)));
-        if (e != cudaSuccess) return (int)e;
-        sized[dev] = true;
-    }
-    return launch(quantize_kernel<T, W>, grid, kQuantThreads, smem, s, a);
+    return launch(quantize_kernel<T, W>, grid, kQuantThreads, a.codes_t ? kQuantSmem : 0, s, a);
 }
 
 template <typename T>
@@ -427,8 +410,8 @@ int sidco_mx4_quantize(const void* x, int x_type, int64_t rows, int64_t cols, in
     if (!aligned(x, size) || !aligned(codes, 16) || !aligned(scales, 16) || !aligned(codes_t, 16) || !aligned(scales_t, 16))
         return SIDCO_E_ALIGN;
     QuantArgs a{x, rows, cols, ld, codes, scales, codes_t, scales_t, blocks_of(cols) * 16, blocks_of(rows) * 16,
-                (blocks_of(cols) + 3) / 4, (blocks_of(rows) + 3) / 4, (cols + kTile - 1) / kTile};
-    const int64_t grid = (rows + kTile - 1) / kTile * a.tiles_c;
+                (blocks_of(cols) + 3) / 4, (blocks_of(rows) + 3) / 4, (cols + kQuantCols - 1) / kQuantCols};
+    const int64_t grid = (rows + kTileRows - 1) / kTileRows * (kTileRows / kQuantRows) * a.tiles_c;
     if (grid > 0x7fffffff) return SIDCO_E_SIZE;
     cudaStream_t s = (cudaStream_t)stream;
     if (x_type == SIDCO_T_F32) return quantize_typed<float>(a, grid, s);
