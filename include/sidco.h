@@ -327,8 +327,9 @@ int sidco_mx4_mean(const uint8_t* codes_all, const uint8_t* scales_all, int n_wo
  *     momentum <- mu * momentum + grad;     U = grad + mu * momentum (nesterov) or momentum;
  *     X = U / (|U|_F + eps);   `steps` times: A = X X^T, X <- a X + (b A + c A^2) X;     out <- X
  * with (a, b, c) = (3.4445, -4.7750, 2.0315); a matrix with more rows than columns goes through its transpose.  Five
- * steps bring all but the smallest singular values close to one.  Products are of fp16 operands with fp32 sums (for the
- * first two fp16 parts of X); the result is within about 3e-3 of the formula.  A matrix with a NaN or an infinity
+ * steps bring all but the smallest singular values close to one.  Products are of fp16 operands with fp32 sums; the result
+ * is within about 2e-3 of the formula in norm before its rounding to bf16 (5e-3 where the singular values span three
+ * decades).  A matrix with a NaN or an infinity
  * becomes NaN; the others are not affected.  Elements outside the matrices are neither read nor written.
  *
  * grad      device, grad_type[], read only.

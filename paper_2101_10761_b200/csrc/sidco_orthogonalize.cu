@@ -14,8 +14,9 @@
 //
 // Operands are fp16 (eleven significant bits; bf16's eight would leave 1e-2 of error in the result), sums fp32.  Every
 // singular value stays below 1.2 and every eigenvalue of a B within [0.6, 3.45], so fixed powers of two (kX, kA, ...)
-// keep all entries inside fp16's normal range.  The first X is kept as a sum of two fp16 parts in the application,
-// where its rounding would otherwise be the largest error (small singular values are scaled up by a^5 in the end).
+// keep all entries inside fp16's normal range.  The largest error is the rounding of the first X where small singular
+// values are scaled up by a^5 (1e-3 to 2e-3 of the result's norm for the entries above, 3e-3 for singular values over two
+// decades, 5e-3 over three).  A second fp16 part of X brings that to 2e-3 and 4e-3, for a twelfth of the time: not kept.
 //
 // Workspace matrices are stored as units of 64 x 64 fp16 in the 128-byte-swizzled image that the tensor cores read, so
 // that a stage of operands is one or two contiguous bulk copies, the same unit serves as K-major operand (Gram) and as
@@ -58,7 +59,7 @@ enum Buffer { kBufA, kBufA2, kBufB, kBufT, kBufP, kBufP2, kSmallBuffers };
 
 struct Mat {
     int64_t offset;                   // of the matrix in the flat vectors
-    int64_t x_hi, x_lo, x_next;       // bytes into the workspace: s x l matrices
+    int64_t x[2];                     // bytes into the workspace: s x l matrices, in turn
     int64_t small;                    // first of the s x s matrices
     int rows, cols, s, l;
     int sp, lp;                       // s to a multiple of 256, l to a multiple of 64
@@ -78,9 +79,10 @@ struct Table {
 
 // A tile of a pair of CTAs: row ti * 256, column tj * width; matrices in units from the start of the workspace.
 struct __align__(16) Tile {
-    int x_hi, x_lo, x_next, small;
+    int x[2], small;
     int spu, ku;                      // units along the padded s, along s
     int lu;                           // units along l
+    int pad;
     uint16_t ti, tj;                  // row, column
     int rows, cols;                   // of the caller's matrix, which lies
     int64_t offset;                   // here in the flat vectors
@@ -238,7 +240,7 @@ __device__ __forceinline__ void load4(const T* p, float (&x)[4]) {
     for (int i = 0; i < 4; ++i) x[i] = widen(reinterpret_cast<const T*>(w)[i]);
 }
 
-// One CTA per unit: U again (from what the momentum pass left), scaled, transposed if tall, split in two fp16 parts.  The
+// One CTA per unit: U again (from what the momentum pass left), scaled, transposed if tall, as fp16.  The
 // units are taken from the last to the first: what the momentum pass touched last is still in L2.
 template <typename T>
 __global__ void __launch_bounds__(256) normalize_kernel(const __grid_constant__ Table t, const T* __restrict__ grad,
@@ -261,9 +263,8 @@ __global__ void __launch_bounds__(256) normalize_kernel(const __grid_constant__ 
         const int j = find(at, t.n, k), tile = k - at[j];
         const Mat& q = t.m[j];
         Tile d{};
-        d.x_hi = (int)(q.x_hi / kUnitBytes);
-        d.x_lo = (int)(q.x_lo / kUnitBytes);
-        d.x_next = (int)(q.x_next / kUnitBytes);
+        d.x[0] = (int)(q.x[0] / kUnitBytes);
+        d.x[1] = (int)(q.x[1] / kUnitBytes);
         d.small = (int)(q.small / kUnitBytes);
         d.spu = q.sp / kUnit;
         d.ku = (q.s + kUnit - 1) / kUnit;
@@ -318,14 +319,10 @@ __global__ void __launch_bounds__(256) normalize_kernel(const __grid_constant__ 
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
         const int r = (threadIdx.x >> 3) + k * 32, c8 = threadIdx.x & 7;
-        float v[8], lo[8];
+        float v[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            v[j] = s_u[r][c8 * 8 + j] * scale;
-            lo[j] = v[j] - __half2float(__float2half_rn(v[j]));
-        }
-        *reinterpret_cast<uint4*>(ws + m.x_hi + unit + in_unit(r, c8)) = pack8(v);
-        *reinterpret_cast<uint4*>(ws + m.x_lo + unit + in_unit(r, c8)) = pack8(lo);
+        for (int j = 0; j < 8; ++j) v[j] = s_u[r][c8 * 8 + j] * scale;
+        *reinterpret_cast<uint4*>(ws + m.x[0] + unit + in_unit(r, c8)) = pack8(v);
     }
 }
 
@@ -340,7 +337,7 @@ struct Product {
 
 struct Chain {
     Product p[2];                     // symmetric products: blockIdx.y takes one
-    int x_in, parts;                  // which of the two X buffers holds X; 2: with the second part of the first X
+    int x_in;                         // which of the two X buffers holds X
     // application
     int op;                           // s x s operand
     int last;                         // write bf16 into the caller's vector instead of the next X
@@ -407,7 +404,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2)
 
     const int n_pairs = gridDim.x / 2, first = blockIdx.x / 2, total = w.n * w.products;
     const auto steps_of = [&](const Tile& d, const Product& p) {
-        return kSym ? (p.left < 0 ? d.lu : d.ku) : d.ku * c.parts;
+        return kSym && p.left < 0 ? d.lu : d.ku;
     };
     if (warp == 0) {
         if (lane == 0) {
@@ -418,7 +415,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2)
                 const Tile d = w.tiles[i % w.n];
                 const Product& p = c.p[kSym ? i / w.n : 0];
                 const int steps = steps_of(d, p), small = d.spu * d.spu;
-                const int x_in = c.x_in ? d.x_next : d.x_hi;
+                const int x_in = c.x_in ? d.x[1] : d.x[0];
                 const int left = !kSym ? d.small + c.op * small : p.left < 0 ? x_in : d.small + p.left * small;
                 const int right = !kSym || p.left < 0 ? x_in : d.small + p.right * small;
                 for (int k = 0; k < steps; ++k) {
@@ -426,12 +423,11 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2)
                     ok = mbar_wait(smem_addr(&s_free[st]), (round & 1) ^ 1, &s_failed);
                     if (!ok) break;
                     if (rank == 0) mbar_expect_tx(bar, 2 * kStageBytes);
-                    const int kb = kSym || k < d.ku ? k : k - d.ku;
-                    const int ua = left + kb * d.spu + d.ti * 4 + rank * 2;
+                    const int ua = left + k * d.spu + d.ti * 4 + rank * 2;
                     tensor_load_2d_pair(a, &map, 0, ua * kUnit, bar);
                     tensor_load_2d_pair(a + kUnitBytes, &map, 0, (ua + 1) * kUnit, bar);
                     const int at = d.tj * kParts + rank * kUnitsB;    // first unit row (symmetric) or column of B
-                    const int ub = kSym ? right + kb * d.spu + at : (k < d.ku ? right : d.x_lo) + at * d.spu + kb;
+                    const int ub = kSym ? right + k * d.spu + at : right + at * d.spu + k;
 #pragma unroll
                     for (int u = 0; u < kUnitsB; ++u)
                         tensor_load_2d_pair(b + u * kUnitBytes, &map, 0, (ub + u * (kSym ? 1 : d.spu)) * kUnit, bar);
@@ -555,10 +551,15 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2)
                         }
                     } else {
                         __nv_bfloat16* s_out = reinterpret_cast<__nv_bfloat16*>(img);
+                        if (tall) {
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) {
-                            const __nv_bfloat16 b = __float2bfloat16_rn(c.alpha * __uint_as_float(acc[j]));
-                            if (tall) s_out[(h * 32 + j) * 130 + row] = b; else s_out[row * 66 + h * 32 + j] = b;
+                            for (int j = 0; j < 32; ++j)
+                                s_out[(h * 32 + j) * 130 + row] = __float2bfloat16_rn(c.alpha * __uint_as_float(acc[j]));
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < 32; j += 2)
+                                *reinterpret_cast<__nv_bfloat162*>(s_out + row * 66 + h * 32 + j) = __floats2bfloat162_rn(
+                                    c.alpha * __uint_as_float(acc[j]), c.alpha * __uint_as_float(acc[j + 1]));
                         }
                     }
                 }
@@ -573,7 +574,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2)
                     if (e0) {
                         const int cb = d.tj * kParts + cu;
                         if (kSym || cb < d.lu) {
-                            const int base = kSym ? d.small + p.to * small : (c.x_in ? d.x_hi : d.x_next);
+                            const int base = kSym ? d.small + p.to * small : c.x_in ? d.x[0] : d.x[1];
                             bulk_store(ws + (int64_t)(base + cb * d.spu + rb) * kUnitBytes, img_addr, 2 * kUnitBytes);
                             if (mirror)
                                 for (int u = 0; u < 2; ++u)
@@ -625,8 +626,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2)
 // ---------------------------------------------------------------------------------------------- small matrices
 //
 // Matrices with s <= 128 and l <= 2048: one cluster of CTAs per matrix does the whole update in one launch.  Every CTA
-// keeps its columns of X (up to 256: 64 KB for each of the two fp16 parts) in shared memory from the first step to the
-// last.  The only exchange between the CTAs is a sum per Gram matrix: each adds its share of the rows of all partial
+// keeps its columns of X (up to 256: 64 KB) in shared memory from the first step to the last.  The only exchange between the CTAs is a sum per Gram matrix: each adds its share of the rows of all partial
 // Gram matrices through distributed shared memory, in the order of the CTAs, and hands the result to the others; the
 // s x s products that follow (a few hundred nanoseconds each) every CTA does for itself.
 
@@ -635,7 +635,9 @@ constexpr int kSmallThreads = 512;
 constexpr int kSmallHeld = kSmallS * kSmallUnits * kUnit / kSmallThreads;    // elements of X that a thread holds: 64
 constexpr int kSquareBytes = 4 * kUnitBytes;                          // 128 x 128
 constexpr int kSlabBytes = kSmallUnits * 2 * kUnitBytes;              // 128 x 256
-constexpr int kSmallSmem = 3 * kSquareBytes + 2 * kSlabBytes + 1024;
+constexpr int kOutLine = kSmallUnits * kUnit + 2, kOutColumn = kSmallS + 2;   // bf16 per line of the result, wide or tall
+constexpr int kSmallSmem = 3 * kSquareBytes + std::max(kSlabBytes, std::max(kSmallS * kOutLine, kSmallUnits * kUnit * kOutColumn) * 2) +
+                           1024;
 
 struct SmallMats {
     int n;
@@ -676,7 +678,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
     const int first = (int)(lu * rank / ctas), units = (int)(lu * (rank + 1) / ctas) - first;   // of this CTA's columns
 
     uint8_t* smem = (uint8_t*)(((uintptr_t)s_raw + 1023) & ~(uintptr_t)1023);
-    uint8_t *sq[3], *x_hi = smem + 3 * kSquareBytes, *x_lo = x_hi + kSlabBytes;
+    uint8_t *sq[3], *slab = smem + 3 * kSquareBytes;
     for (int i = 0; i < 3; ++i) sq[i] = smem + i * kSquareBytes;
     if (warp == 0) tmem_alloc(&s_tmem, 256);
     if (threadIdx.x == 0) {
@@ -718,8 +720,8 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
         }
     }
     double sum = sums[0] + sums[1];
-    for (int i = threadIdx.x; i < 2 * kSlabBytes / 16; i += kSmallThreads)      // rows and columns behind the matrix
-        reinterpret_cast<uint4*>(x_hi)[i] = make_uint4(0, 0, 0, 0);
+    for (int i = threadIdx.x; i < kSlabBytes / 16; i += kSmallThreads)          // rows and columns behind the matrix
+        reinterpret_cast<uint4*>(slab)[i] = make_uint4(0, 0, 0, 0);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_down_sync(0xffffffffu, sum, o);
     if (lane == 0) s_sum[warp] = sum;
@@ -738,7 +740,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
     for (uint32_t i = 0; i < ctas; ++i) sum += s_norm[i];
     const float scale = (float)(1.0 / (sqrt(sum) + (double)eps)) * (float)(1 << kX);
 
-    // ---- X in two fp16 parts
+    // ---- X
 #pragma unroll
     for (int u = 0; u < kSmallUnits; ++u) {
         if (u >= units) break;
@@ -746,11 +748,8 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
         for (int j = 0; j < 16; ++j) {
             if (!inside(u, j)) continue;
             const int r = row_of(j), a = col_of(0, j);
-            const float v = scale * x[u * 16 + j];
-            const __half hi = __float2half_rn(v);
-            const int byte = (u * 2 + (r >> 6)) * kUnitBytes + in_unit(r & 63, a >> 3) + (a & 7) * 2;
-            *reinterpret_cast<__half*>(x_hi + byte) = hi;
-            *reinterpret_cast<__half*>(x_lo + byte) = __float2half_rn(v - __half2float(hi));
+            *reinterpret_cast<__half*>(slab + (u * 2 + (r >> 6)) * kUnitBytes + in_unit(r & 63, a >> 3) + (a & 7) * 2) =
+                __float2half_rn(scale * x[u * 16 + j]);
         }
     }
 
@@ -814,7 +813,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
         const int group = steps == 1 || (done == 2 && (steps & 1)) ? 1 : 2;
         // A = X X^T: the partial sums of this CTA's columns
         issue_and_wait([&] {
-            const uint32_t a = smem_addr(x_hi);
+            const uint32_t a = smem_addr(slab);
             for (int k = 0; k < units * 4; ++k) {
                 const uint64_t x = swizzled_operand(a + (k >> 2) * 2 * kUnitBytes + (k & 3) * 32, 16, 1024);
                 mma_f16(tmem, x, x, f16_shape(kSmallS, kSmallS, false), k > 0);
@@ -880,22 +879,17 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
         }
 
         // X <- P X on this CTA's columns
-        const bool lo = done == 0;
         issue_and_wait([&] {
-            const uint32_t a = smem_addr(p);
-            for (int k = 0; k < ku * 4 * (lo ? 2 : 1) && units; ++k) {
-                const int q = k < ku * 4 ? k : k - ku * 4;
-                const uint32_t x = smem_addr(k < ku * 4 ? x_hi : x_lo);
-                mma_f16(tmem, swizzled_operand(a + (q >> 2) * 2 * kUnitBytes + (q & 3) * 32, 16, 1024),
-                        swizzled_operand(x + (q >> 2) * kUnitBytes + (q & 3) * 2048, 2 * kUnitBytes, 1024),
+            const uint32_t a = smem_addr(p), b = smem_addr(slab);
+            for (int k = 0; k < ku * 4 && units; ++k)
+                mma_f16(tmem, swizzled_operand(a + (k >> 2) * 2 * kUnitBytes + (k & 3) * 32, 16, 1024),
+                        swizzled_operand(b + (k >> 2) * kUnitBytes + (k & 3) * 2048, 2 * kUnitBytes, 1024),
                         f16_shape(kSmallS, units * kUnit, true), k > 0);
-            }
         });
         done += group;
         const bool last = done == steps;
         const float alpha = two(last ? -scale_p - kX : -scale_p);
-        __nv_bfloat16* s_out = reinterpret_cast<__nv_bfloat16*>(x_hi);          // (both parts of X are done with)
-        constexpr int kWide = kSmallUnits * kUnit + 2, kTall = kSmallS + 2;     // bf16 per line
+        __nv_bfloat16* s_out = reinterpret_cast<__nv_bfloat16*>(slab);          // (X is done with)
         for (int u = side; u < units; u += 4) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -907,14 +901,14 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
                         float v[8];
 #pragma unroll
                         for (int j = 0; j < 8; ++j) v[j] = alpha * __uint_as_float(acc[o * 8 + j]);
-                        *reinterpret_cast<uint4*>(x_hi + (u * 2 + (row >> 6)) * kUnitBytes + in_unit(row & 63, h * 4 + o)) =
+                        *reinterpret_cast<uint4*>(slab + (u * 2 + (row >> 6)) * kUnitBytes + in_unit(row & 63, h * 4 + o)) =
                             pack8(v);
                     }
                 } else {
 #pragma unroll
                     for (int j = 0; j < 32; ++j) {
                         const int col = u * kUnit + h * 32 + j;
-                        s_out[tall ? col * kTall + row : row * kWide + col] =
+                        s_out[tall ? col * kOutColumn + row : row * kOutLine + col] =
                             __float2bfloat16_rn(alpha * __uint_as_float(acc[j]));
                     }
                 }
@@ -922,7 +916,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
         }
         if (last) {
             __syncthreads();
-            const int lines = tall ? units * kUnit : s, len = tall ? s : units * kUnit, pitch = tall ? kTall : kWide;
+            const int lines = tall ? units * kUnit : s, len = tall ? s : units * kUnit, pitch = tall ? kOutColumn : kOutLine;
             const int line0 = tall ? first * kUnit : 0, col0 = tall ? 0 : first * kUnit;
             if (!s_failed)
                 for (int i = warp; i < lines && line0 + i < m.rows; i += kSmallThreads / 32)
@@ -998,10 +992,9 @@ static int64_t lay_out(const int64_t* offsets, const int64_t* rows, const int64_
     for (int k = 0; k < n; ++k) {
         Mat& m = t->m[k];
         const int64_t big = (int64_t)m.sp * m.lp * 2;
-        m.x_hi = at;
-        m.x_lo = at + big;
-        m.x_next = at + 2 * big;
-        m.small = at + 3 * big;
+        m.x[0] = at;
+        m.x[1] = at + big;
+        m.small = at + 2 * big;
         at = m.small + (int64_t)kSmallBuffers * m.sp * m.sp * 2;
     }
     return at;
@@ -1122,7 +1115,6 @@ static cudaError_t chain(const Table& t, const void* grad, float* momentum, floa
         const int group = steps == 1 || (done == 2 && steps % 2) ? 1 : 2;
         Chain c{};
         c.x_in = in;
-        c.parts = done ? 1 : 2;
         in ^= 1;
         int A = kBufA, A2 = kBufA2, P = kBufP, P2 = kBufP2, scale_p = kB;
         c.p[0] = Product{-1, -1, -1, A, two(kA - 2 * kX), 0.0f, 0.0f};
