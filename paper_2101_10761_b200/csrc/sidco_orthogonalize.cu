@@ -55,7 +55,7 @@ constexpr int kMostPairs = 74;        // pairs of SMs of the device
 constexpr int kMaxMats = 128;         // matrices of one chain of launches
 constexpr int kChunk = 16384;         // elements of a matrix per CTA of the momentum pass
 
-enum Buffer { kBufA, kBufA2, kBufB, kBufT, kBufP, kBufP2, kSmallBuffers };
+enum Buffer { kBufA, kBufA2, kBufB, kBufT, kBufP, kSmallBuffers };
 
 struct Mat {
     int64_t offset;                   // of the matrix in the flat vectors
@@ -328,50 +328,75 @@ __global__ void __launch_bounds__(256) normalize_kernel(const __grid_constant__ 
 
 // ---------------------------------------------------------------------------------------------- products
 
-struct Product {
-    int left, right;                  // s x s operands; left = -1: the Gram product of X
-    int plus;                         // matrix added times beta (-1: none)
-    int to;
-    float alpha, beta, gamma;         // to = alpha (left right) + beta plus + gamma I
+// One phase of the chain: the same product for every matrix.
+struct Phase {
+    int8_t sym;                       // a symmetric product of s x s matrices (or the Gram product), or P X
+    int8_t left, right;               // s x s operands; left = -1: the Gram product of X; an application has P on its left
+    int8_t plus, to;                  // matrix added times beta (-1: none); where the result goes
+    int8_t x_in;                      // which of the two X buffers holds X
+    int8_t last;                      // an application that writes bf16 into the caller's vector, not the next X
+    int8_t pad;
+    float alpha, beta, gamma;         // result = alpha (left right) + beta plus + gamma I
+};
+constexpr int kMaxPhases = (SIDCO_ORTHO_MAX_STEPS + 1) / 2 * 7;
+
+struct Phases {
+    int n;
+    int sym_width, sym_tiles;         // columns of the tiles of symmetric products, their number; they come first
+    int apply_width, apply_tiles;
+    Phase p[kMaxPhases];
 };
 
-struct Chain {
-    Product p[2];                     // symmetric products: blockIdx.y takes one
-    int x_in;                         // which of the two X buffers holds X
-    // application
-    int op;                           // s x s operand
-    int last;                         // write bf16 into the caller's vector instead of the next X
-    float alpha;
-};
-
-// ---------------------------------------------------------------------------------------------- pair tiles
+// ---------------------------------------------------------------------------------------------- chain of products
 //
-// The other matrices: tiles of 256 x 256 (or 256 x 128), each by a cluster of two CTAs on two SMs (one tcgen05 product over
-// both: every operand byte is loaded once per pair, which halves the L2 traffic of 128 x 128 tiles).  Persistent: a pair
-// takes tiles in turn, and its two sets of sums in tensor memory let the end of a tile run under the products of the next.
+// The other matrices: one persistent cooperative kernel runs all products of all steps.  Tiles of 256 x 256 (or 256 x 128)
+// go to clusters of two CTAs on two SMs (one tcgen05 product over both: every operand byte is loaded once per pair, which
+// halves the L2 traffic of 128 x 128 tiles).  Two sets of sums in tensor memory let the end of a tile run under the
+// products of the next.
 //   warp 0     feeds the stages (each CTA its half of the rows of A and of B)
 //   warp 1     issues the products (first CTA)
 //   warps 2-5  take the sums out, a quarter of the CTA's 128 rows each
+// Between phases only the thread that feeds the stages and the one that fetches matrices to add wait for the others
+// (bounded): every CTA counts itself into the phase when its results are stored.  As launches of their own the phases cost 3 us more
+// each (set-up, first loads, start and end of a kernel).
 
 constexpr int kOutBytes = 4 * kUnitBytes;                             // 64 columns: the images of a tile part and its mirror
-constexpr int kPairThreads = 192;
-template <int N> constexpr int kPairStages = N == 256 ? 5 : 6;
-template <int N> constexpr int kPairStageBytes = (2 + N / 128) * kUnitBytes;    // per CTA: 128 x 64 of A, N / 2 x 64 of B
-template <int N> constexpr int kPairSmem = kPairStages<N> * kPairStageBytes<N> + 2 * kOutBytes + 1024;
-
-struct PairWork {
-    const Tile* tiles;
-    int n;                            // tiles of one product
-    int products;
-};
+constexpr int kChainThreads = 192;
+constexpr int kStages = 5;
+constexpr int kStageBytes = 4 * kUnitBytes;                           // per CTA: 128 x 64 of A, up to 128 x 64 of B
+constexpr int kChainSmem = kStages * kStageBytes + 2 * kOutBytes + 1024;
 
 __device__ __forceinline__ void epilogue_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
 
-template <bool kSym, int N>
-__global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2)
-    pair_kernel(const __grid_constant__ CUtensorMap map, const PairWork w, uint8_t* ws,
-                const __grid_constant__ Chain c, __nv_bfloat16* __restrict__ out, int* timeouts) {
-    constexpr int kStages = kPairStages<N>, kStageBytes = kPairStageBytes<N>, kParts = N / 64, kUnitsB = N / 128;
+// The same, telling whether all of the 128 threads say so.  (They go on or stop together: one that stopped alone would leave
+// the others at the next barrier.)
+__device__ __forceinline__ bool epilogue_all(bool ok) {
+    uint32_t all;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.and.aligned.pred q, 1, 128, p;\n\t"
+                 "selp.b32 %0, 1, 0, q;\n\t}"
+                 : "=r"(all) : "r"((uint32_t)ok) : "memory");
+    return all != 0;
+}
+
+// Wait (bounded) until `count` CTAs have counted themselves in.
+__device__ __forceinline__ bool wait_arrivals(const unsigned* arrived, unsigned count, volatile int* failed) {
+    const unsigned long long start = time_ns();
+    for (uint32_t i = 1;; ++i) {
+        unsigned v;
+        asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(arrived) : "memory");
+        if (v >= count) break;
+        if ((i & 63u) == 0u && (*failed || time_ns() - start > kWaitLimitNs)) {
+            *failed = 1;
+            return false;
+        }
+    }
+    fence_async_all();                                                // (what they stored is read by bulk copies)
+    return true;
+}
+
+__global__ void __launch_bounds__(kChainThreads, 1) __cluster_dims__(2)
+    chain_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ Phases ph, const Tile* tiles, uint8_t* ws,
+                 __nv_bfloat16* __restrict__ out, unsigned* arrived, int* timeouts) {
     extern __shared__ uint8_t s_raw[];
     __shared__ uint64_t s_full[kStages], s_free[kStages], s_sums[2], s_taken[2], s_plus[2];
     __shared__ uint32_t s_tmem;
@@ -380,7 +405,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2)
     const uint32_t rank = cluster_rank();
     uint8_t* smem = (uint8_t*)(((uintptr_t)s_raw + 1023) & ~(uintptr_t)1023);
     const uint32_t stage0 = smem_addr(smem);
-    if (warp == 1) tmem_alloc_pair(&s_tmem, 2 * N);
+    if (warp == 1) tmem_alloc_pair(&s_tmem, 512);
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i) {
             mbar_init(smem_addr(&s_full[i]), 1);
@@ -399,73 +424,86 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2)
     cluster_sync();
     fence_after_sync();
     const uint32_t tmem = s_tmem;
-    wait_prerequisites();
-    launch_dependents();                 // (behind the wait: then all but the kernel before it are done when one starts)
 
-    const int n_pairs = gridDim.x / 2, first = blockIdx.x / 2, total = w.n * w.products;
-    const auto steps_of = [&](const Tile& d, const Product& p) {
-        return kSym && p.left < 0 ? d.lu : d.ku;
-    };
+    const int n_pairs = gridDim.x / 2, first = blockIdx.x / 2;
+    const auto steps_of = [](const Tile& d, const Phase& p) { return p.sym && p.left < 0 ? d.lu : d.ku; };
     if (warp == 0) {
-        if (lane == 0) {
+        if (elect_one()) {
             int st = 0;
             uint32_t round = 0;
             bool ok = true;
-            for (int i = first; i < total && ok; i += n_pairs) {
-                const Tile d = w.tiles[i % w.n];
-                const Product& p = c.p[kSym ? i / w.n : 0];
-                const int steps = steps_of(d, p), small = d.spu * d.spu;
-                const int x_in = c.x_in ? d.x[1] : d.x[0];
-                const int left = !kSym ? d.small + c.op * small : p.left < 0 ? x_in : d.small + p.left * small;
-                const int right = !kSym || p.left < 0 ? x_in : d.small + p.right * small;
-                for (int k = 0; k < steps; ++k) {
-                    const uint32_t a = stage0 + st * kStageBytes, b = a + 2 * kUnitBytes, bar = smem_addr(&s_full[st]);
-                    ok = mbar_wait(smem_addr(&s_free[st]), (round & 1) ^ 1, &s_failed);
-                    if (!ok) break;
-                    if (rank == 0) mbar_expect_tx(bar, 2 * kStageBytes);
-                    const int ua = left + k * d.spu + d.ti * 4 + rank * 2;
-                    tensor_load_2d_pair(a, &map, 0, ua * kUnit, bar);
-                    tensor_load_2d_pair(a + kUnitBytes, &map, 0, (ua + 1) * kUnit, bar);
-                    const int at = d.tj * kParts + rank * kUnitsB;    // first unit row (symmetric) or column of B
-                    const int ub = kSym ? right + k * d.spu + at : right + at * d.spu + k;
-#pragma unroll
-                    for (int u = 0; u < kUnitsB; ++u)
-                        tensor_load_2d_pair(b + u * kUnitBytes, &map, 0, (ub + u * (kSym ? 1 : d.spu)) * kUnit, bar);
-                    if (++st == kStages) { st = 0; ++round; }
+            for (int f = 0; f < ph.n && ok; ++f) {
+                const Phase& p = ph.p[f];
+                const int width = p.sym ? ph.sym_width : ph.apply_width, units_b = width / 128, parts = width / 64;
+                const int total = p.sym ? ph.sym_tiles : ph.apply_tiles;
+                const Tile* list = tiles + (p.sym ? 0 : ph.sym_tiles);
+                bool waited = f == 0;
+                for (int i = first; i < total && ok; i += n_pairs) {
+                    const Tile d = list[i];
+                    if (!waited) {
+                        ok = wait_arrivals(arrived + f - 1, gridDim.x, &s_failed);
+                        waited = true;
+                        if (!ok) break;
+                    }
+                    const int steps = steps_of(d, p), small = d.spu * d.spu;
+                    const int x_in = p.x_in ? d.x[1] : d.x[0];
+                    const int left = p.left < 0 ? x_in : d.small + p.left * small;
+                    const int right = !p.sym || p.left < 0 ? x_in : d.small + p.right * small;
+                    // first unit row (symmetric) or column of B, and the way to its next unit and to the next stage
+                    const int at = d.tj * parts + (int)rank * units_b;
+                    const int ub0 = p.sym ? right + at : right + at * d.spu;
+                    const int ub_unit = p.sym ? 1 : d.spu, ub_step = p.sym ? d.spu : 1;
+                    const int ua0 = left + d.ti * 4 + (int)rank * 2;
+                    for (int k = 0; k < steps; ++k) {
+                        const uint32_t a = stage0 + st * kStageBytes, b = a + 2 * kUnitBytes, bar = smem_addr(&s_full[st]);
+                        ok = mbar_wait(smem_addr(&s_free[st]), (round & 1) ^ 1, &s_failed);
+                        if (!ok) break;
+                        if (rank == 0) mbar_expect_tx(bar, 2 * (2 + units_b) * kUnitBytes);
+                        const int ua = ua0 + k * d.spu, ub = ub0 + k * ub_step;
+                        tensor_load_2d_pair(a, &map, 0, ua * kUnit, bar);
+                        tensor_load_2d_pair(a + kUnitBytes, &map, 0, (ua + 1) * kUnit, bar);
+                        tensor_load_2d_pair(b, &map, 0, ub * kUnit, bar);
+                        if (units_b == 2) tensor_load_2d_pair(b + kUnitBytes, &map, 0, (ub + ub_unit) * kUnit, bar);
+                        if (++st == kStages) { st = 0; ++round; }
+                    }
                 }
             }
         }
     } else if (warp == 1) {
         // (the whole warp waits, one thread issues)
         if (rank == 0) {
-            const uint32_t shape = f16_shape(kRows, N, !kSym);
             int st = 0, n = 0;
             uint32_t round = 0;
             bool ok = true;
-            for (int i = first; i < total && ok; i += n_pairs, ++n) {
-                const Tile d = w.tiles[i % w.n];
-                const int steps = steps_of(d, c.p[kSym ? i / w.n : 0]);
-                const int buf = n & 1;
-                const uint32_t sums = tmem + buf * N;
-                ok = mbar_wait(smem_addr(&s_taken[buf]), ((n >> 1) & 1) ^ 1, &s_failed);
-                for (int k = 0; k < steps && ok; ++k) {
-                    ok = __all_sync(0xffffffffu, mbar_wait(smem_addr(&s_full[st]), round & 1, &s_failed));
-                    if (!ok) break;
-                    fence_after_sync();
-                    const uint32_t a = stage0 + st * kStageBytes, b = a + 2 * kUnitBytes;
-                    if (elect_one()) {
+            for (int f = 0; f < ph.n && ok; ++f) {
+                const Phase& p = ph.p[f];
+                const bool sym = p.sym;
+                const int total = sym ? ph.sym_tiles : ph.apply_tiles;
+                const Tile* list = tiles + (sym ? 0 : ph.sym_tiles);
+                const uint32_t shape = f16_shape(kRows, sym ? ph.sym_width : ph.apply_width, !sym);
+                // (K-major operands move 32 bytes on along K, the MN-major B of an application sixteen rows of 128)
+                const uint32_t b_step = sym ? 32 : 2048, b_lead = sym ? 16 : kUnitBytes;
+                for (int i = first; i < total && ok; i += n_pairs, ++n) {
+                    const int steps = p.sym && p.left < 0 ? list[i].lu : list[i].ku;
+                    const int buf = n & 1;
+                    const uint32_t sums = tmem + buf * 256;
+                    ok = mbar_wait(smem_addr(&s_taken[buf]), ((n >> 1) & 1) ^ 1, &s_failed);
+                    for (int k = 0; k < steps && ok; ++k) {
+                        ok = __all_sync(0xffffffffu, mbar_wait(smem_addr(&s_full[st]), round & 1, &s_failed));
+                        if (!ok) break;
+                        fence_after_sync();
+                        const uint32_t a = stage0 + st * kStageBytes, b = a + 2 * kUnitBytes;
+                        if (elect_one()) {
 #pragma unroll
-                        for (int q = 0; q < kUnit / 16; ++q) {
-                            const uint64_t da = swizzled_operand(a + q * 32, 16, 1024);
-                            const uint64_t db = kSym ? swizzled_operand(b + q * 32, 16, 1024)
-                                                     : swizzled_operand(b + q * 2048, kUnitBytes, 1024);
-                            mma_f16_pair(sums, da, db, shape, k > 0 || q > 0);
+                            for (int q = 0; q < kUnit / 16; ++q)
+                                mma_f16_pair(sums, swizzled_operand(a + q * 32, 16, 1024),
+                                             swizzled_operand(b + q * b_step, b_lead, 1024), shape, k > 0 || q > 0);
+                            tc_commit_pair(smem_addr(&s_free[st]));
+                            if (k + 1 == steps) tc_commit_pair(smem_addr(&s_sums[buf]));
                         }
-                        tc_commit_pair(smem_addr(&s_free[st]));
-                        if (k + 1 == steps) tc_commit_pair(smem_addr(&s_sums[buf]));
+                        __syncwarp();
+                        if (++st == kStages) { st = 0; ++round; }
                     }
-                    __syncwarp();
-                    if (++st == kStages) { st = 0; ++round; }
                 }
             }
         }
@@ -475,142 +513,160 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2)
         uint8_t* out_smem = smem + kStages * kStageBytes;
         const uint32_t taken[2] = {in_cta(smem_addr(&s_taken[0]), 0), in_cta(smem_addr(&s_taken[1]), 0)};
         int n = 0, part = 0, fetched = 0;
-        for (int i = first; i < total; i += n_pairs, ++n) {
-            const Tile d = w.tiles[i % w.n];
-            const Product& p = c.p[kSym ? i / w.n : 0];
-            const int small = d.spu * d.spu, buf = n & 1;
-            const int rb = d.ti * 4 + rank * 2;                       // first unit row of this CTA's part
-            const bool mirror = kSym && d.tj < d.ti * (kRows / N), tall = d.rows > d.cols;
-            // 64 columns of the matrix to add are brought to where their sums will be written, one part ahead
-            const bool plus = kSym && p.plus >= 0;
-            const auto fetch = [&](int cu, int to) {                  // (the buffer's last stores are done reading)
-                asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
-                const uint32_t bar = smem_addr(&s_plus[to]);
-                mbar_expect_tx(bar, 2 * kUnitBytes);
-                bulk_load(out0 + to * kOutBytes,
-                          ws + (int64_t)(d.small + p.plus * small + (d.tj * kParts + cu) * d.spu + rb) * kUnitBytes,
-                          2 * kUnitBytes, bar);
-            };
-            if (plus && e0) fetch(0, part & 1);
-            const int diagonal = d.ti * kRows + (int)rank * 128 + row - d.tj * N;     // the column on the diagonal
-            const bool ok = mbar_wait(smem_addr(&s_sums[buf]), (n >> 1) & 1, &s_failed);
-            __syncwarp();
-            if (!ok) break;
-            fence_after_sync();
-#pragma unroll 1
-            for (int cu = 0; cu < kParts; ++cu, ++part) {
-                uint8_t* img = out_smem + (part & 1) * kOutBytes;
-                const uint32_t img_addr = out0 + (part & 1) * kOutBytes;
-                if (plus) {
-                    mbar_wait(smem_addr(&s_plus[part & 1]), (fetched >> 1) & 1, &s_failed);
-                    ++fetched;
-                    __syncwarp();
-                } else {
-                    // the stores that read this buffer two parts ago are done reading
-                    if (e0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
-                    epilogue_sync();
+        bool ok = true;
+        for (int f = 0; f < ph.n && ok; ++f) {
+            const Phase& p = ph.p[f];
+            const bool sym = p.sym, last = p.last, plus = p.plus >= 0;
+            const int width = sym ? ph.sym_width : ph.apply_width, parts = width / 64;
+            const int total = sym ? ph.sym_tiles : ph.apply_tiles;
+            const Tile* list = tiles + (sym ? 0 : ph.sym_tiles);
+            const float alpha = p.alpha, beta = p.beta, gamma = p.gamma;
+            bool waited = f == 0;
+            for (int i = first; i < total; i += n_pairs, ++n) {
+                const Tile d = list[i];
+                const int small = d.spu * d.spu, buf = n & 1;
+                const int rb = d.ti * 4 + rank * 2;                   // first unit row of this CTA's part
+                const bool mirror = sym && d.tj < d.ti * (kRows / width), tall = d.rows > d.cols;
+                const int base = sym ? d.small + p.to * small : p.x_in ? d.x[0] : d.x[1];
+                // 64 columns of the matrix to add are brought to where their sums will be written, one part ahead
+                const auto fetch = [&](int cu, int to) {              // (the buffer's last stores are done reading)
+                    asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+                    const uint32_t bar = smem_addr(&s_plus[to]);
+                    mbar_expect_tx(bar, 2 * kUnitBytes);
+                    bulk_load(out0 + to * kOutBytes,
+                              ws + (int64_t)(d.small + p.plus * small + (d.tj * parts + cu) * d.spu + rb) * kUnitBytes,
+                              2 * kUnitBytes, bar);
+                };
+                if (plus && e0) {
+                    if (!waited) wait_arrivals(arrived + f - 1, gridDim.x, &s_failed);
+                    waited = true;
+                    fetch(0, part & 1);
                 }
+                const int diagonal = d.ti * kRows + (int)rank * 128 + row - d.tj * width;     // the column on the diagonal
+                ok = mbar_wait(smem_addr(&s_sums[buf]), (n >> 1) & 1, &s_failed);
+                __syncwarp();
+                ok = epilogue_all(ok);
+                if (!ok) break;
+                fence_after_sync();
+#pragma unroll 1
+                for (int cu = 0; cu < parts; ++cu, ++part) {
+                    uint8_t* img = out_smem + (part & 1) * kOutBytes;
+                    const uint32_t img_addr = out0 + (part & 1) * kOutBytes;
+                    if (plus) {
+                        mbar_wait(smem_addr(&s_plus[part & 1]), (fetched >> 1) & 1, &s_failed);
+                        ++fetched;
+                        __syncwarp();
+                    } else {
+                        // the stores that read this buffer two parts ago are done reading
+                        if (e0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+                        epilogue_sync();
+                    }
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int q = cu * 2 + h;
-                    uint32_t acc[32];
-                    tmem_load32(tmem + buf * N + ((uint32_t)(quarter * 32) << 16) + q * 32, acc);
-                    if (kSym || !c.last) {
-                        const float alpha = kSym ? p.alpha : c.alpha;
+                    for (int h = 0; h < 2; ++h) {
+                        const int q = cu * 2 + h;
+                        uint32_t acc[32];
+                        tmem_load32(tmem + buf * 256 + ((uint32_t)(quarter * 32) << 16) + q * 32, acc);
+                        if (!last) {
 #pragma unroll
-                        for (int o = 0; o < 4; ++o) {
-                            float v[8];
+                            for (int o = 0; o < 4; ++o) {
+                                float v[8];
 #pragma unroll
-                            for (int j = 0; j < 8; ++j) v[j] = alpha * __uint_as_float(acc[o * 8 + j]);
-                            uint4* at = reinterpret_cast<uint4*>(img + (row >> 6) * kUnitBytes + in_unit(row & 63, h * 4 + o));
-                            if (kSym && plus) {
-                                const uint4 e = *at;
-                                const __half2* x = reinterpret_cast<const __half2*>(&e);
+                                for (int j = 0; j < 8; ++j) v[j] = alpha * __uint_as_float(acc[o * 8 + j]);
+                                uint4* at = reinterpret_cast<uint4*>(img + (row >> 6) * kUnitBytes + in_unit(row & 63, h * 4 + o));
+                                if (plus) {
+                                    const uint4 e = *at;
+                                    const __half2* x = reinterpret_cast<const __half2*>(&e);
 #pragma unroll
-                                for (int j = 0; j < 4; ++j) {
-                                    const float2 f = __half22float2(x[j]);
-                                    v[2 * j] = fmaf(p.beta, f.x, v[2 * j]);
-                                    v[2 * j + 1] = fmaf(p.beta, f.y, v[2 * j + 1]);
+                                    for (int j = 0; j < 4; ++j) {
+                                        const float2 y = __half22float2(x[j]);
+                                        v[2 * j] = fmaf(beta, y.x, v[2 * j]);
+                                        v[2 * j + 1] = fmaf(beta, y.y, v[2 * j + 1]);
+                                    }
+                                    // (gamma comes with a matrix to add; a select: a branch would be taken by one lane at
+                                    // a time)
+#pragma unroll
+                                    for (int j = 0; j < 8; ++j) v[j] += diagonal == q * 32 + o * 8 + j ? gamma : 0.0f;
+                                }
+                                const uint4 packed = pack8(v);
+                                *at = packed;
+                                if (mirror) {
+                                    const __half* hv = reinterpret_cast<const __half*>(&packed);
+#pragma unroll
+                                    for (int j = 0; j < 8; ++j)
+                                        *reinterpret_cast<__half*>(img + (2 + (row >> 6)) * kUnitBytes +
+                                                                   in_unit(h * 32 + o * 8 + j, (row & 63) >> 3) +
+                                                                   (row & 7) * 2) = hv[j];
                                 }
                             }
-                            if (kSym) {
-                                // (a select: a branch would be taken by one lane at a time)
-#pragma unroll
-                                for (int j = 0; j < 8; ++j) v[j] += diagonal == q * 32 + o * 8 + j ? p.gamma : 0.0f;
-                            }
-                            const uint4 packed = pack8(v);
-                            *at = packed;
-                            if (mirror) {
-                                const __half* hv = reinterpret_cast<const __half*>(&packed);
-#pragma unroll
-                                for (int j = 0; j < 8; ++j)
-                                    *reinterpret_cast<__half*>(img + (2 + (row >> 6)) * kUnitBytes +
-                                                               in_unit(h * 32 + o * 8 + j, (row & 63) >> 3) +
-                                                               (row & 7) * 2) = hv[j];
-                            }
-                        }
-                    } else {
-                        __nv_bfloat16* s_out = reinterpret_cast<__nv_bfloat16*>(img);
-                        if (tall) {
-#pragma unroll
-                            for (int j = 0; j < 32; ++j)
-                                s_out[(h * 32 + j) * 130 + row] = __float2bfloat16_rn(c.alpha * __uint_as_float(acc[j]));
                         } else {
+                            __nv_bfloat16* s_out = reinterpret_cast<__nv_bfloat16*>(img);
+                            if (tall) {
 #pragma unroll
-                            for (int j = 0; j < 32; j += 2)
-                                *reinterpret_cast<__nv_bfloat162*>(s_out + row * 66 + h * 32 + j) = __floats2bfloat162_rn(
-                                    c.alpha * __uint_as_float(acc[j]), c.alpha * __uint_as_float(acc[j + 1]));
+                                for (int j = 0; j < 32; ++j)
+                                    s_out[(h * 32 + j) * 130 + row] = __float2bfloat16_rn(alpha * __uint_as_float(acc[j]));
+                            } else {
+#pragma unroll
+                                for (int j = 0; j < 32; j += 2)
+                                    *reinterpret_cast<__nv_bfloat162*>(s_out + row * 66 + h * 32 + j) = __floats2bfloat162_rn(
+                                        alpha * __uint_as_float(acc[j]), alpha * __uint_as_float(acc[j + 1]));
+                            }
                         }
                     }
-                }
-                if (cu == kParts - 1) {                                        // the sums have been read
-                    fence_before_sync();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive_cluster(taken[buf]);
-                }
-                if (kSym || !c.last) {
-                    fence_async_shared();
-                    epilogue_sync();
-                    if (e0) {
-                        const int cb = d.tj * kParts + cu;
-                        if (kSym || cb < d.lu) {
-                            const int base = kSym ? d.small + p.to * small : c.x_in ? d.x[0] : d.x[1];
-                            bulk_store(ws + (int64_t)(base + cb * d.spu + rb) * kUnitBytes, img_addr, 2 * kUnitBytes);
-                            if (mirror)
-                                for (int u = 0; u < 2; ++u)
-                                    bulk_store(ws + (int64_t)(base + (rb + u) * d.spu + cb) * kUnitBytes,
-                                               img_addr + (2 + u) * kUnitBytes, kUnitBytes);
-                        }
-                        bulk_store_commit();
-                        if (plus && cu < kParts - 1) fetch(cu + 1, (part & 1) ^ 1);
+                    if (cu == parts - 1) {                            // the sums have been read
+                        fence_before_sync();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive_cluster(taken[buf]);
                     }
-                } else {
-                    epilogue_sync();
-                    const __nv_bfloat16* s_out = reinterpret_cast<const __nv_bfloat16*>(img);
-                    const int r_x = rb * kUnit, c_x = (d.tj * kParts + cu) * kUnit;   // first row, column of X
-                    const int a0 = tall ? c_x : r_x, n0 = tall ? r_x : c_x;
-                    const int lines = tall ? 64 : 128, len = tall ? 128 : 64, pitch = tall ? 130 : 66;
-                    __nv_bfloat16* to = out + d.offset + (int64_t)a0 * d.cols + n0;
-                    const int n_lines = min(lines, d.rows - a0), n_len = min(len, d.cols - n0);
-                    const bool even = ((d.offset | d.cols) & 1) == 0 && ((uintptr_t)out & 3) == 0;
-                    if (even) {
-                        const int k = lane * 2;
-#pragma unroll 8
-                        for (int a = quarter; a < n_lines; a += 4) {
-                            const __nv_bfloat16* from = s_out + a * pitch;
-                            __nv_bfloat16* line = to + (int64_t)a * d.cols;
-                            if (k < n_len)
-                                *reinterpret_cast<uint32_t*>(line + k) = *reinterpret_cast<const uint32_t*>(from + k);
-                            if (k + 64 < n_len)
-                                *reinterpret_cast<uint32_t*>(line + k + 64) = *reinterpret_cast<const uint32_t*>(from + k + 64);
+                    if (!last) {
+                        fence_async_shared();
+                        epilogue_sync();
+                        if (e0) {
+                            const int cb = d.tj * parts + cu;
+                            if (sym || cb < d.lu) {
+                                bulk_store(ws + (int64_t)(base + cb * d.spu + rb) * kUnitBytes, img_addr, 2 * kUnitBytes);
+                                if (mirror)
+                                    for (int u = 0; u < 2; ++u)
+                                        bulk_store(ws + (int64_t)(base + (rb + u) * d.spu + cb) * kUnitBytes,
+                                                   img_addr + (2 + u) * kUnitBytes, kUnitBytes);
+                            }
+                            bulk_store_commit();
+                            if (plus && cu < parts - 1) fetch(cu + 1, (part & 1) ^ 1);
                         }
                     } else {
+                        epilogue_sync();
+                        const __nv_bfloat16* s_out = reinterpret_cast<const __nv_bfloat16*>(img);
+                        const int r_x = rb * kUnit, c_x = (d.tj * parts + cu) * kUnit;       // first row, column of X
+                        const int a0 = tall ? c_x : r_x, n0 = tall ? r_x : c_x;
+                        const int lines = tall ? 64 : 128, len = tall ? 128 : 64, pitch = tall ? 130 : 66;
+                        __nv_bfloat16* to = out + d.offset + (int64_t)a0 * d.cols + n0;
+                        const int n_lines = min(lines, d.rows - a0), n_len = min(len, d.cols - n0);
+                        const bool even = ((d.offset | d.cols) & 1) == 0 && ((uintptr_t)out & 3) == 0;
+                        if (even) {
+                            const int k = lane * 2;
+#pragma unroll 8
+                            for (int a = quarter; a < n_lines; a += 4) {
+                                const __nv_bfloat16* from = s_out + a * pitch;
+                                __nv_bfloat16* line = to + (int64_t)a * d.cols;
+                                if (k < n_len)
+                                    *reinterpret_cast<uint32_t*>(line + k) = *reinterpret_cast<const uint32_t*>(from + k);
+                                if (k + 64 < n_len)
+                                    *reinterpret_cast<uint32_t*>(line + k + 64) =
+                                        *reinterpret_cast<const uint32_t*>(from + k + 64);
+                            }
+                        } else {
 #pragma unroll 4
-                        for (int a = quarter; a < n_lines; a += 4)
-                            for (int k = lane; k < n_len; k += 32) to[(int64_t)a * d.cols + k] = s_out[a * pitch + k];
+                            for (int a = quarter; a < n_lines; a += 4)
+                                for (int k = lane; k < n_len; k += 32) to[(int64_t)a * d.cols + k] = s_out[a * pitch + k];
+                        }
+                        if (e0) bulk_store_commit();                  // (an empty group keeps the count of parts)
                     }
-                    if (e0) bulk_store_commit();                      // (an empty group keeps the count of parts)
                 }
+            }
+            if (e0 && !last) {                                        // stored: count this CTA in
+                bulk_store_wait();
+                fence_async_all();
+                __threadfence();
+                asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(arrived + f) : "memory");
             }
         }
         if (e0) bulk_store_wait();
@@ -620,7 +676,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2)
     __syncthreads();
     if (threadIdx.x == 0 && s_failed) atomicAdd(timeouts, 1);
     cluster_sync();
-    if (warp == 1) tmem_free_pair(tmem, 2 * N);
+    if (warp == 1) tmem_free_pair(tmem, 512);
 }
 
 // ---------------------------------------------------------------------------------------------- small matrices
@@ -986,7 +1042,7 @@ static int64_t lay_out(const int64_t* offsets, const int64_t* rows, const int64_
     t->unit_at[n] = (int)units;
     if (chunks > 0x7fffffff || units > 0x7fffffff || sym + apply > 0x7fffffff) return -1;
     at = up(at + chunks * 8, 1024);
-    at = up(at + n * 8, 1024);                                        // inverse norms, arrival counters
+    at = up(at + n * 8 + kMaxPhases * 4, 1024);                       // inverse norms, arrival counters
     t->tiles = at;
     at = up(at + (sym + apply) * (int64_t)sizeof(Tile), kUnitBytes);
     for (int k = 0; k < n; ++k) {
@@ -1059,15 +1115,15 @@ static cudaError_t launch(void (*kernel)(Args...), dim3 grid, int threads, size_
 static cudaError_t resident_pairs(int* n) {
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(2);
-    cfg.blockDim = dim3(kPairThreads);
-    cfg.dynamicSmemBytes = kPairSmem<256>;
+    cfg.blockDim = dim3(kChainThreads);
+    cfg.dynamicSmemBytes = kChainSmem;
     cudaLaunchAttribute attr{};
     attr.id = cudaLaunchAttributeClusterDimension;
     attr.val.clusterDim.x = 2;
     attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    const cudaError_t e = cudaOccupancyMaxActiveClusters(n, pair_kernel<true, 256>, &cfg);
+    const cudaError_t e = cudaOccupancyMaxActiveClusters(n, chain_kernel, &cfg);
     *n = std::min(*n, kMostPairs);
     return e == cudaSuccess && *n < 1 ? cudaErrorInvalidConfiguration : e;
 }
@@ -1080,7 +1136,7 @@ static cudaError_t chain(const Table& t, const void* grad, float* momentum, floa
     const int64_t at = up((int64_t)t.chunk_at[t.n] * 8, 1024);
     float* inv_norm = reinterpret_cast<float*>(ws + at);
     int* arrived = reinterpret_cast<int*>(ws + at) + t.n;
-    if ((e = cudaMemsetAsync(arrived, 0, t.n * sizeof(int), s)) != cudaSuccess) return e;
+    if ((e = cudaMemsetAsync(arrived, 0, (t.n + kMaxPhases) * sizeof(int), s)) != cudaSuccess) return e;
     // whole sectors per lane (and with them 16-byte accesses of the second pass)
     const int vec = (uintptr_t)grad % (8 * sizeof(T)) == 0 && (uintptr_t)momentum % 32 == 0;
     // (a plain launch: the first kernel waits for everything before it)
@@ -1091,60 +1147,52 @@ static cudaError_t chain(const Table& t, const void* grad, float* momentum, floa
     if ((e = launch(normalize_kernel<T>, dim3(t.unit_at[t.n]), 256, 0, s, t, (const T*)grad, (const float*)momentum, mu,
                     nesterov, vec, (const float*)inv_norm, ws)) != cudaSuccess)
         return e;
-    const auto two = [](int k) { return ldexpf(1.0f, k); };
     // the workspace as rows of 128 bytes; a box is one unit (its bytes are in the tensor cores' order already)
     CUtensorMap map{};
-    if (!sidco_internal::byte_map(&map, ws, 128, ws_bytes / 128, 128, 128, kUnit, false))
-        return cudaErrorNotSupported;
-    const int n_sym = t.sym_at[t.n], n_apply = t.apply_at[t.n];
-    const Tile* tiles = reinterpret_cast<const Tile*>(ws + t.tiles);
-    const auto pair = [&](auto kernel, int smem, const Tile* first, int n, int products, const Chain& c) {
-        return launch(kernel, dim3(2 * std::min(max_pairs, n * products)), kPairThreads, (size_t)smem, s, map,
-                      PairWork{first, n, products}, ws, c, (__nv_bfloat16*)out, timeouts);
+    if (!sidco_internal::byte_map(&map, ws, 128, ws_bytes / 128, 128, 128, kUnit, false)) return cudaErrorNotSupported;
+    Phases ph{};
+    ph.sym_width = t.sym_width;
+    ph.sym_tiles = t.sym_at[t.n];
+    ph.apply_width = t.apply_width;
+    ph.apply_tiles = t.apply_at[t.n];
+    const auto two = [](int k) { return ldexpf(1.0f, k); };
+    int in = 0;
+    const auto sym = [&](int left, int right, int plus, int to, float alpha, float beta, float gamma) {
+        ph.p[ph.n++] = Phase{1, (int8_t)left, (int8_t)right, (int8_t)plus, (int8_t)to, (int8_t)in, 0, 0, alpha, beta, gamma};
     };
-    const auto sym = [&](const Chain& c, int products) {
-        return t.sym_width == 256 ? pair(pair_kernel<true, 256>, kPairSmem<256>, tiles, n_sym, products, c)
-                                  : pair(pair_kernel<true, 128>, kPairSmem<128>, tiles, n_sym, products, c);
+    const auto polynomial = [&](int a, int to) {
+        sym(a, a, a, to, kCc * two(kB - 2 * kA), kCb * two(kB - kA), kCa * two(kB));
     };
-    const auto apply = [&](const Chain& c) {
-        return t.apply_width == 256 ? pair(pair_kernel<false, 256>, kPairSmem<256>, tiles + n_sym, n_apply, 1, c)
-                                    : pair(pair_kernel<false, 128>, kPairSmem<128>, tiles + n_sym, n_apply, 1, c);
-    };
-    int done = 0, in = 0;
-    while (done < steps) {
+    for (int done = 0; done < steps;) {
         const int group = steps == 1 || (done == 2 && steps % 2) ? 1 : 2;
-        Chain c{};
-        c.x_in = in;
-        in ^= 1;
-        int A = kBufA, A2 = kBufA2, P = kBufP, P2 = kBufP2, scale_p = kB;
-        c.p[0] = Product{-1, -1, -1, A, two(kA - 2 * kX), 0.0f, 0.0f};
-        if ((e = sym(c, 1)) != cudaSuccess) return e;
-        for (int i = 0; i < group; ++i) {
-            const int B = i == 0 ? P : (int)kBufB;
-            c.p[0] = Product{A, A, A, B, kCc * two(kB - 2 * kA), kCb * two(kB - kA), kCa * two(kB)};
-            if ((e = sym(c, 1)) != cudaSuccess) return e;
-            int n = 0;
-            const bool more = i + 1 < group;
-            if (more) c.p[n++] = Product{B, A, -1, kBufT, two(-kB), 0.0f, 0.0f};
-            if (i > 0) {
-                c.p[n++] = Product{B, P, -1, P2, two(kP - kB - scale_p), 0.0f, 0.0f};
-                std::swap(P, P2);
-                scale_p = kP;
-            }
-            if (n > 0 && (e = sym(c, n)) != cudaSuccess) return e;
-            if (more) {
-                c.p[0] = Product{kBufT, B, -1, A2, two(-kB), 0.0f, 0.0f};
-                if ((e = sym(c, 1)) != cudaSuccess) return e;
-                std::swap(A, A2);
-            }
+        sym(-1, -1, -1, kBufA, two(kA - 2 * kX), 0.0f, 0.0f);
+        polynomial(kBufA, kBufB);
+        if (group == 2) {
+            sym(kBufB, kBufA, -1, kBufT, two(-kB), 0.0f, 0.0f);                       // B A
+            sym(kBufT, kBufB, -1, kBufA2, two(-kB), 0.0f, 0.0f);                      // the next A = B A B
+            polynomial(kBufA2, kBufT);
+            sym(kBufT, kBufB, -1, kBufP, two(kP - 2 * kB), 0.0f, 0.0f);
         }
         done += group;
-        c.op = P;
-        c.last = done == steps;
-        c.alpha = c.last ? two(-scale_p - kX) : two(-scale_p);
-        if ((e = apply(c)) != cudaSuccess) return e;
+        const int scale_p = group == 2 ? kP : kB, last = done == steps;
+        ph.p[ph.n++] = Phase{0, (int8_t)(group == 2 ? kBufP : kBufB), 0, -1, 0, (int8_t)in, (int8_t)last, 0,
+                             last ? two(-scale_p - kX) : two(-scale_p), 0.0f, 0.0f};
+        in ^= 1;
     }
-    return cudaSuccess;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(2 * max_pairs);
+    cfg.blockDim = dim3(kChainThreads);
+    cfg.dynamicSmemBytes = kChainSmem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeCooperative;                         // all CTAs are resident: they wait for one another
+    attr.val.cooperative = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    e = cudaLaunchKernelEx(&cfg, chain_kernel, map, ph, (const Tile*)(ws + t.tiles), ws, (__nv_bfloat16*)out,
+                           (unsigned*)(arrived + t.n), timeouts);
+    if (e == cudaSuccess) sidco_internal::note_launch();
+    return e;
 }
 
 // Small matrices with equally many CTAs each: a cluster as large as the longest needs.
@@ -1224,10 +1272,7 @@ static int orthogonalize(const void* grad, int grad_type, float* momentum, float
         if ((e = cudaFuncSetAttribute(small_kernel<float>, most, kSmallSmem)) != cudaSuccess ||
             (e = cudaFuncSetAttribute(small_kernel<__nv_bfloat16>, most, kSmallSmem)) != cudaSuccess ||
             (e = cudaFuncSetAttribute(small_kernel<__half>, most, kSmallSmem)) != cudaSuccess ||
-            (e = cudaFuncSetAttribute(pair_kernel<true, 256>, most, kPairSmem<256>)) != cudaSuccess ||
-            (e = cudaFuncSetAttribute(pair_kernel<false, 256>, most, kPairSmem<256>)) != cudaSuccess ||
-            (e = cudaFuncSetAttribute(pair_kernel<true, 128>, most, kPairSmem<128>)) != cudaSuccess ||
-            (e = cudaFuncSetAttribute(pair_kernel<false, 128>, most, kPairSmem<128>)) != cudaSuccess ||
+            (e = cudaFuncSetAttribute(chain_kernel, most, kChainSmem)) != cudaSuccess ||
             (e = resident_pairs(&pairs)) != cudaSuccess)
             return (int)e;
         pair_count[dev] = pairs;
