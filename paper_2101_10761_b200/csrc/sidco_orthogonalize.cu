@@ -355,24 +355,24 @@ struct Phases {
 // products of the next.
 //   warp 0     feeds the stages (each CTA its half of the rows of A and of B)
 //   warp 1     issues the products (first CTA)
-//   warps 2-5  take the sums out, a quarter of the CTA's 128 rows each
+//   warps 2-9  take the sums out: a quarter of the CTA's 128 rows, one half of every 64 columns
 // Between phases only the thread that feeds the stages and the one that fetches matrices to add wait for the others
 // (bounded): every CTA counts itself into the phase when its results are stored.  As launches of their own the phases cost 3 us more
 // each (set-up, first loads, start and end of a kernel).
 
 constexpr int kOutBytes = 4 * kUnitBytes;                             // 64 columns: the images of a tile part and its mirror
-constexpr int kChainThreads = 192;
+constexpr int kChainThreads = 320;
 constexpr int kStages = 5;
 constexpr int kStageBytes = 4 * kUnitBytes;                           // per CTA: 128 x 64 of A, up to 128 x 64 of B
 constexpr int kChainSmem = kStages * kStageBytes + 2 * kOutBytes + 1024;
 
-__device__ __forceinline__ void epilogue_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
+__device__ __forceinline__ void epilogue_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 
-// The same, telling whether all of the 128 threads say so.  (They go on or stop together: one that stopped alone would leave
+// The same, telling whether all of the 256 threads say so.  (They go on or stop together: one that stopped alone would leave
 // the others at the next barrier.)
 __device__ __forceinline__ bool epilogue_all(bool ok) {
     uint32_t all;
-    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.and.aligned.pred q, 1, 128, p;\n\t"
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.and.aligned.pred q, 1, 256, p;\n\t"
                  "selp.b32 %0, 1, 0, q;\n\t}"
                  : "=r"(all) : "r"((uint32_t)ok) : "memory");
     return all != 0;
@@ -413,7 +413,7 @@ __global__ void __launch_bounds__(kChainThreads, 1) __cluster_dims__(2)
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(smem_addr(&s_sums[i]), 1);
-            mbar_init(smem_addr(&s_taken[i]), 8);                     // four warps of both CTAs
+            mbar_init(smem_addr(&s_taken[i]), 16);                    // eight warps of both CTAs
             mbar_init(smem_addr(&s_plus[i]), 1);
         }
         s_failed = 0;
@@ -508,7 +508,7 @@ __global__ void __launch_bounds__(kChainThreads, 1) __cluster_dims__(2)
             }
         }
     } else {
-        const int quarter = warp & 3, row = quarter * 32 + lane, e0 = threadIdx.x == 64;
+        const int quarter = warp & 3, h = (warp - 2) >> 2, row = quarter * 32 + lane, e0 = threadIdx.x == 64;
         const uint32_t out0 = stage0 + kStages * kStageBytes;
         uint8_t* out_smem = smem + kStages * kStageBytes;
         const uint32_t taken[2] = {in_cta(smem_addr(&s_taken[0]), 0), in_cta(smem_addr(&s_taken[1]), 0)};
@@ -556,13 +556,13 @@ __global__ void __launch_bounds__(kChainThreads, 1) __cluster_dims__(2)
                         mbar_wait(smem_addr(&s_plus[part & 1]), (fetched >> 1) & 1, &s_failed);
                         ++fetched;
                         __syncwarp();
-                    } else {
-                        // the stores that read this buffer two parts ago are done reading
+                    } else if (!last) {
+                        // the stores that read this buffer two parts ago are done reading (rows for the caller are read
+                        // by all warps before the barrier of the next part)
                         if (e0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
                         epilogue_sync();
                     }
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
+                    {
                         const int q = cu * 2 + h;
                         uint32_t acc[32];
                         tmem_load32(tmem + buf * 256 + ((uint32_t)(quarter * 32) << 16) + q * 32, acc);
@@ -644,7 +644,7 @@ __global__ void __launch_bounds__(kChainThreads, 1) __cluster_dims__(2)
                         if (even) {
                             const int k = lane * 2;
 #pragma unroll 8
-                            for (int a = quarter; a < n_lines; a += 4) {
+                            for (int a = warp - 2; a < n_lines; a += 8) {
                                 const __nv_bfloat16* from = s_out + a * pitch;
                                 __nv_bfloat16* line = to + (int64_t)a * d.cols;
                                 if (k < n_len)
@@ -655,10 +655,9 @@ __global__ void __launch_bounds__(kChainThreads, 1) __cluster_dims__(2)
                             }
                         } else {
 #pragma unroll 4
-                            for (int a = quarter; a < n_lines; a += 4)
+                            for (int a = warp - 2; a < n_lines; a += 8)
                                 for (int k = lane; k < n_len; k += 32) to[(int64_t)a * d.cols + k] = s_out[a * pitch + k];
                         }
-                        if (e0) bulk_store_commit();                  // (an empty group keeps the count of parts)
                     }
                 }
             }
