@@ -356,25 +356,28 @@ struct Phases {
 //   warp 0     feeds the stages (each CTA its half of the rows of A and of B)
 //   warp 1     issues the products (first CTA)
 //   warps 2-9  take the sums out: a quarter of the CTA's 128 rows, one half of every 64 columns
-// Between phases only the thread that feeds the stages and the one that fetches matrices to add wait for the others
-// (bounded): every CTA counts itself into the phase when its results are stored.  As launches of their own the phases cost 3 us more
+//   warp 10    stores what they have put together, and fetches matrices to add (a warp that did both lost 0.5 us per store)
+// Between phases only the threads that start loads wait for the others (bounded): every CTA counts itself into the phase when its results are stored.  As launches of their own the phases cost 3 us more
 // each (set-up, first loads, start and end of a kernel).
 
 constexpr int kOutBytes = 4 * kUnitBytes;                             // 64 columns: the images of a tile part and its mirror
-constexpr int kChainThreads = 320;
+constexpr int kChainThreads = 352;
 constexpr int kStages = 5;
 constexpr int kStageBytes = 4 * kUnitBytes;                           // per CTA: 128 x 64 of A, up to 128 x 64 of B
 constexpr int kChainSmem = kStages * kStageBytes + 2 * kOutBytes + 1024;
 
+// Barriers of the 256 threads that take the sums out, and of these with the warp that stores.
 __device__ __forceinline__ void epilogue_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+constexpr int kFreeBarrier = 2, kFilledBarrier = 4, kGoBarrier = 6;   // (one per buffer)
+__device__ __forceinline__ void store_sync(int id) { asm volatile("bar.sync %0, 288;" ::"r"(id) : "memory"); }
+__device__ __forceinline__ void store_arrive(int id) { asm volatile("bar.arrive %0, 288;" ::"r"(id) : "memory"); }
 
-// The same, telling whether all of the 256 threads say so.  (They go on or stop together: one that stopped alone would leave
-// the others at the next barrier.)
-__device__ __forceinline__ bool epilogue_all(bool ok) {
+// Whether all 288 say so.  (They go on or stop together: one that stopped alone would leave the others at a barrier.)
+__device__ __forceinline__ bool store_all(bool ok) {
     uint32_t all;
-    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.and.aligned.pred q, 1, 256, p;\n\t"
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.and.aligned.pred q, %2, 288, p;\n\t"
                  "selp.b32 %0, 1, 0, q;\n\t}"
-                 : "=r"(all) : "r"((uint32_t)ok) : "memory");
+                 : "=r"(all) : "r"((uint32_t)ok), "n"(kGoBarrier) : "memory");
     return all != 0;
 }
 
@@ -507,9 +510,70 @@ __global__ void __launch_bounds__(kChainThreads, 1) __cluster_dims__(2)
                 }
             }
         }
-    } else {
-        const int quarter = warp & 3, h = (warp - 2) >> 2, row = quarter * 32 + lane, e0 = threadIdx.x == 64;
+    } else if (warp == 10) {
         const uint32_t out0 = stage0 + kStages * kStageBytes;
+        int part = 0;
+        bool ok = true;
+        for (int f = 0; f < ph.n && ok; ++f) {
+            const Phase& p = ph.p[f];
+            const bool sym = p.sym, last = p.last, plus = p.plus >= 0;
+            const int width = sym ? ph.sym_width : ph.apply_width, parts = width / 64;
+            const int total = sym ? ph.sym_tiles : ph.apply_tiles;
+            const Tile* list = tiles + (sym ? 0 : ph.sym_tiles);
+            bool waited = f == 0;
+            for (int i = first; i < total; i += n_pairs) {
+                const Tile d = list[i];
+                const int small = d.spu * d.spu, rb = d.ti * 4 + (int)rank * 2;
+                const bool mirror = sym && d.tj < d.ti * (kRows / width);
+                const int base = sym ? d.small + p.to * small : p.x_in ? d.x[0] : d.x[1];
+                // part `cu` of the tile may be filled: its buffer has been read, and holds the 64 columns to add
+                const auto prepare = [&](int cu, int to) {
+                    if (elect_one()) {
+                        bulk_store_wait_read();
+                        if (plus) {
+                            const uint32_t bar = smem_addr(&s_plus[to]);
+                            mbar_expect_tx(bar, 2 * kUnitBytes);
+                            bulk_load(out0 + to * kOutBytes,
+                                      ws + (int64_t)(d.small + p.plus * small + (d.tj * parts + cu) * d.spu + rb) * kUnitBytes,
+                                      2 * kUnitBytes, bar);
+                        }
+                    }
+                    __syncwarp();
+                    if (!plus) store_arrive(kFreeBarrier + to);
+                };
+                if (plus && !waited) wait_arrivals(arrived + f - 1, gridDim.x, &s_failed);
+                waited = true;
+                __syncwarp();
+                if (!last) prepare(0, part & 1);
+                ok = store_all(true);
+                if (!ok) break;
+                if (last) continue;
+                for (int cu = 0; cu < parts; ++cu, ++part) {
+                    if (cu + 1 < parts) prepare(cu + 1, (part & 1) ^ 1);
+                    store_sync(kFilledBarrier + (part & 1));
+                    const int cb = d.tj * parts + cu;
+                    if (elect_one() && (sym || cb < d.lu)) {
+                        const uint32_t img = out0 + (part & 1) * kOutBytes;
+                        bulk_store(ws + (int64_t)(base + cb * d.spu + rb) * kUnitBytes, img, 2 * kUnitBytes);
+                        if (mirror)
+                            for (int u = 0; u < 2; ++u)
+                                bulk_store(ws + (int64_t)(base + (rb + u) * d.spu + cb) * kUnitBytes, img + (2 + u) * kUnitBytes,
+                                           kUnitBytes);
+                        bulk_store_commit();
+                    }
+                    __syncwarp();
+                }
+            }
+            if (!last && elect_one()) {                               // stored: count this CTA in
+                bulk_store_wait();
+                fence_async_all();
+                __threadfence();
+                asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(arrived + f) : "memory");
+            }
+            __syncwarp();
+        }
+    } else {
+        const int quarter = warp & 3, h = (warp - 2) >> 2, row = quarter * 32 + lane;
         uint8_t* out_smem = smem + kStages * kStageBytes;
         const uint32_t taken[2] = {in_cta(smem_addr(&s_taken[0]), 0), in_cta(smem_addr(&s_taken[1]), 0)};
         int n = 0, part = 0, fetched = 0;
@@ -521,47 +585,29 @@ __global__ void __launch_bounds__(kChainThreads, 1) __cluster_dims__(2)
             const int total = sym ? ph.sym_tiles : ph.apply_tiles;
             const Tile* list = tiles + (sym ? 0 : ph.sym_tiles);
             const float alpha = p.alpha, beta = p.beta, gamma = p.gamma;
-            bool waited = f == 0;
             for (int i = first; i < total; i += n_pairs, ++n) {
                 const Tile d = list[i];
-                const int small = d.spu * d.spu, buf = n & 1;
-                const int rb = d.ti * 4 + rank * 2;                   // first unit row of this CTA's part
+                const int buf = n & 1;
+                const int rb = d.ti * 4 + (int)rank * 2;              // first unit row of this CTA's part
                 const bool mirror = sym && d.tj < d.ti * (kRows / width), tall = d.rows > d.cols;
-                const int base = sym ? d.small + p.to * small : p.x_in ? d.x[0] : d.x[1];
-                // 64 columns of the matrix to add are brought to where their sums will be written, one part ahead
-                const auto fetch = [&](int cu, int to) {              // (the buffer's last stores are done reading)
-                    asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
-                    const uint32_t bar = smem_addr(&s_plus[to]);
-                    mbar_expect_tx(bar, 2 * kUnitBytes);
-                    bulk_load(out0 + to * kOutBytes,
-                              ws + (int64_t)(d.small + p.plus * small + (d.tj * parts + cu) * d.spu + rb) * kUnitBytes,
-                              2 * kUnitBytes, bar);
-                };
-                if (plus && e0) {
-                    if (!waited) wait_arrivals(arrived + f - 1, gridDim.x, &s_failed);
-                    waited = true;
-                    fetch(0, part & 1);
-                }
                 const int diagonal = d.ti * kRows + (int)rank * 128 + row - d.tj * width;     // the column on the diagonal
                 ok = mbar_wait(smem_addr(&s_sums[buf]), (n >> 1) & 1, &s_failed);
                 __syncwarp();
-                ok = epilogue_all(ok);
+                ok = store_all(ok);
                 if (!ok) break;
                 fence_after_sync();
 #pragma unroll 1
                 for (int cu = 0; cu < parts; ++cu, ++part) {
                     uint8_t* img = out_smem + (part & 1) * kOutBytes;
-                    const uint32_t img_addr = out0 + (part & 1) * kOutBytes;
+                    __syncwarp();
                     if (plus) {
                         mbar_wait(smem_addr(&s_plus[part & 1]), (fetched >> 1) & 1, &s_failed);
                         ++fetched;
                         __syncwarp();
                     } else if (!last) {
-                        // the stores that read this buffer two parts ago are done reading (rows for the caller are read
-                        // by all warps before the barrier of the next part)
-                        if (e0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
-                        epilogue_sync();
-                    }
+                        store_sync(kFreeBarrier + (part & 1));
+                    }                                                 // (rows for the caller are read by all warps before
+                                                                      // the barrier of the next part)
                     {
                         const int q = cu * 2 + h;
                         uint32_t acc[32];
@@ -617,21 +663,10 @@ __global__ void __launch_bounds__(kChainThreads, 1) __cluster_dims__(2)
                         __syncwarp();
                         if (lane == 0) mbar_arrive_cluster(taken[buf]);
                     }
+                    __syncwarp();
                     if (!last) {
                         fence_async_shared();
-                        epilogue_sync();
-                        if (e0) {
-                            const int cb = d.tj * parts + cu;
-                            if (sym || cb < d.lu) {
-                                bulk_store(ws + (int64_t)(base + cb * d.spu + rb) * kUnitBytes, img_addr, 2 * kUnitBytes);
-                                if (mirror)
-                                    for (int u = 0; u < 2; ++u)
-                                        bulk_store(ws + (int64_t)(base + (rb + u) * d.spu + cb) * kUnitBytes,
-                                                   img_addr + (2 + u) * kUnitBytes, kUnitBytes);
-                            }
-                            bulk_store_commit();
-                            if (plus && cu < parts - 1) fetch(cu + 1, (part & 1) ^ 1);
-                        }
+                        store_arrive(kFilledBarrier + (part & 1));
                     } else {
                         epilogue_sync();
                         const __nv_bfloat16* s_out = reinterpret_cast<const __nv_bfloat16*>(img);
@@ -661,14 +696,7 @@ __global__ void __launch_bounds__(kChainThreads, 1) __cluster_dims__(2)
                     }
                 }
             }
-            if (e0 && !last) {                                        // stored: count this CTA in
-                bulk_store_wait();
-                fence_async_all();
-                __threadfence();
-                asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(arrived + f) : "memory");
-            }
         }
-        if (e0) bulk_store_wait();
     }
     __syncwarp();
     fence_before_sync();
