@@ -386,13 +386,14 @@ __device__ __forceinline__ bool wait_arrivals(const unsigned* arrived, unsigned 
     const unsigned long long start = time_ns();
     for (uint32_t i = 1;; ++i) {
         unsigned v;
-        asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(arrived) : "memory");
+        asm volatile("ld.relaxed.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(arrived) : "memory");
         if (v >= count) break;
         if ((i & 63u) == 0u && (*failed || time_ns() - start > kWaitLimitNs)) {
             *failed = 1;
             return false;
         }
     }
+    asm volatile("fence.acq_rel.gpu;" ::: "memory");
     fence_async_all();                                                // (what they stored is read by bulk copies)
     return true;
 }
@@ -567,7 +568,6 @@ __global__ void __launch_bounds__(kChainThreads, 1) __cluster_dims__(2)
             if (!last && elect_one()) {                               // stored: count this CTA in
                 bulk_store_wait();
                 fence_async_all();
-                __threadfence();
                 asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(arrived + f) : "memory");
             }
             __syncwarp();
