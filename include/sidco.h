@@ -43,14 +43,14 @@ extern "C" {
 
 /* argument errors (returned before any work is enqueued) */
 #define SIDCO_E_NULL        (-1)   /* a required pointer is NULL */
-#define SIDCO_E_SEGMENTS    (-2)   /* n_segs < 1, offsets[0] != 0, offsets decreasing, or d too large */
+#define SIDCO_E_SEGMENTS    (-2)   /* n_segs < 1, offsets[0] != 0, offsets decreasing, or d too large; matrices that overlap */
 #define SIDCO_E_DELTA       (-3)   /* delta not in (0, 1) */
 #define SIDCO_E_SID         (-4)   /* unknown sid_type */
 #define SIDCO_E_STAGES      (-5)   /* max_stages == 0 or |max_stages| > SIDCO_MAX_STAGES */
 #define SIDCO_E_PARAMS      (-6)   /* sidco_set_params: value out of range */
 #define SIDCO_E_UNKNOWN_KEY (-7)   /* no state exists for this residual pointer */
 #define SIDCO_E_WORKSPACE   (-8)   /* caller-provided workspace too small or misaligned */
-#define SIDCO_E_ALIAS       (-9)   /* grad and residual overlap */
+#define SIDCO_E_ALIAS       (-9)   /* buffers that must not overlap do */
 #define SIDCO_E_SIZE        (-10)  /* size beyond the limit of this entry point */
 #define SIDCO_E_CAPTURE     (-11)  /* the call would have to allocate or upload tables while `stream` is capturing */
 #define SIDCO_E_UNSUPPORTED (-12)  /* the function needs a build of the library with another compile-time switch */
@@ -336,11 +336,17 @@ int sidco_mx4_mean(const uint8_t* codes_all, const uint8_t* scales_all, int n_wo
  * momentum  device, float[], in/out; NULL: U = grad (mu and nesterov are not used).
  * mu        in [0, 1).     eps >= 0.     steps in 1 .. SIDCO_ORTHO_MAX_STEPS.
  * offsets, rows, cols   HOST, int64[n_mats], read during the call only.  Empty matrices are allowed; the longer side is
- *           at most SIDCO_ORTHO_MAX_DIM, the shorter at most SIDCO_ORTHO_MAX_SHORT.  Matrices must not overlap.
- * out_bf16  device, bf16 bit patterns, same layout as grad; must not overlap grad or momentum.
+ *           at most SIDCO_ORTHO_MAX_DIM, the shorter at most SIDCO_ORTHO_MAX_SHORT.  Matrices that overlap are refused
+ *           (SIDCO_E_SEGMENTS).
+ * out_bf16  device, bf16 bit patterns, same layout as grad.  grad, momentum and out_bf16 must not overlap between the first
+ *           element of the first matrix and the last of the last (SIDCO_E_ALIAS).
  * workspace device, 256-byte aligned, at least sidco_orthogonalize_workspace_bytes(rows, cols, n_mats) bytes; caller-owned,
- *           nothing is kept in it between calls; not to be shared by calls that overlap.
- * stream    everything is enqueued here (about twenty launches for five steps); no synchronisation, no allocation.
+ *           nothing is kept in it between calls; not to be shared by calls that overlap.  Matrices with a shorter side of
+ *           at most 128 and a longer one of at most 2048 need none: the size may be 0, the pointer NULL.
+ * stream    everything is enqueued here (one launch for small matrices, three and a small clear for others, for up to 128
+ *           matrices of a kind); no synchronisation, no device allocation.  With matrices of both kinds the small ones run
+ *           on a stream of the library that is forked from and joined to this one within the call (not while this one
+ *           is being captured).  The kernel for larger matrices is launched cooperatively.
  */
 #define SIDCO_ORTHO_MAX_DIM   4194304
 #define SIDCO_ORTHO_MAX_SHORT 16384

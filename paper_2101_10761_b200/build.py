@@ -14,7 +14,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 SOURCES = sorted(glob.glob(os.path.join(CSRC, "*.cu")))
-DEPS = SOURCES + sorted(glob.glob(os.path.join(CSRC, "*.cuh"))) + \
+DEPS = SOURCES + sorted(glob.glob(os.path.join(CSRC, "*.cuh"))) + sorted(glob.glob(os.path.join(CSRC, "*.h"))) + \
     sorted(glob.glob(os.path.join(os.path.dirname(HERE), "include", "*.h")))
 VARIANTS = {"": [], "profile": ["-DSIDCO_PROFILE"], "check": ["-DSIDCO_BOUNDS_CHECK"]}
 

@@ -934,14 +934,14 @@ const char* sidco_error_string(int code) {
     switch (code) {
         case 0: return "success";
         case SIDCO_E_NULL: return "a required pointer is NULL";
-        case SIDCO_E_SEGMENTS: return "bad segment table (n_segs < 1, offsets[0] != 0, decreasing, or d too large)";
+        case SIDCO_E_SEGMENTS: return "bad segment table (n_segs < 1, offsets[0] != 0, decreasing, or d too large) or overlapping matrices";
         case SIDCO_E_DELTA: return "delta must lie in (0, 1)";
         case SIDCO_E_SID: return "unknown sid_type";
         case SIDCO_E_STAGES: return "max_stages must be non-zero and at most SIDCO_MAX_STAGES in magnitude";
         case SIDCO_E_PARAMS: return "parameter out of range";
         case SIDCO_E_UNKNOWN_KEY: return "no state for this residual pointer";
         case SIDCO_E_WORKSPACE: return "workspace too small, misaligned, or set too late";
-        case SIDCO_E_ALIAS: return "grad and residual overlap";
+        case SIDCO_E_ALIAS: return "buffers that must not overlap do";
         case SIDCO_E_SIZE: return "size beyond the limit of this entry point";
         case SIDCO_E_CAPTURE:
             return "first call for this residual and segment table must be made before stream capture begins";

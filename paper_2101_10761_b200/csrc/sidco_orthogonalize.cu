@@ -30,6 +30,7 @@
 #include <algorithm>
 #include <atomic>
 #include <mutex>
+#include <utility>
 #include <vector>
 
 #include "../../include/sidco.h"
@@ -1108,6 +1109,25 @@ static int check_shapes(const int64_t* rows, const int64_t* cols, int n) {
     return 0;
 }
 
+// The matrices lie apart from each other, and so do the parts of the vectors that they take up.
+static int check_places(const int64_t* offsets, const int64_t* rows, const int64_t* cols, int n, uintptr_t grad, uintptr_t size,
+                        uintptr_t momentum, uintptr_t out) {
+    std::vector<std::pair<int64_t, int64_t>> at;
+    for (int i = 0; i < n; ++i) {
+        if (offsets[i] < 0 || offsets[i] > (int64_t)1 << 46) return SIDCO_E_SEGMENTS;
+        if (rows[i] && cols[i]) at.emplace_back(offsets[i], offsets[i] + rows[i] * cols[i]);
+    }
+    std::sort(at.begin(), at.end());
+    for (size_t i = 1; i < at.size(); ++i)
+        if (at[i].first < at[i - 1].second) return SIDCO_E_SEGMENTS;
+    const uintptr_t lo = (uintptr_t)at.front().first, hi = (uintptr_t)at.back().second;
+    const auto meet = [&](uintptr_t p, uintptr_t p_size, uintptr_t q, uintptr_t q_size) {
+        return p + lo * p_size < q + hi * q_size && q + lo * q_size < p + hi * p_size;
+    };
+    if (meet(grad, size, out, 2) || (momentum && (meet(grad, size, momentum, 4) || meet(out, 2, momentum, 4)))) return SIDCO_E_ALIAS;
+    return 0;
+}
+
 static int64_t workspace_bytes(const int64_t* rows, const int64_t* cols, int n) {
     const std::vector<int> order = order_of(rows, cols, n, false);
     std::vector<Table> t(1);
@@ -1207,7 +1227,7 @@ static cudaError_t chain(const Table& t, const void* grad, float* momentum, floa
         in ^= 1;
     }
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(2 * max_pairs);
+    cfg.gridDim = dim3(2 * std::min(max_pairs, std::max(ph.sym_tiles, ph.apply_tiles)));
     cfg.blockDim = dim3(kChainThreads);
     cfg.dynamicSmemBytes = kChainSmem;
     cfg.stream = s;
@@ -1281,10 +1301,10 @@ static int orthogonalize(const void* grad, int grad_type, float* momentum, float
     const std::vector<int> order = order_of(rows, cols, n_mats, false), small = order_of(rows, cols, n_mats, true);
     if (order.empty() && small.empty()) return 0;
     if (!grad || !out_bf16 || !offsets || (!workspace && !order.empty())) return SIDCO_E_NULL;
-    for (int i = 0; i < n_mats; ++i)
-        if (offsets[i] < 0) return SIDCO_E_SEGMENTS;
     const uintptr_t size = grad_type == SIDCO_T_F32 ? 4 : 2;
     if ((uintptr_t)grad % size || (uintptr_t)momentum % 4 || (uintptr_t)out_bf16 % 2) return SIDCO_E_ALIGN;
+    if ((rc = check_places(offsets, rows, cols, n_mats, (uintptr_t)grad, size, (uintptr_t)momentum, (uintptr_t)out_bf16)))
+        return rc;
     const int64_t need = sidco_ortho::workspace_bytes(rows, cols, n_mats);
     if (need < 0) return (int)need;
     if (need > 0 && ((uintptr_t)workspace % 256 || workspace_bytes < (size_t)need)) return SIDCO_E_WORKSPACE;

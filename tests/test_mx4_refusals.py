@@ -110,6 +110,8 @@ def test_orthogonalize_refuses(B):
     big = dict(rows=(300,), cols=(200,))                          # (small matrices need no workspace)
     assert call(grad=None) == -1 and call(out=None) == -1 and call(ws=None, **big) == -1
     assert call(off=(-4,)) == -2
+    assert call(off=(0, 63), rows=(8, 4), cols=(8, 4)) == -2 and call(off=(3, 0), rows=(8, 2), cols=(8, 2)) == -2    # overlap
+    assert call(out=P + 16) == -9 and call(mom=P + 128) == -9 and call(mom=3 * P - 128) == -9
     assert call(grad=P + 2) == -14 and call(mom=P + 1) == -14 and call(out=P + 1) == -14
     need = B.sidco_orthogonalize_workspace_bytes([300], [200])
     assert call(n=need - 1, **big) == -8 and call(ws=4 * P + 8, **big) == -8
