@@ -29,6 +29,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <initializer_list>
 #include <mutex>
 #include <utility>
 #include <vector>
@@ -712,7 +713,9 @@ __global__ void __launch_bounds__(kChainThreads, 1) __cluster_dims__(2)
 // Matrices with s <= 128 and l <= 2048: one cluster of CTAs per matrix does the whole update in one launch.  Every CTA
 // keeps its columns of X (up to 256: 64 KB) in shared memory from the first step to the last.  The only exchange between the CTAs is a sum per Gram matrix: each adds its share of the rows of all partial
 // Gram matrices through distributed shared memory, in the order of the CTAs, and hands the result to the others; the
-// s x s products that follow (a few hundred nanoseconds each) every CTA does for itself.
+// s x s products that follow (a few hundred nanoseconds each) every CTA does for itself.  The B and their product are kept
+// as sums of two fp16 parts: with few rows their rounding is the largest error (2.0e-3 instead of 2.9e-3 for 32 x 288), and
+// the products of the second parts cost next to nothing here.
 
 constexpr int kSmallS = 128, kSmallUnits = 4, kSmallCluster = 8;      // units of columns per CTA, CTAs per matrix: at most
 constexpr int kSmallThreads = 512;
@@ -720,7 +723,8 @@ constexpr int kSmallHeld = kSmallS * kSmallUnits * kUnit / kSmallThreads;    // 
 constexpr int kSquareBytes = 4 * kUnitBytes;                          // 128 x 128
 constexpr int kSlabBytes = kSmallUnits * 2 * kUnitBytes;              // 128 x 256
 constexpr int kOutLine = kSmallUnits * kUnit + 2, kOutColumn = kSmallS + 2;   // bf16 per line of the result, wide or tall
-constexpr int kSmallSmem = 3 * kSquareBytes + std::max(kSlabBytes, std::max(kSmallS * kOutLine, kSmallUnits * kUnit * kOutColumn) * 2) +
+constexpr int kSquares = 5;
+constexpr int kSmallSmem = kSquares * kSquareBytes + std::max(kSlabBytes, std::max(kSmallS * kOutLine, kSmallUnits * kUnit * kOutColumn) * 2) +
                            1024;
 
 struct SmallMats {
@@ -762,8 +766,8 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
     const int first = (int)(lu * rank / ctas), units = (int)(lu * (rank + 1) / ctas) - first;   // of this CTA's columns
 
     uint8_t* smem = (uint8_t*)(((uintptr_t)s_raw + 1023) & ~(uintptr_t)1023);
-    uint8_t *sq[3], *slab = smem + 3 * kSquareBytes;
-    for (int i = 0; i < 3; ++i) sq[i] = smem + i * kSquareBytes;
+    uint8_t *sq[kSquares], *slab = smem + kSquares * kSquareBytes;
+    for (int i = 0; i < kSquares; ++i) sq[i] = smem + i * kSquareBytes;
     if (warp == 0) tmem_alloc(&s_tmem, 256);
     if (threadIdx.x == 0) {
         mbar_init(smem_addr(&s_done), 1);
@@ -858,15 +862,19 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
         ++uses;
         fence_after_sync();
     };
-    // to = alpha (left right) + beta plus + gamma I, all 128 x 128
-    const auto square = [&](const uint8_t* left, const uint8_t* right, const uint8_t* plus, uint8_t* to, float alpha,
+    // to + to_lo = alpha (left right + left_2 right_2 + left_3 right_3) + beta plus + gamma I, all 128 x 128
+    struct Term { const uint8_t *left, *right; };
+    const auto square = [&](std::initializer_list<Term> terms, const uint8_t* plus, uint8_t* to, uint8_t* to_lo, float alpha,
                             float beta, float gamma) {
         issue_and_wait([&] {
-            const uint32_t a = smem_addr(left), b = smem_addr(right);
-            for (int k = 0; k < ku * 4; ++k)
-                mma_f16(tmem, swizzled_operand(a + (k >> 2) * 2 * kUnitBytes + (k & 3) * 32, 16, 1024),
-                        swizzled_operand(b + (k >> 2) * 2 * kUnitBytes + (k & 3) * 32, 16, 1024),
-                        f16_shape(kSmallS, kSmallS, false), k > 0);
+            bool add = false;
+            for (const Term& t : terms) {
+                const uint32_t a = smem_addr(t.left), b = smem_addr(t.right);
+                for (int k = 0; k < ku * 4; ++k, add = true)
+                    mma_f16(tmem, swizzled_operand(a + (k >> 2) * 2 * kUnitBytes + (k & 3) * 32, 16, 1024),
+                            swizzled_operand(b + (k >> 2) * 2 * kUnitBytes + (k & 3) * 32, 16, 1024),
+                            f16_shape(kSmallS, kSmallS, false), add);
+            }
         });
         uint32_t acc[32];
         tmem_load32(lanes + side * 32, acc);
@@ -889,6 +897,11 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] += row == side * 32 + o * 8 + j ? gamma : 0.0f;
             *reinterpret_cast<uint4*>(to + at) = pack8(v);
+            if (to_lo) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] -= __half2float(__float2half_rn(v[j]));
+                *reinterpret_cast<uint4*>(to_lo + at) = pack8(v);
+            }
         }
     };
     const auto two = [](int k) { return __uint_as_float((uint32_t)(127 + k) << 23); };
@@ -949,26 +962,32 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
         fence_async_all();                                            // (read by the tensor cores of the other CTAs)
         cluster_sync();
 
-        // A in sq[0]; B in sq[1]; for a second step T, then the next B in sq[2], A and the product in sq[0]
-        uint8_t* p = sq[1];
+        // A in sq[0], B in sq[1] + sq[2]; for a second step T in sq[3], the next A in sq[0], the next B in sq[3] + sq[4] and
+        // the product of both in sq[0] + sq[1]
+        const uint8_t *p = sq[1], *p_lo = sq[2];
         int scale_p = kB;
-        square(sq[0], sq[0], sq[0], sq[1], kCc * two(kB - 2 * kA), kCb * two(kB - kA), kCa * two(kB));
+        const float poly = kCc * two(kB - 2 * kA), linear = kCb * two(kB - kA), unit = kCa * two(kB);
+        square({{sq[0], sq[0]}}, sq[0], sq[1], sq[2], poly, linear, unit);
         if (group == 2) {
-            square(sq[1], sq[0], nullptr, sq[2], two(-kB), 0.0f, 0.0f);
-            square(sq[2], sq[1], nullptr, sq[0], two(-kB), 0.0f, 0.0f);
-            square(sq[0], sq[0], sq[0], sq[2], kCc * two(kB - 2 * kA), kCb * two(kB - kA), kCa * two(kB));
-            square(sq[2], sq[1], nullptr, sq[0], two(kP - 2 * kB), 0.0f, 0.0f);
+            square({{sq[1], sq[0]}, {sq[2], sq[0]}}, nullptr, sq[3], nullptr, two(-kB), 0.0f, 0.0f);
+            square({{sq[3], sq[1]}, {sq[3], sq[2]}}, nullptr, sq[0], nullptr, two(-kB), 0.0f, 0.0f);
+            square({{sq[0], sq[0]}}, sq[0], sq[3], sq[4], poly, linear, unit);
+            square({{sq[3], sq[1]}, {sq[3], sq[2]}, {sq[4], sq[1]}}, nullptr, sq[0], sq[1], two(kP - 2 * kB), 0.0f, 0.0f);
             p = sq[0];
+            p_lo = sq[1];
             scale_p = kP;
         }
 
         // X <- P X on this CTA's columns
         issue_and_wait([&] {
-            const uint32_t a = smem_addr(p), b = smem_addr(slab);
-            for (int k = 0; k < ku * 4 && units; ++k)
-                mma_f16(tmem, swizzled_operand(a + (k >> 2) * 2 * kUnitBytes + (k & 3) * 32, 16, 1024),
-                        swizzled_operand(b + (k >> 2) * kUnitBytes + (k & 3) * 2048, 2 * kUnitBytes, 1024),
+            const uint32_t b = smem_addr(slab);
+            for (int k = 0; k < ku * 8 && units; ++k) {
+                const int q = k < ku * 4 ? k : k - ku * 4;
+                const uint32_t a = smem_addr(k < ku * 4 ? p : p_lo);
+                mma_f16(tmem, swizzled_operand(a + (q >> 2) * 2 * kUnitBytes + (q & 3) * 32, 16, 1024),
+                        swizzled_operand(b + (q >> 2) * kUnitBytes + (q & 3) * 2048, 2 * kUnitBytes, 1024),
                         f16_shape(kSmallS, units * kUnit, true), k > 0);
+            }
         });
         done += group;
         const bool last = done == steps;
