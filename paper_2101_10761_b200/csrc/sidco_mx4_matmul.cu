@@ -8,6 +8,10 @@
 //
 //   pair_kernel   large C: tiles of 256 x 256 by pairs of CTAs, persistent
 //   split_kernel  everything else: tiles of 128 x (16 .. 128), K split over a cluster of CTAs
+//
+// Measured: 8192^3 into bf16 216 us alone (5.1 PFLOP/s, 1000 W: the power limit holds the clock at 1.64 GHz), 255 us in a
+// long loop; 6000 x 1500 x 700 added to fp32 18 us (75 MB, 0.62 of the copy rate); one token times 6000 x 1500 4.6 us
+// inside a graph (4.8 MB: start, one trip to memory, exchange of the sums), times 8192 x 8192 10 us (0.53 of the copy rate).
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -68,7 +72,8 @@ __device__ __forceinline__ int quarters_of(const Args& A, int k) {
 //   warp 0     feeds the stages        warp 1     issues the products (first CTA)
 //   warps 2-9  take the sums out: a quarter of the CTA's 128 rows, two of the four times 64 columns
 // Sums leave through shared memory as boxes of 32 rows x 128 bytes: the tensor copies write (or, in fp32, add) them as whole
-// lines and leave out what lies behind C; rows written by their own lanes took 33 us per tile, ten times as long.
+// lines and leave out what lies behind C.  (Transposed in shared memory and written by single elements they took 33 us per
+// tile, twice the products; 6000 x 1500 x 700 added to fp32 29 us instead of 18.)
 
 constexpr int kPairTile = 256;
 constexpr int kPairThreads = 320;
