@@ -151,11 +151,12 @@ def lib() -> C.CDLL:
 
 def _ptr(x) -> Optional[int]:
     """Raw address of a torch tensor, a numpy array or an int; None stays NULL."""
-    if x is None or isinstance(x, int):
-        return x
-    if isinstance(x, np.ndarray):
-        return x.ctypes.data
-    return x.data_ptr()
+    if x is None:
+        return None
+    try:
+        return x.data_ptr()
+    except AttributeError:
+        return x.ctypes.data if isinstance(x, np.ndarray) else int(x)
 
 
 def _offsets(seg_offsets: Sequence[int]):
