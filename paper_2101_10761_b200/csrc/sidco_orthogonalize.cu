@@ -727,11 +727,10 @@ __global__ void __launch_bounds__(kChainThreads, 1) __cluster_dims__(2)
 
 constexpr int kSmallS = 128, kSmallUnits = 4, kSmallCluster = 8;      // units of columns per CTA, CTAs per matrix: at most
 constexpr int kSmallThreads = 512;
-constexpr int kSmallHeld = kSmallS * kSmallUnits * kUnit / kSmallThreads;    // elements of X that a thread holds: 64
 constexpr int kSquareBytes = 4 * kUnitBytes;                          // 128 x 128
 constexpr int kSlabBytes = kSmallUnits * 2 * kUnitBytes;              // 128 x 256
 constexpr int kOutLine = kSmallUnits * kUnit + 2, kOutColumn = kSmallS + 2;   // bf16 per line of the result, wide or tall
-constexpr int kSquares = 5;
+constexpr int kSquares = 5;                                           // (together larger than X's part in fp32)
 constexpr int kSmallSmem = kSquares * kSquareBytes + std::max(kSlabBytes, std::max(kSmallS * kOutLine, kSmallUnits * kUnit * kOutColumn) * 2) +
                            1024;
 
@@ -754,7 +753,7 @@ __device__ __forceinline__ void remote_store_f64(uint32_t addr, double v) {
     asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(addr), "d"(v) : "memory");
 }
 
-template <typename T>
+template <typename T, int kCtas>
 __global__ void __launch_bounds__(kSmallThreads, 1)
     small_kernel(const __grid_constant__ SmallMats mats, const T* __restrict__ grad, float* __restrict__ momentum, float mu,
                  int nesterov, int steps, float eps, __nv_bfloat16* __restrict__ out, int* timeouts) {
@@ -764,8 +763,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
     __shared__ uint32_t s_tmem;
     __shared__ int s_failed;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    uint32_t ctas;
-    asm("mov.u32 %0, %cluster_nctaid.x;" : "=r"(ctas));
+    constexpr uint32_t ctas = kCtas;
     const uint32_t rank = cluster_rank();
     const auto& m = mats.m[blockIdx.x / ctas];
     const bool tall = m.rows > m.cols;
@@ -783,41 +781,40 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
         mbar_init_fence();
     }
 
-    // ---- momentum and norm.  A thread holds 16 elements of each unit of columns, threads next to each other neighbours of
-    // a row of the caller's matrix: element (unit u, j) is row r, column a of X's part here
+    // ---- momentum and norm.  A thread takes 16 elements of each unit of columns, threads next to each other neighbours of
+    // a row of the caller's matrix.  U waits for its norm, in fp32, where the squares will be: as rows, or as columns if the
+    // matrix is tall, one word longer than they need be against bank conflicts.
     const int r0 = tall ? threadIdx.x & 127 : threadIdx.x >> 6, a0 = tall ? threadIdx.x >> 7 : threadIdx.x & 63;
     const auto row_of = [&](int j) { return tall ? r0 : r0 + 8 * j; };
     const auto col_of = [&](int u, int j) { return u * kUnit + (tall ? a0 + 4 * j : a0); };
     const auto inside = [&](int u, int j) { return u < units && row_of(j) < s && first * kUnit + col_of(u, j) < l; };
     const int64_t base = m.offset + (tall ? (int64_t)(first * kUnit + a0) * m.cols + r0 : (int64_t)r0 * m.cols + first * kUnit + a0);
     const int64_t by_u = (int64_t)kUnit * (tall ? m.cols : 1), by_j = (int64_t)(tall ? 4 : 8) * m.cols;
-    float x[kSmallHeld];
+    float* held = reinterpret_cast<float*>(smem);
+    const int by_row = tall ? 1 : kSmallUnits * kUnit + 1, by_col = tall ? kSmallS + 1 : 1;
     double sums[2] = {};
-#pragma unroll
-    for (int u = 0; u < kSmallUnits; ++u) {
-        if (u >= units) break;
-        float v[16];
+#pragma unroll 1
+    for (int u = 0; u < units; ++u) {
+        const int64_t at = base + u * by_u;
+        float g[16], v[16];
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
             const bool in = inside(u, j);
-            const int64_t at = base + u * by_u + j * by_j;
-            x[u * 16 + j] = in ? widen(grad[at]) : 0.0f;
-            v[j] = in && momentum ? momentum[at] : 0.0f;
+            g[j] = in ? widen(grad[at + j * by_j]) : 0.0f;
+            v[j] = in && momentum ? momentum[at + j * by_j] : 0.0f;
         }
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
-            float& y = x[u * 16 + j];
             if (momentum) {
-                const float mom = fmaf(mu, v[j], y);
-                if (inside(u, j)) momentum[base + u * by_u + j * by_j] = mom;
-                y = nesterov ? fmaf(mu, mom, y) : mom;
+                const float mom = fmaf(mu, v[j], g[j]);
+                if (inside(u, j)) momentum[at + j * by_j] = mom;
+                g[j] = nesterov ? fmaf(mu, mom, g[j]) : mom;
             }
-            sums[j & 1] = fma((double)y, (double)y, sums[j & 1]);
+            held[row_of(j) * by_row + col_of(u, j) * by_col] = g[j];   // (zeros outside the matrix)
+            sums[j & 1] = fma((double)g[j], (double)g[j], sums[j & 1]);
         }
     }
     double sum = sums[0] + sums[1];
-    for (int i = threadIdx.x; i < kSlabBytes / 16; i += kSmallThreads)          // rows and columns behind the matrix
-        reinterpret_cast<uint4*>(slab)[i] = make_uint4(0, 0, 0, 0);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_down_sync(0xffffffffu, sum, o);
     if (lane == 0) s_sum[warp] = sum;
@@ -836,17 +833,13 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
     for (uint32_t i = 0; i < ctas; ++i) sum += s_norm[i];
     const float scale = (float)(1.0 / (sqrt(sum) + (double)eps)) * (float)(1 << kX);
 
-    // ---- X
+    // ---- X, eight neighbours of a row at a time
+    for (int i = threadIdx.x; i < units * 8 * kSmallS; i += kSmallThreads) {
+        const int r = i & (kSmallS - 1), c8 = i >> 7;
+        float v8[8];
 #pragma unroll
-    for (int u = 0; u < kSmallUnits; ++u) {
-        if (u >= units) break;
-#pragma unroll
-        for (int j = 0; j < 16; ++j) {
-            if (!inside(u, j)) continue;
-            const int r = row_of(j), a = col_of(0, j);
-            *reinterpret_cast<__half*>(slab + (u * 2 + (r >> 6)) * kUnitBytes + in_unit(r & 63, a >> 3) + (a & 7) * 2) =
-                __float2half_rn(scale * x[u * 16 + j]);
-        }
+        for (int j = 0; j < 8; ++j) v8[j] = scale * held[r * by_row + (c8 * 8 + j) * by_col];
+        *reinterpret_cast<uint4*>(slab + ((c8 >> 3) * 2 + (r >> 6)) * kUnitBytes + in_unit(r & 63, c8 & 7)) = pack8(v8);
     }
 
     // ---- products: one thread issues, then everybody takes its rows and columns of the sums
@@ -924,51 +917,66 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
                 mma_f16(tmem, x, x, f16_shape(kSmallS, kSmallS, false), k > 0);
             }
         });
-        // (a CTA without columns adds zeros)
-        float* partial = reinterpret_cast<float*>(sq[1]);             // [128][128] over two squares, words swizzled
-        {
-            uint32_t acc[32];
-            tmem_load32(lanes + side * 32, acc);
+        uint32_t acc[32];
+        tmem_load32(lanes + side * 32, acc);
+        if constexpr (kCtas == 1) {
+#pragma unroll
+            for (int o = 0; o < 4; ++o) {
+                float v8[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v8[j] = two(kA - 2 * kX) * __uint_as_float(acc[o * 8 + j]);
+                *reinterpret_cast<uint4*>(sq[0] + ((side & ~1) + (row >> 6)) * kUnitBytes +
+                                          in_unit(row & 63, (side & 1) * 4 + o)) = pack8(v8);
+            }
+        } else {
+            // (a CTA without columns adds zeros)
+            float* partial = reinterpret_cast<float*>(sq[1]);         // [128][128] over two squares, words swizzled
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const int c4 = side * 8 + j;                          // four columns; rows differ in their bank
-                const float4 v = units ? make_float4(__uint_as_float(acc[j * 4]), __uint_as_float(acc[j * 4 + 1]),
-                                                     __uint_as_float(acc[j * 4 + 2]), __uint_as_float(acc[j * 4 + 3]))
-                                       : make_float4(0, 0, 0, 0);
-                reinterpret_cast<float4*>(partial)[row * 32 + (c4 ^ (row & 7))] = v;
+                const float4 v4 = units ? make_float4(__uint_as_float(acc[j * 4]), __uint_as_float(acc[j * 4 + 1]),
+                                                      __uint_as_float(acc[j * 4 + 2]), __uint_as_float(acc[j * 4 + 3]))
+                                        : make_float4(0, 0, 0, 0);
+                reinterpret_cast<float4*>(partial)[row * 32 + (c4 ^ (row & 7))] = v4;
             }
-        }
-        fence_before_sync();
-        __syncthreads();
-        cluster_sync();
-        // rows rank, rank + ctas, ... of the sum, four columns at a time, to every CTA's A
-        for (int i = threadIdx.x; i < kSmallS / (int)ctas * 32; i += kSmallThreads) {
-            const int r = (i >> 5) * (int)ctas + (int)rank, c4 = i & 31;
-            const uint32_t from = smem_addr(partial) + (uint32_t)(r * 32 + (c4 ^ (r & 7))) * 16;
-            uint4 w[kSmallCluster];
+            fence_before_sync();
+            __syncthreads();
+            cluster_sync();
+            // rows rank, rank + ctas, ... of the sum, four columns at a time, to every CTA's A
+            constexpr int kItems = kSmallS / kCtas * 32 / kSmallThreads, kAtOnce = kItems < 2 ? kItems : 2;     // (8, 4, 2, 1)
+            for (int n = 0; n < kItems; n += kAtOnce) {
+                uint4 w[kAtOnce][kCtas];
 #pragma unroll
-            for (uint32_t q = 0; q < kSmallCluster; ++q)
-                if (q < ctas) w[q] = remote_load16(in_cta(from, q));
-            float v[4] = {};
+                for (int t = 0; t < kAtOnce; ++t) {
+                    const int i = threadIdx.x + (n + t) * kSmallThreads, r = (i >> 5) * kCtas + (int)rank;
+                    const uint32_t from = smem_addr(partial) + (uint32_t)(r * 32 + ((i & 31) ^ (r & 7))) * 16;
 #pragma unroll
-            for (uint32_t q = 0; q < kSmallCluster; ++q)
-                if (q < ctas) {
-                    v[0] += __uint_as_float(w[q].x);
-                    v[1] += __uint_as_float(w[q].y);
-                    v[2] += __uint_as_float(w[q].z);
-                    v[3] += __uint_as_float(w[q].w);
+                    for (uint32_t q = 0; q < kCtas; ++q) w[t][q] = remote_load16(in_cta(from, q));
                 }
-            const float f = two(kA - 2 * kX);
-            const __half2 h0 = __floats2half2_rn(f * v[0], f * v[1]), h1 = __floats2half2_rn(f * v[2], f * v[3]);
-            const uint32_t to = smem_addr(sq[0]) + ((c4 >> 4) * 2 + (r >> 6)) * kUnitBytes +
-                                in_unit(r & 63, (c4 >> 1) & 7) + (c4 & 1) * 8;
 #pragma unroll
-            for (uint32_t q = 0; q < kSmallCluster; ++q)
-                if (q < ctas)
-                    remote_store8(in_cta(to, q), *reinterpret_cast<const uint32_t*>(&h0), *reinterpret_cast<const uint32_t*>(&h1));
+                for (int t = 0; t < kAtOnce; ++t) {
+                    const int i = threadIdx.x + (n + t) * kSmallThreads, r = (i >> 5) * kCtas + (int)rank, c4 = i & 31;
+                    float v4[4] = {};
+#pragma unroll
+                    for (uint32_t q = 0; q < kCtas; ++q) {
+                        v4[0] += __uint_as_float(w[t][q].x);
+                        v4[1] += __uint_as_float(w[t][q].y);
+                        v4[2] += __uint_as_float(w[t][q].z);
+                        v4[3] += __uint_as_float(w[t][q].w);
+                    }
+                    const float f = two(kA - 2 * kX);
+                    const __half2 h0 = __floats2half2_rn(f * v4[0], f * v4[1]), h1 = __floats2half2_rn(f * v4[2], f * v4[3]);
+                    const uint32_t to = smem_addr(sq[0]) + ((c4 >> 4) * 2 + (r >> 6)) * kUnitBytes +
+                                        in_unit(r & 63, (c4 >> 1) & 7) + (c4 & 1) * 8;
+#pragma unroll
+                    for (uint32_t q = 0; q < kCtas; ++q)
+                        remote_store8(in_cta(to, q), *reinterpret_cast<const uint32_t*>(&h0),
+                                      *reinterpret_cast<const uint32_t*>(&h1));
+                }
+            }
+            fence_async_all();                                        // (read by the tensor cores of the other CTAs)
+            cluster_sync();
         }
-        fence_async_all();                                            // (read by the tensor cores of the other CTAs)
-        cluster_sync();
 
         // A in sq[0], B in sq[1] + sq[2]; for a second step T in sq[3], the next A in sq[0], the next B in sq[3] + sq[4] and
         // the product of both in sq[0] + sq[1]
@@ -1269,6 +1277,15 @@ static cudaError_t chain(const Table& t, const void* grad, float* momentum, floa
     return e;
 }
 
+template <typename T>
+static cudaError_t allow_small() {
+    for (const auto kernel : {small_kernel<T, 1>, small_kernel<T, 2>, small_kernel<T, 4>, small_kernel<T, 8>}) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmallSmem);
+        if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
+}
+
 // Small matrices with equally many CTAs each: a cluster as large as the longest needs.
 template <typename T>
 static cudaError_t small_launch(const SmallMats& mats, int ctas, const void* grad, float* momentum, float mu, int nesterov,
@@ -1284,7 +1301,8 @@ static cudaError_t small_launch(const SmallMats& mats, int ctas, const void* gra
     attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, small_kernel<T>, mats, (const T*)grad, momentum, mu, nesterov, steps, eps,
+    const auto kernel = ctas == 1 ? small_kernel<T, 1> : ctas == 2 ? small_kernel<T, 2> : ctas == 4 ? small_kernel<T, 4> : small_kernel<T, 8>;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, mats, (const T*)grad, momentum, mu, nesterov, steps, eps,
                                              (__nv_bfloat16*)out, timeouts);
     if (e == cudaSuccess) sidco_internal::note_launch();
     return e;
@@ -1343,9 +1361,8 @@ static int orthogonalize(const void* grad, int grad_type, float* momentum, float
     if (!pair_count[dev].load()) {           // (setting it twice from two threads is harmless)
         const auto most = cudaFuncAttributeMaxDynamicSharedMemorySize;
         int pairs = 0;
-        if ((e = cudaFuncSetAttribute(small_kernel<float>, most, kSmallSmem)) != cudaSuccess ||
-            (e = cudaFuncSetAttribute(small_kernel<__nv_bfloat16>, most, kSmallSmem)) != cudaSuccess ||
-            (e = cudaFuncSetAttribute(small_kernel<__half>, most, kSmallSmem)) != cudaSuccess ||
+        if ((e = allow_small<float>()) != cudaSuccess || (e = allow_small<__nv_bfloat16>()) != cudaSuccess ||
+            (e = allow_small<__half>()) != cudaSuccess ||
             (e = cudaFuncSetAttribute(chain_kernel, most, kChainSmem)) != cudaSuccess ||
             (e = resident_pairs(&pairs)) != cudaSuccess)
             return (int)e;
