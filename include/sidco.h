@@ -361,6 +361,13 @@ int sidco_orthogonalize(const void* grad, int grad_type, float* momentum, float 
  * device; meant for tests and logging. */
 int sidco_wait_timeouts(void);
 
+/* Switches for tests of sidco_orthogonalize; production code has no reason to call this.
+ *   wait_us     microseconds after which a wait between the phases of its products gives up (0: two seconds).
+ *   drop_phase  >= 0: this phase's results are stored but not counted, so that the CTAs waiting for them run into wait_us;
+ *               -1: off.
+ * Also sets its count in sidco_wait_timeouts back to 0 (and synchronises the device for that). */
+int sidco_set_product_test_hooks(long long wait_us, int drop_phase);
+
 /* Bytes of device scratch one residual key needs for a vector of d elements in n_segs segments. */
 size_t sidco_workspace_bytes(int64_t d, int n_segs);
 

@@ -47,7 +47,7 @@ EXPORTS = [
     "sidco_reference_workspace_bytes", "sidco_topk", "sidco_dgc", "sidco_set_policy",
     "sidco_mx4_code_bytes", "sidco_mx4_scale_bytes", "sidco_mx4_quantize", "sidco_mx4_dequantize", "sidco_mx4_matmul",
     "sidco_mx4_compress", "sidco_mx4_mean", "sidco_orthogonalize_workspace_bytes", "sidco_orthogonalize",
-    "sidco_wait_timeouts",
+    "sidco_wait_timeouts", "sidco_set_product_test_hooks",
 ]
 
 _lib = None
@@ -145,6 +145,8 @@ def lib() -> C.CDLL:
     L.sidco_orthogonalize.restype = i32
     L.sidco_wait_timeouts.argtypes = []
     L.sidco_wait_timeouts.restype = i32
+    L.sidco_set_product_test_hooks.argtypes = [C.c_longlong, i32]
+    L.sidco_set_product_test_hooks.restype = i32
     _lib = L
     return L
 
@@ -504,3 +506,10 @@ def sidco_wait_timeouts() -> int:
     if n < 0:
         raise SidcoError(-n, "sidco_wait_timeouts")
     return n
+
+
+def sidco_set_product_test_hooks(wait_us: int = 0, drop_phase: int = -1) -> None:
+    """Test switches of sidco_orthogonalize (see sidco.h); the defaults restore normal operation."""
+    rc = lib().sidco_set_product_test_hooks(wait_us, drop_phase)
+    if rc:
+        raise SidcoError(rc, "sidco_set_product_test_hooks")

@@ -155,7 +155,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2)
             bool ok = true;
             for (int i = first; i < total && ok; i += n_pairs, ++n) {
                 const uint32_t sums = tmem + (n & 1) * kSecondSums;
-                if (n) ok = mbar_wait(smem_addr(&s_shared), (n - 1) & 1, &s_failed);
+                if (n) ok = __all_sync(0xffffffffu, mbar_wait(smem_addr(&s_shared), (n - 1) & 1, &s_failed));
                 for (int k = 0; k < steps && ok; ++k, ++used) {
                     ok = mbar_wait(smem_addr(&s_full[st]), round & 1, &s_failed);
                     // the columns for the scales: free when the products of four stages ago are done
@@ -230,7 +230,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2)
                     __syncwarp();
                     if (lane == 0) mbar_arrive_cluster(shared_taken);
                 }
-                if (*(volatile int*)&s_failed) break;
+                if (__any_sync(0xffffffffu, *(volatile int*)&s_failed)) break;
                 if (boxes) {
                     constexpr int kPer = 16 / (int)sizeof(T);         // elements of 16 bytes
 #pragma unroll
@@ -289,14 +289,18 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2)
                     }
                 }
             }
-            if (*(volatile int*)&s_failed) break;
+            if (__any_sync(0xffffffffu, *(volatile int*)&s_failed)) break;
         }
         if (lane == 0) bulk_store_wait();
     }
     __syncwarp();
     fence_before_sync();
     __syncthreads();
-    if (threadIdx.x == 0 && s_failed) atomicAdd(A.timeouts, 1);
+    if (threadIdx.x == 0 && s_failed) {
+        atomicAdd(A.timeouts, 1);
+        let_work_end();
+    }
+    __syncthreads();
     cluster_sync();
     if (warp == 1) tmem_free_pair(tmem, 512);
 }
@@ -483,7 +487,10 @@ __global__ void __launch_bounds__(kSplitThreads, 2)
                     if (col + j < A.n) at[j] = narrow<T>(v[j]);
             }
         }
-    if (threadIdx.x == 0 && s_failed) atomicAdd(A.timeouts, 1);
+    if (threadIdx.x == 0 && s_failed) {
+        atomicAdd(A.timeouts, 1);
+        let_work_end();
+    }
     __syncthreads();
     cluster_sync();                                                   // nobody reads this CTA's sums any more
     if (warp == 0) tmem_free(tmem, kColumns);

@@ -21,7 +21,7 @@
 // Measured: 66 M elements in six matrices 1500 wide (LSTM-shaped, bf16 gradients) 1.38 ms: momentum 0.11 (0.93 of the copy
 // rate), normalisation 0.10, products 1.10 ms (1.26 Tflop, 0.69 of cuBLAS's bf16 rate: applications 126 us each at that rate,
 // Gram products 95 us where 70 would do if 10000 and 6000 rows divided evenly, the others 25 us each for 15 us of work);
-// VGG-16-shaped 0.28 ms, of which 0.2 in 17 dependent phases of 7 to 24 us; twenty small matrices (ResNet-20) 47 us.
+// VGG-16-shaped 0.28 ms, of which 0.2 in 17 dependent phases of 7 to 24 us; twenty small matrices (ResNet-20) 45 us.
 //
 // Workspace matrices are stored as units of 64 x 64 fp16 in the 128-byte-swizzled image that the tensor cores read, so
 // that a stage of operands is one or two contiguous bulk copies, the same unit serves as K-major operand (Gram) and as
@@ -351,6 +351,8 @@ struct Phases {
     int n;
     int sym_width, sym_tiles;         // columns of the tiles of symmetric products, their number; they come first
     int apply_width, apply_tiles;
+    int drop;                         // (tests) this phase is not counted; -1: none
+    unsigned long long wait_ns;       // limit of the waits between phases
     Phase p[kMaxPhases];
 };
 
@@ -392,13 +394,14 @@ __device__ __forceinline__ bool store_all(bool ok) {
 }
 
 // Wait (bounded) until `count` CTAs have counted themselves in.
-__device__ __forceinline__ bool wait_arrivals(const unsigned* arrived, unsigned count, volatile int* failed) {
+__device__ __forceinline__ bool wait_arrivals(const unsigned* arrived, unsigned count, unsigned long long limit_ns,
+                                              volatile int* failed) {
     const unsigned long long start = time_ns();
     for (uint32_t i = 1;; ++i) {
         unsigned v;
         asm volatile("ld.relaxed.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(arrived) : "memory");
         if (v >= count) break;
-        if ((i & 63u) == 0u && (*failed || time_ns() - start > kWaitLimitNs)) {
+        if ((i & 63u) == 0u && (*failed || time_ns() - start > limit_ns)) {
             *failed = 1;
             return false;
         }
@@ -455,7 +458,7 @@ __global__ void __launch_bounds__(kChainThreads, 1) __cluster_dims__(2)
                 for (int i = first; i < total && ok; i += n_pairs) {
                     const Tile d = list[i];
                     if (!waited) {
-                        ok = wait_arrivals(arrived + f - 1, gridDim.x, &s_failed);
+                        ok = wait_arrivals(arrived + f - 1, gridDim.x, ph.wait_ns, &s_failed);
                         waited = true;
                         if (!ok) break;
                     }
@@ -501,7 +504,7 @@ __global__ void __launch_bounds__(kChainThreads, 1) __cluster_dims__(2)
                     const int steps = p.sym && p.left < 0 ? list[i].lu : list[i].ku;
                     const int buf = n & 1;
                     const uint32_t sums = tmem + buf * 256;
-                    ok = mbar_wait(smem_addr(&s_taken[buf]), ((n >> 1) & 1) ^ 1, &s_failed);
+                    ok = __all_sync(0xffffffffu, mbar_wait(smem_addr(&s_taken[buf]), ((n >> 1) & 1) ^ 1, &s_failed));
                     for (int k = 0; k < steps && ok; ++k) {
                         ok = __all_sync(0xffffffffu, mbar_wait(smem_addr(&s_full[st]), round & 1, &s_failed));
                         if (!ok) break;
@@ -552,11 +555,11 @@ __global__ void __launch_bounds__(kChainThreads, 1) __cluster_dims__(2)
                     __syncwarp();
                     if (!plus) store_arrive(kFreeBarrier + to);
                 };
-                if (plus && !waited) wait_arrivals(arrived + f - 1, gridDim.x, &s_failed);
+                if (plus && !waited)
+                    ok = __all_sync(0xffffffffu, wait_arrivals(arrived + f - 1, gridDim.x, ph.wait_ns, &s_failed));
                 waited = true;
-                __syncwarp();
-                if (!last) prepare(0, part & 1);
-                ok = store_all(true);
+                if (!last && ok) prepare(0, part & 1);
+                ok = store_all(ok);
                 if (!ok) break;
                 if (last) continue;
                 for (int cu = 0; cu < parts; ++cu, ++part) {
@@ -575,7 +578,7 @@ __global__ void __launch_bounds__(kChainThreads, 1) __cluster_dims__(2)
                     __syncwarp();
                 }
             }
-            if (!last && elect_one()) {                               // stored: count this CTA in
+            if (!last && ok && f != ph.drop && elect_one()) {         // stored: count this CTA in
                 bulk_store_wait();
                 fence_async_all();
                 asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(arrived + f) : "memory");
@@ -711,7 +714,11 @@ __global__ void __launch_bounds__(kChainThreads, 1) __cluster_dims__(2)
     __syncwarp();
     fence_before_sync();
     __syncthreads();
-    if (threadIdx.x == 0 && s_failed) atomicAdd(timeouts, 1);
+    if (threadIdx.x == 0 && s_failed) {
+        atomicAdd(timeouts, 1);
+        let_work_end();
+    }
+    __syncthreads();
     cluster_sync();
     if (warp == 1) tmem_free_pair(tmem, 512);
 }
@@ -1045,7 +1052,11 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
     }
     fence_before_sync();
     __syncthreads();
-    if (threadIdx.x == 0 && s_failed) atomicAdd(timeouts, 1);
+    if (threadIdx.x == 0 && s_failed) {
+        atomicAdd(timeouts, 1);
+        let_work_end();
+    }
+    __syncthreads();
     cluster_sync();                                                   // nobody reads or writes this CTA's memory any more
     if (warp == 0) tmem_free(tmem, 256);
 }
@@ -1194,6 +1205,9 @@ static cudaError_t launch(void (*kernel)(Args...), dim3 grid, int threads, size_
     return e;
 }
 
+static std::atomic<unsigned long long> g_wait_ns{kWaitLimitNs};
+static std::atomic<int> g_drop_phase{-1};
+
 static cudaError_t resident_pairs(int* n) {
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(2);
@@ -1233,6 +1247,8 @@ static cudaError_t chain(const Table& t, const void* grad, float* momentum, floa
     CUtensorMap map{};
     if (!sidco_internal::byte_map(&map, ws, 128, ws_bytes / 128, 128, 128, kUnit, false)) return cudaErrorNotSupported;
     Phases ph{};
+    ph.wait_ns = g_wait_ns.load();
+    ph.drop = g_drop_phase.load();
     ph.sym_width = t.sym_width;
     ph.sym_tiles = t.sym_at[t.n];
     ph.apply_width = t.apply_width;
@@ -1333,6 +1349,14 @@ struct Beside {
 
 int sidco_internal::orthogonalize_timeouts(int* count) {
     return (int)cudaMemcpyFromSymbol(count, sidco_ortho::g_timeouts, sizeof(int));
+}
+
+int sidco_set_product_test_hooks(long long wait_us, int drop_phase) {
+    if (wait_us < 0 || wait_us > 2000000 || drop_phase < -1) return SIDCO_E_PARAMS;
+    sidco_ortho::g_wait_ns.store(wait_us ? (unsigned long long)wait_us * 1000ull : sidco_tc::kWaitLimitNs);
+    sidco_ortho::g_drop_phase.store(drop_phase);
+    const int zero = 0;
+    return (int)cudaMemcpyToSymbol(sidco_ortho::g_timeouts, &zero, sizeof(int));
 }
 
 static int orthogonalize(const void* grad, int grad_type, float* momentum, float mu, int nesterov, const int64_t* offsets,

@@ -51,8 +51,9 @@ __device__ __forceinline__ unsigned long long time_ns() {
 }
 
 // Every wait is bounded.  The first that runs out raises *failed (a word in shared memory); all later waits of the CTA
-// then return at once, its threads run through their loops without issuing work, and it ends with its tensor memory
-// freed.  A healthy wait lasts microseconds; the bound is two seconds.
+// then return at once, its threads run through their loops without issuing work, copies and products that are still in
+// flight are given time to end, and the CTA ends with its tensor memory freed.  A healthy wait lasts microseconds; the
+// bound is two seconds.
 constexpr unsigned long long kWaitLimitNs = 2000000000ull;
 
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* failed) {
@@ -67,6 +68,12 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
     }
     *failed = 1;
     return false;
+}
+
+// After a failure: one millisecond, in which whatever was issued ends (microseconds are enough).
+__device__ __forceinline__ void let_work_end() {
+    const unsigned long long start = time_ns();
+    while (time_ns() - start < 1000000ull) __nanosleep(1000);
 }
 
 // Barriers of the other CTA of a pair: an address of this CTA's shared memory in CTA `rank` of the cluster.

@@ -178,3 +178,56 @@ def test_optimizer_object_takes_the_flat_gradient():
             assert np.linalg.norm(up[o:o + r * c].reshape(r, c) - want) <= TOL * np.linalg.norm(want)
     with pytest.raises(ValueError):
         opt.step(torch.zeros(10, device="cuda"))
+
+
+def test_both_kinds_follow_and_precede_the_stream():
+    """Small matrices run beside the others on another stream; the call still starts after what the caller's stream holds
+    and its results are there for what comes next."""
+    import torch
+    from paper_2101_10761_b200 import binding as B
+    rows, cols, offsets = [64, 300, 16], [576, 200, 27], [0, 36864, 96864]
+    d = 96864 + 432
+    need = B.sidco_orthogonalize_workspace_bytes(rows, cols)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    source = torch.randn(d, device="cuda")
+    want = torch.empty(d, dtype=torch.bfloat16, device="cuda")
+    B.sidco_orthogonalize(source, None, 0, False, offsets, rows, cols, 5, want, ws, need)
+    torch.cuda.synchronize()
+    big = torch.randn(4096, 4096, device="cuda")
+    for s in (torch.cuda.Stream(), torch.cuda.Stream()):
+        with torch.cuda.stream(s):
+            grad = torch.full((d,), float("nan"), device="cuda")
+            out = torch.full((d,), 7.0, dtype=torch.bfloat16, device="cuda")
+            for _ in range(8):
+                big = big @ big * 1e-4                        # keeps the stream busy for a while
+            grad.copy_(source)
+            B.sidco_orthogonalize(grad, None, 0, False, offsets, rows, cols, 5, out, ws, need)
+            got = out.clone()
+            grad.fill_(float("nan"))
+        s.synchronize()
+        assert torch.equal(got, want)
+
+
+def test_a_wait_that_runs_out_ends_the_kernel_and_is_counted():
+    """One phase is withheld (its results are stored but not counted): the kernel gives up after the shortened limit, says
+    so, and the next call is right again."""
+    import torch
+    from paper_2101_10761_b200 import binding as B
+    rows, cols = [300], [200]
+    need = B.sidco_orthogonalize_workspace_bytes(rows, cols)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    grad = torch.randn(60000, device="cuda")
+    outs = [torch.zeros(60000, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    B.sidco_orthogonalize(grad, None, 0, False, [0], rows, cols, 5, outs[0], ws, need)
+    assert B.sidco_wait_timeouts() == 0
+    try:
+        for drop in (0, 1, 5, 6):                             # a Gram product, a polynomial, a product, an application
+            B.sidco_set_product_test_hooks(5000, drop)
+            B.sidco_orthogonalize(grad, None, 0, False, [0], rows, cols, 5, outs[1], ws, need)
+            torch.cuda.synchronize()
+            assert B.sidco_wait_timeouts() > 0
+    finally:
+        B.sidco_set_product_test_hooks()
+    B.sidco_orthogonalize(grad, None, 0, False, [0], rows, cols, 5, outs[1], ws, need)
+    torch.cuda.synchronize()
+    assert B.sidco_wait_timeouts() == 0 and torch.equal(outs[0], outs[1])

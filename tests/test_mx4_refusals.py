@@ -126,6 +126,13 @@ def test_orthogonalize_refuses(B):
         B.sidco_orthogonalize_workspace_bytes([200] * 256, [150] * 256) > 0
 
 
+def test_hooks_refuse(B):
+    for bad in ((-1, -1), (3000000, -1), (0, -2)):
+        with pytest.raises(B.SidcoError) as e:
+            B.sidco_set_product_test_hooks(*bad)
+        assert e.value.code == -6
+
+
 def test_error_texts_name_the_reason(B):
     assert "type" in B.sidco_error_string(-13) and "aligned" in B.sidco_error_string(-14)
 
