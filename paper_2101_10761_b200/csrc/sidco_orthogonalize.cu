@@ -21,7 +21,7 @@
 // Measured: 66 M elements in six matrices 1500 wide (LSTM-shaped, bf16 gradients) 1.38 ms: momentum 0.11 (0.93 of the copy
 // rate), normalisation 0.10, products 1.10 ms (1.26 Tflop, 0.69 of cuBLAS's bf16 rate: applications 126 us each at that rate,
 // Gram products 95 us where 70 would do if 10000 and 6000 rows divided evenly, the others 25 us each for 15 us of work);
-// VGG-16-shaped 0.28 ms, of which 0.2 in 17 dependent phases of 7 to 24 us; twenty small matrices (ResNet-20) 45 us.
+// VGG-16-shaped 0.28 ms, of which 0.2 in 17 dependent phases of 7 to 24 us; twenty small matrices (ResNet-20) 41 us.
 //
 // Workspace matrices are stored as units of 64 x 64 fp16 in the 128-byte-swizzled image that the tensor cores read, so
 // that a stage of operands is one or two contiguous bulk copies, the same unit serves as K-major operand (Gram) and as
@@ -34,7 +34,6 @@
 
 #include <algorithm>
 #include <atomic>
-#include <initializer_list>
 #include <mutex>
 #include <utility>
 #include <vector>
@@ -728,13 +727,15 @@ __global__ void __launch_bounds__(kChainThreads, 1) __cluster_dims__(2)
 // Matrices with s <= 128 and l <= 2048: one cluster of CTAs per matrix does the whole update in one launch.  Every CTA
 // keeps its columns of X (up to 256: 64 KB) in shared memory from the first step to the last.  The only exchange between the CTAs is a sum per Gram matrix: each adds its share of the rows of all partial
 // Gram matrices through distributed shared memory, in the order of the CTAs, and hands the result to the others; the
-// s x s products that follow (a few hundred nanoseconds each) every CTA does for itself.  The B and their product are kept
-// as sums of two fp16 parts: with few rows their rounding is the largest error (2.0e-3 instead of 2.9e-3 for 32 x 288), and
-// the products of the second parts cost next to nothing here.
+// s x s products that follow (0.8 us each) every CTA does for itself.
+// With few rows the rounding of the s x s matrices is the largest error, and products of second fp16 parts cost next to
+// nothing here.  With s <= 64 all of them are sums of two parts: two of 16 x 139 are off by 1.7e-3 of their norm, the rounding
+// to bf16, instead of 2.8e-3 with two parts of the B and their product only, and ResNet-20 takes 41 us instead of 45, because
+// the exchange moves 64 x 64.  Above, where a square is twice that, A and T have one part (100 x 333: 1.9e-3).
 
 constexpr int kSmallS = 128, kSmallUnits = 4, kSmallCluster = 8;      // units of columns per CTA, CTAs per matrix: at most
 constexpr int kSmallThreads = 512;
-constexpr int kSquareBytes = 4 * kUnitBytes;                          // 128 x 128
+constexpr int kSquareBytes = 4 * kUnitBytes;                          // 128 x 128 (with s <= 64: 128 x 64, half of it)
 constexpr int kSlabBytes = kSmallUnits * 2 * kUnitBytes;              // 128 x 256
 constexpr int kOutLine = kSmallUnits * kUnit + 2, kOutColumn = kSmallS + 2;   // bf16 per line of the result, wide or tall
 constexpr int kSquares = 5;                                           // (together larger than X's part in fp32)
@@ -779,8 +780,15 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
     const int first = (int)(lu * rank / ctas), units = (int)(lu * (rank + 1) / ctas) - first;   // of this CTA's columns
 
     uint8_t* smem = (uint8_t*)(((uintptr_t)s_raw + 1023) & ~(uintptr_t)1023);
-    uint8_t *sq[kSquares], *slab = smem + kSquares * kSquareBytes;
-    for (int i = 0; i < kSquares; ++i) sq[i] = smem + i * kSquareBytes;
+    uint8_t* slab = smem + kSquares * kSquareBytes;
+    // the squares: six small ones or five large ones; A and T have a second part if they are small (rows from 64 on of the
+    // small ones are whatever was there: they take part in sums of their own rows only, and nobody reads those)
+    const auto sq = [&](int i) { return smem + i * ku * (kSquareBytes / 2); };
+    struct Square { uint8_t *hi, *lo; };
+    const bool fine = ku == 1;
+    const Square sq_a = {sq(0), fine ? sq(1) : nullptr}, sq_b = fine ? Square{sq(2), sq(3)} : Square{sq(1), sq(2)},
+                 sq_t = {fine ? sq(4) : sq(3), fine ? sq(5) : nullptr}, sq_b2 = fine ? Square{sq(4), sq(5)} : Square{sq(3), sq(4)},
+                 sq_p = {sq(0), sq(1)};
     if (warp == 0) tmem_alloc(&s_tmem, 256);
     if (threadIdx.x == 0) {
         mbar_init(smem_addr(&s_done), 1);
@@ -870,20 +878,32 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
         ++uses;
         fence_after_sync();
     };
-    // to + to_lo = alpha (left right + left_2 right_2 + left_3 right_3) + beta plus + gamma I, all 128 x 128
-    struct Term { const uint8_t *left, *right; };
-    const auto square = [&](std::initializer_list<Term> terms, const uint8_t* plus, uint8_t* to, uint8_t* to_lo, float alpha,
-                            float beta, float gamma) {
+    // eight neighbours of a row of a square: as one fp16 part or two
+    const auto put = [&](const Square& to, int o, float (&v)[8]) {
+        const int at = ((side & ~1) + (row >> 6)) * kUnitBytes + in_unit(row & 63, (side & 1) * 4 + o);
+        *reinterpret_cast<uint4*>(to.hi + at) = pack8(v);
+        if (to.lo) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] -= __half2float(__float2half_rn(v[j]));
+            *reinterpret_cast<uint4*>(to.lo + at) = pack8(v);
+        }
+    };
+    // to = alpha left right + beta plus + gamma I (the product of two second parts is left out)
+    const auto square = [&](const Square& left, const Square& right, const Square* plus, const Square& to, float alpha, float beta,
+                            float gamma) {
         issue_and_wait([&] {
             bool add = false;
-            for (const Term& t : terms) {
-                const uint32_t a = smem_addr(t.left), b = smem_addr(t.right);
+            for (int t = 0; t < 3; ++t) {
+                const uint8_t *l = t == 2 ? left.lo : left.hi, *r = t == 1 ? right.lo : right.hi;
+                if (!l || !r) continue;
+                const uint32_t a = smem_addr(l), b = smem_addr(r);
                 for (int k = 0; k < ku * 4; ++k, add = true)
                     mma_f16(tmem, swizzled_operand(a + (k >> 2) * 2 * kUnitBytes + (k & 3) * 32, 16, 1024),
                             swizzled_operand(b + (k >> 2) * 2 * kUnitBytes + (k & 3) * 32, 16, 1024),
-                            f16_shape(kSmallS, kSmallS, false), add);
+                            f16_shape(kSmallS, ku * kUnit, false), add);
             }
         });
+        if (side >= 2 * ku) return;
         uint32_t acc[32];
         tmem_load32(lanes + side * 32, acc);
 #pragma unroll
@@ -892,8 +912,10 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
             float v[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] = alpha * __uint_as_float(acc[o * 8 + j]);
-            if (plus) {
-                const uint4 w = *reinterpret_cast<const uint4*>(plus + at);
+            for (int t = 0; t < 2 && plus; ++t) {
+                const uint8_t* from = t ? plus->lo : plus->hi;
+                if (!from) break;
+                const uint4 w = *reinterpret_cast<const uint4*>(from + at);
                 const __half2* h = reinterpret_cast<const __half2*>(&w);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
@@ -904,12 +926,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
             }
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] += row == side * 32 + o * 8 + j ? gamma : 0.0f;
-            *reinterpret_cast<uint4*>(to + at) = pack8(v);
-            if (to_lo) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] -= __half2float(__float2half_rn(v[j]));
-                *reinterpret_cast<uint4*>(to_lo + at) = pack8(v);
-            }
+            put(to, o, v);
         }
     };
     const auto two = [](int k) { return __uint_as_float((uint32_t)(127 + k) << 23); };
@@ -921,48 +938,58 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
             const uint32_t a = smem_addr(slab);
             for (int k = 0; k < units * 4; ++k) {
                 const uint64_t x = swizzled_operand(a + (k >> 2) * 2 * kUnitBytes + (k & 3) * 32, 16, 1024);
-                mma_f16(tmem, x, x, f16_shape(kSmallS, kSmallS, false), k > 0);
+                mma_f16(tmem, x, x, f16_shape(kSmallS, ku * kUnit, false), k > 0);
             }
         });
-        uint32_t acc[32];
-        tmem_load32(lanes + side * 32, acc);
+        const float gram_scale = two(kA - 2 * kX);
         if constexpr (kCtas == 1) {
+            if (side < 2 * ku) {
+                uint32_t acc[32];
+                tmem_load32(lanes + side * 32, acc);
 #pragma unroll
-            for (int o = 0; o < 4; ++o) {
-                float v8[8];
+                for (int o = 0; o < 4; ++o) {
+                    float v8[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v8[j] = two(kA - 2 * kX) * __uint_as_float(acc[o * 8 + j]);
-                *reinterpret_cast<uint4*>(sq[0] + ((side & ~1) + (row >> 6)) * kUnitBytes +
-                                          in_unit(row & 63, (side & 1) * 4 + o)) = pack8(v8);
+                    for (int j = 0; j < 8; ++j) v8[j] = gram_scale * __uint_as_float(acc[o * 8 + j]);
+                    put(sq_a, o, v8);
+                }
             }
         } else {
-            // (a CTA without columns adds zeros)
-            float* partial = reinterpret_cast<float*>(sq[1]);         // [128][128] over two squares, words swizzled
+            // [64 ku][64 ku] where B will be, words swizzled; a CTA without columns adds zeros
+            float* partial = reinterpret_cast<float*>(sq_b.hi);
+            const int fours = 16 * ku, shift = 3 + ku;                // (16 or 32 times four columns)
+            if (side < 2 * ku && row < kUnit * ku) {
+                uint32_t acc[32];
+                tmem_load32(lanes + side * 32, acc);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int c4 = side * 8 + j;                          // four columns; rows differ in their bank
-                const float4 v4 = units ? make_float4(__uint_as_float(acc[j * 4]), __uint_as_float(acc[j * 4 + 1]),
-                                                      __uint_as_float(acc[j * 4 + 2]), __uint_as_float(acc[j * 4 + 3]))
-                                        : make_float4(0, 0, 0, 0);
-                reinterpret_cast<float4*>(partial)[row * 32 + (c4 ^ (row & 7))] = v4;
+                for (int j = 0; j < 8; ++j) {
+                    const int c4 = side * 8 + j;                      // rows differ in their bank
+                    const float4 v4 = units ? make_float4(__uint_as_float(acc[j * 4]), __uint_as_float(acc[j * 4 + 1]),
+                                                          __uint_as_float(acc[j * 4 + 2]), __uint_as_float(acc[j * 4 + 3]))
+                                            : make_float4(0, 0, 0, 0);
+                    reinterpret_cast<float4*>(partial)[row * fours + (c4 ^ (row & 7))] = v4;
+                }
             }
             fence_before_sync();
             __syncthreads();
             cluster_sync();
             // rows rank, rank + ctas, ... of the sum, four columns at a time, to every CTA's A
-            constexpr int kItems = kSmallS / kCtas * 32 / kSmallThreads, kAtOnce = kItems < 2 ? kItems : 2;     // (8, 4, 2, 1)
-            for (int n = 0; n < kItems; n += kAtOnce) {
+            constexpr int kAtOnce = kCtas == 8 ? 1 : 2;               // (128 rows: 8, 4, 2 per thread)
+            const int items = kUnit * ku / kCtas * fours;
+            for (int i0 = threadIdx.x; i0 < items; i0 += kAtOnce * kSmallThreads) {
                 uint4 w[kAtOnce][kCtas];
 #pragma unroll
                 for (int t = 0; t < kAtOnce; ++t) {
-                    const int i = threadIdx.x + (n + t) * kSmallThreads, r = (i >> 5) * kCtas + (int)rank;
-                    const uint32_t from = smem_addr(partial) + (uint32_t)(r * 32 + ((i & 31) ^ (r & 7))) * 16;
+                    const int i = i0 + t * kSmallThreads, r = (i >> shift) * kCtas + (int)rank;
+                    const uint32_t from = smem_addr(partial) + (uint32_t)(r * fours + ((i & (fours - 1)) ^ (r & 7))) * 16;
 #pragma unroll
-                    for (uint32_t q = 0; q < kCtas; ++q) w[t][q] = remote_load16(in_cta(from, q));
+                    for (uint32_t q = 0; q < kCtas; ++q)
+                        if (i < items) w[t][q] = remote_load16(in_cta(from, q));
                 }
 #pragma unroll
                 for (int t = 0; t < kAtOnce; ++t) {
-                    const int i = threadIdx.x + (n + t) * kSmallThreads, r = (i >> 5) * kCtas + (int)rank, c4 = i & 31;
+                    const int i = i0 + t * kSmallThreads, r = (i >> shift) * kCtas + (int)rank, c4 = i & (fours - 1);
+                    if (i >= items) break;
                     float v4[4] = {};
 #pragma unroll
                     for (uint32_t q = 0; q < kCtas; ++q) {
@@ -971,33 +998,39 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
                         v4[2] += __uint_as_float(w[t][q].z);
                         v4[3] += __uint_as_float(w[t][q].w);
                     }
-                    const float f = two(kA - 2 * kX);
-                    const __half2 h0 = __floats2half2_rn(f * v4[0], f * v4[1]), h1 = __floats2half2_rn(f * v4[2], f * v4[3]);
-                    const uint32_t to = smem_addr(sq[0]) + ((c4 >> 4) * 2 + (r >> 6)) * kUnitBytes +
-                                        in_unit(r & 63, (c4 >> 1) & 7) + (c4 & 1) * 8;
+                    const uint32_t at = ((c4 >> 4) * 2 + (r >> 6)) * kUnitBytes + in_unit(r & 63, (c4 >> 1) & 7) + (c4 & 1) * 8;
 #pragma unroll
-                    for (uint32_t q = 0; q < kCtas; ++q)
-                        remote_store8(in_cta(to, q), *reinterpret_cast<const uint32_t*>(&h0),
-                                      *reinterpret_cast<const uint32_t*>(&h1));
+                    for (int j = 0; j < 4; ++j) v4[j] *= gram_scale;
+                    const auto send = [&](const uint8_t* to) {
+                        const __half2 h0 = __floats2half2_rn(v4[0], v4[1]), h1 = __floats2half2_rn(v4[2], v4[3]);
+#pragma unroll
+                        for (uint32_t q = 0; q < kCtas; ++q)
+                            remote_store8(in_cta(smem_addr(to) + at, q), *reinterpret_cast<const uint32_t*>(&h0),
+                                          *reinterpret_cast<const uint32_t*>(&h1));
+                    };
+                    send(sq_a.hi);
+                    if (sq_a.lo) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) v4[j] -= __half2float(__float2half_rn(v4[j]));
+                        send(sq_a.lo);
+                    }
                 }
             }
             fence_async_all();                                        // (read by the tensor cores of the other CTAs)
             cluster_sync();
         }
 
-        // A in sq[0], B in sq[1] + sq[2]; for a second step T in sq[3], the next A in sq[0], the next B in sq[3] + sq[4] and
-        // the product of both in sq[0] + sq[1]
-        const uint8_t *p = sq[1], *p_lo = sq[2];
+        // B; for a second step T = B A, the next A = T B, its B where T was, and the product of both where A was
+        Square p = sq_b;
         int scale_p = kB;
         const float poly = kCc * two(kB - 2 * kA), linear = kCb * two(kB - kA), unit = kCa * two(kB);
-        square({{sq[0], sq[0]}}, sq[0], sq[1], sq[2], poly, linear, unit);
+        square(sq_a, sq_a, &sq_a, sq_b, poly, linear, unit);
         if (group == 2) {
-            square({{sq[1], sq[0]}, {sq[2], sq[0]}}, nullptr, sq[3], nullptr, two(-kB), 0.0f, 0.0f);
-            square({{sq[3], sq[1]}, {sq[3], sq[2]}}, nullptr, sq[0], nullptr, two(-kB), 0.0f, 0.0f);
-            square({{sq[0], sq[0]}}, sq[0], sq[3], sq[4], poly, linear, unit);
-            square({{sq[3], sq[1]}, {sq[3], sq[2]}, {sq[4], sq[1]}}, nullptr, sq[0], sq[1], two(kP - 2 * kB), 0.0f, 0.0f);
-            p = sq[0];
-            p_lo = sq[1];
+            square(sq_b, sq_a, nullptr, sq_t, two(-kB), 0.0f, 0.0f);
+            square(sq_t, sq_b, nullptr, sq_a, two(-kB), 0.0f, 0.0f);
+            square(sq_a, sq_a, &sq_a, sq_b2, poly, linear, unit);
+            square(sq_b2, sq_b, nullptr, sq_p, two(kP - 2 * kB), 0.0f, 0.0f);
+            p = sq_p;
             scale_p = kP;
         }
 
@@ -1006,7 +1039,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
             const uint32_t b = smem_addr(slab);
             for (int k = 0; k < ku * 8 && units; ++k) {
                 const int q = k < ku * 4 ? k : k - ku * 4;
-                const uint32_t a = smem_addr(k < ku * 4 ? p : p_lo);
+                const uint32_t a = smem_addr(k < ku * 4 ? p.hi : p.lo);
                 mma_f16(tmem, swizzled_operand(a + (q >> 2) * 2 * kUnitBytes + (q & 3) * 32, 16, 1024),
                         swizzled_operand(b + (q >> 2) * kUnitBytes + (q & 3) * 2048, 2 * kUnitBytes, 1024),
                         f16_shape(kSmallS, units * kUnit, true), k > 0);
