@@ -18,10 +18,11 @@
 // values are scaled up by a^5 (1e-3 to 2e-3 of the result's norm for the entries above, 3e-3 for singular values over two
 // decades, 5e-3 over three).  A second fp16 part of X brings that to 2e-3 and 4e-3, for a twelfth of the time: not kept.
 //
-// Measured: 66 M elements in six matrices 1500 wide (LSTM-shaped, bf16 gradients) 1.38 ms: momentum 0.11 (0.93 of the copy
-// rate), normalisation 0.10, products 1.10 ms (1.26 Tflop, 0.69 of cuBLAS's bf16 rate: applications 126 us each at that rate,
-// Gram products 95 us where 70 would do if 10000 and 6000 rows divided evenly, the others 25 us each for 15 us of work);
-// VGG-16-shaped 0.28 ms, of which 0.2 in 17 dependent phases of 7 to 24 us; twenty small matrices (ResNet-20) 41 us.
+// Measured: 66 M elements in six matrices 1500 wide (LSTM-shaped, bf16 gradients) 1.25 ms, 1.35 once the power limit has set
+// in: momentum and first X 0.13 (0.92 of the copy rate), products 1.02 ms (1.26 Tflop, 0.74 of cuBLAS's bf16 rate:
+// applications 126 us each at that rate, Gram products 95 us where 70 would do if 10000 and 6000 rows divided evenly, the
+// others 25 us each for 15 us of work); VGG-16-shaped 0.29 ms, of which 0.21 in 17 dependent phases of 7 to 24 us; twenty
+// small matrices (ResNet-20) 41 us.
 //
 // Workspace matrices are stored as units of 64 x 64 fp16 in the 128-byte-swizzled image that the tensor cores read, so
 // that a stage of operands is one or two contiguous bulk copies, the same unit serves as K-major operand (Gram) and as
@@ -58,8 +59,11 @@ constexpr int kUnit = 64;             // units of 64 x 64
 constexpr int kUnitBytes = kUnit * kUnit * 2;
 constexpr int kRows = 256;           // products of larger matrices: tiles of 256 rows x 256 or 128 columns
 constexpr int kMostPairs = 74;        // pairs of SMs of the device
-constexpr int kMaxMats = 128;         // matrices of one chain of launches
-constexpr int kChunk = 16384;         // elements of a matrix per CTA of the momentum pass
+constexpr int kMaxMats = 128;         // matrices of one chain of launches (at most 256)
+constexpr int kMostUnits = 8;         // units of a matrix per CTA of the momentum pass: at most
+constexpr int kMomentumCtas = 4;      // its CTAs per SM
+constexpr int kMaxPhases = (SIDCO_ORTHO_MAX_STEPS + 1) / 2 * 7;   // products of a chain
+constexpr int kSamples = 2048;        // elements of a matrix from which its norm is estimated
 
 enum Buffer { kBufA, kBufA2, kBufB, kBufT, kBufP, kSmallBuffers };
 
@@ -69,13 +73,13 @@ struct Mat {
     int64_t small;                    // first of the s x s matrices
     int rows, cols, s, l;
     int sp, lp;                       // s to a multiple of 256, l to a multiple of 64
-    int partial0, n_chunks;           // partial sums of squares
+    int n_chunks;                     // CTAs of the momentum pass
 };
 
 struct Table {
     int n;
-    int chunk_at[kMaxMats + 1];       // first CTA of every matrix: momentum pass,
-    int unit_at[kMaxMats + 1];        // normalisation,
+    int chunk;                        // units per CTA of the momentum pass
+    int chunk_at[kMaxMats + 1];       // first CTA of every matrix
     int sym_at[kMaxMats + 1];         // first tile of every matrix: symmetric products,
     int apply_at[kMaxMats + 1];       // applications
     int sym_width, apply_width;       // columns of their tiles
@@ -88,7 +92,7 @@ struct __align__(16) Tile {
     int x[2], small;
     int spu, ku;                      // units along the padded s, along s
     int lu;                           // units along l
-    int pad;
+    int mat;                          // which matrix
     uint16_t ti, tj;                  // row, column
     int rows, cols;                   // of the caller's matrix, which lies
     int64_t offset;                   // here in the flat vectors
@@ -108,110 +112,6 @@ __device__ __forceinline__ float widen(__nv_bfloat16 x) { return __bfloat162floa
 __device__ __forceinline__ float widen(__half x) { return __half2float(x); }
 
 // ---------------------------------------------------------------------------------------------- momentum, norm
-
-// Eight neighbours: fp32 32 bytes, 16-bit types 16.
-template <typename T>
-__device__ __forceinline__ void load8(const T* p, float (&x)[8]) {
-    uint32_t w[2 * sizeof(T)];
-    if constexpr (sizeof(T) == 4) {
-        asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-                     : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
-                     : "l"(p));
-    } else {
-        *reinterpret_cast<uint4*>(w) = *reinterpret_cast<const uint4*>(p);
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = widen(reinterpret_cast<const T*>(w)[i]);
-}
-
-__device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
-    asm volatile("st.global.v8.f32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]),
-                 "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7])
-                 : "memory");
-}
-
-// M <- mu M + G and the sum of squares of U per chunk of 16384 elements (fp64: gradients may be tiny or huge).  Chunks
-// start at multiples of eight elements of the flat vector; eights that lie inside the matrix move in one access where
-// the vectors' bases allow it (`vec`).  The last chunk of a matrix to arrive adds the chunks' sums in their order.
-template <typename T>
-__global__ void __launch_bounds__(256, 4) momentum_kernel(const __grid_constant__ Table t, const T* __restrict__ grad,
-                                                       float* __restrict__ momentum, float mu, int nesterov, float eps,
-                                                       int vec, double* __restrict__ partial, int* __restrict__ arrived,
-                                                       float* __restrict__ inv_norm) {
-    __shared__ double s_sum[8];
-    __shared__ int s_last;
-    launch_dependents();
-    const int i = find(t.chunk_at, t.n, blockIdx.x), chunk = blockIdx.x - t.chunk_at[i];
-    const Mat& m = t.m[i];
-    const int64_t lo = m.offset, hi = lo + (int64_t)m.rows * m.cols, from = (lo & ~(int64_t)7) + (int64_t)chunk * kChunk;
-    double sums[4] = {};
-    constexpr int U = 2;
-#pragma unroll 1
-    for (int o0 = threadIdx.x; o0 < kChunk / 8; o0 += 256 * U) {
-        float g[U][8], v[U][8] = {};
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int64_t e = from + (o0 + u * 256) * 8;
-            if (vec && e >= lo && e + 8 <= hi) {
-                load8(grad + e, g[u]);
-                if (momentum) load8(momentum + e, v[u]);
-            } else {
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const bool in = e + k >= lo && e + k < hi;
-                    g[u][k] = in ? widen(grad[e + k]) : 0.0f;
-                    v[u][k] = in && momentum ? momentum[e + k] : 0.0f;
-                }
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int64_t e = from + (o0 + u * 256) * 8;
-            if (momentum) {
-#pragma unroll
-                for (int k = 0; k < 8; ++k) v[u][k] = fmaf(mu, v[u][k], g[u][k]);
-                if (vec && e >= lo && e + 8 <= hi) {
-                    store8(momentum + e, v[u]);
-                } else {
-#pragma unroll
-                    for (int k = 0; k < 8; ++k)
-                        if (e + k >= lo && e + k < hi) momentum[e + k] = v[u][k];
-                }
-#pragma unroll
-                for (int k = 0; k < 8; ++k) g[u][k] = nesterov ? fmaf(mu, v[u][k], g[u][k]) : v[u][k];
-            }
-#pragma unroll
-            for (int k = 0; k < 8; ++k) sums[k & 3] = fma((double)g[u][k], (double)g[u][k], sums[k & 3]);
-        }
-    }
-    double sum = (sums[0] + sums[1]) + (sums[2] + sums[3]);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum += __shfl_down_sync(0xffffffffu, sum, o);
-    if ((threadIdx.x & 31) == 0) s_sum[threadIdx.x >> 5] = sum;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        sum = 0.0;
-        for (int w = 0; w < 8; ++w) sum += s_sum[w];
-        partial[m.partial0 + chunk] = sum;
-        __threadfence();
-        s_last = atomicAdd(arrived + i, 1) == m.n_chunks - 1;
-        __threadfence();
-    }
-    __syncthreads();
-    if (!s_last) return;
-    sum = 0.0;
-    for (int c = threadIdx.x; c < m.n_chunks; c += 256) sum += __ldcg(partial + m.partial0 + c);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum += __shfl_down_sync(0xffffffffu, sum, o);
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) s_sum[threadIdx.x >> 5] = sum;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        sum = 0.0;
-        for (int w = 0; w < 8; ++w) sum += s_sum[w];
-        inv_norm[i] = (float)(1.0 / (sqrt(sum) + (double)eps));
-    }
-}
 
 // Tile `i` of those that cover the lower triangle, row by row: row r has (r + 1) * per tiles (per = 256 / width).
 __device__ __forceinline__ void triangle(int i, int per, uint16_t* row, uint16_t* col) {
@@ -246,23 +146,61 @@ __device__ __forceinline__ void load4(const T* p, float (&x)[4]) {
     for (int i = 0; i < 4; ++i) x[i] = widen(reinterpret_cast<const T*>(w)[i]);
 }
 
-// One CTA per unit: U again (from what the momentum pass left), scaled, transposed if tall, as fp16.  The
-// units are taken from the last to the first: what the momentum pass touched last is still in L2.
+// What the passes know of every matrix.
+struct Norms {
+    int* exponent;                    // X is first stored as U * 2^exponent
+    float* factor;                    // and that times `factor` is X * 2^kX
+    float* inverse;                   // 1 / (|U|_F + eps)
+    int* again;                       // the estimate was too far off: X has to be written again
+    int* arrived;                     // CTAs of the momentum pass that are done
+};
+
+// The scale of X without its norm.  X as U * 2^q in fp16 has the accuracy of X * 2^kX for any q with which the norm stays
+// below 2^15 (no entry overflows) and the root mean square of the entries above 2^-13 (what falls below fp16's normal
+// numbers is rounded to 2^-25, and so by less than 2^-12 of that).  Between the two there is a factor of 2^28 / sqrt(r c),
+// 2^16 for 16 M entries, so the norm of 2048 entries tells q well enough.  Only entries that hide from the samples mislead
+// it; the momentum pass, which adds all of them up, sees that and has X written again.  The rest of the factor joins the
+// first Gram product (squared) and the first application.
+// Also: counters to zero, the list of tiles.
 template <typename T>
-__global__ void __launch_bounds__(256) normalize_kernel(const __grid_constant__ Table t, const T* __restrict__ grad,
-                                                        const float* __restrict__ momentum, float mu, int nesterov,
-                                                        int quads, const float* __restrict__ inv_norm,
-                                                        uint8_t* __restrict__ ws) {
-    __shared__ float s_u[kUnit][kUnit + 1];
+__global__ void __launch_bounds__(256) prepare_kernel(const __grid_constant__ Table t, const T* __restrict__ grad,
+                                                      const float* __restrict__ momentum, float mu, int nesterov, Norms norms,
+                                                      unsigned* __restrict__ phases, uint8_t* __restrict__ ws) {
+    __shared__ double s_sum[8];
     launch_dependents();
-    const int block = gridDim.x - 1 - blockIdx.x, i = find(t.unit_at, t.n, block), u = block - t.unit_at[i];
-    const Mat& m = t.m[i];
-    const int rb = u % (m.sp / kUnit), cb = u / (m.sp / kUnit);
-    const bool tall = m.rows > m.cols;
-    wait_prerequisites();
-    // (the tiles of the kernels behind this one)
+    if ((int)blockIdx.x < t.n) {
+        const Mat& m = t.m[blockIdx.x];
+        const uint64_t size = (uint64_t)m.rows * m.cols;
+        float g[kSamples / 256], v[kSamples / 256] = {};
+#pragma unroll
+        for (int k = 0; k < kSamples / 256; ++k) {                    // multiples of the golden section are spread evenly
+            const uint64_t e = __umul64hi((threadIdx.x + k * 256 + 1) * 0x9e3779b97f4a7c15ull, size);
+            g[k] = widen(grad[m.offset + e]);
+            if (momentum) v[k] = momentum[m.offset + e];
+        }
+        double sum = 0.0;
+#pragma unroll
+        for (int k = 0; k < kSamples / 256; ++k) {
+            const float mom = fmaf(mu, v[k], g[k]), u = nesterov && momentum ? fmaf(mu, mom, g[k]) : mom;
+            sum = fma((double)u, (double)u, sum);
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_down_sync(0xffffffffu, sum, o);
+        if ((threadIdx.x & 31) == 0) s_sum[threadIdx.x >> 5] = sum;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            sum = 0.0;
+            for (int w = 0; w < 8; ++w) sum += s_sum[w];
+            // |U| 2^q in the middle between sqrt(r c) 2^-13 and 2^15
+            const double bits = 0.25 * log2((double)size) + 1.0 - 0.5 * log2(sum * ((double)size / kSamples));
+            norms.exponent[blockIdx.x] = bits > -126.0 && bits < 126.0 ? (int)rint(bits) : 0;
+            norms.arrived[blockIdx.x] = 0;
+        }
+    }
+    const int first = blockIdx.x * 256 + threadIdx.x, all = gridDim.x * 256;
+    for (int w = first; w < kMaxPhases; w += all) phases[w] = 0;
     const int n_sym = t.sym_at[t.n], n_apply = t.apply_at[t.n];
-    for (int w = blockIdx.x * 256 + threadIdx.x; w < n_sym + n_apply; w += gridDim.x * 256) {
+    for (int w = first; w < n_sym + n_apply; w += all) {
         const bool sym = w < n_sym;
         const int k = sym ? w : w - n_sym;
         const int* at = sym ? t.sym_at : t.apply_at;
@@ -275,6 +213,7 @@ __global__ void __launch_bounds__(256) normalize_kernel(const __grid_constant__ 
         d.spu = q.sp / kUnit;
         d.ku = (q.s + kUnit - 1) / kUnit;
         d.lu = q.lp / kUnit;
+        d.mat = j;
         d.rows = q.rows;
         d.cols = q.cols;
         d.offset = q.offset;
@@ -287,48 +226,214 @@ __global__ void __launch_bounds__(256) normalize_kernel(const __grid_constant__ 
         }
         reinterpret_cast<Tile*>(ws + t.tiles)[w] = d;
     }
-    const float inv = __ldcg(inv_norm + i);
-    // four neighbours along the matrix's own rows (X's columns, or X's rows if tall) per thread and step
-    const int along = (threadIdx.x & 15) * 4, across0 = threadIdx.x >> 4;
-    const int my_r = (tall ? rb : cb) * kUnit + along;
-    const bool fours = quads && ((m.offset | m.cols) & 3) == 0;
-    float x[4][4];
+}
+
+// A unit of X and the elements of the caller's matrix under it: four neighbours of a row (X's columns, or X's rows if the
+// matrix is tall) per thread and step.
+struct UnitOf {
+    bool tall, fours;
+    int r, a;                         // column, first row (of four, 16 apart) in the caller's matrix
+    int64_t e, by;                    // the first element, the way to the next
+    int64_t image;                    // where the unit lies, bytes from the start of the workspace
+
+    __device__ __forceinline__ UnitOf(const Mat& m, int u, int quads) {
+        const int rbs = m.sp / kUnit, cbs = m.lp / kUnit;
+        tall = m.rows > m.cols;
+        fours = quads && ((m.offset | m.cols) & 3) == 0;
+        // (units next to each other are neighbours in the caller's rows)
+        const int rb = tall ? u % rbs : u / cbs, cb = tall ? u / rbs : u % cbs;
+        r = (tall ? rb : cb) * kUnit + (threadIdx.x & 15) * 4;
+        a = (tall ? cb : rb) * kUnit + (threadIdx.x >> 4);
+        e = m.offset + (int64_t)a * m.cols + r;
+        by = 16 * (int64_t)m.cols;
+        image = m.x[0] + ((int64_t)cb * rbs + rb) * kUnitBytes;
+    }
+    // into shared memory, transposed if tall
+    __device__ __forceinline__ void put(const float (&x)[4][4], float (*s_u)[kUnit + 1]) const {
+        const int along = (threadIdx.x & 15) * 4, across0 = threadIdx.x >> 4;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const int my_a = (tall ? cb : rb) * kUnit + across0 + k * 16;
-        const int64_t e = m.offset + (int64_t)my_a * m.cols + my_r;
-        float g[4] = {}, v[4] = {};
-        if (my_a < m.rows && fours && my_r < m.cols) {
-            if (momentum) *reinterpret_cast<float4*>(v) = __ldcg(reinterpret_cast<const float4*>(momentum + e));
-            if (!momentum || nesterov) load4(grad + e, g);
-        } else if (my_a < m.rows) {
+        for (int k = 0; k < 4; ++k)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                if (my_r + j >= m.cols) continue;
-                if (momentum) v[j] = __ldcg(momentum + e + j);
-                if (!momentum || nesterov) g[j] = widen(grad[e + j]);
+                const int across = across0 + k * 16;
+                if (tall) s_u[along + j][across] = x[k][j]; else s_u[across][along + j] = x[k][j];
             }
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) x[k][j] = !momentum ? g[j] : nesterov ? fmaf(mu, v[j], g[j]) : v[j];
     }
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int across = across0 + k * 16;
-            if (tall) s_u[along + j][across] = x[k][j]; else s_u[across][along + j] = x[k][j];
-        }
-    __syncthreads();
-    const float scale = inv * (float)(1 << kX);
-    const int64_t unit = ((int64_t)cb * (m.sp / kUnit) + rb) * kUnitBytes;
+};
+
+// From there as fp16 in the tensor cores' order.
+__device__ __forceinline__ void store_image(uint8_t* to, const float (*s_u)[kUnit + 1]) {
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-        const int r = (threadIdx.x >> 3) + k * 32, c8 = threadIdx.x & 7;
+        const int row = (threadIdx.x >> 3) + k * 32, c8 = threadIdx.x & 7;
         float v[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = s_u[r][c8 * 8 + j] * scale;
-        *reinterpret_cast<uint4*>(ws + m.x[0] + unit + in_unit(r, c8)) = pack8(v);
+        for (int j = 0; j < 8; ++j) v[j] = s_u[row][c8 * 8 + j];
+        *reinterpret_cast<uint4*>(to + in_unit(row, c8)) = pack8(v);
+    }
+}
+
+// M <- mu M + G, U as X and its sum of squares (fp64: gradients may be tiny or huge), in one pass.  The last CTA of a matrix
+// to arrive adds the sums of all in their order.  66 M elements with bf16 gradients take 133 us, 0.92 of the copy rate
+// (with the norm from a pass of its own and X from a second one 110 + 100).  The loads of a unit are under way while the one
+// before it is stored: without that 181; CTAs that take eight neighbouring units each instead of going side by side 206.
+template <typename T>
+__global__ void __launch_bounds__(256, kMomentumCtas) momentum_kernel(const __grid_constant__ Table t, const T* __restrict__ grad,
+                                                          float* __restrict__ momentum, float mu, int nesterov, float eps,
+                                                          int quads, double* __restrict__ partial, Norms norms,
+                                                          uint8_t* __restrict__ ws) {
+    __shared__ float s_u[kUnit][kUnit + 1];
+    __shared__ double s_sum[8];
+    __shared__ int s_last;
+    launch_dependents();
+    const int i = find(t.chunk_at, t.n, blockIdx.x), chunk = blockIdx.x - t.chunk_at[i];
+    const Mat& m = t.m[i];
+    // (its CTAs go through the matrix side by side: what they touch at one time lies together)
+    const int units = (m.sp / kUnit) * (m.lp / kUnit);
+    double sum = 0.0;
+    struct alignas(4 * sizeof(T)) Four { uint32_t w[sizeof(T)]; };
+    Four raw[4];                                                      // (taken apart where it is used: until then nothing waits)
+    float v[4][4];
+    const auto load = [&](const UnitOf& at) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int64_t e = at.e + k * at.by;
+            const bool in = at.a + k * 16 < m.rows && at.r < m.cols;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[k][j] = 0.0f;
+            raw[k] = Four{};
+            if (in && at.fours) {
+                raw[k] = *reinterpret_cast<const Four*>(grad + e);
+                if (momentum) load4((const float*)momentum + e, v[k]);
+            } else if (in) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (at.r + j >= m.cols) continue;
+                    reinterpret_cast<T*>(raw[k].w)[j] = grad[e + j];
+                    if (momentum) v[k][j] = momentum[e + j];
+                }
+            }
+        }
+    };
+    load(UnitOf(m, chunk, quads));
+    wait_prerequisites();                                             // (which reads the momentum too)
+    const float scale = __uint_as_float((uint32_t)(127 + __ldcg(norms.exponent + i)) << 23);
+#pragma unroll 1
+    for (int u = chunk; u < units; u += m.n_chunks) {
+        const UnitOf at(m, u, quads);
+        float g[4][4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) g[k][j] = widen(reinterpret_cast<const T*>(raw[k].w)[j]);
+            if (momentum) {
+                const int64_t e = at.e + k * at.by;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    v[k][j] = fmaf(mu, v[k][j], g[k][j]);
+                    g[k][j] = nesterov ? fmaf(mu, v[k][j], g[k][j]) : v[k][j];
+                }
+                if (at.a + k * 16 < m.rows && at.r < m.cols) {
+                    if (at.fours) {
+                        *reinterpret_cast<float4*>(momentum + e) = *reinterpret_cast<const float4*>(v[k]);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            if (at.r + j < m.cols) momentum[e + j] = v[k][j];
+                    }
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                sum = fma((double)g[k][j], (double)g[k][j], sum);
+                g[k][j] *= scale;
+            }
+        }
+        at.put(g, s_u);
+        if (u + m.n_chunks < units) load(UnitOf(m, u + m.n_chunks, quads));   // under way while this unit is stored
+        __syncthreads();
+        store_image(ws + at.image, s_u);
+        __syncthreads();
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_down_sync(0xffffffffu, sum, o);
+    if ((threadIdx.x & 31) == 0) s_sum[threadIdx.x >> 5] = sum;
+    __syncthreads();
+    partial += t.chunk_at[i];
+    if (threadIdx.x == 0) {
+        sum = 0.0;
+        for (int w = 0; w < 8; ++w) sum += s_sum[w];
+        partial[chunk] = sum;
+        __threadfence();
+        s_last = atomicAdd(norms.arrived + i, 1) == m.n_chunks - 1;
+        __threadfence();
+    }
+    __syncthreads();
+    if (!s_last) return;
+    sum = 0.0;
+#pragma unroll 8
+    for (int c = threadIdx.x; c < m.n_chunks; c += 256) sum += __ldcg(partial + c);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_down_sync(0xffffffffu, sum, o);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) s_sum[threadIdx.x >> 5] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        sum = 0.0;
+        for (int w = 0; w < 8; ++w) sum += s_sum[w];
+        const double norm = sqrt(sum), stored = norm * (double)scale;
+        const bool good = stored <= 32768.0 && stored >= sqrt((double)m.rows * m.cols) * (1.0 / 8192);
+        norms.inverse[i] = (float)(1.0 / (norm + (double)eps));
+        norms.factor[i] = good ? (float)((double)(1 << kX) / (double)scale / (norm + (double)eps)) : 1.0f;
+        norms.again[i] = !good;
+    }
+}
+
+// X of the matrices whose scale was wrong (or whose entries are zero or not finite): U again, from what the momentum pass
+// left, by its norm.
+template <typename T>
+__global__ void __launch_bounds__(256) again_kernel(const __grid_constant__ Table t, const T* __restrict__ grad,
+                                                    const float* __restrict__ momentum, float mu, int nesterov, int quads,
+                                                    Norms norms, uint8_t* __restrict__ ws) {
+    __shared__ float s_u[kUnit][kUnit + 1];
+    __shared__ int s_again[kMaxMats];
+    wait_prerequisites();
+    int mine = 0;
+    if ((int)threadIdx.x < t.n) s_again[threadIdx.x] = mine = __ldcg(norms.again + threadIdx.x);
+    if (!__syncthreads_or(mine)) return;
+    for (int i = 0; i < t.n; ++i) {
+        if (!s_again[i]) continue;
+        const Mat& m = t.m[i];
+        const int units = (m.sp / kUnit) * (m.lp / kUnit);
+        const float scale = __ldcg(norms.inverse + i) * (float)(1 << kX);
+        for (int u = blockIdx.x; u < units; u += gridDim.x) {
+            const UnitOf at(m, u, quads);
+            float x[4][4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int64_t e = at.e + k * at.by;
+                float g[4] = {}, v[4] = {};
+                if (at.a + k * 16 < m.rows && at.r < m.cols) {
+                    if (at.fours) {
+                        if (momentum) *reinterpret_cast<float4*>(v) = __ldcg(reinterpret_cast<const float4*>(momentum + e));
+                        if (!momentum || nesterov) load4(grad + e, g);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            if (at.r + j >= m.cols) continue;
+                            if (momentum) v[j] = __ldcg(momentum + e + j);
+                            if (!momentum || nesterov) g[j] = widen(grad[e + j]);
+                        }
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x[k][j] = (!momentum ? g[j] : nesterov ? fmaf(mu, v[j], g[j]) : v[j]) * scale;
+            }
+            __syncthreads();                                          // (s_u has been read)
+            at.put(x, s_u);
+            __syncthreads();
+            store_image(ws + at.image, s_u);
+        }
     }
 }
 
@@ -341,10 +446,9 @@ struct Phase {
     int8_t plus, to;                  // matrix added times beta (-1: none); where the result goes
     int8_t x_in;                      // which of the two X buffers holds X
     int8_t last;                      // an application that writes bf16 into the caller's vector, not the next X
-    int8_t pad;
+    int8_t by_norm;                   // power of the factor of X in alpha: X is as the momentum pass has left it
     float alpha, beta, gamma;         // result = alpha (left right) + beta plus + gamma I
 };
-constexpr int kMaxPhases = (SIDCO_ORTHO_MAX_STEPS + 1) / 2 * 7;
 
 struct Phases {
     int n;
@@ -412,7 +516,7 @@ __device__ __forceinline__ bool wait_arrivals(const unsigned* arrived, unsigned 
 
 __global__ void __launch_bounds__(kChainThreads, 1) __cluster_dims__(2)
     chain_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ Phases ph, const Tile* tiles, uint8_t* ws,
-                 __nv_bfloat16* __restrict__ out, unsigned* arrived, int* timeouts) {
+                 __nv_bfloat16* __restrict__ out, const float* __restrict__ factor, unsigned* arrived, int* timeouts) {
     extern __shared__ uint8_t s_raw[];
     __shared__ uint64_t s_full[kStages], s_free[kStages], s_sums[2], s_taken[2], s_plus[2];
     __shared__ uint32_t s_tmem;
@@ -596,12 +700,14 @@ __global__ void __launch_bounds__(kChainThreads, 1) __cluster_dims__(2)
             const int width = sym ? ph.sym_width : ph.apply_width, parts = width / 64;
             const int total = sym ? ph.sym_tiles : ph.apply_tiles;
             const Tile* list = tiles + (sym ? 0 : ph.sym_tiles);
-            const float alpha = p.alpha, beta = p.beta, gamma = p.gamma;
+            const float beta = p.beta, gamma = p.gamma;
             for (int i = first; i < total; i += n_pairs, ++n) {
                 const Tile d = list[i];
                 const int buf = n & 1;
                 const int rb = d.ti * 4 + (int)rank * 2;              // first unit row of this CTA's part
                 const bool mirror = sym && d.tj < d.ti * (kRows / width), tall = d.rows > d.cols;
+                float alpha = p.alpha;
+                for (int k = 0; k < p.by_norm; ++k) alpha *= __ldg(factor + d.mat);
                 const int diagonal = d.ti * kRows + (int)rank * 128 + row - d.tj * width;     // the column on the diagonal
                 ok = mbar_wait(smem_addr(&s_sums[buf]), (n >> 1) & 1, &s_failed);
                 __syncwarp();
@@ -1116,12 +1222,16 @@ static int64_t lay_out(const int64_t* offsets, const int64_t* rows, const int64_
         m.l = (int)std::max(r, c);
         m.sp = (int)up(m.s, kRows);
         m.lp = (int)up(m.l, kUnit);
-        t->chunk_at[k] = (int)chunks;
-        t->unit_at[k] = (int)units;
-        m.partial0 = (int)chunks;
-        m.n_chunks = (int)((r * c + 7 + kChunk - 1) / kChunk);          // (up to seven elements before the first)
-        chunks += m.n_chunks;
         units += (int64_t)(m.sp / kUnit) * (m.lp / kUnit);
+    }
+    // whole rounds of the momentum pass' CTAs, each a part of one matrix
+    const int64_t at_once = 2 * kMostPairs * kMomentumCtas, rounds = (units + at_once * kMostUnits - 1) / (at_once * kMostUnits);
+    t->chunk = (int)((units + at_once * rounds - n - 1) / (at_once * rounds - n));
+    for (int k = 0; k < n; ++k) {
+        Mat& m = t->m[k];
+        t->chunk_at[k] = (int)chunks;
+        m.n_chunks = (int)(((int64_t)(m.sp / kUnit) * (m.lp / kUnit) + t->chunk - 1) / t->chunk);
+        chunks += m.n_chunks;
     }
     // Columns of a tile: 256 give the tensor cores two thirds of the operand traffic per operation, 128 give twice as many
     // tiles for few matrices.  A tile of 128 columns takes about 0.6 of the time of one of 256.
@@ -1146,10 +1256,9 @@ static int64_t lay_out(const int64_t* offsets, const int64_t* rows, const int64_
     sym = choose(true, &t->sym_width);
     apply = choose(false, &t->apply_width);
     t->chunk_at[n] = (int)chunks;
-    t->unit_at[n] = (int)units;
-    if (chunks > 0x7fffffff || units > 0x7fffffff || sym + apply > 0x7fffffff) return -1;
+    if (chunks > 0x7fffffff || sym + apply > 0x7fffffff) return -1;
     at = up(at + chunks * 8, 1024);
-    at = up(at + n * 8 + kMaxPhases * 4, 1024);                       // inverse norms, arrival counters
+    at = up(at + (5 * n + kMaxPhases) * 4, 1024);                     // norms, arrival counters
     t->tiles = at;
     at = up(at + (sym + apply) * (int64_t)sizeof(Tile), kUnitBytes);
     for (int k = 0; k < n; ++k) {
@@ -1165,6 +1274,13 @@ static int64_t lay_out(const int64_t* offsets, const int64_t* rows, const int64_
 
 static bool is_small(int64_t rows, int64_t cols) {
     return std::min(rows, cols) <= kSmallS && std::max(rows, cols) <= kSmallCluster * kSmallUnits * kUnit;
+}
+
+// CTAs of a cluster that holds a small matrix.
+static int small_ctas(int64_t l) {
+    int ctas = 1;
+    while ((int64_t)ctas * kSmallUnits * kUnit < l) ctas *= 2;
+    return ctas;
 }
 
 // The small matrices or the others; longer ones first, so that the last tiles of a launch are short ones.
@@ -1257,24 +1373,59 @@ static cudaError_t resident_pairs(int* n) {
     return e == cudaSuccess && *n < 1 ? cudaErrorInvalidConfiguration : e;
 }
 
+// A stream per device on which the small matrices run beside the momentum pass of the others (not beside their products: a
+// cooperative launch waits for the SMs, 169 us become 214 with four matrices of 128 x 1152).  It takes over from the caller's
+// stream and hands back to it within one call, under the lock.  Its CTAs need whole SMs, which they get only if they come
+// first: the stream has priority, and the caller's goes on when this one has been reached (300 x 1000 beside five of
+// 64 x 576: 134 us instead of 140; 132 alone).
+struct Beside {
+    cudaStream_t stream = nullptr;
+    cudaEvent_t fork = nullptr, ready = nullptr, join = nullptr;
+    std::mutex lock;
+
+    cudaError_t begin(cudaStream_t from) {
+        cudaError_t e;
+        if (!stream) {
+            int least, greatest;
+            if ((e = cudaDeviceGetStreamPriorityRange(&least, &greatest)) != cudaSuccess) return e;
+            if ((e = cudaStreamCreateWithPriority(&stream, cudaStreamNonBlocking, greatest)) != cudaSuccess) return e;
+        }
+        if (!fork && (e = cudaEventCreateWithFlags(&fork, cudaEventDisableTiming)) != cudaSuccess) return e;
+        if (!join && (e = cudaEventCreateWithFlags(&join, cudaEventDisableTiming)) != cudaSuccess) return e;
+        if (!ready && (e = cudaEventCreateWithFlags(&ready, cudaEventDisableTiming)) != cudaSuccess) return e;
+        if ((e = cudaEventRecord(fork, from)) != cudaSuccess) return e;
+        if ((e = cudaStreamWaitEvent(stream, fork, 0)) != cudaSuccess) return e;
+        if ((e = cudaEventRecord(ready, stream)) != cudaSuccess) return e;
+        return cudaStreamWaitEvent(from, ready, 0);
+    }
+    cudaError_t end(cudaStream_t to) {
+        const cudaError_t e = cudaEventRecord(join, stream);
+        return e != cudaSuccess ? e : cudaStreamWaitEvent(to, join, 0);
+    }
+};
+
 template <typename T>
 static cudaError_t chain(const Table& t, const void* grad, float* momentum, float mu, int nesterov, int steps, float eps,
                          uint16_t* out, uint8_t* ws, int64_t ws_bytes, int max_pairs, int* timeouts, cudaStream_t s) {
     cudaError_t e;
     double* partial = reinterpret_cast<double*>(ws);
     const int64_t at = up((int64_t)t.chunk_at[t.n] * 8, 1024);
-    float* inv_norm = reinterpret_cast<float*>(ws + at);
-    int* arrived = reinterpret_cast<int*>(ws + at) + t.n;
-    if ((e = cudaMemsetAsync(arrived, 0, (t.n + kMaxPhases) * sizeof(int), s)) != cudaSuccess) return e;
-    // whole sectors per lane (and with them 16-byte accesses of the second pass)
-    const int vec = (uintptr_t)grad % (8 * sizeof(T)) == 0 && (uintptr_t)momentum % 32 == 0;
+    int* words = reinterpret_cast<int*>(ws + at);
+    const Norms norms = {words, (float*)(words + t.n), (float*)(words + 2 * t.n), words + 3 * t.n, words + 4 * t.n};
+    unsigned* phases = (unsigned*)(words + 5 * t.n);
+    // 16-byte accesses (where the matrix allows them)
+    const int quads = (uintptr_t)grad % (4 * sizeof(T)) == 0 && (uintptr_t)momentum % 16 == 0;
     // (a plain launch: the first kernel waits for everything before it)
-    momentum_kernel<T><<<t.chunk_at[t.n], 256, 0, s>>>(t, (const T*)grad, momentum, mu, nesterov, eps, vec,
-                                                       partial, arrived, inv_norm);
+    const int n_tiles = t.sym_at[t.n] + t.apply_at[t.n];
+    prepare_kernel<T><<<std::max(t.n, std::min(2 * kMostPairs, (n_tiles + 255) / 256)), 256, 0, s>>>(
+        t, (const T*)grad, (const float*)momentum, mu, nesterov, norms, phases, ws);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
     sidco_internal::note_launch();
-    if ((e = launch(normalize_kernel<T>, dim3(t.unit_at[t.n]), 256, 0, s, t, (const T*)grad, (const float*)momentum, mu,
-                    nesterov, vec, (const float*)inv_norm, ws)) != cudaSuccess)
+    if ((e = launch(momentum_kernel<T>, dim3(t.chunk_at[t.n]), 256, 0, s, t, (const T*)grad, momentum, mu, nesterov, eps, quads,
+                    partial, norms, ws)) != cudaSuccess)
+        return e;
+    if ((e = launch(again_kernel<T>, dim3(4 * kMostPairs), 256, 0, s, t, (const T*)grad, (const float*)momentum, mu, nesterov,
+                    quads, norms, ws)) != cudaSuccess)
         return e;
     // the workspace as rows of 128 bytes; a box is one unit (its bytes are in the tensor cores' order already)
     CUtensorMap map{};
@@ -1289,7 +1440,9 @@ static cudaError_t chain(const Table& t, const void* grad, float* momentum, floa
     const auto two = [](int k) { return ldexpf(1.0f, k); };
     int in = 0;
     const auto sym = [&](int left, int right, int plus, int to, float alpha, float beta, float gamma) {
-        ph.p[ph.n++] = Phase{1, (int8_t)left, (int8_t)right, (int8_t)plus, (int8_t)to, (int8_t)in, 0, 0, alpha, beta, gamma};
+        const int by_norm = ph.n == 0 ? 2 : 0;                        // (the first Gram product)
+        ph.p[ph.n++] = Phase{1, (int8_t)left, (int8_t)right, (int8_t)plus, (int8_t)to, (int8_t)in, 0, (int8_t)by_norm,
+                             alpha, beta, gamma};
     };
     const auto polynomial = [&](int a, int to) {
         sym(a, a, a, to, kCc * two(kB - 2 * kA), kCb * two(kB - kA), kCa * two(kB));
@@ -1305,9 +1458,9 @@ static cudaError_t chain(const Table& t, const void* grad, float* momentum, floa
             sym(kBufT, kBufB, -1, kBufP, two(kP - 2 * kB), 0.0f, 0.0f);
         }
         done += group;
-        const int scale_p = group == 2 ? kP : kB, last = done == steps;
-        ph.p[ph.n++] = Phase{0, (int8_t)(group == 2 ? kBufP : kBufB), 0, -1, 0, (int8_t)in, (int8_t)last, 0,
-                             last ? two(-scale_p - kX) : two(-scale_p), 0.0f, 0.0f};
+        const int scale_p = group == 2 ? kP : kB, last = done == steps, by_norm = done == group;
+        ph.p[ph.n++] = Phase{0, (int8_t)(group == 2 ? kBufP : kBufB), 0, -1, 0, (int8_t)in, (int8_t)last,
+                             (int8_t)by_norm, last ? two(-scale_p - kX) : two(-scale_p), 0.0f, 0.0f};
         in ^= 1;
     }
     cudaLaunchConfig_t cfg{};
@@ -1321,7 +1474,7 @@ static cudaError_t chain(const Table& t, const void* grad, float* momentum, floa
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
     e = cudaLaunchKernelEx(&cfg, chain_kernel, map, ph, (const Tile*)(ws + t.tiles), ws, (__nv_bfloat16*)out,
-                           (unsigned*)(arrived + t.n), timeouts);
+                           (const float*)norms.factor, phases, timeouts);
     if (e == cudaSuccess) sidco_internal::note_launch();
     return e;
 }
@@ -1356,27 +1509,6 @@ static cudaError_t small_launch(const SmallMats& mats, int ctas, const void* gra
     if (e == cudaSuccess) sidco_internal::note_launch();
     return e;
 }
-
-// A stream per device on which the small matrices run beside the others (they need a third of the SMs for a part of the
-// time).  It takes over from the caller's stream and hands back to it within one call, under the lock.
-struct Beside {
-    cudaStream_t stream = nullptr;
-    cudaEvent_t fork = nullptr, join = nullptr;
-    std::mutex lock;
-
-    cudaError_t begin(cudaStream_t from) {
-        cudaError_t e;
-        if (!stream && (e = cudaStreamCreateWithFlags(&stream, cudaStreamNonBlocking)) != cudaSuccess) return e;
-        if (!fork && (e = cudaEventCreateWithFlags(&fork, cudaEventDisableTiming)) != cudaSuccess) return e;
-        if (!join && (e = cudaEventCreateWithFlags(&join, cudaEventDisableTiming)) != cudaSuccess) return e;
-        if ((e = cudaEventRecord(fork, from)) != cudaSuccess) return e;
-        return cudaStreamWaitEvent(stream, fork, 0);
-    }
-    cudaError_t end(cudaStream_t to) {
-        const cudaError_t e = cudaEventRecord(join, stream);
-        return e != cudaSuccess ? e : cudaStreamWaitEvent(to, join, 0);
-    }
-};
 
 }  // namespace sidco_ortho
 
@@ -1434,8 +1566,7 @@ static int orthogonalize(const void* grad, int grad_type, float* momentum, float
         for (size_t from = 0; from < small.size() && r == cudaSuccess;) {
             SmallMats mats;
             const int64_t longest = std::max(rows[small[from]], cols[small[from]]);
-            int ctas = 1;
-            while ((int64_t)ctas * kSmallUnits * kUnit < longest) ctas *= 2;
+            const int ctas = small_ctas(longest);
             for (mats.n = 0; from < small.size() && mats.n < kMaxMats; ++from, ++mats.n)
                 mats.m[mats.n] = {offsets[small[from]], (int)rows[small[from]], (int)cols[small[from]]};
             if (grad_type == SIDCO_T_F32)

@@ -240,3 +240,23 @@ def test_few_rows_keep_two_parts_of_their_products(shape):
     1.5e-3 at worst.  Next to bf16's 1.7e-3 that makes sqrt(1.7^2 + 1.5^2) e-3 = 2.3e-3 of the norm."""
     check([shape, shape], tol=2.3e-3)
     check([shape, shape], tol=2.3e-3, dtype="bfloat16", nesterov=False)
+
+
+@pytest.mark.parametrize("shape", [(150, 700), (700, 150), (300, 301), (130, 129)])
+@pytest.mark.parametrize("low, high", [(0.0, 1e-3), (0.0, 1e7), (1e-6, 1e6), (0.0, 3e-30), (1e6, 1e6)])
+@pytest.mark.parametrize("with_momentum", [False, True])
+def test_norms_that_hide_in_one_entry(shape, low, high, with_momentum):
+    """A matrix whose norm no sample of its entries tells: one entry holds it.  Beside it in the call a matrix like any."""
+    r, c = shape
+    r_ = rng(r + c)
+    other = (140, 200)
+    grads = [r_.laplace(0, 1, shape) * low, r_.laplace(0, 1, other)]
+    grads[0][r // 3, c // 2 + 1] = high
+    moms = [np.zeros(shape), r_.laplace(0, 1, other).astype(np.float32)]
+    mu = 0.9 if with_momentum else None
+    out, mom, held = run([shape, other], [0, r * c + 3], r * c + 3 + 28000, grads, moms, mu, with_momentum, 5, eps=0.0)
+    for (rows, cols), o, m in zip([shape, other], [0, r * c + 3], moms):
+        g = held[o:o + rows * cols].reshape(rows, cols)
+        want, _ = N.orthogonalize(g, m if with_momentum else None, float(np.float32(mu or 0)), with_momentum, 5, eps=0.0)
+        err = np.linalg.norm(out[o:o + rows * cols].reshape(rows, cols) - want) / np.linalg.norm(want)
+        assert err <= TOL, ((rows, cols), err)
