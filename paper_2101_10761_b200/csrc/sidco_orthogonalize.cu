@@ -21,7 +21,7 @@
 // Measured: 66 M elements in six matrices 1500 wide (LSTM-shaped, bf16 gradients) 1.25 ms, 1.35 once the power limit has set
 // in: momentum and first X 0.13 (0.92 of the copy rate), products 1.02 ms (1.26 Tflop, 0.74 of cuBLAS's bf16 rate:
 // applications 126 us each at that rate, Gram products 95 us where 70 would do if 10000 and 6000 rows divided evenly, the
-// others 25 us each for 15 us of work); VGG-16-shaped 0.29 ms, of which 0.21 in 17 dependent phases of 7 to 24 us; twenty
+// others 25 us each for 15 us of work); VGG-16-shaped 0.28 ms, of which 0.2 in 17 dependent phases of 6 to 23 us; twenty
 // small matrices (ResNet-20) 41 us.
 //
 // Workspace matrices are stored as units of 64 x 64 fp16 in the 128-byte-swizzled image that the tensor cores read, so
@@ -470,10 +470,11 @@ struct Phases {
 //   warps 2-9  take the sums out: a quarter of the CTA's 128 rows, one half of every 64 columns
 //   warp 10    stores what they have put together, and fetches matrices to add (a warp that did both lost 0.5 us per store)
 // Between phases only the threads that start loads wait for the others (bounded): every CTA counts itself into the phase
-// when its results are stored, 2.5 us before the others have seen it and start to load.  As launches of their own the 17
-// phases of five steps cost the LSTM-shaped model 50 us more.  Counting per matrix, so that pairs go on to matrices that
+// when its results are stored, 1.7 us before the others have seen it and start to load (2.5 with proxy fences over all of
+// memory instead of the global one and a fence behind the polling loop instead of loads that acquire: 300 x 1000 137 us
+// instead of 121).  As launches of their own the 17 phases of five steps cost the LSTM-shaped model 50 us more.  Counting per matrix, so that pairs go on to matrices that
 // are ready, and a list from which pairs take tiles as they come free changed nothing: a tile's way through a phase (loads
-// 1.2, products of K = 1500 8.6, sums out 2.5, counting 2.5 us) is as long as the phase.
+// 1.2, products of K = 1500 8.6, sums out 2.5, counting 1.7 us) is as long as the phase.
 
 constexpr int kOutBytes = 4 * kUnitBytes;                             // 64 columns: the images of a tile part and its mirror
 constexpr int kChainThreads = 352;
@@ -502,15 +503,14 @@ __device__ __forceinline__ bool wait_arrivals(const unsigned* arrived, unsigned 
     const unsigned long long start = time_ns();
     for (uint32_t i = 1;; ++i) {
         unsigned v;
-        asm volatile("ld.relaxed.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(arrived) : "memory");
+        asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(arrived) : "memory");
         if (v >= count) break;
         if ((i & 63u) == 0u && (*failed || time_ns() - start > limit_ns)) {
             *failed = 1;
             return false;
         }
     }
-    asm volatile("fence.acq_rel.gpu;" ::: "memory");
-    fence_async_all();                                                // (what they stored is read by bulk copies)
+    fence_async_global();                                             // (what they stored is read by bulk copies)
     return true;
 }
 
@@ -683,7 +683,7 @@ __global__ void __launch_bounds__(kChainThreads, 1) __cluster_dims__(2)
             }
             if (!last && ok && f != ph.drop && elect_one()) {         // stored: count this CTA in
                 bulk_store_wait();
-                fence_async_all();
+                fence_async_global();
                 asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(arrived + f) : "memory");
             }
             __syncwarp();

@@ -143,6 +143,7 @@ __device__ __forceinline__ void tensor_load_2d_pair(uint32_t dst, const void* ma
 }
 
 __device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void fence_async_global() { asm volatile("fence.proxy.async.global;" ::: "memory"); }
 __device__ __forceinline__ void fence_async_all() { asm volatile("fence.proxy.async;" ::: "memory"); }
 
 // Dependent launches: let the next kernel of the stream be set up / wait for everything the kernels before wrote.
