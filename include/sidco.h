@@ -329,8 +329,8 @@ int sidco_mx4_mean(const uint8_t* codes_all, const uint8_t* scales_all, int n_wo
  * with (a, b, c) = (3.4445, -4.7750, 2.0315); a matrix with more rows than columns goes through its transpose.  Five
  * steps bring all but the smallest singular values close to one.  Products are of fp16 operands with fp32 sums; the result
  * is within about 2e-3 of the formula in norm before its rounding to bf16 (5e-3 where the singular values span three
- * decades).  A matrix with a NaN or an infinity
- * becomes NaN; the others are not affected.  Elements outside the matrices are neither read nor written.
+ * decades).  A matrix with a NaN or an infinity becomes NaN; the others are not affected.  Elements outside the matrices are
+ * neither read nor written.
  *
  * grad      device, grad_type[], read only.
  * momentum  device, float[], in/out; NULL: U = grad (mu and nesterov are not used).
@@ -343,10 +343,10 @@ int sidco_mx4_mean(const uint8_t* codes_all, const uint8_t* scales_all, int n_wo
  * workspace device, 256-byte aligned, at least sidco_orthogonalize_workspace_bytes(rows, cols, n_mats) bytes; caller-owned,
  *           nothing is kept in it between calls; not to be shared by calls that overlap.  Matrices with a shorter side of
  *           at most 128 and a longer one of at most 2048 need none: the size may be 0, the pointer NULL.
- * stream    everything is enqueued here (one launch for small matrices, three and a small clear for others, for up to 128
- *           matrices of a kind); no synchronisation, no device allocation.  With matrices of both kinds the small ones run
- *           on a stream of the library that is forked from and joined to this one within the call (not while this one
- *           is being captured).  The kernel for larger matrices is launched cooperatively.
+ * stream    everything is enqueued here (one launch for small matrices, four for others, for up to 128 matrices of a kind);
+ *           no synchronisation, no device allocation.  With matrices of both kinds the small ones run on a stream of the
+ *           library that is forked from and joined to this one within the call (not while this one is being captured).
+ *           The kernel for larger matrices is launched cooperatively.
  */
 #define SIDCO_ORTHO_MAX_DIM   4194304
 #define SIDCO_ORTHO_MAX_SHORT 16384
