@@ -327,9 +327,13 @@ int sidco_mx4_mean(const uint8_t* codes_all, const uint8_t* scales_all, int n_wo
  *     momentum <- mu * momentum + grad;     U = grad + mu * momentum (nesterov) or momentum;
  *     X = U / (|U|_F + eps);   `steps` times: A = X X^T, X <- a X + (b A + c A^2) X;     out <- X
  * with (a, b, c) = (3.4445, -4.7750, 2.0315); a matrix with more rows than columns goes through its transpose.  Five
- * steps bring all but the smallest singular values close to one.  Products are of fp16 operands with fp32 sums; the result
- * is within about 2e-3 of the formula in norm before its rounding to bf16 (5e-3 where the singular values span three
- * decades).  A matrix with a NaN or an infinity becomes NaN; the others are not affected.  Elements outside the matrices are
+ * steps bring all but the smallest singular values close to one.  Products are of fp16 operands with fp32 sums, X as the sum
+ * of two fp16 numbers where more than two steps follow.  For up to six steps the result is within 3e-3 of the formula in
+ * norm, its rounding to bf16 (1.7e-3) included; within 4e-3 where the singular values span three decades and 6e-3 where the
+ * rank is below the shorter side (2e-3 for any rank if that side is at most 64, 3e-3 if it is at most 128).  Beyond six steps
+ * the rounding of what is zero in a matrix of low rank grows by a with every step, as in any 32-bit iteration.  Where |U|_F is
+ * far below eps, entries of X lose their bits below 2^-38.  A matrix with a NaN or an infinity becomes NaN; the others are
+ * not affected.  Elements outside the matrices are
  * neither read nor written.
  *
  * grad      device, grad_type[], read only.

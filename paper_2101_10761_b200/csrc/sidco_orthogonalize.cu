@@ -7,22 +7,33 @@
 // The steps are taken in groups (two, then one if their number is odd, then twos).  Inside a group only s x s matrices
 // are multiplied: with B = a I + b A + c A^2 the Gram matrix of the next X is B A B, and the group's product of the B is
 // applied to X once.  That replaces a Gram product and an application over the long side (3 s^2 l) by four products
-// (4 s^3) of which only half the tiles are computed and mirrored (all of them are symmetric: polynomials of one A).
+// (4 s^3), of all but the last of which only half the tiles are computed and mirrored (they are symmetric: polynomials of
+// one A).
 // Longer groups would save more, but each step of a group amplifies the rounding of A by up to a^2: groups of three
 // and two have 3e-3 of error where these have 1.1e-3 to 2e-3, as much as single steps (Laplace entries with eight
 // strong directions, 64 x 64 to 512 x 4608).
 //
 // Operands are fp16 (eleven significant bits; bf16's eight would leave 1e-2 of error in the result), sums fp32.  Every
 // singular value stays below 1.2 and every eigenvalue of a B within [0.6, 3.45], so fixed powers of two (kX, kA, ...)
-// keep all entries inside fp16's normal range.  The largest error is the rounding of the first X where small singular
-// values are scaled up by a^5 (1e-3 to 2e-3 of the result's norm for the entries above, 3e-3 for singular values over two
-// decades, 5e-3 over three).  A second fp16 part of X brings that to 2e-3 and 4e-3, for a twelfth of the time: not kept.
+// keep all entries inside fp16's normal range.
 //
-// Measured: 66 M elements in six matrices 1500 wide (LSTM-shaped, bf16 gradients) 1.25 ms, 1.35 once the power limit has set
-// in: momentum and first X 0.13 (0.92 of the copy rate), products 1.02 ms (1.26 Tflop, 0.74 of cuBLAS's bf16 rate:
-// applications 126 us each at that rate, Gram products 95 us where 70 would do if 10000 and 6000 rows divided evenly, the
-// others 25 us each for 15 us of work); VGG-16-shaped 0.28 ms, of which 0.2 in 17 dependent phases of 6 to 23 us; twenty
-// small matrices (ResNet-20) 41 us.
+// X has two fp16 parts, X = H + L, wherever more than two steps follow.  What rounding adds to X where X has no singular
+// values of its own is multiplied by a with every step, by a^5 = 485 in five, and a gradient of few rows, which is of low
+// rank, is little else in the end: with H alone its update is off by 1.4e-1 (rank 1), 3e-2 (8), 2e-2 (64) of its norm.
+// H suffices for the Gram matrix (an error of A turns the columns of X, but adds no rank: with L in it the results are the
+// same); the applications take both, P H + P L.  The last group (up to two steps) takes H alone.  Off by, in norm, with the
+// rounding to bf16 (1.7e-3) included:
+//     Laplace entries                                1.8e-3 to 2.4e-3
+//     singular values over three decades             2.9e-3 to 3.1e-3
+//     rank 8 beside noise of a hundredth of its norm 2.7e-3 to 2.8e-3
+//     rank 1, 2 / 8, 64                              4.4e-3 to 5.4e-3 / 4.0e-3 to 4.3e-3: the rounding of the s x s matrices
+// (256 x 256 to 1500 x 6000, five steps; beyond six the rounding of 2^-22 itself comes to be seen in matrices of low rank,
+// as it would in a 32-bit iteration: a^10 2^-24 = 1.4e-2).
+// L costs a quarter of the time of large models (LSTM-shaped 1.34 -> 1.68 ms), and P in all its tiles another 3 % (below).
+//
+// Measured: 66 M elements in six matrices 1500 wide (LSTM-shaped, bf16 gradients) 1.73 ms: momentum and first X 0.16 (0.86 of
+// the copy rate for 924 MB), products 1.31 ms under ncu (1.7 Tflop, 0.78 of cuBLAS's bf16 rate), longer in a loop, where the
+// power limit sets in; VGG-16-shaped 0.31 ms, of which 0.23 in 17 dependent phases; twenty small matrices (ResNet-20) 45 us.
 //
 // Workspace matrices are stored as units of 64 x 64 fp16 in the 128-byte-swizzled image that the tensor cores read, so
 // that a stage of operands is one or two contiguous bulk copies, the same unit serves as K-major operand (Gram) and as
@@ -65,11 +76,14 @@ constexpr int kMomentumCtas = 4;      // its CTAs per SM
 constexpr int kMaxPhases = (SIDCO_ORTHO_MAX_STEPS + 1) / 2 * 7;   // products of a chain
 constexpr int kSamples = 2048;        // elements of a matrix from which its norm is estimated
 
+// Lists of tiles: of s x s results the lower triangle (the rest is its mirror image) or all, applications.
+enum List { kLower, kWhole, kApply, kLists };
+
 enum Buffer { kBufA, kBufA2, kBufB, kBufT, kBufP, kSmallBuffers };
 
 struct Mat {
     int64_t offset;                   // of the matrix in the flat vectors
-    int64_t x[2];                     // bytes into the workspace: s x l matrices, in turn
+    int64_t x[2];                     // bytes into the workspace: s x l matrices, in turn; their second parts follow both
     int64_t small;                    // first of the s x s matrices
     int rows, cols, s, l;
     int sp, lp;                       // s to a multiple of 256, l to a multiple of 64
@@ -80,10 +94,9 @@ struct Table {
     int n;
     int chunk;                        // units per CTA of the momentum pass
     int chunk_at[kMaxMats + 1];       // first CTA of every matrix
-    int sym_at[kMaxMats + 1];         // first tile of every matrix: symmetric products,
-    int apply_at[kMaxMats + 1];       // applications
-    int sym_width, apply_width;       // columns of their tiles
-    int64_t tiles;                    // bytes into the workspace: Tile[], symmetric products, then applications
+    int tiles_at[kLists][kMaxMats + 1];   // first tile of every matrix
+    int width[kLists];                // columns of the tiles
+    int64_t tiles;                    // bytes into the workspace: Tile[], list after list
     Mat m[kMaxMats];
 };
 
@@ -155,10 +168,10 @@ struct Norms {
     int* arrived;                     // CTAs of the momentum pass that are done
 };
 
-// The scale of X without its norm.  X as U * 2^q in fp16 has the accuracy of X * 2^kX for any q with which the norm stays
-// below 2^15 (no entry overflows) and the root mean square of the entries above 2^-13 (what falls below fp16's normal
-// numbers is rounded to 2^-25, and so by less than 2^-12 of that).  Between the two there is a factor of 2^28 / sqrt(r c),
-// 2^16 for 16 M entries, so the norm of 2048 entries tells q well enough.  Only entries that hide from the samples mislead
+// The scale of X without its norm.  X as U * 2^q in two fp16 parts is accurate enough for any q with which the norm stays
+// below 2^15 (no entry overflows) and the root mean square of the entries above 2^-6 (the second part ends at 2^-25, which
+// is 2^-19 of that, and five steps make of it 485 times as much at worst).  Between the two there is a factor of
+// 2^21 / sqrt(r c), 2^9 for 16 M entries, so the norm of 2048 entries tells q well enough.  Only entries that hide from the samples mislead
 // it; the momentum pass, which adds all of them up, sees that and has X written again.  The rest of the factor joins the
 // first Gram product (squared) and the first application.
 // Also: counters to zero, the list of tiles.
@@ -191,19 +204,19 @@ __global__ void __launch_bounds__(256) prepare_kernel(const __grid_constant__ Ta
         if (threadIdx.x == 0) {
             sum = 0.0;
             for (int w = 0; w < 8; ++w) sum += s_sum[w];
-            // |U| 2^q in the middle between sqrt(r c) 2^-13 and 2^15
-            const double bits = 0.25 * log2((double)size) + 1.0 - 0.5 * log2(sum * ((double)size / kSamples));
+            // |U| 2^q in the middle between sqrt(r c) 2^-6 and 2^15
+            const double bits = 0.25 * log2((double)size) + 4.5 - 0.5 * log2(sum * ((double)size / kSamples));
             norms.exponent[blockIdx.x] = bits > -126.0 && bits < 126.0 ? (int)rint(bits) : 0;
             norms.arrived[blockIdx.x] = 0;
         }
     }
     const int first = blockIdx.x * 256 + threadIdx.x, all = gridDim.x * 256;
     for (int w = first; w < kMaxPhases; w += all) phases[w] = 0;
-    const int n_sym = t.sym_at[t.n], n_apply = t.apply_at[t.n];
-    for (int w = first; w < n_sym + n_apply; w += all) {
-        const bool sym = w < n_sym;
-        const int k = sym ? w : w - n_sym;
-        const int* at = sym ? t.sym_at : t.apply_at;
+    const int ends[kLists] = {t.tiles_at[kLower][t.n], t.tiles_at[kWhole][t.n], t.tiles_at[kApply][t.n]};
+    for (int w = first; w < ends[kLower] + ends[kWhole] + ends[kApply]; w += all) {
+        const int list = w < ends[kLower] ? kLower : w < ends[kLower] + ends[kWhole] ? kWhole : kApply;
+        const int k = list == kLower ? w : list == kWhole ? w - ends[kLower] : w - ends[kLower] - ends[kWhole];
+        const int* at = t.tiles_at[list];
         const int j = find(at, t.n, k), tile = k - at[j];
         const Mat& q = t.m[j];
         Tile d{};
@@ -217,10 +230,10 @@ __global__ void __launch_bounds__(256) prepare_kernel(const __grid_constant__ Ta
         d.rows = q.rows;
         d.cols = q.cols;
         d.offset = q.offset;
-        if (sym) {
-            triangle(tile, kRows / t.sym_width, &d.ti, &d.tj);
+        const int mt = q.sp / kRows;
+        if (list == kLower) {
+            triangle(tile, kRows / t.width[kLower], &d.ti, &d.tj);
         } else {
-            const int mt = q.sp / kRows;
             d.ti = (uint16_t)(tile % mt);
             d.tj = (uint16_t)(tile / mt);
         }
@@ -261,8 +274,14 @@ struct UnitOf {
     }
 };
 
-// From there as fp16 in the tensor cores' order.
-__device__ __forceinline__ void store_image(uint8_t* to, const float (*s_u)[kUnit + 1]) {
+// Where the second parts of an X lie behind the first.
+__device__ __forceinline__ int64_t second_part(const Mat& m) { return 4 * (int64_t)m.sp * m.lp; }
+
+// What fp16 leaves of a value.
+__device__ __forceinline__ float rest(float v) { return v - __half2float(__float2half_rn(v)); }
+
+// From there as fp16 in the tensor cores' order; with `lo`, what that leaves of the values as well.
+__device__ __forceinline__ void store_image(uint8_t* to, uint8_t* lo, const float (*s_u)[kUnit + 1]) {
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
         const int row = (threadIdx.x >> 3) + k * 32, c8 = threadIdx.x & 7;
@@ -270,17 +289,23 @@ __device__ __forceinline__ void store_image(uint8_t* to, const float (*s_u)[kUni
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = s_u[row][c8 * 8 + j];
         *reinterpret_cast<uint4*>(to + in_unit(row, c8)) = pack8(v);
+        if (lo) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = rest(v[j]);
+            *reinterpret_cast<uint4*>(lo + in_unit(row, c8)) = pack8(v);
+        }
     }
 }
 
 // M <- mu M + G, U as X and its sum of squares (fp64: gradients may be tiny or huge), in one pass.  The last CTA of a matrix
-// to arrive adds the sums of all in their order.  66 M elements with bf16 gradients take 133 us, 0.92 of the copy rate
-// (with the norm from a pass of its own and X from a second one 110 + 100).  The loads of a unit are under way while the one
-// before it is stored: without that 181; CTAs that take eight neighbouring units each instead of going side by side 206.
+// to arrive adds the sums of all in their order.  66 M elements with bf16 gradients take 164 us, 0.86 of the copy rate (with
+// the first parts of X alone 133; the norm from a pass of its own and those from a second one 110 + 100).  The loads of a unit
+// are under way while the one before it is stored: without that 181 instead of 133; CTAs that take eight neighbouring units
+// each instead of going side by side 206.
 template <typename T>
 __global__ void __launch_bounds__(256, kMomentumCtas) momentum_kernel(const __grid_constant__ Table t, const T* __restrict__ grad,
                                                           float* __restrict__ momentum, float mu, int nesterov, float eps,
-                                                          int quads, double* __restrict__ partial, Norms norms,
+                                                          int quads, int parts, double* __restrict__ partial, Norms norms,
                                                           uint8_t* __restrict__ ws) {
     __shared__ float s_u[kUnit][kUnit + 1];
     __shared__ double s_sum[8];
@@ -352,7 +377,7 @@ __global__ void __launch_bounds__(256, kMomentumCtas) momentum_kernel(const __gr
         at.put(g, s_u);
         if (u + m.n_chunks < units) load(UnitOf(m, u + m.n_chunks, quads));   // under way while this unit is stored
         __syncthreads();
-        store_image(ws + at.image, s_u);
+        store_image(ws + at.image, parts == 2 ? ws + at.image + second_part(m) : nullptr, s_u);
         __syncthreads();
     }
 #pragma unroll
@@ -384,7 +409,7 @@ __global__ void __launch_bounds__(256, kMomentumCtas) momentum_kernel(const __gr
         // (zeros are zeros at any scale, and a NaN or an infinity makes X NaN)
         const double norm = sqrt(sum), stored = norm * (double)scale, inverse = 1.0 / (norm + (double)eps);
         const bool finite = norm < __longlong_as_double(0x7ff0000000000000ll);
-        const bool good = !finite || sum == 0.0 || (stored <= 32768.0 && stored >= sqrt((double)m.rows * m.cols) * (1.0 / 8192));
+        const bool good = !finite || sum == 0.0 || (stored <= 32768.0 && stored >= sqrt((double)m.rows * m.cols) * (1.0 / 64));
         norms.inverse[i] = (float)inverse;
         norms.factor[i] = !finite ? __int_as_float(0x7fffffff) : good ? (float)((double)(1 << kX) / (double)scale * inverse) : 1.0f;
         norms.again[i] = !good;
@@ -396,7 +421,7 @@ __global__ void __launch_bounds__(256, kMomentumCtas) momentum_kernel(const __gr
 template <typename T>
 __global__ void __launch_bounds__(256) again_kernel(const __grid_constant__ Table t, const T* __restrict__ grad,
                                                     const float* __restrict__ momentum, float mu, int nesterov, int quads,
-                                                    Norms norms, uint8_t* __restrict__ ws) {
+                                                    int parts, Norms norms, uint8_t* __restrict__ ws) {
     __shared__ float s_u[kUnit][kUnit + 1];
     __shared__ int s_again[kMaxMats];
     wait_prerequisites();
@@ -434,7 +459,7 @@ __global__ void __launch_bounds__(256) again_kernel(const __grid_constant__ Tabl
             __syncthreads();                                          // (s_u has been read)
             at.put(x, s_u);
             __syncthreads();
-            store_image(ws + at.image, s_u);
+            store_image(ws + at.image, parts == 2 ? ws + at.image + second_part(m) : nullptr, s_u);
         }
     }
 }
@@ -443,19 +468,21 @@ __global__ void __launch_bounds__(256) again_kernel(const __grid_constant__ Tabl
 
 // One phase of the chain: the same product for every matrix.
 struct Phase {
-    int8_t sym;                       // a symmetric product of s x s matrices (or the Gram product), or P X
+    int8_t sym;                       // a product of symmetric s x s matrices (or the Gram product), or P X
+    int8_t list;                      // its tiles
     int8_t left, right;               // s x s operands; left = -1: the Gram product of X; an application has P on its left
     int8_t plus, to;                  // matrix added times beta (-1: none); where the result goes
     int8_t x_in;                      // which of the two X buffers holds X
     int8_t last;                      // an application that writes bf16 into the caller's vector, not the next X
+    int8_t parts;                     // an application: fp16 parts of X
+    int8_t keep;                      // an application that keeps a second part of its result
     int8_t by_norm;                   // power of the factor of X in alpha: X is as the momentum pass has left it
     float alpha, beta, gamma;         // result = alpha (left right) + beta plus + gamma I
 };
 
 struct Phases {
     int n;
-    int sym_width, sym_tiles;         // columns of the tiles of symmetric products, their number; they come first
-    int apply_width, apply_tiles;
+    int width[kLists], tiles[kLists], first[kLists];      // columns of the tiles, their number, the first
     int drop;                         // (tests) this phase is not counted; -1: none
     unsigned long long wait_ns;       // limit of the waits between phases
     Phase p[kMaxPhases];
@@ -548,7 +575,7 @@ __global__ void __launch_bounds__(kChainThreads, 1) __cluster_dims__(2)
     const uint32_t tmem = s_tmem;
 
     const int n_pairs = gridDim.x / 2, first = blockIdx.x / 2;
-    const auto steps_of = [](const Tile& d, const Phase& p) { return p.sym && p.left < 0 ? d.lu : d.ku; };
+    const auto steps_of = [](const Tile& d, const Phase& p) { return p.sym ? p.left < 0 ? d.lu : d.ku : d.ku * p.parts; };
     if (warp == 0) {
         if (elect_one()) {
             int st = 0;
@@ -556,9 +583,9 @@ __global__ void __launch_bounds__(kChainThreads, 1) __cluster_dims__(2)
             bool ok = true;
             for (int f = 0; f < ph.n && ok; ++f) {
                 const Phase& p = ph.p[f];
-                const int width = p.sym ? ph.sym_width : ph.apply_width, units_b = width / 128, parts = width / 64;
-                const int total = p.sym ? ph.sym_tiles : ph.apply_tiles;
-                const Tile* list = tiles + (p.sym ? 0 : ph.sym_tiles);
+                const int width = ph.width[p.list], units_b = width / 128, parts = width / 64;
+                const int total = ph.tiles[p.list];
+                const Tile* list = tiles + ph.first[p.list];
                 bool waited = f == 0;
                 for (int i = first; i < total && ok; i += n_pairs) {
                     const Tile d = list[i];
@@ -581,7 +608,10 @@ __global__ void __launch_bounds__(kChainThreads, 1) __cluster_dims__(2)
                         ok = mbar_wait(smem_addr(&s_free[st]), (round & 1) ^ 1, &s_failed);
                         if (!ok) break;
                         if (rank == 0) mbar_expect_tx(bar, 2 * (2 + units_b) * kUnitBytes);
-                        const int ua = ua0 + k * d.spu, ub = ub0 + k * ub_step;
+                        // (the second part of X, behind both X, meets the same P)
+                        const bool lo = !p.sym && k >= d.ku;
+                        const int kk = lo ? k - d.ku : k;
+                        const int ua = ua0 + kk * d.spu, ub = ub0 + kk * ub_step + (lo ? 2 * d.spu * d.lu : 0);
                         tensor_load_2d_pair(a, &map, 0, ua * kUnit, bar);
                         tensor_load_2d_pair(a + kUnitBytes, &map, 0, (ua + 1) * kUnit, bar);
                         tensor_load_2d_pair(b, &map, 0, ub * kUnit, bar);
@@ -600,13 +630,13 @@ __global__ void __launch_bounds__(kChainThreads, 1) __cluster_dims__(2)
             for (int f = 0; f < ph.n && ok; ++f) {
                 const Phase& p = ph.p[f];
                 const bool sym = p.sym;
-                const int total = sym ? ph.sym_tiles : ph.apply_tiles;
-                const Tile* list = tiles + (sym ? 0 : ph.sym_tiles);
-                const uint32_t shape = f16_shape(kRows, sym ? ph.sym_width : ph.apply_width, !sym);
+                const int total = ph.tiles[p.list];
+                const Tile* list = tiles + ph.first[p.list];
+                const uint32_t shape = f16_shape(kRows, ph.width[p.list], !sym);
                 // (K-major operands move 32 bytes on along K, the MN-major B of an application sixteen rows of 128)
                 const uint32_t b_step = sym ? 32 : 2048, b_lead = sym ? 16 : kUnitBytes;
                 for (int i = first; i < total && ok; i += n_pairs, ++n) {
-                    const int steps = p.sym && p.left < 0 ? list[i].lu : list[i].ku;
+                    const int steps = steps_of(list[i], p);
                     const int buf = n & 1;
                     const uint32_t sums = tmem + buf * 256;
                     ok = __all_sync(0xffffffffu, mbar_wait(smem_addr(&s_taken[buf]), ((n >> 1) & 1) ^ 1, &s_failed));
@@ -636,14 +666,14 @@ __global__ void __launch_bounds__(kChainThreads, 1) __cluster_dims__(2)
         for (int f = 0; f < ph.n && ok; ++f) {
             const Phase& p = ph.p[f];
             const bool sym = p.sym, last = p.last, plus = p.plus >= 0;
-            const int width = sym ? ph.sym_width : ph.apply_width, parts = width / 64;
-            const int total = sym ? ph.sym_tiles : ph.apply_tiles;
-            const Tile* list = tiles + (sym ? 0 : ph.sym_tiles);
+            const int width = ph.width[p.list], parts = width / 64;
+            const int total = ph.tiles[p.list];
+            const Tile* list = tiles + ph.first[p.list];
             bool waited = f == 0;
             for (int i = first; i < total; i += n_pairs) {
                 const Tile d = list[i];
                 const int small = d.spu * d.spu, rb = d.ti * 4 + (int)rank * 2;
-                const bool mirror = sym && d.tj < d.ti * (kRows / width);
+                const bool mirror = p.list == kLower && d.tj < d.ti * (kRows / width);
                 const int base = sym ? d.small + p.to * small : p.x_in ? d.x[0] : d.x[1];
                 // part `cu` of the tile may be filled: its buffer has been read, and holds the 64 columns to add
                 const auto prepare = [&](int cu, int to) {
@@ -678,6 +708,9 @@ __global__ void __launch_bounds__(kChainThreads, 1) __cluster_dims__(2)
                             for (int u = 0; u < 2; ++u)
                                 bulk_store(ws + (int64_t)(base + (rb + u) * d.spu + cb) * kUnitBytes, img + (2 + u) * kUnitBytes,
                                            kUnitBytes);
+                        if (p.keep)
+                            bulk_store(ws + (int64_t)(base + (2 * d.lu + cb) * d.spu + rb) * kUnitBytes, img + 2 * kUnitBytes,
+                                       2 * kUnitBytes);
                         bulk_store_commit();
                     }
                     __syncwarp();
@@ -699,15 +732,16 @@ __global__ void __launch_bounds__(kChainThreads, 1) __cluster_dims__(2)
         for (int f = 0; f < ph.n && ok; ++f) {
             const Phase& p = ph.p[f];
             const bool sym = p.sym, last = p.last, plus = p.plus >= 0;
-            const int width = sym ? ph.sym_width : ph.apply_width, parts = width / 64;
-            const int total = sym ? ph.sym_tiles : ph.apply_tiles;
-            const Tile* list = tiles + (sym ? 0 : ph.sym_tiles);
+            const int width = ph.width[p.list], parts = width / 64;
+            const int total = ph.tiles[p.list];
+            const Tile* list = tiles + ph.first[p.list];
+            const bool keep = p.keep;
             const float beta = p.beta, gamma = p.gamma;
             for (int i = first; i < total; i += n_pairs, ++n) {
                 const Tile d = list[i];
                 const int buf = n & 1;
                 const int rb = d.ti * 4 + (int)rank * 2;              // first unit row of this CTA's part
-                const bool mirror = sym && d.tj < d.ti * (kRows / width), tall = d.rows > d.cols;
+                const bool mirror = p.list == kLower && d.tj < d.ti * (kRows / width), tall = d.rows > d.cols;
                 float alpha = p.alpha;
                 for (int k = 0; k < p.by_norm; ++k) alpha *= __ldg(factor + d.mat);
                 const int diagonal = d.ti * kRows + (int)rank * 128 + row - d.tj * width;     // the column on the diagonal
@@ -755,6 +789,11 @@ __global__ void __launch_bounds__(kChainThreads, 1) __cluster_dims__(2)
                                 }
                                 const uint4 packed = pack8(v);
                                 *at = packed;
+                                if (keep) {                           // (an application has no mirror: its place is free)
+#pragma unroll
+                                    for (int j = 0; j < 8; ++j) v[j] = rest(v[j]);
+                                    at[2 * kUnitBytes / 16] = pack8(v);
+                                }
                                 if (mirror) {
                                     const __half* hv = reinterpret_cast<const __half*>(&packed);
 #pragma unroll
@@ -833,19 +872,22 @@ __global__ void __launch_bounds__(kChainThreads, 1) __cluster_dims__(2)
 // ---------------------------------------------------------------------------------------------- small matrices
 //
 // Matrices with s <= 128 and l <= 2048: one cluster of CTAs per matrix does the whole update in one launch.  Every CTA
-// keeps its columns of X (up to 256: 64 KB) in shared memory from the first step to the last.  The only exchange between the CTAs is a sum per Gram matrix: each adds its share of the rows of all partial
+// keeps its columns of X (up to 256) from the first step to the last: the first parts (64 KB) in shared memory, the second in
+// tensor memory, from where they come into the place of squares that are done with for every application (4 us of a
+// call).  The only exchange between the CTAs is a sum per Gram matrix: each adds its share of the rows of all partial
 // Gram matrices through distributed shared memory, in the order of the CTAs, and hands the result to the others; the
 // s x s products that follow (0.8 us each) every CTA does for itself.
 // With few rows the rounding of the s x s matrices is the largest error, and products of second fp16 parts cost next to
-// nothing here.  With s <= 64 all of them are sums of two parts: two of 16 x 139 are off by 1.7e-3 of their norm, the rounding
-// to bf16, instead of 2.8e-3 with two parts of the B and their product only, and ResNet-20 takes 41 us instead of 45, because
-// the exchange moves 64 x 64.  Above, where a square is twice that, A and T have one part (100 x 333: 1.9e-3).
+// nothing here.  With s <= 64 all of them are sums of two parts: any rank of 64 x 576 is off by 1.7e-3 of its norm, the rounding
+// to bf16, and the exchange moves 64 x 64.  Above, where a square is twice that, A and T have one part (128 x 1152: 1.8e-3 to
+// 2.3e-3).
 
 constexpr int kSmallS = 128, kSmallUnits = 4, kSmallCluster = 8;      // units of columns per CTA, CTAs per matrix: at most
 constexpr int kSmallThreads = 512;
 constexpr int kSquareBytes = 4 * kUnitBytes;                          // 128 x 128 (with s <= 64: 128 x 64, half of it)
 constexpr int kSlabBytes = kSmallUnits * 2 * kUnitBytes;              // 128 x 256
 constexpr int kOutLine = kSmallUnits * kUnit + 2, kOutColumn = kSmallS + 2;   // bf16 per line of the result, wide or tall
+constexpr int kRests = 256;                                           // columns of tensor memory: sums, then second parts of X
 constexpr int kSquares = 5;                                           // (together larger than X's part in fp32)
 constexpr int kSmallSmem = kSquares * kSquareBytes + std::max(kSlabBytes, std::max(kSmallS * kOutLine, kSmallUnits * kUnit * kOutColumn) * 2) +
                            1024;
@@ -897,7 +939,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
     const Square sq_a = {sq(0), fine ? sq(1) : nullptr}, sq_b = fine ? Square{sq(2), sq(3)} : Square{sq(1), sq(2)},
                  sq_t = {fine ? sq(4) : sq(3), fine ? sq(5) : nullptr}, sq_b2 = fine ? Square{sq(4), sq(5)} : Square{sq(3), sq(4)},
                  sq_p = {sq(0), sq(1)};
-    if (warp == 0) tmem_alloc(&s_tmem, 256);
+    if (warp == 0) tmem_alloc(&s_tmem, 512);
     if (threadIdx.x == 0) {
         mbar_init(smem_addr(&s_done), 1);
         s_failed = 0;
@@ -956,19 +998,33 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
     for (uint32_t i = 0; i < ctas; ++i) sum += s_norm[i];
     const float scale = (float)(1.0 / (sqrt(sum) + (double)eps)) * (float)(1 << kX);
 
-    // ---- X, eight neighbours of a row at a time
-    for (int i = threadIdx.x; i < units * 8 * kSmallS; i += kSmallThreads) {
-        const int r = i & (kSmallS - 1), c8 = i >> 7;
-        float v8[8];
+    // ---- X: a thread has a row of a unit of columns, eight neighbours at a time.  The first parts go to the slab, the second
+    // wait in tensor memory behind the sums, two to a word.
+    const int row = (warp & 3) * 32 + lane, side = warp >> 2;         // row, unit of columns (quarter of a square's columns)
+    const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+    const auto put_x = [&](int o, float (&v)[8], uint32_t* lo) {
+        *reinterpret_cast<uint4*>(slab + (side * 2 + (row >> 6)) * kUnitBytes + in_unit(row & 63, o)) = pack8(v);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v8[j] = scale * held[r * by_row + (c8 * 8 + j) * by_col];
-        *reinterpret_cast<uint4*>(slab + ((c8 >> 3) * 2 + (r >> 6)) * kUnitBytes + in_unit(r & 63, c8 & 7)) = pack8(v8);
+        for (int j = 0; j < 8; ++j) v[j] = rest(v[j]);
+        *reinterpret_cast<uint4*>(lo) = pack8(v);
+    };
+    if (side < units) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            alignas(16) uint32_t lo[16];
+#pragma unroll
+            for (int o = 0; o < 4; ++o) {
+                float v8[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v8[j] = scale * held[row * by_row + (side * kUnit + h * 32 + o * 8 + j) * by_col];
+                put_x(h * 4 + o, v8, lo + o * 4);
+            }
+            tmem_store16(lanes + kRests + side * 32 + h * 16, lo);
+        }
     }
 
     // ---- products: one thread issues, then everybody takes its rows and columns of the sums
     int uses = 0;
-    const int row = (warp & 3) * 32 + lane, side = warp >> 2;         // row of the sums, quarter of their columns
-    const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
     const auto issue_and_wait = [&](auto products) {
         fence_async_shared();
         fence_before_sync();
@@ -1142,39 +1198,48 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
             scale_p = kP;
         }
 
-        // X <- P X on this CTA's columns
+        // X <- P X on this CTA's columns, the second parts of X from the squares that are done with
+        uint8_t* rests = sq(fine ? 4 : 3);
+        if (side < units) {
+            alignas(16) uint32_t lo[32];
+            tmem_load32(lanes + kRests + side * 32, lo);
+#pragma unroll
+            for (int o = 0; o < 8; ++o)
+                *reinterpret_cast<uint4*>(rests + (side * 2 + (row >> 6)) * kUnitBytes + in_unit(row & 63, o)) =
+                    *reinterpret_cast<const uint4*>(lo + o * 4);
+        }
         issue_and_wait([&] {
-            const uint32_t b = smem_addr(slab);
-            for (int k = 0; k < ku * 8 && units; ++k) {
-                const int q = k < ku * 4 ? k : k - ku * 4;
-                const uint32_t a = smem_addr(k < ku * 4 ? p.hi : p.lo);
-                mma_f16(tmem, swizzled_operand(a + (q >> 2) * 2 * kUnitBytes + (q & 3) * 32, 16, 1024),
-                        swizzled_operand(b + (q >> 2) * kUnitBytes + (q & 3) * 2048, 2 * kUnitBytes, 1024),
-                        f16_shape(kSmallS, units * kUnit, true), k > 0);
+            for (int t = 0; t < 3 && units; ++t) {                    // (not the product of both second parts)
+                const uint32_t a0 = smem_addr(t == 1 ? p.lo : p.hi), b0 = smem_addr(t == 2 ? rests : slab);
+                for (int k = 0; k < ku * 4; ++k)
+                    mma_f16(tmem, swizzled_operand(a0 + (k >> 2) * 2 * kUnitBytes + (k & 3) * 32, 16, 1024),
+                            swizzled_operand(b0 + (k >> 2) * kUnitBytes + (k & 3) * 2048, 2 * kUnitBytes, 1024),
+                            f16_shape(kSmallS, units * kUnit, true), t > 0 || k > 0);
             }
         });
         done += group;
         const bool last = done == steps;
         const float alpha = two(last ? -scale_p - kX : -scale_p);
         __nv_bfloat16* s_out = reinterpret_cast<__nv_bfloat16*>(slab);          // (X is done with)
-        for (int u = side; u < units; u += 4) {
+        if (side < units) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 uint32_t acc[32];
-                tmem_load32(lanes + u * kUnit + h * 32, acc);
+                tmem_load32(lanes + side * kUnit + h * 32, acc);
                 if (!last) {
+                    alignas(16) uint32_t lo[16];
 #pragma unroll
                     for (int o = 0; o < 4; ++o) {
                         float v[8];
 #pragma unroll
                         for (int j = 0; j < 8; ++j) v[j] = alpha * __uint_as_float(acc[o * 8 + j]);
-                        *reinterpret_cast<uint4*>(slab + (u * 2 + (row >> 6)) * kUnitBytes + in_unit(row & 63, h * 4 + o)) =
-                            pack8(v);
+                        put_x(h * 4 + o, v, lo + o * 4);
                     }
+                    tmem_store16(lanes + kRests + side * 32 + h * 16, lo);
                 } else {
 #pragma unroll
                     for (int j = 0; j < 32; ++j) {
-                        const int col = u * kUnit + h * 32 + j;
+                        const int col = side * kUnit + h * 32 + j;
                         s_out[tall ? col * kOutColumn + row : row * kOutLine + col] =
                             __float2bfloat16_rn(alpha * __uint_as_float(acc[j]));
                     }
@@ -1199,7 +1264,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
     }
     __syncthreads();
     cluster_sync();                                                   // nobody reads or writes this CTA's memory any more
-    if (warp == 0) tmem_free(tmem, 256);
+    if (warp == 0) tmem_free(tmem, 512);
 }
 
 __device__ int g_timeouts;
@@ -1212,7 +1277,7 @@ static int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 static int64_t lay_out(const int64_t* offsets, const int64_t* rows, const int64_t* cols, const int* order, int n,
                        int max_pairs, Table* t) {
     int64_t at = 0;
-    int64_t chunks = 0, units = 0, sym = 0, apply = 0;
+    int64_t chunks = 0, units = 0, all_tiles = 0;
     t->n = n;
     for (int k = 0; k < n; ++k) {
         Mat& m = t->m[k];
@@ -1237,38 +1302,37 @@ static int64_t lay_out(const int64_t* offsets, const int64_t* rows, const int64_
     }
     // Columns of a tile: 256 give the tensor cores two thirds of the operand traffic per operation, 128 give twice as many
     // tiles for few matrices.  A tile of 128 columns takes about 0.6 of the time of one of 256.
-    const auto tiles_of = [&](bool is_sym, int width) {
+    const auto tiles_of = [&](int list, int width) {
         int64_t all = 0;
         for (int k = 0; k < n; ++k) {
             const Mat& m = t->m[k];
             const int64_t mt = m.sp / kRows;
-            (is_sym ? t->sym_at : t->apply_at)[k] = (int)all;
-            all += is_sym ? mt * (mt + 1) / 2 * (kRows / width) : mt * ((m.lp + width - 1) / width);
+            t->tiles_at[list][k] = (int)all;
+            all += list == kApply ? mt * ((m.lp + width - 1) / width)
+                                  : (list == kLower ? mt * (mt + 1) / 2 : mt * mt) * (kRows / width);
         }
-        (is_sym ? t->sym_at : t->apply_at)[n] = (int)all;
+        t->tiles_at[list][n] = (int)all;
         return all;
     };
-    const auto choose = [&](bool is_sym, int* width) {
-        const auto rounds = [&](int64_t tiles) { return (double)((tiles + max_pairs - 1) / max_pairs); };
-        const int64_t wide = tiles_of(is_sym, 256), narrow = tiles_of(is_sym, 128);
-        *width = 0.6 * rounds(narrow) < rounds(wide) ? 128 : 256;
-        if (*width == 256) tiles_of(is_sym, 256);
-        return narrow;                                                // (room for either)
-    };
-    sym = choose(true, &t->sym_width);
-    apply = choose(false, &t->apply_width);
+    const auto rounds_of = [&](int64_t tiles) { return (double)((tiles + max_pairs - 1) / max_pairs); };
+    for (int list = 0; list < kLists; ++list) {
+        const int64_t wide = tiles_of(list, 256), narrow = tiles_of(list, 128);
+        t->width[list] = 0.6 * rounds_of(narrow) < rounds_of(wide) ? 128 : 256;
+        if (t->width[list] == 256) tiles_of(list, 256);
+        all_tiles += narrow;                                          // (room for either)
+    }
     t->chunk_at[n] = (int)chunks;
-    if (chunks > 0x7fffffff || sym + apply > 0x7fffffff) return -1;
+    if (chunks > 0x7fffffff || all_tiles > 0x7fffffff) return -1;
     at = up(at + chunks * 8, 1024);
     at = up(at + (5 * n + kMaxPhases) * 4, 1024);                     // norms, arrival counters
     t->tiles = at;
-    at = up(at + (sym + apply) * (int64_t)sizeof(Tile), kUnitBytes);
+    at = up(at + all_tiles * (int64_t)sizeof(Tile), kUnitBytes);
     for (int k = 0; k < n; ++k) {
         Mat& m = t->m[k];
         const int64_t big = (int64_t)m.sp * m.lp * 2;
         m.x[0] = at;
         m.x[1] = at + big;
-        m.small = at + 2 * big;
+        m.small = at + 4 * big;
         at = m.small + (int64_t)kSmallBuffers * m.sp * m.sp * 2;
     }
     return at;
@@ -1418,16 +1482,20 @@ static cudaError_t chain(const Table& t, const void* grad, float* momentum, floa
     // 16-byte accesses (where the matrix allows them)
     const int quads = (uintptr_t)grad % (4 * sizeof(T)) == 0 && (uintptr_t)momentum % 16 == 0;
     // (a plain launch: the first kernel waits for everything before it)
-    const int n_tiles = t.sym_at[t.n] + t.apply_at[t.n];
+    int n_tiles = 0, most_tiles = 0;
+    for (int list = 0; list < kLists; ++list) {
+        n_tiles += t.tiles_at[list][t.n];
+        most_tiles = std::max(most_tiles, t.tiles_at[list][t.n]);
+    }
     prepare_kernel<T><<<std::max(t.n, std::min(2 * kMostPairs, (n_tiles + 255) / 256)), 256, 0, s>>>(
         t, (const T*)grad, (const float*)momentum, mu, nesterov, norms, phases, ws);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
     sidco_internal::note_launch();
     if ((e = launch(momentum_kernel<T>, dim3(t.chunk_at[t.n]), 256, 0, s, t, (const T*)grad, momentum, mu, nesterov, eps, quads,
-                    partial, norms, ws)) != cudaSuccess)
+                    steps > 2 ? 2 : 1, partial, norms, ws)) != cudaSuccess)
         return e;
     if ((e = launch(again_kernel<T>, dim3(4 * kMostPairs), 256, 0, s, t, (const T*)grad, (const float*)momentum, mu, nesterov,
-                    quads, norms, ws)) != cudaSuccess)
+                    quads, steps > 2 ? 2 : 1, norms, ws)) != cudaSuccess)
         return e;
     // the workspace as rows of 128 bytes; a box is one unit (its bytes are in the tensor cores' order already)
     CUtensorMap map{};
@@ -1435,38 +1503,44 @@ static cudaError_t chain(const Table& t, const void* grad, float* momentum, floa
     Phases ph{};
     ph.wait_ns = g_wait_ns.load();
     ph.drop = g_drop_phase.load();
-    ph.sym_width = t.sym_width;
-    ph.sym_tiles = t.sym_at[t.n];
-    ph.apply_width = t.apply_width;
-    ph.apply_tiles = t.apply_at[t.n];
+    for (int list = 0, first = 0; list < kLists; ++list) {
+        ph.width[list] = t.width[list];
+        ph.tiles[list] = t.tiles_at[list][t.n];
+        ph.first[list] = first;
+        first += ph.tiles[list];
+    }
     const auto two = [](int k) { return ldexpf(1.0f, k); };
     int in = 0;
-    const auto sym = [&](int left, int right, int plus, int to, float alpha, float beta, float gamma) {
+    const auto sym = [&](int left, int right, int plus, int to, float alpha, float beta, float gamma, int list = kLower) {
         const int by_norm = ph.n == 0 ? 2 : 0;                        // (the first Gram product)
-        ph.p[ph.n++] = Phase{1, (int8_t)left, (int8_t)right, (int8_t)plus, (int8_t)to, (int8_t)in, 0, (int8_t)by_norm,
+        ph.p[ph.n++] = Phase{1, (int8_t)list, (int8_t)left, (int8_t)right, (int8_t)plus, (int8_t)to, (int8_t)in, 0, 1, 0, (int8_t)by_norm,
                              alpha, beta, gamma};
     };
     const auto polynomial = [&](int a, int to) {
         sym(a, a, a, to, kCc * two(kB - 2 * kA), kCb * two(kB - kA), kCa * two(kB));
     };
+    const auto group_at = [&](int done) { return steps == 1 || (done == 2 && steps % 2) ? 1 : 2; };
     for (int done = 0; done < steps;) {
-        const int group = steps == 1 || (done == 2 && steps % 2) ? 1 : 2;
+        const int group = group_at(done);
         sym(-1, -1, -1, kBufA, two(kA - 2 * kX), 0.0f, 0.0f);
         polynomial(kBufA, kBufB);
         if (group == 2) {
             sym(kBufB, kBufA, -1, kBufT, two(-kB), 0.0f, 0.0f);                       // B A
             sym(kBufT, kBufB, -1, kBufA2, two(-kB), 0.0f, 0.0f);                      // the next A = B A B
             polynomial(kBufA2, kBufT);
-            sym(kBufT, kBufB, -1, kBufP, two(kP - 2 * kB), 0.0f, 0.0f);
+            // (both factors are rounded, so their product is only nearly symmetric, and a mirror image of one half, taken
+            // for P, would turn the columns of an X of low rank: 512 x 2304 of rank 8 off by 6.0e-3 instead of 4.2e-3)
+            sym(kBufT, kBufB, -1, kBufP, two(kP - 2 * kB), 0.0f, 0.0f, kWhole);
         }
         done += group;
         const int scale_p = group == 2 ? kP : kB, last = done == steps, by_norm = done == group;
-        ph.p[ph.n++] = Phase{0, (int8_t)(group == 2 ? kBufP : kBufB), 0, -1, 0, (int8_t)in, (int8_t)last,
-                             (int8_t)by_norm, last ? two(-scale_p - kX) : two(-scale_p), 0.0f, 0.0f};
+        const int keep = !last && done + group_at(done) < steps;      // (what the last group takes has one part)
+        ph.p[ph.n++] = Phase{0, kApply, (int8_t)(group == 2 ? kBufP : kBufB), 0, -1, 0, (int8_t)in, (int8_t)last,
+                             (int8_t)(last ? 1 : 2), (int8_t)keep, (int8_t)by_norm, last ? two(-scale_p - kX) : two(-scale_p), 0.0f, 0.0f};
         in ^= 1;
     }
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(2 * std::min(max_pairs, std::max(ph.sym_tiles, ph.apply_tiles)));
+    cfg.gridDim = dim3(2 * std::min(max_pairs, most_tiles));
     cfg.blockDim = dim3(kChainThreads);
     cfg.dynamicSmemBytes = kChainSmem;
     cfg.stream = s;
