@@ -406,12 +406,17 @@ __global__ void __launch_bounds__(256, kMomentumCtas) momentum_kernel(const __gr
     if (threadIdx.x == 0) {
         sum = 0.0;
         for (int w = 0; w < 8; ++w) sum += s_sum[w];
-        // (zeros are zeros at any scale, and a NaN or an infinity makes X NaN)
+        // (zeros are zeros at any scale, NaN if eps is 0 as well; a NaN or an infinity makes X NaN)
         const double norm = sqrt(sum), stored = norm * (double)scale, inverse = 1.0 / (norm + (double)eps);
         const bool finite = norm < __longlong_as_double(0x7ff0000000000000ll);
         const bool good = !finite || sum == 0.0 || (stored <= 32768.0 && stored >= sqrt((double)m.rows * m.cols) * (1.0 / 64));
         norms.inverse[i] = (float)inverse;
-        norms.factor[i] = !finite ? __int_as_float(0x7fffffff) : good ? (float)((double)(1 << kX) / (double)scale * inverse) : 1.0f;
+        // (X = 0 / eps: the factor, squared, would be infinite for a small eps, and infinity times zero NaN)
+        const bool zero = sum == 0.0 && eps > 0.0f;
+        norms.factor[i] = !finite ? __int_as_float(0x7fffffff)
+                          : zero  ? 0.0f
+                          : good  ? (float)((double)(1 << kX) / (double)scale * inverse)
+                                  : 1.0f;
         norms.again[i] = !good;
     }
 }
