@@ -159,11 +159,27 @@ __device__ __forceinline__ void load4(const T* p, float (&x)[4]) {
     for (int i = 0; i < 4; ++i) x[i] = widen(reinterpret_cast<const T*>(w)[i]);
 }
 
+// 2^kX / (|U|_F + eps) as two factors, the first a power of two: the norm of an fp32 matrix may be as small as 2^-149, and
+// with it the quotient beyond fp32, or so large that the quotient would be subnormal.
+struct Factors {
+    float power, other;
+
+    __device__ __forceinline__ Factors(float p, float o) : power(p), other(o) {}
+    __device__ __forceinline__ explicit Factors(double norm_and_eps) {
+        const double s = (double)(1 << kX) / norm_and_eps;
+        const bool usual = s > 0.0 && s < __longlong_as_double(0x7ff0000000000000ll);
+        const int half = usual ? ilogb(s) >> 1 : 0;                   // (within -75 and 82)
+        power = __uint_as_float((uint32_t)(127 + half) << 23);
+        other = (float)(s * __longlong_as_double((long long)(1023 - half) << 52));
+    }
+    __device__ __forceinline__ float operator*(float u) const { return u * power * other; }
+};
+
 // What the passes know of every matrix.
 struct Norms {
     int* exponent;                    // X is first stored as U * 2^exponent
     float* factor;                    // and that times `factor` is X * 2^kX
-    float* inverse;                   // 1 / (|U|_F + eps)
+    float *power, *other;             // factors of 2^kX / (|U|_F + eps)
     int* again;                       // the estimate was too far off: X has to be written again
     int* arrived;                     // CTAs of the momentum pass that are done
 };
@@ -407,15 +423,17 @@ __global__ void __launch_bounds__(256, kMomentumCtas) momentum_kernel(const __gr
         sum = 0.0;
         for (int w = 0; w < 8; ++w) sum += s_sum[w];
         // (zeros are zeros at any scale, NaN if eps is 0 as well; a NaN or an infinity makes X NaN)
-        const double norm = sqrt(sum), stored = norm * (double)scale, inverse = 1.0 / (norm + (double)eps);
+        const double norm = sqrt(sum), stored = norm * (double)scale;
+        const Factors f(norm + (double)eps);
         const bool finite = norm < __longlong_as_double(0x7ff0000000000000ll);
         const bool good = !finite || sum == 0.0 || (stored <= 32768.0 && stored >= sqrt((double)m.rows * m.cols) * (1.0 / 64));
-        norms.inverse[i] = (float)inverse;
+        norms.power[i] = f.power;
+        norms.other[i] = f.other;
         // (X = 0 / eps: the factor, squared, would be infinite for a small eps, and infinity times zero NaN)
         const bool zero = sum == 0.0 && eps > 0.0f;
         norms.factor[i] = !finite ? __int_as_float(0x7fffffff)
                           : zero  ? 0.0f
-                          : good  ? (float)((double)(1 << kX) / (double)scale * inverse)
+                          : good  ? (float)((double)(1 << kX) / (double)scale / (norm + (double)eps))
                                   : 1.0f;
         norms.again[i] = !good;
     }
@@ -437,7 +455,7 @@ __global__ void __launch_bounds__(256) again_kernel(const __grid_constant__ Tabl
         if (!s_again[i]) continue;
         const Mat& m = t.m[i];
         const int units = (m.sp / kUnit) * (m.lp / kUnit);
-        const float scale = __ldcg(norms.inverse + i) * (float)(1 << kX);
+        const Factors scale(__ldcg(norms.power + i), __ldcg(norms.other + i));
         for (int u = blockIdx.x; u < units; u += gridDim.x) {
             const UnitOf at(m, u, quads);
             float x[4][4];
@@ -459,7 +477,7 @@ __global__ void __launch_bounds__(256) again_kernel(const __grid_constant__ Tabl
                     }
                 }
 #pragma unroll
-                for (int j = 0; j < 4; ++j) x[k][j] = (!momentum ? g[j] : nesterov ? fmaf(mu, v[j], g[j]) : v[j]) * scale;
+                for (int j = 0; j < 4; ++j) x[k][j] = scale * (!momentum ? g[j] : nesterov ? fmaf(mu, v[j], g[j]) : v[j]);
             }
             __syncthreads();                                          // (s_u has been read)
             at.put(x, s_u);
@@ -1001,7 +1019,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
     cluster_sync();
     sum = 0.0;
     for (uint32_t i = 0; i < ctas; ++i) sum += s_norm[i];
-    const float scale = (float)(1.0 / (sqrt(sum) + (double)eps)) * (float)(1 << kX);
+    const Factors scale(sqrt(sum) + (double)eps);
 
     // ---- X: a thread has a row of a unit of columns, eight neighbours at a time.  The first parts go to the slab, the second
     // wait in tensor memory behind the sums, two to a word.
@@ -1329,7 +1347,7 @@ static int64_t lay_out(const int64_t* offsets, const int64_t* rows, const int64_
     t->chunk_at[n] = (int)chunks;
     if (chunks > 0x7fffffff || all_tiles > 0x7fffffff) return -1;
     at = up(at + chunks * 8, 1024);
-    at = up(at + (5 * n + kMaxPhases) * 4, 1024);                     // norms, arrival counters
+    at = up(at + (6 * n + kMaxPhases) * 4, 1024);                     // norms, arrival counters
     t->tiles = at;
     at = up(at + all_tiles * (int64_t)sizeof(Tile), kUnitBytes);
     for (int k = 0; k < n; ++k) {
@@ -1482,8 +1500,9 @@ static cudaError_t chain(const Table& t, const void* grad, float* momentum, floa
     double* partial = reinterpret_cast<double*>(ws);
     const int64_t at = up((int64_t)t.chunk_at[t.n] * 8, 1024);
     int* words = reinterpret_cast<int*>(ws + at);
-    const Norms norms = {words, (float*)(words + t.n), (float*)(words + 2 * t.n), words + 3 * t.n, words + 4 * t.n};
-    unsigned* phases = (unsigned*)(words + 5 * t.n);
+    const Norms norms = {words,           (float*)(words + t.n), (float*)(words + 2 * t.n), (float*)(words + 3 * t.n),
+                         words + 4 * t.n, words + 5 * t.n};
+    unsigned* phases = (unsigned*)(words + 6 * t.n);
     // 16-byte accesses (where the matrix allows them)
     const int quads = (uintptr_t)grad % (4 * sizeof(T)) == 0 && (uintptr_t)momentum % 16 == 0;
     // (a plain launch: the first kernel waits for everything before it)

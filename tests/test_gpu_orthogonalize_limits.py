@@ -40,7 +40,7 @@ def near(got, want, tol=TOL):
     assert np.linalg.norm(got - want) <= tol * np.linalg.norm(want), np.linalg.norm(got - want) / np.linalg.norm(want)
 
 
-@pytest.mark.parametrize("eps", [1e-7, 1e-20])
+@pytest.mark.parametrize("eps", [1e-7, 1e-20, 1e-37])
 @pytest.mark.parametrize("mu", [None, 0.9])
 def test_a_zero_matrix_stays_zero(eps, mu):
     r = rng(1)
@@ -58,6 +58,26 @@ def test_a_zero_matrix_without_eps_is_not_a_number_as_the_formula_says():
     assert np.isnan(got[0][0]).all() and np.isnan(got[1][0]).all()
     near(*got[2])
     near(*got[3])
+
+
+@pytest.mark.parametrize("shape", [SMALL, LARGE, TALL])
+@pytest.mark.parametrize("scale", [1e-40, 1e-37, 1e-30, 1e-18, 1e15, 1e30, 3e36])
+@pytest.mark.parametrize("mu", [None, 0.9])
+def test_any_scale_without_eps(shape, scale, mu):
+    r = rng(3)
+    grads = [r.laplace(0, 1, shape) * scale, r.laplace(0, 1, shape)]
+    moms = [r.laplace(0, 1, shape) * scale, r.laplace(0, 1, shape)]
+    for got, want in call(grads, moms, mu, eps=0.0):
+        near(got, want)
+
+
+@pytest.mark.parametrize("shape", [(600, 700), (700, 300)])
+@pytest.mark.parametrize("scale", [1e-43, 1e-36, 1e-30, 1e30, 1e38])
+def test_any_scale_that_the_samples_miss(shape, scale):
+    g = np.zeros(shape)
+    g[np.ix_([3, 77, 140], [2, 30, 31, 90, 149])] = np.arange(1, 16).reshape(3, 5) % 7 / 7 * scale
+    for got, want in call([g, rng(4).standard_normal(shape)], eps=0.0):
+        near(got, want)
 
 
 @pytest.mark.parametrize("shape", [SMALL, LARGE, TALL])
