@@ -349,7 +349,9 @@ int sidco_mx4_mean(const uint8_t* codes_all, const uint8_t* scales_all, int n_wo
  *           at most 128 and a longer one of at most 2048 need none: the size may be 0, the pointer NULL.
  * stream    everything is enqueued here (one launch for small matrices, four for others, for up to 128 matrices of a kind);
  *           no synchronisation, no device allocation.  With matrices of both kinds the small ones run on a stream of the
- *           library that is forked from and joined to this one within the call (not while this one is being captured).
+ *           library that is forked from and joined to this one within the call (not while this one is being captured); each
+ *           of the first 16 streams of a device that call with both kinds gets one of its own, so that callers on several
+ *           streams do not wait for one another, later ones take the small matrices themselves.
  *           The kernel for larger matrices is launched cooperatively.
  */
 #define SIDCO_ORTHO_MAX_DIM   4194304

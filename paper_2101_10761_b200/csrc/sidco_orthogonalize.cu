@@ -1462,26 +1462,40 @@ static cudaError_t resident_pairs(int* n) {
     return e == cudaSuccess && *n < 1 ? cudaErrorInvalidConfiguration : e;
 }
 
-// A stream per device on which the small matrices run beside the momentum pass of the others (not beside their products: a
+// A stream on which the small matrices run beside the momentum pass of the others (not beside their products: a
 // cooperative launch waits for the SMs, 169 us become 214 with four matrices of 128 x 1152).  It takes over from the caller's
 // stream and hands back to it within one call, under the lock.  Its CTAs need whole SMs, which they get only if they come
 // first: the stream has priority, and the caller's goes on when this one has been reached (300 x 1000 beside five of
 // 64 x 576: 134 us instead of 140; 132 alone).
+// Every stream of a caller has one of its own: with one for all, a call would wait for whatever another caller's stream is
+// held up by.  They are kept (a stream's id is never given to another); callers' streams after the first kMostBesides
+// of a device take their small matrices themselves.
+constexpr int kMostBesides = 16;
+
 struct Beside {
+    unsigned long long of = 0;        // id of the caller's stream
     cudaStream_t stream = nullptr;
     cudaEvent_t fork = nullptr, ready = nullptr, join = nullptr;
     std::mutex lock;
 
-    cudaError_t begin(cudaStream_t from) {
+    cudaError_t create() {
         cudaError_t e;
         if (!stream) {
             int least, greatest;
             if ((e = cudaDeviceGetStreamPriorityRange(&least, &greatest)) != cudaSuccess) return e;
             if ((e = cudaStreamCreateWithPriority(&stream, cudaStreamNonBlocking, greatest)) != cudaSuccess) return e;
         }
-        if (!fork && (e = cudaEventCreateWithFlags(&fork, cudaEventDisableTiming)) != cudaSuccess) return e;
-        if (!join && (e = cudaEventCreateWithFlags(&join, cudaEventDisableTiming)) != cudaSuccess) return e;
-        if (!ready && (e = cudaEventCreateWithFlags(&ready, cudaEventDisableTiming)) != cudaSuccess) return e;
+        for (cudaEvent_t* event : {&fork, &ready, &join})
+            if (!*event && (e = cudaEventCreateWithFlags(event, cudaEventDisableTiming)) != cudaSuccess) return e;
+        return cudaSuccess;
+    }
+    cudaError_t begin(cudaStream_t from) {
+        cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;     // (another thread may be capturing)
+        cudaError_t e = cudaThreadExchangeStreamCaptureMode(&mode);
+        if (e != cudaSuccess) return e;
+        e = create();
+        const cudaError_t back = cudaThreadExchangeStreamCaptureMode(&mode);
+        if (e != cudaSuccess || (e = back) != cudaSuccess) return e;
         if ((e = cudaEventRecord(fork, from)) != cudaSuccess) return e;
         if ((e = cudaStreamWaitEvent(stream, fork, 0)) != cudaSuccess) return e;
         if ((e = cudaEventRecord(ready, stream)) != cudaSuccess) return e;
@@ -1492,6 +1506,26 @@ struct Beside {
         return e != cudaSuccess ? e : cudaStreamWaitEvent(to, join, 0);
     }
 };
+
+// The one of a caller's stream, null if there are no more.
+static cudaError_t beside_of(int dev, cudaStream_t s, Beside** found) {
+    static Beside all[64][kMostBesides];
+    static int used[64];
+    static std::mutex lock;
+    unsigned long long id;
+    const cudaError_t e = cudaStreamGetId(s, &id);
+    if (e != cudaSuccess) return e;
+    const std::lock_guard<std::mutex> hold(lock);
+    Beside *b = all[dev], *end = b + used[dev];
+    while (b < end && b->of != id) ++b;
+    if (b == end && used[dev] < kMostBesides) {
+        b->of = id;
+        end = b + 1;
+        ++used[dev];
+    }
+    *found = b < end ? b : nullptr;
+    return cudaSuccess;
+}
 
 template <typename T>
 static cudaError_t chain(const Table& t, const void* grad, float* momentum, float mu, int nesterov, int steps, float eps,
@@ -1681,17 +1715,19 @@ static int orthogonalize(const void* grad, int grad_type, float* momentum, float
     // (a stream that is being captured keeps to itself: a graph being built and a running call must not meet on a stream)
     cudaStreamCaptureStatus capture;
     if ((e = cudaStreamIsCapturing(s, &capture)) != cudaSuccess) return (int)e;
-    const bool both = !small.empty() && !order.empty() && capture == cudaStreamCaptureStatusNone;
-    static Beside beside[64];
-    std::unique_lock<std::mutex> hold(beside[dev].lock, std::defer_lock);
-    if (both) {
-        hold.lock();
-        if ((e = beside[dev].begin(s)) != cudaSuccess) return (int)e;
-        e = run_small(beside[dev].stream);
+    Beside* beside = nullptr;
+    if (!small.empty() && !order.empty() && capture == cudaStreamCaptureStatusNone &&
+        (e = beside_of(dev, s, &beside)) != cudaSuccess)
+        return (int)e;
+    std::unique_lock<std::mutex> hold;
+    if (beside) {
+        hold = std::unique_lock<std::mutex>(beside->lock);
+        if ((e = beside->begin(s)) != cudaSuccess) return (int)e;
+        e = run_small(beside->stream);
     } else if (!small.empty()) {
         e = run_small(s);
     }
-    if (e != cudaSuccess && !both) return (int)e;
+    if (e != cudaSuccess && !beside) return (int)e;
     std::vector<Table> t(1);
     for (size_t from = 0; from < order.size() && e == cudaSuccess; from += kMaxMats) {
         lay_out(offsets, rows, cols, order.data() + from, (int)std::min<size_t>(kMaxMats, order.size() - from),
@@ -1704,8 +1740,8 @@ static int orthogonalize(const void* grad, int grad_type, float* momentum, float
         else
             e = chain<__half>(t[0], grad, momentum, mu, nesterov, steps, eps, out_bf16, ws, need, max_pairs, timeouts, s);
     }
-    if (both) {                              // (also after an error: what was forked is joined)
-        const cudaError_t r = beside[dev].end(s);
+    if (beside) {                            // (also after an error: what was forked is joined)
+        const cudaError_t r = beside->end(s);
         if (e == cudaSuccess) e = r;
     }
     return (int)e;

@@ -106,6 +106,64 @@ def test_non_finite_matrices_leave_the_others_alone(bad, mu):
         near(*got[i])
 
 
+def test_callers_on_two_streams_do_not_wait_for_each_other():
+    """A call with matrices of both kinds behind a stream that is held up must not hold up a call on another stream.  (Of four
+    pairs of streams: one pair, or what the library forks from it, may share a queue of the hardware.)"""
+    import torch
+    from paper_2101_10761_b200 import binding as B
+    rows, cols, offsets = [64, 300, 16], [576, 200, 27], [0, 36864, 96864]
+    d = 96864 + 432
+    need = B.sidco_orthogonalize_workspace_bytes(rows, cols)
+    grad = torch.randn(d, device="cuda")
+    apart = 0
+    for _ in range(4):
+        spaces = [torch.empty(need, dtype=torch.uint8, device="cuda") for _ in range(2)]
+        outs = [torch.zeros(d, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+        streams = [torch.cuda.Stream() for _ in range(2)]
+        torch.cuda.synchronize()
+
+        def step(i):
+            B.sidco_orthogonalize(grad, None, 0, False, offsets, rows, cols, 5, outs[i], spaces[i], need, stream=streams[i])
+        for i in (0, 1):                                       # (what the first call of a stream sets up)
+            step(i)
+        torch.cuda.synchronize()
+        for o in outs:
+            o.zero_()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(streams[0]):
+            torch.cuda._sleep(1_000_000_000)                   # cycles: about half a second
+        step(0)
+        step(1)
+        done = [torch.cuda.Event() for _ in range(2)]
+        for e, s in zip(done, streams):
+            e.record(s)
+        done[1].synchronize()
+        apart += not done[0].query()
+        torch.cuda.synchronize()
+        assert outs[1].any() and torch.equal(outs[0], outs[1])
+    assert apart, "the second stream always waited for the first"
+
+
+def test_many_streams_one_after_the_other():
+    """More streams than the library keeps streams of its own for."""
+    import torch
+    from paper_2101_10761_b200 import binding as B
+    rows, cols, offsets = [64, 300], [576, 200], [0, 36864]
+    need = B.sidco_orthogonalize_workspace_bytes(rows, cols)
+    grad = torch.randn(96864, device="cuda")
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    want = torch.zeros(96864, dtype=torch.bfloat16, device="cuda")
+    B.sidco_orthogonalize(grad, None, 0, False, offsets, rows, cols, 5, want, ws, need)
+    torch.cuda.synchronize()
+    for _ in range(40):
+        s = torch.cuda.Stream()
+        out = torch.zeros_like(want)
+        s.wait_stream(torch.cuda.current_stream())
+        B.sidco_orthogonalize(grad, None, 0, False, offsets, rows, cols, 5, out, ws, need, stream=s)
+        s.synchronize()
+        assert torch.equal(out, want)
+
+
 FIRST = r'''
 import sys
 sys.path.insert(0, %r)
