@@ -222,7 +222,7 @@ __global__ void __launch_bounds__(256) dequantize_kernel(const uint8_t* __restri
     for (int u = 0; u < kDequantU; ++u) {
         const int o = o0 + u * lanes;
         c[u] = o < octs ? from[o] : 0u;
-        b[u] = o < octs ? scale[(o >> 4) * kTileBytes + ((o >> 2) & 3)] : 0u;
+        b[u] = o < octs ? scale[scale_of_oct(o)] : 0u;
     }
 #pragma unroll
     for (int u = 0; u < kDequantU; ++u) {

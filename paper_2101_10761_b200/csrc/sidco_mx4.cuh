@@ -28,6 +28,11 @@ __host__ __device__ constexpr int scale_in_tile(int row, int block) {
     return (row & 31) * 16 + ((row >> 5) & 3) * 4 + (block & 3);
 }
 
+// From the first scale of a row to that of its eight neighbours `oct`: 64 bits, a row may have 2^31 columns.
+__host__ __device__ constexpr int64_t scale_of_oct(int64_t oct) {
+    return (oct >> 4) * kTileBytes + ((oct >> 2) & (kTileBlocks - 1));
+}
+
 // Scale byte from the bits of the largest magnitude of a block.
 __device__ __forceinline__ uint32_t scale_byte(uint32_t max_bits) {
     const uint32_t ex = max_bits >> 23;
