@@ -8,6 +8,7 @@ from __future__ import annotations
 from typing import List, Optional, Sequence, Tuple
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding as B
 
@@ -50,7 +51,11 @@ def matmul(a: Quantized, b: Quantized, m: int, n: int, k: int, dtype: torch.dtyp
 
 
 class _Linear(torch.autograd.Function):
-    """Y = X W^T; the gradients are those of the product of the quantised operands (straight through the rounding)."""
+    """Y = X W^T of operands quantised along their rows, the axis of the sums.
+
+    The gradients pass straight through the rounding: dX = dY W and dW = dY^T X, with all three quantised along the axis of
+    these sums, so X and W by their columns.  They differ from the derivatives of the computed Y by the two roundings.  There
+    are no second derivatives: a graph through the backward pass raises."""
 
     @staticmethod
     def forward(ctx, x, weight):
@@ -64,6 +69,7 @@ class _Linear(torch.autograd.Function):
         return matmul(x_row, w_row, m, n, k, x.dtype)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         m, n, k = ctx.sizes
         saved = list(ctx.saved_tensors)
