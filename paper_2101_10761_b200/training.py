@@ -36,9 +36,22 @@ def quantize(x: torch.Tensor, rowwise: bool = True, transposed: bool = True
     return r, t
 
 
+def _check(name: str, form: Quantized, rows: int, cols: int, device) -> None:
+    """The buffers of a quantised [rows, cols] lie on `device` and are as large as the kernels read."""
+    for what, t, least in zip(("codes", "scales"), form, (B.sidco_mx4_code_bytes(rows, cols),
+                                                          B.sidco_mx4_scale_bytes(rows, cols))):
+        if t.device != device or t.dtype != torch.uint8 or not t.is_contiguous() or t.numel() < least:
+            raise ValueError(f"the {what} of {name} must be {least} contiguous bytes on {device} for [{rows}, {cols}], got "
+                             f"{tuple(t.shape)} of {t.dtype} on {t.device}")
+
+
 def matmul(a: Quantized, b: Quantized, m: int, n: int, k: int, dtype: torch.dtype = torch.bfloat16,
            out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """A [m, k] B [n, k]^T of quantised matrices as a new [m, n], or added to `out`."""
+    _check("a", a, m, k, a[0].device)
+    _check("b", b, n, k, a[0].device)
+    if out is not None and out.device != a[0].device:
+        raise ValueError(f"out is on {out.device}, the operands on {a[0].device}")
     with torch.cuda.device(a[0].device):
         if out is None:
             c = torch.empty(m, n, dtype=dtype, device=a[0].device)

@@ -17,3 +17,30 @@ def test_a_penalty_on_the_gradient_raises_instead_of_counting_nothing(monkeypatc
     assert torch.allclose(dx, 2 * (x @ w.T) @ w) and torch.allclose(dw, 2 * (x @ w.T).T @ x)
     with pytest.raises(RuntimeError, match="once_differentiable"):
         dx.square().sum().backward()
+
+
+def form(rows, cols, device="meta"):
+    from paper_2101_10761_b200 import binding as B
+    return (torch.empty(B.sidco_mx4_code_bytes(rows, cols), dtype=torch.uint8, device=device),
+            torch.empty(B.sidco_mx4_scale_bytes(rows, cols), dtype=torch.uint8, device=device))
+
+
+@pytest.mark.parametrize("m, n, k", [(41, 20, 33), (40, 21, 33), (40, 20, 65), (200, 20, 33), (40, 200, 33)])
+def test_product_refuses_sizes_that_its_operands_do_not_have(m, n, k):
+    """Operands of [40, 33] and [20, 33] (on the meta device: nothing may be launched)."""
+    with pytest.raises(ValueError, match="contiguous bytes"):
+        T.matmul(form(40, 33), form(20, 33), m, n, k)
+
+
+def test_product_refuses_other_buffers():
+    a, b = form(40, 33), form(20, 33)
+    with pytest.raises(ValueError, match="scales of b"):
+        T.matmul(a, (b[0], b[1][:-1]), 40, 20, 33)
+    with pytest.raises(ValueError, match="codes of a"):
+        T.matmul((a[0].float(), a[1]), b, 40, 20, 33)
+    with pytest.raises(ValueError, match="codes of a"):
+        T.matmul((torch.empty(2 * a[0].numel(), dtype=torch.uint8, device="meta")[::2], a[1]), b, 40, 20, 33)
+    with pytest.raises(ValueError, match="codes of b"):
+        T.matmul(a, form(20, 33, "cpu"), 40, 20, 33)
+    with pytest.raises(ValueError, match="out is on"):
+        T.matmul(a, b, 40, 20, 33, out=torch.zeros(40, 20))
