@@ -124,6 +124,8 @@ class OrthogonalizedUpdate:
         """The update (bf16, flat) for a flat gradient; the caller scales and subtracts it."""
         if grad.numel() < self.momentum.numel() or not grad.is_contiguous():
             raise ValueError("the gradient must be a contiguous flat vector over all matrices")
+        if grad.device != self.momentum.device:
+            raise ValueError(f"the gradient is on {grad.device}, the momentum on {self.momentum.device}")
         with torch.cuda.device(self.momentum.device):
             B.sidco_orthogonalize(grad, self.momentum, self.mu, self.nesterov, self.offsets, self.rows, self.cols,
                                   self.steps, self.update, self.workspace, self.workspace.numel())

@@ -44,3 +44,9 @@ def test_product_refuses_other_buffers():
         T.matmul(a, form(20, 33, "cpu"), 40, 20, 33)
     with pytest.raises(ValueError, match="out is on"):
         T.matmul(a, b, 40, 20, 33, out=torch.zeros(40, 20))
+
+
+def test_optimizer_object_refuses_a_gradient_from_elsewhere():
+    opt = T.OrthogonalizedUpdate([(4, 5)], device="meta")
+    with pytest.raises(ValueError, match="momentum on meta"):
+        opt.step(torch.zeros(20))
