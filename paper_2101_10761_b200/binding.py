@@ -8,6 +8,7 @@ built (``python -m paper_2101_10761_b200.build``): there is no fallback path.
 from __future__ import annotations
 
 import ctypes as C
+import operator
 import os
 from typing import Optional, Sequence
 
@@ -158,7 +159,7 @@ def _ptr(x) -> Optional[int]:
     try:
         return x.data_ptr()
     except AttributeError:
-        return x.ctypes.data if isinstance(x, np.ndarray) else int(x)
+        return x.ctypes.data if isinstance(x, np.ndarray) else operator.index(x)
 
 
 def _offsets(seg_offsets: Sequence[int]):
