@@ -109,7 +109,7 @@ __device__ __forceinline__ void bulk_store(void* dst, uint32_t src, uint32_t byt
     asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(src), "r"(bytes) : "memory");
 }
 
-// A box from shared memory into a tensor, or added to it (fp32; subnormal sums become zero); what lies outside is left out.
+// A box from shared memory into a tensor, or added to it (fp32; subnormal numbers are kept); what lies outside is left out.
 __device__ __forceinline__ void tensor_store_2d(const void* map, int x, int y, uint32_t src) {
     asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y),
                  "r"(src)
