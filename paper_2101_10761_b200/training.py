@@ -57,7 +57,7 @@ def matmul(a: Quantized, b: Quantized, m: int, n: int, k: int, dtype: torch.dtyp
             c = torch.empty(m, n, dtype=dtype, device=a[0].device)
             B.sidco_mx4_matmul(*a, *b, m, n, k, c, n)
             return c
-        if out.shape != (m, n) or out.stride(1) != 1 or (m > 1 and out.stride(0) < n):
+        if out.shape != (m, n) or (n > 1 and out.stride(1) != 1) or (m > 1 and out.stride(0) < n):
             raise ValueError(f"out must be [{m}, {n}] with contiguous rows")
         B.sidco_mx4_matmul(*a, *b, m, n, k, out, max(out.stride(0), n), add=True)
         return out

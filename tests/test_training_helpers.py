@@ -1,4 +1,6 @@
 """What the layer and the optimiser object refuse, on the CPU."""
+import contextlib
+
 import pytest
 import torch
 
@@ -50,3 +52,15 @@ def test_optimizer_object_refuses_a_gradient_from_elsewhere():
     opt = T.OrthogonalizedUpdate([(4, 5)], device="meta")
     with pytest.raises(ValueError, match="momentum on meta"):
         opt.step(torch.zeros(20))
+
+
+def test_product_takes_a_single_column_whatever_its_second_stride(monkeypatch):
+    """(m, 1) with strides (1, m), as the transpose of a row has: its rows have one element each."""
+    seen = []
+    monkeypatch.setattr(T.B, "sidco_mx4_matmul", lambda *a, **k: seen.append(a[8]))
+    monkeypatch.setattr(T.torch.cuda, "device", lambda d: contextlib.nullcontext())
+    out = torch.zeros(1, 40, device="meta").T
+    assert out.stride() == (1, 40)
+    assert T.matmul(form(40, 33), form(1, 33), 40, 1, 33, out=out) is out and seen == [1]
+    with pytest.raises(ValueError, match="contiguous rows"):
+        T.matmul(form(40, 33), form(2, 33), 40, 2, 33, out=torch.zeros(2, 40, device="meta").T)
