@@ -2,7 +2,8 @@
 
 libsidco.so is the product.  Two more builds of the same sources exist for tests and profiling:
 libsidco_profile.so (-DSIDCO_PROFILE: device timestamps at phase boundaries) and libsidco_check.so
-(-DSIDCO_BOUNDS_CHECK: every index into a caller or workspace buffer is range-checked on the device).
+(-DSIDCO_BOUNDS_CHECK: every index of the sparsifier into a caller or workspace buffer is range-checked on the device; the
+aggregation, the reference points and the matrix operators are the same in all three).
 """
 from __future__ import annotations
 

@@ -9,7 +9,9 @@
 // conversions per eight elements.  Measured (share of the copy rate of 6549 GB/s on the bytes that have to move):
 //   compress  25.6 M bf16 gradients: 42 us, 269 MB, 0.98: bound by memory
 //   mean      8 x 25.6 M: 38 us, 211 MB, 0.84: four fifths of the issue slots are busy with conversions and sums
-//   quantize  10000 x 1500 fp32, both forms: 17 us, 76 MB, 0.68; reading one form back to bf16: 9 us: both bound by issue
+//   quantize  10000 x 1500 fp32, both forms: 17 us, 76 MB, 0.68: bound by neither memory nor issue (0.6 of the slots): a CTA
+//             loads, then converts both forms, and has no other loads under way meanwhile
+//   reading one form of it back to bf16: 9 us, 38 MB, 0.65: three quarters of the issue slots are busy with conversions
 // Small calls take 3 to 4 us on the device, less than the host needs to launch them; every kernel may be set up under the
 // end of the one before.
 #include <cuda_runtime.h>

@@ -587,6 +587,9 @@ static int matmul_typed(const Operands& o, Args a, cudaStream_t s) {
     if ((e = cudaGetSymbolAddress((void**)&a.timeouts, g_timeouts)) != cudaSuccess) return (int)e;
     const int64_t tiles_m = (a.m + kPairTile - 1) / kPairTile, tiles_n = (a.n + kPairTile - 1) / kPairTile;
     int rc;
+    // Pairs of CTAs from as many tiles on as there are pairs.  Measured on both sides (us, pairs / split): 40 tiles, K = 256
+    // 5.4 / 9.5, K = 8192 19.1 / 22.7; 72 tiles 5.9 / 9.6 and 19.7 / 23.9; 80 tiles (two rounds) 7.4 / 15.3 and 33.7 / 41.2;
+    // 150 tiles 9.8 / 24.0 and 48.2 / 61.1.  So the line might lie at 40 tiles or lower; below that it was not measured.
     if (tiles_m * tiles_n >= max_pairs && a.m > 64 && a.n > 64) {
         if (tiles_m * tiles_n > 0x7fffffff / 2) return SIDCO_E_SIZE;
         CUtensorMap map_a, map_b, map_sa, map_sb, map_c{};

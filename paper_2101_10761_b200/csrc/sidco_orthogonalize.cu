@@ -1466,7 +1466,7 @@ static cudaError_t resident_pairs(int* n) {
 // cooperative launch waits for the SMs, 169 us become 214 with four matrices of 128 x 1152).  It takes over from the caller's
 // stream and hands back to it within one call, under the lock.  Its CTAs need whole SMs, which they get only if they come
 // first: the stream has priority, and the caller's goes on when this one has been reached (300 x 1000 beside five of
-// 64 x 576: 134 us instead of 140; 132 alone).
+// 64 x 576: 128 us, 174 one after the other; 126 alone).
 // Every stream of a caller has one of its own: with one for all, a call would wait for whatever another caller's stream is
 // held up by.  They are kept (a stream's id is never given to another); callers' streams after the first kMostBesides
 // of a device take their small matrices themselves.
