@@ -98,7 +98,7 @@ def mx4_linear(x: torch.Tensor, weight: torch.Tensor) -> torch.Tensor:
     """x [..., k] times weight [n, k]^T with 4-bit operands in the forward and both backward products."""
     if x.shape[-1] != weight.shape[1]:
         raise ValueError(f"x has {x.shape[-1]} columns, weight {weight.shape[1]}")
-    y = _Linear.apply(x.reshape(-1, x.shape[-1]), weight)
+    y = _Linear.apply(x.reshape(x.shape[:-1].numel(), x.shape[-1]), weight)
     return y.reshape(*x.shape[:-1], weight.shape[0])
 
 

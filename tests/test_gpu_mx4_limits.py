@@ -41,3 +41,16 @@ def test_subnormal_products_and_sums_are_kept(m, n, k, ldc):
         want = c0.astype(np.float64)
         want[:, :n] = want[:, :n] * add - 2.0 ** (exponent - 63)
         assert np.array_equal(c.cpu().numpy().astype(np.float64), want)
+
+
+@pytest.mark.parametrize("shape", [(3, 0), (2, 3, 0), (0,), (0, 5), (5,)])
+def test_linear_layer_of_empty_sums_and_of_a_single_row(shape):
+    import torch
+    from paper_2101_10761_b200.training import mx4_linear
+    x = torch.ones(shape, device="cuda").requires_grad_()
+    w = torch.ones(4, shape[-1], device="cuda").requires_grad_()
+    y = mx4_linear(x, w)
+    assert y.shape == shape[:-1] + (4,) and (y == shape[-1]).all()
+    y.sum().backward()
+    assert x.grad.shape == x.shape and (x.grad == 4).all()
+    assert w.grad.shape == w.shape and (w.grad == x[..., :1].numel()).all()
