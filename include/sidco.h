@@ -61,6 +61,9 @@ extern "C" {
 #define SIDCO_T_F32  0
 #define SIDCO_T_BF16 1
 #define SIDCO_T_F16  2
+/* types of tokens and labels */
+#define SIDCO_T_I32  3
+#define SIDCO_T_I64  4
 
 /* per-segment status bits */
 #define SIDCO_ST_NONFINITE  1   /* a magnitude was NaN/Inf: nothing is selected in the segment */
@@ -361,6 +364,63 @@ int64_t sidco_orthogonalize_workspace_bytes(const int64_t* rows, const int64_t* 
 int sidco_orthogonalize(const void* grad, int grad_type, float* momentum, float mu, int nesterov, const int64_t* offsets,
                         const int64_t* rows, const int64_t* cols, int n_mats, int steps, float eps, uint16_t* out_bf16,
                         void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The two ends of a language model's training step: lookup of the tokens' rows and its gradient, dropout, and the cross
+ * entropy of the output projection with its gradients.  Everything is enqueued on `stream`; nothing is allocated or
+ * synchronised, no state is kept, and the calls may be captured in a graph.  Results do not depend on how the work is
+ * split: no atomic additions of floating-point numbers.
+ *
+ * Dropout.  Element i of a tensor (rows one behind the other, without what may lie between them) is dropped if its random
+ * word is below round(p * 2^32), and multiplied by 1 / (1 - p) otherwise.  The word is number i % 4 of
+ * Philox4x32-10(counter = (i / 4, call + *step), key = seed), the low half of each 64-bit number first: a function of the
+ * position, so that the backward pass draws the same mask again.  A dropped element is zero whatever it was, NaN included.
+ *   p     in [0, 1]; below 2^-33 nothing is dropped.
+ *   call  number of the call under this seed; tensors with different numbers have independent masks.
+ *   step  device, uint64, 8-byte aligned, or NULL (0): added to call when the kernel runs, for captured graphs, which are
+ *         replayed with the same arguments.
+ */
+
+/*
+ * sidco_dropout - out = dropout(x) (+ residual).
+ *
+ * x, residual, out   device, type[n]; residual may be NULL; out may be x or residual, but not overlap them in part
+ *                    (SIDCO_E_ALIAS).  16-byte aligned buffers take the vector path.     n <= 2^40.
+ * The sum is taken in fp32 and rounded once.  Backward: the same call on dy without the residual, whose gradient is dy.
+ */
+int sidco_dropout(const void* x, int type, int64_t n, float p, uint64_t seed, uint64_t call, const uint64_t* step,
+                  const void* residual, void* out, void* stream);
+
+/*
+ * sidco_embedding - out[i] = scale * dropout(table[tokens[i]]), rounded once.
+ *
+ * table    device, table_type[vocab][ld], ld >= cols.          tokens  device, token_type[n] (SIDCO_T_I32 or SIDCO_T_I64).
+ * out      device, out_type[n][ldo], ldo >= cols; must not overlap table or tokens.  Elements behind a row's cols are left.
+ * A negative token is padding: its row is zero.  So is that of a token >= vocab, which is reported:
+ * status   device, int32, optional (NULL to ignore): cleared on `stream`, then SIDCO_EMBEDDING_ST_TOKEN if there was one.
+ * n, vocab <= 2^31 - 2^16, cols <= 2^24.
+ */
+#define SIDCO_EMBEDDING_ST_TOKEN 1
+int sidco_embedding(const void* table, int table_type, int64_t vocab, int64_t cols, int64_t ld, const void* tokens,
+                    int token_type, int64_t n, float scale, float p, uint64_t seed, uint64_t call, const uint64_t* step,
+                    void* out, int out_type, int64_t ldo, int32_t* status, void* stream);
+
+/*
+ * sidco_embedding_grad - gradient of the table: row v = scale * (sum over i with tokens[i] = v of dropout(dy[i])).
+ *
+ * The sum is taken in fp32 in an order that depends on the tokens alone, and rounded once.  Without `add` all rows of
+ * dtable are written (zeros where a token did not occur); with it the sums are added to the rows of the tokens that occur
+ * and the others are left as they are.  Rows of dy whose token is negative or >= vocab are not read.
+ *
+ * dy        device, dy_type[n][ld_dy].       dtable  device, dtable_type[vocab][ldd]; must not overlap dy or tokens.
+ * workspace device, 256-byte aligned, at least sidco_embedding_grad_workspace_bytes(n, vocab, cols) bytes; caller-owned,
+ *           nothing is kept in it between calls; not to be shared by calls that overlap.
+ */
+int64_t sidco_embedding_grad_workspace_bytes(int64_t n, int64_t vocab, int64_t cols);       /* negative: SIDCO_E_SIZE */
+int sidco_embedding_grad(const void* dy, int dy_type, int64_t ld_dy, const void* tokens, int token_type, int64_t n,
+                         int64_t vocab, int64_t cols, float scale, float p, uint64_t seed, uint64_t call,
+                         const uint64_t* step, void* dtable, int dtable_type, int64_t ldd, int add, void* workspace,
+                         size_t workspace_bytes, void* stream);
 
 /* How many CTAs of the product kernels (sidco_mx4_matmul, sidco_orthogonalize) have given up a bounded wait since the
  * library was loaded; anything but 0 means that an output is incomplete.  Negative: a CUDA error.  Synchronises the

@@ -49,6 +49,7 @@ EXPORTS = [
     "sidco_mx4_code_bytes", "sidco_mx4_scale_bytes", "sidco_mx4_quantize", "sidco_mx4_dequantize", "sidco_mx4_matmul",
     "sidco_mx4_compress", "sidco_mx4_mean", "sidco_orthogonalize_workspace_bytes", "sidco_orthogonalize",
     "sidco_wait_timeouts", "sidco_set_product_test_hooks",
+    "sidco_dropout", "sidco_embedding", "sidco_embedding_grad_workspace_bytes", "sidco_embedding_grad",
 ]
 
 _lib = None
@@ -148,6 +149,16 @@ def lib() -> C.CDLL:
     L.sidco_wait_timeouts.restype = i32
     L.sidco_set_product_test_hooks.argtypes = [C.c_longlong, i32]
     L.sidco_set_product_test_hooks.restype = i32
+    u64, sz = C.c_uint64, C.c_size_t
+    L.sidco_dropout.argtypes = [vp, i32, i64, f32, u64, u64, vp, vp, vp, vp]
+    L.sidco_dropout.restype = i32
+    L.sidco_embedding.argtypes = [vp, i32, i64, i64, i64, vp, i32, i64, f32, f32, u64, u64, vp, vp, i32, i64, vp, vp]
+    L.sidco_embedding.restype = i32
+    L.sidco_embedding_grad_workspace_bytes.argtypes = [i64, i64, i64]
+    L.sidco_embedding_grad_workspace_bytes.restype = i64
+    L.sidco_embedding_grad.argtypes = [vp, i32, i64, vp, i32, i64, i64, i64, f32, f32, u64, u64, vp, vp, i32, i64, i32, vp,
+                                       sz, vp]
+    L.sidco_embedding_grad.restype = i32
     _lib = L
     return L
 
@@ -514,3 +525,64 @@ def sidco_set_product_test_hooks(wait_us: int = 0, drop_phase: int = -1) -> None
     rc = lib().sidco_set_product_test_hooks(wait_us, drop_phase)
     if rc:
         raise SidcoError(rc, "sidco_set_product_test_hooks")
+
+
+# ---- the ends of a language model's training step: lookup, dropout, cross entropy (see sidco.h)
+
+T_I32, T_I64 = 3, 4
+EMBEDDING_ST_TOKEN = 1
+_TOKEN_TYPES = {"torch.int32": T_I32, "torch.int64": T_I64, "int32": T_I32, "int64": T_I64}
+_seen_token_types = {}
+
+
+def _token_type(x, given: Optional[int]) -> int:
+    """The SIDCO_T_I* code of a tensor or array of tokens or labels; raw addresses need `given`."""
+    if given is not None:
+        return given
+    dtype = getattr(x, "dtype", None)
+    code = _seen_token_types.get(dtype)
+    if code is None:
+        code = _TOKEN_TYPES.get(str(dtype))
+        if code is None:
+            raise SidcoError(-13, "type of tokens %s:" % ("of a raw address" if dtype is None else dtype))
+        _seen_token_types[dtype] = code
+    return code
+
+
+def sidco_dropout(x, n: int, p: float, seed: int, call: int, out, residual=None, step=None, x_type=None,
+                  stream=None) -> None:
+    """out = dropout(x) (+ residual) of n elements; the mask is a function of seed, call and position."""
+    rc = lib().sidco_dropout(_ptr(x), _type(x, x_type), n, p, seed, call, _ptr(step), _ptr(residual), _ptr(out),
+                             _stream(stream))
+    if rc:
+        raise SidcoError(rc, "sidco_dropout")
+
+
+def sidco_embedding(table, vocab: int, cols: int, ld: int, tokens, n: int, scale: float, out, ldo: int, p: float = 0.0,
+                    seed: int = 0, call: int = 0, step=None, status=None, table_type=None, token_type=None,
+                    out_type=None, stream=None) -> None:
+    """out[i] = scale * dropout(table[tokens[i]])."""
+    rc = lib().sidco_embedding(_ptr(table), _type(table, table_type), vocab, cols, ld, _ptr(tokens),
+                               _token_type(tokens, token_type), n, scale, p, seed, call, _ptr(step), _ptr(out),
+                               _type(out, out_type), ldo, _ptr(status), _stream(stream))
+    if rc:
+        raise SidcoError(rc, "sidco_embedding")
+
+
+def sidco_embedding_grad_workspace_bytes(n: int, vocab: int, cols: int) -> int:
+    size = int(lib().sidco_embedding_grad_workspace_bytes(n, vocab, cols))
+    if size < 0:
+        raise SidcoError(size, "sidco_embedding_grad_workspace_bytes")
+    return size
+
+
+def sidco_embedding_grad(dy, ld_dy: int, tokens, n: int, vocab: int, cols: int, scale: float, dtable, ldd: int, workspace,
+                         workspace_bytes: int, add: bool = False, p: float = 0.0, seed: int = 0, call: int = 0, step=None,
+                         dy_type=None, token_type=None, dtable_type=None, stream=None) -> None:
+    """Gradient of the table of sidco_embedding, written (all rows) or added (the rows of tokens that occur)."""
+    rc = lib().sidco_embedding_grad(_ptr(dy), _type(dy, dy_type), ld_dy, _ptr(tokens), _token_type(tokens, token_type), n,
+                                    vocab, cols, scale, p, seed, call, _ptr(step), _ptr(dtable),
+                                    _type(dtable, dtable_type), ldd, int(add), _ptr(workspace), workspace_bytes,
+                                    _stream(stream))
+    if rc:
+        raise SidcoError(rc, "sidco_embedding_grad")

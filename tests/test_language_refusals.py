@@ -1,0 +1,102 @@
+"""Argument errors of dropout, embedding and cross entropy, found on the host before any CUDA call (no GPU)."""
+import numpy as np
+import pytest
+
+P = 0x100000                                   # never dereferenced: every call below fails validation first
+Q = 0x4000000
+BIG = 1 << 31
+NAN = float("nan")
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_2101_10761_b200 import binding, build
+    build.build()
+    return binding
+
+
+def code(call, *args, **kw):
+    from paper_2101_10761_b200 import binding
+    with pytest.raises(binding.SidcoError) as e:
+        call(*args, stream=0, **kw)
+    return e.value.code
+
+
+def test_dropout_refuses(B):
+    d = B.sidco_dropout
+    assert code(d, P, -1, .5, 0, 0, Q, x_type=0) == -10
+    assert code(d, P, (1 << 40) + 1, .5, 0, 0, Q, x_type=0) == -10
+    assert code(d, P, 8, .5, 0, 0, Q, x_type=3) == -13
+    assert code(d, P, 8, .5, 0, 0, Q) == -13                       # a raw address without a type
+    for p in (-.1, 1.001, NAN, float("inf")):
+        assert code(d, P, 8, p, 0, 0, Q, x_type=1) == -6
+    assert code(d, None, 8, .5, 0, 0, Q, x_type=0) == -1
+    assert code(d, P, 8, .5, 0, 0, None, x_type=0) == -1
+    assert code(d, P + 2, 8, .5, 0, 0, Q, x_type=0) == -14
+    assert code(d, P, 8, .5, 0, 0, Q + 1, x_type=1) == -14
+    assert code(d, P, 8, .5, 0, 0, Q, residual=P + 1, x_type=1) == -14
+    assert code(d, P, 8, .5, 0, 0, Q, step=P + 4, x_type=1) == -14
+    assert code(d, P, 8, .5, 0, 0, P + 4, x_type=0) == -9
+    assert code(d, Q, 8, .5, 0, 0, P + 4, residual=P, x_type=0) == -9
+    d(None, 0, .5, 0, 0, None, x_type=0, stream=0)                 # nothing to do
+
+
+def test_embedding_refuses(B):
+    e = B.sidco_embedding
+    kw = dict(table_type=0, token_type=4, out_type=1)
+
+    def with_(**k):
+        return {**kw, **k}
+    assert code(e, P, BIG, 8, 8, P, 4, 1., Q, 8, **kw) == -10
+    assert code(e, P, 9, (1 << 24) + 1, BIG, P, 4, 1., Q, BIG, **kw) == -10
+    assert code(e, P, 9, 8, 8, P, -1, 1., Q, 8, **kw) == -10
+    assert code(e, P, 9, 8, 8, P, 4, 1., Q, 8, **with_(table_type=3)) == -13
+    assert code(e, P, 9, 8, 8, P, 4, 1., Q, 8, **with_(out_type=-1)) == -13
+    assert code(e, P, 9, 8, 8, P, 4, 1., Q, 8, **with_(token_type=0)) == -13
+    assert code(e, P, 9, 8, 8, np.zeros(4, np.float32), 4, 1., Q, 8, table_type=0, out_type=0) == -13
+    assert code(e, P, 9, 8, 7, P, 4, 1., Q, 8, **kw) == -6
+    assert code(e, P, 9, 8, 8, P, 4, 1., Q, 7, **kw) == -6
+    assert code(e, P, 9, 8, 8, P, 4, 1., Q, 8, p=NAN, **kw) == -6
+    assert code(e, P, 9, 8, 8, P, 4, 1., Q, 8, p=.5, step=P + 1, **kw) == -14
+    for args in ((None, P, Q), (P, None, Q), (P, P, None)):
+        assert code(e, args[0], 9, 8, 8, args[1], 4, 1., args[2], 8, **kw) == -1
+    assert code(e, P + 2, 9, 8, 8, P, 4, 1., Q, 8, **kw) == -14
+    assert code(e, P, 9, 8, 8, P + 4, 4, 1., Q, 8, **kw) == -14
+    assert code(e, P, 9, 8, 8, P, 4, 1., Q + 1, 8, **kw) == -14
+    assert code(e, P, 9, 8, 8, P, 4, 1., Q, 8, status=P + 2, **kw) == -14
+    assert code(e, P, 9, 8, 8, Q, 4, 1., P + 9 * 32 - 4, 8, **kw) == -9       # the last element of the table
+    assert code(e, P, 9, 8, 8, Q, 4, 1., Q + 24, 8, **kw) == -9
+
+
+def test_embedding_grad_refuses(B):
+    g = B.sidco_embedding_grad
+    W = 0x8000000
+    kw = dict(dy_type=1, token_type=3, dtable_type=0)
+    need = B.sidco_embedding_grad_workspace_bytes(4, 9, 8)
+
+    def with_(**k):
+        return {**kw, **k}
+    assert need > 0 and B.sidco_embedding_grad_workspace_bytes(0, 9, 8) == 0
+    with pytest.raises(B.SidcoError) as err:
+        B.sidco_embedding_grad_workspace_bytes(BIG, 9, 8)
+    assert err.value.code == -10
+    assert code(g, P, 8, P, 4, BIG, 8, 1., Q, 8, W, need, **kw) == -10
+    assert code(g, P, 8, P, 4, 9, 8, 1., Q, 8, W, need, **with_(dy_type=7)) == -13
+    assert code(g, P, 8, P, 4, 9, 8, 1., Q, 8, W, need, **with_(dtable_type=7)) == -13
+    assert code(g, P, 8, P, 4, 9, 8, 1., Q, 8, W, need, **with_(token_type=2)) == -13
+    assert code(g, P, 7, P, 4, 9, 8, 1., Q, 8, W, need, **kw) == -6
+    assert code(g, P, 8, P, 4, 9, 8, 1., Q, 7, W, need, **kw) == -6
+    assert code(g, P, 8, P, 4, 9, 8, 1., Q, 8, W, need, p=2., **kw) == -6
+    for args in ((None, P, Q), (P, None, Q), (P, P, None)):
+        assert code(g, args[0], 8, args[1], 4, 9, 8, 1., args[2], 8, W, need, **kw) == -1
+    assert code(g, P + 1, 8, P, 4, 9, 8, 1., Q, 8, W, need, **kw) == -14
+    assert code(g, P, 8, P + 2, 4, 9, 8, 1., Q, 8, W, need, **kw) == -14
+    assert code(g, P, 8, P, 4, 9, 8, 1., Q + 2, 8, W, need, **kw) == -14
+    assert code(g, P, 8, P, 4, 9, 8, 1., Q, 8, None, need, **kw) == -8
+    assert code(g, P, 8, P, 4, 9, 8, 1., Q, 8, W, need - 1, **kw) == -8
+    assert code(g, P, 8, P, 4, 9, 8, 1., Q, 8, W + 128, need, **kw) == -8
+    assert code(g, P, 8, W, 4, 9, 8, 1., P + 60, 8, Q, need, **kw) == -9
+    assert code(g, P, 8, Q + 4, 4, 9, 8, 1., Q, 8, W, need, **kw) == -9
+    assert code(g, W, 8, P, 4, 9, 8, 1., Q, 8, W, need, **kw) == -9
+    assert code(g, P, 8, W + 256, 4, 9, 8, 1., Q, 8, W, need, **kw) == -9
+    assert code(g, P, 8, P, 4, 9, 8, 1., W, 8, W, need, **kw) == -9
