@@ -422,7 +422,45 @@ int sidco_embedding_grad(const void* dy, int dy_type, int64_t ld_dy, const void*
                          const uint64_t* step, void* dtable, int dtable_type, int64_t ldd, int add, void* workspace,
                          size_t workspace_bytes, void* stream);
 
-/* How many CTAs of the product kernels (sidco_mx4_matmul, sidco_orthogonalize) have given up a bounded wait since the
+/*
+ * sidco_linear_cross_entropy - softmax cross entropy of an output projection over a vocabulary, with its gradients, without
+ * storing the logits.
+ *
+ *     s = scale * x w^T;   row_losses[i] = log(sum_v exp(s[i][v])) - s[i][labels[i]];   loss = sum_i c_i row_losses[i];
+ *     dx = d loss / d x;   dw = d loss / d w (with add_dw: added to dw)
+ *
+ * with c_i = row_weights[i], or 1 / (number of rows that have a label) where row_weights is NULL: the mean.  A row with a
+ * negative label has none: its loss and its row of dx are zero and nothing of it, NaN included, reaches dw; rows without a
+ * label cost no products.  So does a label >= vocab, which is reported in `status` (SIDCO_CROSS_ENTROPY_ST_LABEL).  Without any label the
+ * loss is 0.  Logits, sums and statistics are held in fp32.  The gradient of the logits is held in `type`, rounded twice:
+ * dx and dw carry an error of about 2^-8 (bf16) or 2^-11 (fp16) of the size of their terms, also where dw is fp32.
+ *
+ * x          device, type[rows][ldx], type SIDCO_T_BF16 or SIDCO_T_F16.     labels  device, label_type[rows].
+ * w          device, w_type[vocab][ldw], w_type = type, or SIDCO_T_F32, which is rounded to `type`.  Rows that are not 16-byte
+ *            aligned, and fp32, are copied to the workspace in every call.
+ * row_losses device, float[rows], or NULL.       loss  device, float, or NULL.
+ * dx         device, type[rows][lddx], or NULL: not wanted.
+ * dw         device, dw_type[vocab][lddw], dw_type = type or SIDCO_T_F32, or NULL: not wanted.
+ * piece_rows rows whose gradient of the logits is held at a time (rounded up to 256); 0: as many as fit into 512 MB or what
+ *            dw takes in 32 bits, whichever is more.  With several pieces dw is summed in fp32 in the workspace.
+ * status     device, int32, or NULL: cleared on `stream`, then as above.
+ * workspace  device, 256-byte aligned, at least sidco_linear_cross_entropy_workspace_bytes(w, type, w_type, ldw, rows, vocab,
+ *            hidden, grads, piece_rows) bytes, grads 1: dx, 2: dw, 3: both, 0: neither, of w only the alignment is looked
+ *            at; caller-owned, nothing is kept in it between calls; not to be shared by calls that overlap.
+ * Buffers that are written must not overlap others (SIDCO_E_ALIAS).  rows, vocab <= 2^28, hidden <= 2^20; vocab and hidden
+ * at least 1.
+ */
+#define SIDCO_CROSS_ENTROPY_ST_LABEL 1
+int64_t sidco_linear_cross_entropy_workspace_bytes(const void* w, int type, int w_type, int64_t ldw, int64_t rows,
+                                                   int64_t vocab, int64_t hidden, int grads,
+                                                   int64_t piece_rows);                     /* negative: SIDCO_E_* */
+int sidco_linear_cross_entropy(const void* x, int type, int64_t ldx, const void* w, int w_type, int64_t ldw,
+                               const void* labels, int label_type, const float* row_weights, float scale, int64_t rows,
+                               int64_t vocab, int64_t hidden, float* row_losses, float* loss, void* dx, int64_t lddx,
+                               void* dw, int dw_type, int64_t lddw, int add_dw, int64_t piece_rows, int32_t* status,
+                               void* workspace, size_t workspace_bytes, void* stream);
+
+/* How many CTAs of the product kernels (sidco_mx4_matmul, sidco_orthogonalize, sidco_linear_cross_entropy) have given up a bounded wait since the
  * library was loaded; anything but 0 means that an output is incomplete.  Negative: a CUDA error.  Synchronises the
  * device; meant for tests and logging. */
 int sidco_wait_timeouts(void);

@@ -50,6 +50,7 @@ EXPORTS = [
     "sidco_mx4_compress", "sidco_mx4_mean", "sidco_orthogonalize_workspace_bytes", "sidco_orthogonalize",
     "sidco_wait_timeouts", "sidco_set_product_test_hooks",
     "sidco_dropout", "sidco_embedding", "sidco_embedding_grad_workspace_bytes", "sidco_embedding_grad",
+    "sidco_linear_cross_entropy_workspace_bytes", "sidco_linear_cross_entropy",
 ]
 
 _lib = None
@@ -159,6 +160,11 @@ def lib() -> C.CDLL:
     L.sidco_embedding_grad.argtypes = [vp, i32, i64, vp, i32, i64, i64, i64, f32, f32, u64, u64, vp, vp, i32, i64, i32, vp,
                                        sz, vp]
     L.sidco_embedding_grad.restype = i32
+    L.sidco_linear_cross_entropy_workspace_bytes.argtypes = [vp, i32, i32, i64, i64, i64, i64, i32, i64]
+    L.sidco_linear_cross_entropy_workspace_bytes.restype = i64
+    L.sidco_linear_cross_entropy.argtypes = [vp, i32, i64, vp, i32, i64, vp, i32, vp, f32, i64, i64, i64, vp, vp, vp, i64, vp,
+                                             i32, i64, i32, i64, vp, vp, sz, vp]
+    L.sidco_linear_cross_entropy.restype = i32
     _lib = L
     return L
 
@@ -586,3 +592,31 @@ def sidco_embedding_grad(dy, ld_dy: int, tokens, n: int, vocab: int, cols: int, 
                                     _stream(stream))
     if rc:
         raise SidcoError(rc, "sidco_embedding_grad")
+
+
+CROSS_ENTROPY_ST_LABEL = 1
+
+
+def sidco_linear_cross_entropy_workspace_bytes(x, w, ldw: int, rows: int, vocab: int, hidden: int, grads=True,
+                                               piece_rows: int = 0, x_type=None, w_type=None) -> int:
+    """`grads`: True (dx and dw), False, or 1 for dx and 2 for dw alone."""
+    size = int(lib().sidco_linear_cross_entropy_workspace_bytes(
+        _ptr(w), _type(x, x_type), _type(w, w_type), ldw, rows, vocab, hidden, 3 if grads is True else int(grads),
+        piece_rows))
+    if size < 0:
+        raise SidcoError(size, "sidco_linear_cross_entropy_workspace_bytes")
+    return size
+
+
+def sidco_linear_cross_entropy(x, ldx: int, w, ldw: int, labels, rows: int, vocab: int, hidden: int, row_losses, loss, dx,
+                               lddx: int, dw, lddw: int, workspace, workspace_bytes: int, row_weights=None,
+                               scale: float = 1.0, add: bool = False, piece_rows: int = 0, status=None, x_type=None,
+                               w_type=None, label_type=None, dw_type=None, stream=None) -> None:
+    """Cross entropy of scale * x w^T against labels: losses and, where dx / dw are given, the gradients."""
+    rc = lib().sidco_linear_cross_entropy(
+        _ptr(x), _type(x, x_type), ldx, _ptr(w), _type(w, w_type), ldw, _ptr(labels), _token_type(labels, label_type),
+        _ptr(row_weights), scale, rows, vocab, hidden, _ptr(row_losses), _ptr(loss), _ptr(dx), lddx, _ptr(dw),
+        0 if dw is None else _type(dw, dw_type), lddw, int(add), piece_rows, _ptr(status), _ptr(workspace),
+        workspace_bytes, _stream(stream))
+    if rc:
+        raise SidcoError(rc, "sidco_linear_cross_entropy")

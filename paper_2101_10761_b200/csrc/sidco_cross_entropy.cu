@@ -1,0 +1,1094 @@
+// Softmax cross entropy of an output projection, s = scale * X W^T over a large vocabulary, with its gradients, without the
+// logits ever being stored: the products run on the tensor cores (bf16 or fp16 operands, fp32 sums in tensor memory).
+//
+//   lse_i = log sum_v exp s_iv;   loss_i = lse_i - s_i,y_i;   total = sum_i c_i loss_i
+//   D_iv = c_i scale (exp(s_iv - lse_i) - [v = y_i]);   dX = D W;   dW (+)= D^T X
+//
+//   prepare_kernel  rows with a label are gathered (the others cost nothing from here on and their contents, NaN included,
+//                   reach nothing); W is copied if its rows do not suit tensor copies or its type is another
+//   logits_kernel   tiles of X W^T; of each half of a tile's columns the largest logit and the sum of exponentials, and
+//                   with gradients e = exp(s - largest) in 16 bits
+//   scale_kernel    lse and loss of a row; e becomes D in place; the entry of the label is computed from its fp32 logit
+//   grads_kernel    dX and dW as one list of tiles
+//   join_kernel     adds the parts of dX where its sums over the vocabulary were split
+//   total_kernel    the total
+//
+// Why not the logits, or a second product in place of e: e is a relative quantity, so 16 bits cost it half a step of 2^-8
+// (bf16) or 2^-11 (fp16) whatever the size of the logit, and reading and writing it once costs a tenth of computing the
+// logits again (2 of 8 instead of 6 parts).  What it takes is bounded: rows go in pieces, so that e never takes more than
+// 512 MB or what the gradient of W takes in 32 bits, whichever is more; over several pieces dW is summed in fp32.
+// D is rounded twice (as e and as D); dX and dW are sums of such terms in fp32, rounded once to their type.
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <atomic>
+#include <type_traits>
+
+#include "../../include/sidco.h"
+#include "sidco_elements.cuh"
+#include "sidco_internal.h"
+#include "sidco_tc.cuh"
+
+namespace sidco_ce {
+
+using namespace sidco_tc;
+using namespace sidco_elements;
+
+constexpr int kTile = 256;            // rows and columns of a pair's tile
+constexpr int kStageK = 64;           // 128 bytes of 16-bit elements
+constexpr int kUnit = 64 * 128;       // a box: 64 rows of 128 bytes
+constexpr int kStages = 6;
+constexpr int kStageBytes = 4 * kUnit;
+constexpr int kBox = 32 * 128;        // of an epilogue warp
+constexpr int kThreads = 320;
+constexpr int kSmem = kStages * kStageBytes + 8 * kBox + 1024;
+constexpr int kMostParts = 16;
+
+struct Head {                         // written by prepare_kernel
+    int counted;                      // rows with a label
+    float lift, unlift;               // power of two that D is stored times, and its inverse
+    float mean;                       // 1 / counted
+};
+
+struct Sizes {
+    int rows, vocab, hidden;
+    int piece, first;                 // rows per piece, first gathered row of this one
+};
+
+__device__ int g_timeouts;
+
+template <typename T> constexpr bool kIsHalf = std::is_same<T, __half>::value;
+// fp16 has too little range for exponentials far below the largest: it keeps them times 2^14
+template <typename T> constexpr float kUp = kIsHalf<T> ? 14.0f : 0.0f;
+
+__device__ __forceinline__ int rows_of_piece(const Sizes& z, const Head* head) {
+    return max(0, min(z.piece, head->counted - z.first));
+}
+
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+template <typename T> __device__ __forceinline__ uint32_t pack2(float a, float b);
+template <> __device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float a, float b) {
+    const __nv_bfloat162 t = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&t);
+}
+template <> __device__ __forceinline__ uint32_t pack2<__half>(float a, float b) {
+    const __half2 t = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&t);
+}
+
+// ---------------------------------------------------------------------------------------------- gathering
+
+constexpr int kPrepareThreads = 256;
+
+struct Prepare {
+    const void* x;
+    int64_t ldx;
+    const void* w;
+    int64_t ldw;
+    const void* labels;
+    int wide;
+    const float* weights;
+    float scale;
+    int rows, vocab, hidden;
+    int64_t pitch;                    // elements between rows of the copies
+    void* x_to;
+    void* w_to;                       // NULL: W is used where it is
+    void* dx;                         // NULL: not wanted
+    int64_t lddx;
+    float* each;                      // NULL: not wanted
+    Head* head;
+    int *map, *target;
+    float* weight;
+    int32_t* status;
+    int x_blocks, x_rows;             // CTAs for the rows of X, rows of each
+    int x_vector, w_vector, dx_vector;
+};
+
+// One warp copies a row, `vector` elements at a time.
+template <typename TI, typename TO, int V>
+__device__ __forceinline__ void copy_vectors(const TI* from, TO* to, int cols, int lane) {
+    const int whole = cols / V;
+#pragma unroll 4
+    for (int i = lane; i < whole; i += 32) {
+        alignas(16) TI a[V];
+        alignas(16) TO b[V];
+        constexpr int kBytes = V * (int)sizeof(TI);
+        if constexpr (kBytes == 16) *reinterpret_cast<uint4*>(a) = *reinterpret_cast<const uint4*>(from + i * V);
+        else if constexpr (kBytes == 8) *reinterpret_cast<uint2*>(a) = *reinterpret_cast<const uint2*>(from + i * V);
+        else if constexpr (kBytes == 4) *reinterpret_cast<uint32_t*>(a) = *reinterpret_cast<const uint32_t*>(from + i * V);
+        else a[0] = from[i];
+        constexpr int kOut = V * (int)sizeof(TO);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            if constexpr (std::is_same<TI, TO>::value) b[j] = a[j];
+            else b[j] = narrow<TO>(widen(a[j]));
+        }
+        if constexpr (kOut == 16) *reinterpret_cast<uint4*>(to + i * V) = *reinterpret_cast<const uint4*>(b);
+        else if constexpr (kOut == 8) *reinterpret_cast<uint2*>(to + i * V) = *reinterpret_cast<const uint2*>(b);
+        else if constexpr (kOut == 4) *reinterpret_cast<uint32_t*>(to + i * V) = *reinterpret_cast<const uint32_t*>(b);
+        else to[i] = b[0];
+    }
+    for (int i = whole * V + lane; i < cols; i += 32) {
+        if constexpr (std::is_same<TI, TO>::value) to[i] = from[i];
+        else to[i] = narrow<TO>(widen(from[i]));
+    }
+}
+
+template <typename TI, typename TO>
+__device__ __forceinline__ void copy_row(const TI* from, TO* to, int cols, int vector, int lane) {
+    if (sizeof(TI) == 2 && vector == 8) copy_vectors<TI, TO, sizeof(TI) == 2 ? 8 : 4>(from, to, cols, lane);
+    else if (vector >= 4) copy_vectors<TI, TO, 4>(from, to, cols, lane);
+    else if (vector == 2) copy_vectors<TI, TO, sizeof(TI) == 2 ? 2 : 1>(from, to, cols, lane);
+    else copy_vectors<TI, TO, 1>(from, to, cols, lane);
+}
+
+template <typename T>
+__device__ __forceinline__ void zero_row(T* to, int cols, int vector, int lane) {
+    const T zero = narrow<T>(0.0f);
+    if (vector == 8) {
+        for (int i = lane; i < cols / 8; i += 32) reinterpret_cast<uint4*>(to)[i] = uint4{};
+        for (int i = cols / 8 * 8 + lane; i < cols; i += 32) to[i] = zero;
+    } else {
+        for (int i = lane; i < cols; i += 32) to[i] = zero;
+    }
+}
+
+__device__ __forceinline__ bool has_label(int64_t y, int vocab) { return y >= 0 && y < vocab; }
+
+// Sum over the CTA, in all threads.
+__device__ __forceinline__ int block_sum(int v, int* s_part) {
+    v = __reduce_add_sync(0xffffffffu, v);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) s_part[threadIdx.x >> 5] = v;
+    __syncthreads();
+    int all = 0;
+    for (int i = 0; i < kPrepareThreads / 32; ++i) all += s_part[i];
+    return all;
+}
+
+template <typename T, typename TW>
+__global__ void __launch_bounds__(kPrepareThreads) prepare_kernel(const Prepare a) {
+    __shared__ int s_part[kPrepareThreads / 32];
+    __shared__ uint32_t s_most[kPrepareThreads / 32];
+    __shared__ int s_to[kPrepareThreads];                             // where a row goes, or -1
+    wait_prerequisites();
+    launch_dependents();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if ((int)blockIdx.x >= a.x_blocks) {
+        const int64_t workers = (int64_t)(gridDim.x - a.x_blocks) * (kPrepareThreads / 32);
+        for (int64_t r = (int64_t)(blockIdx.x - a.x_blocks) * (kPrepareThreads / 32) + warp; r < a.vocab; r += workers)
+            copy_row(static_cast<const TW*>(a.w) + r * a.ldw, static_cast<T*>(a.w_to) + r * a.pitch, a.hidden, a.w_vector, lane);
+        return;
+    }
+    // labelled rows before this CTA's and in all; the largest weight (every CTA counts for itself: nobody waits)
+    const int first = min(a.rows, (int)blockIdx.x * a.x_rows), end = min(a.rows, first + a.x_rows);
+    int before = 0, all = 0;
+    uint32_t most = 0;
+    for (int i = threadIdx.x; i < a.rows; i += kPrepareThreads) {
+        const bool has = has_label(token_at(a.labels, a.wide, i), a.vocab);
+        all += has;
+        before += has && i < first;
+        if (has && a.weights) most = max(most, __float_as_uint(a.weights[i]) & 0x7fffffffu);
+    }
+    before = block_sum(before, s_part);
+    all = block_sum(all, s_part);
+    if (blockIdx.x == 0) {
+        most = __reduce_max_sync(0xffffffffu, most);
+        if (lane == 0) s_most[warp] = most;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            Head h;
+            h.counted = all;
+            h.mean = all ? 1.0f / (float)all : 0.0f;
+            for (int i = 0; i < kPrepareThreads / 32; ++i) most = max(most, s_most[i]);
+            // fp16: the largest |c scale| is brought to [2^13, 2^14) as far as the powers of two reach, so that D keeps
+            // eleven bits down to 2^-28 of it
+            h.lift = h.unlift = 1.0f;
+            const float top = fabsf((a.weights ? __uint_as_float(most) : h.mean) * a.scale);
+            if (kIsHalf<T> && top > 0.0f && top < INFINITY) {
+                const int e = max(-100, min(100, 13 - ilogbf(top)));
+                h.lift = ldexpf(1.0f, e);
+                h.unlift = ldexpf(1.0f, -e);
+            }
+            *a.head = h;
+        }
+        // the rows behind the last, up to a whole step of the products over rows
+        const int up = (all + kStageK - 1) / kStageK * kStageK;
+        for (int r = all + warp; r < up; r += kPrepareThreads / 32)
+            zero_row(static_cast<T*>(a.x_to) + r * a.pitch, a.hidden, 8, lane);
+    }
+    for (int r0 = first; r0 < end; r0 += kPrepareThreads) {
+        const int r = r0 + threadIdx.x;
+        const int64_t y = r < end ? token_at(a.labels, a.wide, r) : -1;
+        const bool has = has_label(y, a.vocab);
+        if (a.status && y >= a.vocab) atomicOr(a.status, SIDCO_CROSS_ENTROPY_ST_LABEL);
+        const uint32_t in = __ballot_sync(0xffffffffu, has);
+        __syncthreads();
+        if (lane == 0) s_part[warp] = __popc(in);
+        __syncthreads();
+        int to = before + __popc(in & ((1u << lane) - 1));
+        for (int i = 0; i < kPrepareThreads / 32; ++i) {
+            if (i < warp) to += s_part[i];
+            before += s_part[i];
+        }
+        s_to[threadIdx.x] = has ? to : -1;
+        if (has) {
+            a.map[to] = r;
+            a.target[to] = (int)y;
+            a.weight[to] = a.weights ? a.weights[r] : all ? 1.0f / (float)all : 0.0f;
+        } else if (r < end && a.each) {
+            a.each[r] = 0.0f;
+        }
+        __syncthreads();
+        for (int i = warp; i < min(kPrepareThreads, end - r0); i += kPrepareThreads / 32) {
+            if (s_to[i] >= 0)
+                copy_row(static_cast<const T*>(a.x) + (r0 + i) * a.ldx, static_cast<T*>(a.x_to) + s_to[i] * a.pitch, a.hidden,
+                         a.x_vector, lane);
+            else if (a.dx)
+                zero_row(static_cast<T*>(a.dx) + (r0 + i) * a.lddx, a.hidden, a.dx_vector, lane);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- products
+//
+// Tiles of 256 x 256 by pairs of CTAs, each with 128 rows of A and half of B's 256 rows; K in stages of 64; two sets of sums
+// in tensor memory, so that the sums of one tile are taken out under the products of the next.
+//   warp 0     feeds the stages        warp 1     issues the products (first CTA)
+//   warps 2-9  take the sums out: a quarter of the CTA's 128 rows, half of the columns each
+// An operand whose rows run along K is K-major; one whose rows run along M or N is read as it lies, MN-major, so that
+// no transpose of P, X or W is ever made.
+
+struct Operand {
+    const CUtensorMap* map;
+    bool mn;                          // rows of the matrix run along K: a unit is 64 of them, 64 elements of M or N wide
+    int row0;                         // added to the matrix's row
+};
+
+// Two units: 128 M or N indices from `at` on, stage k.
+__device__ __forceinline__ void load_operand(uint32_t dst, const Operand& o, int at, int k, uint32_t bar) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        if (o.mn) tensor_load_2d_pair(dst + u * kUnit, o.map, (at + u * 64) * 2, o.row0 + k * kStageK, bar);
+        else tensor_load_2d_pair(dst + u * kUnit, o.map, k * 128, o.row0 + at + u * 64, bar);
+    }
+}
+
+template <typename T> __device__ constexpr uint32_t shape_of(bool a_mn, bool b_mn) {
+    const uint32_t type = kIsHalf<T> ? 0 : 1;
+    return (1u << 4) | (type << 7) | (type << 10) | ((a_mn ? 1u : 0u) << 15) | ((b_mn ? 1u : 0u) << 16) |
+           ((uint32_t)(kTile >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
+}
+
+struct Job {                          // a tile, or a part of K of one
+    Operand a, b;
+    int ti, tj, from, to;             // stages
+    int kind, part;
+};
+
+struct Shared {
+    uint64_t full[kStages], free[kStages], sums[2], taken[2];
+    uint32_t tmem;
+    int failed;
+};
+
+// The three roles over the jobs that next(it, job) gives; finish(job, sums, quarter, half, take) takes a tile's sums out and
+// calls take() when it has read them.
+template <typename T, typename Next, typename Finish>
+__device__ __forceinline__ void run_jobs(Shared& s, uint8_t* smem, Next next, Finish finish) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_rank(), stage0 = smem_addr(smem), tmem = s.tmem;
+    Job j;
+    if (warp == 0) {
+        if (elect_one()) {
+            int st = 0;
+            uint32_t round = 0;
+            bool ok = true;
+            for (int it = 0; ok && next(it, j); ++it) {
+                const int row_a = j.ti * kTile + (int)rank * 128, row_b = j.tj * kTile + (int)rank * 128;
+                for (int k = j.from; k < j.to; ++k) {
+                    const uint32_t a = stage0 + st * kStageBytes, bar = smem_addr(&s.full[st]);
+                    ok = mbar_wait(smem_addr(&s.free[st]), (round & 1) ^ 1, &s.failed);
+                    if (!ok) break;
+                    if (rank == 0) mbar_expect_tx(bar, 2 * kStageBytes);
+                    load_operand(a, j.a, row_a, k, bar);
+                    load_operand(a + 2 * kUnit, j.b, row_b, k, bar);
+                    if (++st == kStages) { st = 0; ++round; }
+                }
+            }
+        }
+    } else if (warp == 1) {
+        if (rank == 0) {                                              // (the whole warp waits, one thread issues)
+            int st = 0;
+            uint32_t round = 0;
+            bool ok = true;
+            for (int it = 0; ok && next(it, j); ++it) {
+                const int buf = it & 1;
+                const uint32_t sums = tmem + buf * kTile;
+                const uint32_t a_step = j.a.mn ? 2048 : 32, a_lead = j.a.mn ? kUnit : 16;
+                const uint32_t b_step = j.b.mn ? 2048 : 32, b_lead = j.b.mn ? kUnit : 16;
+                const uint32_t shape = shape_of<T>(j.a.mn, j.b.mn);
+                ok = __all_sync(0xffffffffu, mbar_wait(smem_addr(&s.taken[buf]), ((it >> 1) & 1) ^ 1, &s.failed));
+                for (int k = j.from; k < j.to && ok; ++k) {
+                    ok = __all_sync(0xffffffffu, mbar_wait(smem_addr(&s.full[st]), round & 1, &s.failed));
+                    if (!ok) break;
+                    fence_after_sync();
+                    const uint32_t a = stage0 + st * kStageBytes, b = a + 2 * kUnit;
+                    if (elect_one()) {
+#pragma unroll
+                        for (int q = 0; q < kStageK / 16; ++q)
+                            mma_f16_pair(sums, swizzled_operand(a + q * a_step, a_lead, 1024),
+                                         swizzled_operand(b + q * b_step, b_lead, 1024), shape, k > j.from || q > 0);
+                        tc_commit_pair(smem_addr(&s.free[st]));
+                        if (k + 1 == j.to) tc_commit_pair(smem_addr(&s.sums[buf]));
+                    }
+                    __syncwarp();
+                    if (++st == kStages) { st = 0; ++round; }
+                }
+            }
+        }
+    } else {
+        const int quarter = warp & 3, half = (warp - 2) >> 2;
+        const uint32_t taken[2] = {in_cta(smem_addr(&s.taken[0]), 0), in_cta(smem_addr(&s.taken[1]), 0)};
+        for (int it = 0; next(it, j); ++it) {
+            const int buf = it & 1;
+            bool ok = mbar_wait(smem_addr(&s.sums[buf]), (it >> 1) & 1, &s.failed);
+            if (!__all_sync(0xffffffffu, ok)) break;
+            fence_after_sync();
+            finish(j, tmem + buf * kTile + half * 128 + ((uint32_t)(quarter * 32) << 16), (int)rank * 128 + quarter * 32,
+                   half * 128, smem + kStages * kStageBytes + (warp - 2) * kBox, [&] {
+                       fence_before_sync();
+                       __syncwarp();
+                       if (lane == 0) mbar_arrive_cluster(taken[buf]);
+                   });
+        }
+    }
+}
+
+__device__ __forceinline__ uint8_t* set_up(Shared& s, uint8_t* raw) {
+    const int warp = threadIdx.x >> 5;
+    if (warp == 1) tmem_alloc_pair(&s.tmem, 512);
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kStages; ++i) {
+            mbar_init(smem_addr(&s.full[i]), 1);
+            mbar_init(smem_addr(&s.free[i]), 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(smem_addr(&s.sums[i]), 1);
+            mbar_init(smem_addr(&s.taken[i]), 16);                    // eight warps of both CTAs
+        }
+        s.failed = 0;
+        mbar_init_fence();
+    }
+    fence_before_sync();
+    __syncthreads();
+    cluster_sync();
+    fence_after_sync();
+    return (uint8_t*)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
+}
+
+__device__ __forceinline__ void tear_down(Shared& s, int* timeouts) {
+    __syncwarp();
+    fence_before_sync();
+    __syncthreads();
+    if (threadIdx.x == 0 && s.failed) {
+        atomicAdd(timeouts, 1);
+        let_work_end();
+    }
+    __syncthreads();
+    cluster_sync();
+    if ((threadIdx.x >> 5) == 1) tmem_free_pair(s.tmem, 512);
+}
+
+// ---------------------------------------------------------------------------------------------- logits
+
+struct Logits {
+    Sizes z;
+    const Head* head;
+    const int* target;
+    float scale2;                     // scale log2(e): logits in powers of two
+    float2* stats;                    // [rows of a piece][2 tiles]: largest, sum of 2^(s - largest)
+    int tiles_n;
+    float* label;                     // logit of the label
+    int store;                        // e is wanted
+    int* timeouts;
+};
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2)
+    logits_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w,
+                  const __grid_constant__ CUtensorMap map_e, const Logits g) {
+    extern __shared__ uint8_t s_raw[];
+    __shared__ Shared s;
+    uint8_t* smem = set_up(s, s_raw);
+    wait_prerequisites();
+    launch_dependents();
+    const int lane = threadIdx.x & 31;
+    const int rows = rows_of_piece(g.z, g.head), tiles_m = (rows + kTile - 1) / kTile, total = tiles_m * g.tiles_n;
+    const int n_pairs = gridDim.x / 2, stages = (g.z.hidden + kStageK - 1) / kStageK;
+    // tiles in bands of eight tile rows, column by column, so that pairs at work at the same time share operands in L2
+    const auto next = [&](int it, Job& j) {
+        const int64_t i = blockIdx.x / 2 + (int64_t)it * n_pairs;
+        if (i >= total) return false;
+        const int per = 8 * g.tiles_n, band = (int)(i / per), in = (int)(i - (int64_t)band * per), high = min(8, tiles_m - band * 8);
+        j = Job{{&map_x, false, g.z.first}, {&map_w, false, 0}, band * 8 + in % high, in / high, 0, stages, 0, 0};
+        return true;
+    };
+    const auto finish = [&](const Job& j, uint32_t sums, int row_in, int col_in, uint8_t* box, auto take) {
+        const int r0 = j.ti * kTile + row_in, r = r0 + lane, c0 = j.tj * kTile + col_in;
+        uint32_t acc[128];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) tmem_load32(sums + q * 32, *reinterpret_cast<uint32_t(*)[32]>(acc + q * 32));
+        take();
+        const bool mine = r < rows;
+        const int target = mine ? g.target[g.z.first + r] - c0 : -1;
+        float most = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 128; ++i) {
+            float v = __uint_as_float(acc[i]) * g.scale2;
+            if (c0 + 128 > g.z.vocab && c0 + i >= g.z.vocab) v = -INFINITY;
+            acc[i] = __float_as_uint(v);
+            most = fmaxf(most, v);
+        }
+        if (__any_sync(0xffffffffu, (unsigned)target < 128u)) {       // a few tiles only
+            float v = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 128; ++i)
+                if (target == i) v = __uint_as_float(acc[i]);
+            if ((unsigned)target < 128u) g.label[r] = v;
+        }
+        const float base = (most == -INFINITY ? 0.0f : most) - kUp<T>;      // (nothing but -inf: zeros)
+        float sum[4] = {};
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            if (g.store) {
+                if (lane == 0) bulk_store_wait_read();
+                __syncwarp();
+            }
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                uint32_t t[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float a = exp2_fast(__uint_as_float(acc[h * 64 + q * 8 + 2 * i]) - base);
+                    const float b = exp2_fast(__uint_as_float(acc[h * 64 + q * 8 + 2 * i + 1]) - base);
+                    sum[i] += a + b;
+                    t[i] = pack2<T>(a, b);
+                }
+                if (g.store)
+                    *reinterpret_cast<uint4*>(box + lane * 128 + ((q ^ (lane & 7)) << 4)) = make_uint4(t[0], t[1], t[2], t[3]);
+            }
+            if (g.store) {
+                fence_async_shared();
+                __syncwarp();
+                if (lane == 0) {
+                    if (r0 < rows && c0 + h * 64 < g.z.vocab) tensor_store_2d(&map_e, c0 + h * 64, r0, smem_addr(box));
+                    bulk_store_commit();
+                }
+            }
+        }
+        if (mine)
+            g.stats[(int64_t)r * 2 * g.tiles_n + c0 / 128] =
+                make_float2(most, ((sum[0] + sum[1]) + (sum[2] + sum[3])) * (kIsHalf<T> ? 0x1p-14f : 1.0f));
+    };
+    run_jobs<T>(s, smem, next, finish);
+    if ((threadIdx.x >> 5) >= 2 && lane == 0) bulk_store_wait();
+    tear_down(s, g.timeouts);
+}
+
+// ---------------------------------------------------------------------------------------------- from e to D
+
+constexpr int kScaleThreads = 256;
+
+struct Scale {
+    Sizes z;
+    const Head* head;
+    const int *map, *target;
+    const float* weight;
+    float scale;
+    const float2* stats;
+    int tiles_n;
+    const float* label;
+    void* e;                          // NULL: no gradients
+    int64_t pitch;
+    float* each;                      // NULL: not wanted
+    float* share;                     // weight times loss, of the gathered rows
+};
+
+template <typename T> __global__ void __launch_bounds__(kScaleThreads) scale_kernel(const Scale a) {
+    __shared__ float s_part[kScaleThreads / 32];
+    wait_prerequisites();
+    launch_dependents();
+    const int rows = rows_of_piece(a.z, a.head), r = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    T* e = a.e ? static_cast<T*>(a.e) + r * a.pitch : nullptr;
+    const int vectors = (int)((a.z.vocab + 7) / 8);
+    if (r >= rows) {
+        if (e && r < (rows + kStageK - 1) / kStageK * kStageK)
+            for (int i = threadIdx.x; i < vectors; i += kScaleThreads) reinterpret_cast<uint4*>(e)[i] = uint4{};
+        return;
+    }
+    const int parts = (a.z.vocab + 127) / 128;
+    const float2* stats = a.stats + (int64_t)r * 2 * a.tiles_n;
+    float most = -INFINITY;
+    for (int i = threadIdx.x; i < parts; i += kScaleThreads) most = fmaxf(most, stats[i].x);
+#pragma unroll
+    for (int o = 16; o; o /= 2) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+    if (lane == 0) s_part[warp] = most;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kScaleThreads / 32; ++i) most = fmaxf(most, s_part[i]);
+    __syncthreads();
+    float sum = 0.0f;
+    for (int i = threadIdx.x; i < parts; i += kScaleThreads) {
+        const float2 v = stats[i];
+        sum += v.x == -INFINITY ? v.y : v.y * exp2f(v.x - most);      // (v.y is 0 or NaN there)
+    }
+#pragma unroll
+    for (int o = 16; o; o /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (lane == 0) s_part[warp] = sum;
+    __syncthreads();
+    sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kScaleThreads / 32; ++i) sum += s_part[i];
+    const float lse = most + log2f(sum), own = a.label[r];            // in powers of two
+    const float weight = a.weight[a.z.first + r];
+    const int target = a.target[a.z.first + r];
+    constexpr float kLn2 = 0.693147180559945f;
+    if (threadIdx.x == 0) {
+        const float loss = (lse - own) * kLn2;
+        if (a.each) a.each[a.map[a.z.first + r]] = loss;
+        a.share[a.z.first + r] = weight * loss;
+    }
+    if (!e) return;
+    const float c = weight * a.scale * a.head->lift;
+    for (int i = threadIdx.x; i < vectors; i += kScaleThreads) {
+        const float top = stats[i / 16].x;
+        const float f = top == -INFINITY ? c : c * exp2f(top - lse - kUp<T>);
+        float v[8];
+        load(e + i * 8, v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] *= f;
+        if (target / 8 == i) {
+            const float d = c * expm1f((own - lse) * kLn2);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (target % 8 == j) v[j] = d;
+        }
+        store(e + i * 8, v);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- gradients
+
+struct Grads {
+    Sizes z;
+    const Head* head;
+    const int* map;
+    void* dx;                         // NULL: not wanted
+    int64_t lddx;
+    float* dx_parts;                  // [parts][rows of a piece][pitch], where the sums over the vocabulary are split
+    int parts;
+    void* dw;                         // NULL: not wanted
+    int64_t lddw;
+    int add;
+    float* dw_sums;                   // [vocab][pitch], over pieces
+    int more, last;                   // not the first piece, the last piece
+    int64_t pitch;
+    int dx_vector, dw_vector;         // elements that can be accessed at once
+    int* timeouts;
+};
+
+// 32 rows x 32 columns of fp32 from a warp's box (16-byte units swizzled by row) to memory, E neighbours per lane.
+// row, sums_row: where this lane's row lies in `out` and in `sums`, or -1.
+template <typename TO, int E>
+__device__ __forceinline__ void put(const float* box, int64_t row, int64_t sums_row, TO* out, int64_t ld, int64_t col0,
+                                    int64_t cols, float factor, bool add, const float* sums_in, float* sums_out, int64_t pitch) {
+    constexpr int kLanes = 32 / E;
+    const int lane = threadIdx.x & 31, c = lane % kLanes * E;
+    const int64_t col = col0 + c;
+#pragma unroll 2
+    for (int it = 0; it < 32 / E; ++it) {
+        const int r = it * E + lane / kLanes;
+        const int64_t at = __shfl_sync(0xffffffffu, row, r), sums_at = __shfl_sync(0xffffffffu, sums_row, r);
+        if (at < 0 || col >= cols) continue;
+        float v[E];
+        if constexpr (E >= 4) {
+#pragma unroll
+            for (int q = 0; q < E / 4; ++q)
+                *reinterpret_cast<float4*>(v + q * 4) =
+                    *reinterpret_cast<const float4*>(box + r * 32 + (((c / 4 + q) ^ (r & 7)) << 2));
+        } else {
+            v[0] = box[r * 32 + (((c / 4) ^ (r & 7)) << 2) + c % 4];
+        }
+        if (sums_in) {
+            float o[E];
+            if constexpr (E >= 4) load(sums_in + sums_at * pitch + col, o);
+            else o[0] = sums_in[sums_at * pitch + col];
+#pragma unroll
+            for (int j = 0; j < E; ++j) v[j] += o[j];
+        }
+        if (sums_out) {
+            if constexpr (E >= 4) store(sums_out + sums_at * pitch + col, v);
+            else sums_out[sums_at * pitch + col] = v[0];
+            continue;
+        }
+        TO* to = out + at * ld + col;
+#pragma unroll
+        for (int j = 0; j < E; ++j) v[j] *= factor;
+        if constexpr (E >= 4) {
+            if (col + E <= cols) {
+                if (add) {
+                    float o[E];
+                    load(to, o);
+#pragma unroll
+                    for (int j = 0; j < E; ++j) v[j] += o[j];
+                }
+                store(to, v);
+                continue;
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < E; ++j)
+            if (col + j < cols) to[j] = narrow<TO>(add ? v[j] + widen(to[j]) : v[j]);
+    }
+}
+
+template <typename T, typename TW>
+__global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2)
+    grads_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w,
+                 const __grid_constant__ CUtensorMap map_d, const Grads g) {
+    extern __shared__ uint8_t s_raw[];
+    __shared__ Shared s;
+    uint8_t* smem = set_up(s, s_raw);
+    wait_prerequisites();
+    launch_dependents();
+    const int lane = threadIdx.x & 31;
+    const int rows = rows_of_piece(g.z, g.head), tiles_m = (rows + kTile - 1) / kTile;
+    const int tiles_h = (g.z.hidden + kTile - 1) / kTile, tiles_v = (g.z.vocab + kTile - 1) / kTile;
+    const int n_pairs = gridDim.x / 2, pair = blockIdx.x / 2;
+    const int steps_v = (g.z.vocab + kStageK - 1) / kStageK, steps_r = (rows + kStageK - 1) / kStageK;
+    const float unlift = g.head->unlift;
+    // dX first, its long sums split into parts, then dW.  Where the units of dX do not come out even, the pairs with one
+    // less take as many tiles of dW ahead of the others as last as long.
+    const int per_part = tiles_m * tiles_h, n_dx = g.dx ? per_part * g.parts : 0, n_dw = g.dw && steps_r ? tiles_v * tiles_h : 0;
+    const int heavy = n_dx % n_pairs, light = n_pairs - heavy, units = n_dx / n_pairs + (pair < heavy);
+    const int ahead = heavy && steps_r ? max(0, steps_v / g.parts / steps_r) : 0;
+    const int early = (int)min((int64_t)n_dw, (int64_t)ahead * light);
+    const int my_early = pair < heavy ? 0 : max(0, (early - (pair - heavy) + light - 1) / light);
+    const auto next = [&](int it, Job& j) {
+        if (it < units) {
+            const int u = it * n_pairs + pair, part = u / per_part, t = u - part * per_part;
+            j = Job{{&map_d, false, 0}, {&map_w, true, 0}, t % tiles_m, t / tiles_m,
+                    (int)((int64_t)steps_v * part / g.parts), (int)((int64_t)steps_v * (part + 1) / g.parts), 0, part};
+            return true;
+        }
+        it -= units;
+        const int t = it < my_early ? pair - heavy + it * light : early + (it - my_early) * n_pairs + pair;
+        if (t >= n_dw) return false;
+        j = Job{{&map_d, true, 0}, {&map_x, true, g.z.first}, t / tiles_h, t % tiles_h, 0, steps_r, 1, 0};
+        return true;
+    };
+    const auto finish = [&](const Job& j, uint32_t sums, int row_in, int col_in, uint8_t* raw, auto take) {
+        float* box = reinterpret_cast<float*>(raw);
+        const int r = j.ti * kTile + row_in + lane;
+        const bool is_dx = j.kind == 0;
+        int64_t row = -1, sums_row = -1;
+        if (is_dx) {
+            if (r < rows) row = g.map[g.z.first + r], sums_row = (int64_t)j.part * g.z.piece + r;
+        } else if (r < g.z.vocab) {
+            row = sums_row = r;
+        }
+        const float* sums_in = is_dx || !g.more ? nullptr : g.dw_sums;
+        float* sums_out = is_dx ? g.dx_parts : g.last ? nullptr : g.dw_sums;
+#pragma unroll 1
+        for (int q = 0; q < 4; ++q) {
+            uint32_t acc[32];
+            tmem_load32(sums + q * 32, acc);
+            if (q == 3) take();
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                *reinterpret_cast<uint4*>(box + lane * 32 + ((i ^ (lane & 7)) << 2)) =
+                    make_uint4(acc[i * 4], acc[i * 4 + 1], acc[i * 4 + 2], acc[i * 4 + 3]);
+            __syncwarp();
+            const int64_t col = (int64_t)j.tj * kTile + col_in + q * 32;
+            if (is_dx) {
+                T* out = static_cast<T*>(g.dx);
+                if (g.dx_vector == 8) put<T, 8>(box, row, sums_row, out, g.lddx, col, g.z.hidden, unlift, false, sums_in, sums_out, g.pitch);
+                else if (g.dx_vector == 4) put<T, 4>(box, row, sums_row, out, g.lddx, col, g.z.hidden, unlift, false, sums_in, sums_out, g.pitch);
+                else put<T, 1>(box, row, sums_row, out, g.lddx, col, g.z.hidden, unlift, false, sums_in, sums_out, g.pitch);
+            } else {
+                TW* out = static_cast<TW*>(g.dw);
+                if (sizeof(TW) == 2 && g.dw_vector == 8)
+                    put<TW, sizeof(TW) == 2 ? 8 : 4>(box, row, sums_row, out, g.lddw, col, g.z.hidden, unlift, g.add, sums_in, sums_out, g.pitch);
+                else if (g.dw_vector >= 4)
+                    put<TW, 4>(box, row, sums_row, out, g.lddw, col, g.z.hidden, unlift, g.add, sums_in, sums_out, g.pitch);
+                else
+                    put<TW, 1>(box, row, sums_row, out, g.lddw, col, g.z.hidden, unlift, g.add, sums_in, sums_out, g.pitch);
+            }
+            __syncwarp();
+        }
+    };
+    run_jobs<T>(s, smem, next, finish);
+    // a piece without rows has no products: what the pieces before have left, or nothing, is still the gradient
+    if (g.dw && steps_r == 0 && (g.last || !g.more)) {
+        TW* out = static_cast<TW*>(g.dw);
+        for (int64_t r = blockIdx.x; r < g.z.vocab; r += gridDim.x)
+            for (int c = threadIdx.x; c < g.z.hidden; c += kThreads) {
+                const float v = g.more ? g.dw_sums[r * g.pitch + c] : 0.0f;
+                TW* to = out + r * g.lddw + c;
+                if (!g.last) g.dw_sums[r * g.pitch + c] = v;
+                else if (g.add) { if (g.more) *to = narrow<TW>(widen(*to) + v * unlift); }
+                else *to = narrow<TW>(v * unlift);
+            }
+    }
+    tear_down(s, g.timeouts);
+}
+
+// ---------------------------------------------------------------------------------------------- joining
+
+constexpr int kJoinThreads = 256;
+
+// dX = the parts of its sums, in order.
+template <typename T>
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(const Grads g) {
+    wait_prerequisites();
+    launch_dependents();
+    const int rows = rows_of_piece(g.z, g.head), r = blockIdx.x;
+    if (r >= rows) return;
+    const float unlift = g.head->unlift;
+    T* out = static_cast<T*>(g.dx) + g.map[g.z.first + r] * g.lddx;
+    for (int c = (blockIdx.y * kJoinThreads + threadIdx.x) * 4; c < g.z.hidden; c += gridDim.y * kJoinThreads * 4) {
+        const float* p = g.dx_parts + (int64_t)r * g.pitch + c;
+        float v[4];
+        load(p, v);
+        for (int k = 1; k < g.parts; ++k) {
+            float o[4];
+            load(p + (int64_t)k * g.z.piece * g.pitch, o);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] += o[j];
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] *= unlift;
+        if (g.dx_vector >= 4 && c + 4 <= g.z.hidden) {
+            store(out + c, v);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (c + j < g.z.hidden) out[c + j] = narrow<T>(v[j]);
+        }
+    }
+}
+
+constexpr int kTotalThreads = 1024;
+
+__global__ void __launch_bounds__(kTotalThreads) total_kernel(const Head* head, const float* share, float* total) {
+    __shared__ double s_part[kTotalThreads / 32];
+    wait_prerequisites();
+    launch_dependents();
+    double sum = 0.0;
+    for (int i = threadIdx.x; i < head->counted; i += kTotalThreads) sum += share[i];
+#pragma unroll
+    for (int o = 16; o; o /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if ((threadIdx.x & 31) == 0) s_part[threadIdx.x >> 5] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        sum = 0.0;
+        for (int i = 0; i < kTotalThreads / 32; ++i) sum += s_part[i];
+        *total = (float)sum;
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- host side
+
+constexpr int64_t kMostRows = (int64_t)1 << 28, kMostVocab = (int64_t)1 << 28, kMostHidden = (int64_t)1 << 20;
+constexpr int kPairs = 74;            // of a whole B200: what the split of dX is planned for
+
+static int64_t up_to(int64_t n, int64_t step) { return (n + step - 1) / step * step; }
+
+struct Plan {
+    int64_t pitch, e_pitch;           // of the copies of X and W, of e
+    int64_t piece, pieces, tiles_n;
+    int parts;
+    int64_t head, map, target, weight, share, label, stats, x, w, e, dx_parts, dw_sums, bytes;
+    bool countable;                   // its tiles can be counted in 31 bits
+};
+
+// Parts of dX's sums over the vocabulary: the number that ends first, by the longest list of stages of a pair, and what
+// writing and reading the parts takes (a stage lasts 512 cycles, in which an SM pair moves about 24 KB).
+static int parts_of(int64_t rows, int64_t vocab, int64_t hidden, bool dw) {
+    const int64_t tiles_m = (rows + kTile - 1) / kTile, tiles_h = (hidden + kTile - 1) / kTile;
+    const int64_t steps_v = (vocab + kStageK - 1) / kStageK, steps_r = (rows + kStageK - 1) / kStageK;
+    const int64_t work_w = dw ? (vocab + kTile - 1) / kTile * tiles_h * steps_r : 0;
+    int best = 1;
+    double least = 1e300;
+    for (int p = 1; p <= kMostParts && p <= steps_v; ++p) {
+        const int64_t units = tiles_m * tiles_h * p, unit = (steps_v + p - 1) / p;
+        const double alone = (double)((units + kPairs - 1) / kPairs) * unit;
+        const double even = (double)(tiles_m * tiles_h * steps_v + work_w) / kPairs + (dw ? 0.5 * steps_r : 0.0);
+        const double joined = p > 1 ? (double)p * rows * hidden * 8 / kPairs / 24576 + 12 : 0.0;
+        const double cost = std::max(alone, even) + joined;
+        if (cost < least * 0.999) {
+            least = cost;
+            best = p;
+        }
+    }
+    return best;
+}
+
+static Plan plan_of(int64_t rows, int64_t vocab, int64_t hidden, int grads, bool copy_w, int64_t piece_rows) {
+    Plan p{};
+    p.pitch = up_to(hidden, 64);
+    p.e_pitch = up_to(vocab, 64);
+    p.tiles_n = (vocab + kTile - 1) / kTile;
+    if (piece_rows > 0) p.piece = up_to(piece_rows, kTile);
+    else p.piece = std::max<int64_t>(kTile, std::max<int64_t>((int64_t)1 << 29, vocab * p.pitch * 4) / (p.e_pitch * 2) / kTile * kTile);
+    if (!grads && piece_rows <= 0)                                     // (only the statistics: 16 bytes per tile and row)
+        p.piece = std::max<int64_t>(kTile, ((int64_t)1 << 29) / (p.tiles_n * 16) / kTile * kTile);
+    p.piece = std::min(p.piece, up_to(rows, kTile));
+    p.pieces = (rows + p.piece - 1) / p.piece;
+    p.parts = grads & 1 ? parts_of(std::min(rows, p.piece), vocab, hidden, grads & 2) : 1;
+    int64_t at = 0;
+    const auto take = [&](int64_t bytes) {
+        const int64_t here = at;
+        at += up_to(bytes, 256);
+        return here;
+    };
+    p.head = take(sizeof(Head));
+    p.map = take(rows * 4);
+    p.target = take(rows * 4);
+    p.weight = take(rows * 4);
+    p.share = take(rows * 4);
+    p.label = take(p.piece * 4);
+    p.stats = take(p.piece * p.tiles_n * 16);
+    p.x = take(up_to(rows, kStageK) * p.pitch * 2);
+    p.w = take(copy_w ? vocab * p.pitch * 2 : 0);
+    p.e = take(grads ? p.piece * p.e_pitch * 2 : 0);
+    p.dx_parts = take(p.parts > 1 ? p.parts * p.piece * p.pitch * 4 : 0);
+    p.dw_sums = take(grads & 2 && p.pieces > 1 ? vocab * p.pitch * 4 : 0);
+    p.bytes = at;
+    const int64_t most = (int64_t)1 << 30, tiles_h = (hidden + kTile - 1) / kTile, tiles_m = p.piece / kTile;
+    p.countable = tiles_m <= most / p.tiles_n && tiles_h <= most / p.tiles_n && tiles_m <= most / (tiles_h * p.parts);
+    return p;
+}
+
+static int check(int64_t rows, int64_t vocab, int64_t hidden, int64_t piece_rows) {
+    return rows < 0 || vocab < 0 || hidden < 0 || rows > kMostRows || vocab > kMostVocab || hidden > kMostHidden ||
+                   piece_rows < 0 || piece_rows > kMostRows
+               ? SIDCO_E_SIZE
+               : 0;
+}
+
+// W cannot be read in place by tensor copies.
+static bool needs_copy(const void* w, int w_type, int64_t ldw, int type) {
+    return w_type != type || (uintptr_t)w % 16 || ldw * 2 % 16;
+}
+
+static int vector_of(const void* p, int64_t ld, int type) {
+    for (int n = type == SIDCO_T_F32 ? 4 : 8; n > 1; n /= 2)
+        if ((uintptr_t)p % (uintptr_t)(n * size_of(type)) == 0 && ld % n == 0) return n;
+    return 1;
+}
+
+template <typename T, typename TW> static cudaError_t prepare_device(int* pairs) {
+    const auto most = cudaFuncAttributeMaxDynamicSharedMemorySize;
+    cudaError_t e;
+    if ((e = cudaFuncSetAttribute(logits_kernel<T>, most, kSmem)) != cudaSuccess ||
+        (e = cudaFuncSetAttribute(grads_kernel<T, TW>, most, kSmem)) != cudaSuccess)
+        return e;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(2);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = kSmem;
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = 2;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    e = cudaOccupancyMaxActiveClusters(pairs, grads_kernel<T, TW>, &cfg);
+    return e == cudaSuccess && *pairs < 1 ? cudaErrorInvalidConfiguration : e;
+}
+
+struct Call {
+    const void* x;
+    int type;
+    int64_t ldx;
+    const void* w;
+    int w_type;
+    int64_t ldw;
+    const void* labels;
+    int label_type;
+    const float* weights;
+    float scale;
+    int64_t rows, vocab, hidden;
+    float *each, *total;
+    void* dx;
+    int64_t lddx;
+    void* dw;
+    int dw_type;
+    int64_t lddw;
+    int add;
+    int32_t* status;
+    uint8_t* ws;
+    cudaStream_t s;
+};
+
+#define SIDCO_CE_LAUNCH(...)                                     \
+    do {                                                         \
+        const cudaError_t e_ = launch(__VA_ARGS__);              \
+        if (e_ != cudaSuccess) return (int)e_;                   \
+        sidco_internal::note_launch();                           \
+    } while (0)
+
+template <typename T, typename TW> static int run(const Call& c, const Plan& p, bool copy_w) {
+    static std::atomic<int> pairs_of[64];
+    int dev = 0, sms = 0, *timeouts = nullptr;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return (int)e;
+    if (dev < 0 || dev >= 64) return SIDCO_E_SIZE;
+    if (!pairs_of[dev].load()) {             // (setting it twice from two threads is harmless)
+        int n = 0;
+        if ((e = prepare_device<T, TW>(&n)) != cudaSuccess) return (int)e;
+        pairs_of[dev].store(n);
+    }
+    const int pairs = pairs_of[dev].load();
+    if ((e = cudaGetSymbolAddress((void**)&timeouts, g_timeouts)) != cudaSuccess ||
+        (e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess)
+        return (int)e;
+    Head* head = reinterpret_cast<Head*>(c.ws + p.head);
+    int *map = reinterpret_cast<int*>(c.ws + p.map), *target = reinterpret_cast<int*>(c.ws + p.target);
+    float* weight = reinterpret_cast<float*>(c.ws + p.weight);
+    const void* w = copy_w ? c.ws + p.w : c.w;
+    const int64_t w_pitch = copy_w ? p.pitch : c.ldw;
+    const bool grads = c.dx || c.dw;
+
+    Prepare a{};
+    a.x = c.x, a.ldx = c.ldx, a.w = c.w, a.ldw = c.ldw, a.labels = c.labels, a.wide = c.label_type == SIDCO_T_I64;
+    a.weights = c.weights, a.scale = c.scale;
+    a.rows = (int)c.rows, a.vocab = (int)c.vocab, a.hidden = (int)c.hidden, a.pitch = p.pitch;
+    a.x_to = c.ws + p.x, a.w_to = copy_w ? c.ws + p.w : nullptr;
+    a.dx = c.dx, a.lddx = c.lddx, a.each = c.each, a.head = head, a.map = map, a.target = target, a.weight = weight;
+    a.status = c.status;
+    a.x_blocks = (int)std::min<int64_t>(c.rows, sms), a.x_rows = (int)((c.rows + a.x_blocks - 1) / a.x_blocks);
+    a.x_vector = vector_of(c.x, c.ldx, c.type), a.w_vector = vector_of(c.w, c.ldw, c.w_type);
+    a.dx_vector = vector_of(c.dx, c.lddx, c.type);
+    const unsigned blocks = (unsigned)(a.x_blocks + (copy_w ? std::min<int64_t>((c.vocab + 7) / 8, 6 * sms) : 0));
+    if (c.w_type == SIDCO_T_F32) SIDCO_CE_LAUNCH(prepare_kernel<T, float>, dim3(blocks), kPrepareThreads, 0, c.s, 1, a);
+    else SIDCO_CE_LAUNCH(prepare_kernel<T, T>, dim3(blocks), kPrepareThreads, 0, c.s, 1, a);
+
+    CUtensorMap map_x, map_w, map_e{}, map_d{};
+    if (!sidco_internal::byte_map(&map_x, c.ws + p.x, c.hidden * 2, up_to(c.rows, kStageK), p.pitch * 2, 128, 64, true) ||
+        !sidco_internal::byte_map(&map_w, w, c.hidden * 2, c.vocab, w_pitch * 2, 128, 64, true) ||
+        (grads && (!sidco_internal::out_map(&map_e, c.ws + p.e, c.type, p.e_pitch, p.piece, p.e_pitch, 64, 32) ||
+                   !sidco_internal::byte_map(&map_d, c.ws + p.e, c.vocab * 2, p.piece, p.e_pitch * 2, 128, 64, true))))
+        return SIDCO_E_UNSUPPORTED;
+    float* share = reinterpret_cast<float*>(c.ws + p.share);
+    for (int64_t i = 0; i < p.pieces; ++i) {
+        const Sizes z{(int)c.rows, (int)c.vocab, (int)c.hidden, (int)p.piece, (int)(i * p.piece)};
+        const int64_t most = std::min(p.piece, c.rows - z.first);      // rows if all have labels
+        Logits l{z, head, target, c.scale * 1.44269504088896f, reinterpret_cast<float2*>(c.ws + p.stats), (int)p.tiles_n,
+                 reinterpret_cast<float*>(c.ws + p.label), grads, timeouts};
+        const int64_t tiles = (most + kTile - 1) / kTile * p.tiles_n;
+        SIDCO_CE_LAUNCH(logits_kernel<T>, dim3((unsigned)(2 * std::min<int64_t>(pairs, tiles))), kThreads, kSmem, c.s, 1, map_x,
+                        map_w, map_e, l);
+        Scale k{z, head, map, target, weight, c.scale, l.stats, l.tiles_n, l.label, grads ? c.ws + p.e : nullptr, p.e_pitch,
+                c.each, share};
+        SIDCO_CE_LAUNCH(scale_kernel<T>, dim3((unsigned)up_to(most, kStageK)), kScaleThreads, 0, c.s, 1, k);
+        if (!grads) continue;
+        Grads g{z, head, map, c.dx, c.lddx, p.parts > 1 ? reinterpret_cast<float*>(c.ws + p.dx_parts) : nullptr, p.parts, c.dw,
+                c.lddw, c.add, p.pieces > 1 ? reinterpret_cast<float*>(c.ws + p.dw_sums) : nullptr, i > 0, i + 1 == p.pieces,
+                p.pitch, vector_of(c.dx, c.lddx, c.type), vector_of(c.dw, c.lddw, c.dw_type), timeouts};
+        SIDCO_CE_LAUNCH((grads_kernel<T, TW>), dim3(2 * (unsigned)pairs), kThreads, kSmem, c.s, 1, map_x, map_w, map_d, g);
+        if (c.dx && p.parts > 1)
+            SIDCO_CE_LAUNCH(join_kernel<T>, dim3((unsigned)most, (unsigned)((c.hidden + 1023) / 1024)), kJoinThreads, 0, c.s, 1, g);
+    }
+    if (c.total) SIDCO_CE_LAUNCH(total_kernel, dim3(1), kTotalThreads, 0, c.s, 1, head, share, c.total);
+    return 0;
+}
+
+}  // namespace sidco_ce
+
+int sidco_internal::cross_entropy_timeouts(int* count) {
+    return (int)cudaMemcpyFromSymbol(count, sidco_ce::g_timeouts, sizeof(int));
+}
+
+extern "C" {
+
+int64_t sidco_linear_cross_entropy_workspace_bytes(const void* w, int type, int w_type, int64_t ldw, int64_t rows, int64_t vocab,
+                                                   int64_t hidden, int grads, int64_t piece_rows) {
+    using namespace sidco_ce;
+    if (check(rows, vocab, hidden, piece_rows)) return SIDCO_E_SIZE;
+    if ((type != SIDCO_T_BF16 && type != SIDCO_T_F16) || (w_type != SIDCO_T_F32 && w_type != type)) return SIDCO_E_TYPE;
+    if (grads < 0 || grads > 3 || ldw < hidden) return SIDCO_E_PARAMS;
+    if (rows == 0 || vocab == 0 || hidden == 0) return 0;
+    const Plan p = plan_of(rows, vocab, hidden, grads, needs_copy(w, w_type, ldw, type), piece_rows);
+    return p.countable ? p.bytes : SIDCO_E_SIZE;
+}
+
+int sidco_linear_cross_entropy(const void* x, int type, int64_t ldx, const void* w, int w_type, int64_t ldw, const void* labels,
+                               int label_type, const float* row_weights, float scale, int64_t rows, int64_t vocab,
+                               int64_t hidden, float* row_losses, float* loss, void* dx, int64_t lddx, void* dw, int dw_type,
+                               int64_t lddw, int add_dw, int64_t piece_rows, int32_t* status, void* workspace,
+                               size_t workspace_bytes, void* stream) {
+    using namespace sidco_ce;
+    if (const int rc = check(rows, vocab, hidden, piece_rows)) return rc;
+    if ((type != SIDCO_T_BF16 && type != SIDCO_T_F16) || (w_type != SIDCO_T_F32 && w_type != type) ||
+        (dw && dw_type != SIDCO_T_F32 && dw_type != type) || (label_type != SIDCO_T_I32 && label_type != SIDCO_T_I64))
+        return SIDCO_E_TYPE;
+    if (ldx < hidden || ldw < hidden || (dx && lddx < hidden) || (dw && lddw < hidden) || !(scale - scale == 0.0f))
+        return SIDCO_E_PARAMS;
+    if (hidden == 0 || vocab == 0) return SIDCO_E_SIZE;
+    const int64_t label_size = label_type == SIDCO_T_I64 ? 8 : 4;
+    if (rows > 0 && (!x || !w || !labels)) return SIDCO_E_NULL;
+    if ((uintptr_t)x % 2 || (uintptr_t)dx % 2 || (uintptr_t)w % size_of(w_type) || (dw && (uintptr_t)dw % size_of(dw_type)) ||
+        (uintptr_t)labels % (uintptr_t)label_size || (uintptr_t)row_weights % 4 || (uintptr_t)row_losses % 4 ||
+        (uintptr_t)loss % 4 || (uintptr_t)status % 4)
+        return SIDCO_E_ALIGN;
+    cudaStream_t s = (cudaStream_t)stream;
+    const int grads = (dx ? 1 : 0) | (dw ? 2 : 0);
+    const bool copy_w = needs_copy(w, w_type, ldw, type);
+    if (rows > 0) {
+        const Plan p = plan_of(rows, vocab, hidden, grads, copy_w, piece_rows);
+        if (!p.countable) return SIDCO_E_SIZE;
+        if (!workspace || workspace_bytes < (size_t)p.bytes || (uintptr_t)workspace % 256) return SIDCO_E_WORKSPACE;
+        // every buffer that is written against every other
+        const struct { const void* p; int64_t bytes; bool out; } all[] = {
+            {dx, extent(rows, hidden, lddx, type), true}, {dw, extent(vocab, hidden, lddw, dw_type), true},
+            {row_losses, rows * 4, true},                 {loss, 4, true},
+            {workspace, p.bytes, true},                   {status, 4, true},
+            {x, extent(rows, hidden, ldx, type), false},  {w, extent(vocab, hidden, ldw, w_type), false},
+            {labels, rows * label_size, false},           {row_weights, rows * 4, false}};
+        const int n = (int)(sizeof(all) / sizeof(all[0]));
+        for (int i = 0; i < n; ++i)
+            for (int k = i + 1; k < n; ++k)
+                if (all[i].out && overlap(all[i].p, all[i].bytes, all[k].p, all[k].bytes)) return SIDCO_E_ALIAS;
+        if (status) {
+            const cudaError_t e = cudaMemsetAsync(status, 0, sizeof(int32_t), s);
+            if (e != cudaSuccess) return (int)e;
+        }
+        const Call c{x, type, ldx, w, w_type, ldw, labels, label_type, row_weights, scale, rows, vocab, hidden, row_losses, loss,
+                     dx, lddx, dw, dw_type, lddw, add_dw != 0, status, static_cast<uint8_t*>(workspace), s};
+        if (type == SIDCO_T_BF16)
+            return dw && dw_type == SIDCO_T_F32 ? run<__nv_bfloat16, float>(c, p, copy_w) : run<__nv_bfloat16, __nv_bfloat16>(c, p, copy_w);
+        return dw && dw_type == SIDCO_T_F32 ? run<__half, float>(c, p, copy_w) : run<__half, __half>(c, p, copy_w);
+    }
+    // no rows: no loss, no gradient
+    cudaError_t e = cudaSuccess;
+    if (status) e = cudaMemsetAsync(status, 0, sizeof(int32_t), s);
+    if (e == cudaSuccess && loss) e = cudaMemsetAsync(loss, 0, sizeof(float), s);
+    if (e == cudaSuccess && dw && !add_dw)
+        e = cudaMemset2DAsync(dw, lddw * size_of(dw_type), 0, hidden * size_of(dw_type), vocab, s);
+    return (int)e;
+}
+
+}  // extern "C"

@@ -20,5 +20,6 @@ bool out_map(CUtensorMap* map, void* base, int type, int64_t width, int64_t rows
 // How many CTAs of the product kernels gave up a bounded wait on the current device (synchronises it).
 int orthogonalize_timeouts(int* count);
 int mx4_matmul_timeouts(int* count);
+int cross_entropy_timeouts(int* count);
 
 }  // namespace sidco_internal

@@ -698,10 +698,11 @@ int sidco_mx4_matmul(const uint8_t* a_codes, const uint8_t* a_scales, const uint
 }
 
 int sidco_wait_timeouts(void) {
-    int a = 0, b = 0, rc;
-    if ((rc = sidco_internal::orthogonalize_timeouts(&a)) || (rc = sidco_internal::mx4_matmul_timeouts(&b)))
+    int a = 0, b = 0, c = 0, rc;
+    if ((rc = sidco_internal::orthogonalize_timeouts(&a)) || (rc = sidco_internal::mx4_matmul_timeouts(&b)) ||
+        (rc = sidco_internal::cross_entropy_timeouts(&c)))
         return rc > 0 ? -rc : rc;
-    return a + b;
+    return a + b + c;
 }
 
 }  // extern "C"

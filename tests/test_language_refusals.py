@@ -100,3 +100,65 @@ def test_embedding_grad_refuses(B):
     assert code(g, W, 8, P, 4, 9, 8, 1., Q, 8, W, need, **kw) == -9
     assert code(g, P, 8, W + 256, 4, 9, 8, 1., Q, 8, W, need, **kw) == -9
     assert code(g, P, 8, P, 4, 9, 8, 1., W, 8, W, need, **kw) == -9
+
+
+def test_cross_entropy_refuses(B):
+    f = B.sidco_linear_cross_entropy
+    x, w, y, each, loss, dx, dw, ws, c = (0x10000000 * (i + 1) for i in range(9))
+    kw = dict(x_type=1, w_type=1, label_type=4, dw_type=1)
+    need = B.sidco_linear_cross_entropy_workspace_bytes(0, w, 8, 4, 9, 8, x_type=1, w_type=1)
+
+    def args(**k):
+        a = dict(x=x, ldx=8, w=w, ldw=8, labels=y, rows=4, vocab=9, hidden=8, each=each, loss=loss, dx=dx, lddx=8, dw=dw,
+                 lddw=8, ws=ws, need=need)
+        a.update({n: v for n, v in k.items() if n in a})
+        return list(a.values()), {**kw, **{n: v for n, v in k.items() if n not in a}}
+
+    def refused(**k):
+        a, b = args(**k)
+        return code(f, *a, **b)
+    for n in ("rows", "vocab", "hidden"):
+        assert refused(**{n: -1}) == -10
+    assert refused(rows=(1 << 28) + 1) == -10 and refused(vocab=(1 << 28) + 1) == -10 and refused(piece_rows=-1) == -10
+    assert refused(hidden=(1 << 20) + 1, ldx=1 << 21) == -10
+    assert refused(vocab=0) == -10 and refused(hidden=0) == -10
+    assert refused(vocab=1 << 28, hidden=1 << 20, ldx=1 << 20, ldw=1 << 20, lddx=1 << 20, lddw=1 << 20) == -10      # too many tiles
+    for t in (0, 3, -1):
+        assert refused(x_type=t) == -13
+    assert refused(w_type=2) == -13 and refused(dw_type=2) == -13 and refused(label_type=0) == -13
+    assert refused(x_type=2, w_type=0, dw_type=1) == -13
+    for n in ("ldx", "ldw", "lddx", "lddw"):
+        assert refused(**{n: 7}) == -6
+    for s in (NAN, float("inf")):
+        assert refused(scale=s) == -6
+    for n in ("x", "w", "labels"):
+        assert refused(**{n: None}) == -1
+    for n, v in (("x", x), ("w", w), ("dx", dx), ("dw", dw), ("labels", y), ("each", each), ("loss", loss)):
+        assert refused(**{n: v + 1}) == -14
+    assert refused(labels=y + 4) == -14 and refused(row_weights=c + 2) == -14 and refused(status=c + 2) == -14
+    assert refused(w=w + 2, w_type=0) == -14
+    assert refused(ws=None) == -8 and refused(need=need - 1) == -8 and refused(ws=ws + 128) == -8
+    assert refused(w=w + 8) == -8                                  # its copy does not fit
+    assert refused(dx=x) == -9 and refused(dw=w) == -9 and refused(each=dw + 9 * 16 - 4) == -9
+    assert refused(ws=x) == -9 and refused(loss=each + 12) == -9 and refused(row_weights=each) == -9
+    assert refused(dx=ws + 256) == -9 and refused(status=loss) == -9 and refused(labels=dx + 56) == -9
+
+    size = B.sidco_linear_cross_entropy_workspace_bytes
+    plain = size(0, 0, 1504, 700, 10000, 1500, x_type=1, w_type=1)
+    assert 700 * 10000 * 2 < plain < 80 << 20
+    assert size(0, 0, 1500, 700, 10000, 1500, x_type=1, w_type=1) >= plain + 10000 * 1500 * 2      # W is copied
+    assert size(0, 0, 1504, 700, 10000, 1500, x_type=1, w_type=0) >= plain + 10000 * 1500 * 2
+    assert size(0, 0, 1504, 700, 10000, 1500, grads=False, x_type=1, w_type=1) < 6 << 20
+    # e never takes more than 512 MB or the gradient of w in 32 bits
+    assert size(0, 0, 64, 1 << 20, 50000, 64, x_type=1, w_type=1) < (1 << 29) + (1 << 20) * 64 * 2 + 50000 * 64 * 4 + (400 << 20)
+    for bad in (dict(rows=-1), dict(vocab=-1), dict(piece_rows=-1), dict(rows=1 << 29)):
+        a = dict(ldw=8, rows=4, vocab=9, hidden=8)
+        a.update(bad)
+        with pytest.raises(B.SidcoError) as e:
+            size(0, 0, x_type=1, w_type=1, **a)
+        assert e.value.code == -10
+    for bad, want in ((dict(x_type=0, w_type=1), -13), (dict(x_type=1, w_type=2), -13), (dict(x_type=1, w_type=1, grads=4), -6)):
+        with pytest.raises(B.SidcoError) as e:
+            size(0, 0, 8, 4, 9, 8, **bad)
+        assert e.value.code == want
+    assert size(0, 0, 8, 0, 9, 8, x_type=1, w_type=1) == 0
