@@ -9,9 +9,9 @@
 //   logits_kernel   tiles of X W^T; of each half of a tile's columns the largest logit and the sum of exponentials, and
 //                   with gradients e = exp(s - largest) in 16 bits
 //   scale_kernel    lse and loss of a row; e becomes D in place; the entry of the label is computed from its fp32 logit
-//   grads_kernel    dX and dW as one list of tiles
+//                   (without gradients loss_kernel: losses only, the last row adds up the total)
+//   grads_kernel    dX and dW as one list of tiles, and the total
 //   join_kernel     adds the parts of dX where its sums over the vocabulary were split
-//   total_kernel    the total
 //
 // Why not the logits, or a second product in place of e: e is a relative quantity, so 16 bits cost it half a step of 2^-8
 // (bf16) or 2^-11 (fp16) whatever the size of the logit, and reading and writing it once costs a tenth of computing the
@@ -47,11 +47,14 @@ constexpr int kBox = 32 * 128;        // of an epilogue warp
 constexpr int kThreads = 320;
 constexpr int kSmem = kStages * kStageBytes + 8 * kBox + 1024;
 constexpr int kMostParts = 16;
+constexpr int kPairs = 74;            // of a whole B200: what the split of dX is planned for
 
 struct Head {                         // written by prepare_kernel
     int counted;                      // rows with a label
     float lift, unlift;               // power of two that D is stored times, and its inverse
     float mean;                       // 1 / counted
+    int done;                         // rows whose loss is known
+    int parts;                        // of dX's sums, for the piece at work (scale_kernel)
 };
 
 struct Sizes {
@@ -74,6 +77,8 @@ __device__ __forceinline__ float exp2_fast(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+
+__device__ __forceinline__ void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 
 template <typename T> __device__ __forceinline__ uint32_t pack2(float a, float b);
 template <> __device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float a, float b) {
@@ -104,57 +109,122 @@ struct Prepare {
     void* w_to;                       // NULL: W is used where it is
     void* dx;                         // NULL: not wanted
     int64_t lddx;
-    float* each;                      // NULL: not wanted
+    float *each, *total;              // NULL: not wanted
     Head* head;
     int *map, *target;
     float* weight;
     int32_t* status;
     int x_blocks, x_rows;             // CTAs for the rows of X, rows of each
-    int x_vector, w_vector, dx_vector;
+    int w_vector, dx_vector;          // rows can be accessed 16 bytes at once
 };
 
-// One warp copies a row, `vector` elements at a time.
-template <typename TI, typename TO, int V>
-__device__ __forceinline__ void copy_vectors(const TI* from, TO* to, int cols, int lane) {
-    const int whole = cols / V;
-#pragma unroll 4
-    for (int i = lane; i < whole; i += 32) {
-        alignas(16) TI a[V];
-        alignas(16) TO b[V];
-        constexpr int kBytes = V * (int)sizeof(TI);
-        if constexpr (kBytes == 16) *reinterpret_cast<uint4*>(a) = *reinterpret_cast<const uint4*>(from + i * V);
-        else if constexpr (kBytes == 8) *reinterpret_cast<uint2*>(a) = *reinterpret_cast<const uint2*>(from + i * V);
-        else if constexpr (kBytes == 4) *reinterpret_cast<uint32_t*>(a) = *reinterpret_cast<const uint32_t*>(from + i * V);
-        else a[0] = from[i];
-        constexpr int kOut = V * (int)sizeof(TO);
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            if constexpr (std::is_same<TI, TO>::value) b[j] = a[j];
-            else b[j] = narrow<TO>(widen(a[j]));
-        }
-        if constexpr (kOut == 16) *reinterpret_cast<uint4*>(to + i * V) = *reinterpret_cast<const uint4*>(b);
-        else if constexpr (kOut == 8) *reinterpret_cast<uint2*>(to + i * V) = *reinterpret_cast<const uint2*>(b);
-        else if constexpr (kOut == 4) *reinterpret_cast<uint32_t*>(to + i * V) = *reinterpret_cast<const uint32_t*>(b);
-        else to[i] = b[0];
+// An aligned 16 bytes in elements of kSize, of which some may lie outside [lo, hi): those are not read.
+template <int kSize> __device__ __noinline__ uint4 load_edge(uintptr_t at, uintptr_t lo, uintptr_t hi) {
+    uint64_t h[2] = {};
+#pragma unroll 1
+    for (int b = 0; b < 16; b += kSize) {
+        const uintptr_t p = at + b;
+        uint64_t v = 0;
+        if (p >= lo && p < hi) v = kSize == 2 ? *reinterpret_cast<const uint16_t*>(p) : *reinterpret_cast<const uint32_t*>(p);
+        if (b < 8) h[0] |= v << (8 * b);
+        else h[1] |= v << (8 * (b - 8));
     }
-    for (int i = whole * V + lane; i < cols; i += 32) {
-        if constexpr (std::is_same<TI, TO>::value) to[i] = from[i];
-        else to[i] = narrow<TO>(widen(from[i]));
+    return make_uint4((uint32_t)h[0], (uint32_t)(h[0] >> 32), (uint32_t)h[1], (uint32_t)(h[1] >> 32));
+}
+
+// N words that start `shift` bytes (even, below 16) into w.
+template <int N> __device__ __forceinline__ void shift_words(uint32_t (&w)[N + 4], int shift) {
+    if (shift & 4) {
+#pragma unroll
+        for (int i = 0; i < N + 3; ++i) w[i] = w[i + 1];
+    }
+    if (shift & 8) {
+#pragma unroll
+        for (int i = 0; i < N + 2; ++i) w[i] = w[i + 2];
+    }
+    const int bits = (shift & 2) * 8;
+#pragma unroll
+    for (int i = 0; i < N; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], bits);
+}
+
+constexpr int kCopyAhead = 4;
+
+// One warp copies a row of 16-bit elements of any alignment to an aligned one whose padding may be written too: aligned
+// 16-byte reads, put together from two neighbours.  [lo, hi): the matrix.
+__device__ __forceinline__ void copy_bits(const void* from, void* to, int cols, uintptr_t lo, uintptr_t hi, int lane) {
+    const uintptr_t start = (uintptr_t)from & ~(uintptr_t)15;
+    const int shift = (int)((uintptr_t)from & 15), units = (cols + 7) / 8;
+    if (start < lo || start + 16 * (units + 1) > hi) {                // the first and the last row: single elements
+        for (int i0 = lane; i0 < cols; i0 += 32 * 16) {
+            uint16_t v[16];
+#pragma unroll
+            for (int k = 0; k < 16; ++k) v[k] = static_cast<const uint16_t*>(from)[min(i0 + k * 32, cols - 1)];
+#pragma unroll
+            for (int k = 0; k < 16; ++k)
+                if (i0 + k * 32 < cols) static_cast<uint16_t*>(to)[i0 + k * 32] = v[k];
+        }
+    } else if (shift) {
+        for (int i0 = lane; i0 < units; i0 += 32 * kCopyAhead) {
+            uint4 a[kCopyAhead], b[kCopyAhead];                       // (all reads before the first write)
+#pragma unroll
+            for (int k = 0; k < kCopyAhead; ++k) {
+                const int i = min(i0 + k * 32, units - 1);
+                a[k] = reinterpret_cast<const uint4*>(start)[i];
+                b[k] = reinterpret_cast<const uint4*>(start)[i + 1];
+            }
+#pragma unroll
+            for (int k = 0; k < kCopyAhead; ++k) {
+                uint32_t w[8] = {a[k].x, a[k].y, a[k].z, a[k].w, b[k].x, b[k].y, b[k].z, b[k].w};
+                shift_words<4>(w, shift);
+                if (i0 + k * 32 < units) static_cast<uint4*>(to)[i0 + k * 32] = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+        }
+    } else {
+        for (int i0 = lane; i0 < units; i0 += 32 * kCopyAhead) {
+            uint4 a[kCopyAhead];
+#pragma unroll
+            for (int k = 0; k < kCopyAhead; ++k) a[k] = reinterpret_cast<const uint4*>(start)[min(i0 + k * 32, units - 1)];
+#pragma unroll
+            for (int k = 0; k < kCopyAhead; ++k)
+                if (i0 + k * 32 < units) static_cast<uint4*>(to)[i0 + k * 32] = a[k];
+        }
     }
 }
 
-template <typename TI, typename TO>
-__device__ __forceinline__ void copy_row(const TI* from, TO* to, int cols, int vector, int lane) {
-    if (sizeof(TI) == 2 && vector == 8) copy_vectors<TI, TO, sizeof(TI) == 2 ? 8 : 4>(from, to, cols, lane);
-    else if (vector >= 4) copy_vectors<TI, TO, 4>(from, to, cols, lane);
-    else if (vector == 2) copy_vectors<TI, TO, sizeof(TI) == 2 ? 2 : 1>(from, to, cols, lane);
-    else copy_vectors<TI, TO, 1>(from, to, cols, lane);
+template <typename T, typename TI>
+__device__ __forceinline__ void copy_row(const TI* from, T* to, int cols, bool vector, uintptr_t lo, uintptr_t hi, int lane) {
+    if constexpr (std::is_same<T, TI>::value) {
+        copy_bits(from, to, cols, lo, hi, lane);
+    } else {
+        if (vector) {                                                 // four fp32 at a time
+            const int whole = cols / 4;
+            for (int i0 = lane; i0 < whole; i0 += 32 * kCopyAhead) {
+                float4 v[kCopyAhead];
+#pragma unroll
+                for (int k = 0; k < kCopyAhead; ++k) v[k] = reinterpret_cast<const float4*>(from)[min(i0 + k * 32, whole - 1)];
+#pragma unroll
+                for (int k = 0; k < kCopyAhead; ++k)
+                    if (i0 + k * 32 < whole)
+                        reinterpret_cast<uint2*>(to)[i0 + k * 32] = make_uint2(pack2<T>(v[k].x, v[k].y), pack2<T>(v[k].z, v[k].w));
+            }
+            for (int i = whole * 4 + lane; i < cols; i += 32) to[i] = narrow<T>(from[i]);
+        } else {
+            for (int i0 = lane; i0 < cols; i0 += 32 * kCopyAhead) {
+                float v[kCopyAhead];
+#pragma unroll
+                for (int k = 0; k < kCopyAhead; ++k) v[k] = from[min(i0 + k * 32, cols - 1)];
+#pragma unroll
+                for (int k = 0; k < kCopyAhead; ++k)
+                    if (i0 + k * 32 < cols) to[i0 + k * 32] = narrow<T>(v[k]);
+            }
+        }
+    }
 }
 
 template <typename T>
-__device__ __forceinline__ void zero_row(T* to, int cols, int vector, int lane) {
+__device__ __forceinline__ void zero_row(T* to, int cols, bool vector, int lane) {
     const T zero = narrow<T>(0.0f);
-    if (vector == 8) {
+    if (vector) {
         for (int i = lane; i < cols / 8; i += 32) reinterpret_cast<uint4*>(to)[i] = uint4{};
         for (int i = cols / 8 * 8 + lane; i < cols; i += 32) to[i] = zero;
     } else {
@@ -186,7 +256,8 @@ __global__ void __launch_bounds__(kPrepareThreads) prepare_kernel(const Prepare 
     if ((int)blockIdx.x >= a.x_blocks) {
         const int64_t workers = (int64_t)(gridDim.x - a.x_blocks) * (kPrepareThreads / 32);
         for (int64_t r = (int64_t)(blockIdx.x - a.x_blocks) * (kPrepareThreads / 32) + warp; r < a.vocab; r += workers)
-            copy_row(static_cast<const TW*>(a.w) + r * a.ldw, static_cast<T*>(a.w_to) + r * a.pitch, a.hidden, a.w_vector, lane);
+            copy_row(static_cast<const TW*>(a.w) + r * a.ldw, static_cast<T*>(a.w_to) + r * a.pitch, a.hidden, a.w_vector,
+                     (uintptr_t)a.w, (uintptr_t)(static_cast<const TW*>(a.w) + (a.vocab - 1) * a.ldw + a.hidden), lane);
         return;
     }
     // labelled rows before this CTA's and in all; the largest weight (every CTA counts for itself: nobody waits)
@@ -209,6 +280,9 @@ __global__ void __launch_bounds__(kPrepareThreads) prepare_kernel(const Prepare 
             Head h;
             h.counted = all;
             h.mean = all ? 1.0f / (float)all : 0.0f;
+            h.done = 0;
+            h.parts = 1;
+            if (!all && a.total) *a.total = 0.0f;                     // (otherwise the last row's CTA writes it)
             for (int i = 0; i < kPrepareThreads / 32; ++i) most = max(most, s_most[i]);
             // fp16: the largest |c scale| is brought to [2^13, 2^14) as far as the powers of two reach, so that D keeps
             // eleven bits down to 2^-28 of it
@@ -224,7 +298,7 @@ __global__ void __launch_bounds__(kPrepareThreads) prepare_kernel(const Prepare 
         // the rows behind the last, up to a whole step of the products over rows
         const int up = (all + kStageK - 1) / kStageK * kStageK;
         for (int r = all + warp; r < up; r += kPrepareThreads / 32)
-            zero_row(static_cast<T*>(a.x_to) + r * a.pitch, a.hidden, 8, lane);
+            zero_row(static_cast<T*>(a.x_to) + r * a.pitch, a.hidden, true, lane);
     }
     for (int r0 = first; r0 < end; r0 += kPrepareThreads) {
         const int r = r0 + threadIdx.x;
@@ -244,15 +318,15 @@ __global__ void __launch_bounds__(kPrepareThreads) prepare_kernel(const Prepare 
         if (has) {
             a.map[to] = r;
             a.target[to] = (int)y;
-            a.weight[to] = a.weights ? a.weights[r] : all ? 1.0f / (float)all : 0.0f;
+            a.weight[to] = a.weights ? a.weights[r] : 1.0f / (float)all;
         } else if (r < end && a.each) {
             a.each[r] = 0.0f;
         }
         __syncthreads();
         for (int i = warp; i < min(kPrepareThreads, end - r0); i += kPrepareThreads / 32) {
             if (s_to[i] >= 0)
-                copy_row(static_cast<const T*>(a.x) + (r0 + i) * a.ldx, static_cast<T*>(a.x_to) + s_to[i] * a.pitch, a.hidden,
-                         a.x_vector, lane);
+                copy_bits(static_cast<const T*>(a.x) + (r0 + i) * a.ldx, static_cast<T*>(a.x_to) + s_to[i] * a.pitch, a.hidden,
+                          (uintptr_t)a.x, (uintptr_t)(static_cast<const T*>(a.x) + (a.rows - 1) * a.ldx + a.hidden), lane);
             else if (a.dx)
                 zero_row(static_cast<T*>(a.dx) + (r0 + i) * a.lddx, a.hidden, a.dx_vector, lane);
         }
@@ -293,6 +367,7 @@ struct Job {                          // a tile, or a part of K of one
     Operand a, b;
     int ti, tj, from, to;             // stages
     int kind, part;
+    bool dry;                         // the way out is only walked through
 };
 
 struct Shared {
@@ -302,9 +377,9 @@ struct Shared {
 };
 
 // The three roles over the jobs that next(it, job) gives; finish(job, sums, quarter, half, take) takes a tile's sums out and
-// calls take() when it has read them.
-template <typename T, typename Next, typename Finish>
-__device__ __forceinline__ void run_jobs(Shared& s, uint8_t* smem, Next next, Finish finish) {
+// calls take() when it has read them; ahead(job, row, column) comes before the sums are there.
+template <typename T, typename Next, typename Finish, typename Ahead>
+__device__ __forceinline__ void run_jobs(Shared& s, uint8_t* smem, Next next, Finish finish, Ahead ahead) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank(), stage0 = smem_addr(smem), tmem = s.tmem;
     Job j;
@@ -359,16 +434,22 @@ __device__ __forceinline__ void run_jobs(Shared& s, uint8_t* smem, Next next, Fi
     } else {
         const int quarter = warp & 3, half = (warp - 2) >> 2;
         const uint32_t taken[2] = {in_cta(smem_addr(&s.taken[0]), 0), in_cta(smem_addr(&s.taken[1]), 0)};
-        for (int it = 0; next(it, j); ++it) {
+        // Before the first sums are there, the way out is walked through once without writing anything: its instructions then
+        // lie in the SM's caches when the first tile is done (the first tile took 7 us instead of 4).
+        for (int it = -1; next(max(it, 0), j); ++it) {
             const int buf = it & 1;
-            bool ok = mbar_wait(smem_addr(&s.sums[buf]), (it >> 1) & 1, &s.failed);
-            if (!__all_sync(0xffffffffu, ok)) break;
-            fence_after_sync();
+            j.dry = it < 0;
+            if (it >= 0) {
+                ahead(j, (int)rank * 128 + quarter * 32, half * 128);
+                const bool ok = mbar_wait(smem_addr(&s.sums[buf]), (it >> 1) & 1, &s.failed);
+                if (!__all_sync(0xffffffffu, ok)) break;
+                fence_after_sync();
+            }
             finish(j, tmem + buf * kTile + half * 128 + ((uint32_t)(quarter * 32) << 16), (int)rank * 128 + quarter * 32,
                    half * 128, smem + kStages * kStageBytes + (warp - 2) * kBox, [&] {
                        fence_before_sync();
                        __syncwarp();
-                       if (lane == 0) mbar_arrive_cluster(taken[buf]);
+                       if (lane == 0 && it >= 0) mbar_arrive_cluster_relaxed(taken[buf]);
                    });
         }
     }
@@ -440,16 +521,18 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2)
         const int64_t i = blockIdx.x / 2 + (int64_t)it * n_pairs;
         if (i >= total) return false;
         const int per = 8 * g.tiles_n, band = (int)(i / per), in = (int)(i - (int64_t)band * per), high = min(8, tiles_m - band * 8);
-        j = Job{{&map_x, false, g.z.first}, {&map_w, false, 0}, band * 8 + in % high, in / high, 0, stages, 0, 0};
+        j = Job{{&map_x, false, g.z.first}, {&map_w, false, 0}, band * 8 + in % high, in / high, 0, stages, 0, 0, false};
         return true;
     };
     const auto finish = [&](const Job& j, uint32_t sums, int row_in, int col_in, uint8_t* box, auto take) {
         const int r0 = j.ti * kTile + row_in, r = r0 + lane, c0 = j.tj * kTile + col_in;
         uint32_t acc[128];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) tmem_load32(sums + q * 32, *reinterpret_cast<uint32_t(*)[32]>(acc + q * 32));
+        for (int q = 0; q < 4; ++q) tmem_load32_async(sums + q * 32, *reinterpret_cast<uint32_t(*)[32]>(acc + q * 32));
+#pragma unroll
+        for (int q = 0; q < 4; ++q) tmem_load_wait(*reinterpret_cast<uint32_t(*)[32]>(acc + q * 32));
         take();
-        const bool mine = r < rows;
+        const bool mine = r < rows && !j.dry;
         const int target = mine ? g.target[g.z.first + r] - c0 : -1;
         float most = -INFINITY;
 #pragma unroll
@@ -491,7 +574,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2)
                 fence_async_shared();
                 __syncwarp();
                 if (lane == 0) {
-                    if (r0 < rows && c0 + h * 64 < g.z.vocab) tensor_store_2d(&map_e, c0 + h * 64, r0, smem_addr(box));
+                    if (r0 < rows && c0 + h * 64 < g.z.vocab && !j.dry) tensor_store_2d(&map_e, c0 + h * 64, r0, smem_addr(box));
                     bulk_store_commit();
                 }
             }
@@ -500,7 +583,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2)
             g.stats[(int64_t)r * 2 * g.tiles_n + c0 / 128] =
                 make_float2(most, ((sum[0] + sum[1]) + (sum[2] + sum[3])) * (kIsHalf<T> ? 0x1p-14f : 1.0f));
     };
-    run_jobs<T>(s, smem, next, finish);
+    run_jobs<T>(s, smem, next, finish, [](const Job&, int, int) {});
     if ((threadIdx.x >> 5) >= 2 && lane == 0) bulk_store_wait();
     tear_down(s, g.timeouts);
 }
@@ -511,7 +594,7 @@ constexpr int kScaleThreads = 256;
 
 struct Scale {
     Sizes z;
-    const Head* head;
+    Head* head;
     const int *map, *target;
     const float* weight;
     float scale;
@@ -520,70 +603,164 @@ struct Scale {
     const float* label;
     void* e;                          // NULL: no gradients
     int64_t pitch;
-    float* each;                      // NULL: not wanted
+    float *each, *total;              // NULL: not wanted
     float* share;                     // weight times loss, of the gathered rows
+    int64_t part_rows;                // room for parts of dX
+    int dw;                           // dW is wanted
 };
 
+// What p parts of dX's sums over the vocabulary cost, in stages of a pair: its longest list of units, or its share of all work,
+// and writing and reading the parts (a stage lasts 512 cycles, in which an SM pair moves about 24 KB).
+__host__ __device__ inline float cost_of_parts(int p, int rows, int vocab, int hidden, bool dw) {
+    const int tiles_m = (rows + kTile - 1) / kTile, tiles_h = (hidden + kTile - 1) / kTile;
+    const int steps_v = (vocab + kStageK - 1) / kStageK, steps_r = (rows + kStageK - 1) / kStageK;
+    const float units = (float)tiles_m * tiles_h * p, unit = (float)((steps_v + p - 1) / p);
+    const float work_w = dw ? (float)((vocab + kTile - 1) / kTile) * tiles_h * steps_r : 0.0f;
+    const float even = ((float)tiles_m * tiles_h * steps_v + work_w) / kPairs + (dw ? 0.5f * steps_r : 0.0f);
+    const float joined = p > 1 ? (float)p * rows * hidden * 8 / kPairs / 24576 + 12 : 0.0f;
+    return fmaxf(ceilf(units / kPairs) * unit, even) + joined;
+}
+
+__host__ __device__ inline bool parts_fit(int p, int rows, int vocab, int64_t room) {
+    return p == 1 || (p <= kMostParts && p <= (vocab + kStageK - 1) / kStageK && (int64_t)p * rows <= room);
+}
+
+__device__ __forceinline__ double lanes_sum(double v) {
+#pragma unroll
+    for (int o = 16; o; o /= 2) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+
+// log2 of the sum of a row's exponentials, by a whole warp: no barrier, every warp of a row's CTA finds it for itself.
+__device__ __forceinline__ float lse2_of(const float2* stats, int parts, int lane) {
+    float most = -INFINITY, sum = 0.0f;
+    for (int i0 = lane; i0 < parts; i0 += 32 * 4) {
+        float2 v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = i0 + k * 32 < parts ? stats[i0 + k * 32] : make_float2(-INFINITY, 0.0f);
+        float top = most;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) top = fmaxf(top, v[k].x);
+        sum *= most == top ? 1.0f : exp2f(most - top);                // (both may be -inf)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) sum += v[k].x == -INFINITY ? v[k].y : v[k].y * exp2f(v[k].x - top);       // (y is 0 or NaN there)
+        most = top;
+    }
+    float top = most;
+#pragma unroll
+    for (int o = 16; o; o /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    sum *= most == top ? 1.0f : exp2f(most - top);
+#pragma unroll
+    for (int o = 16; o; o /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    return top + log2f(sum);
+}
+
+constexpr float kLn2 = 0.693147180559945f;
+
+// The loss of gathered row r of the piece; one thread.
+__device__ __forceinline__ void finish_row(const Scale& a, int r, float weight, float loss) {
+    if (a.each) a.each[a.map[a.z.first + r]] = loss;
+    a.share[a.z.first + r] = weight * loss;
+}
+
+// Without gradients: a warp per row, and the last row to arrive adds up the total.
+__global__ void __launch_bounds__(kScaleThreads) loss_kernel(const Scale a) {
+    __shared__ double s_sum[kScaleThreads / 32];
+    __shared__ int s_last;
+    wait_prerequisites();
+    launch_dependents();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rows = rows_of_piece(a.z, a.head);
+    const int first = blockIdx.x * (kScaleThreads / 32), r = first + warp;
+    if (first >= rows) return;
+    if (r < rows) {
+        const float own = a.label[r], weight = a.weight[a.z.first + r];
+        const float lse = lse2_of(a.stats + (int64_t)r * 2 * a.tiles_n, (a.z.vocab + 127) / 128, lane);
+        if (lane == 0) finish_row(a, r, weight, (lse - own) * kLn2);
+    }
+    if (!a.total) return;
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        const int mine = min(kScaleThreads / 32, rows - first);       // (all rows of all pieces are counted)
+        s_last = atomicAdd(&a.head->done, mine) + mine == a.head->counted;
+    }
+    __syncthreads();
+    if (!s_last) return;
+    __threadfence();
+    double total = 0.0;
+    for (int i = threadIdx.x; i < a.head->counted; i += kScaleThreads) total += __ldcg(a.share + i);
+    total = lanes_sum(total);
+    if (lane == 0) s_sum[warp] = total;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        total = 0.0;
+#pragma unroll
+        for (int i = 0; i < kScaleThreads / 32; ++i) total += s_sum[i];
+        *a.total = (float)total;
+    }
+}
+
 template <typename T> __global__ void __launch_bounds__(kScaleThreads) scale_kernel(const Scale a) {
-    __shared__ float s_part[kScaleThreads / 32];
     wait_prerequisites();
     launch_dependents();
     const int rows = rows_of_piece(a.z, a.head), r = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    T* e = a.e ? static_cast<T*>(a.e) + r * a.pitch : nullptr;
-    const int vectors = (int)((a.z.vocab + 7) / 8);
+    T* e = static_cast<T*>(a.e) + r * a.pitch;
+    const int vectors = (a.z.vocab + 7) / 8;
+    if (r == 0 && warp == kScaleThreads / 32 - 1) {                   // a lane per number of parts
+        const int p = lane + 1;
+        const uint32_t cost = parts_fit(p, rows, a.z.vocab, a.part_rows)
+                                  ? __float_as_uint(cost_of_parts(p, rows, a.z.vocab, a.z.hidden, a.dw)) : 0xffffffffu;
+        const uint32_t least = __reduce_min_sync(0xffffffffu, cost);
+        const int best = __ffs(__ballot_sync(0xffffffffu, cost == least));
+        if (lane == 0) a.head->parts = best;
+    }
     if (r >= rows) {
-        if (e && r < (rows + kStageK - 1) / kStageK * kStageK)
+        if (r < (rows + kStageK - 1) / kStageK * kStageK)
             for (int i = threadIdx.x; i < vectors; i += kScaleThreads) reinterpret_cast<uint4*>(e)[i] = uint4{};
         return;
     }
-    const int parts = (a.z.vocab + 127) / 128;
     const float2* stats = a.stats + (int64_t)r * 2 * a.tiles_n;
-    float most = -INFINITY;
-    for (int i = threadIdx.x; i < parts; i += kScaleThreads) most = fmaxf(most, stats[i].x);
+    // (vectors of the row are read a batch ahead; the first batch comes while its statistics are added up)
+    constexpr int kAhead = 4;
+    uint4 bits[kAhead];
+    const auto read = [&](int i0) {
 #pragma unroll
-    for (int o = 16; o; o /= 2) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
-    if (lane == 0) s_part[warp] = most;
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kScaleThreads / 32; ++i) most = fmaxf(most, s_part[i]);
-    __syncthreads();
-    float sum = 0.0f;
-    for (int i = threadIdx.x; i < parts; i += kScaleThreads) {
-        const float2 v = stats[i];
-        sum += v.x == -INFINITY ? v.y : v.y * exp2f(v.x - most);      // (v.y is 0 or NaN there)
-    }
-#pragma unroll
-    for (int o = 16; o; o /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    if (lane == 0) s_part[warp] = sum;
-    __syncthreads();
-    sum = 0.0f;
-#pragma unroll
-    for (int i = 0; i < kScaleThreads / 32; ++i) sum += s_part[i];
-    const float lse = most + log2f(sum), own = a.label[r];            // in powers of two
-    const float weight = a.weight[a.z.first + r];
-    const int target = a.target[a.z.first + r];
-    constexpr float kLn2 = 0.693147180559945f;
-    if (threadIdx.x == 0) {
-        const float loss = (lse - own) * kLn2;
-        if (a.each) a.each[a.map[a.z.first + r]] = loss;
-        a.share[a.z.first + r] = weight * loss;
-    }
-    if (!e) return;
-    const float c = weight * a.scale * a.head->lift;
-    for (int i = threadIdx.x; i < vectors; i += kScaleThreads) {
-        const float top = stats[i / 16].x;
-        const float f = top == -INFINITY ? c : c * exp2f(top - lse - kUp<T>);
-        float v[8];
-        load(e + i * 8, v);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] *= f;
-        if (target / 8 == i) {
-            const float d = c * expm1f((own - lse) * kLn2);
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (target % 8 == j) v[j] = d;
+        for (int k = 0; k < kAhead; ++k) {
+            const int i = i0 + k * kScaleThreads;
+            if (i < vectors) bits[k] = reinterpret_cast<const uint4*>(e)[i];
         }
-        store(e + i * 8, v);
+    };
+    read(threadIdx.x);
+    const float own = a.label[r];                                     // in powers of two
+    const float weight = a.weight[a.z.first + r], c = weight * a.scale * a.head->lift;
+    const int target = a.target[a.z.first + r];
+    const float lse = lse2_of(stats, (a.z.vocab + 127) / 128, lane);
+    if (threadIdx.x == 0) finish_row(a, r, weight, (lse - own) * kLn2);
+    for (int i0 = threadIdx.x; i0 < vectors; i0 += kAhead * kScaleThreads) {
+        uint4 now[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) now[k] = bits[k];
+        read(i0 + kAhead * kScaleThreads);
+        float top[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) top[k] = stats[min(i0 + k * kScaleThreads, vectors - 1) / 16].x;
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int i = i0 + k * kScaleThreads;
+            const float f = top[k] == -INFINITY ? c : c * exp2f(top[k] - lse - kUp<T>);
+            alignas(16) T t[8];
+            *reinterpret_cast<uint4*>(t) = now[k];
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = widen(t[j]) * f;
+            if (target / 8 == i) {
+                const float d = c * expm1f((own - lse) * kLn2);
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (target % 8 == j) v[j] = d;
+            }
+            if (i < vectors) store(e + i * 8, v);
+        }
     }
 }
 
@@ -595,70 +772,176 @@ struct Grads {
     const int* map;
     void* dx;                         // NULL: not wanted
     int64_t lddx;
-    float* dx_parts;                  // [parts][rows of a piece][pitch], where the sums over the vocabulary are split
-    int parts;
+    float* dx_parts;                  // [parts][labelled rows of the piece][pitch], where the sums over the vocabulary are split
     void* dw;                         // NULL: not wanted
     int64_t lddw;
     int add;
     float* dw_sums;                   // [vocab][pitch], over pieces
     int more, last;                   // not the first piece, the last piece
+    const float* share;
+    float* total;                     // NULL: not wanted
     int64_t pitch;
-    int dx_vector, dw_vector;         // elements that can be accessed at once
+    int dx_unit, dw_unit;             // bytes that rows are aligned to, at most 16
     int* timeouts;
 };
 
-// 32 rows x 32 columns of fp32 from a warp's box (16-byte units swizzled by row) to memory, E neighbours per lane.
-// row, sums_row: where this lane's row lies in `out` and in `sums`, or -1.
-template <typename TO, int E>
-__device__ __forceinline__ void put(const float* box, int64_t row, int64_t sums_row, TO* out, int64_t ld, int64_t col0,
-                                    int64_t cols, float factor, bool add, const float* sums_in, float* sums_out, int64_t pitch) {
-    constexpr int kLanes = 32 / E;
-    const int lane = threadIdx.x & 31, c = lane % kLanes * E;
-    const int64_t col = col0 + c;
-#pragma unroll 2
-    for (int it = 0; it < 32 / E; ++it) {
-        const int r = it * E + lane / kLanes;
-        const int64_t at = __shfl_sync(0xffffffffu, row, r), sums_at = __shfl_sync(0xffffffffu, sums_row, r);
-        if (at < 0 || col >= cols) continue;
-        float v[E];
-        if constexpr (E >= 4) {
-#pragma unroll
-            for (int q = 0; q < E / 4; ++q)
-                *reinterpret_cast<float4*>(v + q * 4) =
-                    *reinterpret_cast<const float4*>(box + r * 32 + (((c / 4 + q) ^ (r & 7)) << 2));
-        } else {
-            v[0] = box[r * 32 + (((c / 4) ^ (r & 7)) << 2) + c % 4];
+// The way out of a warp's 32 rows x 128 columns of sums: a lane has a row; rounded to their type, 128 bytes of each row go
+// through shared memory (a box, its 16-byte units swizzled by row), so that neighbouring lanes write neighbouring bytes.
+// They are rounded before because the bandwidth of shared memory, which the operands of the products share, bounds this; and
+// what they are added to is read by the lane that has the row, all of it before the first use (behind a branch per element,
+// or between the writes, every read would wait for the one before).
+
+__device__ __forceinline__ const uint8_t* in_box(const uint8_t* box, int r, int byte) {
+    return box + r * 128 + (((byte >> 4) ^ (r & 7)) << 4) + (byte & 15);
+}
+
+// A box to rows of `out` (at the first of its columns) of which `left` columns exist.  row: of this lane, or -1.
+// unit: 16 or 8 bytes that rows are aligned to, or less.
+template <typename TO>
+__device__ __forceinline__ void put_box(const uint8_t* box, int row, TO* out, int64_t ld, int left, int unit) {
+    constexpr int kSize = (int)sizeof(TO), kCols = 128 / kSize, kEdge = 16 / kSize;
+    const int lane = threadIdx.x & 31;
+    if (left < kCols) {                                               // the last columns: single elements
+#pragma unroll 4
+        for (int i = lane; i < 32 * kCols; i += 32) {
+            const int r = i / kCols, c = i % kCols, at = __shfl_sync(0xffffffffu, row, r);
+            if (at >= 0 && c < left) out[at * ld + c] = *reinterpret_cast<const TO*>(in_box(box, r, c * kSize));
         }
-        if (sums_in) {
-            float o[E];
-            if constexpr (E >= 4) load(sums_in + sums_at * pitch + col, o);
-            else o[0] = sums_in[sums_at * pitch + col];
+    } else if (unit == 16) {
+        uint4 v[8];
 #pragma unroll
-            for (int j = 0; j < E; ++j) v[j] += o[j];
+        for (int i = 0; i < 8; ++i) v[i] = *reinterpret_cast<const uint4*>(in_box(box, i * 4 + lane / 8, lane % 8 * 16));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int at = __shfl_sync(0xffffffffu, row, i * 4 + lane / 8);
+            if (at >= 0) reinterpret_cast<uint4*>(out + at * ld)[lane % 8] = v[i];
         }
-        if (sums_out) {
-            if constexpr (E >= 4) store(sums_out + sums_at * pitch + col, v);
-            else sums_out[sums_at * pitch + col] = v[0];
-            continue;
+    } else if (unit == 8) {
+        uint2 v[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = *reinterpret_cast<const uint2*>(in_box(box, i * 2 + lane / 16, lane % 16 * 8));
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int at = __shfl_sync(0xffffffffu, row, i * 2 + lane / 16);
+            if (at >= 0) reinterpret_cast<uint2*>(out + at * ld)[lane % 16] = v[i];
         }
-        TO* to = out + at * ld + col;
+    } else {
+        // the aligned 16-byte units inside the row's 128 bytes, then the elements before and behind them (none, or 16 bytes)
+#pragma unroll 1
+        for (int i0 = 0; i0 < 8; i0 += 4) {
+            uint32_t w[4][8];
+            uint8_t* to[4];
 #pragma unroll
-        for (int j = 0; j < E; ++j) v[j] *= factor;
-        if constexpr (E >= 4) {
-            if (col + E <= cols) {
-                if (add) {
-                    float o[E];
-                    load(to, o);
+            for (int i = 0; i < 4; ++i) {
+                const int r = (i0 + i) * 4 + lane / 8, at = __shfl_sync(0xffffffffu, row, r);
+                to[i] = reinterpret_cast<uint8_t*>(out + at * ld);
+                const int b = (int)(-(uintptr_t)to[i] & 15) + lane % 8 * 16;
+                to[i] = at >= 0 && b + 16 <= 128 ? to[i] + b : nullptr;
+                const uint4 lo = *reinterpret_cast<const uint4*>(in_box(box, r, b & 0x70));
+                const uint4 hi = *reinterpret_cast<const uint4*>(in_box(box, r, (b + 16) & 0x70));
+                w[i][0] = lo.x, w[i][1] = lo.y, w[i][2] = lo.z, w[i][3] = lo.w;
+                w[i][4] = hi.x, w[i][5] = hi.y, w[i][6] = hi.z, w[i][7] = hi.w;
+                shift_words<4>(w[i], b & 15);
+            }
 #pragma unroll
-                    for (int j = 0; j < E; ++j) v[j] += o[j];
+            for (int i = 0; i < 4; ++i)
+                if (to[i]) *reinterpret_cast<uint4*>(to[i]) = make_uint4(w[i][0], w[i][1], w[i][2], w[i][3]);
+        }
+        TO edge[kEdge];
+#pragma unroll
+        for (int i = 0; i < kEdge; ++i) {
+            const int r = (i * 32 + lane) / kEdge, at = __shfl_sync(0xffffffffu, row, r);
+            const int front = (int)(-(uintptr_t)(out + at * ld) & 15), e = lane % kEdge * kSize;
+            edge[i] = *reinterpret_cast<const TO*>(in_box(box, r, e < front ? e : 112 + e));
+        }
+#pragma unroll
+        for (int i = 0; i < kEdge; ++i) {
+            const int at = __shfl_sync(0xffffffffu, row, (i * 32 + lane) / kEdge);
+            uint8_t* to = reinterpret_cast<uint8_t*>(out + at * ld);
+            const int front = (int)(-(uintptr_t)to & 15), e = lane % kEdge * kSize;
+            if (at >= 0 && front) *reinterpret_cast<TO*>(to + (e < front ? e : 112 + e)) = edge[i];
+        }
+    }
+}
+
+struct Added {
+    bool out;                         // what `out` holds is added after the factor; it lies in [lo, hi)
+    uintptr_t lo, hi;
+    const float* sums;                // added before the factor, aligned; or NULL
+    int64_t pitch;
+};
+
+template <typename TO, typename Take>
+__device__ __forceinline__ void put_tile(uint32_t tmem, uint8_t* box, int row, TO* out, int64_t ld, int left, float factor, int unit,
+                                         const Added& more, Take take) {
+    constexpr int kSize = (int)sizeof(TO), kCols = 128 / kSize, kSteps = 128 / kCols;
+    const int lane = threadIdx.x & 31;
+#pragma unroll 1
+    for (int q = 0; q < kSteps; ++q) {
+        const int here = left - q * kCols;
+        uint32_t old[36];
+        if (more.out && here > 0) {
+            const uintptr_t first = (uintptr_t)(out + max(row, 0) * ld + q * kCols), start = first & ~(uintptr_t)15;
+            const int shift = (int)(first & 15);
+            if (__all_sync(0xffffffffu, start >= more.lo && start + 144 <= more.hi)) {
+#pragma unroll
+                for (int i = 0; i < 9; ++i) {
+                    const uint4 v = reinterpret_cast<const uint4*>(start)[i];
+                    old[i * 4] = v.x, old[i * 4 + 1] = v.y, old[i * 4 + 2] = v.z, old[i * 4 + 3] = v.w;
                 }
-                store(to, v);
-                continue;
+            } else {                                                  // at the ends of the matrix
+#pragma unroll
+                for (int i = 0; i < 9; ++i) {
+                    const uint4 v = load_edge<kSize>(start + 16 * i, more.lo, more.hi);
+                    old[i * 4] = v.x, old[i * 4 + 1] = v.y, old[i * 4 + 2] = v.z, old[i * 4 + 3] = v.w;
+                }
+            }
+            if (unit < 16) shift_words<32>(old, shift);
+        }
+        uint32_t acc[kCols];
+#pragma unroll
+        for (int i = 0; i < kCols / 32; ++i)
+            tmem_load32(tmem + q * kCols + i * 32, *reinterpret_cast<uint32_t(*)[32]>(acc + i * 32));
+        if (q + 1 == kSteps) take();
+        if (here <= 0) continue;
+        if (more.sums) {
+            const float4* from = reinterpret_cast<const float4*>(more.sums + max(row, 0) * more.pitch + q * kCols);
+#pragma unroll
+            for (int i = 0; i < kCols / 4; ++i) {
+                const float4 v = from[i];
+                acc[i * 4] = __float_as_uint(__uint_as_float(acc[i * 4]) + v.x);
+                acc[i * 4 + 1] = __float_as_uint(__uint_as_float(acc[i * 4 + 1]) + v.y);
+                acc[i * 4 + 2] = __float_as_uint(__uint_as_float(acc[i * 4 + 2]) + v.z);
+                acc[i * 4 + 3] = __float_as_uint(__uint_as_float(acc[i * 4 + 3]) + v.w);
             }
         }
 #pragma unroll
-        for (int j = 0; j < E; ++j)
-            if (col + j < cols) to[j] = narrow<TO>(add ? v[j] + widen(to[j]) : v[j]);
+        for (int i = 0; i < kCols; ++i) acc[i] = __float_as_uint(__uint_as_float(acc[i]) * factor);
+        if (more.out) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+                if constexpr (kSize == 4) {
+                    acc[i] = __float_as_uint(__uint_as_float(acc[i]) + __uint_as_float(old[i]));
+                } else {
+                    const TO* t = reinterpret_cast<const TO*>(&old[i]);
+                    acc[2 * i] = __float_as_uint(__uint_as_float(acc[2 * i]) + widen(t[0]));
+                    acc[2 * i + 1] = __float_as_uint(__uint_as_float(acc[2 * i + 1]) + widen(t[1]));
+                }
+            }
+        }
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            uint32_t t[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if constexpr (kSize == 4) t[j] = acc[i * 4 + j];
+                else t[j] = pack2<TO>(__uint_as_float(acc[i * 8 + 2 * j]), __uint_as_float(acc[i * 8 + 2 * j + 1]));
+            }
+            *reinterpret_cast<uint4*>(box + lane * 128 + ((i ^ (lane & 7)) << 4)) = make_uint4(t[0], t[1], t[2], t[3]);
+        }
+        __syncwarp();
+        put_box(box, row, out + q * kCols, ld, here, unit);
     }
 }
 
@@ -677,68 +960,70 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2)
     const int n_pairs = gridDim.x / 2, pair = blockIdx.x / 2;
     const int steps_v = (g.z.vocab + kStageK - 1) / kStageK, steps_r = (rows + kStageK - 1) / kStageK;
     const float unlift = g.head->unlift;
+    const int parts = g.head->parts;
     // dX first, its long sums split into parts, then dW.  Where the units of dX do not come out even, the pairs with one
     // less take as many tiles of dW ahead of the others as last as long.
-    const int per_part = tiles_m * tiles_h, n_dx = g.dx ? per_part * g.parts : 0, n_dw = g.dw && steps_r ? tiles_v * tiles_h : 0;
+    const int per_part = tiles_m * tiles_h, n_dx = g.dx ? per_part * parts : 0, n_dw = g.dw && steps_r ? tiles_v * tiles_h : 0;
     const int heavy = n_dx % n_pairs, light = n_pairs - heavy, units = n_dx / n_pairs + (pair < heavy);
-    const int ahead = heavy && steps_r ? max(0, steps_v / g.parts / steps_r) : 0;
+    const int ahead = heavy && steps_r ? max(0, steps_v / parts / steps_r) : 0;
     const int early = (int)min((int64_t)n_dw, (int64_t)ahead * light);
     const int my_early = pair < heavy ? 0 : max(0, (early - (pair - heavy) + light - 1) / light);
     const auto next = [&](int it, Job& j) {
         if (it < units) {
             const int u = it * n_pairs + pair, part = u / per_part, t = u - part * per_part;
             j = Job{{&map_d, false, 0}, {&map_w, true, 0}, t % tiles_m, t / tiles_m,
-                    (int)((int64_t)steps_v * part / g.parts), (int)((int64_t)steps_v * (part + 1) / g.parts), 0, part};
+                    (int)((int64_t)steps_v * part / parts), (int)((int64_t)steps_v * (part + 1) / parts), 0, part, false};
             return true;
         }
         it -= units;
         const int t = it < my_early ? pair - heavy + it * light : early + (it - my_early) * n_pairs + pair;
         if (t >= n_dw) return false;
-        j = Job{{&map_d, true, 0}, {&map_x, true, g.z.first}, t / tiles_h, t % tiles_h, 0, steps_r, 1, 0};
+        j = Job{{&map_d, true, 0}, {&map_x, true, g.z.first}, t / tiles_h, t % tiles_h, 0, steps_r, 1, 0, false};
         return true;
     };
-    const auto finish = [&](const Job& j, uint32_t sums, int row_in, int col_in, uint8_t* raw, auto take) {
-        float* box = reinterpret_cast<float*>(raw);
-        const int r = j.ti * kTile + row_in + lane;
-        const bool is_dx = j.kind == 0;
-        int64_t row = -1, sums_row = -1;
-        if (is_dx) {
-            if (r < rows) row = g.map[g.z.first + r], sums_row = (int64_t)j.part * g.z.piece + r;
-        } else if (r < g.z.vocab) {
-            row = sums_row = r;
+    const auto finish = [&](const Job& j, uint32_t sums, int row_in, int col_in, uint8_t* box, auto take) {
+        const int r = j.ti * kTile + row_in + lane, col = j.tj * kTile + col_in, left = g.z.hidden - col;
+        const bool is_dx = j.kind == 0, split = is_dx && parts > 1;
+        if (left <= 0) {
+            take();
+            return;
         }
-        const float* sums_in = is_dx || !g.more ? nullptr : g.dw_sums;
-        float* sums_out = is_dx ? g.dx_parts : g.last ? nullptr : g.dw_sums;
-#pragma unroll 1
-        for (int q = 0; q < 4; ++q) {
-            uint32_t acc[32];
-            tmem_load32(sums + q * 32, acc);
-            if (q == 3) take();
-            __syncwarp();
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                *reinterpret_cast<uint4*>(box + lane * 32 + ((i ^ (lane & 7)) << 2)) =
-                    make_uint4(acc[i * 4], acc[i * 4 + 1], acc[i * 4 + 2], acc[i * 4 + 3]);
-            __syncwarp();
-            const int64_t col = (int64_t)j.tj * kTile + col_in + q * 32;
-            if (is_dx) {
-                T* out = static_cast<T*>(g.dx);
-                if (g.dx_vector == 8) put<T, 8>(box, row, sums_row, out, g.lddx, col, g.z.hidden, unlift, false, sums_in, sums_out, g.pitch);
-                else if (g.dx_vector == 4) put<T, 4>(box, row, sums_row, out, g.lddx, col, g.z.hidden, unlift, false, sums_in, sums_out, g.pitch);
-                else put<T, 1>(box, row, sums_row, out, g.lddx, col, g.z.hidden, unlift, false, sums_in, sums_out, g.pitch);
-            } else {
-                TW* out = static_cast<TW*>(g.dw);
-                if (sizeof(TW) == 2 && g.dw_vector == 8)
-                    put<TW, sizeof(TW) == 2 ? 8 : 4>(box, row, sums_row, out, g.lddw, col, g.z.hidden, unlift, g.add, sums_in, sums_out, g.pitch);
-                else if (g.dw_vector >= 4)
-                    put<TW, 4>(box, row, sums_row, out, g.lddw, col, g.z.hidden, unlift, g.add, sums_in, sums_out, g.pitch);
-                else
-                    put<TW, 1>(box, row, sums_row, out, g.lddw, col, g.z.hidden, unlift, g.add, sums_in, sums_out, g.pitch);
-            }
-            __syncwarp();
+        const int row = j.dry || r >= (is_dx ? rows : g.z.vocab) ? -1 : is_dx && !split ? g.map[g.z.first + r] : r;
+        // (rows of the workspace are whole: their columns do not end inside a step)
+        if (split || (!is_dx && !g.last)) {
+            float* out = split ? g.dx_parts + (int64_t)j.part * rows * g.pitch : g.dw_sums;
+            const Added more{false, 0, 0, !is_dx && g.more ? out + col : nullptr, g.pitch};
+            put_tile(sums, box, row, out + col, g.pitch, (int)g.pitch - col, 1.0f, 16, more, take);
+        } else if (is_dx) {
+            put_tile(sums, box, row, static_cast<T*>(g.dx) + col, g.lddx, left, unlift, g.dx_unit, Added{}, take);
+        } else {
+            TW* out = static_cast<TW*>(g.dw);
+            const Added more{g.add != 0, (uintptr_t)out, (uintptr_t)(out + (g.z.vocab - 1) * g.lddw + g.z.hidden),
+                             g.more ? g.dw_sums + col : nullptr, g.pitch};
+            put_tile(sums, box, row, out + col, g.lddw, left, unlift, g.dw_unit, more, take);
         }
     };
-    run_jobs<T>(s, smem, next, finish);
+    // what a tile of dW is added to is brought into L2 while its products run
+    const auto ahead_of = [&](const Job& j, int row_in, int col_in) {
+        const int r = j.ti * kTile + row_in + lane, col = j.tj * kTile + col_in, left = min(128, g.z.hidden - col);
+        if (j.kind == 0 || !g.add || !g.last || r >= g.z.vocab || left <= 0) return;
+        const TW* at = static_cast<const TW*>(g.dw) + r * g.lddw + col;
+        for (int c = 0; c < left; c += 128 / (int)sizeof(TW)) prefetch_l2(at + c);
+        prefetch_l2(at + left - 1);
+    };
+    // the total, by a warp that has nothing to issue: the 256 sums that loss_kernel's last CTA would take, eight to a lane
+    if (blockIdx.x == 1 && threadIdx.x / 32 == 1 && g.last && g.total && g.head->counted) {
+        double sum[8] = {}, total = 0.0;
+        for (int i = lane; i < g.head->counted; i += 256)
+#pragma unroll
+            for (int w = 0; w < 8; ++w)
+                if (i + w * 32 < g.head->counted) sum[w] += g.share[i + w * 32];
+#pragma unroll
+        for (int w = 0; w < 8; ++w) total += lanes_sum(sum[w]);
+        if (lane == 0) *g.total = (float)total;
+        __syncwarp();
+    }
+    run_jobs<T>(s, smem, next, finish, ahead_of);
     // a piece without rows has no products: what the pieces before have left, or nothing, is still the gradient
     if (g.dw && steps_r == 0 && (g.last || !g.more)) {
         TW* out = static_cast<TW*>(g.dw);
@@ -763,23 +1048,23 @@ template <typename T>
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(const Grads g) {
     wait_prerequisites();
     launch_dependents();
-    const int rows = rows_of_piece(g.z, g.head), r = blockIdx.x;
-    if (r >= rows) return;
+    const int rows = rows_of_piece(g.z, g.head), r = blockIdx.x, parts = g.head->parts;
+    if (r >= rows || parts == 1) return;
     const float unlift = g.head->unlift;
     T* out = static_cast<T*>(g.dx) + g.map[g.z.first + r] * g.lddx;
     for (int c = (blockIdx.y * kJoinThreads + threadIdx.x) * 4; c < g.z.hidden; c += gridDim.y * kJoinThreads * 4) {
         const float* p = g.dx_parts + (int64_t)r * g.pitch + c;
         float v[4];
         load(p, v);
-        for (int k = 1; k < g.parts; ++k) {
+        for (int k = 1; k < parts; ++k) {
             float o[4];
-            load(p + (int64_t)k * g.z.piece * g.pitch, o);
+            load(p + (int64_t)k * rows * g.pitch, o);
 #pragma unroll
             for (int j = 0; j < 4; ++j) v[j] += o[j];
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j) v[j] *= unlift;
-        if (g.dx_vector >= 4 && c + 4 <= g.z.hidden) {
+        if (g.dx_unit >= 8 && c + 4 <= g.z.hidden) {
             store(out + c, v);
         } else {
 #pragma unroll
@@ -789,61 +1074,19 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const Grads g) {
     }
 }
 
-constexpr int kTotalThreads = 1024;
-
-__global__ void __launch_bounds__(kTotalThreads) total_kernel(const Head* head, const float* share, float* total) {
-    __shared__ double s_part[kTotalThreads / 32];
-    wait_prerequisites();
-    launch_dependents();
-    double sum = 0.0;
-    for (int i = threadIdx.x; i < head->counted; i += kTotalThreads) sum += share[i];
-#pragma unroll
-    for (int o = 16; o; o /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    if ((threadIdx.x & 31) == 0) s_part[threadIdx.x >> 5] = sum;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        sum = 0.0;
-        for (int i = 0; i < kTotalThreads / 32; ++i) sum += s_part[i];
-        *total = (float)sum;
-    }
-}
-
 // ---------------------------------------------------------------------------------------------- host side
 
 constexpr int64_t kMostRows = (int64_t)1 << 28, kMostVocab = (int64_t)1 << 28, kMostHidden = (int64_t)1 << 20;
-constexpr int kPairs = 74;            // of a whole B200: what the split of dX is planned for
 
 static int64_t up_to(int64_t n, int64_t step) { return (n + step - 1) / step * step; }
 
 struct Plan {
     int64_t pitch, e_pitch;           // of the copies of X and W, of e
     int64_t piece, pieces, tiles_n;
-    int parts;
+    int64_t part_rows;                // room for the parts of dX: rows of any part
     int64_t head, map, target, weight, share, label, stats, x, w, e, dx_parts, dw_sums, bytes;
     bool countable;                   // its tiles can be counted in 31 bits
 };
-
-// Parts of dX's sums over the vocabulary: the number that ends first, by the longest list of stages of a pair, and what
-// writing and reading the parts takes (a stage lasts 512 cycles, in which an SM pair moves about 24 KB).
-static int parts_of(int64_t rows, int64_t vocab, int64_t hidden, bool dw) {
-    const int64_t tiles_m = (rows + kTile - 1) / kTile, tiles_h = (hidden + kTile - 1) / kTile;
-    const int64_t steps_v = (vocab + kStageK - 1) / kStageK, steps_r = (rows + kStageK - 1) / kStageK;
-    const int64_t work_w = dw ? (vocab + kTile - 1) / kTile * tiles_h * steps_r : 0;
-    int best = 1;
-    double least = 1e300;
-    for (int p = 1; p <= kMostParts && p <= steps_v; ++p) {
-        const int64_t units = tiles_m * tiles_h * p, unit = (steps_v + p - 1) / p;
-        const double alone = (double)((units + kPairs - 1) / kPairs) * unit;
-        const double even = (double)(tiles_m * tiles_h * steps_v + work_w) / kPairs + (dw ? 0.5 * steps_r : 0.0);
-        const double joined = p > 1 ? (double)p * rows * hidden * 8 / kPairs / 24576 + 12 : 0.0;
-        const double cost = std::max(alone, even) + joined;
-        if (cost < least * 0.999) {
-            least = cost;
-            best = p;
-        }
-    }
-    return best;
-}
 
 static Plan plan_of(int64_t rows, int64_t vocab, int64_t hidden, int grads, bool copy_w, int64_t piece_rows) {
     Plan p{};
@@ -856,7 +1099,17 @@ static Plan plan_of(int64_t rows, int64_t vocab, int64_t hidden, int grads, bool
         p.piece = std::max<int64_t>(kTile, ((int64_t)1 << 29) / (p.tiles_n * 16) / kTile * kTile);
     p.piece = std::min(p.piece, up_to(rows, kTile));
     p.pieces = (rows + p.piece - 1) / p.piece;
-    p.parts = grads & 1 ? parts_of(std::min(rows, p.piece), vocab, hidden, grads & 2) : 1;
+    // how many rows have a label is known on the device only, and with it the number of parts: room for what any number of
+    // rows takes (sixteen are looked at)
+    for (int i = 1; grads & 1 && i <= 16; ++i) {
+        const int64_t some = std::min(rows, std::max<int64_t>(1, std::min(rows, p.piece) * i / 16));
+        int parts = 1;
+        for (int n = 2; parts_fit(n, (int)some, (int)vocab, (int64_t)1 << 60); ++n)
+            if (cost_of_parts(n, (int)some, (int)vocab, (int)hidden, grads & 2) <
+                cost_of_parts(parts, (int)some, (int)vocab, (int)hidden, grads & 2))
+                parts = n;
+        if (parts > 1) p.part_rows = std::max(p.part_rows, parts * some);
+    }
     int64_t at = 0;
     const auto take = [&](int64_t bytes) {
         const int64_t here = at;
@@ -873,11 +1126,11 @@ static Plan plan_of(int64_t rows, int64_t vocab, int64_t hidden, int grads, bool
     p.x = take(up_to(rows, kStageK) * p.pitch * 2);
     p.w = take(copy_w ? vocab * p.pitch * 2 : 0);
     p.e = take(grads ? p.piece * p.e_pitch * 2 : 0);
-    p.dx_parts = take(p.parts > 1 ? p.parts * p.piece * p.pitch * 4 : 0);
+    p.dx_parts = take(p.part_rows * p.pitch * 4);
     p.dw_sums = take(grads & 2 && p.pieces > 1 ? vocab * p.pitch * 4 : 0);
     p.bytes = at;
     const int64_t most = (int64_t)1 << 30, tiles_h = (hidden + kTile - 1) / kTile, tiles_m = p.piece / kTile;
-    p.countable = tiles_m <= most / p.tiles_n && tiles_h <= most / p.tiles_n && tiles_m <= most / (tiles_h * p.parts);
+    p.countable = tiles_m <= most / p.tiles_n && tiles_h <= most / p.tiles_n && tiles_m <= most / (tiles_h * kMostParts);
     return p;
 }
 
@@ -893,10 +1146,11 @@ static bool needs_copy(const void* w, int w_type, int64_t ldw, int type) {
     return w_type != type || (uintptr_t)w % 16 || ldw * 2 % 16;
 }
 
-static int vector_of(const void* p, int64_t ld, int type) {
-    for (int n = type == SIDCO_T_F32 ? 4 : 8; n > 1; n /= 2)
-        if ((uintptr_t)p % (uintptr_t)(n * size_of(type)) == 0 && ld % n == 0) return n;
-    return 1;
+// Bytes, 16 at most, that all rows are aligned to.
+static int unit_of(const void* p, int64_t ld, int type) {
+    int n = 16;
+    while (n > 1 && ((uintptr_t)p % (uintptr_t)n || ld * size_of(type) % n)) n /= 2;
+    return n;
 }
 
 template <typename T, typename TW> static cudaError_t prepare_device(int* pairs) {
@@ -977,12 +1231,11 @@ template <typename T, typename TW> static int run(const Call& c, const Plan& p, 
     a.weights = c.weights, a.scale = c.scale;
     a.rows = (int)c.rows, a.vocab = (int)c.vocab, a.hidden = (int)c.hidden, a.pitch = p.pitch;
     a.x_to = c.ws + p.x, a.w_to = copy_w ? c.ws + p.w : nullptr;
-    a.dx = c.dx, a.lddx = c.lddx, a.each = c.each, a.head = head, a.map = map, a.target = target, a.weight = weight;
+    a.dx = c.dx, a.lddx = c.lddx, a.each = c.each, a.total = c.total, a.head = head, a.map = map, a.target = target, a.weight = weight;
     a.status = c.status;
     a.x_blocks = (int)std::min<int64_t>(c.rows, sms), a.x_rows = (int)((c.rows + a.x_blocks - 1) / a.x_blocks);
-    a.x_vector = vector_of(c.x, c.ldx, c.type), a.w_vector = vector_of(c.w, c.ldw, c.w_type);
-    a.dx_vector = vector_of(c.dx, c.lddx, c.type);
-    const unsigned blocks = (unsigned)(a.x_blocks + (copy_w ? std::min<int64_t>((c.vocab + 7) / 8, 6 * sms) : 0));
+    a.w_vector = unit_of(c.w, c.ldw, c.w_type) == 16, a.dx_vector = unit_of(c.dx, c.lddx, c.type) == 16;
+    const unsigned blocks = (unsigned)(a.x_blocks + (copy_w ? std::min<int64_t>((c.vocab + 7) / 8, 16 * sms) : 0));
     if (c.w_type == SIDCO_T_F32) SIDCO_CE_LAUNCH(prepare_kernel<T, float>, dim3(blocks), kPrepareThreads, 0, c.s, 1, a);
     else SIDCO_CE_LAUNCH(prepare_kernel<T, T>, dim3(blocks), kPrepareThreads, 0, c.s, 1, a);
 
@@ -1002,17 +1255,19 @@ template <typename T, typename TW> static int run(const Call& c, const Plan& p, 
         SIDCO_CE_LAUNCH(logits_kernel<T>, dim3((unsigned)(2 * std::min<int64_t>(pairs, tiles))), kThreads, kSmem, c.s, 1, map_x,
                         map_w, map_e, l);
         Scale k{z, head, map, target, weight, c.scale, l.stats, l.tiles_n, l.label, grads ? c.ws + p.e : nullptr, p.e_pitch,
-                c.each, share};
+                c.each, c.total, share, p.part_rows, c.dw != nullptr};
+        if (!grads) {
+            SIDCO_CE_LAUNCH(loss_kernel, dim3((unsigned)((most + 7) / 8)), kScaleThreads, 0, c.s, 1, k);
+            continue;
+        }
         SIDCO_CE_LAUNCH(scale_kernel<T>, dim3((unsigned)up_to(most, kStageK)), kScaleThreads, 0, c.s, 1, k);
-        if (!grads) continue;
-        Grads g{z, head, map, c.dx, c.lddx, p.parts > 1 ? reinterpret_cast<float*>(c.ws + p.dx_parts) : nullptr, p.parts, c.dw,
-                c.lddw, c.add, p.pieces > 1 ? reinterpret_cast<float*>(c.ws + p.dw_sums) : nullptr, i > 0, i + 1 == p.pieces,
-                p.pitch, vector_of(c.dx, c.lddx, c.type), vector_of(c.dw, c.lddw, c.dw_type), timeouts};
+        Grads g{z, head, map, c.dx, c.lddx, reinterpret_cast<float*>(c.ws + p.dx_parts), c.dw, c.lddw, c.add,
+                reinterpret_cast<float*>(c.ws + p.dw_sums), i > 0, i + 1 == p.pieces, share, c.total, p.pitch,
+                unit_of(c.dx, c.lddx, c.type), unit_of(c.dw, c.lddw, c.dw_type), timeouts};
         SIDCO_CE_LAUNCH((grads_kernel<T, TW>), dim3(2 * (unsigned)pairs), kThreads, kSmem, c.s, 1, map_x, map_w, map_d, g);
-        if (c.dx && p.parts > 1)
+        if (c.dx && p.part_rows)
             SIDCO_CE_LAUNCH(join_kernel<T>, dim3((unsigned)most, (unsigned)((c.hidden + 1023) / 1024)), kJoinThreads, 0, c.s, 1, g);
     }
-    if (c.total) SIDCO_CE_LAUNCH(total_kernel, dim3(1), kTotalThreads, 0, c.s, 1, head, share, c.total);
     return 0;
 }
 
