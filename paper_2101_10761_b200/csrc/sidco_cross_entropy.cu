@@ -132,21 +132,6 @@ template <int kSize> __device__ __noinline__ uint4 load_edge(uintptr_t at, uintp
     return make_uint4((uint32_t)h[0], (uint32_t)(h[0] >> 32), (uint32_t)h[1], (uint32_t)(h[1] >> 32));
 }
 
-// N words that start `shift` bytes (even, below 16) into w.
-template <int N> __device__ __forceinline__ void shift_words(uint32_t (&w)[N + 4], int shift) {
-    if (shift & 4) {
-#pragma unroll
-        for (int i = 0; i < N + 3; ++i) w[i] = w[i + 1];
-    }
-    if (shift & 8) {
-#pragma unroll
-        for (int i = 0; i < N + 2; ++i) w[i] = w[i + 2];
-    }
-    const int bits = (shift & 2) * 8;
-#pragma unroll
-    for (int i = 0; i < N; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], bits);
-}
-
 constexpr int kCopyAhead = 4;
 
 // One warp copies a row of 16-bit elements of any alignment to an aligned one whose padding may be written too: aligned

@@ -14,11 +14,14 @@ namespace sidco_dropout_impl {
 using namespace sidco_elements;
 
 constexpr int kThreads = 256;
-constexpr int kEach = 8;              // neighbours per thread: two blocks of the generator
+
+// kEach neighbours per thread: 32 bytes, or 16 where they cannot be accessed at once.
+template <typename T, bool kVector> constexpr int kEachOf = (kVector ? 32 : 16) / (int)sizeof(T);
 
 template <typename T, bool kDrop, bool kVector>
 __global__ void __launch_bounds__(kThreads)
     dropout_kernel(const T* x, const T* residual, T* out, int64_t n, const Dropout d) {
+    constexpr int kEach = kEachOf<T, kVector>;
     sidco_tc::wait_prerequisites();
     sidco_tc::launch_dependents();
     const int64_t i = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * kEach;
@@ -35,10 +38,21 @@ __global__ void __launch_bounds__(kThreads)
             if (residual && i + j < n) r[j] = widen(residual[i + j]);
         }
     }
-    if (kDrop) drop(d, call_of(d), (uint64_t)i / 4, v);
-    if (residual) {
+    if (kDrop) {
+        // (a CTA's elements lie in one aligned span: the high word of their blocks is the CTA's)
+        const uint64_t base = (uint64_t)blockIdx.x * (kThreads * kEach / 4);
+        uint32_t w[kEach / 4][4];
+        random_blocks(d, call_of(d), (uint32_t)base + threadIdx.x * (kEach / 4), (uint32_t)(base >> 32), w);
+        if (residual) {
 #pragma unroll
-        for (int j = 0; j < kEach; ++j) v[j] += r[j];
+            for (int j = 0; j < kEach; ++j) v[j] = dropped(d, w[j / 4][j % 4]) ? r[j] : fmaf(v[j], d.factor, r[j]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < kEach; ++j) v[j] = dropped(d, w[j / 4][j % 4]) ? 0.0f : v[j] * d.factor;
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) v[j] = residual ? v[j] + r[j] : v[j];
     }
     if (whole) {
         store(out + i, v);
@@ -66,7 +80,7 @@ extern "C" int sidco_dropout(const void* x, int type, int64_t n, float p, uint64
     if ((x != out && overlap(x, bytes, out, bytes)) || (residual != out && overlap(residual, bytes, out, bytes)))
         return SIDCO_E_ALIAS;
     const bool vector = ((uintptr_t)x | (uintptr_t)residual | (uintptr_t)out) % 16 == 0;
-    const int64_t per = (int64_t)kThreads * kEach, blocks = (n + per - 1) / per;
+    const int64_t per = (int64_t)kThreads * (vector ? 32 : 16) / size_of(type), blocks = (n + per - 1) / per;
     const int rc = with_type(type, [&](auto* t) {
         using T = std::remove_pointer_t<decltype(t)>;
         const auto kernel = on ? vector ? dropout_kernel<T, true, true> : dropout_kernel<T, true, false>

@@ -45,6 +45,21 @@ template <int N, typename T> __device__ __forceinline__ void store(T* p, const f
         for (int i = 0; i < kBytes / 16; ++i) reinterpret_cast<uint4*>(p)[i] = reinterpret_cast<const uint4*>(t)[i];
 }
 
+// N words that start `shift` bytes (even, below 16) into w.
+template <int N> __device__ __forceinline__ void shift_words(uint32_t (&w)[N + 4], int shift) {
+    if (shift & 4) {
+#pragma unroll
+        for (int i = 0; i < N + 3; ++i) w[i] = w[i + 1];
+    }
+    if (shift & 8) {
+#pragma unroll
+        for (int i = 0; i < N + 2; ++i) w[i] = w[i + 2];
+    }
+    const int bits = (shift & 2) * 8;
+#pragma unroll
+    for (int i = 0; i < N; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], bits);
+}
+
 constexpr int size_of(int type) { return type == SIDCO_T_F32 ? 4 : 2; }
 
 // Whether `n` neighbours of a row that starts at p, with rows `ld` elements apart, can be accessed by load / store.
@@ -79,11 +94,12 @@ __device__ __forceinline__ int64_t token_at(const void* tokens, bool wide, int64
 // ---------------------------------------------------------------------------------------------- dropout
 //
 // Words 4b .. 4b+3 belong to elements 4b .. 4b+3: Philox4x32-10 (Salmon, Moraes, Dror, Shaw, "Parallel random numbers: as
-// easy as 1, 2, 3", 2011) of the counter (b, call) under the key `seed`.  Ten rounds of two 32 x 32 -> 64-bit products: 10
-// wide multiplications and 10 three-input xors per two elements, which an HBM-bound kernel hides.
+// easy as 1, 2, 3", 2011) of the counter (b, call) under the key `seed`: ten rounds of two 32 x 32 -> 64-bit products and two
+// three-input xors per four elements.  The rounds' keys come from the host: added up in the kernel they took a fifth of its
+// instructions.
 
 struct Dropout {
-    uint32_t seed[2];
+    uint32_t key[10][2];              // of every round: the seed plus multiples of the generator's constants
     uint32_t last;                    // words up to this one drop (p = (last + 1) 2^-32)
     float factor;                     // 1 / (1 - p)
     uint64_t call;
@@ -92,33 +108,68 @@ struct Dropout {
 
 __device__ __forceinline__ uint64_t call_of(const Dropout& d) { return d.step ? d.call + *d.step : d.call; }
 
-__device__ __forceinline__ void random4(const Dropout& d, uint64_t call, uint64_t block, uint32_t (&c)[4]) {
-    c[0] = (uint32_t)block;
-    c[1] = (uint32_t)(block >> 32);
-    c[2] = (uint32_t)call;
-    c[3] = (uint32_t)(call >> 32);
-    uint32_t k0 = d.seed[0], k1 = d.seed[1];
+// The words of N blocks from (low, high) on; the blocks do not pass 2^32 in their low word.
+template <int N>
+__device__ __forceinline__ void random_blocks(const Dropout& d, uint64_t call, uint32_t low, uint32_t high, uint32_t (&c)[N][4]) {
 #pragma unroll
-    for (int r = 0; r < 10; ++r) {
-        const uint64_t a = (uint64_t)c[0] * 0xD2511F53u, b = (uint64_t)c[2] * 0xCD9E8D57u;
-        c[0] = (uint32_t)(b >> 32) ^ c[1] ^ k0;
-        c[2] = (uint32_t)(a >> 32) ^ c[3] ^ k1;
-        c[1] = (uint32_t)b;
-        c[3] = (uint32_t)a;
-        k0 += 0x9E3779B9u;
-        k1 += 0xBB67AE85u;
+    for (int q = 0; q < N; ++q) {
+        c[q][0] = low + q;
+        c[q][1] = high;
+        c[q][2] = (uint32_t)call;
+        c[q][3] = (uint32_t)(call >> 32);
+    }
+#pragma unroll
+    for (int r = 0; r < 10; ++r)
+#pragma unroll
+        for (int q = 0; q < N; ++q) {
+            const uint64_t a = (uint64_t)c[q][0] * 0xD2511F53u, b = (uint64_t)c[q][2] * 0xCD9E8D57u;
+            c[q][0] = (uint32_t)(b >> 32) ^ c[q][1] ^ d.key[r][0];
+            c[q][2] = (uint32_t)(a >> 32) ^ c[q][3] ^ d.key[r][1];
+            c[q][1] = (uint32_t)b;
+            c[q][3] = (uint32_t)a;
+        }
+}
+
+// The words of N elements (a multiple of four) from any `first` on.  Where first is no multiple of four (known to whoever
+// compiles, or the same for a whole warp) one block more is drawn.
+template <int N, bool kWhole>
+__device__ __forceinline__ void random_words(const Dropout& d, uint64_t call, uint64_t first, uint32_t (&w)[N]) {
+    constexpr int kBlocks = N / 4 + (kWhole ? 0 : 1);
+    const uint64_t block = first / 4;
+    uint32_t c[kBlocks][4];
+    if ((uint32_t)block + (kBlocks - 1) >= (uint32_t)block) {
+        random_blocks(d, call, (uint32_t)block, (uint32_t)(block >> 32), c);
+    } else {                                                          // once in 2^32 blocks
+#pragma unroll 1
+        for (int q = 0; q < kBlocks; ++q) {
+            uint32_t one[1][4];
+            random_blocks(d, call, (uint32_t)(block + q), (uint32_t)((block + q) >> 32), one);
+#pragma unroll
+            for (int k = 0; k < kBlocks; ++k)
+                if (k == q) c[k][0] = one[0][0], c[k][1] = one[0][1], c[k][2] = one[0][2], c[k][3] = one[0][3];
+        }
+    }
+    const int shift = (int)(first % 4);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        if constexpr (kWhole) {
+            w[i] = c[i / 4][i % 4];
+        } else {
+            const uint32_t a = shift & 1 ? c[(i + 1) / 4][(i + 1) % 4] : c[i / 4][i % 4];
+            const uint32_t b = shift & 1 ? c[(i + 3) / 4][(i + 3) % 4] : c[(i + 2) / 4][(i + 2) % 4];
+            w[i] = shift & 2 ? b : a;
+        }
     }
 }
 
-// v of the N (a multiple of four) elements from element 4 * block on.  What is dropped becomes zero whatever it was.
-template <int N> __device__ __forceinline__ void drop(const Dropout& d, uint64_t call, uint64_t block, float (&v)[N]) {
+__device__ __forceinline__ bool dropped(const Dropout& d, uint32_t word) { return word <= d.last; }
+
+// v of the N elements from `first` on.  What is dropped becomes zero whatever it was.
+template <int N, bool kWhole = true> __device__ __forceinline__ void drop(const Dropout& d, uint64_t call, uint64_t first, float (&v)[N]) {
+    uint32_t w[N];
+    random_words<N, kWhole>(d, call, first, w);
 #pragma unroll
-    for (int q = 0; q < N / 4; ++q) {
-        uint32_t c[4];
-        random4(d, call, block + q, c);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[q * 4 + i] = c[i] <= d.last ? 0.0f : v[q * 4 + i] * d.factor;
-    }
+    for (int i = 0; i < N; ++i) v[i] = dropped(d, w[i]) ? 0.0f : v[i] * d.factor;
 }
 
 // Checks p and fills d; *on: whether anything is dropped.
@@ -127,8 +178,10 @@ inline int make_dropout(float p, uint64_t seed, uint64_t call, const uint64_t* s
     if ((uintptr_t)step % 8) return SIDCO_E_ALIGN;
     const uint64_t words = (uint64_t)((double)p * 4294967296.0 + 0.5);
     *on = words > 0;
-    d->seed[0] = (uint32_t)seed;
-    d->seed[1] = (uint32_t)(seed >> 32);
+    for (uint32_t r = 0; r < 10; ++r) {
+        d->key[r][0] = (uint32_t)seed + r * 0x9E3779B9u;
+        d->key[r][1] = (uint32_t)(seed >> 32) + r * 0xBB67AE85u;
+    }
     d->last = (uint32_t)(words - 1);
     d->factor = p < 1.0f ? (float)(1.0 / (1.0 - (double)p)) : 0.0f;
     d->call = call;

@@ -199,6 +199,8 @@ GRADS = [  # n, vocab, cols, ld_dy, ldd, shift, p, kind of tokens
     (5000, 40, 17, 20, 19, 1, 0.1, "skewed"), (4096, 256, 64, 64, 64, 0, 0.0, "one"), (4097, 3, 64, 64, 64, 2, 0.0, "one"),
     (40000, 5003, 65, 65, 65, 0, 0.1, "skewed"), (9000, 2, 8, 8, 8, 0, 0.0, "any"), (257, 17, 5, 5, 5, 0, 0.5, "none"),
     (100000, 66000, 4, 4, 4, 0, 0.0, "skewed"), (8192, 65536, 4, 4, 4, 0, 0.0, "falling"),
+    (2048, 7, 300, 300, 300, 0, 0.3, "skewed"), (2049, 2048, 264, 264, 264, 0, 0.1, "any"), (1500, 1, 9, 9, 9, 0, 0.0, "any"),
+    (2500, 30, 264, 272, 264, 8, 0.25, "skewed"),
 ]
 
 

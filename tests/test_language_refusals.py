@@ -71,35 +71,36 @@ def test_embedding_refuses(B):
 def test_embedding_grad_refuses(B):
     g = B.sidco_embedding_grad
     W = 0x8000000
+    N = 4000                                   # (up to 2048 tokens need no workspace)
     kw = dict(dy_type=1, token_type=3, dtable_type=0)
-    need = B.sidco_embedding_grad_workspace_bytes(4, 9, 8)
+    need = B.sidco_embedding_grad_workspace_bytes(N, 9, 8)
 
     def with_(**k):
         return {**kw, **k}
-    assert need > 0 and B.sidco_embedding_grad_workspace_bytes(0, 9, 8) == 0
+    assert need > 0 and B.sidco_embedding_grad_workspace_bytes(2048, 9, 8) == 0
     with pytest.raises(B.SidcoError) as err:
         B.sidco_embedding_grad_workspace_bytes(BIG, 9, 8)
     assert err.value.code == -10
-    assert code(g, P, 8, P, 4, BIG, 8, 1., Q, 8, W, need, **kw) == -10
-    assert code(g, P, 8, P, 4, 9, 8, 1., Q, 8, W, need, **with_(dy_type=7)) == -13
-    assert code(g, P, 8, P, 4, 9, 8, 1., Q, 8, W, need, **with_(dtable_type=7)) == -13
-    assert code(g, P, 8, P, 4, 9, 8, 1., Q, 8, W, need, **with_(token_type=2)) == -13
-    assert code(g, P, 7, P, 4, 9, 8, 1., Q, 8, W, need, **kw) == -6
-    assert code(g, P, 8, P, 4, 9, 8, 1., Q, 7, W, need, **kw) == -6
-    assert code(g, P, 8, P, 4, 9, 8, 1., Q, 8, W, need, p=2., **kw) == -6
+    assert code(g, P, 8, P, N, BIG, 8, 1., Q, 8, W, need, **kw) == -10
+    assert code(g, P, 8, P, N, 9, 8, 1., Q, 8, W, need, **with_(dy_type=7)) == -13
+    assert code(g, P, 8, P, N, 9, 8, 1., Q, 8, W, need, **with_(dtable_type=7)) == -13
+    assert code(g, P, 8, P, N, 9, 8, 1., Q, 8, W, need, **with_(token_type=2)) == -13
+    assert code(g, P, 7, P, N, 9, 8, 1., Q, 8, W, need, **kw) == -6
+    assert code(g, P, 8, P, N, 9, 8, 1., Q, 7, W, need, **kw) == -6
+    assert code(g, P, 8, P, N, 9, 8, 1., Q, 8, W, need, p=2., **kw) == -6
     for args in ((None, P, Q), (P, None, Q), (P, P, None)):
-        assert code(g, args[0], 8, args[1], 4, 9, 8, 1., args[2], 8, W, need, **kw) == -1
-    assert code(g, P + 1, 8, P, 4, 9, 8, 1., Q, 8, W, need, **kw) == -14
-    assert code(g, P, 8, P + 2, 4, 9, 8, 1., Q, 8, W, need, **kw) == -14
-    assert code(g, P, 8, P, 4, 9, 8, 1., Q + 2, 8, W, need, **kw) == -14
-    assert code(g, P, 8, P, 4, 9, 8, 1., Q, 8, None, need, **kw) == -8
-    assert code(g, P, 8, P, 4, 9, 8, 1., Q, 8, W, need - 1, **kw) == -8
-    assert code(g, P, 8, P, 4, 9, 8, 1., Q, 8, W + 128, need, **kw) == -8
-    assert code(g, P, 8, W, 4, 9, 8, 1., P + 60, 8, Q, need, **kw) == -9
-    assert code(g, P, 8, Q + 4, 4, 9, 8, 1., Q, 8, W, need, **kw) == -9
-    assert code(g, W, 8, P, 4, 9, 8, 1., Q, 8, W, need, **kw) == -9
-    assert code(g, P, 8, W + 256, 4, 9, 8, 1., Q, 8, W, need, **kw) == -9
-    assert code(g, P, 8, P, 4, 9, 8, 1., W, 8, W, need, **kw) == -9
+        assert code(g, args[0], 8, args[1], N, 9, 8, 1., args[2], 8, W, need, **kw) == -1
+    assert code(g, P + 1, 8, P, N, 9, 8, 1., Q, 8, W, need, **kw) == -14
+    assert code(g, P, 8, P + 2, N, 9, 8, 1., Q, 8, W, need, **kw) == -14
+    assert code(g, P, 8, P, N, 9, 8, 1., Q + 2, 8, W, need, **kw) == -14
+    assert code(g, P, 8, P, N, 9, 8, 1., Q, 8, None, need, **kw) == -8
+    assert code(g, P, 8, P, N, 9, 8, 1., Q, 8, W, need - 1, **kw) == -8
+    assert code(g, P, 8, P, N, 9, 8, 1., Q, 8, W + 128, need, **kw) == -8
+    assert code(g, P, 8, W, N, 9, 8, 1., P + 60, 8, Q, need, **kw) == -9
+    assert code(g, P, 8, Q + 4, N, 9, 8, 1., Q, 8, W, need, **kw) == -9
+    assert code(g, W, 8, P, N, 9, 8, 1., Q, 8, W, need, **kw) == -9
+    assert code(g, P, 8, W + 256, N, 9, 8, 1., Q, 8, W, need, **kw) == -9
+    assert code(g, P, 8, P, N, 9, 8, 1., W, 8, W, need, **kw) == -9
 
 
 def test_cross_entropy_refuses(B):
