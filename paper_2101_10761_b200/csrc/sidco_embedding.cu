@@ -23,265 +23,16 @@ namespace sidco_embedding_impl {
 using namespace sidco_elements;
 
 constexpr int kThreads = 256;
+constexpr int kEach = 8;              // neighbours of a row per lane
 
-// ---------------------------------------------------------------------------------------------- lookup
-
-// N neighbours of a row at a time: `lanes` lanes have a row, each kAhead groups of it in flight; a warp has 32 / lanes rows.
-// kVector: rows are aligned for groups and hold whole ones.  Otherwise groups start where the flat output's index is a multiple
-// of four, so that they are blocks of the generator, and a row's first and last group may be shared with its neighbours.
-constexpr int kAhead = 4;
-
-template <typename TI, typename TO, int N, bool kVector, bool kDrop>
-__global__ void __launch_bounds__(kThreads)
-    lookup_kernel(const TI* __restrict__ table, int64_t vocab, int cols, int64_t ld, const void* __restrict__ tokens, int wide,
-                  int64_t n, float scale, TO* __restrict__ out, int64_t ldo, const Dropout d, int lanes, int spans, int32_t* status) {
-    sidco_tc::wait_prerequisites();
-    sidco_tc::launch_dependents();
-    const int lane = threadIdx.x & (lanes - 1), rows = 32 / lanes;
-    const uint64_t call = kDrop ? call_of(d) : 0;
-    const int64_t workers = (int64_t)gridDim.x * (kThreads / 32), units = (n + rows - 1) / rows * spans;
-    // (a unit: the rows of a warp, one span of `lanes` x kAhead groups of them)
-    for (int64_t u = (int64_t)blockIdx.x * (kThreads / 32) + threadIdx.x / 32; u < units; u += workers) {
-        const int64_t i = u / spans * rows + (threadIdx.x & 31) / lanes;
-        if (i >= n) continue;
-        const int span = (int)(u % spans);
-        const int64_t t = token_at(tokens, wide, i);
-        const bool known = t >= 0 && t < vocab;
-        if (status && t >= vocab && lane == 0 && span == 0) atomicOr(status, SIDCO_EMBEDDING_ST_TOKEN);
-        const int64_t base = i * cols;                                // of the flat output
-        const int shift = kVector ? 0 : (int)(base % 4);
-        const TI* row = table + (known ? t * ld : 0);
-        TO* to = out + i * ldo;
-        const int first = (span * kAhead * lanes + lane) * N - shift;
-        float v[kAhead][N];
-#pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-            const int c = first + k * lanes * N;
-            if (kVector) {
-                if (known && c < cols) load(row + c, v[k]);
-            } else {
-#pragma unroll
-                for (int j = 0; j < N; ++j) v[k][j] = known && c + j >= 0 && c + j < cols ? widen(row[c + j]) : 0.0f;
-            }
-        }
-#pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-            const int c = first + k * lanes * N;
-            if (c >= cols) break;
-#pragma unroll
-            for (int j = 0; j < N; ++j) v[k][j] = known ? v[k][j] * scale : 0.0f;
-            if (kDrop) drop(d, call, (uint64_t)(base + c), v[k]);
-            if (kVector) {
-                store(to + c, v[k]);
-            } else {
-#pragma unroll
-                for (int j = 0; j < N; ++j)
-                    if (c + j >= 0 && c + j < cols) to[c + j] = narrow<TO>(v[k][j]);
-            }
-        }
-    }
-}
-
-// ---------------------------------------------------------------------------------------------- sorting
-//
-// Least significant digit first, eight bits at most per pass.  Items lie in contiguous parts per CTA, and within a CTA per
-// warp, so that (CTA, warp, step, lane) is the order of the items and ranking by it is stable.  A pass: every warp counts its
-// digits (lanes of one digit find each other by a match), counts become offsets (over warps in shared memory, over the CTAs
-// of the cluster in theirs), every warp places its items.  CTAs meet at cluster barriers; nothing spins.
-// Padding and tokens outside the table get the largest key and end up behind the others.
-
-constexpr int kSortThreads = 1024;
-constexpr int kSortWarps = kSortThreads / 32;
-constexpr int kSortMost = 8;                                          // CTAs of the sorting cluster
-constexpr int kDigits = 256;
-constexpr int kBatch = 8;                                             // steps whose reads are in flight together
-
-struct Sort {
-    const void* tokens;
-    int wide;
-    uint32_t n;
-    int64_t vocab;
-    uint32_t* keys[2];
-    uint32_t* at[2];
-    int passes, bits;                 // bits per pass
-    void* fill;                       // gradient to be set to zero, or NULL
-    int64_t rows, row_bytes, pitch_bytes;
-};
-
-__device__ __forceinline__ uint32_t remote_load4(uint32_t addr) {
-    uint32_t v;
-    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr));
-    return v;
-}
-
-// 0xff for 16-byte units of a row from its first aligned byte on, single bytes at its ends (rows may have any alignment)
-__device__ void fill_rows(const Sort& s, int64_t worker, int64_t workers) {
-    if (s.pitch_bytes == s.row_bytes) {                               // one row
-        uint8_t* p = static_cast<uint8_t*>(s.fill);
-        const int64_t bytes = s.rows * s.row_bytes;
-        const int64_t head = min(bytes, (int64_t)((16 - (uintptr_t)p % 16) % 16)), units = (bytes - head) / 16;
-        uint4* q = reinterpret_cast<uint4*>(p + head);
-        for (int64_t i = worker * kSortThreads + threadIdx.x; i < units; i += workers * kSortThreads) q[i] = uint4{};
-        if (worker == 0) {
-            for (int64_t i = threadIdx.x; i < head; i += kSortThreads) p[i] = 0;
-            for (int64_t i = head + units * 16 + threadIdx.x; i < bytes; i += kSortThreads) p[i] = 0;
-        }
-        return;
-    }
-    for (int64_t r = worker * kSortWarps + threadIdx.x / 32; r < s.rows; r += workers * kSortWarps) {
-        uint8_t* p = static_cast<uint8_t*>(s.fill) + r * s.pitch_bytes;
-        const int64_t head = min(s.row_bytes, (int64_t)((16 - (uintptr_t)p % 16) % 16)), units = (s.row_bytes - head) / 16;
-        uint4* q = reinterpret_cast<uint4*>(p + head);
-        for (int64_t i = threadIdx.x & 31; i < units; i += 32) q[i] = uint4{};
-        for (int64_t i = threadIdx.x & 31; i < head; i += 32) p[i] = 0;
-        for (int64_t i = head + units * 16 + (threadIdx.x & 31); i < s.row_bytes; i += 32) p[i] = 0;
-    }
-}
-
-__global__ void __launch_bounds__(kSortThreads) sort_kernel(const Sort s) {
-    __shared__ uint32_t s_count[kSortWarps][kDigits];                 // of every warp, then its next place
-    __shared__ uint32_t s_total[kDigits];                             // of the CTA
-    __shared__ uint32_t s_base[4][kDigits];                           // where a quarter of the warps begins
-    __shared__ uint32_t s_warp[8];
-    sidco_tc::wait_prerequisites();
-    sidco_tc::launch_dependents();
-    constexpr int ctas = kSortMost;
-    if ((int)blockIdx.x >= ctas) {
-        fill_rows(s, (int64_t)blockIdx.x - ctas, (int64_t)gridDim.x - ctas);
-        return;
-    }
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t rank = blockIdx.x;
-    // whole steps of 32 items per warp
-    const uint32_t per_warp = (uint32_t)(((uint64_t)s.n + (uint64_t)ctas * kSortWarps * 32 - 1) / ((uint64_t)ctas * kSortWarps * 32)) * 32;
-    const uint64_t from = (uint64_t)(rank * kSortWarps + warp) * per_warp;
-    const uint32_t first = (uint32_t)min(from, (uint64_t)s.n), end = (uint32_t)min(from + per_warp, (uint64_t)s.n);
-    for (int pass = 0; pass < s.passes; ++pass) {
-        const int shift = pass * s.bits;
-        const uint32_t mask = (1u << s.bits) - 1;
-        const uint32_t *keys = s.keys[pass & 1], *at = s.at[pass & 1];
-        uint32_t *to_keys = s.keys[(pass & 1) ^ 1], *to_at = s.at[(pass & 1) ^ 1];
-        const auto key_of = [&](uint32_t i) -> uint32_t {
-            if (pass) return __ldcg(keys + i);
-            const int64_t t = token_at(s.tokens, s.wide, i);
-            return t >= 0 && t < s.vocab ? (uint32_t)t : (uint32_t)s.vocab;
-        };
-        for (int i = lane; i < kDigits; i += 32) s_count[warp][i] = 0;
-        __syncwarp();
-        for (uint32_t i0 = first; i0 < end; i0 += 32 * kBatch) {
-            uint32_t key[kBatch];
-#pragma unroll
-            for (int k = 0; k < kBatch; ++k) key[k] = key_of(min(i0 + k * 32 + lane, end - 1));
-#pragma unroll
-            for (int k = 0; k < kBatch; ++k) {
-                if (i0 + k * 32 >= end) break;
-                const bool mine = i0 + k * 32 + lane < end;
-                const uint32_t digit = mine ? key[k] >> shift & mask : kDigits;
-                const uint32_t same = __match_any_sync(0xffffffffu, digit);
-                if (mine && (same & ((1u << lane) - 1)) == 0) s_count[warp][digit] += __popc(same);
-                __syncwarp();
-            }
-        }
-        __syncthreads();
-        // offsets of the warps, by a quarter of them per thread; totals
-        const int digit = threadIdx.x % kDigits, quarter = threadIdx.x / kDigits;
-        {
-            uint32_t c[kSortWarps / 4], sum = 0;
-#pragma unroll
-            for (int w = 0; w < kSortWarps / 4; ++w) c[w] = s_count[quarter * (kSortWarps / 4) + w][digit];
-#pragma unroll
-            for (int w = 0; w < kSortWarps / 4; ++w) {
-                s_count[quarter * (kSortWarps / 4) + w][digit] = sum;
-                sum += c[w];
-            }
-            s_base[quarter][digit] = sum;
-        }
-        __syncthreads();
-        if (threadIdx.x < kDigits) s_total[digit] = s_base[0][digit] + s_base[1][digit] + s_base[2][digit] + s_base[3][digit];
-        sidco_tc::cluster_sync();
-        uint32_t before = 0;
-        if (threadIdx.x < kDigits) {
-            uint32_t all = 0;                                         // this digit in the CTAs before / in all
-            for (int c = 0; c < kSortMost; ++c) {
-                const uint32_t v = remote_load4(sidco_tc::in_cta(sidco_tc::smem_addr(s_total + digit), c));
-                if (c < (int)rank) before += v;
-                all += v;
-            }
-            uint32_t up = all;                                        // digits up to this one: within the warp, then over warps
-#pragma unroll
-            for (int o = 1; o < 32; o *= 2) {
-                const uint32_t v = __shfl_up_sync(0xffffffffu, up, o);
-                if (lane >= o) up += v;
-            }
-            if (lane == 31) s_warp[warp] = up;
-            before += up - all;
-        }
-        __syncthreads();
-        if (threadIdx.x < kDigits) {
-            for (int w = 0; w < warp; ++w) before += s_warp[w];
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const uint32_t v = s_base[q][digit];
-                s_base[q][digit] = before;
-                before += v;
-            }
-        }
-        __syncthreads();
-        for (uint32_t i0 = first; i0 < end; i0 += 32 * kBatch) {
-            uint32_t key[kBatch], from[kBatch];
-#pragma unroll
-            for (int k = 0; k < kBatch; ++k) {
-                const uint32_t i = min(i0 + k * 32 + lane, end - 1);
-                key[k] = key_of(i);
-                from[k] = pass ? __ldcg(at + i) : i;
-            }
-#pragma unroll
-            for (int k = 0; k < kBatch; ++k) {
-                if (i0 + k * 32 >= end) break;
-                const bool mine = i0 + k * 32 + lane < end;
-                const uint32_t digit = mine ? key[k] >> shift & mask : kDigits;
-                const uint32_t same = __match_any_sync(0xffffffffu, digit), lower = same & ((1u << lane) - 1);
-                const uint32_t next = mine ? s_count[warp][digit] + __popc(lower) : 0;
-                __syncwarp();
-                if (mine) {
-                    if (lower == 0) s_count[warp][digit] = next + __popc(same);
-                    const uint32_t place = s_base[warp / (kSortWarps / 4)][digit] + next;
-                    to_keys[place] = key[k];
-                    to_at[place] = from[k];
-                }
-                __syncwarp();
-            }
-        }
-        // what the other CTAs have placed is read in the next pass (the barrier orders it); their totals have been read
-        sidco_tc::cluster_sync();
-    }
-}
-
-// ---------------------------------------------------------------------------------------------- sums
-
-struct Sums {
-    const uint32_t *keys, *at;        // sorted
-    uint32_t n, vocab;
-    int cols, chunk;                  // sorted positions per warp, at most 32
-    int64_t ld_dy, ldd;
-    uintptr_t lo, hi;                 // dy
-    float scale;
-    int add;
-    float* partial;                   // [chunks][2][pitch]: of the run that enters a chunk and of the one that leaves it
-    int64_t pitch;
-};
-
-constexpr int kEach = 8;              // columns per lane
-constexpr int kSlab = 32 * kEach;
-
-// kEach elements of a row of dy as they lie.  kVector: aligned and whole.  Otherwise of any alignment: two (three) aligned
-// 16-byte reads are put together; where these would leave dy, at its ends, single elements are read.
+// kEach elements of a row as they lie.  kVector: aligned and whole.  Otherwise of any alignment: two (three) aligned 16-byte
+// reads are put together; where these would leave the matrix, [lo, hi), single elements are read.
 template <typename T, bool kVector> struct Raw {
     static constexpr int kWords = kEach * (int)sizeof(T) / 4, kRead = kWords + (kVector ? 0 : 4);
     uint32_t w[kRead];
-    __device__ __forceinline__ void read(const T* p, int left, const Sums& s) {
+    __device__ __forceinline__ void read(const T* p, int left, uintptr_t lo, uintptr_t hi) {
         const uintptr_t start = (uintptr_t)p & ~(uintptr_t)15;
-        if (kVector || (start >= s.lo && start + kRead * 4 <= s.hi)) {
+        if (kVector || (start >= lo && start + kRead * 4 <= hi)) {
 #pragma unroll
             for (int i = 0; i < kRead / 4; ++i) {
                 const uint4 v = reinterpret_cast<const uint4*>(start)[i];
@@ -321,6 +72,354 @@ template <typename T, bool kVector> struct Raw {
     }
 };
 
+
+// ---------------------------------------------------------------------------------------------- lookup
+
+// N neighbours of a row at a time: `lanes` lanes have a row, each kAhead groups of it in flight; a warp has 32 / lanes rows.
+// kVector: rows are aligned for groups and hold whole ones.  Otherwise groups start where the flat output's index is a multiple
+// of four, so that they are blocks of the generator, and a row's first and last group may be shared with its neighbours.
+constexpr int kAhead = 4;
+
+template <typename TI, typename TO, int N, bool kVector, bool kDrop>
+__global__ void __launch_bounds__(kThreads, 4)
+    lookup_kernel(const TI* __restrict__ table, int64_t vocab, int cols, int64_t ld, const void* __restrict__ tokens, int wide,
+                  int64_t n, float scale, TO* __restrict__ out, int64_t ldo, const Dropout d, int lanes, int spans, int32_t* status) {
+    sidco_tc::wait_prerequisites();
+    sidco_tc::launch_dependents();
+    const int lane = threadIdx.x & (lanes - 1), rows = 32 / lanes;
+    const uint64_t call = kDrop ? call_of(d) : 0;
+    const int64_t workers = (int64_t)gridDim.x * (kThreads / 32), units = (n + rows - 1) / rows * spans;
+    // (a unit: the rows of a warp, one span of `lanes` x kAhead groups of them)
+    for (int64_t u = (int64_t)blockIdx.x * (kThreads / 32) + threadIdx.x / 32; u < units; u += workers) {
+        const int64_t i = u / spans * rows + (threadIdx.x & 31) / lanes;
+        if (i >= n) continue;
+        const int span = (int)(u % spans);
+        const int64_t t = token_at(tokens, wide, i);
+        const bool known = t >= 0 && t < vocab;
+        if (status && t >= vocab && lane == 0 && span == 0) atomicOr(status, SIDCO_EMBEDDING_ST_TOKEN);
+        const int64_t base = i * cols;                                // of the flat output
+        const int shift = kVector ? 0 : (int)(base % 4);
+        const TI* row = table + (known ? t * ld : 0);
+        TO* to = out + i * ldo;
+        const int first = (span * kAhead * lanes + lane) * N - shift;
+        alignas(16) TI raw[kAhead][N];                                // (as they lie: registers make warps)
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int c = first + k * lanes * N;
+            if (kVector) {
+                constexpr int kBytes = N * (int)sizeof(TI);
+                if (known && c < cols) {
+                    if constexpr (kBytes == 8) *reinterpret_cast<uint2*>(raw[k]) = *reinterpret_cast<const uint2*>(row + c);
+                    else
+#pragma unroll
+                        for (int i16 = 0; i16 < kBytes / 16; ++i16)
+                            reinterpret_cast<uint4*>(raw[k])[i16] = reinterpret_cast<const uint4*>(row + c)[i16];
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < N; ++j) raw[k][j] = known && c + j >= 0 && c + j < cols ? row[c + j] : narrow<TI>(0.0f);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int c = first + k * lanes * N;
+            if (c >= cols) break;
+            float v[N];
+#pragma unroll
+            for (int j = 0; j < N; ++j) v[j] = known ? widen(raw[k][j]) * scale : 0.0f;
+            if (kDrop) drop(d, call, (uint64_t)(base + c), v);
+            if (kVector) {
+                store(to + c, v);
+            } else {
+#pragma unroll
+                for (int j = 0; j < N; ++j)
+                    if (c + j >= 0 && c + j < cols) to[c + j] = narrow<TO>(v[j]);
+            }
+        }
+    }
+}
+
+// Rows without alignment, behind one another in `out`, which is aligned itself: groups of eight neighbours of the flat output,
+// written at once; a group belongs to the row in which it begins, and fetches the elements of the next one by one.
+template <typename TI, typename TO, bool kDrop>
+__global__ void __launch_bounds__(kThreads, 4)
+    flat_lookup_kernel(const TI* __restrict__ table, int64_t vocab, int cols, int64_t ld, const void* __restrict__ tokens, int wide,
+                       int64_t n, float scale, TO* __restrict__ out, const Dropout d, int lanes, int each, int spans, int32_t* status) {
+    constexpr int kGroups = 2;                                        // in flight
+    sidco_tc::wait_prerequisites();
+    sidco_tc::launch_dependents();
+    const int lane = threadIdx.x & (lanes - 1), rows = 32 / lanes;
+    const uint64_t call = kDrop ? call_of(d) : 0;
+    const uintptr_t lo = (uintptr_t)table, hi = vocab ? (uintptr_t)(table + (vocab - 1) * ld + cols) : lo;
+    const int64_t workers = (int64_t)gridDim.x * (kThreads / 32), units = (n + rows - 1) / rows * spans, all = n * cols;
+    for (int64_t u = (int64_t)blockIdx.x * (kThreads / 32) + threadIdx.x / 32; u < units; u += workers) {
+        const int64_t i = u / spans * rows + (threadIdx.x & 31) / lanes;
+        if (i >= n) continue;
+        const int span = (int)(u % spans);
+        const int64_t t = token_at(tokens, wide, i);
+        const bool known = t >= 0 && t < vocab;
+        if (status && t >= vocab && lane == 0 && span == 0) atomicOr(status, SIDCO_EMBEDDING_ST_TOKEN);
+        const int64_t base = i * cols;
+        const TI* row = table + (known ? t * ld : 0);
+        const int first = (int)(-base & 7) + (span * each * lanes + lane) * kEach;
+#pragma unroll 1
+        for (int k0 = 0; k0 < each; k0 += kGroups) {
+            Raw<TI, false> raw[kGroups];
+#pragma unroll
+            for (int k = 0; k < kGroups; ++k) {
+                const int c = first + (k0 + k) * lanes * kEach;
+                if (known && c < cols && k0 + k < each) raw[k].read(row + c, cols - c, lo, hi);
+            }
+#pragma unroll
+            for (int k = 0; k < kGroups; ++k) {
+                const int c = first + (k0 + k) * lanes * kEach;
+                if (c >= cols || k0 + k >= each) break;
+                float v[kEach] = {};
+                if (known) raw[k].widened(row + c, v);
+                if (c + kEach > cols) {
+                    int64_t r = i;
+                    int at = c;
+                    const TI* from = known ? row : nullptr;
+#pragma unroll
+                    for (int j = 0; j < kEach; ++j) {
+                        while (at >= cols && r < n) {                 // (rows may be shorter than a group)
+                            at -= cols;
+                            if (++r < n) {
+                                const int64_t other = token_at(tokens, wide, r);
+                                from = other >= 0 && other < vocab ? table + other * ld : nullptr;
+                            }
+                        }
+                        if (r > i) v[j] = r < n && from ? widen(from[at]) : 0.0f;
+                        ++at;
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < kEach; ++j) v[j] *= scale;
+                if (kDrop) drop(d, call, (uint64_t)(base + c), v);
+                TO* to = out + base + c;
+                if (base + c + kEach <= all) {
+                    store(to, v);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < kEach; ++j)
+                        if (base + c + j < all) to[j] = narrow<TO>(v[j]);
+                }
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- sorting
+//
+// Least significant digit first, nine bits at most per pass.  Items lie in contiguous parts per CTA, and within a CTA per
+// warp, so that (CTA, warp, step, lane) is the order of the items and ranking by it is stable.  A pass: every warp counts its
+// digits (lanes of one digit find each other by votes), counts become offsets (over warps in shared memory, over the CTAs
+// of the cluster in theirs), every warp places its items.  CTAs meet at cluster barriers; nothing spins.
+// Padding and tokens outside the table get the largest key and end up behind the others.
+// Bound by the writes: 32 items of a warp go to 32 places (key and position apart took twice as long), and by five barriers a
+// pass.  65536 tokens of 5003 words 26 us.
+
+constexpr int kSortThreads = 1024;
+constexpr int kSortWarps = kSortThreads / 32;
+constexpr int kSortMost = 16;                                         // CTAs of the sorting cluster
+constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits;
+constexpr int kParts = kSortThreads / kDigits;
+constexpr int kBatch = 8;                                             // steps whose reads are in flight together
+constexpr int kSortSmem = kSortWarps * kDigits * 4;
+
+struct Sort {
+    const void* tokens;
+    int wide;
+    uint32_t n;
+    int64_t vocab;
+    uint2* items[2];                  // (key, position)
+    int passes, bits;                 // bits per pass
+    int ctas;                         // that sort
+    void* fill;                       // gradient to be set to zero, or NULL
+    int64_t rows, row_bytes, pitch_bytes;
+};
+
+__device__ __forceinline__ uint32_t remote_load4(uint32_t addr) {
+    uint32_t v;
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr));
+    return v;
+}
+
+// 0xff for 16-byte units of a row from its first aligned byte on, single bytes at its ends (rows may have any alignment)
+__device__ void fill_rows(const Sort& s, int64_t worker, int64_t workers) {
+    if (s.pitch_bytes == s.row_bytes) {                               // one row
+        uint8_t* p = static_cast<uint8_t*>(s.fill);
+        const int64_t bytes = s.rows * s.row_bytes;
+        const int64_t head = min(bytes, (int64_t)((16 - (uintptr_t)p % 16) % 16)), units = (bytes - head) / 16;
+        uint4* q = reinterpret_cast<uint4*>(p + head);
+        for (int64_t i = worker * kSortThreads + threadIdx.x; i < units; i += workers * kSortThreads) q[i] = uint4{};
+        if (worker == 0) {
+            for (int64_t i = threadIdx.x; i < head; i += kSortThreads) p[i] = 0;
+            for (int64_t i = head + units * 16 + threadIdx.x; i < bytes; i += kSortThreads) p[i] = 0;
+        }
+        return;
+    }
+    for (int64_t r = worker * kSortWarps + threadIdx.x / 32; r < s.rows; r += workers * kSortWarps) {
+        uint8_t* p = static_cast<uint8_t*>(s.fill) + r * s.pitch_bytes;
+        const int64_t head = min(s.row_bytes, (int64_t)((16 - (uintptr_t)p % 16) % 16)), units = (s.row_bytes - head) / 16;
+        uint4* q = reinterpret_cast<uint4*>(p + head);
+        for (int64_t i = threadIdx.x & 31; i < units; i += 32) q[i] = uint4{};
+        for (int64_t i = threadIdx.x & 31; i < head; i += 32) p[i] = 0;
+        for (int64_t i = head + units * 16 + (threadIdx.x & 31); i < s.row_bytes; i += 32) p[i] = 0;
+    }
+}
+
+// The lanes whose digit is this lane's, by a vote per bit.
+__device__ __forceinline__ uint32_t lanes_alike(uint32_t digit, int bits, bool mine) {
+    uint32_t same = __ballot_sync(0xffffffffu, mine);
+    for (int b = 0; b < bits; ++b) {
+        const uint32_t set = __ballot_sync(0xffffffffu, digit >> b & 1);
+        same &= digit >> b & 1 ? set : ~set;
+    }
+    return same;
+}
+
+__global__ void __launch_bounds__(kSortThreads) sort_kernel(const Sort s) {
+    extern __shared__ uint32_t s_counts[];                            // [warp][digit]: how many, then where its next goes
+    __shared__ uint32_t s_total[kDigits];                             // of the CTA
+    __shared__ uint32_t s_base[kParts][kDigits];                      // where a part of the warps begins
+    __shared__ uint32_t s_warp[kDigits / 32];
+    sidco_tc::wait_prerequisites();
+    sidco_tc::launch_dependents();
+    if ((int)blockIdx.x >= s.ctas) {
+        fill_rows(s, (int64_t)blockIdx.x - s.ctas, (int64_t)gridDim.x - s.ctas);
+        return;
+    }
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = blockIdx.x;
+    uint32_t* count = s_counts + warp * kDigits;
+    // whole steps of 32 items per warp
+    const uint64_t warps = s.ctas * kSortWarps;
+    const uint32_t per_warp = (uint32_t)((s.n + warps * 32 - 1) / (warps * 32)) * 32;
+    const uint64_t from = (rank * kSortWarps + warp) * (uint64_t)per_warp;
+    const uint32_t first = (uint32_t)min(from, (uint64_t)s.n), end = (uint32_t)min(from + per_warp, (uint64_t)s.n);
+    const uint32_t mask = (1u << s.bits) - 1;
+    for (int pass = 0; pass < s.passes; ++pass) {
+        const int shift = pass * s.bits;
+        const uint2* items = s.items[pass & 1];
+        uint2* to = s.items[(pass & 1) ^ 1];
+        uint2 item[kBatch];
+        const auto read = [&](uint32_t i0) {
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+                const uint32_t i = min(i0 + k * 32 + lane, end - 1);
+                if (pass) {
+                    item[k] = __ldcg(items + i);
+                } else {
+                    const int64_t t = token_at(s.tokens, s.wide, i);
+                    item[k] = make_uint2(t >= 0 && t < s.vocab ? (uint32_t)t : (uint32_t)s.vocab, i);
+                }
+            }
+        };
+        for (int i = lane; i < kDigits; i += 32) count[i] = 0;
+        __syncwarp();
+        for (uint32_t i0 = first; i0 < end; i0 += 32 * kBatch) {
+            read(i0);
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+                if (i0 + k * 32 >= end) break;
+                const bool mine = i0 + k * 32 + lane < end;
+                const uint32_t digit = item[k].x >> shift & mask, same = lanes_alike(digit, s.bits, mine);
+                if (mine && (same & ((1u << lane) - 1)) == 0) count[digit] += __popc(same);
+                __syncwarp();
+            }
+        }
+        __syncthreads();
+        // offsets of the warps, by a part of them per thread; totals
+        const int digit = threadIdx.x % kDigits, part = threadIdx.x / kDigits;
+        {
+            uint32_t c[kSortWarps / kParts], sum = 0;
+            uint32_t* at = s_counts + part * (kSortWarps / kParts) * kDigits + digit;
+#pragma unroll
+            for (int w = 0; w < kSortWarps / kParts; ++w) c[w] = at[w * kDigits];
+#pragma unroll
+            for (int w = 0; w < kSortWarps / kParts; ++w) {
+                at[w * kDigits] = sum;
+                sum += c[w];
+            }
+            s_base[part][digit] = sum;
+        }
+        __syncthreads();
+        if (threadIdx.x < kDigits) {
+            uint32_t sum = 0;
+#pragma unroll
+            for (int q = 0; q < kParts; ++q) sum += s_base[q][digit];
+            s_total[digit] = sum;
+        }
+        sidco_tc::cluster_sync();
+        uint32_t before = 0;
+        if (threadIdx.x < kDigits) {
+            uint32_t v[kSortMost], all = 0;                           // this digit in the CTAs before / in all
+#pragma unroll
+            for (int c = 0; c < kSortMost; ++c) v[c] = c >= s.ctas ? 0 : remote_load4(sidco_tc::in_cta(sidco_tc::smem_addr(s_total + digit), c));
+#pragma unroll
+            for (int c = 0; c < kSortMost; ++c) {
+                if (c < (int)rank) before += v[c];
+                all += v[c];
+            }
+            uint32_t up = all;                                        // digits up to this one: within the warp, then over warps
+#pragma unroll
+            for (int o = 1; o < 32; o *= 2) {
+                const uint32_t w = __shfl_up_sync(0xffffffffu, up, o);
+                if (lane >= o) up += w;
+            }
+            if (lane == 31) s_warp[warp] = up;
+            before += up - all;
+        }
+        __syncthreads();
+        if (threadIdx.x < kDigits) {
+            for (int w = 0; w < warp; ++w) before += s_warp[w];
+#pragma unroll
+            for (int q = 0; q < kParts; ++q) {
+                const uint32_t w = s_base[q][digit];
+                s_base[q][digit] = before;
+                before += w;
+            }
+        }
+        __syncthreads();
+        const uint32_t* base = s_base[warp / (kSortWarps / kParts)];
+        for (uint32_t i0 = first; i0 < end; i0 += 32 * kBatch) {
+            if (per_warp > 32 * kBatch) read(i0);                     // (a single batch is still there)
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+                if (i0 + k * 32 >= end) break;
+                const bool mine = i0 + k * 32 + lane < end;
+                const uint32_t digit = item[k].x >> shift & mask, same = lanes_alike(digit, s.bits, mine), lower = same & ((1u << lane) - 1);
+                const uint32_t next = mine ? count[digit] + __popc(lower) : 0;
+                __syncwarp();
+                if (mine) {
+                    if (lower == 0) count[digit] = next + __popc(same);
+                    to[base[digit] + next] = item[k];
+                }
+                __syncwarp();
+            }
+        }
+        // what the other CTAs have placed is read in the next pass (the barrier orders it); their totals have been read
+        sidco_tc::cluster_sync();
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- sums
+
+struct Sums {
+    const uint2* items;               // sorted (key, position)
+    uint32_t n, vocab;
+    int cols, chunk;                  // sorted positions per warp, at most 32
+    int64_t ld_dy, ldd;
+    uintptr_t lo, hi;                 // dy
+    float scale;
+    int add;
+    float* partial;                   // [chunks][2][pitch]: of the run that enters a chunk and of the one that leaves it
+    int64_t pitch;
+};
+
+constexpr int kSlab = 32 * kEach;
+
 // vector: 8 or 4 columns can be written at once (and there are whole ones), or 1.
 template <typename TO>
 __device__ __forceinline__ void write_row(const Sums& s, TO* row, int left, int vector, const float (&sum)[kEach]) {
@@ -354,58 +453,66 @@ __device__ __forceinline__ void write_row(const Sums& s, TO* row, int left, int 
 }
 
 // Sorted positions 0 .. count-1 of a chunk, for one slab of columns: row_at(k) is the position's row of dy, ends(k) whether a
-// run ends behind it, done(k) takes a run's sum (in `sum`) there.  The next row comes while one is added: with more rows in
-// flight per warp fewer warps fit, and the generator's code is there once per row.
-template <typename TI, bool kVector, bool kDrop, typename RowAt, typename Ends, typename Done>
+// run ends behind it, done(k) takes a run's sum (in `sum`) there.  kRows rows come while kRows are added: one where words are
+// drawn (that is bound by the generator's products, and its code is there once), four otherwise.
+template <int kRows, typename TI, bool kVector, bool kDrop, typename RowAt, typename Ends, typename Done>
 __device__ __forceinline__ void add_up(const TI* dy, const Sums& s, const Dropout& d, uint64_t call, int c, int left, int count,
                                        RowAt row_at, Ends ends, Done done, float (&sum)[kEach]) {
-    Raw<TI, kVector> raw, coming;
-    uint32_t at = 0, at_next = 0;
-    if (count > 0) {
-        at_next = row_at(0);
-        if (left > 0) coming.read(dy + at_next * s.ld_dy + c, left, s);
-    }
-#pragma unroll 1
-    for (int k = 0; k < count; ++k) {
-        raw = coming;
-        at = at_next;
-        at_next = row_at(min(k + 1, count - 1));
-        if (left > 0 && k + 1 < count) coming.read(dy + at_next * s.ld_dy + c, left, s);
-        float v[kEach];
-        raw.widened(dy + at * s.ld_dy + c, v);
-        if (kDrop) {
-            const uint64_t first = (uint64_t)at * s.cols + c;
-            if (first % 4 == 0) drop(d, call, first, v);              // (the same for the whole warp)
-            else drop<kEach, false>(d, call, first, v);
+    Raw<TI, kVector> now[kRows], next[kRows];
+    uint32_t at[kRows], at_next[kRows];
+    const auto read = [&](int k) {
+#pragma unroll
+        for (int j = 0; j < kRows; ++j) {
+            at_next[j] = row_at(min(k + j, count - 1));
+            if (left > 0 && k + j < count) next[j].read(dy + at_next[j] * s.ld_dy + c, left, s.lo, s.hi);
         }
+    };
+    if (count > 0) read(0);
+#pragma unroll 1
+    for (int k = 0; k < count; k += kRows) {
 #pragma unroll
-        for (int e = 0; e < kEach; ++e) sum[e] += v[e];
-        if (ends(k)) {
-            done(k);
+        for (int j = 0; j < kRows; ++j) now[j] = next[j], at[j] = at_next[j];
+        read(k + kRows);
 #pragma unroll
-            for (int e = 0; e < kEach; ++e) sum[e] = 0.0f;
+        for (int j = 0; j < kRows; ++j) {
+            if (k + j >= count) break;
+            float v[kEach];
+            now[j].widened(dy + at[j] * s.ld_dy + c, v);
+            if (kDrop) {
+                const uint64_t first = (uint64_t)at[j] * s.cols + c;
+                if (first % 4 == 0) drop(d, call, first, v);          // (the same for the whole warp)
+                else drop<kEach, false>(d, call, first, v);
+            }
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) sum[e] += v[e];
+            if (ends(k + j)) {
+                done(k + j);
+#pragma unroll
+                for (int e = 0; e < kEach; ++e) sum[e] = 0.0f;
+            }
         }
     }
 }
 
 template <typename TI, typename TO, bool kVector, bool kDrop>
-__global__ void __launch_bounds__(kThreads, 4)
+__global__ void __launch_bounds__(kThreads, kDrop ? 4 : 2)
     sum_kernel(const TI* __restrict__ dy, TO* __restrict__ out, const Sums s, const Dropout d, uint32_t chunks, int slabs, int out_vector) {
     sidco_tc::wait_prerequisites();
     sidco_tc::launch_dependents();
     const int lane = threadIdx.x & 31;
     const uint64_t unit = (uint64_t)blockIdx.x * (kThreads / 32) + threadIdx.x / 32;
     if (unit >= (uint64_t)chunks * slabs) return;
+    const uint64_t call = kDrop ? call_of(d) : 0;
+    float sum[kEach] = {};
     const uint32_t chunk = (uint32_t)(unit / slabs);
     const int c = (int)(unit % slabs) * kSlab + lane * kEach, left = s.cols - c;
     const uint32_t first = chunk * s.chunk;
     const int count = (int)min((uint32_t)s.chunk, s.n - first);
     // (lane l holds the l-th key and position)
-    const uint32_t my_key = lane < count ? s.keys[first + lane] : s.vocab;
-    const uint32_t my_at = lane < count ? s.at[first + lane] : 0;
-    const uint32_t before = first ? s.keys[first - 1] : s.vocab;
-    const uint32_t behind = first + count < s.n ? s.keys[first + count] : s.vocab;
-    const uint64_t call = kDrop ? call_of(d) : 0;
+    const uint2 mine = lane < count ? s.items[first + lane] : make_uint2(s.vocab, 0);
+    const uint32_t my_key = mine.x, my_at = mine.y;
+    const uint32_t before = first ? s.items[first - 1].x : s.vocab;
+    const uint32_t behind = first + count < s.n ? s.items[first + count].x : s.vocab;
     const int valid = __popc(__ballot_sync(0xffffffffu, my_key < s.vocab));        // (padding is behind all others)
     if (valid == 0) return;
     uint32_t next = __shfl_down_sync(0xffffffffu, my_key, 1);
@@ -413,8 +520,7 @@ __global__ void __launch_bounds__(kThreads, 4)
     const uint32_t ends = __ballot_sync(0xffffffffu, my_key != next);              // a run ends behind position l
     bool entered = __shfl_sync(0xffffffffu, my_key, 0) == before;                  // the run began before this chunk
     float* partial = s.partial + (uint64_t)chunk * 2 * s.pitch + c;
-    float sum[kEach] = {};
-    add_up<TI, kVector, kDrop>(
+    add_up<kDrop ? 1 : 4, TI, kVector, kDrop>(
         dy, s, d, call, c, left, valid, [&](int k) { return __shfl_sync(0xffffffffu, my_at, k); },
         [&](int k) { return (ends >> k & 1) != 0; },
         [&](int k) {
@@ -427,43 +533,46 @@ __global__ void __launch_bounds__(kThreads, 4)
     if (valid == count && !(ends >> (count - 1) & 1) && left > 0) store(partial + (entered ? 0 : s.pitch), sum);
 }
 
+constexpr int kJoinEach = 4, kJoinSlab = 32 * kJoinEach;              // columns per lane: a long run needs many rows in flight
+
 // A run that leaves the chunk in which it began: its partial sums, one per chunk, in order.
 template <typename TO>
 __global__ void __launch_bounds__(kThreads, 2) join_kernel(TO* __restrict__ out, const Sums s, uint32_t chunks, int slabs, int out_vector) {
-    constexpr int kRows = 8;
+    constexpr int kRows = 16;
     sidco_tc::wait_prerequisites();
     sidco_tc::launch_dependents();
     const uint64_t unit = (uint64_t)blockIdx.x * (kThreads / 32) + threadIdx.x / 32;
     if (unit >= (uint64_t)chunks * slabs) return;
     const uint32_t chunk = (uint32_t)(unit / slabs);
-    const int lane = threadIdx.x & 31, c = (int)(unit % slabs) * kSlab + lane * kEach, left = s.cols - c;
+    const int lane = threadIdx.x & 31, c = (int)(unit % slabs) * kJoinSlab + lane * kJoinEach, left = s.cols - c;
     const uint32_t first = chunk * s.chunk, next = first + s.chunk;
     if (next >= s.n) return;
-    const uint32_t key = s.keys[next - 1];
-    if (key >= s.vocab || s.keys[next] != key) return;                // it ends here
-    if (s.keys[first] == key && first && s.keys[first - 1] == key) return;      // it began earlier
+    const uint32_t key = s.items[next - 1].x;
+    if (key >= s.vocab || s.items[next].x != key) return;             // it ends here
+    if (s.items[first].x == key && first && s.items[first - 1].x == key) return;        // it began earlier
     // how many of the following chunks it reaches: looked up by 32 lanes at a time
     uint32_t more = 0;
     for (;;) {
         const uint64_t p = (uint64_t)next + (uint64_t)(more + lane) * s.chunk;
-        const uint32_t in = __ballot_sync(0xffffffffu, p < s.n && s.keys[p] == key);
+        const uint32_t in = __ballot_sync(0xffffffffu, p < s.n && s.items[p].x == key);
         more += in == 0xffffffffu ? 32 : __ffs(~in) - 1;
         if (in != 0xffffffffu) break;
     }
     if (left <= 0) return;
     const float* p = s.partial + (uint64_t)chunk * 2 * s.pitch + c;
-    float sum[kEach];
+    float sum[kJoinEach];
     load(p + s.pitch, sum);
     for (uint32_t k = 1; k <= more; k += kRows) {
-        float v[kRows][kEach];
+        float v[kRows][kJoinEach];
 #pragma unroll
         for (int j = 0; j < kRows; ++j) load(p + (uint64_t)min(k + j, more) * 2 * s.pitch, v[j]);
 #pragma unroll
         for (int j = 0; j < kRows; ++j)
 #pragma unroll
-            for (int e = 0; e < kEach; ++e) sum[e] += k + j <= more ? v[j][e] : 0.0f;
+            for (int e = 0; e < kJoinEach; ++e) sum[e] += k + j <= more ? v[j][e] : 0.0f;
     }
-    write_row(s, out + (int64_t)key * s.ldd + c, left, out_vector, sum);
+    const float whole[kEach] = {sum[0], sum[1], sum[2], sum[3]};
+    write_row(s, out + (int64_t)key * s.ldd + c, min(left, kJoinEach), min(out_vector, kJoinEach), whole);
 }
 
 // ---------------------------------------------------------------------------------------------- few tokens
@@ -471,7 +580,7 @@ __global__ void __launch_bounds__(kThreads, 2) join_kernel(TO* __restrict__ out,
 // Up to kFewMost tokens take one launch: a CTA has a range of the table's rows and a slab of its columns.  It picks its tokens
 // out of all, sends zeros to the rows that have none (they leave while it goes on), and ranks its tokens by counting; its warps take equal parts of
 // the sorted list, whose runs they join in shared memory where they cross from one part to the next.  Nobody waits for another
-// CTA.  (Three launches took 25 us for 700 tokens of 10000 x 1500, this takes FEWUS.)
+// CTA.  (Three launches took 25 us for 700 tokens of 10000 x 1500, this takes 16.)
 
 constexpr int kFewMost = 2048, kFewThreads = 512, kFewWarps = kFewThreads / 32, kFewEach = kFewMost / kFewThreads;
 constexpr int kFewRange = 8192;       // rows of a range, at most
@@ -563,7 +672,7 @@ __global__ void __launch_bounds__(kFewThreads, 2)
     const int part = (found + kFewWarps - 1) / kFewWarps, first = min(found, warp * part), count = min(part, found - first);
     bool entered = count > 0 && first > 0 && s_sorted[first - 1] == s_sorted[first];
     float sum[kEach] = {};
-    add_up<TI, kVector, kDrop>(
+    add_up<1, TI, kVector, kDrop>(
         dy, s, d, call, c, left, count, [&](int k) { return (uint32_t)s_at[first + k]; },
         [&](int k) { return first + k + 1 == found || s_sorted[first + k + 1] != s_sorted[first + k]; },
         [&](int k) {
@@ -602,18 +711,16 @@ static int chunk_of(int64_t n, int64_t cols) {
 }
 
 struct Layout {
-    int64_t keys[2], at[2], partial, pitch, bytes;
+    int64_t items[2], partial, pitch, bytes;
 };
 
 static Layout layout_of(int64_t n, int64_t cols) {
     Layout l{};
     if (n <= kFewMost) return l;                                      // (one launch, no lists)
-    const int64_t list = (n * 4 + 255) / 256 * 256, chunk = chunk_of(n, cols);
-    l.keys[0] = 0;
-    l.keys[1] = list;
-    l.at[0] = 2 * list;
-    l.at[1] = 3 * list;
-    l.partial = 4 * list;
+    const int64_t list = (n * 8 + 255) / 256 * 256, chunk = chunk_of(n, cols);
+    l.items[0] = 0;
+    l.items[1] = list;
+    l.partial = 2 * list;
     l.pitch = (cols + kEach - 1) / kEach * kEach;
     l.bytes = l.partial + (n + chunk - 1) / chunk * 2 * l.pitch * 4;
     return l;
@@ -663,10 +770,13 @@ int sidco_embedding(const void* table, int table_type, int64_t vocab, int64_t co
         return cols % k == 0 && aligned(table, ld, table_type, k) && aligned(out, ldo, out_type, k);
     };
     const int vector = fits(8) ? 8 : fits(4) ? 4 : 0;
-    const int64_t groups = vector ? cols / vector : (cols + 3) / 4 + 1;
+    const bool flat = !vector && ldo == cols && (uintptr_t)out % 16 == 0;
+    const int64_t groups = vector ? cols / vector : flat ? (cols + 7) / 8 : (cols + 3) / 4 + 1;
     int lanes = 1;
     while (lanes < 32 && lanes < groups) lanes *= 2;
-    const int64_t spans = (groups + lanes * kAhead - 1) / (lanes * kAhead), rows = 32 / lanes;
+    // (rows without alignment: up to eight groups per lane, as many in every span)
+    const int64_t most = flat ? 8 : kAhead, spans = (groups + lanes * most - 1) / (lanes * most), rows = 32 / lanes;
+    const int each = (int)((groups + lanes * spans - 1) / (lanes * spans));
     int sms = 0;
     if (const cudaError_t e = sm_count(&sms); e != cudaSuccess) return (int)e;
     // (eight CTAs are resident per SM; four rounds of them even out)
@@ -675,6 +785,10 @@ int sidco_embedding(const void* table, int table_type, int64_t vocab, int64_t co
         return with_type(out_type, [&](auto* b) {
             using TI = std::remove_pointer_t<decltype(a)>;
             using TO = std::remove_pointer_t<decltype(b)>;
+            if (flat)
+                return (int)launch(on ? flat_lookup_kernel<TI, TO, true> : flat_lookup_kernel<TI, TO, false>, grid, kThreads, 0, s, 1,
+                                   (const TI*)table, vocab, (int)cols, ld, tokens, (int)(token_type == SIDCO_T_I64), n, scale,
+                                   (TO*)out, d, lanes, each, (int)spans, status);
             const auto kernel = vector == 8   ? on ? lookup_kernel<TI, TO, 8, true, true> : lookup_kernel<TI, TO, 8, true, false>
                                 : vector == 4 ? on ? lookup_kernel<TI, TO, 4, true, true> : lookup_kernel<TI, TO, 4, true, false>
                                 : on          ? lookup_kernel<TI, TO, 4, false, true>
@@ -768,32 +882,35 @@ int sidco_embedding_grad(const void* dy, int dy_type, int64_t ld_dy, const void*
     so.n = (uint32_t)n;
     so.vocab = vocab;
     for (int i = 0; i < 2; ++i) {
-        so.keys[i] = reinterpret_cast<uint32_t*>(ws + l.keys[i]);
-        so.at[i] = reinterpret_cast<uint32_t*>(ws + l.at[i]);
+        so.items[i] = reinterpret_cast<uint2*>(ws + l.items[i]);
     }
     int bits = 1;
     while ((vocab >> bits) > 0) ++bits;                               // keys 0 .. vocab
-    so.passes = (bits + 7) / 8;
+    so.passes = (bits + kDigitBits - 1) / kDigitBits;
     so.bits = (bits + so.passes - 1) / so.passes;
     so.fill = add ? nullptr : dtable;
     so.rows = vocab;
     so.row_bytes = cols * size_of(dtable_type);
     so.pitch_bytes = vocab > 1 ? ldd * size_of(dtable_type) : so.row_bytes;
-    const int ctas = kSortMost;
-    int grid = ctas;
-    if (!add) grid += std::max(ctas, (2 * sms - ctas) / ctas * ctas);
-    e = launch(sort_kernel, dim3((unsigned)grid), kSortThreads, 0, st, ctas, so);
+    // Sixteen CTAs sort faster than eight (65536 tokens 25 us instead of 34), but clusters of sixteen leave SMs out, and the
+    // zeros, which take longer than the sorting, want all of them (32768 x 2048 of 128000 154 us instead of 161).
+    so.ctas = add ? kSortMost : kSortMost / 2;
+    const int grid = add ? so.ctas : 2 * sms / so.ctas * so.ctas;
+    e = cudaFuncSetAttribute(sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSortSmem);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(sort_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e == cudaSuccess) e = launch(sort_kernel, dim3((unsigned)grid), kSortThreads, kSortSmem, st, so.ctas, so);
     if (e != cudaSuccess) return (int)e;
     sidco_internal::note_launch();
 
-    su.keys = so.keys[so.passes & 1];
-    su.at = so.at[so.passes & 1];
+    su.items = so.items[so.passes & 1];
     su.chunk = chunk_of(n, cols);
     su.partial = reinterpret_cast<float*>(ws + l.partial);
     su.pitch = l.pitch;
     const uint32_t chunks = (uint32_t)((n + su.chunk - 1) / su.chunk);
     const int64_t blocks = ((int64_t)chunks * slabs + kThreads / 32 - 1) / (kThreads / 32);
-    if (blocks > 0x7fffffff) return SIDCO_E_SIZE;
+    const int join_slabs = (int)((cols + kJoinSlab - 1) / kJoinSlab);
+    const int64_t join_blocks = ((int64_t)chunks * join_slabs + kThreads / 32 - 1) / (kThreads / 32);
+    if (join_blocks > 0x7fffffff) return SIDCO_E_SIZE;
     const int rc = with_type(dtable_type, [&](auto* b) {
         using TO = std::remove_pointer_t<decltype(b)>;
         const int first = with_type(dy_type, [&](auto* a) {
@@ -805,7 +922,7 @@ int sidco_embedding_grad(const void* dy, int dy_type, int64_t ld_dy, const void*
         });
         if (first) return first;
         sidco_internal::note_launch();
-        return (int)launch(join_kernel<TO>, dim3((unsigned)blocks), kThreads, 0, st, 1, (TO*)dtable, su, chunks, slabs,
+        return (int)launch(join_kernel<TO>, dim3((unsigned)join_blocks), kThreads, 0, st, 1, (TO*)dtable, su, chunks, join_slabs,
                            out_vector);
     });
     if (rc == 0) sidco_internal::note_launch();
