@@ -594,11 +594,17 @@ struct Scale {
     int dw;                           // dW is wanted
 };
 
+// Stages that a tile of dW takes: its own, but not fewer than pass while its sums leave (4.5 us; a stage takes 0.35).
+__host__ __device__ inline int stages_of_dw(int rows) {
+    const int steps = (rows + kStageK - 1) / kStageK;
+    return steps > 13 ? steps : 13;
+}
+
 // What p parts of dX's sums over the vocabulary cost, in stages of a pair: its longest list of units, or its share of all work,
 // and writing and reading the parts (a stage lasts 512 cycles, in which an SM pair moves about 24 KB).
 __host__ __device__ inline float cost_of_parts(int p, int rows, int vocab, int hidden, bool dw) {
     const int tiles_m = (rows + kTile - 1) / kTile, tiles_h = (hidden + kTile - 1) / kTile;
-    const int steps_v = (vocab + kStageK - 1) / kStageK, steps_r = (rows + kStageK - 1) / kStageK;
+    const int steps_v = (vocab + kStageK - 1) / kStageK, steps_r = stages_of_dw(rows);
     const float units = (float)tiles_m * tiles_h * p, unit = (float)((steps_v + p - 1) / p);
     const float work_w = dw ? (float)((vocab + kTile - 1) / kTile) * tiles_h * steps_r : 0.0f;
     const float even = ((float)tiles_m * tiles_h * steps_v + work_w) / kPairs + (dw ? 0.5f * steps_r : 0.0f);
@@ -690,8 +696,10 @@ template <typename T> __global__ void __launch_bounds__(kScaleThreads) scale_ker
     launch_dependents();
     const int rows = rows_of_piece(a.z, a.head), r = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     T* e = static_cast<T*>(a.e) + r * a.pitch;
-    const int vectors = (a.z.vocab + 7) / 8;
-    if (r == 0 && warp == kScaleThreads / 32 - 1) {                   // a lane per number of parts
+    // (where there are few rows, several CTAs share one)
+    const int all = (a.z.vocab + 7) / 8, share = (all + (int)gridDim.y - 1) / (int)gridDim.y;
+    const int from = (int)blockIdx.y * share, vectors = min(all, from + share);
+    if (r == 0 && blockIdx.y == 0 && warp == kScaleThreads / 32 - 1) {                   // a lane per number of parts
         const int p = lane + 1;
         const uint32_t cost = parts_fit(p, rows, a.z.vocab, a.part_rows)
                                   ? __float_as_uint(cost_of_parts(p, rows, a.z.vocab, a.z.hidden, a.dw)) : 0xffffffffu;
@@ -701,7 +709,7 @@ template <typename T> __global__ void __launch_bounds__(kScaleThreads) scale_ker
     }
     if (r >= rows) {
         if (r < (rows + kStageK - 1) / kStageK * kStageK)
-            for (int i = threadIdx.x; i < vectors; i += kScaleThreads) reinterpret_cast<uint4*>(e)[i] = uint4{};
+            for (int i = from + threadIdx.x; i < vectors; i += kScaleThreads) reinterpret_cast<uint4*>(e)[i] = uint4{};
         return;
     }
     const float2* stats = a.stats + (int64_t)r * 2 * a.tiles_n;
@@ -715,13 +723,13 @@ template <typename T> __global__ void __launch_bounds__(kScaleThreads) scale_ker
             if (i < vectors) bits[k] = reinterpret_cast<const uint4*>(e)[i];
         }
     };
-    read(threadIdx.x);
+    read(from + threadIdx.x);
     const float own = a.label[r];                                     // in powers of two
     const float weight = a.weight[a.z.first + r], c = weight * a.scale * a.head->lift;
     const int target = a.target[a.z.first + r];
     const float lse = lse2_of(stats, (a.z.vocab + 127) / 128, lane);
-    if (threadIdx.x == 0) finish_row(a, r, weight, (lse - own) * kLn2);
-    for (int i0 = threadIdx.x; i0 < vectors; i0 += kAhead * kScaleThreads) {
+    if (threadIdx.x == 0 && blockIdx.y == 0) finish_row(a, r, weight, (lse - own) * kLn2);
+    for (int i0 = from + threadIdx.x; i0 < vectors; i0 += kAhead * kScaleThreads) {
         uint4 now[kAhead];
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) now[k] = bits[k];
@@ -950,7 +958,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2)
     // less take as many tiles of dW ahead of the others as last as long.
     const int per_part = tiles_m * tiles_h, n_dx = g.dx ? per_part * parts : 0, n_dw = g.dw && steps_r ? tiles_v * tiles_h : 0;
     const int heavy = n_dx % n_pairs, light = n_pairs - heavy, units = n_dx / n_pairs + (pair < heavy);
-    const int ahead = heavy && steps_r ? max(0, steps_v / parts / steps_r) : 0;
+    const int ahead = heavy ? steps_v / parts / stages_of_dw(rows) : 0;
     const int early = (int)min((int64_t)n_dw, (int64_t)ahead * light);
     const int my_early = pair < heavy ? 0 : max(0, (early - (pair - heavy) + light - 1) / light);
     const auto next = [&](int it, Job& j) {
@@ -1245,7 +1253,8 @@ template <typename T, typename TW> static int run(const Call& c, const Plan& p, 
             SIDCO_CE_LAUNCH(loss_kernel, dim3((unsigned)((most + 7) / 8)), kScaleThreads, 0, c.s, 1, k);
             continue;
         }
-        SIDCO_CE_LAUNCH(scale_kernel<T>, dim3((unsigned)up_to(most, kStageK)), kScaleThreads, 0, c.s, 1, k);
+        const int64_t shares = std::max<int64_t>(1, std::min(4 * sms / up_to(most, kStageK), c.vocab / (8 * 4 * kScaleThreads)));
+        SIDCO_CE_LAUNCH(scale_kernel<T>, dim3((unsigned)up_to(most, kStageK), (unsigned)shares), kScaleThreads, 0, c.s, 1, k);
         Grads g{z, head, map, c.dx, c.lddx, reinterpret_cast<float*>(c.ws + p.dx_parts), c.dw, c.lddw, c.add,
                 reinterpret_cast<float*>(c.ws + p.dw_sums), i > 0, i + 1 == p.pieces, share, c.total, p.pitch,
                 unit_of(c.dx, c.lddx, c.type), unit_of(c.dw, c.lddw, c.dw_type), timeouts};
