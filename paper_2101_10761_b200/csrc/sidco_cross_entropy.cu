@@ -333,24 +333,26 @@ struct Operand {
     int row0;                         // added to the matrix's row
 };
 
-// Two units: 128 M or N indices from `at` on, stage k.
-__device__ __forceinline__ void load_operand(uint32_t dst, const Operand& o, int at, int k, uint32_t bar) {
+// One or two units: 64 or 128 M or N indices from `at` on, stage k.
+__device__ __forceinline__ void load_operand(uint32_t dst, const Operand& o, int at, int k, int units, uint32_t bar) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
+        if (u == units) break;
         if (o.mn) tensor_load_2d_pair(dst + u * kUnit, o.map, (at + u * 64) * 2, o.row0 + k * kStageK, bar);
         else tensor_load_2d_pair(dst + u * kUnit, o.map, k * 128, o.row0 + at + u * 64, bar);
     }
 }
 
-template <typename T> __device__ constexpr uint32_t shape_of(bool a_mn, bool b_mn) {
+template <typename T> __device__ __forceinline__ uint32_t shape_of(bool a_mn, bool b_mn, int width) {
     const uint32_t type = kIsHalf<T> ? 0 : 1;
     return (1u << 4) | (type << 7) | (type << 10) | ((a_mn ? 1u : 0u) << 15) | ((b_mn ? 1u : 0u) << 16) |
-           ((uint32_t)(kTile >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
+           ((uint32_t)(width >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
 }
 
 struct Job {                          // a tile, or a part of K of one
     Operand a, b;
-    int ti, tj, from, to;             // stages
+    int ti, tj, width;                // columns: fewer in the last tile of a row, a multiple of 32
+    int from, to;                     // stages
     int kind, part;
     bool dry;                         // the way out is only walked through
 };
@@ -363,6 +365,8 @@ struct Shared {
 
 // The three roles over the jobs that next(it, job) gives; finish(job, sums, quarter, half, take) takes a tile's sums out and
 // calls take() when it has read them; ahead(job, row, column) comes before the sums are there.
+__device__ __forceinline__ int width_of(int tj, int columns) { return min(kTile, (columns - tj * kTile + 31) / 32 * 32); }
+
 template <typename T, typename Next, typename Finish, typename Ahead>
 __device__ __forceinline__ void run_jobs(Shared& s, uint8_t* smem, Next next, Finish finish, Ahead ahead) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -374,14 +378,16 @@ __device__ __forceinline__ void run_jobs(Shared& s, uint8_t* smem, Next next, Fi
             uint32_t round = 0;
             bool ok = true;
             for (int it = 0; ok && next(it, j); ++it) {
-                const int row_a = j.ti * kTile + (int)rank * 128, row_b = j.tj * kTile + (int)rank * 128;
+                // (of B each CTA holds half of the tile's columns)
+                const int row_a = j.ti * kTile + (int)rank * 128, row_b = j.tj * kTile + (int)rank * (j.width / 2);
+                const int units_b = j.width > 128 ? 2 : 1;
                 for (int k = j.from; k < j.to; ++k) {
                     const uint32_t a = stage0 + st * kStageBytes, bar = smem_addr(&s.full[st]);
                     ok = mbar_wait(smem_addr(&s.free[st]), (round & 1) ^ 1, &s.failed);
                     if (!ok) break;
-                    if (rank == 0) mbar_expect_tx(bar, 2 * kStageBytes);
-                    load_operand(a, j.a, row_a, k, bar);
-                    load_operand(a + 2 * kUnit, j.b, row_b, k, bar);
+                    if (rank == 0) mbar_expect_tx(bar, 2 * (2 + units_b) * kUnit);
+                    load_operand(a, j.a, row_a, k, 2, bar);
+                    load_operand(a + 2 * kUnit, j.b, row_b, k, units_b, bar);
                     if (++st == kStages) { st = 0; ++round; }
                 }
             }
@@ -396,7 +402,7 @@ __device__ __forceinline__ void run_jobs(Shared& s, uint8_t* smem, Next next, Fi
                 const uint32_t sums = tmem + buf * kTile;
                 const uint32_t a_step = j.a.mn ? 2048 : 32, a_lead = j.a.mn ? kUnit : 16;
                 const uint32_t b_step = j.b.mn ? 2048 : 32, b_lead = j.b.mn ? kUnit : 16;
-                const uint32_t shape = shape_of<T>(j.a.mn, j.b.mn);
+                const uint32_t shape = shape_of<T>(j.a.mn, j.b.mn, j.width);
                 ok = __all_sync(0xffffffffu, mbar_wait(smem_addr(&s.taken[buf]), ((it >> 1) & 1) ^ 1, &s.failed));
                 for (int k = j.from; k < j.to && ok; ++k) {
                     ok = __all_sync(0xffffffffu, mbar_wait(smem_addr(&s.full[st]), round & 1, &s.failed));
@@ -506,7 +512,8 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2)
         const int64_t i = blockIdx.x / 2 + (int64_t)it * n_pairs;
         if (i >= total) return false;
         const int per = 8 * g.tiles_n, band = (int)(i / per), in = (int)(i - (int64_t)band * per), high = min(8, tiles_m - band * 8);
-        j = Job{{&map_x, false, g.z.first}, {&map_w, false, 0}, band * 8 + in % high, in / high, 0, stages, 0, 0, false};
+        j = Job{{&map_x, false, g.z.first}, {&map_w, false, 0}, band * 8 + in % high, in / high, width_of(in / high, g.z.vocab), 0, stages,
+                0, 0, false};
         return true;
     };
     const auto finish = [&](const Job& j, uint32_t sums, int row_in, int col_in, uint8_t* box, auto take) {
@@ -964,14 +971,15 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2)
     const auto next = [&](int it, Job& j) {
         if (it < units) {
             const int u = it * n_pairs + pair, part = u / per_part, t = u - part * per_part;
-            j = Job{{&map_d, false, 0}, {&map_w, true, 0}, t % tiles_m, t / tiles_m,
+            j = Job{{&map_d, false, 0}, {&map_w, true, 0}, t % tiles_m, t / tiles_m, width_of(t / tiles_m, g.z.hidden),
                     (int)((int64_t)steps_v * part / parts), (int)((int64_t)steps_v * (part + 1) / parts), 0, part, false};
             return true;
         }
         it -= units;
         const int t = it < my_early ? pair - heavy + it * light : early + (it - my_early) * n_pairs + pair;
         if (t >= n_dw) return false;
-        j = Job{{&map_d, true, 0}, {&map_x, true, g.z.first}, t / tiles_h, t % tiles_h, 0, steps_r, 1, 0, false};
+        j = Job{{&map_d, true, 0}, {&map_x, true, g.z.first}, t / tiles_h, t % tiles_h, width_of(t % tiles_h, g.z.hidden), 0, steps_r,
+                1, 0, false};
         return true;
     };
     const auto finish = [&](const Job& j, uint32_t sums, int row_in, int col_in, uint8_t* box, auto take) {
