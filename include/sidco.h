@@ -460,6 +460,11 @@ int sidco_linear_cross_entropy(const void* x, int type, int64_t ldx, const void*
                                void* dw, int dw_type, int64_t lddw, int add_dw, int64_t piece_rows, int32_t* status,
                                void* workspace, size_t workspace_bytes, void* stream);
 
+/* sidco_scale_gradient - x *= *factor, for gradients that were computed before the factor in front of the loss was known.
+ * x device, type[n], aligned to its element, n <= 2^40; factor device, float.  The product is rounded once; a factor of 1
+ * reads and writes nothing. */
+int sidco_scale_gradient(void* x, int type, int64_t n, const float* factor, void* stream);
+
 /* How many CTAs of the product kernels (sidco_mx4_matmul, sidco_orthogonalize, sidco_linear_cross_entropy) have given up a bounded wait since the
  * library was loaded; anything but 0 means that an output is incomplete.  Negative: a CUDA error.  Synchronises the
  * device; meant for tests and logging. */

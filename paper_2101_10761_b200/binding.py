@@ -50,7 +50,7 @@ EXPORTS = [
     "sidco_mx4_compress", "sidco_mx4_mean", "sidco_orthogonalize_workspace_bytes", "sidco_orthogonalize",
     "sidco_wait_timeouts", "sidco_set_product_test_hooks",
     "sidco_dropout", "sidco_embedding", "sidco_embedding_grad_workspace_bytes", "sidco_embedding_grad",
-    "sidco_linear_cross_entropy_workspace_bytes", "sidco_linear_cross_entropy",
+    "sidco_linear_cross_entropy_workspace_bytes", "sidco_linear_cross_entropy", "sidco_scale_gradient",
 ]
 
 _lib = None
@@ -165,6 +165,8 @@ def lib() -> C.CDLL:
     L.sidco_linear_cross_entropy.argtypes = [vp, i32, i64, vp, i32, i64, vp, i32, vp, f32, i64, i64, i64, vp, vp, vp, i64, vp,
                                              i32, i64, i32, i64, vp, vp, sz, vp]
     L.sidco_linear_cross_entropy.restype = i32
+    L.sidco_scale_gradient.argtypes = [vp, i32, i64, vp, vp]
+    L.sidco_scale_gradient.restype = i32
     _lib = L
     return L
 
@@ -620,3 +622,10 @@ def sidco_linear_cross_entropy(x, ldx: int, w, ldw: int, labels, rows: int, voca
         workspace_bytes, _stream(stream))
     if rc:
         raise SidcoError(rc, "sidco_linear_cross_entropy")
+
+
+def sidco_scale_gradient(x, n: int, factor, x_type=None, stream=None) -> None:
+    """x *= *factor (a float on the device); a factor of one costs nothing."""
+    rc = lib().sidco_scale_gradient(_ptr(x), _type(x, x_type), n, _ptr(factor), _stream(stream))
+    if rc:
+        raise SidcoError(rc, "sidco_scale_gradient")

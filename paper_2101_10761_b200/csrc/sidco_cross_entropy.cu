@@ -46,6 +46,7 @@ constexpr int kStageBytes = 4 * kUnit;
 constexpr int kBox = 32 * 128;        // of an epilogue warp
 constexpr int kThreads = 320;
 constexpr int kSmem = kStages * kStageBytes + 8 * kBox + 1024;
+constexpr int kBand = 16;             // tile rows
 constexpr int kMostParts = 16;
 constexpr int kPairs = 74;            // of a whole B200: what the split of dX is planned for
 
@@ -507,12 +508,13 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2)
     const int lane = threadIdx.x & 31;
     const int rows = rows_of_piece(g.z, g.head), tiles_m = (rows + kTile - 1) / kTile, total = tiles_m * g.tiles_n;
     const int n_pairs = gridDim.x / 2, stages = (g.z.hidden + kStageK - 1) / kStageK;
-    // tiles in bands of eight tile rows, column by column, so that pairs at work at the same time share operands in L2
+    // tiles in bands of tile rows, column by column, so that pairs at work at the same time share operands in L2: W is read once
+    // for each band, whose rows of X stay there
     const auto next = [&](int it, Job& j) {
         const int64_t i = blockIdx.x / 2 + (int64_t)it * n_pairs;
         if (i >= total) return false;
-        const int per = 8 * g.tiles_n, band = (int)(i / per), in = (int)(i - (int64_t)band * per), high = min(8, tiles_m - band * 8);
-        j = Job{{&map_x, false, g.z.first}, {&map_w, false, 0}, band * 8 + in % high, in / high, width_of(in / high, g.z.vocab), 0, stages,
+        const int per = kBand * g.tiles_n, band = (int)(i / per), in = (int)(i - (int64_t)band * per), high = min(kBand, tiles_m - band * kBand);
+        j = Job{{&map_x, false, g.z.first}, {&map_w, false, 0}, band * kBand + in % high, in / high, width_of(in / high, g.z.vocab), 0, stages,
                 0, 0, false};
         return true;
     };

@@ -4,6 +4,7 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "../../include/sidco.h"
@@ -77,9 +78,46 @@ __global__ void __launch_bounds__(kThreads)
     }
 }
 
+template <typename T, bool kVector>
+__global__ void __launch_bounds__(kThreads) scale_gradient_kernel(T* x, int64_t n, const float* factor) {
+    constexpr int kEach = Few<T, kVector>::kEach;
+    sidco_tc::wait_prerequisites();
+    sidco_tc::launch_dependents();
+    const float f = *factor;
+    if (f == 1.0f) return;
+    for (int64_t i = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * kEach; i < n; i += (int64_t)gridDim.x * kThreads * kEach) {
+        Few<T, kVector> a;
+        a.read(x + i, n - i);
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) a.t[j] = narrow<T>(widen(a.t[j]) * f);
+        a.write(x + i, n - i);
+    }
+}
+
 }  // namespace sidco_dropout_impl
 
-extern "C" int sidco_dropout(const void* x, int type, int64_t n, float p, uint64_t seed, uint64_t call,
+extern "C" {
+
+int sidco_scale_gradient(void* x, int type, int64_t n, const float* factor, void* stream) {
+    using namespace sidco_dropout_impl;
+    if (n < 0 || n > ((int64_t)1 << 40)) return SIDCO_E_SIZE;
+    if (type < SIDCO_T_F32 || type > SIDCO_T_F16) return SIDCO_E_TYPE;
+    if (n == 0) return 0;
+    if (!x || !factor) return SIDCO_E_NULL;
+    if ((uintptr_t)x % size_of(type) || (uintptr_t)factor % 4) return SIDCO_E_ALIGN;
+    if (overlap(x, n * size_of(type), factor, 4)) return SIDCO_E_ALIAS;
+    // (few CTAs: the usual factor is one, and then they only have to end)
+    const int64_t blocks = std::min<int64_t>((n + 8 * kThreads - 1) / (8 * kThreads), 148 * 8);
+    const int rc = with_type(type, [&](auto* t) {
+        using T = std::remove_pointer_t<decltype(t)>;
+        return (int)launch((uintptr_t)x % 16 ? scale_gradient_kernel<T, false> : scale_gradient_kernel<T, true>, dim3((unsigned)blocks),
+                           kThreads, 0, (cudaStream_t)stream, 1, (T*)x, n, factor);
+    });
+    if (rc == 0) sidco_internal::note_launch();
+    return rc;
+}
+
+int sidco_dropout(const void* x, int type, int64_t n, float p, uint64_t seed, uint64_t call,
                              const uint64_t* step, const void* residual, void* out, void* stream) {
     using namespace sidco_dropout_impl;
     if (n < 0 || n > ((int64_t)1 << 40)) return SIDCO_E_SIZE;
@@ -111,3 +149,5 @@ extern "C" int sidco_dropout(const void* x, int type, int64_t n, float p, uint64
     if (rc == 0) sidco_internal::note_launch();
     return rc;
 }
+
+}  // extern "C"

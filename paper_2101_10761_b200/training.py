@@ -1,4 +1,5 @@
-"""A linear layer whose three products are 4-bit, and the optimiser step on the averaged gradient.
+"""What a training step calls around the exchange of gradients: a linear layer whose three products are 4-bit, the lookup of
+tokens, dropout, the cross entropy of the output projection, and the optimiser step on the averaged gradient.
 
 Thin ``torch`` plumbing around :mod:`binding` (buffers, autograd bookkeeping); all arithmetic on matrices runs in the
 library's kernels.
@@ -100,6 +101,168 @@ def mx4_linear(x: torch.Tensor, weight: torch.Tensor) -> torch.Tensor:
         raise ValueError(f"x has {x.shape[-1]} columns, weight {weight.shape[1]}")
     y = _Linear.apply(x.reshape(x.shape[:-1].numel(), x.shape[-1]), weight)
     return y.reshape(*x.shape[:-1], weight.shape[0])
+
+
+def _rows(x: torch.Tensor) -> Tuple[torch.Tensor, int]:
+    """A matrix whose elements of a row are neighbours, and the distance of its rows."""
+    rows, cols = x.shape
+    if x.numel() and ((cols > 1 and x.stride(1) != 1) or (rows > 1 and x.stride(0) < cols)):
+        x = x.contiguous()
+    return x, max(x.stride(0), cols) if rows > 1 else cols
+
+
+def _check_random(p: float, step: Optional[torch.Tensor], device) -> None:
+    if not 0.0 <= p <= 1.0:
+        raise ValueError(f"p must lie in [0, 1], got {p}")
+    if step is not None and (step.dtype not in (torch.int64, torch.uint64) or step.numel() != 1 or step.device != device):
+        raise ValueError(f"step must be one 64-bit integer on {device}")
+
+
+_WORDS = 1 << 64
+
+
+class _Embedding(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, table, tokens, scale, p, seed, call, step, dtype):
+        vocab, cols = table.shape
+        n = tokens.numel()
+        rows, ld = _rows(table)
+        flat = tokens.reshape(-1).contiguous()
+        out = torch.empty(n, cols, dtype=dtype, device=table.device)
+        with torch.cuda.device(table.device):
+            B.sidco_embedding(rows, vocab, cols, ld, flat, n, scale, out, cols, p=p, seed=seed, call=call, step=step)
+        ctx.save_for_backward(flat, step)
+        ctx.args, ctx.sizes, ctx.type = (scale, p, seed, call), (n, vocab, cols), table.dtype
+        return out
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy):
+        (flat, step), (n, vocab, cols) = ctx.saved_tensors, ctx.sizes
+        scale, p, seed, call = ctx.args
+        dy, ld = _rows(dy)
+        need = B.sidco_embedding_grad_workspace_bytes(n, vocab, cols)
+        with torch.cuda.device(dy.device):
+            dtable = torch.empty(vocab, cols, dtype=ctx.type, device=dy.device)
+            workspace = torch.empty(need, dtype=torch.uint8, device=dy.device)
+            B.sidco_embedding_grad(dy, ld, flat, n, vocab, cols, scale, dtable, cols, workspace, need, p=p, seed=seed,
+                                   call=call, step=step)
+        return dtable, None, None, None, None, None, None, None
+
+
+def embedding(tokens: torch.Tensor, table: torch.Tensor, scale: float = 1.0, p: float = 0.0, seed: int = 0, call: int = 0,
+              step: Optional[torch.Tensor] = None, dtype: Optional[torch.dtype] = None) -> torch.Tensor:
+    """scale * dropout(table[tokens]), [..., cols] in `dtype` (that of the table by default).
+
+    A negative token is padding: its row is zero and it has no gradient, as a token beyond the table.  The mask is a
+    function of (seed, call + step, position), see :func:`dropout`.  The gradient is dense, in the table's type."""
+    if table.dim() != 2:
+        raise ValueError(f"the table must be a matrix, got {table.dim()} dimensions")
+    if tokens.dtype not in (torch.int32, torch.int64):
+        raise ValueError(f"tokens must be int32 or int64, got {tokens.dtype}")
+    if tokens.device != table.device:
+        raise ValueError(f"the tokens are on {tokens.device}, the table on {table.device}")
+    _check_random(p, step, table.device)
+    y = _Embedding.apply(table, tokens, float(scale), float(p), seed % _WORDS, call % _WORDS, step, dtype or table.dtype)
+    return y.reshape(*tokens.shape, table.shape[1])
+
+
+class _Dropout(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, p, seed, call, step, residual):
+        x = x.contiguous()
+        out = torch.empty_like(x)
+        with torch.cuda.device(x.device):
+            B.sidco_dropout(x, x.numel(), p, seed, call, out, residual=None if residual is None else residual.contiguous(),
+                            step=step)
+        ctx.save_for_backward(step)
+        ctx.args = (p, seed, call)
+        return out
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy):
+        (step,), dx = ctx.saved_tensors, None
+        if ctx.needs_input_grad[0]:
+            dy = dy.contiguous()
+            dx = torch.empty_like(dy)
+            with torch.cuda.device(dy.device):
+                B.sidco_dropout(dy, dy.numel(), *ctx.args, dx, step=step)
+        return dx, None, None, None, None, dy if ctx.needs_input_grad[5] else None
+
+
+def dropout(x: torch.Tensor, p: float, seed: int, call: int = 0, step: Optional[torch.Tensor] = None,
+            residual: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """dropout(x) (+ residual) with a mask that is never stored: it is a function of the element's index, `seed` and the
+    number of the call, call + step.  Give each use in a step its own `call`; `step`, one 64-bit integer on the device, is
+    read when the kernels run, so that a captured step draws new masks (count it up behind the backward pass, which draws
+    the same mask again)."""
+    if residual is not None and (residual.shape != x.shape or residual.dtype != x.dtype or residual.device != x.device):
+        raise ValueError(f"the residual must be {tuple(x.shape)} of {x.dtype} on {x.device}, as x")
+    _check_random(p, step, x.device)
+    return _Dropout.apply(x, float(p), seed % _WORDS, call % _WORDS, step, residual)
+
+
+class _LinearCrossEntropy(torch.autograd.Function):
+    """The gradients come from the forward pass, where the logits are; the backward pass multiplies them by the factor in
+    front of the loss, in place, and hands them out, once."""
+
+    @staticmethod
+    def forward(ctx, x, weight, labels, row_weights, scale, piece_rows):
+        (rows, hidden), vocab = x.shape, weight.shape[0]
+        need_x, need_w = ctx.needs_input_grad[:2]
+        x, ldx = _rows(x)
+        w, ldw = _rows(weight)
+        loss = torch.empty((), dtype=torch.float32, device=x.device)
+        dx = torch.empty(rows, hidden, dtype=x.dtype, device=x.device) if need_x else None
+        dw = torch.empty(vocab, hidden, dtype=weight.dtype, device=x.device) if need_w else None
+        need = B.sidco_linear_cross_entropy_workspace_bytes(x, w, ldw, rows, vocab, hidden, need_x + 2 * need_w, piece_rows)
+        with torch.cuda.device(x.device):
+            workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
+            B.sidco_linear_cross_entropy(x, ldx, w, ldw, labels, rows, vocab, hidden, None, loss, dx, hidden, dw, hidden,
+                                         workspace, need, row_weights=row_weights, scale=scale, piece_rows=piece_rows)
+        ctx.grads = (dx, dw)
+        return loss
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dloss):
+        if ctx.grads is None:
+            raise RuntimeError("the gradients of linear_cross_entropy are handed out once; call it again")
+        grads, ctx.grads = ctx.grads, None
+        dloss = dloss.float()
+        for g in grads:
+            if g is not None:
+                with torch.cuda.device(g.device):
+                    B.sidco_scale_gradient(g, g.numel(), dloss)
+        return grads + (None, None, None, None)
+
+
+def linear_cross_entropy(x: torch.Tensor, weight: torch.Tensor, labels: torch.Tensor,
+                         row_weights: Optional[torch.Tensor] = None, scale: float = 1.0, piece_rows: int = 0) -> torch.Tensor:
+    """Softmax cross entropy of scale * x weight^T against `labels`, without the logits ever being stored.
+
+    x [..., hidden] in bf16 or fp16, weight [vocab, hidden] in the same type or fp32 (a master copy: rounded for the
+    products, its gradient in fp32), labels [...] int32 or int64.  Rows with a negative label do not count.  The result is
+    the mean over the others, or with row_weights [...] (fp32) the sum of the rows' losses times these."""
+    if x.dtype not in (torch.bfloat16, torch.float16):
+        raise ValueError(f"x must be bf16 or fp16, got {x.dtype}")
+    if weight.dim() != 2 or x.dim() < 1 or x.shape[-1] != weight.shape[1] or not weight.numel():
+        raise ValueError(f"x {tuple(x.shape)} and weight {tuple(weight.shape)} do not fit")
+    if weight.dtype not in (x.dtype, torch.float32):
+        raise ValueError(f"weight must be {x.dtype} or fp32, got {weight.dtype}")
+    if labels.shape != x.shape[:-1] or labels.dtype not in (torch.int32, torch.int64):
+        raise ValueError(f"labels must be {tuple(x.shape[:-1])} of int32 or int64, got {tuple(labels.shape)} of {labels.dtype}")
+    if row_weights is not None and (row_weights.shape != labels.shape or row_weights.dtype != torch.float32):
+        raise ValueError(f"row_weights must be {tuple(labels.shape)} of fp32, got {tuple(row_weights.shape)} of "
+                         f"{row_weights.dtype}")
+    for t in (weight, labels, row_weights):
+        if t is not None and t.device != x.device:
+            raise ValueError(f"all arguments must be on {x.device}, got one on {t.device}")
+    rows = labels.numel()
+    return _LinearCrossEntropy.apply(x.reshape(rows, x.shape[-1]), weight, labels.reshape(-1).contiguous(),
+                                     None if row_weights is None else row_weights.reshape(-1).contiguous(), float(scale),
+                                     int(piece_rows))
 
 
 class OrthogonalizedUpdate:

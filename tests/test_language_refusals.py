@@ -163,3 +163,13 @@ def test_cross_entropy_refuses(B):
             size(0, 0, 8, 4, 9, 8, **bad)
         assert e.value.code == want
     assert size(0, 0, 8, 0, 9, 8, x_type=1, w_type=1) == 0
+
+
+def test_scale_gradient_refuses(B):
+    f = B.sidco_scale_gradient
+    assert code(f, P, -1, Q, x_type=0) == -10 and code(f, P, (1 << 40) + 1, Q, x_type=0) == -10
+    assert code(f, P, 4, Q, x_type=5) == -13
+    assert code(f, None, 4, Q, x_type=0) == -1 and code(f, P, 4, None, x_type=0) == -1
+    assert code(f, P + 2, 4, Q, x_type=0) == -14 and code(f, P, 4, Q + 2, x_type=0) == -14
+    assert code(f, P, 4, P + 12, x_type=0) == -9
+    f(None, 0, None, x_type=0, stream=0)
