@@ -365,7 +365,7 @@ struct Shared {
 };
 
 // The three roles over the jobs that next(it, job) gives; finish(job, sums, quarter, half, take) takes a tile's sums out and
-// calls take() when it has read them; ahead(job, row, column) comes before the sums are there.
+// calls take() when it has read them; ahead(job, row, column) comes a job earlier.
 __device__ __forceinline__ int width_of(int tj, int columns) { return min(kTile, (columns - tj * kTile + 31) / 32 * 32); }
 
 template <typename T, typename Next, typename Finish, typename Ahead>
@@ -428,11 +428,15 @@ __device__ __forceinline__ void run_jobs(Shared& s, uint8_t* smem, Next next, Fi
         const uint32_t taken[2] = {in_cta(smem_addr(&s.taken[0]), 0), in_cta(smem_addr(&s.taken[1]), 0)};
         // Before the first sums are there, the way out is walked through once without writing anything: its instructions then
         // lie in the SM's caches when the first tile is done (the first tile took 7 us instead of 4).
-        for (int it = -1; next(max(it, 0), j); ++it) {
+        Job coming;
+        bool more = next(0, coming);
+        for (int it = -1; more; ++it) {
             const int buf = it & 1;
+            j = coming;
             j.dry = it < 0;
+            if (it >= 0) more = next(it + 1, coming);
+            if (it >= 0) ahead(j, (int)rank * 128 + quarter * 32, half * 128);
             if (it >= 0) {
-                ahead(j, (int)rank * 128 + quarter * 32, half * 128);
                 const bool ok = mbar_wait(smem_addr(&s.sums[buf]), (it >> 1) & 1, &s.failed);
                 if (!__all_sync(0xffffffffu, ok)) break;
                 fence_after_sync();
@@ -878,28 +882,27 @@ __device__ __forceinline__ void put_tile(uint32_t tmem, uint8_t* box, int row, T
                                          const Added& more, Take take) {
     constexpr int kSize = (int)sizeof(TO), kCols = 128 / kSize, kSteps = 128 / kCols;
     const int lane = threadIdx.x & 31;
+    uint32_t old[36];
+    const auto read_old = [&](int q) {
+        const uintptr_t first = (uintptr_t)(out + max(row, 0) * ld + q * kCols), start = first & ~(uintptr_t)15;
+        if (__all_sync(0xffffffffu, start >= more.lo && start + 144 <= more.hi)) {
+#pragma unroll
+            for (int i = 0; i < 9; ++i) {
+                const uint4 v = reinterpret_cast<const uint4*>(start)[i];
+                old[i * 4] = v.x, old[i * 4 + 1] = v.y, old[i * 4 + 2] = v.z, old[i * 4 + 3] = v.w;
+            }
+        } else {                                                      // at the ends of the matrix
+#pragma unroll
+            for (int i = 0; i < 9; ++i) {
+                const uint4 v = load_edge<kSize>(start + 16 * i, more.lo, more.hi);
+                old[i * 4] = v.x, old[i * 4 + 1] = v.y, old[i * 4 + 2] = v.z, old[i * 4 + 3] = v.w;
+            }
+        }
+    };
 #pragma unroll 1
     for (int q = 0; q < kSteps; ++q) {
         const int here = left - q * kCols;
-        uint32_t old[36];
-        if (more.out && here > 0) {
-            const uintptr_t first = (uintptr_t)(out + max(row, 0) * ld + q * kCols), start = first & ~(uintptr_t)15;
-            const int shift = (int)(first & 15);
-            if (__all_sync(0xffffffffu, start >= more.lo && start + 144 <= more.hi)) {
-#pragma unroll
-                for (int i = 0; i < 9; ++i) {
-                    const uint4 v = reinterpret_cast<const uint4*>(start)[i];
-                    old[i * 4] = v.x, old[i * 4 + 1] = v.y, old[i * 4 + 2] = v.z, old[i * 4 + 3] = v.w;
-                }
-            } else {                                                  // at the ends of the matrix
-#pragma unroll
-                for (int i = 0; i < 9; ++i) {
-                    const uint4 v = load_edge<kSize>(start + 16 * i, more.lo, more.hi);
-                    old[i * 4] = v.x, old[i * 4 + 1] = v.y, old[i * 4 + 2] = v.z, old[i * 4 + 3] = v.w;
-                }
-            }
-            if (unit < 16) shift_words<32>(old, shift);
-        }
+        if (more.out && here > 0) read_old(q);
         uint32_t acc[kCols];
 #pragma unroll
         for (int i = 0; i < kCols / 32; ++i)
@@ -920,6 +923,7 @@ __device__ __forceinline__ void put_tile(uint32_t tmem, uint8_t* box, int row, T
 #pragma unroll
         for (int i = 0; i < kCols; ++i) acc[i] = __float_as_uint(__uint_as_float(acc[i]) * factor);
         if (more.out) {
+            if (unit < 16) shift_words<32>(old, (int)((uintptr_t)(out + max(row, 0) * ld + q * kCols) & 15));
 #pragma unroll
             for (int i = 0; i < 32; ++i) {
                 if constexpr (kSize == 4) {
@@ -1006,7 +1010,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2)
             put_tile(sums, box, row, out + col, g.lddw, left, unlift, g.dw_unit, more, take);
         }
     };
-    // what a tile of dW is added to is brought into L2 while its products run
+    // what a tile of dW is added to is brought into L2 while the tile before it leaves
     const auto ahead_of = [&](const Job& j, int row_in, int col_in) {
         const int r = j.ti * kTile + row_in + lane, col = j.tj * kTile + col_in, left = min(128, g.z.hidden - col);
         if (j.kind == 0 || !g.add || !g.last || r >= g.z.vocab || left <= 0) return;
