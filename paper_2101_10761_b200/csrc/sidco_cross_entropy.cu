@@ -1050,33 +1050,37 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2)
 
 constexpr int kJoinThreads = 256;
 
-// dX = the parts of its sums, in order.
+// dX = the parts of its sums, in order (where they are one part after all, it has nothing to do: few CTAs).
 template <typename T>
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(const Grads g) {
     wait_prerequisites();
     launch_dependents();
-    const int rows = rows_of_piece(g.z, g.head), r = blockIdx.x, parts = g.head->parts;
-    if (r >= rows || parts == 1) return;
+    const int rows = rows_of_piece(g.z, g.head), parts = g.head->parts;
+    if (parts == 1) return;
     const float unlift = g.head->unlift;
-    T* out = static_cast<T*>(g.dx) + g.map[g.z.first + r] * g.lddx;
-    for (int c = (blockIdx.y * kJoinThreads + threadIdx.x) * 4; c < g.z.hidden; c += gridDim.y * kJoinThreads * 4) {
+    const int fours = (g.z.hidden + 3) / 4;
+    for (int64_t i = (int64_t)blockIdx.x * kJoinThreads + threadIdx.x; i < (int64_t)rows * fours; i += (int64_t)gridDim.x * kJoinThreads) {
+        const int r = (int)(i / fours), c = (int)(i % fours) * 4;
         const float* p = g.dx_parts + (int64_t)r * g.pitch + c;
-        float v[4];
-        load(p, v);
-        for (int k = 1; k < parts; ++k) {
-            float o[4];
-            load(p + (int64_t)k * rows * g.pitch, o);
+        float v[4] = {};
+        for (int k0 = 0; k0 < parts; k0 += 4) {
+            float o[4][4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] += o[j];
+            for (int k = 0; k < 4; ++k) load(p + (int64_t)min(k0 + k, parts - 1) * rows * g.pitch, o[k]);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] += k0 + k < parts ? o[k][j] : 0.0f;
         }
+        T* out = static_cast<T*>(g.dx) + g.map[g.z.first + r] * g.lddx + c;
 #pragma unroll
         for (int j = 0; j < 4; ++j) v[j] *= unlift;
         if (g.dx_unit >= 8 && c + 4 <= g.z.hidden) {
-            store(out + c, v);
+            store(out, v);
         } else {
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                if (c + j < g.z.hidden) out[c + j] = narrow<T>(v[j]);
+                if (c + j < g.z.hidden) out[j] = narrow<T>(v[j]);
         }
     }
 }
@@ -1274,7 +1278,8 @@ template <typename T, typename TW> static int run(const Call& c, const Plan& p, 
                 unit_of(c.dx, c.lddx, c.type), unit_of(c.dw, c.lddw, c.dw_type), timeouts};
         SIDCO_CE_LAUNCH((grads_kernel<T, TW>), dim3(2 * (unsigned)pairs), kThreads, kSmem, c.s, 1, map_x, map_w, map_d, g);
         if (c.dx && p.part_rows)
-            SIDCO_CE_LAUNCH(join_kernel<T>, dim3((unsigned)most, (unsigned)((c.hidden + 1023) / 1024)), kJoinThreads, 0, c.s, 1, g);
+            SIDCO_CE_LAUNCH(join_kernel<T>, dim3((unsigned)std::min<int64_t>((most * ((c.hidden + 3) / 4) + kJoinThreads - 1) / kJoinThreads, 8 * sms)),
+                            kJoinThreads, 0, c.s, 1, g);
     }
     return 0;
 }

@@ -412,7 +412,7 @@ struct Sums {
     int cols, chunk;                  // sorted positions per warp, at most 32
     int64_t ld_dy, ldd;
     uintptr_t lo, hi;                 // dy
-    float scale;
+    float scale;                      // times the dropout's factor
     int add;
     float* partial;                   // [chunks][2][pitch]: of the run that enters a chunk and of the one that leaves it
     int64_t pitch;
@@ -478,13 +478,18 @@ __device__ __forceinline__ void add_up(const TI* dy, const Sums& s, const Dropou
             if (k + j >= count) break;
             float v[kEach];
             now[j].widened(dy + at[j] * s.ld_dy + c, v);
-            if (kDrop) {
+            if (kDrop) {                                              // (the factor is part of the scale)
                 const uint64_t first = (uint64_t)at[j] * s.cols + c;
-                if (first % 4 == 0) drop(d, call, first, v);          // (the same for the whole warp)
-                else drop<kEach, false>(d, call, first, v);
-            }
+                uint32_t w[kEach];
+                if (first % 4 == 0) random_words<kEach, true>(d, call, first, w);      // (the same for the whole warp)
+                else random_words<kEach, false>(d, call, first, w);
 #pragma unroll
-            for (int e = 0; e < kEach; ++e) sum[e] += v[e];
+                for (int e = 0; e < kEach; ++e)
+                    if (!dropped(d, w[e])) sum[e] += v[e];
+            } else {
+#pragma unroll
+                for (int e = 0; e < kEach; ++e) sum[e] += v[e];
+            }
             if (ends(k + j)) {
                 done(k + j);
 #pragma unroll
@@ -547,9 +552,11 @@ __global__ void __launch_bounds__(kThreads, 2) join_kernel(TO* __restrict__ out,
     const int lane = threadIdx.x & 31, c = (int)(unit % slabs) * kJoinSlab + lane * kJoinEach, left = s.cols - c;
     const uint32_t first = chunk * s.chunk, next = first + s.chunk;
     if (next >= s.n) return;
-    const uint32_t key = s.items[next - 1].x;
-    if (key >= s.vocab || s.items[next].x != key) return;             // it ends here
-    if (s.items[first].x == key && first && s.items[first - 1].x == key) return;        // it began earlier
+    // (all four at once: most warps have nothing to do, and should know it after one trip to memory)
+    const uint32_t key = s.items[next - 1].x, behind = s.items[next].x, begin = s.items[first].x,
+                   before = first ? s.items[first - 1].x : 0xffffffffu;
+    if (key >= s.vocab || behind != key) return;                      // it ends here
+    if (begin == key && before == key) return;                        // it began earlier
     // how many of the following chunks it reaches: looked up by 32 lanes at a time
     uint32_t more = 0;
     for (;;) {
@@ -851,7 +858,7 @@ int sidco_embedding_grad(const void* dy, int dy_type, int64_t ld_dy, const void*
     su.ldd = ldd;
     su.lo = (uintptr_t)dy;
     su.hi = (uintptr_t)dy + (uintptr_t)dy_bytes;
-    su.scale = scale;
+    su.scale = on ? scale * d.factor : scale;
     su.add = add != 0;
 
     if (n <= kFewMost) {

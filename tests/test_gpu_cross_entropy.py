@@ -199,6 +199,28 @@ def test_pieces(add, ignored, dw_dtype):
         assert not grads or np.array_equal(part[3], got[3])
 
 
+@pytest.mark.parametrize("dtype,dw_dtype,hidden,lddw", [("float16", "float16", 141, 0), ("bfloat16", "float32", 141, 2),
+                                                        ("bfloat16", "bfloat16", 264, 0), ("float16", "float32", 40, 3)])
+def test_pieces_added_to_rows_of_any_alignment(dtype, dw_dtype, hidden, lddw):
+    x, w, labels = inputs(700, 500, hidden, seed=20, ignored=0.2)
+    old = rng(9).standard_normal(w.shape) * 1e-3
+    for shift in (0, 1):
+        got = call(x, w, labels, dtype, dw_dtype=dw_dtype, piece_rows=256, old=old, lds=(0, 0, 0, lddw), shift=shift)
+        check(got, labels, dtype, dw_dtype, add=True)
+
+
+@pytest.mark.parametrize("rows,vocab,hidden", [(3, 70001, 24), (1, 300, 4097), (40, 33000, 72), (513, 257, 1028)])
+def test_long_and_wide(rows, vocab, hidden):
+    x, w, labels = inputs(rows, vocab, hidden, seed=rows + vocab + hidden)
+    check(call(x, w, labels, "bfloat16"), labels, "bfloat16")
+
+
+@pytest.mark.parametrize("hidden", [32, 33, 64, 96, 128, 129, 160, 256, 257, 288])
+def test_last_tiles_of_every_width(hidden):
+    x, w, labels = inputs(150, 256 + hidden, hidden, seed=hidden)
+    check(call(x, w, labels, "float16"), labels, "float16")
+
+
 @pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
 @pytest.mark.parametrize("piece_rows", [0, 256])
 def test_no_label_at_all(dtype, piece_rows):
