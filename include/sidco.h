@@ -432,8 +432,8 @@ int sidco_embedding_grad(const void* dy, int dy_type, int64_t ld_dy, const void*
  * with c_i = row_weights[i], or 1 / (number of rows that have a label) where row_weights is NULL: the mean.  A row with a
  * negative label has none: its loss and its row of dx are zero and nothing of it, NaN included, reaches dw; rows without a
  * label cost no products.  So does a label >= vocab, which is reported in `status` (SIDCO_CROSS_ENTROPY_ST_LABEL).  Without any label the
- * loss is 0.  Logits, sums and statistics are held in fp32.  The gradient of the logits is held in `type`, rounded twice:
- * dx and dw carry an error of about 2^-8 (bf16) or 2^-11 (fp16) of the size of their terms, also where dw is fp32.
+ * loss is 0.  Logits, sums and statistics are held in fp32.  The gradient of the logits is held in `type`, behind exponentials
+ * in fp16: dx and dw carry an error of about 2^-9 (bf16) or 2^-11.5 (fp16) of their norm, also where dw is fp32.
  *
  * x          device, type[rows][ldx], type SIDCO_T_BF16 or SIDCO_T_F16.     labels  device, label_type[rows].
  * w          device, w_type[vocab][ldw], w_type = type, or SIDCO_T_F32, which is rounded to `type`.  Rows that are not 16-byte
