@@ -269,9 +269,10 @@ def test_embedding_grad_repeats_bit_for_bit_and_across_streams():
     assert all(torch.equal(outs[0][0], o) for o, _ in outs)
 
 
-def test_embedding_grad_in_a_graph_follows_its_inputs():
+@pytest.mark.parametrize("n", [1000, 5000])
+def test_embedding_grad_in_a_graph_follows_its_inputs(n):
     torch, B = torch_(), B_()
-    n, vocab, cols = 1000, 300, 60
+    vocab, cols = 300, 60
     t = torch.randint(0, vocab, (n,), device="cuda")
     dy, out = torch.randn(n, cols, device="cuda"), torch.empty(vocab, cols, device="cuda")
     need = B.sidco_embedding_grad_workspace_bytes(n, vocab, cols)
@@ -285,7 +286,7 @@ def test_embedding_grad_in_a_graph_follows_its_inputs():
         out.fill_(9)
         g.replay()
         want = L.embedding_grad(dy.double().cpu().numpy(), t.cpu().numpy(), vocab)
-        assert np.allclose(out.cpu().numpy(), want, atol=1e-4)
+        assert np.allclose(out.cpu().numpy(), want, atol=1e-4)         # sums of some 20 terms below 5
 
 
 def test_nothing_to_do():
