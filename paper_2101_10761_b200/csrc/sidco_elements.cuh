@@ -108,13 +108,10 @@ struct Dropout {
 
 __device__ __forceinline__ uint64_t call_of(const Dropout& d) { return d.step ? d.call + *d.step : d.call; }
 
-// The words of N blocks from (low, high) on; the blocks do not pass 2^32 in their low word.
-template <int N>
-__device__ __forceinline__ void random_blocks(const Dropout& d, uint64_t call, uint32_t low, uint32_t high, uint32_t (&c)[N][4]) {
+// The words of N blocks; c[q][0] and c[q][1] hold their numbers.
+template <int N> __device__ __forceinline__ void random_rounds(const Dropout& d, uint64_t call, uint32_t (&c)[N][4]) {
 #pragma unroll
     for (int q = 0; q < N; ++q) {
-        c[q][0] = low + q;
-        c[q][1] = high;
         c[q][2] = (uint32_t)call;
         c[q][3] = (uint32_t)(call >> 32);
     }
@@ -130,46 +127,29 @@ __device__ __forceinline__ void random_blocks(const Dropout& d, uint64_t call, u
         }
 }
 
-// The words of N elements (a multiple of four) from any `first` on.  Where first is no multiple of four (known to whoever
-// compiles, or the same for a whole warp) one block more is drawn.
-template <int N, bool kWhole>
-__device__ __forceinline__ void random_words(const Dropout& d, uint64_t call, uint64_t first, uint32_t (&w)[N]) {
-    constexpr int kBlocks = N / 4 + (kWhole ? 0 : 1);
-    const uint64_t block = first / 4;
-    uint32_t c[kBlocks][4];
-    if ((uint32_t)block + (kBlocks - 1) >= (uint32_t)block) {
-        random_blocks(d, call, (uint32_t)block, (uint32_t)(block >> 32), c);
-    } else {                                                          // once in 2^32 blocks
-#pragma unroll 1
-        for (int q = 0; q < kBlocks; ++q) {
-            uint32_t one[1][4];
-            random_blocks(d, call, (uint32_t)(block + q), (uint32_t)((block + q) >> 32), one);
+// Blocks (low, high), (low + 1, high) ..: they do not pass 2^32 in their low word.
+template <int N>
+__device__ __forceinline__ void random_blocks(const Dropout& d, uint64_t call, uint32_t low, uint32_t high, uint32_t (&c)[N][4]) {
 #pragma unroll
-            for (int k = 0; k < kBlocks; ++k)
-                if (k == q) c[k][0] = one[0][0], c[k][1] = one[0][1], c[k][2] = one[0][2], c[k][3] = one[0][3];
-        }
-    }
-    const int shift = (int)(first % 4);
+    for (int q = 0; q < N; ++q) c[q][0] = low + q, c[q][1] = high;
+    random_rounds(d, call, c);
+}
+
+// Any N blocks from `block` on.
+template <int N> __device__ __forceinline__ void random_blocks(const Dropout& d, uint64_t call, uint64_t block, uint32_t (&c)[N][4]) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        if constexpr (kWhole) {
-            w[i] = c[i / 4][i % 4];
-        } else {
-            const uint32_t a = shift & 1 ? c[(i + 1) / 4][(i + 1) % 4] : c[i / 4][i % 4];
-            const uint32_t b = shift & 1 ? c[(i + 3) / 4][(i + 3) % 4] : c[(i + 2) / 4][(i + 2) % 4];
-            w[i] = shift & 2 ? b : a;
-        }
-    }
+    for (int q = 0; q < N; ++q) c[q][0] = (uint32_t)(block + q), c[q][1] = (uint32_t)((block + q) >> 32);
+    random_rounds(d, call, c);
 }
 
 __device__ __forceinline__ bool dropped(const Dropout& d, uint32_t word) { return word <= d.last; }
 
-// v of the N elements from `first` on.  What is dropped becomes zero whatever it was.
-template <int N, bool kWhole = true> __device__ __forceinline__ void drop(const Dropout& d, uint64_t call, uint64_t first, float (&v)[N]) {
-    uint32_t w[N];
-    random_words<N, kWhole>(d, call, first, w);
+// v of the N elements (a multiple of four) from element 4 * block on.  What is dropped becomes zero whatever it was.
+template <int N> __device__ __forceinline__ void drop(const Dropout& d, uint64_t call, uint64_t block, float (&v)[N]) {
+    uint32_t c[N / 4][4];
+    random_blocks(d, call, block, c);
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = dropped(d, w[i]) ? 0.0f : v[i] * d.factor;
+    for (int i = 0; i < N; ++i) v[i] = dropped(d, c[i / 4][i % 4]) ? 0.0f : v[i] * d.factor;
 }
 
 // Checks p and fills d; *on: whether anything is dropped.

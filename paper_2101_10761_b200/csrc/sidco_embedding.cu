@@ -127,7 +127,7 @@ __global__ void __launch_bounds__(kThreads, 4)
             float v[N];
 #pragma unroll
             for (int j = 0; j < N; ++j) v[j] = known ? widen(raw[k][j]) * scale : 0.0f;
-            if (kDrop) drop(d, call, (uint64_t)(base + c), v);
+            if (kDrop) drop(d, call, (uint64_t)(base + c) / 4, v);
             if (kVector) {
                 store(to + c, v);
             } else {
@@ -195,7 +195,7 @@ __global__ void __launch_bounds__(kThreads, 4)
                 }
 #pragma unroll
                 for (int j = 0; j < kEach; ++j) v[j] *= scale;
-                if (kDrop) drop(d, call, (uint64_t)(base + c), v);
+                if (kDrop) drop(d, call, (uint64_t)(base + c) / 4, v);
                 TO* to = out + base + c;
                 if (base + c + kEach <= all) {
                     store(to, v);
@@ -467,12 +467,19 @@ __device__ __forceinline__ void add_up(const TI* dy, const Sums& s, const Dropou
             if (left > 0 && k + j < count) next[j].read(dy + at_next[j] * s.ld_dy + c, left, s.lo, s.hi);
         }
     };
+    const int lane = threadIdx.x & 31;
+    const bool whole = s.cols % 4 == 0;                               // every row starts a block of the generator
+    uint32_t extra[1][4] = {};
     if (count > 0) read(0);
 #pragma unroll 1
     for (int k = 0; k < count; k += kRows) {
 #pragma unroll
         for (int j = 0; j < kRows; ++j) now[j] = next[j], at[j] = at_next[j];
         read(k + kRows);
+        // Where rows start inside a block, a lane's last elements lie in its neighbour's first block, and the last lane's in one
+        // that nobody has: lane l draws that one for the l-th of the next 32 rows.
+        if (kDrop && !whole && k % 32 == 0)
+            random_blocks(d, call, ((uint64_t)row_at(min(k + lane, count - 1)) * s.cols + (c - lane * kEach)) / 4 + 2 * 32, extra);
 #pragma unroll
         for (int j = 0; j < kRows; ++j) {
             if (k + j >= count) break;
@@ -480,12 +487,33 @@ __device__ __forceinline__ void add_up(const TI* dy, const Sums& s, const Dropou
             now[j].widened(dy + at[j] * s.ld_dy + c, v);
             if (kDrop) {                                              // (the factor is part of the scale)
                 const uint64_t first = (uint64_t)at[j] * s.cols + c;
-                uint32_t w[kEach];
-                if (first % 4 == 0) random_words<kEach, true>(d, call, first, w);      // (the same for the whole warp)
-                else random_words<kEach, false>(d, call, first, w);
+                const int shift = (int)(first % 4);                   // (the same for the whole warp)
+                uint32_t w[2][4];
+                random_blocks(d, call, first / 4, w);
+                if (shift) {
+                    uint32_t q[kEach + 3];
+#pragma unroll
+                    for (int e = 0; e < kEach; ++e) q[e] = w[e / 4][e % 4];
+#pragma unroll
+                    for (int e = 0; e < 3; ++e) {
+                        const uint32_t mine = __shfl_sync(0xffffffffu, extra[0][e], (k + j) % 32);
+                        q[kEach + e] = __shfl_down_sync(0xffffffffu, w[0][e], 1);
+                        if (lane == 31) q[kEach + e] = mine;
+                    }
+                    if (shift & 1) {
+#pragma unroll
+                        for (int e = 0; e < kEach + 2; ++e) q[e] = q[e + 1];
+                    }
+                    if (shift & 2) {
+#pragma unroll
+                        for (int e = 0; e < kEach; ++e) q[e] = q[e + 2];
+                    }
+#pragma unroll
+                    for (int e = 0; e < kEach; ++e) w[e / 4][e % 4] = q[e];
+                }
 #pragma unroll
                 for (int e = 0; e < kEach; ++e)
-                    if (!dropped(d, w[e])) sum[e] += v[e];
+                    if (!dropped(d, w[e / 4][e % 4])) sum[e] += v[e];
             } else {
 #pragma unroll
                 for (int e = 0; e < kEach; ++e) sum[e] += v[e];
