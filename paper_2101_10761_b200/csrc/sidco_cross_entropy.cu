@@ -53,7 +53,7 @@ constexpr int kPairs = 74;            // of a whole B200: what the split of dX i
 
 struct Head {                         // written by prepare_kernel
     int counted;                      // rows with a label
-    float lift, unlift;               // power of two that D is stored times, and its inverse
+    float lift, unlift;               // factor that D is stored times, and its inverse
     int done;                         // rows whose loss is known
     int parts;                        // of dX's sums, for the piece at work (scale_kernel)
 };
@@ -270,14 +270,17 @@ __global__ void __launch_bounds__(kPrepareThreads) prepare_kernel(const Prepare 
             h.parts = 1;
             if (!all && a.total) *a.total = 0.0f;                     // (otherwise the last row's CTA writes it)
             for (int i = 0; i < kPrepareThreads / 32; ++i) most = max(most, s_most[i]);
-            // fp16: the largest |c scale| is brought to [2^13, 2^14) as far as the powers of two reach, so that D keeps
-            // eleven bits down to 2^-28 of it
+            // The largest |c scale| becomes a power of two: rows of that weight, all of them where the weights are equal, have
+            // D near -2^k (1 - p) at their labels, which is rounded by less than a half step where p is small (and not by the
+            // same amount in every row).  In fp16 2^14, so that D keeps eleven bits down to 2^-28 of it.
             h.lift = h.unlift = 1.0f;
             const float top = fabsf((a.weights ? __uint_as_float(most) : all ? 1.0f / (float)all : 0.0f) * a.scale);
-            if (kIsHalf<T> && top > 0.0f && top < INFINITY) {
-                const int e = max(-100, min(100, 13 - ilogbf(top)));
-                h.lift = ldexpf(1.0f, e);
-                h.unlift = ldexpf(1.0f, -e);
+            if (top > 0x1p-100f && top < 0x1p100f) {
+                h.lift = (kIsHalf<T> ? 0x1p14f : 1.0f) / top;
+                h.unlift = top * (kIsHalf<T> ? 0x1p-14f : 1.0f);
+            } else if (kIsHalf<T> && top > 0.0f && top < INFINITY) {
+                h.lift = top < 1.0f ? 0x1p100f : 0x1p-100f;
+                h.unlift = 1.0f / h.lift;
             }
             *a.head = h;
         }
