@@ -69,6 +69,11 @@ template <typename T> constexpr bool kIsHalf = std::is_same<T, __half>::value;
 // e is held in fp16 whatever the type of the operands, times 2^14: eleven bits down to 2^-28 of the largest of its half tile,
 // nothing below 2^-39.  (In bf16 its rounding would be as large as that of D: dX and dW were off by 2.6e-3 instead of 2.2e-3.)
 constexpr float kUp = 14.0f;
+// Sums in tensor memory are cut to fp32, not rounded, so that logits come out short by a part that grows with `hidden`: measured
+// 0.25 to 0.3 times 2^-24 for every 16 products, from 256 to 16384 products, whether they cancel or not.  The mean of it is put
+// back with the scale, at no cost: 4096 products 2.1e-5 off in the mean square -> 4.9e-6 (logits around 4), losses of 4096 x 32000 x 4096
+// 1.4e-6 -> 5.3e-7.  (Rows with a single product that is not zero are off by as much; the bound of the sum itself is ten times that.)
+constexpr double kCut = 0.27 * 0x1p-24 / 16;
 
 __device__ __forceinline__ int rows_of_piece(const Sizes& z, const Head* head) {
     return max(0, min(z.piece, head->counted - z.first));
@@ -1268,10 +1273,11 @@ template <typename T, typename TW> static int run(const Call& c, const Plan& p, 
                    !sidco_internal::byte_map(&map_d, c.ws + p.e, c.vocab * 2, p.piece, p.e_pitch * 2, 128, 64, true))))
         return SIDCO_E_UNSUPPORTED;
     float* share = reinterpret_cast<float*>(c.ws + p.share);
+    const float scale2 = (float)(c.scale * 1.4426950408889634 * (1 + kCut * c.hidden));
     for (int64_t i = 0; i < p.pieces; ++i) {
         const Sizes z{(int)c.rows, (int)c.vocab, (int)c.hidden, (int)p.piece, (int)(i * p.piece)};
         const int64_t most = std::min(p.piece, c.rows - z.first);      // rows if all have labels
-        Logits l{z, head, target, c.scale * 1.44269504088896f, reinterpret_cast<float2*>(c.ws + p.stats), (int)p.tiles_n,
+        Logits l{z, head, target, scale2, reinterpret_cast<float2*>(c.ws + p.stats), (int)p.tiles_n,
                  reinterpret_cast<float*>(c.ws + p.label), grads, timeouts};
         const int64_t tiles = (most + kTile - 1) / kTile * p.tiles_n;
         SIDCO_CE_LAUNCH(logits_kernel<T>, dim3((unsigned)(2 * std::min<int64_t>(pairs, tiles))), kThreads, kSmem, c.s, 1, map_x,
