@@ -67,7 +67,7 @@ __device__ int g_timeouts;
 
 template <typename T> constexpr bool kIsHalf = std::is_same<T, __half>::value;
 // e is held in fp16 whatever the type of the operands, times 2^14: eleven bits down to 2^-28 of the largest of its half tile,
-// nothing below 2^-39.  (In bf16 its rounding would be as large as that of D: dX and dW were off by 2.6e-3 instead of 2.2e-3.)
+// nothing below 2^-39.  (In bf16 its rounding would be as large as that of D, and add to it in every entry.)
 constexpr float kUp = 14.0f;
 // Sums in tensor memory are cut to fp32, not rounded, so that logits come out short by a part that grows with `hidden`: measured
 // 0.25 to 0.3 times 2^-24 for every 16 products, from 256 to 16384 products, whether they cancel or not.  The mean of it is put
