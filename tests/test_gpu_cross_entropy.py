@@ -256,6 +256,34 @@ def test_sure_rows():
     assert np.median(got[0]) < 1e-3
 
 
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+def test_equal_weights_cost_no_rounding(dtype):
+    """Of 700 rows with 128 equal logits each, the gradients of the logits are -(1 - 2^-7) and 2^-7 times 1 / 700: stored times
+    700 they are numbers of either type, so that dW is off by its own rounding and that of the fp32 sums alone."""
+    x, _, labels = inputs(700, 128, 96, seed=15)
+    each, loss, _, dw, hx, hw, _, _ = call(x, np.zeros((128, 96)), labels, dtype, grads=2)
+    _, want_loss, _, want = L.linear_cross_entropy(hx, hw, labels, None, 1.0)
+    d = np.full((700, 128), 2.0 ** -7 / 700)
+    d[np.arange(700), labels] = (1 - 2.0 ** -7) / 700
+    bound = U[dtype] * np.abs(want) * 1.01 + (700 / 16 + 4) * 2.0 ** -22 * (d.T @ np.abs(hx)) + TINY[dtype]
+    assert (np.abs(dw - want) <= bound).all(), (np.abs(dw - want) / bound).max()
+    assert abs(loss - want_loss) <= 2.0 ** -18
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+def test_long_sums_are_not_short(dtype):
+    """Losses near -s of rows whose label has the logit s, far below another of zero: sums of 8192 products that are cut to fp32
+    512 times.  Cut by half a unit of 2^-23 each time, sums that grow evenly would be short by 0.36 x 512 x 2^-24 of s (what
+    accumulators with more bits lose is less); in the mean over the rows, less than 0.1 times 512 x 2^-24 may be left."""
+    r = rng(16)
+    w = np.stack((r.standard_normal(8192) * 2 * 8192 ** -0.5, np.zeros(8192)))
+    x = r.standard_normal((1000, 8192)) - 2 * (1 + r.random((1000, 1))) * w[0]
+    each, _, _, _, hx, hw, _, _ = call(x, w, np.zeros(1000, dtype=np.int64), dtype, grads=0)
+    s = hx @ hw[0]
+    want = np.logaddexp(s, 0.0) - s
+    assert abs((each - want).mean()) < 0.1 * 512 * 2.0 ** -24 * np.abs(s).mean(), (each - want).mean() / np.abs(s).mean()
+
+
 def test_logits_of_any_size():
     """Logits of thousands, and equal ones; columns far below the others vanish."""
     x, w, labels = inputs(100, 400, 32, seed=14, sharp=600.0)
