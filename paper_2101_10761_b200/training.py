@@ -208,9 +208,9 @@ class _LinearCrossEntropy(torch.autograd.Function):
     front of the loss, in place, and hands them out, once."""
 
     @staticmethod
-    def forward(ctx, x, weight, labels, row_weights, scale, piece_rows):
+    def forward(ctx, x, weight, labels, row_weights, scale, piece_rows, wanted):
         (rows, hidden), vocab = x.shape, weight.shape[0]
-        need_x, need_w = ctx.needs_input_grad[:2]
+        need_x, need_w = (wanted and need for need in ctx.needs_input_grad[:2])
         x, ldx = _rows(x)
         w, ldw = _rows(weight)
         loss = torch.empty((), dtype=torch.float32, device=x.device)
@@ -235,7 +235,7 @@ class _LinearCrossEntropy(torch.autograd.Function):
             if g is not None:
                 with torch.cuda.device(g.device):
                     B.sidco_scale_gradient(g, g.numel(), dloss)
-        return grads + (None, None, None, None)
+        return grads + (None, None, None, None, None)
 
 
 def linear_cross_entropy(x: torch.Tensor, weight: torch.Tensor, labels: torch.Tensor,
@@ -244,7 +244,8 @@ def linear_cross_entropy(x: torch.Tensor, weight: torch.Tensor, labels: torch.Te
 
     x [..., hidden] in bf16 or fp16, weight [vocab, hidden] in the same type or fp32 (a master copy: rounded for the
     products, its gradient in fp32), labels [...] int32 or int64.  Rows with a negative label do not count.  The result is
-    the mean over the others, or with row_weights [...] (fp32) the sum of the rows' losses times these."""
+    the mean over the others, or with row_weights [...] (fp32) the sum of the rows' losses times these.  Under
+    ``torch.no_grad()`` the loss alone is computed, with a third of the operations."""
     if x.dtype not in (torch.bfloat16, torch.float16):
         raise ValueError(f"x must be bf16 or fp16, got {x.dtype}")
     if weight.dim() != 2 or x.dim() < 1 or x.shape[-1] != weight.shape[1] or not weight.numel():
@@ -260,9 +261,10 @@ def linear_cross_entropy(x: torch.Tensor, weight: torch.Tensor, labels: torch.Te
         if t is not None and t.device != x.device:
             raise ValueError(f"all arguments must be on {x.device}, got one on {t.device}")
     rows = labels.numel()
+    # (inside the function gradients look switched off always, and a parameter needs one even where they are)
     return _LinearCrossEntropy.apply(x.reshape(rows, x.shape[-1]), weight, labels.reshape(-1).contiguous(),
                                      None if row_weights is None else row_weights.reshape(-1).contiguous(), float(scale),
-                                     int(piece_rows))
+                                     int(piece_rows), torch.is_grad_enabled())
 
 
 class OrthogonalizedUpdate:
