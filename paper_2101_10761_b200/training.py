@@ -210,18 +210,19 @@ class _LinearCrossEntropy(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, labels, row_weights, scale, piece_rows, wanted):
         (rows, hidden), vocab = x.shape, weight.shape[0]
-        need_x, need_w = (wanted and need for need in ctx.needs_input_grad[:2])
+        need_x, need_w, _, need_c = (wanted and need for need in ctx.needs_input_grad[:4])
         x, ldx = _rows(x)
         w, ldw = _rows(weight)
         loss = torch.empty((), dtype=torch.float32, device=x.device)
         dx = torch.empty(rows, hidden, dtype=x.dtype, device=x.device) if need_x else None
         dw = torch.empty(vocab, hidden, dtype=weight.dtype, device=x.device) if need_w else None
+        dc = torch.empty(rows, dtype=torch.float32, device=x.device) if need_c else None     # (the rows' losses)
         need = B.sidco_linear_cross_entropy_workspace_bytes(x, w, ldw, rows, vocab, hidden, need_x + 2 * need_w, piece_rows)
         with torch.cuda.device(x.device):
             workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
-            B.sidco_linear_cross_entropy(x, ldx, w, ldw, labels, rows, vocab, hidden, None, loss, dx, hidden, dw, hidden,
+            B.sidco_linear_cross_entropy(x, ldx, w, ldw, labels, rows, vocab, hidden, dc, loss, dx, hidden, dw, hidden,
                                          workspace, need, row_weights=row_weights, scale=scale, piece_rows=piece_rows)
-        ctx.grads = (dx, dw)
+        ctx.grads = (dx, dw, dc)
         return loss
 
     @staticmethod
@@ -235,7 +236,8 @@ class _LinearCrossEntropy(torch.autograd.Function):
             if g is not None:
                 with torch.cuda.device(g.device):
                     B.sidco_scale_gradient(g, g.numel(), dloss)
-        return grads + (None, None, None, None, None)
+        dx, dw, dc = grads
+        return dx, dw, None, dc, None, None, None
 
 
 def linear_cross_entropy(x: torch.Tensor, weight: torch.Tensor, labels: torch.Tensor,
@@ -244,7 +246,8 @@ def linear_cross_entropy(x: torch.Tensor, weight: torch.Tensor, labels: torch.Te
 
     x [..., hidden] in bf16 or fp16, weight [vocab, hidden] in the same type or fp32 (a master copy: rounded for the
     products, its gradient in fp32), labels [...] int32 or int64.  Rows with a negative label do not count.  The result is
-    the mean over the others, or with row_weights [...] (fp32) the sum of the rows' losses times these.  Under
+    the mean over the others, or with row_weights [...] (fp32) the sum of the rows' losses times these, which may require a
+    gradient themselves.  Under
     ``torch.no_grad()`` the loss alone is computed, with a third of the operations."""
     if x.dtype not in (torch.bfloat16, torch.float16):
         raise ValueError(f"x must be bf16 or fp16, got {x.dtype}")

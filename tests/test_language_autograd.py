@@ -46,3 +46,24 @@ def test_training_asks_for_the_gradients_that_are_needed(asked):
     with torch.no_grad(), torch.enable_grad():
         T.linear_cross_entropy(x, w, y)
     assert asked == [(2, False, True), (3, True, True), (1, True, False), (2, False, True)]
+
+
+def test_weights_of_the_rows_get_their_gradient(asked, monkeypatch):
+    """It is the rows' losses times the factor in front of the loss; the losses are asked for only then."""
+    rows_asked = []
+    plain = T.B.sidco_linear_cross_entropy
+
+    def call(*a, **kw):
+        rows_asked.append(a[8] is not None)
+        plain(*a, **kw)
+    scaled = []
+    monkeypatch.setattr(T.B, "sidco_linear_cross_entropy", call)
+    monkeypatch.setattr(T.B, "sidco_scale_gradient", lambda g, n, f: scaled.append((g.shape, n)))
+    x, w, y = arguments()
+    c = torch.zeros(2, 3, device="meta", requires_grad=True)
+    T.linear_cross_entropy(x, w.detach(), y, c).backward()
+    assert c.grad.shape == (2, 3) and scaled == [((6,), 6)] and asked == [(0, False, False)]
+    T.linear_cross_entropy(x, w, y, c.detach())
+    with torch.no_grad():
+        T.linear_cross_entropy(x, w, y, c)
+    assert rows_asked == [True, False, False]
