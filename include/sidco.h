@@ -439,7 +439,8 @@ int sidco_embedding_grad(const void* dy, int dy_type, int64_t ld_dy, const void*
  * w          device, w_type[vocab][ldw], w_type = type, or SIDCO_T_F32, which is rounded to `type`.  Rows that are not 16-byte
  *            aligned, and fp32, are copied to the workspace in every call.
  * row_losses device, float[rows], or NULL.       loss  device, float, or NULL.
- * dx         device, type[rows][lddx], or NULL: not wanted.
+ * dx         device, type[rows][lddx], or NULL: not wanted.  In fp16 what lies below 2^-24 is lost, as the gradients of a mean
+ *            over thousands of rows do: let row_weights hold the factor of a scaled loss, or take fp32 (.._typed, dw_type).
  * dw         device, dw_type[vocab][lddw], dw_type = type or SIDCO_T_F32, or NULL: not wanted.
  * piece_rows rows whose gradient of the logits is held at a time (rounded up to 256); 0: as many as fit into 512 MB or what
  *            dw takes in 32 bits, whichever is more.  With several pieces dw is summed in fp32 in the workspace.
@@ -460,10 +461,21 @@ int sidco_linear_cross_entropy(const void* x, int type, int64_t ldx, const void*
                                void* dw, int dw_type, int64_t lddw, int add_dw, int64_t piece_rows, int32_t* status,
                                void* workspace, size_t workspace_bytes, void* stream);
 
+/* sidco_linear_cross_entropy_typed - the same, with dx in `dx_type`: `type`, or SIDCO_T_F32. */
+int sidco_linear_cross_entropy_typed(const void* x, int type, int64_t ldx, const void* w, int w_type, int64_t ldw,
+                                     const void* labels, int label_type, const float* row_weights, float scale, int64_t rows,
+                                     int64_t vocab, int64_t hidden, float* row_losses, float* loss, void* dx, int dx_type,
+                                     int64_t lddx, void* dw, int dw_type, int64_t lddw, int add_dw, int64_t piece_rows,
+                                     int32_t* status, void* workspace, size_t workspace_bytes, void* stream);
+
 /* sidco_scale_gradient - x *= *factor, for gradients that were computed before the factor in front of the loss was known.
  * x device, type[n], aligned to its element, n <= 2^40; factor device, float.  The product is rounded once; a factor of 1
  * reads and writes nothing. */
 int sidco_scale_gradient(void* x, int type, int64_t n, const float* factor, void* stream);
+
+/* sidco_round_gradient - out = *factor * x, rounded once: fp32 to type[n].  For fp16 gradients whose factor (of a scaled loss)
+ * brings them into that type's range: what is rounded before the factor loses what lies below 2^-24.  out must not overlap x. */
+int sidco_round_gradient(const float* x, int64_t n, const float* factor, void* out, int type, void* stream);
 
 /* How many CTAs of the product kernels (sidco_mx4_matmul, sidco_orthogonalize, sidco_linear_cross_entropy) have given up a bounded wait since the
  * library was loaded; anything but 0 means that an output is incomplete.  Negative: a CUDA error.  Synchronises the

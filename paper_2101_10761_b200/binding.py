@@ -50,7 +50,8 @@ EXPORTS = [
     "sidco_mx4_compress", "sidco_mx4_mean", "sidco_orthogonalize_workspace_bytes", "sidco_orthogonalize",
     "sidco_wait_timeouts", "sidco_set_product_test_hooks",
     "sidco_dropout", "sidco_embedding", "sidco_embedding_grad_workspace_bytes", "sidco_embedding_grad",
-    "sidco_linear_cross_entropy_workspace_bytes", "sidco_linear_cross_entropy", "sidco_scale_gradient",
+    "sidco_linear_cross_entropy_workspace_bytes", "sidco_linear_cross_entropy", "sidco_linear_cross_entropy_typed",
+    "sidco_scale_gradient", "sidco_round_gradient",
 ]
 
 _lib = None
@@ -165,6 +166,11 @@ def lib() -> C.CDLL:
     L.sidco_linear_cross_entropy.argtypes = [vp, i32, i64, vp, i32, i64, vp, i32, vp, f32, i64, i64, i64, vp, vp, vp, i64, vp,
                                              i32, i64, i32, i64, vp, vp, sz, vp]
     L.sidco_linear_cross_entropy.restype = i32
+    L.sidco_linear_cross_entropy_typed.argtypes = [vp, i32, i64, vp, i32, i64, vp, i32, vp, f32, i64, i64, i64, vp, vp, vp,
+                                                   i32, i64, vp, i32, i64, i32, i64, vp, vp, sz, vp]
+    L.sidco_linear_cross_entropy_typed.restype = i32
+    L.sidco_round_gradient.argtypes = [vp, i64, vp, vp, i32, vp]
+    L.sidco_round_gradient.restype = i32
     L.sidco_scale_gradient.argtypes = [vp, i32, i64, vp, vp]
     L.sidco_scale_gradient.restype = i32
     _lib = L
@@ -613,15 +619,22 @@ def sidco_linear_cross_entropy_workspace_bytes(x, w, ldw: int, rows: int, vocab:
 def sidco_linear_cross_entropy(x, ldx: int, w, ldw: int, labels, rows: int, vocab: int, hidden: int, row_losses, loss, dx,
                                lddx: int, dw, lddw: int, workspace, workspace_bytes: int, row_weights=None,
                                scale: float = 1.0, add: bool = False, piece_rows: int = 0, status=None, x_type=None,
-                               w_type=None, label_type=None, dw_type=None, stream=None) -> None:
-    """Cross entropy of scale * x w^T against labels: losses and, where dx / dw are given, the gradients."""
-    rc = lib().sidco_linear_cross_entropy(
-        _ptr(x), _type(x, x_type), ldx, _ptr(w), _type(w, w_type), ldw, _ptr(labels), _token_type(labels, label_type),
-        _ptr(row_weights), scale, rows, vocab, hidden, _ptr(row_losses), _ptr(loss), _ptr(dx), lddx, _ptr(dw),
+                               w_type=None, label_type=None, dw_type=None, dx_type=None, stream=None) -> None:
+    """Cross entropy of scale * x w^T against labels: losses and, where dx / dw are given, the gradients.  A dx without a type
+    of its own has that of x."""
+    t = _type(x, x_type)
+    if dx_type is None:
+        dx_type = _type(dx, None) if hasattr(dx, "dtype") else t
+    rc = lib().sidco_linear_cross_entropy_typed(
+        _ptr(x), t, ldx, _ptr(w), _type(w, w_type), ldw, _ptr(labels), _token_type(labels, label_type),
+        _ptr(row_weights), scale, rows, vocab, hidden, _ptr(row_losses), _ptr(loss), _ptr(dx), dx_type, lddx, _ptr(dw),
         0 if dw is None else _type(dw, dw_type), lddw, int(add), piece_rows, _ptr(status), _ptr(workspace),
         workspace_bytes, _stream(stream))
     if rc:
         raise SidcoError(rc, "sidco_linear_cross_entropy")
+
+
+sidco_linear_cross_entropy_typed = sidco_linear_cross_entropy       # (its dx may have a type of its own here too)
 
 
 def sidco_scale_gradient(x, n: int, factor, x_type=None, stream=None) -> None:
@@ -629,3 +642,10 @@ def sidco_scale_gradient(x, n: int, factor, x_type=None, stream=None) -> None:
     rc = lib().sidco_scale_gradient(_ptr(x), _type(x, x_type), n, _ptr(factor), _stream(stream))
     if rc:
         raise SidcoError(rc, "sidco_scale_gradient")
+
+
+def sidco_round_gradient(x, n: int, factor, out, out_type=None, stream=None) -> None:
+    """out = *factor * x, rounded once; x in fp32."""
+    rc = lib().sidco_round_gradient(_ptr(x), n, _ptr(factor), _ptr(out), _type(out, out_type), _stream(stream))
+    if rc:
+        raise SidcoError(rc, "sidco_round_gradient")

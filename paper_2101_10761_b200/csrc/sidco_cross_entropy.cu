@@ -115,6 +115,7 @@ struct Prepare {
     void* x_to;
     void* w_to;                       // NULL: W is used where it is
     void* dx;                         // NULL: not wanted
+    int dx_wide;                      // in fp32
     int64_t lddx;
     float *each, *total;              // NULL: not wanted
     Head* head;
@@ -216,9 +217,10 @@ __device__ __forceinline__ void copy_row(const TI* from, T* to, int cols, bool v
 template <typename T>
 __device__ __forceinline__ void zero_row(T* to, int cols, bool vector, int lane) {
     const T zero = narrow<T>(0.0f);
+    constexpr int kPer = 16 / (int)sizeof(T);
     if (vector) {
-        for (int i = lane; i < cols / 8; i += 32) reinterpret_cast<uint4*>(to)[i] = uint4{};
-        for (int i = cols / 8 * 8 + lane; i < cols; i += 32) to[i] = zero;
+        for (int i = lane; i < cols / kPer; i += 32) reinterpret_cast<uint4*>(to)[i] = uint4{};
+        for (int i = cols / kPer * kPer + lane; i < cols; i += 32) to[i] = zero;
     } else {
         for (int i = lane; i < cols; i += 32) to[i] = zero;
     }
@@ -321,6 +323,8 @@ __global__ void __launch_bounds__(kPrepareThreads) prepare_kernel(const Prepare 
             if (s_to[i] >= 0)
                 copy_bits(static_cast<const T*>(a.x) + (r0 + i) * a.ldx, static_cast<T*>(a.x_to) + s_to[i] * a.pitch, a.hidden,
                           (uintptr_t)a.x, (uintptr_t)(static_cast<const T*>(a.x) + (a.rows - 1) * a.ldx + a.hidden), lane);
+            else if (a.dx && a.dx_wide)
+                zero_row(static_cast<float*>(a.dx) + (r0 + i) * a.lddx, a.hidden, a.dx_vector, lane);
             else if (a.dx)
                 zero_row(static_cast<T*>(a.dx) + (r0 + i) * a.lddx, a.hidden, a.dx_vector, lane);
         }
@@ -966,7 +970,7 @@ __device__ __forceinline__ void put_tile(uint32_t tmem, uint8_t* box, int row, T
     }
 }
 
-template <typename T, typename TW>
+template <typename T, typename TW, typename TX>
 __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2)
     grads_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w,
                  const __grid_constant__ CUtensorMap map_d, const Grads g) {
@@ -1018,7 +1022,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2)
             const Added more{false, 0, 0, !is_dx && g.more ? out + col : nullptr, g.pitch};
             put_tile(sums, box, row, out + col, g.pitch, (int)g.pitch - col, 1.0f, 16, more, take);
         } else if (is_dx) {
-            put_tile(sums, box, row, static_cast<T*>(g.dx) + col, g.lddx, left, unlift, g.dx_unit, Added{}, take);
+            put_tile(sums, box, row, static_cast<TX*>(g.dx) + col, g.lddx, left, unlift, g.dx_unit, Added{}, take);
         } else {
             TW* out = static_cast<TW*>(g.dw);
             const Added more{g.add != 0, (uintptr_t)out, (uintptr_t)(out + (g.z.vocab - 1) * g.lddw + g.z.hidden),
@@ -1067,7 +1071,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2)
 constexpr int kJoinThreads = 256;
 
 // dX = the parts of its sums, in order (where they are one part after all, it has nothing to do: few CTAs).
-template <typename T>
+template <typename TX>
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(const Grads g) {
     wait_prerequisites();
     launch_dependents();
@@ -1088,15 +1092,15 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const Grads g) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) v[j] += k0 + k < parts ? o[k][j] : 0.0f;
         }
-        T* out = static_cast<T*>(g.dx) + g.map[g.z.first + r] * g.lddx + c;
+        TX* out = static_cast<TX*>(g.dx) + g.map[g.z.first + r] * g.lddx + c;
 #pragma unroll
         for (int j = 0; j < 4; ++j) v[j] *= unlift;
-        if (g.dx_unit >= 8 && c + 4 <= g.z.hidden) {
+        if (g.dx_unit >= 4 * (int)sizeof(TX) && c + 4 <= g.z.hidden) {
             store(out, v);
         } else {
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                if (c + j < g.z.hidden) out[j] = narrow<T>(v[j]);
+                if (c + j < g.z.hidden) out[j] = narrow<TX>(v[j]);
         }
     }
 }
@@ -1180,11 +1184,11 @@ static int unit_of(const void* p, int64_t ld, int type) {
     return n;
 }
 
-template <typename T, typename TW> static cudaError_t prepare_device(int* pairs) {
+template <typename T, typename TW, typename TX> static cudaError_t prepare_device(int* pairs) {
     const auto most = cudaFuncAttributeMaxDynamicSharedMemorySize;
     cudaError_t e;
     if ((e = cudaFuncSetAttribute(logits_kernel<T>, most, kSmem)) != cudaSuccess ||
-        (e = cudaFuncSetAttribute(grads_kernel<T, TW>, most, kSmem)) != cudaSuccess)
+        (e = cudaFuncSetAttribute(grads_kernel<T, TW, TX>, most, kSmem)) != cudaSuccess)
         return e;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(2);
@@ -1196,7 +1200,7 @@ template <typename T, typename TW> static cudaError_t prepare_device(int* pairs)
     attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    e = cudaOccupancyMaxActiveClusters(pairs, grads_kernel<T, TW>, &cfg);
+    e = cudaOccupancyMaxActiveClusters(pairs, grads_kernel<T, TW, TX>, &cfg);
     return e == cudaSuccess && *pairs < 1 ? cudaErrorInvalidConfiguration : e;
 }
 
@@ -1214,6 +1218,7 @@ struct Call {
     int64_t rows, vocab, hidden;
     float *each, *total;
     void* dx;
+    int dx_type;
     int64_t lddx;
     void* dw;
     int dw_type;
@@ -1231,7 +1236,7 @@ struct Call {
         sidco_internal::note_launch();                           \
     } while (0)
 
-template <typename T, typename TW> static int run(const Call& c, const Plan& p, bool copy_w) {
+template <typename T, typename TW, typename TX> static int run(const Call& c, const Plan& p, bool copy_w) {
     static std::atomic<int> pairs_of[64];
     int dev = 0, sms = 0, *timeouts = nullptr;
     cudaError_t e = cudaGetDevice(&dev);
@@ -1239,7 +1244,7 @@ template <typename T, typename TW> static int run(const Call& c, const Plan& p, 
     if (dev < 0 || dev >= 64) return SIDCO_E_SIZE;
     if (!pairs_of[dev].load()) {             // (setting it twice from two threads is harmless)
         int n = 0;
-        if ((e = prepare_device<T, TW>(&n)) != cudaSuccess) return (int)e;
+        if ((e = prepare_device<T, TW, TX>(&n)) != cudaSuccess) return (int)e;
         pairs_of[dev].store(n);
     }
     const int pairs = pairs_of[dev].load();
@@ -1258,10 +1263,11 @@ template <typename T, typename TW> static int run(const Call& c, const Plan& p, 
     a.weights = c.weights, a.scale = c.scale;
     a.rows = (int)c.rows, a.vocab = (int)c.vocab, a.hidden = (int)c.hidden, a.pitch = p.pitch;
     a.x_to = c.ws + p.x, a.w_to = copy_w ? c.ws + p.w : nullptr;
-    a.dx = c.dx, a.lddx = c.lddx, a.each = c.each, a.total = c.total, a.head = head, a.map = map, a.target = target, a.weight = weight;
+    a.dx = c.dx, a.dx_wide = c.dx_type == SIDCO_T_F32, a.lddx = c.lddx, a.each = c.each, a.total = c.total;
+    a.head = head, a.map = map, a.target = target, a.weight = weight;
     a.status = c.status;
     a.x_blocks = (int)std::min<int64_t>(c.rows, sms), a.x_rows = (int)((c.rows + a.x_blocks - 1) / a.x_blocks);
-    a.w_vector = unit_of(c.w, c.ldw, c.w_type) == 16, a.dx_vector = unit_of(c.dx, c.lddx, c.type) == 16;
+    a.w_vector = unit_of(c.w, c.ldw, c.w_type) == 16, a.dx_vector = unit_of(c.dx, c.lddx, c.dx_type) == 16;
     const unsigned blocks = (unsigned)(a.x_blocks + (copy_w ? std::min<int64_t>((c.vocab + 7) / 8, 16 * sms) : 0));
     if (c.w_type == SIDCO_T_F32) SIDCO_CE_LAUNCH(prepare_kernel<T, float>, dim3(blocks), kPrepareThreads, 0, c.s, 1, a);
     else SIDCO_CE_LAUNCH(prepare_kernel<T, T>, dim3(blocks), kPrepareThreads, 0, c.s, 1, a);
@@ -1292,13 +1298,19 @@ template <typename T, typename TW> static int run(const Call& c, const Plan& p, 
         SIDCO_CE_LAUNCH(scale_kernel<T>, dim3((unsigned)up_to(most, kStageK), (unsigned)shares), kScaleThreads, 0, c.s, 1, k);
         Grads g{z, head, map, c.dx, c.lddx, reinterpret_cast<float*>(c.ws + p.dx_parts), c.dw, c.lddw, c.add,
                 reinterpret_cast<float*>(c.ws + p.dw_sums), i > 0, i + 1 == p.pieces, share, c.total, p.pitch,
-                unit_of(c.dx, c.lddx, c.type), unit_of(c.dw, c.lddw, c.dw_type), timeouts};
-        SIDCO_CE_LAUNCH((grads_kernel<T, TW>), dim3(2 * (unsigned)pairs), kThreads, kSmem, c.s, 1, map_x, map_w, map_d, g);
+                unit_of(c.dx, c.lddx, c.dx_type), unit_of(c.dw, c.lddw, c.dw_type), timeouts};
+        SIDCO_CE_LAUNCH((grads_kernel<T, TW, TX>), dim3(2 * (unsigned)pairs), kThreads, kSmem, c.s, 1, map_x, map_w, map_d, g);
         if (c.dx && p.part_rows)
-            SIDCO_CE_LAUNCH(join_kernel<T>, dim3((unsigned)std::min<int64_t>((most * ((c.hidden + 3) / 4) + kJoinThreads - 1) / kJoinThreads, 8 * sms)),
+            SIDCO_CE_LAUNCH(join_kernel<TX>, dim3((unsigned)std::min<int64_t>((most * ((c.hidden + 3) / 4) + kJoinThreads - 1) / kJoinThreads, 8 * sms)),
                             kJoinThreads, 0, c.s, 1, g);
     }
     return 0;
+}
+
+template <typename T> static int run(const Call& c, const Plan& p, bool copy_w) {
+    const bool wide_x = c.dx && c.dx_type == SIDCO_T_F32;
+    if (c.dw && c.dw_type == SIDCO_T_F32) return wide_x ? run<T, float, float>(c, p, copy_w) : run<T, float, T>(c, p, copy_w);
+    return wide_x ? run<T, T, float>(c, p, copy_w) : run<T, T, T>(c, p, copy_w);
 }
 
 }  // namespace sidco_ce
@@ -1320,23 +1332,24 @@ int64_t sidco_linear_cross_entropy_workspace_bytes(const void* w, int type, int 
     return p.countable ? p.bytes : SIDCO_E_SIZE;
 }
 
-int sidco_linear_cross_entropy(const void* x, int type, int64_t ldx, const void* w, int w_type, int64_t ldw, const void* labels,
-                               int label_type, const float* row_weights, float scale, int64_t rows, int64_t vocab,
-                               int64_t hidden, float* row_losses, float* loss, void* dx, int64_t lddx, void* dw, int dw_type,
-                               int64_t lddw, int add_dw, int64_t piece_rows, int32_t* status, void* workspace,
-                               size_t workspace_bytes, void* stream) {
+int sidco_linear_cross_entropy_typed(const void* x, int type, int64_t ldx, const void* w, int w_type, int64_t ldw,
+                                     const void* labels, int label_type, const float* row_weights, float scale, int64_t rows,
+                                     int64_t vocab, int64_t hidden, float* row_losses, float* loss, void* dx, int dx_type,
+                                     int64_t lddx, void* dw, int dw_type, int64_t lddw, int add_dw, int64_t piece_rows,
+                                     int32_t* status, void* workspace, size_t workspace_bytes, void* stream) {
     using namespace sidco_ce;
     if (const int rc = check(rows, vocab, hidden, piece_rows)) return rc;
     if ((type != SIDCO_T_BF16 && type != SIDCO_T_F16) || (w_type != SIDCO_T_F32 && w_type != type) ||
-        (dw && dw_type != SIDCO_T_F32 && dw_type != type) || (label_type != SIDCO_T_I32 && label_type != SIDCO_T_I64))
+        (dx && dx_type != SIDCO_T_F32 && dx_type != type) || (dw && dw_type != SIDCO_T_F32 && dw_type != type) ||
+        (label_type != SIDCO_T_I32 && label_type != SIDCO_T_I64))
         return SIDCO_E_TYPE;
     if (ldx < hidden || ldw < hidden || (dx && lddx < hidden) || (dw && lddw < hidden) || !(scale - scale == 0.0f))
         return SIDCO_E_PARAMS;
     if (hidden == 0 || vocab == 0) return SIDCO_E_SIZE;
     const int64_t label_size = label_type == SIDCO_T_I64 ? 8 : 4;
     if (rows > 0 && (!x || !w || !labels)) return SIDCO_E_NULL;
-    if ((uintptr_t)x % 2 || (uintptr_t)dx % 2 || (uintptr_t)w % size_of(w_type) || (dw && (uintptr_t)dw % size_of(dw_type)) ||
-        (uintptr_t)labels % (uintptr_t)label_size || (uintptr_t)row_weights % 4 || (uintptr_t)row_losses % 4 ||
+    if ((uintptr_t)x % 2 || (dx && (uintptr_t)dx % size_of(dx_type)) || (uintptr_t)w % size_of(w_type) ||
+        (dw && (uintptr_t)dw % size_of(dw_type)) || (uintptr_t)labels % (uintptr_t)label_size || (uintptr_t)row_weights % 4 || (uintptr_t)row_losses % 4 ||
         (uintptr_t)loss % 4 || (uintptr_t)status % 4)
         return SIDCO_E_ALIGN;
     cudaStream_t s = (cudaStream_t)stream;
@@ -1348,7 +1361,7 @@ int sidco_linear_cross_entropy(const void* x, int type, int64_t ldx, const void*
         if (!workspace || workspace_bytes < (size_t)p.bytes || (uintptr_t)workspace % 256) return SIDCO_E_WORKSPACE;
         // every buffer that is written against every other
         const struct { const void* p; int64_t bytes; bool out; } all[] = {
-            {dx, extent(rows, hidden, lddx, type), true}, {dw, extent(vocab, hidden, lddw, dw_type), true},
+            {dx, extent(rows, hidden, lddx, dx_type), true}, {dw, extent(vocab, hidden, lddw, dw_type), true},
             {row_losses, rows * 4, true},                 {loss, 4, true},
             {workspace, p.bytes, true},                   {status, 4, true},
             {x, extent(rows, hidden, ldx, type), false},  {w, extent(vocab, hidden, ldw, w_type), false},
@@ -1362,10 +1375,8 @@ int sidco_linear_cross_entropy(const void* x, int type, int64_t ldx, const void*
             if (e != cudaSuccess) return (int)e;
         }
         const Call c{x, type, ldx, w, w_type, ldw, labels, label_type, row_weights, scale, rows, vocab, hidden, row_losses, loss,
-                     dx, lddx, dw, dw_type, lddw, add_dw != 0, status, static_cast<uint8_t*>(workspace), s};
-        if (type == SIDCO_T_BF16)
-            return dw && dw_type == SIDCO_T_F32 ? run<__nv_bfloat16, float>(c, p, copy_w) : run<__nv_bfloat16, __nv_bfloat16>(c, p, copy_w);
-        return dw && dw_type == SIDCO_T_F32 ? run<__half, float>(c, p, copy_w) : run<__half, __half>(c, p, copy_w);
+                     dx, dx_type, lddx, dw, dw_type, lddw, add_dw != 0, status, static_cast<uint8_t*>(workspace), s};
+        return type == SIDCO_T_BF16 ? run<__nv_bfloat16>(c, p, copy_w) : run<__half>(c, p, copy_w);
     }
     // no rows: no loss, no gradient
     cudaError_t e = cudaSuccess;
@@ -1374,6 +1385,16 @@ int sidco_linear_cross_entropy(const void* x, int type, int64_t ldx, const void*
     if (e == cudaSuccess && dw && !add_dw)
         e = cudaMemset2DAsync(dw, lddw * size_of(dw_type), 0, hidden * size_of(dw_type), vocab, s);
     return (int)e;
+}
+
+int sidco_linear_cross_entropy(const void* x, int type, int64_t ldx, const void* w, int w_type, int64_t ldw, const void* labels,
+                               int label_type, const float* row_weights, float scale, int64_t rows, int64_t vocab,
+                               int64_t hidden, float* row_losses, float* loss, void* dx, int64_t lddx, void* dw, int dw_type,
+                               int64_t lddw, int add_dw, int64_t piece_rows, int32_t* status, void* workspace,
+                               size_t workspace_bytes, void* stream) {
+    return sidco_linear_cross_entropy_typed(x, type, ldx, w, w_type, ldw, labels, label_type, row_weights, scale, rows, vocab, hidden,
+                                            row_losses, loss, dx, type, lddx, dw, dw_type, lddw, add_dw, piece_rows, status,
+                                            workspace, workspace_bytes, stream);
 }
 
 }  // extern "C"

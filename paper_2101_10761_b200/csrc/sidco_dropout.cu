@@ -94,6 +94,25 @@ __global__ void __launch_bounds__(kThreads) scale_gradient_kernel(T* x, int64_t 
     }
 }
 
+// Four at a time from fp32 to another type; reads and writes everything once, whatever the factor.
+template <typename T, bool kVector>
+__global__ void __launch_bounds__(kThreads) round_gradient_kernel(const float* x, int64_t n, const float* factor, T* out) {
+    sidco_tc::wait_prerequisites();
+    sidco_tc::launch_dependents();
+    const float f = *factor;
+    for (int64_t i = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * 4; i < n; i += (int64_t)gridDim.x * kThreads * 4) {
+        float v[4];
+        if (kVector && i + 4 <= n) {
+            load(x + i, v);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] *= f;
+            store(out + i, v);
+        } else {
+            for (int j = 0; j < 4 && i + j < n; ++j) out[i + j] = narrow<T>(x[i + j] * f);
+        }
+    }
+}
+
 }  // namespace sidco_dropout_impl
 
 extern "C" {
@@ -112,6 +131,25 @@ int sidco_scale_gradient(void* x, int type, int64_t n, const float* factor, void
         using T = std::remove_pointer_t<decltype(t)>;
         return (int)launch((uintptr_t)x % 16 ? scale_gradient_kernel<T, false> : scale_gradient_kernel<T, true>, dim3((unsigned)blocks),
                            kThreads, 0, (cudaStream_t)stream, 1, (T*)x, n, factor);
+    });
+    if (rc == 0) sidco_internal::note_launch();
+    return rc;
+}
+
+int sidco_round_gradient(const float* x, int64_t n, const float* factor, void* out, int type, void* stream) {
+    using namespace sidco_dropout_impl;
+    if (n < 0 || n > ((int64_t)1 << 40)) return SIDCO_E_SIZE;
+    if (type < SIDCO_T_F32 || type > SIDCO_T_F16) return SIDCO_E_TYPE;
+    if (n == 0) return 0;
+    if (!x || !factor || !out) return SIDCO_E_NULL;
+    if ((uintptr_t)x % 4 || (uintptr_t)factor % 4 || (uintptr_t)out % size_of(type)) return SIDCO_E_ALIGN;
+    if (overlap(out, n * size_of(type), x, n * 4) || overlap(out, n * size_of(type), factor, 4)) return SIDCO_E_ALIAS;
+    const int64_t blocks = std::min<int64_t>((n + 8 * kThreads - 1) / (8 * kThreads), 148 * 8);
+    const int rc = with_type(type, [&](auto* t) {
+        using T = std::remove_pointer_t<decltype(t)>;
+        const bool vector = (uintptr_t)x % 16 == 0 && (uintptr_t)out % (4 * sizeof(T)) == 0;
+        return (int)launch(vector ? round_gradient_kernel<T, true> : round_gradient_kernel<T, false>, dim3((unsigned)blocks), kThreads,
+                           0, (cudaStream_t)stream, 1, x, n, factor, (T*)out);
     });
     if (rc == 0) sidco_internal::note_launch();
     return rc;

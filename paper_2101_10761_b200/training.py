@@ -205,7 +205,8 @@ def dropout(x: torch.Tensor, p: float, seed: int, call: int = 0, step: Optional[
 
 class _LinearCrossEntropy(torch.autograd.Function):
     """The gradients come from the forward pass, where the logits are; the backward pass multiplies them by the factor in
-    front of the loss, in place, and hands them out, once."""
+    front of the loss, in place, and hands them out, once.  Those in fp16 wait in fp32 for the factor, which is the scale of a
+    scaled loss: the gradients of a mean over thousands of rows lie below that type's range without it."""
 
     @staticmethod
     def forward(ctx, x, weight, labels, row_weights, scale, piece_rows, wanted):
@@ -214,15 +215,16 @@ class _LinearCrossEntropy(torch.autograd.Function):
         x, ldx = _rows(x)
         w, ldw = _rows(weight)
         loss = torch.empty((), dtype=torch.float32, device=x.device)
-        dx = torch.empty(rows, hidden, dtype=x.dtype, device=x.device) if need_x else None
-        dw = torch.empty(vocab, hidden, dtype=weight.dtype, device=x.device) if need_w else None
+        wide = {torch.float16: torch.float32}
+        dx = torch.empty(rows, hidden, dtype=wide.get(x.dtype, x.dtype), device=x.device) if need_x else None
+        dw = torch.empty(vocab, hidden, dtype=wide.get(weight.dtype, weight.dtype), device=x.device) if need_w else None
         dc = torch.empty(rows, dtype=torch.float32, device=x.device) if need_c else None     # (the rows' losses)
         need = B.sidco_linear_cross_entropy_workspace_bytes(x, w, ldw, rows, vocab, hidden, need_x + 2 * need_w, piece_rows)
         with torch.cuda.device(x.device):
             workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
             B.sidco_linear_cross_entropy(x, ldx, w, ldw, labels, rows, vocab, hidden, dc, loss, dx, hidden, dw, hidden,
                                          workspace, need, row_weights=row_weights, scale=scale, piece_rows=piece_rows)
-        ctx.grads = (dx, dw, dc)
+        ctx.grads, ctx.types = (dx, dw, dc), (x.dtype, weight.dtype, torch.float32)
         return loss
 
     @staticmethod
@@ -232,12 +234,20 @@ class _LinearCrossEntropy(torch.autograd.Function):
             raise RuntimeError("the gradients of linear_cross_entropy are handed out once; call it again")
         grads, ctx.grads = ctx.grads, None
         dloss = dloss.float()
-        for g in grads:
-            if g is not None:
-                with torch.cuda.device(g.device):
-                    B.sidco_scale_gradient(g, g.numel(), dloss)
-        dx, dw, dc = grads
+        with torch.cuda.device(dloss.device):
+            dx, dw, dc = (_scaled(g, t, dloss) for g, t in zip(grads, ctx.types))
         return dx, dw, None, dc, None, None, None
+
+
+def _scaled(g: Optional[torch.Tensor], dtype: torch.dtype, factor: torch.Tensor) -> Optional[torch.Tensor]:
+    """g times a number on the device: in place, or from fp32 to another type with one rounding."""
+    if g is None or g.dtype == dtype:
+        if g is not None:
+            B.sidco_scale_gradient(g, g.numel(), factor)
+        return g
+    out = torch.empty_like(g, dtype=dtype)
+    B.sidco_round_gradient(g, g.numel(), factor, out)
+    return out
 
 
 def linear_cross_entropy(x: torch.Tensor, weight: torch.Tensor, labels: torch.Tensor,
@@ -245,7 +255,7 @@ def linear_cross_entropy(x: torch.Tensor, weight: torch.Tensor, labels: torch.Te
     """Softmax cross entropy of scale * x weight^T against `labels`, without the logits ever being stored.
 
     x [..., hidden] in bf16 or fp16, weight [vocab, hidden] in the same type or fp32 (a master copy: rounded for the
-    products, its gradient in fp32), labels [...] int32 or int64.  Rows with a negative label do not count.  The result is
+    products, its gradient in fp32; gradients in fp16 are rounded after the factor in front of the loss), labels [...] int32 or int64.  Rows with a negative label do not count.  The result is
     the mean over the others, or with row_weights [...] (fp32) the sum of the rows' losses times these, which may require a
     gradient themselves.  Under
     ``torch.no_grad()`` the loss alone is computed, with a third of the operations."""

@@ -48,3 +48,71 @@ def test_gradient_of_the_row_weights(only):
     off = 3 * (2 * (24 / 16 + 3) * 2.0 ** -22 * size + 2.0 ** -18) + 2.0 ** -24 * want.max()
     assert (c.grad.double() - want).abs().max() <= off and bool((c.grad[y < 0] == 0).all())
     assert only or (x.grad is not None and w.grad is not None)
+
+
+@pytest.mark.parametrize("master", [False, True])
+def test_fp16_gradients_keep_their_bits_under_a_scaled_loss(master):
+    """The mean over 4096 rows: a gradient of x is near 2^-12 times 0.02, at the end of fp16's range, and those of the words that
+    are no labels far below it.  The factor brings them back: off by what the roundings of the gradient of the logits and of the
+    result leave, 2^-11 (1 + 2^-3) of the norm (as in the tests of the call), and hardly an element is zero."""
+    torch, T = T_()
+    g = torch.Generator(device="cuda").manual_seed(3)
+    rows, vocab, hidden, factor = 4096, 6000, 200, 2.0 ** 14
+    x = torch.randn(rows, hidden, generator=g, device="cuda").half().requires_grad_()
+    w = torch.randn(vocab, hidden, generator=g, device="cuda") * 0.02
+    w = (w if master else w.half()).requires_grad_()
+    y = torch.randint(0, vocab, (rows,), generator=g, device="cuda")
+    (T.linear_cross_entropy(x, w, y) * factor).backward()
+    hx, hw = x.detach().double(), w.detach().half().double()
+    d = torch.softmax(hx @ hw.T, 1)
+    d[torch.arange(rows, device="cuda"), y] -= 1
+    d *= factor / rows
+    for got, want, t in ((x.grad, d @ hw, x), (w.grad, d.T @ hx, w)):
+        assert got.dtype == t.dtype
+        assert (got.double() - want).norm() <= 2.0 ** -11 * (1 + 2.0 ** -3) * want.norm()
+        assert (got == 0).double().mean() <= 1e-3
+
+
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16", "float32"])
+@pytest.mark.parametrize("shift", [0, 1])
+def test_round_gradient(dtype, shift):
+    torch, T = T_()
+    dtype = getattr(torch, dtype)
+    x = torch.randn(100010, device="cuda") * 1e-6
+    f = torch.tensor(65536.0 * 3, device="cuda")
+    for n in (1, 3, 4, 1023, 100003):
+        out = torch.full((100010,), 7.0, device="cuda", dtype=dtype)
+        T.B.sidco_round_gradient(x[shift:], n, f, out[shift:])
+        want = torch.full_like(out, 7.0)
+        want[shift:n + shift] = (x[shift:n + shift] * f).to(dtype)
+        assert torch.equal(out, want)
+    out = torch.full((100010,), 7.0, device="cuda", dtype=dtype)
+    T.B.sidco_round_gradient(x, 100003, f, out[shift:])
+    assert torch.equal(out[shift:100003 + shift], (x[:100003] * f).to(dtype))
+
+
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
+@pytest.mark.parametrize("lddx,shift", [(130, 0), (131, 1), (132, 0), (136, 0)])
+def test_dx_in_32_bits(dtype, lddx, shift):
+    """Rounded, dX in 32 bits is dX in 16 bits; rows without a label are zero, what lies between the rows is left."""
+    torch, T = T_()
+    B, rows, vocab, hidden = T.B, 700, 1500, 130
+    dtype = getattr(torch, dtype)
+    g = torch.Generator(device="cuda").manual_seed(4)
+    x = torch.randn(rows, hidden, generator=g, device="cuda").to(dtype)
+    w = (torch.randn(vocab, hidden, generator=g, device="cuda") / 4).to(dtype)
+    y = torch.randint(-300, vocab, (rows,), generator=g, device="cuda")
+    for grads in (1, 3):
+        need = B.sidco_linear_cross_entropy_workspace_bytes(x, w, hidden, rows, vocab, hidden, grads)
+        ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+        got = []
+        for t in (dtype, torch.float32):
+            store = torch.full((rows * lddx + 8,), float("nan"), dtype=t, device="cuda")
+            dw = torch.empty(vocab, hidden, dtype=dtype, device="cuda")
+            B.sidco_linear_cross_entropy(x, hidden, w, hidden, y, rows, vocab, hidden, None, None, store[shift:], lddx,
+                                         dw if grads & 2 else None, hidden, ws, need)
+            inside = store[shift:shift + rows * lddx].view(rows, lddx)
+            got.append(inside[:, :hidden].clone())
+            inside[:, :hidden] = float("nan")
+            assert bool(torch.isnan(store).all())
+        assert torch.equal(got[1].to(dtype), got[0]) and bool((got[1][y < 0] == 0).all()) and bool(got[1].any())
