@@ -82,7 +82,7 @@ constexpr int kAhead = 4;
 
 template <typename TI, typename TO, int N, bool kVector, bool kDrop>
 __global__ void __launch_bounds__(kThreads, 4)
-    lookup_kernel(const TI* __restrict__ table, int64_t vocab, int cols, int64_t ld, const void* __restrict__ tokens, int wide,
+    lookup_kernel(const TI* table, int64_t vocab, int cols, int64_t ld, const void* tokens, int wide,
                   int64_t n, float scale, TO* __restrict__ out, int64_t ldo, const Dropout d, int lanes, int spans, int32_t* status) {
     sidco_tc::wait_prerequisites();
     sidco_tc::launch_dependents();
@@ -143,7 +143,7 @@ __global__ void __launch_bounds__(kThreads, 4)
 // written at once; a group belongs to the row in which it begins, and fetches the elements of the next one by one.
 template <typename TI, typename TO, bool kDrop>
 __global__ void __launch_bounds__(kThreads, 4)
-    flat_lookup_kernel(const TI* __restrict__ table, int64_t vocab, int cols, int64_t ld, const void* __restrict__ tokens, int wide,
+    flat_lookup_kernel(const TI* table, int64_t vocab, int cols, int64_t ld, const void* tokens, int wide,
                        int64_t n, float scale, TO* __restrict__ out, const Dropout d, int lanes, int each, int spans, int32_t* status) {
     constexpr int kGroups = 2;                                        // in flight
     sidco_tc::wait_prerequisites();
@@ -529,7 +529,7 @@ __device__ __forceinline__ void add_up(const TI* dy, const Sums& s, const Dropou
 
 template <typename TI, typename TO, bool kVector, bool kDrop>
 __global__ void __launch_bounds__(kThreads, kDrop ? 4 : 2)
-    sum_kernel(const TI* __restrict__ dy, TO* __restrict__ out, const Sums s, const Dropout d, uint32_t chunks, int slabs, int out_vector) {
+    sum_kernel(const TI* dy, TO* __restrict__ out, const Sums s, const Dropout d, uint32_t chunks, int slabs, int out_vector) {
     sidco_tc::wait_prerequisites();
     sidco_tc::launch_dependents();
     const int lane = threadIdx.x & 31;
@@ -629,7 +629,7 @@ struct Few {
 
 template <typename TI, typename TO, bool kVector, bool kDrop>
 __global__ void __launch_bounds__(kFewThreads, 2)
-    few_kernel(const TI* __restrict__ dy, TO* out, const Few f, const Sums s, const Dropout d, int slabs, int out_vector) {
+    few_kernel(const TI* dy, TO* out, const Few f, const Sums s, const Dropout d, int slabs, int out_vector) {
     __shared__ uint32_t s_key[kFewMost], s_sorted[kFewMost];          // row within the range
     __shared__ uint16_t s_from[kFewMost], s_at[kFewMost];
     __shared__ uint32_t s_mark[kFewRange / 32];                       // rows that have tokens
