@@ -207,8 +207,8 @@ __global__ void __launch_bounds__(kQuantThreads) quantize_kernel(const QuantArgs
 constexpr int kDequantU = 2;
 
 template <typename T, int W>
-__global__ void __launch_bounds__(256) dequantize_kernel(const uint8_t* __restrict__ codes,
-                                                         const uint8_t* __restrict__ scales, int rows, int cols,
+__global__ void __launch_bounds__(256) dequantize_kernel(const uint8_t* codes,
+                                                         const uint8_t* scales, int rows, int cols,
                                                          int64_t pitch, int64_t ktiles, T* __restrict__ out, int64_t ld,
                                                          int octs, int log2_lanes, int parts) {
     begin();
@@ -242,7 +242,7 @@ __global__ void __launch_bounds__(256) dequantize_kernel(const uint8_t* __restri
 // ------------------------------------------------------------------------------------------------ flat vectors
 
 template <typename T, int W, int WR, int U>
-__global__ void __launch_bounds__(256) compress_kernel(const T* __restrict__ grad, float* __restrict__ residual,
+__global__ void __launch_bounds__(256) compress_kernel(const T* grad, float* __restrict__ residual,
                                                        int64_t d, uint8_t* __restrict__ codes,
                                                        uint8_t* __restrict__ scales) {
     begin();
@@ -280,7 +280,7 @@ __global__ void __launch_bounds__(256) compress_kernel(const T* __restrict__ gra
 // takes half a block (one 8-byte load of codes and one scale for sixteen values: the kernel is bound by its instructions,
 // eight values per scale took 49 us where sixteen take 38) and loads those of A workers before it uses any.
 template <int W, int A>
-__global__ void __launch_bounds__(256) mean_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
+__global__ void __launch_bounds__(256) mean_kernel(const uint8_t* codes, const uint8_t* scales,
                                                    int n_workers, int64_t d, float* __restrict__ out) {
     begin();
     const int64_t nb = blocks_of(d), h = (int64_t)blockIdx.x * 256 + threadIdx.x;

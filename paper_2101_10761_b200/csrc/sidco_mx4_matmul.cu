@@ -327,7 +327,7 @@ __device__ __forceinline__ float4 remote_load16(uint32_t addr) {
 template <typename T, int N>
 __global__ void __launch_bounds__(kSplitThreads, 2)
     split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-                 const uint8_t* __restrict__ a_scales, const uint8_t* __restrict__ b_scales, const Args A, int tiles_b,
+                 const uint8_t* a_scales, const uint8_t* b_scales, const Args A, int tiles_b,
                  int swapped, int vec) {
     constexpr int kStages = kSplitStages<N>, kStageBytes = kSplitStageBytes<N>;
     constexpr uint32_t kColumns = N == 128 ? 256 : 128;               // N of sums, 16 of scales per stage

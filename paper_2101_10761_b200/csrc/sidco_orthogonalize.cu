@@ -443,7 +443,7 @@ __global__ void __launch_bounds__(256, kMomentumCtas) momentum_kernel(const __gr
 // momentum pass could do that alone, which saves this launch, 2 us of a call, but takes 25 ms for 10000 x 1500.)
 template <typename T>
 __global__ void __launch_bounds__(256) again_kernel(const __grid_constant__ Table t, const T* __restrict__ grad,
-                                                    const float* __restrict__ momentum, float mu, int nesterov, int quads,
+                                                    const float* momentum, float mu, int nesterov, int quads,
                                                     int parts, Norms norms, uint8_t* __restrict__ ws) {
     __shared__ float s_u[kUnit][kUnit + 1];
     __shared__ int s_again[kMaxMats];

@@ -14,16 +14,22 @@ def kernels(name):
         yield m.group(1), m.group(2), text[m.end():m.end() + 4000].split("\n}\n")[0]
 
 
-@pytest.mark.parametrize("name", ["sidco_embedding.cu", "sidco_dropout.cu", "sidco_cross_entropy.cu"])
+# Inputs that no kernel of their call writes, read behind a kernel of the call that is not started early itself.
+UNCHANGED = {("momentum_kernel", "grad"), ("again_kernel", "grad")}
+
+
+@pytest.mark.parametrize("name", ["sidco_embedding.cu", "sidco_dropout.cu", "sidco_cross_entropy.cu", "sidco_mx4.cu",
+                                  "sidco_mx4_matmul.cu", "sidco_orthogonalize.cu"])
 def test_kernels_that_start_early_claim_no_input_as_unchanging(name):
     """They are resident while the kernel before them still writes what they are going to read: const __restrict__, which says
     that nothing changes it as long as they run, would allow reads ahead of the wait and past the coherent caches."""
     seen = 0
     for kernel, parameters, body in kernels(name):
-        if "wait_prerequisites()" not in body:
+        if not re.search(r"\b(wait_prerequisites|begin)\(\);", body):
             continue
         seen += 1
-        claimed = [p.strip() for p in parameters.split(",") if re.match(r"\s*const\b", p) and "__restrict__" in p]
+        claimed = [p.split()[-1] for p in parameters.split(",") if re.match(r"\s*const\b", p) and "__restrict__" in p]
+        claimed = [p for p in claimed if (kernel, p) not in UNCHANGED]
         assert not claimed, (kernel, claimed)
         assert "__ldg(" not in body, kernel
-    assert seen >= 3
+    assert seen >= 2
