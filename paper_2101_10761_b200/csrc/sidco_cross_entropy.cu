@@ -72,8 +72,11 @@ constexpr float kUp = 14.0f;
 // Sums in tensor memory are cut to fp32, not rounded, so that logits come out short by a part that grows with `hidden`: measured
 // 0.25 to 0.3 times 2^-24 for every 16 products, from 256 to 16384 products, whether they cancel or not.  The mean of it is put
 // back with the scale, at no cost: 4096 products 2.1e-5 off in the mean square -> 4.9e-6 (logits around 4), losses of 4096 x 32000 x 4096
-// 1.4e-6 -> 5.3e-7.  (Rows with a single product that is not zero are off by as much; the bound of the sum itself is ten times that.)
+// 1.4e-6 -> 5.3e-7.  That is the share of sums whose terms cancel; of such that only grow more is cut (1.6 times 2^-24 for every
+// 16 products), and of a single product nothing: what is put back is then the error, 4.1e-6 of the logit at hidden 4096.  It
+// goes no further than 16384 products, 1.65e-5 (at 2^20 it would be 1e-3 of a row whose products are mostly zero).
 constexpr double kCut = 0.27 * 0x1p-24 / 16;
+constexpr int64_t kCutMost = 16384;
 
 __device__ __forceinline__ int rows_of_piece(const Sizes& z, const Head* head) {
     return max(0, min(z.piece, head->counted - z.first));
@@ -1279,7 +1282,7 @@ template <typename T, typename TW, typename TX> static int run(const Call& c, co
                    !sidco_internal::byte_map(&map_d, c.ws + p.e, c.vocab * 2, p.piece, p.e_pitch * 2, 128, 64, true))))
         return SIDCO_E_UNSUPPORTED;
     float* share = reinterpret_cast<float*>(c.ws + p.share);
-    const float scale2 = (float)(c.scale * 1.4426950408889634 * (1 + kCut * c.hidden));
+    const float scale2 = (float)(c.scale * 1.4426950408889634 * (1 + kCut * std::min(c.hidden, kCutMost)));
     for (int64_t i = 0; i < p.pieces; ++i) {
         const Sizes z{(int)c.rows, (int)c.vocab, (int)c.hidden, (int)p.piece, (int)(i * p.piece)};
         const int64_t most = std::min(p.piece, c.rows - z.first);      // rows if all have labels
