@@ -1128,7 +1128,7 @@ static Plan plan_of(int64_t rows, int64_t vocab, int64_t hidden, int grads, bool
     p.e_pitch = up_to(vocab, 64);
     p.tiles_n = (vocab + kTile - 1) / kTile;
     if (piece_rows > 0) p.piece = up_to(piece_rows, kTile);
-    else p.piece = std::max<int64_t>(kTile, std::max<int64_t>((int64_t)1 << 29, vocab * p.pitch * 4) / (p.e_pitch * 2) / kTile * kTile);
+    else p.piece = std::max<int64_t>(kTile, std::max<int64_t>((int64_t)1 << 29, grads & 2 ? vocab * p.pitch * 4 : 0) / (p.e_pitch * 2) / kTile * kTile);
     if (!grads && piece_rows <= 0)                                     // (only the statistics: 16 bytes per tile and row)
         p.piece = std::max<int64_t>(kTile, ((int64_t)1 << 29) / (p.tiles_n * 16) / kTile * kTile);
     p.piece = std::min(p.piece, up_to(rows, kTile));

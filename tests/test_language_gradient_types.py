@@ -34,6 +34,14 @@ def test_round_gradient_refuses(B):
     f(None, 0, None, None, out_type=2, stream=0)                  # nothing to do
 
 
+def test_room_for_the_gradient_of_the_logits(B):
+    """512 MB, or what dw takes in 32 bits where there is one: rows of a piece of 128000 words at hidden 4096."""
+    def need(grads, piece_rows):
+        return B.sidco_linear_cross_entropy_workspace_bytes(0, P, 4096, 16384, 128000, 4096, grads, piece_rows, x_type=1, w_type=1)
+    assert need(1, 0) == need(1, 2048) < need(1, 2049)
+    assert need(2, 0) == need(2, 8192) < need(2, 8193) and need(3, 0) == need(3, 8192)
+
+
 def test_cross_entropy_refuses_types_of_dx(B):
     f = B.sidco_linear_cross_entropy
     x, w, y, dx, dw, ws = (0x10000000 * (i + 1) for i in range(6))
