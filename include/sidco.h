@@ -423,8 +423,9 @@ int sidco_embedding_grad(const void* dy, int dy_type, int64_t ld_dy, const void*
                          size_t workspace_bytes, void* stream);
 
 /*
- * sidco_linear_cross_entropy - softmax cross entropy of an output projection over a vocabulary, with its gradients, without
- * storing the logits.
+ * sidco_linear_cross_entropy - softmax cross entropy of an output projection over a vocabulary, with its gradients.
+ * The logits are not stored.  Where gradients are wanted the workspace holds their exponentials, in 16 bits, for a piece of
+ * the rows at a time (piece_rows; by default up to 512 MB or what dw takes in 32 bits: all of 4096 rows of 128000 words).
  *
  *     s = scale * x w^T;   row_losses[i] = log(sum_v exp(s[i][v])) - s[i][labels[i]];   loss = sum_i c_i row_losses[i];
  *     dx = d loss / d x;   dw = d loss / d w (with add_dw: added to dw)
@@ -435,8 +436,9 @@ int sidco_embedding_grad(const void* dy, int dy_type, int64_t ld_dy, const void*
  * loss is 0.  Logits, sums and statistics are held in fp32.  The tensor cores cut the sums over hidden to fp32 for every 16
  * products: a logit is off by at most (hidden / 16 + 2) 2^-22 of the sum of its products' magnitudes, in the mean by 0.27
  * hidden / 16 2^-24 of itself where the products cancel, which is put back for up to 16384 products.  Logits of few products
- * that are not zero, whose sums are exact, are too large by that: 4.1e-6 at hidden 4096, 1.65e-5 from 16384 on.  The gradient of the logits is held in `type`, behind exponentials
- * in fp16: dx and dw carry an error of about 2^-9 (bf16) or 2^-11.5 (fp16) of their norm, also where dw is fp32.
+ * that are not zero, whose sums are exact, are too large by that: 4.1e-6 at hidden 4096, 1.65e-5 from 16384 on.  The gradient
+ * of the logits is held in `type`, behind exponentials in fp16: dx and dw carry an error of about 2^-9 (bf16) or 2^-11.5 (fp16)
+ * of their norm, also where they are fp32.
  *
  * x          device, type[rows][ldx], type SIDCO_T_BF16 or SIDCO_T_F16.     labels  device, label_type[rows].
  * w          device, w_type[vocab][ldw], w_type = type, or SIDCO_T_F32, which is rounded to `type`.  Rows that are not 16-byte

@@ -1,5 +1,6 @@
-// Softmax cross entropy of an output projection, s = scale * X W^T over a large vocabulary, with its gradients, without the
-// logits ever being stored: the products run on the tensor cores (bf16 or fp16 operands, fp32 sums in tensor memory).
+// Softmax cross entropy of an output projection, s = scale * X W^T over a large vocabulary, with its gradients.  The products
+// run on the tensor cores (bf16 or fp16 operands, fp32 sums in tensor memory).  The logits are never stored; with gradients
+// wanted their exponentials are, in 16 bits, for a piece of the rows at a time.
 //
 //   lse_i = log sum_v exp s_iv;   loss_i = lse_i - s_i,y_i;   total = sum_i c_i loss_i
 //   D_iv = c_i scale (exp(s_iv - lse_i) - [v = y_i]);   dX = D W;   dW (+)= D^T X

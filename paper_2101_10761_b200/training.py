@@ -252,13 +252,15 @@ def _scaled(g: Optional[torch.Tensor], dtype: torch.dtype, factor: torch.Tensor)
 
 def linear_cross_entropy(x: torch.Tensor, weight: torch.Tensor, labels: torch.Tensor,
                          row_weights: Optional[torch.Tensor] = None, scale: float = 1.0, piece_rows: int = 0) -> torch.Tensor:
-    """Softmax cross entropy of scale * x weight^T against `labels`, without the logits ever being stored.
+    """Softmax cross entropy of scale * x weight^T against `labels`.  The logits are not stored; where gradients are wanted,
+    their exponentials are held in 16 bits for `piece_rows` rows at a time, by default as many as fit into 512 MB or what the
+    gradient of weight takes in 32 bits, whichever is more.
 
     x [..., hidden] in bf16 or fp16, weight [vocab, hidden] in the same type or fp32 (a master copy: rounded for the
-    products, its gradient in fp32; gradients in fp16 are rounded after the factor in front of the loss), labels [...] int32 or int64.  Rows with a negative label do not count.  The result is
+    products, its gradient in fp32), labels [...] int32 or int64.  Rows with a negative label do not count.  The result is
     the mean over the others, or with row_weights [...] (fp32) the sum of the rows' losses times these, which may require a
-    gradient themselves.  Under
-    ``torch.no_grad()`` the loss alone is computed, with a third of the operations."""
+    gradient themselves.  Gradients in fp16 are rounded behind the factor in front of the loss.  Under ``torch.no_grad()`` the
+    loss alone is computed, with a third of the operations."""
     if x.dtype not in (torch.bfloat16, torch.float16):
         raise ValueError(f"x must be bf16 or fp16, got {x.dtype}")
     if weight.dim() != 2 or x.dim() < 1 or x.shape[-1] != weight.shape[1] or not weight.numel():
