@@ -118,19 +118,25 @@ def _check_random(p: float, step: Optional[torch.Tensor], device) -> None:
         raise ValueError(f"step must be one 64-bit integer on {device}")
 
 
+def _check_status(status: Optional[torch.Tensor], device) -> None:
+    if status is not None and (status.dtype != torch.int32 or status.numel() != 1 or status.device != device):
+        raise ValueError(f"status must be one int32 on {device}")
+
+
 _WORDS = 1 << 64
 
 
 class _Embedding(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, table, tokens, scale, p, seed, call, step, dtype):
+    def forward(ctx, table, tokens, scale, p, seed, call, step, dtype, status):
         vocab, cols = table.shape
         n = tokens.numel()
         rows, ld = _rows(table)
         flat = tokens.reshape(-1).contiguous()
         out = torch.empty(n, cols, dtype=dtype, device=table.device)
         with torch.cuda.device(table.device):
-            B.sidco_embedding(rows, vocab, cols, ld, flat, n, scale, out, cols, p=p, seed=seed, call=call, step=step)
+            B.sidco_embedding(rows, vocab, cols, ld, flat, n, scale, out, cols, p=p, seed=seed, call=call, step=step,
+                              status=status)
         ctx.save_for_backward(flat, step)
         ctx.args, ctx.sizes, ctx.type = (scale, p, seed, call), (n, vocab, cols), table.dtype
         return out
@@ -147,14 +153,16 @@ class _Embedding(torch.autograd.Function):
             workspace = torch.empty(need, dtype=torch.uint8, device=dy.device)
             B.sidco_embedding_grad(dy, ld, flat, n, vocab, cols, scale, dtable, cols, workspace, need, p=p, seed=seed,
                                    call=call, step=step)
-        return dtable, None, None, None, None, None, None, None
+        return dtable, None, None, None, None, None, None, None, None
 
 
 def embedding(tokens: torch.Tensor, table: torch.Tensor, scale: float = 1.0, p: float = 0.0, seed: int = 0, call: int = 0,
-              step: Optional[torch.Tensor] = None, dtype: Optional[torch.dtype] = None) -> torch.Tensor:
+              step: Optional[torch.Tensor] = None, dtype: Optional[torch.dtype] = None,
+              status: Optional[torch.Tensor] = None) -> torch.Tensor:
     """scale * dropout(table[tokens]), [..., cols] in `dtype` (that of the table by default).
 
-    A negative token is padding: its row is zero and it has no gradient, as a token beyond the table.  The mask is a
+    A negative token is padding: its row is zero and it has no gradient, as a token beyond the table.  The latter is
+    reported in `status`, one int32 on the device that is set to 0 or to ``binding.EMBEDDING_ST_TOKEN``.  The mask is a
     function of (seed, call + step, position), see :func:`dropout`.  The gradient is dense, in the table's type."""
     if table.dim() != 2:
         raise ValueError(f"the table must be a matrix, got {table.dim()} dimensions")
@@ -163,7 +171,8 @@ def embedding(tokens: torch.Tensor, table: torch.Tensor, scale: float = 1.0, p: 
     if tokens.device != table.device:
         raise ValueError(f"the tokens are on {tokens.device}, the table on {table.device}")
     _check_random(p, step, table.device)
-    y = _Embedding.apply(table, tokens, float(scale), float(p), seed % _WORDS, call % _WORDS, step, dtype or table.dtype)
+    _check_status(status, table.device)
+    y = _Embedding.apply(table, tokens, float(scale), float(p), seed % _WORDS, call % _WORDS, step, dtype or table.dtype, status)
     return y.reshape(*tokens.shape, table.shape[1])
 
 
@@ -209,7 +218,7 @@ class _LinearCrossEntropy(torch.autograd.Function):
     scaled loss: the gradients of a mean over thousands of rows lie below that type's range without it."""
 
     @staticmethod
-    def forward(ctx, x, weight, labels, row_weights, scale, piece_rows, wanted):
+    def forward(ctx, x, weight, labels, row_weights, scale, piece_rows, status, wanted):
         (rows, hidden), vocab = x.shape, weight.shape[0]
         need_x, need_w, _, need_c = (wanted and need for need in ctx.needs_input_grad[:4])
         x, ldx = _rows(x)
@@ -223,7 +232,8 @@ class _LinearCrossEntropy(torch.autograd.Function):
         with torch.cuda.device(x.device):
             workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
             B.sidco_linear_cross_entropy(x, ldx, w, ldw, labels, rows, vocab, hidden, dc, loss, dx, hidden, dw, hidden,
-                                         workspace, need, row_weights=row_weights, scale=scale, piece_rows=piece_rows)
+                                         workspace, need, row_weights=row_weights, scale=scale, piece_rows=piece_rows,
+                                         status=status)
         ctx.grads, ctx.types = (dx, dw, dc), (x.dtype, weight.dtype, torch.float32)
         return loss
 
@@ -236,7 +246,7 @@ class _LinearCrossEntropy(torch.autograd.Function):
         dloss = dloss.float()
         with torch.cuda.device(dloss.device):
             dx, dw, dc = (_scaled(g, t, dloss) for g, t in zip(grads, ctx.types))
-        return dx, dw, None, dc, None, None, None
+        return dx, dw, None, dc, None, None, None, None
 
 
 def _scaled(g: Optional[torch.Tensor], dtype: torch.dtype, factor: torch.Tensor) -> Optional[torch.Tensor]:
@@ -251,14 +261,16 @@ def _scaled(g: Optional[torch.Tensor], dtype: torch.dtype, factor: torch.Tensor)
 
 
 def linear_cross_entropy(x: torch.Tensor, weight: torch.Tensor, labels: torch.Tensor,
-                         row_weights: Optional[torch.Tensor] = None, scale: float = 1.0, piece_rows: int = 0) -> torch.Tensor:
+                         row_weights: Optional[torch.Tensor] = None, scale: float = 1.0, piece_rows: int = 0,
+                         status: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Softmax cross entropy of scale * x weight^T against `labels`.  The logits are not stored; where gradients are wanted,
     their exponentials are held in 16 bits for `piece_rows` rows at a time, by default as many as fit into 512 MB or what the
     gradient of weight takes in 32 bits, whichever is more.
 
     x [..., hidden] in bf16 or fp16, weight [vocab, hidden] in the same type or fp32 (a master copy: rounded for the
-    products, its gradient in fp32), labels [...] int32 or int64.  Rows with a negative label do not count.  The result is
-    the mean over the others, or with row_weights [...] (fp32) the sum of the rows' losses times these, which may require a
+    products, its gradient in fp32), labels [...] int32 or int64.  Rows with a negative label do not count, nor do those with
+    a label beyond the vocabulary, which is reported in `status`, one int32 on the device that is set to 0 or to
+    ``binding.CROSS_ENTROPY_ST_LABEL``.  The result is the mean over the others, or with row_weights [...] (fp32) the sum of the rows' losses times these, which may require a
     gradient themselves.  Gradients in fp16 are rounded behind the factor in front of the loss.  Under ``torch.no_grad()`` the
     loss alone is computed, with a third of the operations."""
     if x.dtype not in (torch.bfloat16, torch.float16):
@@ -275,11 +287,12 @@ def linear_cross_entropy(x: torch.Tensor, weight: torch.Tensor, labels: torch.Te
     for t in (weight, labels, row_weights):
         if t is not None and t.device != x.device:
             raise ValueError(f"all arguments must be on {x.device}, got one on {t.device}")
+    _check_status(status, x.device)
     rows = labels.numel()
     # (inside the function gradients look switched off always, and a parameter needs one even where they are)
     return _LinearCrossEntropy.apply(x.reshape(rows, x.shape[-1]), weight, labels.reshape(-1).contiguous(),
                                      None if row_weights is None else row_weights.reshape(-1).contiguous(), float(scale),
-                                     int(piece_rows), torch.is_grad_enabled())
+                                     int(piece_rows), status, torch.is_grad_enabled())
 
 
 class OrthogonalizedUpdate:

@@ -116,3 +116,20 @@ def test_dx_in_32_bits(dtype, lddx, shift):
             inside[:, :hidden] = float("nan")
             assert bool(torch.isnan(store).all())
         assert torch.equal(got[1].to(dtype), got[0]) and bool((got[1][y < 0] == 0).all()) and bool(got[1].any())
+
+
+def test_labels_and_tokens_outside_the_vocabulary_are_reported():
+    torch, T = T_()
+    x, w = torch.randn(4, 5, 16, device="cuda").bfloat16(), torch.randn(30, 16, device="cuda").bfloat16().requires_grad_()
+    y = torch.randint(-1, 30, (4, 5), device="cuda")
+    status = torch.full((1,), 7, dtype=torch.int32, device="cuda")
+    T.linear_cross_entropy(x, w, y, status=status).backward()
+    assert status.item() == 0
+    T.embedding(y, w, status=status.fill_(7))
+    assert status.item() == 0
+    y[1, 2] = 30
+    T.linear_cross_entropy(x, w, y, status=status)
+    assert status.item() == T.B.CROSS_ENTROPY_ST_LABEL
+    rows = T.embedding(y, w, status=status.zero_())
+    assert status.item() == T.B.EMBEDDING_ST_TOKEN and not bool(rows[1, 2].any())
+    rows.float().sum().backward()

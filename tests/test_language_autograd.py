@@ -67,3 +67,25 @@ def test_weights_of_the_rows_get_their_gradient(asked, monkeypatch):
     with torch.no_grad():
         T.linear_cross_entropy(x, w, y, c)
     assert rows_asked == [True, False, False]
+
+
+def test_status_is_handed_on_and_checked(asked, monkeypatch):
+    """Labels and tokens outside the vocabulary can be told apart from padding."""
+    seen = []
+    plain = T.B.sidco_linear_cross_entropy
+
+    def call(*a, **kw):
+        seen.append(kw["status"])
+        plain(*a, **kw)
+    monkeypatch.setattr(T.B, "sidco_linear_cross_entropy", call)
+    monkeypatch.setattr(T.B, "sidco_embedding", lambda *a, **kw: seen.append(kw["status"]))
+    x, w, y = arguments()
+    status = torch.zeros(1, dtype=torch.int32, device="meta")
+    T.linear_cross_entropy(x, w, y, status=status)
+    T.embedding(y, w, status=status)
+    assert len(seen) == 2 and all(s is status for s in seen)
+    for bad in (torch.zeros(2, dtype=torch.int32, device="meta"), torch.zeros(1, device="meta"), torch.zeros(1, dtype=torch.int32)):
+        with pytest.raises(ValueError, match="status must be"):
+            T.linear_cross_entropy(x, w, y, status=bad)
+        with pytest.raises(ValueError, match="status must be"):
+            T.embedding(y, w, status=bad)
