@@ -1259,8 +1259,15 @@ template <typename T, typename TW, typename TX> static int run(const Call& c, co
     int *map = reinterpret_cast<int*>(c.ws + p.map), *target = reinterpret_cast<int*>(c.ws + p.target);
     float* weight = reinterpret_cast<float*>(c.ws + p.weight);
     const void* w = copy_w ? c.ws + p.w : c.w;
-    const int64_t w_pitch = copy_w ? p.pitch : c.ldw;
+    const int64_t w_pitch = copy_w || c.vocab == 1 ? p.pitch : c.ldw;  // (a single row may have any distance)
     const bool grads = c.dx || c.dw;
+    // (before the first launch: what they refuse leaves the outputs as they were)
+    CUtensorMap map_x, map_w, map_e{}, map_d{};
+    if (!sidco_internal::byte_map(&map_x, c.ws + p.x, c.hidden * 2, up_to(c.rows, kStageK), p.pitch * 2, 128, 64, true) ||
+        !sidco_internal::byte_map(&map_w, w, c.hidden * 2, c.vocab, w_pitch * 2, 128, 64, true) ||
+        (grads && (!sidco_internal::out_map(&map_e, c.ws + p.e, c.type, p.e_pitch, p.piece, p.e_pitch, 64, 32) ||
+                   !sidco_internal::byte_map(&map_d, c.ws + p.e, c.vocab * 2, p.piece, p.e_pitch * 2, 128, 64, true))))
+        return SIDCO_E_UNSUPPORTED;
 
     Prepare a{};
     a.x = c.x, a.ldx = c.ldx, a.w = c.w, a.ldw = c.ldw, a.labels = c.labels, a.wide = c.label_type == SIDCO_T_I64;
@@ -1276,12 +1283,6 @@ template <typename T, typename TW, typename TX> static int run(const Call& c, co
     if (c.w_type == SIDCO_T_F32) SIDCO_CE_LAUNCH(prepare_kernel<T, float>, dim3(blocks), kPrepareThreads, 0, c.s, 1, a);
     else SIDCO_CE_LAUNCH(prepare_kernel<T, T>, dim3(blocks), kPrepareThreads, 0, c.s, 1, a);
 
-    CUtensorMap map_x, map_w, map_e{}, map_d{};
-    if (!sidco_internal::byte_map(&map_x, c.ws + p.x, c.hidden * 2, up_to(c.rows, kStageK), p.pitch * 2, 128, 64, true) ||
-        !sidco_internal::byte_map(&map_w, w, c.hidden * 2, c.vocab, w_pitch * 2, 128, 64, true) ||
-        (grads && (!sidco_internal::out_map(&map_e, c.ws + p.e, c.type, p.e_pitch, p.piece, p.e_pitch, 64, 32) ||
-                   !sidco_internal::byte_map(&map_d, c.ws + p.e, c.vocab * 2, p.piece, p.e_pitch * 2, 128, 64, true))))
-        return SIDCO_E_UNSUPPORTED;
     float* share = reinterpret_cast<float*>(c.ws + p.share);
     const float scale2 = (float)(c.scale * 1.4426950408889634 * (1 + kCut * std::min(c.hidden, kCutMost)));
     for (int64_t i = 0; i < p.pieces; ++i) {

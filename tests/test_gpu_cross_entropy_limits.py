@@ -53,3 +53,26 @@ def test_sums_far_longer_than_what_is_put_back(hidden):
     size = (x.double().abs() @ w.double().abs().T).amax(1)
     off = 2 * ((hidden / 16 + 2) * 2.0 ** -22 + 2.0 ** -22) * size + 2.0 ** -18
     assert ((each.double() - want).abs() <= off).all()
+
+
+@pytest.mark.parametrize("ldw", [64, 72, 1 << 39])
+def test_a_single_word_at_any_distance_of_rows(ldw):
+    """ldw of a matrix of one row means nothing.  Losses and gradients are zero up to what the statistics round: with s a logit in
+    powers of two, base = s - 14 and log2 of the sum plus s are off by half a step each, 2^-24 (|s| + 14), the difference from
+    the base by 14 x 2^-24, and exponential and logarithm by two steps of 2^-23 each: below 2^-23 (|s| + 14) + 2^-21 of one
+    in all.  That is the loss (ln 2 of it), and the logit's gradient times the row's weight."""
+    torch, T = T_()
+    B, rows, hidden = T.B, 70, 64
+    x, w = torch.randn(rows, hidden, device="cuda").bfloat16(), torch.randn(1, hidden, device="cuda").bfloat16()
+    y = torch.zeros(rows, dtype=torch.int32, device="cuda")
+    need = B.sidco_linear_cross_entropy_workspace_bytes(x, w, ldw, rows, 1, hidden)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    out = [torch.full(s, 7.0, device="cuda", dtype=t) for s, t in (((rows,), torch.float32), ((), torch.float32),
+                                                                    ((rows, hidden), x.dtype), ((1, hidden), x.dtype))]
+    B.sidco_linear_cross_entropy(x, hidden, w, ldw, y, rows, 1, hidden, out[0], out[1], out[2], hidden, out[3], hidden, ws, need)
+    s = (x.double() @ w[0].double()).abs() * 1.4427
+    off = 2.0 ** -23 * (s + 14) + 2.0 ** -21
+    each, loss, dx, dw = (t.double() for t in out)
+    assert (each.abs() <= off).all() and loss.abs() <= off.mean() * (1 + 2.0 ** -20)
+    assert (dx.abs() <= (off / rows)[:, None] * w.double().abs() * (1 + 2.0 ** -7)).all()
+    assert (dw[0].abs() <= (off / rows) @ x.double().abs() * (1 + 2.0 ** -6)).all()
