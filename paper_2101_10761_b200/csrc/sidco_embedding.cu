@@ -245,7 +245,7 @@ __device__ __forceinline__ uint32_t remote_load4(uint32_t addr) {
     return v;
 }
 
-// 0xff for 16-byte units of a row from its first aligned byte on, single bytes at its ends (rows may have any alignment)
+// Zeros: 16-byte units of a row from its first aligned byte on, single bytes at its ends (rows may have any alignment).
 __device__ void fill_rows(const Sort& s, int64_t worker, int64_t workers) {
     if (s.pitch_bytes == s.row_bytes) {                               // one row
         uint8_t* p = static_cast<uint8_t*>(s.fill);
