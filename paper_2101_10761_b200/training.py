@@ -270,9 +270,12 @@ def linear_cross_entropy(x: torch.Tensor, weight: torch.Tensor, labels: torch.Te
     x [..., hidden] in bf16 or fp16, weight [vocab, hidden] in the same type or fp32 (a master copy: rounded for the
     products, its gradient in fp32), labels [...] int32 or int64.  Rows with a negative label do not count, nor do those with
     a label beyond the vocabulary, which is reported in `status`, one int32 on the device that is set to 0 or to
-    ``binding.CROSS_ENTROPY_ST_LABEL``.  The result is the mean over the others, or with row_weights [...] (fp32) the sum of the rows' losses times these, which may require a
-    gradient themselves.  Gradients in fp16 are rounded behind the factor in front of the loss.  Under ``torch.no_grad()`` the
-    loss alone is computed, with a third of the operations."""
+    ``binding.CROSS_ENTROPY_ST_LABEL``.  The result is the mean over the others, or with row_weights [...] (fp32) the sum of the
+    rows' losses times these, which may require a gradient themselves.
+
+    The gradients are computed with the loss and handed out once: a second backward pass raises.  Those in fp16 are held in
+    fp32 until then and rounded behind the factor in front of the loss.  Under ``torch.no_grad()`` the loss alone is computed,
+    with a third of the operations."""
     if x.dtype not in (torch.bfloat16, torch.float16):
         raise ValueError(f"x must be bf16 or fp16, got {x.dtype}")
     if weight.dim() != 2 or x.dim() < 1 or x.shape[-1] != weight.shape[1] or not weight.numel():

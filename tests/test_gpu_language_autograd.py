@@ -133,3 +133,33 @@ def test_labels_and_tokens_outside_the_vocabulary_are_reported():
     rows = T.embedding(y, w, status=status.zero_())
     assert status.item() == T.B.EMBEDDING_ST_TOKEN and not bool(rows[1, 2].any())
     rows.float().sum().backward()
+
+
+def test_fp16_step_with_weighted_rows_in_a_graph():
+    """Captured and replayed with other inputs and another factor: the gradients of the eager step, bit for bit."""
+    torch, T = T_()
+    g = torch.Generator(device="cuda").manual_seed(6)
+    x = torch.randn(300, 72, generator=g, device="cuda").half().requires_grad_()
+    w = (torch.randn(500, 72, generator=g, device="cuda") / 4).half().requires_grad_()
+    c = torch.rand(300, generator=g, device="cuda").requires_grad_()
+    y = torch.randint(-20, 500, (300,), generator=g, device="cuda")
+    factor = torch.tensor(64.0, device="cuda")
+
+    def step():
+        return torch.autograd.grad(T.linear_cross_entropy(x, w, y, c) * factor, (x, w, c))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = step()
+    for k in range(3):
+        with torch.no_grad():
+            x.normal_(generator=g)
+            y.random_(-20, 500, generator=g)
+            factor.fill_(1.0 if k == 0 else 1000.0 * k)
+        graph.replay()
+        for got, want, t in zip(captured, step(), (x, w, c)):
+            assert got.dtype == t.dtype and got.shape == t.shape and torch.equal(got, want) and bool(torch.isfinite(got).all())
